@@ -247,7 +247,7 @@ def _plan(c, x):
             x["workspace"] = binding.make_norm_workspace(x["norm"])
     else:
         x["ffn"] = binding.make_ffn(c["tokens"], c["dim"], c["hidden"], activation=c["activation"], dtype=dt)
-        x["workspace"] = binding.make_ffn_workspace(x["ffn"])
+        x["workspace"] = binding.make_ffn_workspace(x["ffn"], backward=c["op"] == "ffn_bwd")
         if c["op"] == "ffn_fwd":
             x["out"] = {k: torch.empty((c["tokens"], c["hidden"]), dtype=dt, device="cuda")
                         for k in (("h", "gate", "up") if c["keep"] else ("h",))}
