@@ -8,6 +8,9 @@
  *   sparsp_demand_pack      receiver demand D[r,h,p], exchange volume V_r, row-major packing
  *   sparsp_sparse_attn_fwd  block-sparse softmax(QK^T/sqrt(d))V over M
  *
+ * What a layer computes token by token beside them -- sparsp_rotary_apply, sparsp_layer_norm_fwd / _bwd,
+ * sparsp_gated_ffn_fwd / _bwd -- stands at the end.
+ *
  * Conventions shared by every call
  *   - Return value: SPARSP_OK (0) or a negative SPARSP_ERR_* code.  Argument errors are detected
  *     on the host before anything is launched; sparsp_last_error() returns a text for the calling
@@ -370,6 +373,155 @@ SPARSP_API int sparsp_demand_plan_noalloc(const sparsp_shape* shape, const uint3
                                           const int32_t* rank_of_block, int32_t n_ranks, int32_t flags,
                                           uint32_t* union_mask, int32_t* cnt, int64_t* seg_offset,
                                           int64_t* seg_total, int64_t* volume_bytes, void* stream);
+
+/* Token-wise operators of a layer ------------------------------------------------------------------------------------
+ *
+ * What a layer computes beside its attention: rotary positions on Q and K, layer norm, the gated feed-forward half, each
+ * with its backward pass.  They follow the conventions above and need no block mask, so NB and head_dim are not limited
+ * to what the attention takes.  Element types are SPARSP_BF16, SPARSP_FP16 or SPARSP_FP32; all arithmetic is in fp32,
+ * rounded once where a result is stored.  A result has no order of additions that varies from call to call: the same
+ * inputs give the same bits.
+ */
+#define SPARSP_BF16 0
+#define SPARSP_FP16 1
+#define SPARSP_FP32 2
+
+/* pairing of channels in sparsp_rotary */
+#define SPARSP_PAIRS_INTERLEAVED 0 /* pair i = channels rot_begin + 2i, rot_begin + 2i + 1 */
+#define SPARSP_PAIRS_HALF 1        /* pair i = channels rot_begin + i, rot_begin + n_pairs + i */
+
+/* scaling of sparsp_rotary_frequencies */
+#define SPARSP_SCALING_NONE 0
+#define SPARSP_SCALING_LINEAR 1
+#define SPARSP_SCALING_NTK 2
+#define SPARSP_SCALING_YARN 3
+
+/* activation of sparsp_ffn */
+#define SPARSP_ACT_SILU 0      /* a(x) = x / (1 + e^-x) */
+#define SPARSP_ACT_GELU_TANH 1 /* a(x) = x/2 (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))) */
+#define SPARSP_ACT_GELU 2      /* a(x) = x/2 (1 + erf(x / sqrt 2)) */
+
+/* Rotary positions.  n_pairs = pairs_t + pairs_h + pairs_w channel pairs are rotated; the first pairs_t by the token's
+ * t coordinate, the next pairs_h by h, the last pairs_w by w (a text model uses t alone).  The other channels of a head
+ * keep their values.  len_*: coordinates 0 .. len-1 are in the table; ignored where that coordinate has no pairs. */
+typedef struct sparsp_rotary {
+  int32_t dtype;     /* of the tensors that are rotated */
+  int32_t pairing;   /* SPARSP_PAIRS_* */
+  int32_t rot_begin; /* first rotated channel */
+  int32_t pairs_t, pairs_h, pairs_w;
+  int32_t len_t, len_h, len_w;
+} sparsp_rotary;
+
+/* Frequencies (radians per position) of n_pairs pairs of one coordinate, for contexts `factor` times as long as the
+ * original_length that a model was trained with:
+ *   none    f_i = theta^(-i / n_pairs)                             (factor and original_length are ignored)
+ *   linear  f_i / factor
+ *   ntk     theta * factor^(n/(n-1)) in the place of theta, n = n_pairs > 1 (one pair is not scaled)
+ *   yarn    per pair between f_i and f_i / factor: share s_i = 1 - clamp((i - low) / (high - low), 0, 1) of the first,
+ *           where low = max(floor(at(beta_fast)), 0), high = min(ceil(at(beta_slow)), n - 1), high - low at least 0.001,
+ *           at(b) = n ln(original_length / (2 pi b)) / ln theta is the pair that turns b times over the original length
+ * inv_freq   out  HOST double [n_pairs]; may be NULL with n_pairs = 0
+ * amplitude  out  HOST double: yarn 0.1 ln(factor) + 1, otherwise 1; may be NULL
+ * theta > 1, factor >= 1, original_length >= 1 and, for yarn, beta_fast > beta_slow > 0. */
+SPARSP_API int sparsp_rotary_frequencies(int32_t n_pairs, double theta, int32_t scaling, double factor,
+                                         double original_length, double beta_fast, double beta_slow, double* inv_freq,
+                                         double* amplitude);
+
+/* Bytes of the table of a rotary description: (cos, sin) of every coordinate and pair, fp32
+ * [len_t][pairs_t][2], then [len_h][pairs_h][2], then [len_w][pairs_w][2]. */
+SPARSP_API int sparsp_rotary_table_bytes(const sparsp_rotary* rotary, int64_t* bytes);
+
+/* Fills the table: amplitude * (cos, sin)(coordinate * inv_freq), angles, cos and sin in fp64, rounded to fp32.
+ *   inv_freq  in   DEVICE double [n_pairs], in the order of the pairs
+ *   table     out  sparsp_rotary_table_bytes() bytes, 16-byte aligned */
+SPARSP_API int sparsp_rotary_table(const sparsp_rotary* rotary, const double* inv_freq, double amplitude, float* table,
+                                   void* stream);
+
+/* Rotates Q and, where it is given, K:
+ *   (y0, y1) = (x0 c - x1 s, x0 s + x1 c), (c, s) from the table;  inverse != 0: -s in the place of s, which takes a
+ *   rotation back and, applied to the gradient of the outputs, gives the gradient of the inputs.
+ * Coordinates of token n: with positions, positions[batch * positions_stride_batch + 3 n ..+2]; without, its place on the
+ * latent grid plus (origin_t, origin_h, origin_w), which then has to stay inside the table.  A text token without
+ * positions and a token whose first position is negative keep their values, as does one whose position is not in the
+ * table, which also sets the status word to SPARSP_ERR_INVALID_ARG.
+ *   shape       batch, heads, head_dim, tokens and strides of Q, K and both outputs (elements of rotary->dtype; `block` is
+ *               not looked at); head_dim a multiple of 8, at most 256; batch * tokens < 2^31
+ *   positions   in   DEVICE int32 [batch or 1][N][3]; may be NULL.  positions_stride_batch: elements from one batch item
+ *                    to the next, 0 = the same for all
+ *   Q, K        in   K may be NULL (a K of other heads than Q's takes a call of its own)
+ *   Q_out, K_out out  may be Q and K themselves
+ *   workspace   in   256 bytes (the status word); may be NULL without positions */
+SPARSP_API int sparsp_rotary_apply(const sparsp_shape* shape, const sparsp_rotary* rotary, const float* table,
+                                   const int32_t* positions, int64_t positions_stride_batch, int32_t origin_t,
+                                   int32_t origin_h, int32_t origin_w, const void* Q, const void* K, void* Q_out,
+                                   void* K_out, int32_t inverse, void* workspace, void* stream);
+
+/* Layer norm over rows of `dim` values.  Rows are in groups of rows_per_group (the last may be smaller) and each group has
+ * weights of its own: one group is the usual layer norm, a group per sequence the norm whose scale and shift a
+ * conditioning network gives (weight = 1 + scale). */
+typedef struct sparsp_norm {
+  int64_t rows;           /* 0 is allowed */
+  int64_t rows_per_group; /* 0 = all rows in one group */
+  int64_t stride_x;       /* elements from row to row of X and dX, >= dim */
+  int64_t stride_y;       /* of Y and dY */
+  int32_t dim;            /* 1 .. 16384 */
+  int32_t dtype;          /* of X, Y, dY, dX */
+  int32_t weight_dtype;   /* of weight, bias, dweight, dbias: dtype or SPARSP_FP32 */
+  float eps;              /* >= 0 */
+} sparsp_norm;
+
+/* y = (x - mean) * rstd * weight + bias,  mean = sum x / dim,  rstd = 1 / sqrt(sum (x - mean)^2 / dim + eps)
+ *   X            in   [rows][dim], row stride stride_x
+ *   weight, bias in   [groups][dim] contiguous; each may be NULL (1, 0)
+ *   Y            out  row stride stride_y; may be X itself when the strides are equal
+ *   mean, rstd   out  fp32 [rows], for the backward pass; both or neither may be NULL
+ * Data pointers are aligned to their element type; rows that are 16-byte aligned and a multiple of 16 bytes are faster. */
+SPARSP_API int sparsp_layer_norm_fwd(const sparsp_norm* norm, const void* X, const void* weight, const void* bias,
+                                     void* Y, float* mean, float* rstd, void* stream);
+
+/* Bytes of workspace that the backward pass needs (partial sums of the weights' gradients). */
+SPARSP_API int sparsp_layer_norm_workspace_bytes(const sparsp_norm* norm, int64_t* bytes);
+
+/* With xh = (x - mean) rstd and a = dy * weight:
+ *   dx = rstd (a - sum a / dim - xh sum(a xh) / dim),  dweight = sum over a group's rows of dy xh,  dbias = ... of dy
+ *   dX               out  may be dY itself when the strides are equal
+ *   dweight, dbias   out  [groups][dim]; each may be NULL (not wanted).  Without rows they are zero.
+ *   workspace        in   sparsp_layer_norm_workspace_bytes() bytes, 256-byte aligned; may be NULL when neither is wanted */
+SPARSP_API int sparsp_layer_norm_bwd(const sparsp_norm* norm, const void* dY, const void* X, const void* weight,
+                                     const float* mean, const float* rstd, void* dX, void* dweight, void* dbias,
+                                     void* workspace, void* stream);
+
+/* Gated feed-forward: H = a(X Wgate^T) * (X Wup^T).  Strides in elements from row to row. */
+typedef struct sparsp_ffn {
+  int64_t tokens;        /* 0 is allowed */
+  int64_t stride_x;      /* X, dX: >= dim */
+  int64_t stride_h;      /* H, gate, up, dH: >= hidden */
+  int64_t stride_w;      /* Wgate, Wup, dWgate, dWup: >= dim (2 dim where the two are interleaved row by row) */
+  int32_t dim, hidden;   /* multiples of 8 */
+  int32_t dtype;         /* SPARSP_BF16 or SPARSP_FP16, of every tensor */
+  int32_t activation;    /* SPARSP_ACT_* */
+} sparsp_ffn;
+
+/* Bytes of workspace that the forward call (backward = 0) or the backward call needs: dG and dU for the latter, and in
+ * either case at most 20 MB of partial sums. */
+SPARSP_API int sparsp_gated_ffn_workspace_bytes(const sparsp_ffn* ffn, int32_t backward, int64_t* bytes);
+
+/* Both projections, the activation and the product.  Sums in fp32; H is rounded once, from the fp32 projections.
+ *   X            in   [tokens][dim]
+ *   Wgate, Wup   in   [hidden][dim]
+ *   H            out  [tokens][hidden]
+ *   gate, up     out  [tokens][hidden], the projections rounded to dtype, for the backward pass; both or neither NULL
+ * Base pointers are 16-byte aligned and strides multiples of 8 elements. */
+SPARSP_API int sparsp_gated_ffn_fwd(const sparsp_ffn* ffn, const void* X, const void* Wgate, const void* Wup, void* H,
+                                    void* gate, void* up, void* workspace, void* stream);
+
+/* With dG = dH * up * a'(gate) and dU = dH * a(gate), both rounded to dtype (the tensor cores' operands):
+ *   dX = dG Wgate + dU Wup,  dWgate = dG^T X,  dWup = dU^T X, sums in fp32
+ *   dX             out  may be NULL (not wanted); Wgate and Wup may then be NULL too
+ *   dWgate, dWup   out  both or neither NULL; X may be NULL without them.  Without tokens they are zero. */
+SPARSP_API int sparsp_gated_ffn_bwd(const sparsp_ffn* ffn, const void* dH, const void* X, const void* Wgate,
+                                    const void* Wup, const void* gate, const void* up, void* dX, void* dWgate,
+                                    void* dWup, void* workspace, void* stream);
 
 /* Synchronises `stream` and returns the workspace's status word in *code (SPARSP_OK if no kernel
  * reported a problem since the last reset), then resets it. */

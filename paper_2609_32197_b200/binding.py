@@ -34,10 +34,19 @@ EXPORTS = [
     "sparsp_hop_chunk_mask", "sparsp_selftest_wait_timeout", "sparsp_attn_merge_rows", "sparsp_pack_segment",
     "sparsp_xchg_flag_bytes", "sparsp_xchg_export", "sparsp_xchg_connect", "sparsp_xchg_fence", "sparsp_xchg_acquire",
     "sparsp_xchg_publish", "sparsp_xchg_fetch", "sparsp_xchg_release", "sparsp_xchg_stats", "sparsp_xchg_destroy",
+    "sparsp_rotary_frequencies", "sparsp_rotary_table_bytes", "sparsp_rotary_table", "sparsp_rotary_apply",
+    "sparsp_layer_norm_fwd", "sparsp_layer_norm_workspace_bytes", "sparsp_layer_norm_bwd",
+    "sparsp_gated_ffn_workspace_bytes", "sparsp_gated_ffn_fwd", "sparsp_gated_ffn_bwd",
 ]
 SPARSP_XCHG_HOST_MEMORY = 1
+SPARSP_BF16, SPARSP_FP16, SPARSP_FP32 = 0, 1, 2
+DTYPES = {torch.bfloat16: SPARSP_BF16, torch.float16: SPARSP_FP16, torch.float32: SPARSP_FP32}
+PAIRINGS = {"interleaved": 0, "half": 1}
+SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
+ACTIVATIONS = {"silu": 0, "gelu_tanh": 1, "gelu": 2}
 
-# Argument types of the calls that a layer makes (s: shape, p: pointer, i / l: 32 / 64-bit integer, f: float), so that ctypes
+# Argument types of the calls that a layer makes (s: shape, r / n / m: description of rotary positions, a norm or a
+# feed-forward, p: pointer, i / l: 32 / 64-bit integer, f / d: 32 / 64-bit float), so that ctypes
 # converts plain values itself: a ctypes object per argument costs more than the call.
 _SIGNATURES = {
     "sparsp_block_mask": "sppippppppp",
@@ -51,6 +60,16 @@ _SIGNATURES = {
     "sparsp_attn_merge": "sppppppp",
     "sparsp_attn_merge_rows": "spppppppiiiip",
     "sparsp_pack_segment": "sppiiippppplpp",
+    "sparsp_rotary_frequencies": "ididdddpp",
+    "sparsp_rotary_table_bytes": "rp",
+    "sparsp_rotary_table": "rpdpp",
+    "sparsp_rotary_apply": "srppliiippppipp",
+    "sparsp_layer_norm_fwd": "nppppppp",
+    "sparsp_layer_norm_workspace_bytes": "np",
+    "sparsp_layer_norm_bwd": "npppppppppp",
+    "sparsp_gated_ffn_workspace_bytes": "mip",
+    "sparsp_gated_ffn_fwd": "mpppppppp",
+    "sparsp_gated_ffn_bwd": "mppppppppppp",
 }
 
 
@@ -66,6 +85,23 @@ class sparsp_shape(ctypes.Structure):
                 ("n_text", ctypes.c_int32), ("block", ctypes.c_int32),
                 ("stride_batch", ctypes.c_int64), ("stride_head", ctypes.c_int64),
                 ("stride_token", ctypes.c_int64)]
+
+
+class sparsp_rotary(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("dtype", "pairing", "rot_begin", "pairs_t", "pairs_h", "pairs_w", "len_t",
+                                              "len_h", "len_w")]
+
+
+class sparsp_norm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("rows_per_group", ctypes.c_int64), ("stride_x", ctypes.c_int64),
+                ("stride_y", ctypes.c_int64), ("dim", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("weight_dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class sparsp_ffn(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("stride_x", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("stride_w", ctypes.c_int64), ("dim", ctypes.c_int32), ("hidden", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32)]
 
 
 _lib = None
@@ -90,8 +126,9 @@ def lib() -> ctypes.CDLL:
         L.sparsp_resolve_topk.restype = ctypes.c_int32
         for name in EXPORTS:
             getattr(L, name)  # AttributeError if a declared symbol is not exported
-        kinds = {"s": ctypes.POINTER(sparsp_shape), "p": ctypes.c_void_p, "i": ctypes.c_int32, "l": ctypes.c_int64,
-                 "f": ctypes.c_float}
+        kinds = {"s": ctypes.POINTER(sparsp_shape), "r": ctypes.POINTER(sparsp_rotary),
+                 "n": ctypes.POINTER(sparsp_norm), "m": ctypes.POINTER(sparsp_ffn), "p": ctypes.c_void_p,
+                 "i": ctypes.c_int32, "l": ctypes.c_int64, "f": ctypes.c_float, "d": ctypes.c_double}
         for name, args in _SIGNATURES.items():
             getattr(L, name).argtypes = [kinds[a] for a in args]
         _lib = L
@@ -374,6 +411,121 @@ def sparsp_xchg_stats(x) -> dict:
 
 def sparsp_xchg_destroy(x):
     _check(lib().sparsp_xchg_destroy(x))
+
+
+# ---- token-wise operators of a layer ----
+def _dtype(dtype) -> int:
+    if dtype not in DTYPES:
+        raise ValueError(f"unsupported dtype {dtype}")
+    return DTYPES[dtype]
+
+
+def make_rotary(pairs, lengths, pairing: str = "interleaved", rot_begin: int = 0,
+                dtype=torch.bfloat16) -> sparsp_rotary:
+    """pairs, lengths: channel pairs and positions of the t, h and w coordinates."""
+    return sparsp_rotary(_dtype(dtype), PAIRINGS[pairing], rot_begin, *pairs, *lengths)
+
+
+def sparsp_rotary_frequencies(n_pairs: int, theta: float = 10000.0, scaling: str = "none", factor: float = 1.0,
+                              original_length: float = 4096.0, beta_fast: float = 32.0, beta_slow: float = 1.0):
+    """-> (float64 [n_pairs] on the host, amplitude)"""
+    out = torch.empty(max(n_pairs, 0), dtype=torch.float64)
+    amplitude = ctypes.c_double()
+    _check(lib().sparsp_rotary_frequencies(n_pairs, theta, SCALINGS[scaling], factor, original_length, beta_fast,
+                                           beta_slow, out.data_ptr() or None, ctypes.addressof(amplitude)))
+    return out, amplitude.value
+
+
+def sparsp_rotary_table_bytes(rotary: sparsp_rotary) -> int:
+    out = ctypes.c_int64()
+    _check(lib().sparsp_rotary_table_bytes(rotary, ctypes.addressof(out)))
+    return out.value
+
+
+def sparsp_rotary_table(rotary, inv_freq, amplitude, table):
+    _check(lib().sparsp_rotary_table(rotary, _data(inv_freq), amplitude, _data(table), _stream_handle()))
+
+
+def make_rotary_table(rotary: sparsp_rotary, inv_freq: torch.Tensor, amplitude: float = 1.0,
+                      device="cuda") -> torch.Tensor:
+    """Allocates and fills the table; inv_freq: frequencies of all pairs in their order (any device)."""
+    table = torch.empty(sparsp_rotary_table_bytes(rotary) // 4, dtype=torch.float32, device=device)
+    freq = inv_freq.to(device=device, dtype=torch.float64).contiguous()
+    if freq.numel() != rotary.pairs_t + rotary.pairs_h + rotary.pairs_w:
+        raise ValueError(f"{freq.numel()} frequencies for {rotary.pairs_t + rotary.pairs_h + rotary.pairs_w} pairs")
+    sparsp_rotary_table(rotary, freq, amplitude, table)
+    return table
+
+
+def make_status_workspace(device="cuda") -> torch.Tensor:
+    """A workspace of the status words alone."""
+    return torch.zeros(256, dtype=torch.uint8, device=device)
+
+
+def sparsp_rotary_apply(shape, rotary, table, positions, origin, Q, K, Q_out, K_out, inverse, workspace):
+    """positions: int32 [N][3] (for every batch item) or [B][N][3], or None; origin: first (t, h, w) without them."""
+    stride = 0 if positions is None or positions.dim() < 3 else positions.stride(0)
+    _check(lib().sparsp_rotary_apply(shape, rotary, _data(table), _data(positions), stride, *origin, _data(Q), _data(K),
+                                     _data(Q_out), _data(K_out), 1 if inverse else 0, _data(workspace),
+                                     _stream_handle()))
+
+
+def make_norm(rows: int, dim: int, rows_per_group: int = 0, eps: float = 1e-5, dtype=torch.bfloat16, weight_dtype=None,
+              stride_x: int = 0, stride_y: int = 0) -> sparsp_norm:
+    """Strides of 0: contiguous rows.  weight_dtype None: dtype."""
+    return sparsp_norm(rows, rows_per_group, stride_x or dim, stride_y or dim, dim, _dtype(dtype),
+                       _dtype(dtype if weight_dtype is None else weight_dtype), eps)
+
+
+def sparsp_layer_norm_fwd(norm, X, weight, bias, Y, mean, rstd):
+    _check(lib().sparsp_layer_norm_fwd(norm, _data(X), _data(weight), _data(bias), _data(Y), _data(mean), _data(rstd),
+                                       _stream_handle()))
+
+
+def sparsp_layer_norm_workspace_bytes(norm: sparsp_norm) -> int:
+    out = ctypes.c_int64()
+    _check(lib().sparsp_layer_norm_workspace_bytes(norm, ctypes.addressof(out)))
+    return out.value
+
+
+def make_norm_workspace(norm: sparsp_norm, device="cuda") -> torch.Tensor:
+    ws = torch.empty(sparsp_layer_norm_workspace_bytes(norm), dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+def sparsp_layer_norm_bwd(norm, dY, X, weight, mean, rstd, dX, dweight, dbias, workspace):
+    _check(lib().sparsp_layer_norm_bwd(norm, _data(dY), _data(X), _data(weight), _data(mean), _data(rstd), _data(dX),
+                                       _data(dweight), _data(dbias), _data(workspace), _stream_handle()))
+
+
+def make_ffn(tokens: int, dim: int, hidden: int, activation: str = "silu", dtype=torch.bfloat16, stride_x: int = 0,
+             stride_h: int = 0, stride_w: int = 0) -> sparsp_ffn:
+    """Strides of 0: contiguous rows."""
+    return sparsp_ffn(tokens, stride_x or dim, stride_h or hidden, stride_w or dim, dim, hidden, _dtype(dtype),
+                      ACTIVATIONS[activation])
+
+
+def sparsp_gated_ffn_workspace_bytes(ffn: sparsp_ffn, backward: bool) -> int:
+    out = ctypes.c_int64()
+    _check(lib().sparsp_gated_ffn_workspace_bytes(ffn, 1 if backward else 0, ctypes.addressof(out)))
+    return out.value
+
+
+def make_ffn_workspace(ffn: sparsp_ffn, backward: bool = True, device="cuda") -> torch.Tensor:
+    ws = torch.empty(sparsp_gated_ffn_workspace_bytes(ffn, backward), dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+def sparsp_gated_ffn_fwd(ffn, X, Wgate, Wup, H, gate, up, workspace):
+    _check(lib().sparsp_gated_ffn_fwd(ffn, _data(X), _data(Wgate), _data(Wup), _data(H), _data(gate), _data(up),
+                                      _data(workspace), _stream_handle()))
+
+
+def sparsp_gated_ffn_bwd(ffn, dH, X, Wgate, Wup, gate, up, dX, dWgate, dWup, workspace):
+    _check(lib().sparsp_gated_ffn_bwd(ffn, _data(dH), _data(X), _data(Wgate), _data(Wup), _data(gate), _data(up),
+                                      _data(dX), _data(dWgate), _data(dWup), _data(workspace), _stream_handle()))
 
 
 def sparsp_status(workspace) -> int:

@@ -1,0 +1,562 @@
+// Gated feed-forward: H = a(X Wg^T) * (X Wu^T) in one kernel, and its backward pass.
+//
+// All three products are one matrix kernel.  A pair of CTAs (a cluster of two, tcgen05 cta_group::2) makes a 256-row tile
+// of the result: each CTA loads 128 of its rows of A and half of its columns of B by TMA, the even CTA issues the MMAs for
+// both, and each finds its 128 rows, all columns, as fp32 in its own tensor memory.
+//   forward   A = X (K-major), B = half a tile of Wg's rows in one CTA and the same rows of Wu in the other: the tile's
+//             columns are gate and up of the same features, and the activation and the product happen between tensor
+//             memory and the store.
+//   dX        A = dG then dU (K-major), B = Wg then Wu as they lie (MN-major): the sum over both is one accumulation.
+//   dW        A = dG^T or dU^T (MN-major), B = X (MN-major); summed over tokens.
+// dG and dU, which the last two read, are made element by element before them.
+#include <algorithm>
+
+#include "layer.cuh"
+#include "sm100_ptx.cuh"
+
+namespace sparsp {
+
+enum GemmMode { kForward, kInput, kWeights };
+
+struct GemmParams {
+  void* out[2];           // kForward: H;  kInput: dX;  kWeights: dWg, dWu
+  void* keep[2];          // kForward: gate, up or NULL
+  float* partial;         // sums of a tile's splits, when there are several
+  int64_t ld_out;         // elements from row to row of out and keep
+  int32_t rows, cols;     // of the result (kForward: tokens, hidden; kInput: tokens, dim; kWeights: hidden, dim)
+  int32_t m_tiles, n_tiles, splits, units, band;
+  int32_t k_blocks;       // of 64, of one (A, B); kInput has two of them
+  int32_t activation;
+  uint32_t idesc;
+  int32_t* status;
+  long long wait_limit;
+};
+
+constexpr int kStageK = 64;           // K elements of a stage: one 128-byte swizzled row
+constexpr int kEpilogueWarps = 8;     // two for each quarter of the lanes
+constexpr int kGemmThreads = 32 * (kEpilogueWarps + 2);
+constexpr int kTileRows = 128;        // of one CTA
+
+// BN: columns of the accumulator, and of B over both CTAs.
+template <int BN>
+struct GemmCfg {
+  static constexpr int kA = kTileRows * 128, kB = BN / 2 * 128;  // bytes a stage of one CTA
+  static constexpr int kStage = kA + kB;
+  static constexpr int kStages = 196608 / kStage > 8 ? 8 : 196608 / kStage;
+  static constexpr int kOffBars = kStages * kStage;
+  static constexpr int kBars = 2 * kStages + 4;
+  static constexpr int kBytes = kOffBars + kBars * 8 + 16;
+  static constexpr int kDynamic = kBytes + 1024;  // the tiles are aligned to 1024 bytes
+};
+
+__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.0f, 1.0f + __expf(-x)); }
+constexpr float kTanhA = 2.0f * 0.7978845608028654f, kTanhB = 0.044715f;  // (1 + tanh(u)) / 2 = sigmoid(2u)
+
+__device__ __forceinline__ float activate(int kind, float x) {
+  if (kind == SPARSP_ACT_SILU) return x * sigmoid(x);
+  if (kind == SPARSP_ACT_GELU_TANH) return x * sigmoid(kTanhA * (x + kTanhB * x * x * x));
+  return x * 0.5f * (1.0f + erff(x * 0.70710678118654752f));
+}
+// a(x) and a'(x)
+__device__ __forceinline__ void activate_both(int kind, float x, float& a, float& slope) {
+  if (kind == SPARSP_ACT_SILU) {
+    const float s = sigmoid(x);
+    a = x * s;
+    slope = s * (1.0f + x * (1.0f - s));
+  } else if (kind == SPARSP_ACT_GELU_TANH) {
+    const float s = sigmoid(kTanhA * (x + kTanhB * x * x * x));
+    a = x * s;
+    const float t = s * (1.0f - s);
+    slope = t == 0.0f ? s : s + x * t * kTanhA * (1.0f + 3.0f * kTanhB * x * x);  // far out x * x may be infinite
+  } else {
+    const float c = 0.5f * (1.0f + erff(x * 0.70710678118654752f));
+    a = x * c;
+    slope = c + x * 0.3989422804014327f * __expf(-0.5f * x * x);
+  }
+}
+
+// Tiles go in bands of `band` row tiles, column by column inside a band, so that the tiles at work at one time share
+// both their rows of A and their columns of B in L2.
+__device__ __forceinline__ void tile_at(const GemmParams& p, int tile, int& m, int& n) {
+  const int per_band = p.band * p.n_tiles;
+  const int b = tile / per_band, in = tile - b * per_band;
+  const int height = min(p.band, p.m_tiles - b * p.band);
+  n = in / height;
+  m = b * p.band + in - n * height;
+}
+
+template <typename T, int kMode, int BN>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1,
+                const __grid_constant__ CUtensorMap b0, const __grid_constant__ CUtensorMap b1, const GemmParams p) {
+  using namespace ptx;
+  using C = GemmCfg<BN>;
+  extern __shared__ uint8_t dynamic[];
+  uint8_t* smem = dynamic + ((1024 - (smem_u32(dynamic) & 1023)) & 1023);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::kOffBars);  // of the even CTA: both CTAs' tiles have arrived
+  uint64_t* empty = full + C::kStages;                               // the stage has been multiplied
+  uint64_t* acc_full = empty + C::kStages;                           // [2]
+  uint64_t* acc_empty = acc_full + 2;                                // [2] of the even CTA: both have read theirs
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) {
+      mbar_init(full + s, 1);
+      mbar_init(empty + s, 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(acc_full + a, 1);
+      mbar_init(acc_empty + a, 2 * kEpilogueWarps);
+    }
+    *s_abort = 0;
+    mbar_init_fence();
+  }
+  if (warp == kEpilogueWarps + 1) {
+    tmem_alloc_pair(tmem_slot, 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  wait_previous_grids();
+
+  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+  const int all_blocks = p.k_blocks * (kMode == kInput ? 2 : 1);
+  constexpr bool kAMn = kMode == kWeights, kBMn = kMode != kForward;
+
+  if (warp == kEpilogueWarps) {
+    // ---- loads ----
+    if (elect_one()) {
+      uint32_t full_of_even[C::kStages];
+#pragma unroll
+      for (int s = 0; s < C::kStages; ++s) full_of_even[s] = cluster_addr(full + s, 0);
+      int s = 0;
+      uint32_t round = 0;
+      for (int unit = pair; unit < p.units && !*s_abort; unit += pairs) {
+        const int tile = unit / p.splits, split = unit - tile * p.splits;
+        int m, n;
+        tile_at(p, tile, m, n);
+        const int k0 = (int)((int64_t)all_blocks * split / p.splits);
+        const int k1 = (int)((int64_t)all_blocks * (split + 1) / p.splits);
+        const int half_m = p.m_tiles / 2;  // kWeights: the tiles of dWg, then those of dWu
+        const CUtensorMap* ta = &a0;
+        int row = (m * 2 + (int)rank) * kTileRows;
+        if (kMode == kWeights && m >= half_m) {
+          ta = &a1;
+          row -= half_m * 2 * kTileRows;
+        }
+        for (int k = k0; k < k1; ++k) {
+          mbar_wait_bounded_inline(empty + s, round ^ 1u, s_abort, 1, p.wait_limit);
+          if (*s_abort) break;
+          if (rank == 0) mbar_expect_tx(full + s, 2 * C::kStage);
+          uint8_t* A = smem + s * C::kStage;
+          uint8_t* B = A + C::kA;
+          uint32_t bar = 0;
+#pragma unroll
+          for (int q = 0; q < C::kStages; ++q)
+            if (q == s) bar = full_of_even[q];
+          const bool second = kMode == kInput && k >= p.k_blocks;
+          const int kk = (second ? k - p.k_blocks : k) * kStageK;
+          if constexpr (kAMn) {
+            tma_load_pair(A, ta, bar, row, kk);
+            tma_load_pair(A + 8192, ta, bar, row + 64, kk);
+          } else {
+            tma_load_pair(A, second ? &a1 : &a0, bar, kk, row);
+          }
+          if constexpr (!kBMn) {
+            tma_load_pair(B, rank == 0 ? &b0 : &b1, bar, kk, n * (BN / 2));
+          } else {
+            const CUtensorMap* tb = second ? &b1 : &b0;
+#pragma unroll
+            for (int c = 0; c < BN / 128; ++c)
+              tma_load_pair(B + c * 8192, tb, bar, n * BN + (int)rank * (BN / 2) + c * 64, kk);
+          }
+          if (++s == C::kStages) {
+            s = 0;
+            round ^= 1u;
+          }
+        }
+      }
+      // Copies still in flight after a wait that ran out are waited for, within the same limit: each stage's last phase.
+      if (*s_abort && rank == 0) {
+        const long long t0 = clock64();
+        for (int q = 0; q < C::kStages; ++q) {
+          const uint32_t phase = q < s ? round : round ^ 1u;
+          while (!mbar_try_wait(full + q, phase) && clock64() - t0 < p.wait_limit) {
+          }
+        }
+      }
+    }
+  } else if (warp == kEpilogueWarps + 1) {
+    // ---- products, for both CTAs ----
+    if (rank == 0 && elect_one()) {
+      const uint32_t base = smem_u32(smem);
+      const uint64_t da = make_smem_desc(base, kAMn ? 8192u : 16u, 1024u);
+      const uint64_t db = make_smem_desc(base + C::kA, kBMn ? 8192u : 16u, 1024u);
+      constexpr uint32_t kStepA = kAMn ? 2048 : 32, kStepB = kBMn ? 2048 : 32;  // 16 elements of K
+      int s = 0, acc = 0;
+      uint32_t round = 0, acc_round = 0;
+      for (int unit = pair; unit < p.units && !*s_abort; unit += pairs) {
+        const int split = unit % p.splits;
+        const int k0 = (int)((int64_t)all_blocks * split / p.splits);
+        const int k1 = (int)((int64_t)all_blocks * (split + 1) / p.splits);
+        mbar_wait_bounded_inline(acc_empty + acc, acc_round ^ 1u, s_abort, 2, p.wait_limit);
+        tc_fence_after();
+        for (int k = k0; k < k1; ++k) {
+          mbar_wait_bounded_inline(full + s, round, s_abort, 3, p.wait_limit);
+          tc_fence_after();
+          const uint64_t off = (uint64_t)((s * C::kStage) >> 4);
+#pragma unroll
+          for (int kk = 0; kk < kStageK / 16; ++kk)
+            mma_ss_pair(tmem + acc * BN, da + off + (kk * kStepA >> 4), db + off + (kk * kStepB >> 4), p.idesc,
+                        k > k0 || kk > 0);
+          mma_commit_pair(empty + s);
+          if (++s == C::kStages) {
+            s = 0;
+            round ^= 1u;
+          }
+        }
+        mma_commit_pair(acc_full + acc);
+        acc ^= 1;
+        if (acc == 0) acc_round ^= 1u;
+      }
+    }
+  } else {
+    // ---- results: warp w has the lanes of quarter w % 4, and one half of the columns ----
+    const int quarter = warp & 3, side = warp >> 2;
+    int acc = 0;
+    uint32_t acc_round = 0;
+    const uint32_t even0 = cluster_addr(acc_empty, 0), even1 = cluster_addr(acc_empty + 1, 0);
+    for (int unit = pair; unit < p.units; unit += pairs) {
+      int m, n;
+      tile_at(p, unit / p.splits, m, n);
+      mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 4, p.wait_limit);
+      if (*s_abort) break;
+      tc_fence_after();
+      const uint32_t from = tmem + acc * BN + ((uint32_t)(quarter * 32) << 16);
+      const int in_tile = (int)rank * kTileRows + quarter * 32 + lane;
+      if (p.splits > 1) {
+        // [unit][BN / 4][256 rows] of four columns: lanes are rows, so a warp writes 512 bytes in a piece
+        float4* to = reinterpret_cast<float4*>(p.partial) + (int64_t)unit * (BN / 4) * 256 + in_tile;
+#pragma unroll 1
+        for (int c = side * (BN / 2); c < (side + 1) * (BN / 2); c += 32) {
+          uint32_t r[32];
+          tmem_ld32(from + c, r);
+          tmem_ld_wait(r);
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            to[(c / 4 + e) * 256] = make_float4(__uint_as_float(r[4 * e]), __uint_as_float(r[4 * e + 1]),
+                                                __uint_as_float(r[4 * e + 2]), __uint_as_float(r[4 * e + 3]));
+        }
+      } else if constexpr (kMode == kForward) {
+        const int64_t row = (int64_t)m * 256 + in_tile;
+        const int64_t at = row * p.ld_out;
+#pragma unroll 1
+        for (int c = side * (BN / 4); c < (side + 1) * (BN / 4); c += 32) {
+          uint32_t g[32], u[32];
+          tmem_ld32(from + c, g);
+          tmem_ld32(from + BN / 2 + c, u);
+          tmem_ld_wait(g);
+          tmem_ld_wait(u);
+          const int col = n * (BN / 2) + c;
+          if (row < p.rows) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if (col + 8 * e >= p.cols) continue;
+              uint4 h, kg, ku;
+              uint32_t* hw = &h.x;
+              uint32_t* gw = &kg.x;
+              uint32_t* uw = &ku.x;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                const float ga = __uint_as_float(g[8 * e + 2 * i]), gb = __uint_as_float(g[8 * e + 2 * i + 1]);
+                const float ua = __uint_as_float(u[8 * e + 2 * i]), ub = __uint_as_float(u[8 * e + 2 * i + 1]);
+                hw[i] = pack2<T>(activate(p.activation, ga) * ua, activate(p.activation, gb) * ub);
+                gw[i] = pack2<T>(ga, gb);
+                uw[i] = pack2<T>(ua, ub);
+              }
+              *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out[0]) + at + col + 8 * e) = h;
+              if (p.keep[0] != nullptr) {
+                *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.keep[0]) + at + col + 8 * e) = kg;
+                *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.keep[1]) + at + col + 8 * e) = ku;
+              }
+            }
+          }
+        }
+      } else {
+        const int half_m = p.m_tiles / 2;
+        const bool second = kMode == kWeights && m >= half_m;
+        const int64_t row = (int64_t)(second ? m - half_m : m) * 256 + in_tile;
+        T* to = reinterpret_cast<T*>(second ? p.out[1] : p.out[0]) + row * p.ld_out;
+#pragma unroll 1
+        for (int c = side * (BN / 2); c < (side + 1) * (BN / 2); c += 32) {
+          uint32_t r[32];
+          tmem_ld32(from + c, r);
+          tmem_ld_wait(r);
+          const int col = n * BN + c;
+          if (row < p.rows) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              if (col + 8 * e >= p.cols) continue;
+              uint4 o;
+              uint32_t* w = &o.x;
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                w[i] = pack2<T>(__uint_as_float(r[8 * e + 2 * i]), __uint_as_float(r[8 * e + 2 * i + 1]));
+              *reinterpret_cast<uint4*>(to + col + 8 * e) = o;
+            }
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(acc == 0 ? even0 : even1);
+      acc ^= 1;
+      if (acc == 0) acc_round ^= 1u;
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();  // the other CTA's arrivals and products here have ended
+  if (warp == kEpilogueWarps + 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, 512);
+  }
+  if (threadIdx.x == 0) report_abort(s_abort, p.status);
+}
+
+// Adds the splits of every tile and finishes it as gemm_kernel would have.  A thread has one row and eight columns (for
+// the forward call of both projections).
+template <typename T, int kMode, int BN>
+__global__ void __launch_bounds__(256) gemm_join_kernel(const GemmParams p) {
+  const float* partial = p.partial;
+  enter_grid(partial);
+  constexpr int kCols = kMode == kForward ? BN / 2 : BN;  // result columns of a tile
+  const int tile = blockIdx.x / (kCols / 8), c = (blockIdx.x % (kCols / 8)) * 8;
+  int m, n;
+  tile_at(p, tile, m, n);
+  const float4* from = reinterpret_cast<const float4*>(partial) + (int64_t)tile * p.splits * (BN / 4) * 256 + threadIdx.x;
+  float v[8], u[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = u[i] = 0.0f;
+  for (int s = 0; s < p.splits; ++s, from += (BN / 4) * 256) {
+#pragma unroll
+    for (int q = 0; q < 2; ++q) {
+      const float4 x = from[(c / 4 + q) * 256];
+      v[4 * q] += x.x;
+      v[4 * q + 1] += x.y;
+      v[4 * q + 2] += x.z;
+      v[4 * q + 3] += x.w;
+      if (kMode == kForward) {
+        const float4 y = from[((c + BN / 2) / 4 + q) * 256];
+        u[4 * q] += y.x;
+        u[4 * q + 1] += y.y;
+        u[4 * q + 2] += y.z;
+        u[4 * q + 3] += y.w;
+      }
+    }
+  }
+  const int half_m = p.m_tiles / 2;
+  const bool second = kMode == kWeights && m >= half_m;
+  const int64_t row = (int64_t)(second ? m - half_m : m) * 256 + threadIdx.x;
+  const int col = n * kCols + c;
+  if (row >= p.rows || col >= p.cols) return;
+  const int64_t at = row * p.ld_out + col;
+  uint4 o, kg, ku;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float a = v[2 * i], b = v[2 * i + 1];
+    if (kMode == kForward) {
+      (&o.x)[i] = pack2<T>(activate(p.activation, a) * u[2 * i], activate(p.activation, b) * u[2 * i + 1]);
+      (&kg.x)[i] = pack2<T>(a, b);
+      (&ku.x)[i] = pack2<T>(u[2 * i], u[2 * i + 1]);
+    } else {
+      (&o.x)[i] = pack2<T>(a, b);
+    }
+  }
+  *reinterpret_cast<uint4*>(reinterpret_cast<T*>(second ? p.out[1] : p.out[0]) + at) = o;
+  if (kMode == kForward && p.keep[0] != nullptr) {
+    *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.keep[0]) + at) = kg;
+    *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.keep[1]) + at) = ku;
+  }
+}
+
+// dG = dH * up * a'(gate), dU = dH * a(gate), eight elements a thread.
+template <typename T>
+__global__ void __launch_bounds__(256) gate_grad_kernel(const T* dh, const T* gate, const T* up, T* dg, T* du,
+                                                        int64_t ld, int hidden, int64_t total, int activation) {
+  enter_grid(dh, gate, up);
+  const int per_row = hidden / 8;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= total) return;
+  const int64_t row = i / per_row;
+  const int col = (int)(i - row * per_row) * 8;
+  const int64_t at = row * ld + col;
+  const Vec<T, 8> h = load_once<T, 8>(dh + at), g = load_once<T, 8>(gate + at), u = load_once<T, 8>(up + at);
+  Vec<T, 8> og, ou;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    float a, slope;
+    activate_both(activation, g[e], a, slope);
+    og.set(e, h[e] * u[e] * slope);
+    ou.set(e, h[e] * a);
+  }
+  store_vec<T, 8>(dg + row * hidden + col, og);
+  store_vec<T, 8>(du + row * hidden + col, ou);
+}
+
+__global__ void __launch_bounds__(256) zero_rows_kernel(uint16_t* a, uint16_t* b, int rows, int cols, int64_t ld) {
+  enter_grid();
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)rows * cols; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / cols, at = r * ld + (i - r * cols);
+    a[at] = 0;
+    b[at] = 0;
+  }
+}
+
+// ---- host side ------------------------------------------------------------------------------------------------------
+
+constexpr int kPairs = kSms / 2;
+constexpr int64_t kPartialBytes = (int64_t)kPairs * 256 * 256 * 4;
+
+// [rows][cols] of 16-bit elements in boxes of 64 columns x box_rows rows, 128-byte swizzle
+static int make_map(CUtensorMap* out, int dtype, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
+  return make_matrix_tmap(out, base, dtype == SPARSP_BF16, rows, cols, ld, box_rows);
+}
+
+template <typename T, int kMode, int BN>
+static int launch_gemm_t(GemmParams p, const CUtensorMap (&map)[4], int dtype, char* ws, cudaStream_t st) {
+  using C = GemmCfg<BN>;
+  if ((int64_t)p.m_tiles * p.n_tiles > (1 << 30)) {
+    set_error("%d x %d tiles are too many", p.m_tiles, p.n_tiles);
+    return SPARSP_ERR_UNSUPPORTED;
+  }
+  const int tiles = p.m_tiles * p.n_tiles, blocks = p.k_blocks * (kMode == kInput ? 2 : 1);
+  // K is split where there are fewer tiles than pairs of SMs, into pieces of at least 8 blocks
+  p.splits = std::max(1, std::min(kPairs / std::max(tiles, 1), blocks / 8));
+  p.units = tiles * p.splits;
+  p.band = 8;
+  p.partial = reinterpret_cast<float*>(ws + kStatusWords * 4);
+  p.status = reinterpret_cast<int32_t*>(ws);
+  p.wait_limit = 200000000LL;  // about 0.1 s of SM clocks
+  constexpr int a_mn = kMode == kWeights, b_mn = kMode != kForward;
+  p.idesc = ptx::make_idesc_bf16(256, BN, a_mn, b_mn);
+  if (dtype == SPARSP_FP16) p.idesc &= ~((1u << 7) | (1u << 10));
+  auto kern = gemm_kernel<T, kMode, BN>;
+  SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, C::kDynamic));
+  const unsigned grid = 2u * (unsigned)std::min(p.units, kPairs);
+  SPARSP_CUDA_OK(launch_clusters(kern, dim3(grid), 2, kGemmThreads, C::kDynamic, st, map[0], map[1], map[2], map[3], p));
+  if (p.splits > 1) {
+    constexpr int kCols = kMode == kForward ? BN / 2 : BN;
+    SPARSP_CUDA_OK(launch_kernel(gemm_join_kernel<T, kMode, BN>, dim3((unsigned)(tiles * (kCols / 8))), 256, 0, st, p));
+  }
+  return SPARSP_OK;
+}
+
+template <int kMode, int BN>
+static int launch_gemm(const GemmParams& p, const CUtensorMap (&map)[4], int dtype, char* ws, cudaStream_t st) {
+  return dtype == SPARSP_BF16 ? launch_gemm_t<__nv_bfloat16, kMode, BN>(p, map, dtype, ws, st)
+                              : launch_gemm_t<__half, kMode, BN>(p, map, dtype, ws, st);
+}
+
+static int64_t hidden_bytes(const sparsp_ffn& f) { return align_up(f.tokens * f.hidden * 2, 256); }
+
+int64_t ffn_workspace_bytes(const sparsp_ffn& f, bool backward) {
+  return kStatusWords * 4 + kPartialBytes + (backward ? 2 * hidden_bytes(f) : 0);
+}
+
+static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+int launch_ffn_fwd(const sparsp_ffn& f, const void* X, const void* Wg, const void* Wu, void* H, void* gate, void* up,
+                   char* ws, cudaStream_t st) {
+  constexpr int BN = 256;
+  CUtensorMap map[4];
+  int rc;
+  if ((rc = make_map(map + 0, f.dtype, X, f.tokens, f.dim, f.stride_x, kTileRows)) != SPARSP_OK) return rc;
+  if ((rc = make_map(map + 2, f.dtype, Wg, f.hidden, f.dim, f.stride_w, BN / 2)) != SPARSP_OK) return rc;
+  if ((rc = make_map(map + 3, f.dtype, Wu, f.hidden, f.dim, f.stride_w, BN / 2)) != SPARSP_OK) return rc;
+  map[1] = map[0];
+  GemmParams p = {};
+  p.out[0] = H;
+  p.keep[0] = gate;
+  p.keep[1] = up;
+  p.ld_out = f.stride_h;
+  p.rows = (int32_t)f.tokens;
+  p.cols = f.hidden;
+  p.m_tiles = ceil_div(f.tokens, 256);
+  p.n_tiles = ceil_div(f.hidden, BN / 2);
+  p.k_blocks = ceil_div(f.dim, kStageK);
+  p.activation = f.activation;
+  return launch_gemm<kForward, BN>(p, map, f.dtype, ws, st);
+}
+
+int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const void* Wg, const void* Wu,
+                   const void* gate, const void* up, void* dX, void* dWg, void* dWu, char* ws, cudaStream_t st) {
+  constexpr int BN = 256;
+  if (f.tokens == 0) {
+    if (dWg != nullptr)
+      SPARSP_CUDA_OK(launch_kernel(zero_rows_kernel, dim3(2 * kSms), 256, 0, st, (uint16_t*)dWg, (uint16_t*)dWu,
+                                   f.hidden, f.dim, f.stride_w));
+    return SPARSP_OK;
+  }
+  if (dX == nullptr && dWg == nullptr) return SPARSP_OK;
+  char* dg = ws + kStatusWords * 4 + kPartialBytes;
+  char* du = dg + hidden_bytes(f);
+  const int64_t total = f.tokens * (f.hidden / 8);
+  if (total > 256LL * 0x7fffffff) {
+    set_error("tokens * hidden is too large");
+    return SPARSP_ERR_UNSUPPORTED;
+  }
+  const dim3 grid((unsigned)((total + 255) / 256));
+  if (f.dtype == SPARSP_BF16)
+    SPARSP_CUDA_OK(launch_kernel(gate_grad_kernel<__nv_bfloat16>, grid, 256, 0, st, (const __nv_bfloat16*)dH,
+                                 (const __nv_bfloat16*)gate, (const __nv_bfloat16*)up, (__nv_bfloat16*)dg,
+                                 (__nv_bfloat16*)du, f.stride_h, f.hidden, total, f.activation));
+  else
+    SPARSP_CUDA_OK(launch_kernel(gate_grad_kernel<__half>, grid, 256, 0, st, (const __half*)dH, (const __half*)gate,
+                                 (const __half*)up, (__half*)dg, (__half*)du, f.stride_h, f.hidden, total,
+                                 f.activation));
+  CUtensorMap map[4];
+  int rc;
+  if (dX != nullptr) {
+    if ((rc = make_map(map + 0, f.dtype, dg, f.tokens, f.hidden, f.hidden, kTileRows)) != SPARSP_OK) return rc;
+    if ((rc = make_map(map + 1, f.dtype, du, f.tokens, f.hidden, f.hidden, kTileRows)) != SPARSP_OK) return rc;
+    if ((rc = make_map(map + 2, f.dtype, Wg, f.hidden, f.dim, f.stride_w, kStageK)) != SPARSP_OK) return rc;
+    if ((rc = make_map(map + 3, f.dtype, Wu, f.hidden, f.dim, f.stride_w, kStageK)) != SPARSP_OK) return rc;
+    GemmParams p = {};
+    p.out[0] = dX;
+    p.ld_out = f.stride_x;
+    p.rows = (int32_t)f.tokens;
+    p.cols = f.dim;
+    p.m_tiles = ceil_div(f.tokens, 256);
+    p.n_tiles = ceil_div(f.dim, BN);
+    p.k_blocks = ceil_div(f.hidden, kStageK);
+    if ((rc = launch_gemm<kInput, BN>(p, map, f.dtype, ws, st)) != SPARSP_OK) return rc;
+  }
+  if (dWg != nullptr) {
+    if ((rc = make_map(map + 0, f.dtype, dg, f.tokens, f.hidden, f.hidden, kStageK)) != SPARSP_OK) return rc;
+    if ((rc = make_map(map + 1, f.dtype, du, f.tokens, f.hidden, f.hidden, kStageK)) != SPARSP_OK) return rc;
+    if ((rc = make_map(map + 2, f.dtype, X, f.tokens, f.dim, f.stride_x, kStageK)) != SPARSP_OK) return rc;
+    map[3] = map[2];
+    GemmParams p = {};
+    p.out[0] = dWg;
+    p.out[1] = dWu;
+    p.ld_out = f.stride_w;
+    p.rows = f.hidden;
+    p.cols = f.dim;
+    p.m_tiles = 2 * ceil_div(f.hidden, 256);
+    p.n_tiles = ceil_div(f.dim, BN);
+    p.k_blocks = ceil_div(f.tokens, kStageK);
+    if ((rc = launch_gemm<kWeights, BN>(p, map, f.dtype, ws, st)) != SPARSP_OK) return rc;
+  }
+  return SPARSP_OK;
+}
+
+}  // namespace sparsp

@@ -1,0 +1,124 @@
+// What the token-wise operators of a layer (rotary positions, layer norm, gated feed-forward) share: element types,
+// 16-byte vectors of them, and their launchers.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "common.cuh"
+
+namespace sparsp {
+
+constexpr int kMaxRotaryHeadDim = 256;
+constexpr int kMaxNormDim = 16384;
+// Work is shared out for the multiprocessors of a B200, whatever device a size of workspace is asked on: the shares also
+// decide in which order sums are made.
+constexpr int kSms = 148;
+
+inline int element_bytes(int dtype) { return dtype == SPARSP_FP32 ? 4 : 2; }
+
+#ifdef __CUDACC__
+template <typename T>
+__device__ __forceinline__ float to_float(T v);
+template <>
+__device__ __forceinline__ float to_float<float>(float v) {
+  return v;
+}
+template <>
+__device__ __forceinline__ float to_float<__half>(__half v) {
+  return __half2float(v);
+}
+template <>
+__device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 v) {
+  return __bfloat162float(v);
+}
+template <typename T>
+__device__ __forceinline__ T from_float(float v);
+template <>
+__device__ __forceinline__ float from_float<float>(float v) {
+  return v;
+}
+template <>
+__device__ __forceinline__ __half from_float<__half>(float v) {
+  return __float2half_rn(v);
+}
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) {
+  return __float2bfloat16_rn(v);
+}
+// two values as the type's 32-bit pair, the first in the low half
+template <typename T>
+__device__ __forceinline__ uint32_t pack2(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t pack2<__half>(float a, float b) {
+  const __half2 v = __floats2half2_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <>
+__device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
+  const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+  return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// E consecutive elements as they lie in memory: one 16-byte access, or single elements.
+template <typename T, int E>
+struct alignas(E * sizeof(T)) Vec {
+  T v[E];
+  __device__ __forceinline__ float operator[](int i) const { return to_float<T>(v[i]); }
+  __device__ __forceinline__ void set(int i, float x) { v[i] = from_float<T>(x); }
+};
+template <typename T, int E>
+__device__ __forceinline__ Vec<T, E> load_vec(const T* p) {
+  return *reinterpret_cast<const Vec<T, E>*>(p);
+}
+// ... of data that this kernel reads once: it need not stay in L1
+template <typename T, int E>
+__device__ __forceinline__ Vec<T, E> load_once(const T* p) {
+  if constexpr (E * sizeof(T) == 16) {
+    Vec<T, E> r;
+    *reinterpret_cast<uint4*>(&r) = __ldcs(reinterpret_cast<const uint4*>(p));
+    return r;
+  } else {
+    return load_vec<T, E>(p);
+  }
+}
+template <typename T, int E>
+__device__ __forceinline__ void store_vec(T* p, const Vec<T, E>& x) {
+  *reinterpret_cast<Vec<T, E>*>(p) = x;
+}
+
+// Runs the statements with T as the element type.
+#define SPARSP_WITH_TYPE(dtype, T, ...)      \
+  do {                                       \
+    if ((dtype) == SPARSP_BF16) {            \
+      using T = __nv_bfloat16;               \
+      __VA_ARGS__;                           \
+    } else if ((dtype) == SPARSP_FP16) {     \
+      using T = __half;                      \
+      __VA_ARGS__;                           \
+    } else {                                 \
+      using T = float;                       \
+      __VA_ARGS__;                           \
+    }                                        \
+  } while (0)
+#endif
+
+int launch_rotary_table(const sparsp_rotary& r, const double* inv_freq, double amplitude, float* table,
+                        cudaStream_t st);
+int launch_rotary(const sparsp_shape& s, const sparsp_rotary& r, const float* table, const int32_t* positions,
+                  int64_t positions_stride_batch, const int32_t* origin, const void* Q, const void* K, void* Qo,
+                  void* Ko, int inverse, int32_t* status, cudaStream_t st);
+
+int64_t norm_groups(const sparsp_norm& n);
+int64_t norm_workspace_bytes(const sparsp_norm& n);
+int launch_norm_fwd(const sparsp_norm& n, const void* X, const void* w, const void* b, void* Y, float* mean,
+                    float* rstd, cudaStream_t st);
+int launch_norm_bwd(const sparsp_norm& n, const void* dY, const void* X, const void* w, const float* mean,
+                    const float* rstd, void* dX, void* dw, void* db, char* ws, cudaStream_t st);
+
+int64_t ffn_workspace_bytes(const sparsp_ffn& f, bool backward);
+int launch_ffn_fwd(const sparsp_ffn& f, const void* X, const void* Wg, const void* Wu, void* H, void* gate, void* up,
+                   char* ws, cudaStream_t st);
+int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const void* Wg, const void* Wu,
+                   const void* gate, const void* up, void* dX, void* dWg, void* dWu, char* ws, cudaStream_t st);
+
+}  // namespace sparsp

@@ -1,0 +1,176 @@
+"""Host side of the token-wise operators: frequencies, sizes, and what the calls refuse before anything is launched."""
+import math
+
+import pytest
+
+from paper_2609_32197_b200 import binding
+from paper_2609_32197_b200.binding import SparspError
+
+INVALID, UNSUPPORTED = binding.SPARSP_ERR_INVALID_ARG, binding.SPARSP_ERR_UNSUPPORTED
+
+
+class At:
+    """A tensor of this address, for arguments that are refused before anybody reads them."""
+
+    def __init__(self, address=4096):
+        self.address = address
+
+    def data_ptr(self):
+        return self.address
+
+    def dim(self):
+        return 2
+
+
+@pytest.fixture(autouse=True)
+def no_stream(monkeypatch):
+    monkeypatch.setattr(binding, "_stream_handle", lambda: None)
+
+
+def refused(code, call, *args):
+    with pytest.raises(SparspError) as e:
+        call(*args)
+    assert e.value.code == code, str(e.value)
+
+
+@pytest.mark.parametrize("n", [1, 2, 21, 64])
+def test_frequencies(n):
+    plain, one = binding.sparsp_rotary_frequencies(n, 10000.0)
+    assert one == 1.0
+    for i in range(n):
+        assert math.isclose(plain[i], 10000.0 ** (-i / n), rel_tol=1e-14)
+    linear, one = binding.sparsp_rotary_frequencies(n, 10000.0, "linear", 4.0)
+    assert one == 1.0 and all(math.isclose(a, b / 4, rel_tol=1e-14) for a, b in zip(linear, plain))
+    ntk, one = binding.sparsp_rotary_frequencies(n, 10000.0, "ntk", 8.0)
+    assert one == 1.0 and ntk[0] == 1.0
+    if n > 1:  # the slowest pair is stretched by the factor, the fastest is not
+        assert math.isclose(ntk[n - 1], plain[n - 1] / 8, rel_tol=1e-12)
+    yarn, amplitude = binding.sparsp_rotary_frequencies(n, 10000.0, "yarn", 4.0, 4096.0)
+    assert math.isclose(amplitude, 0.1 * math.log(4.0) + 1.0)
+    for i in range(n):
+        assert plain[i] / 4 * (1 - 1e-14) <= yarn[i] <= plain[i] * (1 + 1e-14)
+    if n == 64:
+        turns = [4096 * float(f) / (2 * math.pi) for f in plain]
+        low = math.floor(64 * math.log(4096 / (2 * math.pi * 32)) / math.log(10000.0))
+        for i in range(n):
+            if i <= low:
+                assert turns[i] > 31 and math.isclose(yarn[i], plain[i], rel_tol=1e-14)
+            if turns[i] < 0.85:
+                assert math.isclose(yarn[i], plain[i] / 4, rel_tol=1e-14)
+
+
+def test_frequencies_refused():
+    f = binding.sparsp_rotary_frequencies
+    refused(INVALID, f, -1)
+    refused(INVALID, f, 4, 1.0)
+    refused(INVALID, f, 4, float("nan"))
+    refused(INVALID, f, 4, 10000.0, "linear", 0.5)
+    refused(INVALID, f, 4, 10000.0, "ntk", float("inf"))
+    refused(INVALID, f, 4, 10000.0, "yarn", 2.0, 0.0)
+    refused(INVALID, f, 4, 10000.0, "yarn", 2.0, 4096.0, 1.0, 1.0)
+    refused(INVALID, f, 4, 10000.0, "yarn", 2.0, 4096.0, 32.0, 0.0)
+    empty, _ = f(0)
+    assert empty.numel() == 0
+
+
+def test_table_bytes():
+    assert binding.sparsp_rotary_table_bytes(binding.make_rotary((3, 0, 5), (10, 99, 7))) == (30 + 35) * 8
+    # 2^31 entries and more are counted in 64 bits
+    assert binding.sparsp_rotary_table_bytes(binding.make_rotary((64, 0, 0), (2 ** 30, 0, 0))) == 64 * 2 ** 33
+
+
+def test_rotary_refused():
+    shape = binding.make_shape(4, 64, (3, 4, 5), 2, 64)
+    ok = binding.make_rotary((8, 8, 8), (3, 4, 5))
+    p, ws = At(), At()
+
+    def call(shape=shape, rotary=ok, table=p, positions=None, origin=(0, 0, 0), q=p, k=p, qo=p, ko=p, ws=ws):
+        binding.sparsp_rotary_apply(shape, rotary, table, positions, origin, q, k, qo, ko, False, ws)
+
+    changed = lambda s, **kw: type(s)(*[kw.get(n, getattr(s, n)) for n, _ in s._fields_])  # noqa: E731
+    refused(INVALID, lambda: call(rotary=changed(ok, dtype=7)))
+    refused(INVALID, lambda: call(rotary=changed(ok, pairing=2)))
+    refused(INVALID, lambda: call(rotary=changed(ok, pairs_t=-1)))
+    refused(INVALID, lambda: call(rotary=changed(ok, pairs_t=0, pairs_h=0, pairs_w=0)))
+    refused(INVALID, lambda: call(rotary=changed(ok, len_h=0)))
+    refused(UNSUPPORTED, lambda: call(rotary=changed(ok, rot_begin=-2)))
+    refused(UNSUPPORTED, lambda: call(rotary=changed(ok, pairs_t=2 ** 30)))
+    refused(INVALID, lambda: call(rotary=changed(ok, rot_begin=17)))  # 17 + 48 > 64
+    refused(INVALID, lambda: call(rotary=changed(ok, len_h=3)))  # the grid has 4
+    refused(INVALID, lambda: call(origin=(0, 0, 1)))
+    refused(INVALID, lambda: call(origin=(-1, 0, 0)))
+    refused(INVALID, lambda: call(origin=(2 ** 31 - 1, 0, 0)))
+    refused(INVALID, lambda: call(shape=changed(shape, grid_w=0)))
+    refused(UNSUPPORTED, lambda: call(shape=changed(shape, head_dim=60)))
+    refused(UNSUPPORTED, lambda: call(shape=changed(shape, head_dim=264, stride_token=264)))
+    refused(INVALID, lambda: call(shape=changed(shape, stride_token=60)))
+    refused(INVALID, lambda: call(shape=changed(shape, stride_head=60)))
+    refused(UNSUPPORTED, lambda: call(shape=changed(shape, grid_h=2 ** 20, grid_w=2 ** 20)))
+    refused(UNSUPPORTED, lambda: call(shape=changed(shape, batch=2 ** 27)))
+    refused(INVALID, lambda: call(q=None))
+    refused(INVALID, lambda: call(q=At(4104)))
+    refused(INVALID, lambda: call(ko=None))
+    refused(INVALID, lambda: call(table=None))
+    refused(INVALID, lambda: call(positions=At(4098)))
+    refused(INVALID, lambda: call(positions=p, ws=None))
+    refused(INVALID, lambda: call(ws=At(4100)))
+
+
+def test_norm_refused():
+    p = At()
+    f = lambda **kw: binding.sparsp_layer_norm_fwd(binding.make_norm(**{"rows": 4, "dim": 64, **kw}), p, p, p, p, p, p)  # noqa: E731
+    refused(INVALID, lambda: f(rows=-1))
+    refused(INVALID, lambda: f(dim=0, stride_x=8, stride_y=8))
+    refused(UNSUPPORTED, lambda: f(dim=16385))
+    refused(INVALID, lambda: f(rows_per_group=-1))
+    refused(INVALID, lambda: f(stride_x=63))
+    refused(INVALID, lambda: f(stride_y=63))
+    refused(INVALID, lambda: f(eps=-1.0))
+    refused(INVALID, lambda: f(eps=float("nan")))
+    refused(UNSUPPORTED, lambda: f(rows=2 ** 40, rows_per_group=1))
+    norm = binding.make_norm(4, 64)
+    bad = binding.make_norm(4, 64)
+    bad.weight_dtype = binding.SPARSP_FP16
+    refused(INVALID, lambda: binding.sparsp_layer_norm_fwd(bad, p, p, p, p, p, p))
+    g = binding.sparsp_layer_norm_fwd
+    refused(INVALID, g, norm, None, p, p, p, p, p)
+    refused(INVALID, g, norm, p, p, p, None, p, p)
+    refused(INVALID, g, norm, At(4097), p, p, p, p, p)
+    refused(INVALID, g, norm, p, p, p, p, p, None)
+    refused(INVALID, g, binding.make_norm(4, 64, stride_y=72), p, p, p, p, None, None)
+    b, q = binding.sparsp_layer_norm_bwd, At(8192)
+    refused(INVALID, b, norm, None, p, p, p, p, q, p, p, p)
+    refused(INVALID, b, norm, p, q, p, None, p, p, p, p, p)
+    refused(INVALID, b, norm, p, q, p, p, p, p, p, p, None)
+    refused(INVALID, b, norm, p, q, p, p, p, p, p, p, At(4112))
+    refused(INVALID, b, norm, p, q, p, p, p, q, p, p, p)  # dX = X
+    refused(INVALID, b, binding.make_norm(4, 64, stride_y=72), p, q, p, p, p, p, p, p, p)
+    assert binding.sparsp_layer_norm_workspace_bytes(norm) > 256
+
+
+def test_ffn_refused():
+    p = At()
+    f = lambda **kw: binding.sparsp_gated_ffn_fwd(binding.make_ffn(**{"tokens": 4, "dim": 64, "hidden": 72, **kw}), p, p, p, p, p, p, p)  # noqa: E731
+    refused(INVALID, lambda: f(tokens=-1))
+    refused(UNSUPPORTED, lambda: f(tokens=2 ** 31))
+    refused(UNSUPPORTED, lambda: f(dim=60))
+    refused(UNSUPPORTED, lambda: f(hidden=76))
+    refused(INVALID, lambda: f(hidden=0, stride_h=8))
+    refused(INVALID, lambda: f(stride_x=56))
+    refused(INVALID, lambda: f(stride_h=76))
+    refused(INVALID, lambda: f(stride_w=68))
+    ffn = binding.make_ffn(4, 64, 72)
+    bad = binding.make_ffn(4, 64, 72)
+    bad.dtype = binding.SPARSP_FP32
+    refused(UNSUPPORTED, lambda: binding.sparsp_gated_ffn_fwd(bad, p, p, p, p, p, p, p))
+    bad.dtype, bad.activation = 0, 3
+    refused(INVALID, lambda: binding.sparsp_gated_ffn_fwd(bad, p, p, p, p, p, p, p))
+    good = [p] * 7
+    for i in (0, 1, 2, 3, 6):
+        refused(INVALID, binding.sparsp_gated_ffn_fwd, ffn, *[None if i == j else a for j, a in enumerate(good)])
+        refused(INVALID, binding.sparsp_gated_ffn_fwd, ffn, *[At(4104) if i == j else a for j, a in enumerate(good)])
+    refused(INVALID, binding.sparsp_gated_ffn_fwd, ffn, p, p, p, p, p, None, p)
+    good = [p] * 10
+    for i in (0, 1, 2, 3, 4, 5, 8, 9):
+        refused(INVALID, binding.sparsp_gated_ffn_bwd, ffn, *[None if i == j else a for j, a in enumerate(good)])
+    assert binding.sparsp_gated_ffn_workspace_bytes(ffn, True) > binding.sparsp_gated_ffn_workspace_bytes(ffn, False)
