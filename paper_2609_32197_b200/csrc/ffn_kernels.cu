@@ -400,14 +400,17 @@ __global__ void __launch_bounds__(256) gate_grad_kernel(const T* dh, const T* ga
   const int col = (int)(i - row * per_row) * 8;
   const int64_t at = row * ld + col;
   const Vec<T, 8> h = load_once<T, 8>(dh + at), g = load_once<T, 8>(gate + at), u = load_once<T, 8>(up + at);
-  Vec<T, 8> og, ou;
+  float fg[8], fu[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     float a, slope;
     activate_both(activation, g[e], a, slope);
-    og.set(e, h[e] * u[e] * slope);
-    ou.set(e, h[e] * a);
+    fg[e] = h[e] * u[e] * slope;
+    fu[e] = h[e] * a;
   }
+  Vec<T, 8> og, ou;
+  og.set(fg);
+  ou.set(fu);
   store_vec<T, 8>(dg + row * hidden + col, og);
   store_vec<T, 8>(du + row * hidden + col, ou);
 }

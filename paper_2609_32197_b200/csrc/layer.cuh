@@ -4,6 +4,8 @@
 
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace sparsp {
@@ -59,31 +61,76 @@ __device__ __forceinline__ uint32_t pack2<__nv_bfloat16>(float a, float b) {
   return *reinterpret_cast<const uint32_t*>(&v);
 }
 
-// E consecutive elements as they lie in memory: one 16-byte access, or single elements.
+// E consecutive elements as they lie in memory: one 16-byte access, or single elements.  Pairs of 16-bit values stay in
+// the 32-bit words they were loaded in until they are used: taken apart at the load, they would make it be waited for.
 template <typename T, int E>
-struct alignas(E * sizeof(T)) Vec {
-  T v[E];
-  __device__ __forceinline__ float operator[](int i) const { return to_float<T>(v[i]); }
-  __device__ __forceinline__ void set(int i, float x) { v[i] = from_float<T>(x); }
+struct Vec {
+  static_assert(E == 1, "");
+  T v;
+  __device__ __forceinline__ float operator[](int) const { return to_float<T>(v); }
+  __device__ __forceinline__ void set(const float* x) { v = from_float<T>(x[0]); }
+};
+template <>
+struct alignas(16) Vec<float, 4> {
+  uint32_t w[4];
+  __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(w[i]); }
+  __device__ __forceinline__ void set(const float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(x[i]);
+  }
+};
+template <typename T>
+struct alignas(16) Vec<T, 8> {
+  uint32_t w[4];
+  __device__ __forceinline__ float operator[](int i) const {
+    const uint32_t x = w[i / 2];
+    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+      return __uint_as_float(i & 1 ? x & 0xffff0000u : x << 16);
+    } else {
+      const __half2 h = *reinterpret_cast<const __half2*>(&x);
+      return i & 1 ? __high2float(h) : __low2float(h);
+    }
+  }
+  __device__ __forceinline__ void set(const float* x) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
+  }
 };
 template <typename T, int E>
 __device__ __forceinline__ Vec<T, E> load_vec(const T* p) {
-  return *reinterpret_cast<const Vec<T, E>*>(p);
+  Vec<T, E> r;
+  if constexpr (E == 1) {
+    r.v = *p;
+  } else {
+    const uint4 x = *reinterpret_cast<const uint4*>(p);
+    r.w[0] = x.x;
+    r.w[1] = x.y;
+    r.w[2] = x.z;
+    r.w[3] = x.w;
+  }
+  return r;
 }
 // ... of data that this kernel reads once: it need not stay in L1
 template <typename T, int E>
 __device__ __forceinline__ Vec<T, E> load_once(const T* p) {
-  if constexpr (E * sizeof(T) == 16) {
-    Vec<T, E> r;
-    *reinterpret_cast<uint4*>(&r) = __ldcs(reinterpret_cast<const uint4*>(p));
-    return r;
+  Vec<T, E> r;
+  if constexpr (E == 1) {
+    r.v = *p;
   } else {
-    return load_vec<T, E>(p);
+    const uint4 x = __ldcs(reinterpret_cast<const uint4*>(p));
+    r.w[0] = x.x;
+    r.w[1] = x.y;
+    r.w[2] = x.z;
+    r.w[3] = x.w;
   }
+  return r;
 }
 template <typename T, int E>
 __device__ __forceinline__ void store_vec(T* p, const Vec<T, E>& x) {
-  *reinterpret_cast<Vec<T, E>*>(p) = x;
+  if constexpr (E == 1)
+    *p = x.v;
+  else
+    *reinterpret_cast<uint4*>(p) = make_uint4(x.w[0], x.w[1], x.w[2], x.w[3]);
 }
 
 // Runs the statements with T as the element type.

@@ -5,12 +5,16 @@
 
 namespace sparsp {
 
-// Rows are worked on by "workers": a warp each where a row fits its registers, otherwise a CTA.  Worker i of n has the
+// Rows are worked on by "workers": a warp each where a row is at most 512 values, otherwise a CTA.  Worker i of n has the
 // consecutive rows [i rows / n, (i + 1) rows / n) and holds the weights of the group it is in, so that they are read once
-// per worker, not once per row; the values of a row stay in registers from their load to the store, with the next row's
-// loads in flight meanwhile.
+// per worker, not once per row.  It takes R rows at a time: their values stay in registers from their load to the store,
+// the loads of the next R are in flight meanwhile, and the R rows share each barrier.  There are as many workers as fit
+// the multiprocessors by their registers, so none waits for another to end.
 constexpr int kNormThreads = 256;  // of a CTA whose warps are workers
-constexpr int kNormCta = 512;      // most threads of a CTA that is a worker: 128 registers each
+
+// By values a thread: most threads of a CTA, and with them the registers that each may have.
+constexpr int norm_threads(int values) { return values <= 8 ? 640 : 512; }
+constexpr int norm_registers(int values) { return values <= 8 ? 96 : 128; }
 
 struct NormParams {
   const void* x;
@@ -48,35 +52,55 @@ __device__ __forceinline__ void load_weights(const void* w, int64_t at, bool fp3
   }
 }
 
-// Sums over the worker's threads, in an order that depends on its size alone; every thread gets the sums.  A CTA's
-// warps meet in `slot`, which the caller alternates so that one barrier a call is enough.
+// Sums N values over the worker's threads, in an order that depends on its size alone; every thread gets the sums.
+// Inside a warp the values are halved with the lanes (after log2 N exchanges a lane carries one of them), so that N sums
+// take little more than one.  A CTA's warps meet in `slot`, which the caller alternates so that one barrier a call is
+// enough.
 template <int N, bool kCta>
 __device__ __forceinline__ void worker_sum(float (&v)[N], float (*slot)[N]) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1)
+  for (int k = N / 2, o = 1; k > 0; k /= 2, o *= 2) {
+    const bool high = lane & o;
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
-  if constexpr (kCta) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    if (lane == 0) {
-#pragma unroll
-      for (int k = 0; k < N; ++k) slot[warp][k] = v[k];
+    for (int i = 0; i < k; ++i) {
+      const float send = high ? v[i] : v[i + k], keep = high ? v[i + k] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
     }
+  }
+  float sum = v[0];  // of value `mine`
+  int mine = 0;
+#pragma unroll
+  for (int k = N / 2, o = 1; k > 0; k /= 2, o *= 2) mine += lane & o ? k : 0;
+#pragma unroll
+  for (int o = N; o < 32; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  if constexpr (kCta) {
+    const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    if (lane < N) slot[warp][mine] = sum;
     __syncthreads();
+    sum = 0.0f;
+    for (int w = lane / N; w < warps; w += 32 / N) sum += slot[w][lane % N];
 #pragma unroll
-    for (int k = 0; k < N; ++k) v[k] = lane < warps ? slot[lane][k] : 0.0f;
+    for (int o = N; o < 32; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
+    for (int i = 0; i < N; ++i) v[i] = __shfl_sync(0xffffffffu, sum, i);
+  } else {
+    // lane whose bits say value i
 #pragma unroll
-      for (int k = 0; k < N; ++k) v[k] += __shfl_xor_sync(0xffffffffu, v[k], o);
+    for (int i = 0; i < N; ++i) {
+      int from = 0;
+#pragma unroll
+      for (int k = N / 2, o = 1; k > 0; k /= 2, o *= 2) from |= i & k ? o : 0;
+      v[i] = __shfl_sync(0xffffffffu, sum, from);
+    }
   }
 }
 
-template <typename T, int E, int NV, bool kCta>
-__global__ void __launch_bounds__(kCta ? kNormCta : kNormThreads) norm_fwd_kernel(const NormParams p) {
+template <typename T, int E, int NV, int R, bool kCta>
+__global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kCta ? 1 : 2) norm_fwd_kernel(const NormParams p) {
   const void* x = p.x;
   enter_grid(x);
-  __shared__ float slots[4][32][1];
+  __shared__ float slots[4][32][R];
   const int lanes = kCta ? blockDim.x : 32;
   const int t = kCta ? threadIdx.x : (threadIdx.x & 31);
   const int64_t worker = kCta ? blockIdx.x : (int64_t)blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
@@ -87,18 +111,20 @@ __global__ void __launch_bounds__(kCta ? kNormCta : kNormThreads) norm_fwd_kerne
   const T* in = reinterpret_cast<const T*>(x);
   T* out = reinterpret_cast<T*>(p.y);
   float w[NV][E], b[NV][E];
-  Vec<T, E> next[NV];
+  Vec<T, E> cur[R][NV], next[R][NV];
+  int64_t g = r / p.rows_per_group, group_end = r;
+  int n_next = (int)min((int64_t)R, min(r1, (g + 1) * p.rows_per_group) - r), phase = 0;
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int e = (v * lanes + t) * E;
-    if (e < p.dim) next[v] = load_once<T, E>(in + r * p.stride_x + e);
-  }
-  int64_t group_end = r;
-  int phase = 0;
-  for (; r < r1; ++r) {
+  for (int k = 0; k < R; ++k)
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      const int e = (v * lanes + t) * E;
+      if (k < n_next && e < p.dim) next[k][v] = load_once<T, E>(in + (r + k) * p.stride_x + e);
+    }
+  while (r < r1) {
     if (r >= group_end) {
-      const int64_t g = r / p.rows_per_group;
-      group_end = (g + 1) * p.rows_per_group;
+      g = r / p.rows_per_group;
+      group_end = min(r1, (g + 1) * p.rows_per_group);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int e = (v * lanes + t) * E;
@@ -108,60 +134,79 @@ __global__ void __launch_bounds__(kCta ? kNormCta : kNormThreads) norm_fwd_kerne
         }
       }
     }
-    Vec<T, E> cur[NV];
-    float sum[1] = {0.0f};
+    const int n = n_next;
+    const int64_t after = r + n;
+    n_next = after < r1 ? (int)min((int64_t)R, (after < group_end ? group_end : min(r1, after + p.rows_per_group)) - after) : 0;
+    float sum[R];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int e = (v * lanes + t) * E;
-      cur[v] = next[v];
-      if (e < p.dim) {
-        if (r + 1 < r1) next[v] = load_once<T, E>(in + (r + 1) * p.stride_x + e);
+    for (int k = 0; k < R; ++k) {
+      sum[k] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < E; ++i) sum[0] += cur[v][i];
-      }
-    }
-    worker_sum<1, kCta>(sum, slots[phase]);
-    const float mean = sum[0] * p.inv_dim;
-    float sq[1] = {0.0f};
+      for (int v = 0; v < NV; ++v) {
+        const int e = (v * lanes + t) * E;
+        cur[k][v] = next[k][v];
+        if (e < p.dim) {
+          if (k < n_next) next[k][v] = load_once<T, E>(in + (after + k) * p.stride_x + e);
+          if (k < n) {
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int e = (v * lanes + t) * E;
-      if (e < p.dim) {
-#pragma unroll
-        for (int i = 0; i < E; ++i) {
-          const float d = cur[v][i] - mean;
-          sq[0] = fmaf(d, d, sq[0]);
+            for (int i = 0; i < E; ++i) sum[k] += cur[k][v][i];
+          }
         }
       }
     }
-    worker_sum<1, kCta>(sq, slots[phase + 1]);
-    phase ^= 2;
-    const float rstd = 1.0f / sqrtf(sq[0] * p.inv_dim + p.eps);
+    worker_sum<R, kCta>(sum, slots[phase]);
+    float sq[R];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int e = (v * lanes + t) * E;
-      if (e < p.dim) {
-        Vec<T, E> o;
+    for (int k = 0; k < R; ++k) {
+      sum[k] *= p.inv_dim;
+      sq[k] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < E; ++i) o.set(i, fmaf((cur[v][i] - mean) * rstd, w[v][i], b[v][i]));
-        store_vec<T, E>(out + r * p.stride_y + e, o);
+      for (int v = 0; v < NV; ++v) {
+        const int e = (v * lanes + t) * E;
+        if (k < n && e < p.dim) {
+#pragma unroll
+          for (int i = 0; i < E; ++i) {
+            const float d = cur[k][v][i] - sum[k];
+            sq[k] = fmaf(d, d, sq[k]);
+          }
+        }
       }
     }
-    if (p.mean != nullptr && t == 0) {
-      p.mean[r] = mean;
-      p.rstd[r] = rstd;
+    worker_sum<R, kCta>(sq, slots[phase + 1]);
+    phase ^= 2;
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      if (k >= n) continue;
+      const float rstd = 1.0f / sqrtf(sq[k] * p.inv_dim + p.eps);
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int e = (v * lanes + t) * E;
+        if (e < p.dim) {
+          float y[E];
+#pragma unroll
+          for (int i = 0; i < E; ++i) y[i] = fmaf((cur[k][v][i] - sum[k]) * rstd, w[v][i], b[v][i]);
+          Vec<T, E> o;
+          o.set(y);
+          store_vec<T, E>(out + (r + k) * p.stride_y + e, o);
+        }
+      }
+      if (p.mean != nullptr && t == 0) {
+        p.mean[r + k] = sum[k];
+        p.rstd[r + k] = rstd;
+      }
     }
+    r = after;
   }
 }
 
 // The gradients of the weights are sums over rows: each worker keeps those of its rows in registers and writes them out
 // when its group or its rows end, into slot worker + group, which no other (worker, group) has, as rows and with them
 // groups ascend from worker to worker.  norm_weights_kernel adds a group's slots.
-template <typename T, int E, int NV, bool kCta>
-__global__ void __launch_bounds__(kCta ? kNormCta : kNormThreads) norm_bwd_kernel(const NormParams p) {
+template <typename T, int E, int NV, int R, bool kCta>
+__global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kCta ? 1 : 2) norm_bwd_kernel(const NormParams p) {
   const void* x = p.x;
   enter_grid(x);
-  __shared__ float slots[2][32][2];
+  __shared__ float slots[2][32][2 * R];
   const int lanes = kCta ? blockDim.x : 32;
   const int t = kCta ? threadIdx.x : (threadIdx.x & 31);
   const int64_t worker = kCta ? blockIdx.x : (int64_t)blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
@@ -173,69 +218,100 @@ __global__ void __launch_bounds__(kCta ? kNormCta : kNormThreads) norm_bwd_kerne
   const T* grad = reinterpret_cast<const T*>(p.dy);
   T* out = reinterpret_cast<T*>(p.y);
   float w[NV][E], dw[NV][E], db[NV][E];
-  Vec<T, E> next_x[NV], next_dy[NV];
+  Vec<T, E> cx[R][NV], cy[R][NV], next_x[R][NV], next_y[R][NV];
+  float next_mean[R], next_rstd[R];
+  int64_t g = r / p.rows_per_group, group_end = r;
+  int n_next = (int)min((int64_t)R, min(r1, (g + 1) * p.rows_per_group) - r), phase = 0;
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int e = (v * lanes + t) * E;
-    if (e < p.dim) {
-      next_x[v] = load_once<T, E>(in + r * p.stride_x + e);
-      next_dy[v] = load_once<T, E>(grad + r * p.stride_y + e);
+  for (int k = 0; k < R; ++k) {
+    next_mean[k] = next_rstd[k] = 0.0f;
+    if (k < n_next) {
+      next_mean[k] = p.mean_in[r + k];
+      next_rstd[k] = p.rstd_in[r + k];
     }
 #pragma unroll
-    for (int i = 0; i < E; ++i) dw[v][i] = db[v][i] = 0.0f;
+    for (int v = 0; v < NV; ++v) {
+      const int e = (v * lanes + t) * E;
+      if (k < n_next && e < p.dim) {
+        next_x[k][v] = load_once<T, E>(in + (r + k) * p.stride_x + e);
+        next_y[k][v] = load_once<T, E>(grad + (r + k) * p.stride_y + e);
+      }
+    }
   }
-  int64_t g = r / p.rows_per_group, group_end = r;
-  int phase = 0;
-  for (; r < r1; ++r) {
+#pragma unroll
+  for (int v = 0; v < NV; ++v)
+#pragma unroll
+    for (int i = 0; i < E; ++i) dw[v][i] = db[v][i] = 0.0f;
+  while (r < r1) {
     if (r >= group_end) {
       g = r / p.rows_per_group;
-      group_end = (g + 1) * p.rows_per_group;
+      group_end = min(r1, (g + 1) * p.rows_per_group);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int e = (v * lanes + t) * E;
         if (e < p.dim) load_weights<T, E>(p.weight, g * p.dim + e, p.weights_fp32, 1.0f, w[v]);
       }
     }
-    const float mean = p.mean_in[r], rstd = p.rstd_in[r];
-    Vec<T, E> cx[NV], cy[NV];
-    float sum[2] = {0.0f, 0.0f};
+    const int n = n_next;
+    const int64_t after = r + n;
+    n_next = after < r1 ? (int)min((int64_t)R, (after < group_end ? group_end : min(r1, after + p.rows_per_group)) - after) : 0;
+    float sum[2 * R], mean[R], rstd[R];
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int e = (v * lanes + t) * E;
-      cx[v] = next_x[v];
-      cy[v] = next_dy[v];
-      if (e < p.dim) {
-        if (r + 1 < r1) {
-          next_x[v] = load_once<T, E>(in + (r + 1) * p.stride_x + e);
-          next_dy[v] = load_once<T, E>(grad + (r + 1) * p.stride_y + e);
-        }
+    for (int k = 0; k < R; ++k) {
+      mean[k] = next_mean[k];
+      rstd[k] = next_rstd[k];
+      if (k < n_next) {
+        next_mean[k] = p.mean_in[after + k];
+        next_rstd[k] = p.rstd_in[after + k];
+      }
+      sum[2 * k] = sum[2 * k + 1] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-          const float xh = (cx[v][i] - mean) * rstd, dy = cy[v][i], a = dy * w[v][i];
-          sum[0] += a;
-          sum[1] = fmaf(a, xh, sum[1]);
-          dw[v][i] = fmaf(dy, xh, dw[v][i]);
-          db[v][i] += dy;
+      for (int v = 0; v < NV; ++v) {
+        const int e = (v * lanes + t) * E;
+        cx[k][v] = next_x[k][v];
+        cy[k][v] = next_y[k][v];
+        if (e < p.dim) {
+          if (k < n_next) {
+            next_x[k][v] = load_once<T, E>(in + (after + k) * p.stride_x + e);
+            next_y[k][v] = load_once<T, E>(grad + (after + k) * p.stride_y + e);
+          }
+          if (k < n) {
+#pragma unroll
+            for (int i = 0; i < E; ++i) {
+              const float xh = (cx[k][v][i] - mean[k]) * rstd[k], dy = cy[k][v][i], a = dy * w[v][i];
+              sum[2 * k] += a;
+              sum[2 * k + 1] = fmaf(a, xh, sum[2 * k + 1]);
+              dw[v][i] = fmaf(dy, xh, dw[v][i]);
+              db[v][i] += dy;
+            }
+          }
         }
       }
     }
-    worker_sum<2, kCta>(sum, slots[phase]);
+    worker_sum<2 * R, kCta>(sum, slots[phase]);
     phase ^= 1;
-    const float c0 = sum[0] * p.inv_dim, c1 = sum[1] * p.inv_dim;
 #pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int e = (v * lanes + t) * E;
-      if (e < p.dim) {
-        Vec<T, E> o;
+    for (int k = 0; k < R; ++k) {
+      if (k >= n) continue;
+      const float c0 = sum[2 * k] * p.inv_dim, c1 = sum[2 * k + 1] * p.inv_dim;
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-          const float xh = (cx[v][i] - mean) * rstd;
-          o.set(i, rstd * (cy[v][i] * w[v][i] - c0 - xh * c1));
+      for (int v = 0; v < NV; ++v) {
+        const int e = (v * lanes + t) * E;
+        if (e < p.dim) {
+          float dx[E];
+#pragma unroll
+          for (int i = 0; i < E; ++i) {
+            const float xh = (cx[k][v][i] - mean[k]) * rstd[k];
+            dx[i] = rstd[k] * (cy[k][v][i] * w[v][i] - c0 - xh * c1);
+          }
+          Vec<T, E> o;
+          o.set(dx);
+          store_vec<T, E>(out + (r + k) * p.stride_x + e, o);
         }
-        store_vec<T, E>(out + r * p.stride_x + e, o);
       }
     }
-    if (p.want_weights && (r + 1 == r1 || r + 1 == group_end)) {
+    r = after;
+    if (p.want_weights && r == group_end) {
       float* mine = p.partial + (worker + g) * 2 * p.dim;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
@@ -305,10 +381,10 @@ int64_t norm_groups(const sparsp_norm& n) {
   return n.rows_per_group == 0 ? 1 : (n.rows + n.rows_per_group - 1) / n.rows_per_group;
 }
 
-// How a row is shared out: by elements and vectors a thread.
+// How a row is shared out: by values a thread.
 struct NormPlan {
   bool vectors, cta;
-  int per_thread, threads;  // vectors (or elements) a thread, threads of a CTA
+  int values, threads;  // of a thread, of a CTA
   int64_t n_workers;
   unsigned grid;
 };
@@ -316,21 +392,19 @@ struct NormPlan {
 static NormPlan plan_norm(const sparsp_norm& n, bool vectors) {
   NormPlan p;
   p.vectors = vectors;
-  const int E = vectors ? 16 / element_bytes(n.dtype) : 1;
-  const int units = (n.dim + E - 1) / E;  // vectors of a row
-  const int most = vectors ? 2 : 16;      // a warp's vectors a thread
-  p.cta = units > 32 * most;
+  p.cta = n.dim > 512;
   if (!p.cta) {
-    p.per_thread = vectors ? (units <= 32 ? 1 : 2) : (units <= 128 ? 4 : 16);
+    p.values = n.dim <= 256 ? 8 : 16;
     p.threads = kNormThreads;
-    p.n_workers = std::min<int64_t>(n.rows, (int64_t)kSms * 4 * (kNormThreads / 32));
+    p.n_workers = std::min<int64_t>(n.rows, (int64_t)kSms * 2 * (kNormThreads / 32));
     p.grid = (unsigned)((p.n_workers + kNormThreads / 32 - 1) / (kNormThreads / 32));
   } else {
-    p.per_thread = vectors ? 2 : 4;
-    while (p.per_thread * kNormCta < units) p.per_thread *= 2;
-    if (!vectors && p.per_thread == 8) p.per_thread = 16;
-    p.threads = ((units + p.per_thread - 1) / p.per_thread + 31) / 32 * 32;
-    const int resident = std::max(1, 1024 / p.threads);
+    p.values = 8;
+    while (p.values * norm_threads(p.values) < n.dim) p.values *= 2;
+    const int E = vectors ? 16 / element_bytes(n.dtype) : 1, per_thread = p.values / E;
+    const int units = (n.dim + E - 1) / E;
+    p.threads = ((units + per_thread - 1) / per_thread + 31) / 32 * 32;
+    const int resident = std::max(1, 65536 / (p.threads * norm_registers(p.values)));
     p.n_workers = std::min<int64_t>(n.rows, (int64_t)kSms * resident);
     p.grid = (unsigned)p.n_workers;
   }
@@ -348,30 +422,30 @@ static bool norm_vectors(const sparsp_norm& n, const void* a, const void* b, con
          (uintptr_t)b % 16 == 0 && (uintptr_t)c % 16 == 0;
 }
 
-template <typename T, int E, int NV, bool kCta>
+// Values a thread, and rows at a time by what its registers hold: forward two vectors a row, backward four and three
+// accumulators.
+template <typename T, int E, int kValues, bool kCta>
 static cudaError_t launch_norm_t(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
-  return launch_kernel(bwd ? norm_bwd_kernel<T, E, NV, kCta> : norm_fwd_kernel<T, E, NV, kCta>, dim3(plan.grid),
-                       plan.threads, 0, st, p);
+  constexpr int kFwdRows = kValues <= 8 ? 4 : kValues <= 16 ? 2 : 1, kBwdRows = kValues <= 8 ? 2 : 1;
+  return launch_kernel(bwd ? norm_bwd_kernel<T, E, kValues / E, kBwdRows, kCta>
+                           : norm_fwd_kernel<T, E, kValues / E, kFwdRows, kCta>,
+                       dim3(plan.grid), plan.threads, 0, st, p);
+}
+
+template <typename T, int E>
+static cudaError_t launch_norm_e(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
+  if (!plan.cta)
+    return plan.values == 8 ? launch_norm_t<T, E, 8, false>(p, plan, bwd, st)
+                            : launch_norm_t<T, E, 16, false>(p, plan, bwd, st);
+  return plan.values == 8    ? launch_norm_t<T, E, 8, true>(p, plan, bwd, st)
+         : plan.values == 16 ? launch_norm_t<T, E, 16, true>(p, plan, bwd, st)
+                             : launch_norm_t<T, E, 32, true>(p, plan, bwd, st);
 }
 
 static cudaError_t launch_norm(int dtype, const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
   cudaError_t e = cudaSuccess;
   SPARSP_WITH_TYPE(dtype, T, {
-    constexpr int E = 16 / sizeof(T);
-    if (plan.vectors && !plan.cta)
-      e = plan.per_thread == 1 ? launch_norm_t<T, E, 1, false>(p, plan, bwd, st)
-                               : launch_norm_t<T, E, 2, false>(p, plan, bwd, st);
-    else if (plan.vectors)
-      e = plan.per_thread == 2   ? launch_norm_t<T, E, 2, true>(p, plan, bwd, st)
-          : plan.per_thread == 4 ? launch_norm_t<T, E, 4, true>(p, plan, bwd, st)
-                                 : launch_norm_t<T, E, 32 / E, true>(p, plan, bwd, st);
-    else if (!plan.cta)
-      e = plan.per_thread == 4 ? launch_norm_t<T, 1, 4, false>(p, plan, bwd, st)
-                               : launch_norm_t<T, 1, 16, false>(p, plan, bwd, st);
-    else
-      e = plan.per_thread == 4    ? launch_norm_t<T, 1, 4, true>(p, plan, bwd, st)
-          : plan.per_thread == 16 ? launch_norm_t<T, 1, 16, true>(p, plan, bwd, st)
-                                  : launch_norm_t<T, 1, 32, true>(p, plan, bwd, st);
+    e = plan.vectors ? launch_norm_e<T, 16 / sizeof(T)>(p, plan, bwd, st) : launch_norm_e<T, 1>(p, plan, bwd, st);
   });
   return e;
 }

@@ -161,15 +161,20 @@ __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const RotaryPara
       for (int k = 0; k < kRotaryHeads; ++k)
         if (h + k < h1) {
           if (turn) {
+            float z[kLoads][V];
 #pragma unroll
             for (int i = 0; i < kPairs; ++i) {
               // the pair's two elements: load and place in it
-              const int la = 0, lb = kHalf ? 1 : 0;
+              constexpr int lb = kHalf ? 1 : 0;
               const int pa = kHalf ? i : 2 * i, pb = kHalf ? i : 2 * i + 1;
-              const float a = v[k][la][pa / VA][pa % VA], b = v[k][lb][pb / VA][pb % VA];
-              v[k][la][pa / VA].set(pa % VA, a * cs[i].x - b * cs[i].y);
-              v[k][lb][pb / VA].set(pb % VA, a * cs[i].y + b * cs[i].x);
+              const float a = v[k][0][pa / VA][pa % VA], b = v[k][lb][pb / VA][pb % VA];
+              z[0][pa] = a * cs[i].x - b * cs[i].y;
+              z[lb][pb] = a * cs[i].y + b * cs[i].x;
             }
+#pragma unroll
+            for (int l = 0; l < kLoads; ++l)
+#pragma unroll
+              for (int j = 0; j < V / VA; ++j) v[k][l][j].set(z[l] + j * VA);
           }
           T* mine = y + (h + k) * p.sH;
 #pragma unroll
