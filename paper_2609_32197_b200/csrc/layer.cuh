@@ -69,6 +69,7 @@ struct Vec {
   T v;
   __device__ __forceinline__ float operator[](int) const { return to_float<T>(v); }
   __device__ __forceinline__ void set(const float* x) { v = from_float<T>(x[0]); }
+  __device__ __forceinline__ void clear() { v = from_float<T>(0.0f); }
 };
 template <>
 struct alignas(16) Vec<float, 4> {
@@ -78,6 +79,7 @@ struct alignas(16) Vec<float, 4> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(x[i]);
   }
+  __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0u; }
 };
 template <typename T>
 struct alignas(16) Vec<T, 8> {
@@ -95,6 +97,7 @@ struct alignas(16) Vec<T, 8> {
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
   }
+  __device__ __forceinline__ void clear() { w[0] = w[1] = w[2] = w[3] = 0u; }
 };
 template <typename T, int E>
 __device__ __forceinline__ Vec<T, E> load_vec(const T* p) {

@@ -7,14 +7,19 @@ namespace sparsp {
 
 // Rows are worked on by "workers": a warp each where a row is at most 512 values, otherwise a CTA.  Worker i of n has the
 // consecutive rows [i rows / n, (i + 1) rows / n) and holds the weights of the group it is in, so that they are read once
-// per worker, not once per row.  It takes R rows at a time: their values stay in registers from their load to the store,
-// the loads of the next R are in flight meanwhile, and the R rows share each barrier.  There are as many workers as fit
-// the multiprocessors by their registers, so none waits for another to end.
+// per worker, not once per row.  It takes R rows at a time, which share each barrier; their values stay in registers from
+// there to the store.  The 2R rows after them are on their way into shared memory: each thread copies the values that it
+// will itself use (cp.async), so nobody waits for anybody else's copies.  There are as many workers as fit the
+// multiprocessors by their registers and their shared memory, so none waits for another to end.
 constexpr int kNormThreads = 256;  // of a CTA whose warps are workers
+constexpr int kAhead = 3;          // batches of R rows in shared memory: one in use, two on their way
 
 // By values a thread: most threads of a CTA, and with them the registers that each may have.
 constexpr int norm_threads(int values) { return values <= 8 ? 640 : 512; }
 constexpr int norm_registers(int values) { return values <= 8 ? 96 : 128; }
+// Rows at a time, by what the registers hold: forward the row and two weights, backward two rows and three weights or
+// sums.
+constexpr int norm_rows(int values, bool bwd) { return values <= 8 ? (bwd ? 2 : 4) : values <= 16 && !bwd ? 2 : 1; }
 
 struct NormParams {
   const void* x;
@@ -29,6 +34,7 @@ struct NormParams {
   float* partial;  // backward: [slots][2][dim]
   int64_t rows, rows_per_group, stride_x, stride_y;
   int32_t dim, weights_fp32, n_workers, want_weights;
+  int32_t ring_bytes;  // of a worker
   float eps, inv_dim;
 };
 
@@ -96,98 +102,218 @@ __device__ __forceinline__ void worker_sum(float (&v)[N], float (*slot)[N]) {
   }
 }
 
-template <typename T, int E, int NV, int R, bool kCta>
-__global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kCta ? 1 : 2) norm_fwd_kernel(const NormParams p) {
+// Two fp32 values in a 64-bit register: one instruction adds or multiplies both.
+struct F2 {
+  unsigned long long v;
+  __device__ __forceinline__ F2() {}
+  __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
+  __device__ __forceinline__ explicit F2(float a) : F2(a, a) {}
+  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+  __device__ __forceinline__ float sum() const {
+    float a, b;
+    get(a, b);
+    return a + b;
+  }
+};
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) {
+  F2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+
+// The rows ahead of a worker, of one tensor.  kRing: through shared memory as above; otherwise (single 16-bit values,
+// rows too long for shared memory) the next R rows through registers.
+template <typename T, int E, int NV, int R, bool kRing>
+struct RowsAhead {
+  Vec<T, E> next[kRing ? 1 : R][kRing ? 1 : NV];
+  const T* base;
+  int64_t stride;
+  char* ring;  // this thread's places, `lanes` vectors from one to the next
+  int lanes, t, dim;
+
+  __device__ __forceinline__ void fetch(int64_t row, int n, int batch) {
+#pragma unroll
+    for (int k = 0; k < R; ++k)
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        const int e = (v * lanes + t) * E;
+        if (k < n && e < dim) {
+          const T* from = base + (row + k) * stride + e;
+          if constexpr (kRing) {
+            char* to = ring + (int64_t)((batch * R + k) * NV + v) * lanes * (E * sizeof(T));
+            if constexpr (E * sizeof(T) == 16)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
+                           "l"(from)
+                           : "memory");
+            else
+              asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
+                           "l"(from)
+                           : "memory");
+          } else {
+            next[k][v] = load_once<T, E>(from);
+          }
+        }
+      }
+  }
+  __device__ __forceinline__ Vec<T, E> get(int k, int v, int batch) const {
+    if constexpr (kRing)
+      return load_vec<T, E>(reinterpret_cast<const T*>(ring + (int64_t)((batch * R + k) * NV + v) * lanes * (E * sizeof(T))));
+    else
+      return next[k][v];
+  }
+};
+// One group of copies per batch of rows (an empty one past the end); waits for the oldest batch.
+__device__ __forceinline__ void close_batch() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void wait_batch() { asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 2) : "memory"); }
+
+// Batches of a worker's rows: at most R at a time, and none across two groups of weights.
+struct Batches {
+  int64_t r1, per_group;
+  __device__ __forceinline__ int size(int64_t r, int R) const {
+    if (r >= r1) return 0;
+    const int64_t end = (r / per_group + 1) * per_group;
+    return (int)min((int64_t)R, min(r1, end) - r);
+  }
+};
+
+template <typename T, int E, int NV, int R, bool kCta, bool kRing>
+__global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kCta ? 1 : 2)
+    norm_fwd_kernel(const NormParams p) {
   const void* x = p.x;
   enter_grid(x);
+  constexpr int K = NV * E;
+  extern __shared__ __align__(16) char ring[];
   __shared__ float slots[4][32][R];
   const int lanes = kCta ? blockDim.x : 32;
   const int t = kCta ? threadIdx.x : (threadIdx.x & 31);
   const int64_t worker = kCta ? blockIdx.x : (int64_t)blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
   if (worker >= p.n_workers) return;
-  const int64_t r1 = first_row(worker + 1, p.n_workers, p.rows);
+  const Batches batches = {first_row(worker + 1, p.n_workers, p.rows), p.rows_per_group};
   int64_t r = first_row(worker, p.n_workers, p.rows);
-  if (r >= r1) return;
-  const T* in = reinterpret_cast<const T*>(x);
   T* out = reinterpret_cast<T*>(p.y);
-  float w[NV][E], b[NV][E];
-  Vec<T, E> cur[R][NV], next[R][NV];
-  int64_t g = r / p.rows_per_group, group_end = r;
-  int n_next = (int)min((int64_t)R, min(r1, (g + 1) * p.rows_per_group) - r), phase = 0;
-#pragma unroll
-  for (int k = 0; k < R; ++k)
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int e = (v * lanes + t) * E;
-      if (k < n_next && e < p.dim) next[k][v] = load_once<T, E>(in + (r + k) * p.stride_x + e);
-    }
-  while (r < r1) {
+  RowsAhead<T, E, NV, R, kRing> rows;
+  rows.base = reinterpret_cast<const T*>(x);
+  rows.stride = p.stride_x;
+  rows.ring = ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes) + t * (E * sizeof(T));
+  rows.lanes = lanes;
+  rows.t = t;
+  rows.dim = p.dim;
+  // n[0]: rows of the batch at work, n[1], n[2]: of the ones after it
+  int n[3];
+  int64_t ahead = r;
+  n[0] = batches.size(ahead, R);
+  rows.fetch(ahead, n[0], 0);
+  ahead += n[0];
+  n[1] = n[2] = 0;
+  if constexpr (kRing) {
+    close_batch();
+    n[1] = batches.size(ahead, R);
+    rows.fetch(ahead, n[1], 1);
+    close_batch();
+    ahead += n[1];
+  }
+  F2 w[K / 2], b[K / 2];
+  int64_t group_end = r;
+  int phase = 0, at = 0;
+  while (n[0] > 0) {
     if (r >= group_end) {
-      g = r / p.rows_per_group;
-      group_end = min(r1, (g + 1) * p.rows_per_group);
+      const int64_t g = r / p.rows_per_group;
+      group_end = (g + 1) * p.rows_per_group;
+      float wf[NV][E], bf[NV][E];
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int e = (v * lanes + t) * E;
+#pragma unroll
+        for (int i = 0; i < E; ++i) wf[v][i] = bf[v][i] = 0.0f;
         if (e < p.dim) {
-          load_weights<T, E>(p.weight, g * p.dim + e, p.weights_fp32, 1.0f, w[v]);
-          load_weights<T, E>(p.bias, g * p.dim + e, p.weights_fp32, 0.0f, b[v]);
+          load_weights<T, E>(p.weight, g * p.dim + e, p.weights_fp32, 1.0f, wf[v]);
+          load_weights<T, E>(p.bias, g * p.dim + e, p.weights_fp32, 0.0f, bf[v]);
         }
       }
+#pragma unroll
+      for (int j = 0; j < K; j += 2) {
+        w[j / 2] = F2(wf[j / E][j % E], wf[(j + 1) / E][(j + 1) % E]);
+        b[j / 2] = F2(bf[j / E][j % E], bf[(j + 1) / E][(j + 1) % E]);
+      }
     }
-    const int n = n_next;
-    const int64_t after = r + n;
-    n_next = after < r1 ? (int)min((int64_t)R, (after < group_end ? group_end : min(r1, after + p.rows_per_group)) - after) : 0;
+    if constexpr (kRing) wait_batch();
+    Vec<T, E> cur[R][NV];
     float sum[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      sum[k] = 0.0f;
+      F2 s(0.0f);
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int e = (v * lanes + t) * E;
-        cur[k][v] = next[k][v];
-        if (e < p.dim) {
-          if (k < n_next) next[k][v] = load_once<T, E>(in + (after + k) * p.stride_x + e);
-          if (k < n) {
-#pragma unroll
-            for (int i = 0; i < E; ++i) sum[k] += cur[k][v][i];
-          }
-        }
+        if (k < n[0] && (v * lanes + t) * E < p.dim)
+          cur[k][v] = rows.get(k, v, at);
+        else
+          cur[k][v].clear();
       }
+#pragma unroll
+      for (int j = 0; j < K; j += 2) s = s + F2(cur[k][j / E][j % E], cur[k][(j + 1) / E][(j + 1) % E]);
+      sum[k] = s.sum();
     }
+    // the batch after the next: into the places of the one before this, or the registers that were just emptied
+    const int more = batches.size(ahead, R);
+    rows.fetch(ahead, more, at == 0 ? 2 : at - 1);
+    if constexpr (kRing) close_batch();
+    ahead += more;
     worker_sum<R, kCta>(sum, slots[phase]);
     float sq[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       sum[k] *= p.inv_dim;
-      sq[k] = 0.0f;
+      const F2 minus(-sum[k]);
+      F2 q(0.0f);
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int e = (v * lanes + t) * E;
-        if (k < n && e < p.dim) {
-#pragma unroll
-          for (int i = 0; i < E; ++i) {
-            const float d = cur[k][v][i] - sum[k];
-            sq[k] = fmaf(d, d, sq[k]);
+      for (int j = 0; j < K; j += 2) {
+        F2 d = F2(cur[k][j / E][j % E], cur[k][(j + 1) / E][(j + 1) % E]) + minus;
+        if (E == 1 || K != E) {  // what lies beyond the row is no deviation
+          const int v0 = j / E, v1 = (j + 1) / E;
+          if (E > 1) {
+            if ((v0 * lanes + t) * E >= p.dim) d = F2(0.0f);
+          } else {
+            float d0, d1;
+            d.get(d0, d1);
+            d = F2(v0 * lanes + t < p.dim ? d0 : 0.0f, v1 * lanes + t < p.dim ? d1 : 0.0f);
           }
+        } else if (t * E >= p.dim) {
+          d = F2(0.0f);
         }
+        q = fma(d, d, q);
       }
+      sq[k] = q.sum();
     }
     worker_sum<R, kCta>(sq, slots[phase + 1]);
     phase ^= 2;
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      if (k >= n) continue;
+      if (k >= n[0]) continue;
       const float rstd = 1.0f / sqrtf(sq[k] * p.inv_dim + p.eps);
+      const F2 minus(-sum[k]), scale(rstd);
+      float y[K];
+#pragma unroll
+      for (int j = 0; j < K; j += 2) {
+        const F2 d = F2(cur[k][j / E][j % E], cur[k][(j + 1) / E][(j + 1) % E]) + minus;
+        fma(d * scale, w[j / 2], b[j / 2]).get(y[j], y[j + 1]);
+      }
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int e = (v * lanes + t) * E;
         if (e < p.dim) {
-          float y[E];
-#pragma unroll
-          for (int i = 0; i < E; ++i) y[i] = fmaf((cur[k][v][i] - sum[k]) * rstd, w[v][i], b[v][i]);
           Vec<T, E> o;
-          o.set(y);
-          store_vec<T, E>(out + (r + k) * p.stride_y + e, o);
+          o.set(y + v * E);
+          store_vec(out + (r + k) * p.stride_y + e, o);
         }
       }
       if (p.mean != nullptr && t == 0) {
@@ -195,136 +321,175 @@ __global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kC
         p.rstd[r + k] = rstd;
       }
     }
-    r = after;
+    r += n[0];
+    if constexpr (kRing) {
+      n[0] = n[1];
+      n[1] = more;
+      at = at == 2 ? 0 : at + 1;
+    } else {
+      n[0] = more;
+    }
   }
 }
 
 // The gradients of the weights are sums over rows: each worker keeps those of its rows in registers and writes them out
 // when its group or its rows end, into slot worker + group, which no other (worker, group) has, as rows and with them
 // groups ascend from worker to worker.  norm_weights_kernel adds a group's slots.
-template <typename T, int E, int NV, int R, bool kCta>
-__global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kCta ? 1 : 2) norm_bwd_kernel(const NormParams p) {
+template <typename T, int E, int NV, int R, bool kCta, bool kRing>
+__global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kCta ? 1 : 2)
+    norm_bwd_kernel(const NormParams p) {
   const void* x = p.x;
   enter_grid(x);
+  constexpr int K = NV * E;
+  extern __shared__ __align__(16) char ring[];
   __shared__ float slots[2][32][2 * R];
   const int lanes = kCta ? blockDim.x : 32;
   const int t = kCta ? threadIdx.x : (threadIdx.x & 31);
   const int64_t worker = kCta ? blockIdx.x : (int64_t)blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
   if (worker >= p.n_workers) return;
-  const int64_t r1 = first_row(worker + 1, p.n_workers, p.rows);
+  const Batches batches = {first_row(worker + 1, p.n_workers, p.rows), p.rows_per_group};
   int64_t r = first_row(worker, p.n_workers, p.rows);
-  if (r >= r1) return;
-  const T* in = reinterpret_cast<const T*>(x);
-  const T* grad = reinterpret_cast<const T*>(p.dy);
   T* out = reinterpret_cast<T*>(p.y);
-  float w[NV][E], dw[NV][E], db[NV][E];
-  Vec<T, E> cx[R][NV], cy[R][NV], next_x[R][NV], next_y[R][NV];
-  float next_mean[R], next_rstd[R];
-  int64_t g = r / p.rows_per_group, group_end = r;
-  int n_next = (int)min((int64_t)R, min(r1, (g + 1) * p.rows_per_group) - r), phase = 0;
-#pragma unroll
-  for (int k = 0; k < R; ++k) {
-    next_mean[k] = next_rstd[k] = 0.0f;
-    if (k < n_next) {
-      next_mean[k] = p.mean_in[r + k];
-      next_rstd[k] = p.rstd_in[r + k];
-    }
-#pragma unroll
-    for (int v = 0; v < NV; ++v) {
-      const int e = (v * lanes + t) * E;
-      if (k < n_next && e < p.dim) {
-        next_x[k][v] = load_once<T, E>(in + (r + k) * p.stride_x + e);
-        next_y[k][v] = load_once<T, E>(grad + (r + k) * p.stride_y + e);
-      }
-    }
-  }
-#pragma unroll
-  for (int v = 0; v < NV; ++v)
-#pragma unroll
-    for (int i = 0; i < E; ++i) dw[v][i] = db[v][i] = 0.0f;
-  while (r < r1) {
-    if (r >= group_end) {
-      g = r / p.rows_per_group;
-      group_end = min(r1, (g + 1) * p.rows_per_group);
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int e = (v * lanes + t) * E;
-        if (e < p.dim) load_weights<T, E>(p.weight, g * p.dim + e, p.weights_fp32, 1.0f, w[v]);
-      }
-    }
-    const int n = n_next;
-    const int64_t after = r + n;
-    n_next = after < r1 ? (int)min((int64_t)R, (after < group_end ? group_end : min(r1, after + p.rows_per_group)) - after) : 0;
-    float sum[2 * R], mean[R], rstd[R];
+  RowsAhead<T, E, NV, R, kRing> xs, ys;
+  xs.base = reinterpret_cast<const T*>(x);
+  ys.base = reinterpret_cast<const T*>(p.dy);
+  xs.stride = p.stride_x;
+  ys.stride = p.stride_y;
+  xs.ring = ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes) + t * (E * sizeof(T));
+  ys.ring = xs.ring + p.ring_bytes / 2;
+  xs.lanes = ys.lanes = lanes;
+  xs.t = ys.t = t;
+  xs.dim = ys.dim = p.dim;
+  float mean[R], rstd[R];  // of the next batch
+  auto stats = [&](int64_t row, int n) {
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      mean[k] = next_mean[k];
-      rstd[k] = next_rstd[k];
-      if (k < n_next) {
-        next_mean[k] = p.mean_in[after + k];
-        next_rstd[k] = p.rstd_in[after + k];
-      }
-      sum[2 * k] = sum[2 * k + 1] = 0.0f;
+      mean[k] = k < n ? p.mean_in[row + k] : 0.0f;
+      rstd[k] = k < n ? p.rstd_in[row + k] : 0.0f;
+    }
+  };
+  int n[3];
+  int64_t ahead = r;
+  n[0] = batches.size(ahead, R);
+  xs.fetch(ahead, n[0], 0);
+  ys.fetch(ahead, n[0], 0);
+  stats(ahead, n[0]);
+  ahead += n[0];
+  n[1] = n[2] = 0;
+  if constexpr (kRing) {
+    close_batch();
+    n[1] = batches.size(ahead, R);
+    xs.fetch(ahead, n[1], 1);
+    ys.fetch(ahead, n[1], 1);
+    close_batch();
+    ahead += n[1];
+  }
+  F2 w[K / 2], dw[K / 2], db[K / 2];
+#pragma unroll
+  for (int j = 0; j < K / 2; ++j) dw[j] = db[j] = F2(0.0f);
+  int64_t g = 0, group_end = r;
+  int phase = 0, at = 0;
+  while (n[0] > 0) {
+    if (r >= group_end) {
+      g = r / p.rows_per_group;
+      group_end = min(batches.r1, (g + 1) * p.rows_per_group);
+      float wf[NV][E];
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int e = (v * lanes + t) * E;
-        cx[k][v] = next_x[k][v];
-        cy[k][v] = next_y[k][v];
-        if (e < p.dim) {
-          if (k < n_next) {
-            next_x[k][v] = load_once<T, E>(in + (after + k) * p.stride_x + e);
-            next_y[k][v] = load_once<T, E>(grad + (after + k) * p.stride_y + e);
-          }
-          if (k < n) {
 #pragma unroll
-            for (int i = 0; i < E; ++i) {
-              const float xh = (cx[k][v][i] - mean[k]) * rstd[k], dy = cy[k][v][i], a = dy * w[v][i];
-              sum[2 * k] += a;
-              sum[2 * k + 1] = fmaf(a, xh, sum[2 * k + 1]);
-              dw[v][i] = fmaf(dy, xh, dw[v][i]);
-              db[v][i] += dy;
-            }
-          }
+        for (int i = 0; i < E; ++i) wf[v][i] = 0.0f;
+        if (e < p.dim) load_weights<T, E>(p.weight, g * p.dim + e, p.weights_fp32, 1.0f, wf[v]);
+      }
+#pragma unroll
+      for (int j = 0; j < K; j += 2) w[j / 2] = F2(wf[j / E][j % E], wf[(j + 1) / E][(j + 1) % E]);
+    }
+    if constexpr (kRing) wait_batch();
+    Vec<T, E> cx[R][NV], cy[R][NV];
+    F2 shift[R], scale[R];
+    float sum[2 * R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      scale[k] = F2(rstd[k]);
+      shift[k] = F2(-mean[k]);
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        if (k < n[0] && (v * lanes + t) * E < p.dim) {
+          cx[k][v] = xs.get(k, v, at);
+          cy[k][v] = ys.get(k, v, at);
+        } else {  // no gradient comes from there
+          cx[k][v].clear();
+          cy[k][v].clear();
         }
       }
+      F2 s0(0.0f), s1(0.0f);
+#pragma unroll
+      for (int j = 0; j < K; j += 2) {
+        const F2 xh = (F2(cx[k][j / E][j % E], cx[k][(j + 1) / E][(j + 1) % E]) + shift[k]) * scale[k];
+        const F2 dy(cy[k][j / E][j % E], cy[k][(j + 1) / E][(j + 1) % E]);
+        const F2 a = dy * w[j / 2];
+        s0 = s0 + a;
+        s1 = fma(a, xh, s1);
+        dw[j / 2] = fma(dy, xh, dw[j / 2]);
+        db[j / 2] = db[j / 2] + dy;
+      }
+      sum[2 * k] = s0.sum();
+      sum[2 * k + 1] = s1.sum();
     }
+    const int more = batches.size(ahead, R);
+    xs.fetch(ahead, more, at == 0 ? 2 : at - 1);
+    ys.fetch(ahead, more, at == 0 ? 2 : at - 1);
+    if constexpr (kRing) close_batch();
+    ahead += more;
+    stats(r + n[0], kRing ? n[1] : more);
     worker_sum<2 * R, kCta>(sum, slots[phase]);
     phase ^= 1;
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      if (k >= n) continue;
-      const float c0 = sum[2 * k] * p.inv_dim, c1 = sum[2 * k + 1] * p.inv_dim;
+      if (k >= n[0]) continue;
+      const F2 c0(-sum[2 * k] * p.inv_dim), c1(-sum[2 * k + 1] * p.inv_dim);
+      float dx[K];
+#pragma unroll
+      for (int j = 0; j < K; j += 2) {
+        const F2 xh = (F2(cx[k][j / E][j % E], cx[k][(j + 1) / E][(j + 1) % E]) + shift[k]) * scale[k];
+        const F2 dy(cy[k][j / E][j % E], cy[k][(j + 1) / E][(j + 1) % E]);
+        (scale[k] * fma(xh, c1, fma(dy, w[j / 2], c0))).get(dx[j], dx[j + 1]);
+      }
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         const int e = (v * lanes + t) * E;
         if (e < p.dim) {
-          float dx[E];
-#pragma unroll
-          for (int i = 0; i < E; ++i) {
-            const float xh = (cx[k][v][i] - mean[k]) * rstd[k];
-            dx[i] = rstd[k] * (cy[k][v][i] * w[v][i] - c0 - xh * c1);
-          }
           Vec<T, E> o;
-          o.set(dx);
-          store_vec<T, E>(out + (r + k) * p.stride_x + e, o);
+          o.set(dx + v * E);
+          store_vec(out + (r + k) * p.stride_x + e, o);
         }
       }
     }
-    r = after;
+    r += n[0];
     if (p.want_weights && r == group_end) {
       float* mine = p.partial + (worker + g) * 2 * p.dim;
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int e = (v * lanes + t) * E;
-        if (e < p.dim) {
+      for (int j = 0; j < K; j += 2) {
+        float a[2], c[2];
+        dw[j / 2].get(a[0], a[1]);
+        db[j / 2].get(c[0], c[1]);
+        dw[j / 2] = db[j / 2] = F2(0.0f);
 #pragma unroll
-          for (int i = 0; i < E; ++i) {
-            mine[e + i] = dw[v][i];
-            mine[p.dim + e + i] = db[v][i];
-            dw[v][i] = db[v][i] = 0.0f;
+        for (int i = 0; i < 2; ++i) {
+          const int e = ((j + i) / E * lanes + t) * E;
+          if (e < p.dim) {
+            mine[e + (j + i) % E] = a[i];
+            mine[p.dim + e + (j + i) % E] = c[i];
           }
         }
       }
+    }
+    if constexpr (kRing) {
+      n[0] = n[1];
+      n[1] = more;
+      at = at == 2 ? 0 : at + 1;
+    } else {
+      n[0] = more;
     }
   }
 }
@@ -383,36 +548,44 @@ int64_t norm_groups(const sparsp_norm& n) {
 
 // How a row is shared out: by values a thread.
 struct NormPlan {
-  bool vectors, cta;
-  int values, threads;  // of a thread, of a CTA
+  bool vectors, cta, ring;
+  int values, threads;         // of a thread, of a CTA
+  int ring_bytes, smem_bytes;  // of a worker, of a CTA
   int64_t n_workers;
   unsigned grid;
 };
 
-static NormPlan plan_norm(const sparsp_norm& n, bool vectors) {
+constexpr int kNormSmem = 224 * 1024;  // of a multiprocessor, for rings
+
+static NormPlan plan_norm(const sparsp_norm& n, bool vectors, bool bwd) {
   NormPlan p;
   p.vectors = vectors;
   p.cta = n.dim > 512;
-  if (!p.cta) {
-    p.values = n.dim <= 256 ? 8 : 16;
-    p.threads = kNormThreads;
-    p.n_workers = std::min<int64_t>(n.rows, (int64_t)kSms * 2 * (kNormThreads / 32));
-    p.grid = (unsigned)((p.n_workers + kNormThreads / 32 - 1) / (kNormThreads / 32));
-  } else {
+  const int bytes = element_bytes(n.dtype), E = vectors ? 16 / bytes : 1;
+  p.values = p.cta || n.dim > 256 ? 16 : 8;
+  int resident = 2;
+  if (p.cta) {
     p.values = 8;
     while (p.values * norm_threads(p.values) < n.dim) p.values *= 2;
-    const int E = vectors ? 16 / element_bytes(n.dtype) : 1, per_thread = p.values / E;
-    const int units = (n.dim + E - 1) / E;
+    const int units = (n.dim + E - 1) / E, per_thread = p.values / E;
     p.threads = ((units + per_thread - 1) / per_thread + 31) / 32 * 32;
-    const int resident = std::max(1, 65536 / (p.threads * norm_registers(p.values)));
-    p.n_workers = std::min<int64_t>(n.rows, (int64_t)kSms * resident);
-    p.grid = (unsigned)p.n_workers;
+    resident = std::max(1, 65536 / (p.threads * norm_registers(p.values)));
+  } else {
+    p.threads = kNormThreads;
   }
+  const int workers = p.cta ? 1 : kNormThreads / 32;  // of a CTA
+  const int lanes = p.cta ? p.threads : 32;
+  p.ring_bytes = kAhead * norm_rows(p.values, bwd) * lanes * p.values * bytes * (bwd ? 2 : 1);
+  p.ring = E * bytes >= 4 && p.ring_bytes * workers <= kNormSmem - 4096;
+  p.smem_bytes = p.ring ? p.ring_bytes * workers : 0;
+  if (p.ring) resident = std::min(resident, kNormSmem / (p.smem_bytes + 4096));
+  p.n_workers = std::min<int64_t>(n.rows, (int64_t)kSms * resident * workers);
+  p.grid = (unsigned)((p.n_workers + workers - 1) / workers);
   return p;
 }
 
 int64_t norm_workspace_bytes(const sparsp_norm& n) {
-  const int64_t workers = std::max(plan_norm(n, true).n_workers, plan_norm(n, false).n_workers);
+  const int64_t workers = std::max(plan_norm(n, true, true).n_workers, plan_norm(n, false, true).n_workers);
   return kStatusWords * 4 + (workers + norm_groups(n)) * 2 * n.dim * 4;
 }
 
@@ -422,14 +595,27 @@ static bool norm_vectors(const sparsp_norm& n, const void* a, const void* b, con
          (uintptr_t)b % 16 == 0 && (uintptr_t)c % 16 == 0;
 }
 
-// Values a thread, and rows at a time by what its registers hold: forward two vectors a row, backward four and three
-// accumulators.
+template <typename T, int E, int kValues, bool kCta, bool kRing>
+static cudaError_t launch_norm_r(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
+  auto kern = bwd ? norm_bwd_kernel<T, E, kValues / E, norm_rows(kValues, true), kCta, kRing>
+                  : norm_fwd_kernel<T, E, kValues / E, norm_rows(kValues, false), kCta, kRing>;
+  if (kRing) {
+    const cudaError_t e = ensure_dynamic_smem((const void*)kern, plan.smem_bytes);
+    if (e != cudaSuccess) return e;
+  }
+  return launch_kernel(kern, dim3(plan.grid), plan.threads, plan.smem_bytes, st, p);
+}
+
+// Without a ring: single 16-bit values, and rows of 32 values a thread that may be too long for shared memory.
 template <typename T, int E, int kValues, bool kCta>
 static cudaError_t launch_norm_t(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
-  constexpr int kFwdRows = kValues <= 8 ? 4 : kValues <= 16 ? 2 : 1, kBwdRows = kValues <= 8 ? 2 : 1;
-  return launch_kernel(bwd ? norm_bwd_kernel<T, E, kValues / E, kBwdRows, kCta>
-                           : norm_fwd_kernel<T, E, kValues / E, kFwdRows, kCta>,
-                       dim3(plan.grid), plan.threads, 0, st, p);
+  if constexpr (E * sizeof(T) < 4)
+    return launch_norm_r<T, E, kValues, kCta, false>(p, plan, bwd, st);
+  else if constexpr (kValues == 32)
+    return plan.ring ? launch_norm_r<T, E, kValues, kCta, true>(p, plan, bwd, st)
+                     : launch_norm_r<T, E, kValues, kCta, false>(p, plan, bwd, st);
+  else
+    return launch_norm_r<T, E, kValues, kCta, true>(p, plan, bwd, st);
 }
 
 template <typename T, int E>
@@ -459,6 +645,7 @@ static NormParams norm_params(const sparsp_norm& n, const NormPlan& plan) {
   p.dim = n.dim;
   p.weights_fp32 = n.weight_dtype == SPARSP_FP32;
   p.n_workers = (int32_t)plan.n_workers;
+  p.ring_bytes = plan.ring_bytes;
   p.eps = n.eps;
   p.inv_dim = 1.0f / (float)n.dim;
   return p;
@@ -467,7 +654,7 @@ static NormParams norm_params(const sparsp_norm& n, const NormPlan& plan) {
 int launch_norm_fwd(const sparsp_norm& n, const void* X, const void* w, const void* b, void* Y, float* mean,
                     float* rstd, cudaStream_t st) {
   if (n.rows == 0) return SPARSP_OK;
-  const NormPlan plan = plan_norm(n, norm_vectors(n, X, Y, nullptr));
+  const NormPlan plan = plan_norm(n, norm_vectors(n, X, Y, nullptr), false);
   NormParams p = norm_params(n, plan);
   p.x = X;
   p.weight = w;
@@ -481,7 +668,7 @@ int launch_norm_fwd(const sparsp_norm& n, const void* X, const void* w, const vo
 
 int launch_norm_bwd(const sparsp_norm& n, const void* dY, const void* X, const void* w, const float* mean,
                     const float* rstd, void* dX, void* dw, void* db, char* ws, cudaStream_t st) {
-  const NormPlan plan = plan_norm(n, norm_vectors(n, X, dY, dX));
+  const NormPlan plan = plan_norm(n, norm_vectors(n, X, dY, dX), true);
   NormParams p = norm_params(n, plan);
   p.want_weights = dw != nullptr || db != nullptr;
   if (n.rows > 0) {
