@@ -14,12 +14,17 @@ namespace sparsp {
 constexpr int kNormThreads = 256;  // of a CTA whose warps are workers
 constexpr int kAhead = 3;          // batches of R rows in shared memory: one in use, two on their way
 
-// By values a thread: most threads of a CTA, and with them the registers that each may have.
-constexpr int norm_threads(int values) { return values <= 8 ? 640 : 512; }
-constexpr int norm_registers(int values) { return values <= 8 ? 96 : 128; }
+// Who works on a row, by its length: a warp with 8 values a thread (up to 256) or 16 (512), or a CTA with 16 values a
+// thread and up to 320 threads (5120), of which a multiprocessor takes two or more, so that one computes while another
+// waits at its barrier; beyond that up to 512 threads with 16 values (8192) or 32.
+enum Worker { kWarp8, kWarp16, kTeam, kLongTeam, kLongestTeam };
+__host__ __device__ constexpr int worker_values(int kind) { return kind == kWarp8 ? 8 : kind == kLongestTeam ? 32 : 16; }
+__host__ __device__ constexpr int worker_threads(int kind) { return kind <= kWarp16 ? kNormThreads : kind == kTeam ? 320 : 512; }  // of a CTA, at most
+__host__ __device__ constexpr int worker_ctas(int kind) { return kind <= kTeam ? 2 : 1; }  // such CTAs that fit a multiprocessor
+__host__ __device__ constexpr int worker_registers(int kind) { return kind == kTeam ? 96 : 128; }
 // Rows at a time, by what the registers hold: forward the row and two weights, backward two rows and three weights or
 // sums.
-constexpr int norm_rows(int values, bool bwd) { return values <= 8 ? (bwd ? 2 : 4) : values <= 16 && !bwd ? 2 : 1; }
+__host__ __device__ constexpr int worker_rows(int kind, bool bwd) { return kind == kWarp8 ? (bwd ? 2 : 4) : kind == kLongestTeam || bwd ? 1 : 2; }
 
 struct NormParams {
   const void* x;
@@ -136,38 +141,40 @@ __device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
 template <typename T, int E, int NV, int R, bool kRing>
 struct RowsAhead {
   Vec<T, E> next[kRing ? 1 : R][kRing ? 1 : NV];
-  const T* base;
+  const T* from;  // this thread's first value of the next row to be fetched
   int64_t stride;
   char* ring;  // this thread's places, `lanes` vectors from one to the next
   int lanes, t, dim;
 
-  __device__ __forceinline__ void fetch(int64_t row, int n, int batch) {
+  __device__ __forceinline__ void fetch(int n, int batch) {
 #pragma unroll
-    for (int k = 0; k < R; ++k)
+    for (int k = 0; k < R; ++k) {
+      if (k >= n) break;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int e = (v * lanes + t) * E;
-        if (k < n && e < dim) {
-          const T* from = base + (row + k) * stride + e;
+        if ((v * lanes + t) * E < dim) {
+          const T* at = from + v * lanes * E;
           if constexpr (kRing) {
-            char* to = ring + (int64_t)((batch * R + k) * NV + v) * lanes * (E * sizeof(T));
+            char* to = ring + ((batch * R + k) * NV + v) * lanes * (int)(E * sizeof(T));
             if constexpr (E * sizeof(T) == 16)
               asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                           "l"(from)
+                           "l"(at)
                            : "memory");
             else
               asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                           "l"(from)
+                           "l"(at)
                            : "memory");
           } else {
-            next[k][v] = load_once<T, E>(from);
+            next[k][v] = load_once<T, E>(at);
           }
         }
       }
+      from += stride;
+    }
   }
   __device__ __forceinline__ Vec<T, E> get(int k, int v, int batch) const {
     if constexpr (kRing)
-      return load_vec<T, E>(reinterpret_cast<const T*>(ring + (int64_t)((batch * R + k) * NV + v) * lanes * (E * sizeof(T))));
+      return load_vec<T, E>(reinterpret_cast<const T*>(ring + ((batch * R + k) * NV + v) * lanes * (int)(E * sizeof(T))));
     else
       return next[k][v];
   }
@@ -176,33 +183,36 @@ struct RowsAhead {
 __device__ __forceinline__ void close_batch() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void wait_batch() { asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 2) : "memory"); }
 
-// Batches of a worker's rows: at most R at a time, and none across two groups of weights.
+// Walks a worker's rows in batches: at most R rows at a time, and none across two groups of weights.
 struct Batches {
-  int64_t r1, per_group;
-  __device__ __forceinline__ int size(int64_t r, int R) const {
-    if (r >= r1) return 0;
-    const int64_t end = (r / per_group + 1) * per_group;
-    return (int)min((int64_t)R, min(r1, end) - r);
+  int64_t at, end, group_end, per_group;
+  __device__ __forceinline__ Batches(const NormParams& p, int64_t worker)
+      : at(first_row(worker, p.n_workers, p.rows)), end(first_row(worker + 1, p.n_workers, p.rows)),
+        group_end((at / p.rows_per_group + 1) * p.rows_per_group), per_group(p.rows_per_group) {}
+  __device__ __forceinline__ int size(int R) const { return (int)min((int64_t)R, min(end, group_end) - at); }
+  __device__ __forceinline__ void take(int n) {
+    at += n;
+    if (at == group_end) group_end += per_group;
   }
 };
 
-template <typename T, int E, int NV, int R, bool kCta, bool kRing>
-__global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kCta ? 1 : 2)
-    norm_fwd_kernel(const NormParams p) {
+template <typename T, int E, int kKind, bool kRing>
+__global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) norm_fwd_kernel(const NormParams p) {
   const void* x = p.x;
   enter_grid(x);
-  constexpr int K = NV * E;
+  constexpr int K = worker_values(kKind), NV = K / E, R = worker_rows(kKind, false);
+  constexpr bool kCta = kKind >= kTeam;
   extern __shared__ __align__(16) char ring[];
   __shared__ float slots[4][32][R];
   const int lanes = kCta ? blockDim.x : 32;
   const int t = kCta ? threadIdx.x : (threadIdx.x & 31);
   const int64_t worker = kCta ? blockIdx.x : (int64_t)blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
   if (worker >= p.n_workers) return;
-  const Batches batches = {first_row(worker + 1, p.n_workers, p.rows), p.rows_per_group};
-  int64_t r = first_row(worker, p.n_workers, p.rows);
-  T* out = reinterpret_cast<T*>(p.y);
+  Batches ahead(p, worker);
+  int64_t r = ahead.at;
+  T* out = reinterpret_cast<T*>(p.y) + r * p.stride_y + t * E;
   RowsAhead<T, E, NV, R, kRing> rows;
-  rows.base = reinterpret_cast<const T*>(x);
+  rows.from = reinterpret_cast<const T*>(x) + r * p.stride_x + t * E;
   rows.stride = p.stride_x;
   rows.ring = ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes) + t * (E * sizeof(T));
   rows.lanes = lanes;
@@ -210,17 +220,16 @@ __global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kC
   rows.dim = p.dim;
   // n[0]: rows of the batch at work, n[1], n[2]: of the ones after it
   int n[3];
-  int64_t ahead = r;
-  n[0] = batches.size(ahead, R);
-  rows.fetch(ahead, n[0], 0);
-  ahead += n[0];
+  n[0] = ahead.size(R);
+  rows.fetch(n[0], 0);
+  ahead.take(n[0]);
   n[1] = n[2] = 0;
   if constexpr (kRing) {
     close_batch();
-    n[1] = batches.size(ahead, R);
-    rows.fetch(ahead, n[1], 1);
+    n[1] = ahead.size(R);
+    rows.fetch(n[1], 1);
     close_batch();
-    ahead += n[1];
+    ahead.take(n[1]);
   }
   F2 w[K / 2], b[K / 2];
   int64_t group_end = r;
@@ -264,10 +273,10 @@ __global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kC
       sum[k] = s.sum();
     }
     // the batch after the next: into the places of the one before this, or the registers that were just emptied
-    const int more = batches.size(ahead, R);
-    rows.fetch(ahead, more, at == 0 ? 2 : at - 1);
+    const int more = ahead.size(R);
+    rows.fetch(more, at == 0 ? 2 : at - 1);
     if constexpr (kRing) close_batch();
-    ahead += more;
+    ahead.take(more);
     worker_sum<R, kCta>(sum, slots[phase]);
     float sq[R];
 #pragma unroll
@@ -299,7 +308,7 @@ __global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kC
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       if (k >= n[0]) continue;
-      const float rstd = 1.0f / sqrtf(sq[k] * p.inv_dim + p.eps);
+      const float rstd = rsqrtf(sq[k] * p.inv_dim + p.eps);
       const F2 minus(-sum[k]), scale(rstd);
       float y[K];
 #pragma unroll
@@ -309,13 +318,13 @@ __global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kC
       }
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int e = (v * lanes + t) * E;
-        if (e < p.dim) {
+        if ((v * lanes + t) * E < p.dim) {
           Vec<T, E> o;
           o.set(y + v * E);
-          store_vec(out + (r + k) * p.stride_y + e, o);
+          store_vec(out + v * lanes * E, o);
         }
       }
+      out += p.stride_y;
       if (p.mean != nullptr && t == 0) {
         p.mean[r + k] = sum[k];
         p.rstd[r + k] = rstd;
@@ -335,24 +344,24 @@ __global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kC
 // The gradients of the weights are sums over rows: each worker keeps those of its rows in registers and writes them out
 // when its group or its rows end, into slot worker + group, which no other (worker, group) has, as rows and with them
 // groups ascend from worker to worker.  norm_weights_kernel adds a group's slots.
-template <typename T, int E, int NV, int R, bool kCta, bool kRing>
-__global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kCta ? 1 : 2)
-    norm_bwd_kernel(const NormParams p) {
+template <typename T, int E, int kKind, bool kRing>
+__global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) norm_bwd_kernel(const NormParams p) {
   const void* x = p.x;
   enter_grid(x);
-  constexpr int K = NV * E;
+  constexpr int K = worker_values(kKind), NV = K / E, R = worker_rows(kKind, true);
+  constexpr bool kCta = kKind >= kTeam;
   extern __shared__ __align__(16) char ring[];
   __shared__ float slots[2][32][2 * R];
   const int lanes = kCta ? blockDim.x : 32;
   const int t = kCta ? threadIdx.x : (threadIdx.x & 31);
   const int64_t worker = kCta ? blockIdx.x : (int64_t)blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
   if (worker >= p.n_workers) return;
-  const Batches batches = {first_row(worker + 1, p.n_workers, p.rows), p.rows_per_group};
-  int64_t r = first_row(worker, p.n_workers, p.rows);
-  T* out = reinterpret_cast<T*>(p.y);
+  Batches ahead(p, worker);
+  int64_t r = ahead.at;
+  T* out = reinterpret_cast<T*>(p.y) + r * p.stride_x + t * E;
   RowsAhead<T, E, NV, R, kRing> xs, ys;
-  xs.base = reinterpret_cast<const T*>(x);
-  ys.base = reinterpret_cast<const T*>(p.dy);
+  xs.from = reinterpret_cast<const T*>(x) + r * p.stride_x + t * E;
+  ys.from = reinterpret_cast<const T*>(p.dy) + r * p.stride_y + t * E;
   xs.stride = p.stride_x;
   ys.stride = p.stride_y;
   xs.ring = ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes) + t * (E * sizeof(T));
@@ -369,20 +378,19 @@ __global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kC
     }
   };
   int n[3];
-  int64_t ahead = r;
-  n[0] = batches.size(ahead, R);
-  xs.fetch(ahead, n[0], 0);
-  ys.fetch(ahead, n[0], 0);
-  stats(ahead, n[0]);
-  ahead += n[0];
+  n[0] = ahead.size(R);
+  xs.fetch(n[0], 0);
+  ys.fetch(n[0], 0);
+  stats(ahead.at, n[0]);
+  ahead.take(n[0]);
   n[1] = n[2] = 0;
   if constexpr (kRing) {
     close_batch();
-    n[1] = batches.size(ahead, R);
-    xs.fetch(ahead, n[1], 1);
-    ys.fetch(ahead, n[1], 1);
+    n[1] = ahead.size(R);
+    xs.fetch(n[1], 1);
+    ys.fetch(n[1], 1);
     close_batch();
-    ahead += n[1];
+    ahead.take(n[1]);
   }
   F2 w[K / 2], dw[K / 2], db[K / 2];
 #pragma unroll
@@ -392,7 +400,7 @@ __global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kC
   while (n[0] > 0) {
     if (r >= group_end) {
       g = r / p.rows_per_group;
-      group_end = min(batches.r1, (g + 1) * p.rows_per_group);
+      group_end = min(ahead.end, (g + 1) * p.rows_per_group);
       float wf[NV][E];
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
@@ -436,11 +444,11 @@ __global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kC
       sum[2 * k] = s0.sum();
       sum[2 * k + 1] = s1.sum();
     }
-    const int more = batches.size(ahead, R);
-    xs.fetch(ahead, more, at == 0 ? 2 : at - 1);
-    ys.fetch(ahead, more, at == 0 ? 2 : at - 1);
+    const int more = ahead.size(R);
+    xs.fetch(more, at == 0 ? 2 : at - 1);
+    ys.fetch(more, at == 0 ? 2 : at - 1);
     if constexpr (kRing) close_batch();
-    ahead += more;
+    ahead.take(more);
     stats(r + n[0], kRing ? n[1] : more);
     worker_sum<2 * R, kCta>(sum, slots[phase]);
     phase ^= 1;
@@ -457,13 +465,13 @@ __global__ void __launch_bounds__(kCta ? norm_threads(NV * E) : kNormThreads, kC
       }
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
-        const int e = (v * lanes + t) * E;
-        if (e < p.dim) {
+        if ((v * lanes + t) * E < p.dim) {
           Vec<T, E> o;
           o.set(dx + v * E);
-          store_vec(out + (r + k) * p.stride_x + e, o);
+          store_vec(out + v * lanes * E, o);
         }
       }
+      out += p.stride_x;
     }
     r += n[0];
     if (p.want_weights && r == group_end) {
@@ -546,10 +554,10 @@ int64_t norm_groups(const sparsp_norm& n) {
   return n.rows_per_group == 0 ? 1 : (n.rows + n.rows_per_group - 1) / n.rows_per_group;
 }
 
-// How a row is shared out: by values a thread.
+// How the rows are shared out.
 struct NormPlan {
-  bool vectors, cta, ring;
-  int values, threads;         // of a thread, of a CTA
+  bool vectors, ring;
+  int kind, threads;           // of a CTA
   int ring_bytes, smem_bytes;  // of a worker, of a CTA
   int64_t n_workers;
   unsigned grid;
@@ -560,22 +568,18 @@ constexpr int kNormSmem = 224 * 1024;  // of a multiprocessor, for rings
 static NormPlan plan_norm(const sparsp_norm& n, bool vectors, bool bwd) {
   NormPlan p;
   p.vectors = vectors;
-  p.cta = n.dim > 512;
   const int bytes = element_bytes(n.dtype), E = vectors ? 16 / bytes : 1;
-  p.values = p.cta || n.dim > 256 ? 16 : 8;
-  int resident = 2;
-  if (p.cta) {
-    p.values = 8;
-    while (p.values * norm_threads(p.values) < n.dim) p.values *= 2;
-    const int units = (n.dim + E - 1) / E, per_thread = p.values / E;
+  p.kind = n.dim <= 256 ? kWarp8 : n.dim <= 512 ? kWarp16 : n.dim <= 5120 ? kTeam : n.dim <= 8192 ? kLongTeam : kLongestTeam;
+  const bool cta = p.kind >= kTeam;
+  p.threads = kNormThreads;
+  if (cta) {
+    const int units = (n.dim + E - 1) / E, per_thread = worker_values(p.kind) / E;
     p.threads = ((units + per_thread - 1) / per_thread + 31) / 32 * 32;
-    resident = std::max(1, 65536 / (p.threads * norm_registers(p.values)));
-  } else {
-    p.threads = kNormThreads;
   }
-  const int workers = p.cta ? 1 : kNormThreads / 32;  // of a CTA
-  const int lanes = p.cta ? p.threads : 32;
-  p.ring_bytes = kAhead * norm_rows(p.values, bwd) * lanes * p.values * bytes * (bwd ? 2 : 1);
+  int resident = std::min(32, 65536 / (p.threads * worker_registers(p.kind)));
+  const int workers = cta ? 1 : kNormThreads / 32;  // of a CTA
+  const int lanes = cta ? p.threads : 32;
+  p.ring_bytes = kAhead * worker_rows(p.kind, bwd) * lanes * worker_values(p.kind) * bytes * (bwd ? 2 : 1);
   p.ring = E * bytes >= 4 && p.ring_bytes * workers <= kNormSmem - 4096;
   p.smem_bytes = p.ring ? p.ring_bytes * workers : 0;
   if (p.ring) resident = std::min(resident, kNormSmem / (p.smem_bytes + 4096));
@@ -595,10 +599,9 @@ static bool norm_vectors(const sparsp_norm& n, const void* a, const void* b, con
          (uintptr_t)b % 16 == 0 && (uintptr_t)c % 16 == 0;
 }
 
-template <typename T, int E, int kValues, bool kCta, bool kRing>
+template <typename T, int E, int kKind, bool kRing>
 static cudaError_t launch_norm_r(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
-  auto kern = bwd ? norm_bwd_kernel<T, E, kValues / E, norm_rows(kValues, true), kCta, kRing>
-                  : norm_fwd_kernel<T, E, kValues / E, norm_rows(kValues, false), kCta, kRing>;
+  auto kern = bwd ? norm_bwd_kernel<T, E, kKind, kRing> : norm_fwd_kernel<T, E, kKind, kRing>;
   if (kRing) {
     const cudaError_t e = ensure_dynamic_smem((const void*)kern, plan.smem_bytes);
     if (e != cudaSuccess) return e;
@@ -606,26 +609,27 @@ static cudaError_t launch_norm_r(const NormParams& p, const NormPlan& plan, bool
   return launch_kernel(kern, dim3(plan.grid), plan.threads, plan.smem_bytes, st, p);
 }
 
-// Without a ring: single 16-bit values, and rows of 32 values a thread that may be too long for shared memory.
-template <typename T, int E, int kValues, bool kCta>
+// Without a ring: single 16-bit values, and rows that are too long for shared memory.
+template <typename T, int E, int kKind>
 static cudaError_t launch_norm_t(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
   if constexpr (E * sizeof(T) < 4)
-    return launch_norm_r<T, E, kValues, kCta, false>(p, plan, bwd, st);
-  else if constexpr (kValues == 32)
-    return plan.ring ? launch_norm_r<T, E, kValues, kCta, true>(p, plan, bwd, st)
-                     : launch_norm_r<T, E, kValues, kCta, false>(p, plan, bwd, st);
+    return launch_norm_r<T, E, kKind, false>(p, plan, bwd, st);
+  else if constexpr (kKind == kLongestTeam)
+    return plan.ring ? launch_norm_r<T, E, kKind, true>(p, plan, bwd, st)
+                     : launch_norm_r<T, E, kKind, false>(p, plan, bwd, st);
   else
-    return launch_norm_r<T, E, kValues, kCta, true>(p, plan, bwd, st);
+    return launch_norm_r<T, E, kKind, true>(p, plan, bwd, st);
 }
 
 template <typename T, int E>
 static cudaError_t launch_norm_e(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
-  if (!plan.cta)
-    return plan.values == 8 ? launch_norm_t<T, E, 8, false>(p, plan, bwd, st)
-                            : launch_norm_t<T, E, 16, false>(p, plan, bwd, st);
-  return plan.values == 8    ? launch_norm_t<T, E, 8, true>(p, plan, bwd, st)
-         : plan.values == 16 ? launch_norm_t<T, E, 16, true>(p, plan, bwd, st)
-                             : launch_norm_t<T, E, 32, true>(p, plan, bwd, st);
+  switch (plan.kind) {
+    case kWarp8: return launch_norm_t<T, E, kWarp8>(p, plan, bwd, st);
+    case kWarp16: return launch_norm_t<T, E, kWarp16>(p, plan, bwd, st);
+    case kTeam: return launch_norm_t<T, E, kTeam>(p, plan, bwd, st);
+    case kLongTeam: return launch_norm_t<T, E, kLongTeam>(p, plan, bwd, st);
+    default: return launch_norm_t<T, E, kLongestTeam>(p, plan, bwd, st);
+  }
 }
 
 static cudaError_t launch_norm(int dtype, const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
