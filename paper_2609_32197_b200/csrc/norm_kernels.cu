@@ -155,7 +155,7 @@ struct RowsAhead {
         if ((v * lanes + t) * E < dim) {
           const T* at = from + v * lanes * E;
           if constexpr (kRing) {
-            char* to = ring + ((batch * R + k) * NV + v) * lanes * (int)(E * sizeof(T));
+            char* to = place(batch * R + k, v);
             if constexpr (E * sizeof(T) == 16)
               asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
                            "l"(at)
@@ -172,29 +172,84 @@ struct RowsAhead {
       from += stride;
     }
   }
-  __device__ __forceinline__ Vec<T, E> get(int k, int v, int batch) const {
-    if constexpr (kRing)
-      return load_vec<T, E>(reinterpret_cast<const T*>(ring + ((batch * R + k) * NV + v) * lanes * (int)(E * sizeof(T))));
-    else
-      return next[k][v];
+  // Makes what lies beyond the row zero, once: nothing is ever fetched to there.
+  __device__ __forceinline__ void clear_beyond() {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      Vec<T, E> zero;
+      zero.clear();
+      if constexpr (kRing) {
+        if ((v * lanes + t) * E >= dim)
+          for (int k = 0; k < kAhead * R; ++k) store_vec(reinterpret_cast<T*>(place(k, v)), zero);
+      } else {
+#pragma unroll
+        for (int k = 0; k < R; ++k) next[k][v] = zero;
+      }
+    }
+  }
+  // Row k of a batch as pairs, zeros beyond the row.  Where the batch has no row k, of an earlier one, or anything.
+  __device__ __forceinline__ void values(F2 (&out)[NV * E / 2], int k, int batch) const {
+    float f[NV * E];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      Vec<T, E> x;
+      if constexpr (kRing)
+        x = load_vec<T, E>(reinterpret_cast<const T*>(place(batch * R + k, v)));
+      else
+        x = next[k][v];
+#pragma unroll
+      for (int i = 0; i < E; ++i) f[v * E + i] = x[i];
+    }
+#pragma unroll
+    for (int j = 0; j < NV * E / 2; ++j) out[j] = F2(f[2 * j], f[2 * j + 1]);
+  }
+  __device__ __forceinline__ char* place(int row, int v) const {
+    return ring + (row * NV + v) * lanes * (int)(E * sizeof(T));
+  }
+  // Makes pair j zero where it lies beyond the row.
+  __device__ __forceinline__ void inside(F2& x, int j) const {
+    if constexpr (E > 1) {
+      if ((2 * j / E * lanes + t) * E >= dim) x = F2(0.0f);
+    } else {
+      float a, b;
+      x.get(a, b);
+      x = F2(2 * j * lanes + t < dim ? a : 0.0f, (2 * j + 1) * lanes + t < dim ? b : 0.0f);
+    }
   }
 };
 // One group of copies per batch of rows (an empty one past the end); waits for the oldest batch.
 __device__ __forceinline__ void close_batch() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void wait_batch() { asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 2) : "memory"); }
 
-// Walks a worker's rows in batches: at most R rows at a time, and none across two groups of weights.
+// A worker's rows in batches: at most R rows at a time, and none across two groups of weights.
 struct Batches {
-  int64_t at, end, group_end, per_group;
-  __device__ __forceinline__ Batches(const NormParams& p, int64_t worker)
-      : at(first_row(worker, p.n_workers, p.rows)), end(first_row(worker + 1, p.n_workers, p.rows)),
-        group_end((at / p.rows_per_group + 1) * p.rows_per_group), per_group(p.rows_per_group) {}
-  __device__ __forceinline__ int size(int R) const { return (int)min((int64_t)R, min(end, group_end) - at); }
+  int left, in_group, per_group;  // rows yet to be fetched, of them in the group
+  __device__ __forceinline__ int size(int R) const { return min(R, min(left, in_group)); }
   __device__ __forceinline__ void take(int n) {
-    at += n;
-    if (at == group_end) group_end += per_group;
+    left -= n;
+    in_group -= n;
+    if (in_group == 0) in_group = per_group;
   }
 };
+
+// A thread's weights of group g; zeros beyond the row.
+template <typename T, int E, int NV>
+__device__ __forceinline__ void load_pairs(const NormParams& p, const void* from, int64_t g, int lanes, int t,
+                                           float missing, F2 (&out)[NV * E / 2]) {
+  float f[NV * E];
+#pragma unroll
+  for (int v = 0; v < NV; ++v) {
+    const int e = (v * lanes + t) * E;
+    float part[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) part[i] = 0.0f;
+    if (e < p.dim) load_weights<T, E>(from, g * p.dim + e, p.weights_fp32, missing, part);
+#pragma unroll
+    for (int i = 0; i < E; ++i) f[v * E + i] = part[i];
+  }
+#pragma unroll
+  for (int j = 0; j < NV * E / 2; ++j) out[j] = F2(f[2 * j], f[2 * j + 1]);
+}
 
 template <typename T, int E, int kKind, bool kRing>
 __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) norm_fwd_kernel(const NormParams p) {
@@ -208,8 +263,12 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
   const int t = kCta ? threadIdx.x : (threadIdx.x & 31);
   const int64_t worker = kCta ? blockIdx.x : (int64_t)blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
   if (worker >= p.n_workers) return;
-  Batches ahead(p, worker);
-  int64_t r = ahead.at;
+  const int64_t r = first_row(worker, p.n_workers, p.rows);
+  int todo = (int)(first_row(worker + 1, p.n_workers, p.rows) - r);
+  int64_t g = r / p.rows_per_group;
+  const int per_group = (int)min(p.rows_per_group, (int64_t)0x7fffffff);
+  int here = (int)min((int64_t)todo, (g + 1) * p.rows_per_group - r);  // rows of the group at work
+  Batches ahead = {todo, (int)min((g + 1) * p.rows_per_group - r, (int64_t)0x7fffffff), per_group};
   T* out = reinterpret_cast<T*>(p.y) + r * p.stride_y + t * E;
   RowsAhead<T, E, NV, R, kRing> rows;
   rows.from = reinterpret_cast<const T*>(x) + r * p.stride_x + t * E;
@@ -218,6 +277,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
   rows.lanes = lanes;
   rows.t = t;
   rows.dim = p.dim;
+  rows.clear_beyond();
   // n[0]: rows of the batch at work, n[1], n[2]: of the ones after it
   int n[3];
   n[0] = ahead.size(R);
@@ -231,112 +291,82 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
     close_batch();
     ahead.take(n[1]);
   }
-  F2 w[K / 2], b[K / 2];
-  int64_t group_end = r;
+  float* mean = p.mean == nullptr ? nullptr : p.mean + r;
+  float* rstds = p.rstd + (p.mean == nullptr ? 0 : r);
   int phase = 0, at = 0;
-  while (n[0] > 0) {
-    if (r >= group_end) {
-      const int64_t g = r / p.rows_per_group;
-      group_end = (g + 1) * p.rows_per_group;
-      float wf[NV][E], bf[NV][E];
+  for (; todo > 0; todo -= here, ++g, here = min(todo, per_group)) {
+    F2 w[K / 2], b[K / 2];
+    load_pairs<T, E, NV>(p, p.weight, g, lanes, t, 1.0f, w);
+    load_pairs<T, E, NV>(p, p.bias, g, lanes, t, 0.0f, b);
+#pragma unroll 1
+    for (int left = here; left > 0;) {
+      if constexpr (kRing) wait_batch();
+      F2 cur[R][K / 2];
+      float sum[R];
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int e = (v * lanes + t) * E;
+      for (int k = 0; k < R; ++k) {
+        rows.values(cur[k], k, at);
+        F2 s = cur[k][0];
 #pragma unroll
-        for (int i = 0; i < E; ++i) wf[v][i] = bf[v][i] = 0.0f;
-        if (e < p.dim) {
-          load_weights<T, E>(p.weight, g * p.dim + e, p.weights_fp32, 1.0f, wf[v]);
-          load_weights<T, E>(p.bias, g * p.dim + e, p.weights_fp32, 0.0f, bf[v]);
+        for (int j = 1; j < K / 2; ++j) s = s + cur[k][j];
+        sum[k] = s.sum();
+      }
+      // the batch after the next: into the places of the one before this, or the registers that were just emptied
+      const int more = ahead.size(R);
+      rows.fetch(more, at == 0 ? 2 : at - 1);
+      if constexpr (kRing) close_batch();
+      ahead.take(more);
+      worker_sum<R, kCta>(sum, slots[phase]);
+      float sq[R];
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        sum[k] *= p.inv_dim;
+        const F2 minus(-sum[k]);
+        F2 q(0.0f);
+#pragma unroll
+        for (int j = 0; j < K / 2; ++j) {
+          cur[k][j] = cur[k][j] + minus;
+          rows.inside(cur[k][j], j);  // what lies beyond the row is no deviation
+          q = fma(cur[k][j], cur[k][j], q);
         }
+        sq[k] = q.sum();
       }
+      worker_sum<R, kCta>(sq, slots[phase + 1]);
+      phase ^= 2;
 #pragma unroll
-      for (int j = 0; j < K; j += 2) {
-        w[j / 2] = F2(wf[j / E][j % E], wf[(j + 1) / E][(j + 1) % E]);
-        b[j / 2] = F2(bf[j / E][j % E], bf[(j + 1) / E][(j + 1) % E]);
-      }
-    }
-    if constexpr (kRing) wait_batch();
-    Vec<T, E> cur[R][NV];
-    float sum[R];
+      for (int k = 0; k < R; ++k) {
+        if (k >= n[0]) continue;
+        const float rstd = rsqrtf(sq[k] * p.inv_dim + p.eps);
+        const F2 scale(rstd);
+        float y[K];
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-      F2 s(0.0f);
+        for (int j = 0; j < K / 2; ++j) fma(cur[k][j] * scale, w[j], b[j]).get(y[2 * j], y[2 * j + 1]);
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        if (k < n[0] && (v * lanes + t) * E < p.dim)
-          cur[k][v] = rows.get(k, v, at);
-        else
-          cur[k][v].clear();
-      }
-#pragma unroll
-      for (int j = 0; j < K; j += 2) s = s + F2(cur[k][j / E][j % E], cur[k][(j + 1) / E][(j + 1) % E]);
-      sum[k] = s.sum();
-    }
-    // the batch after the next: into the places of the one before this, or the registers that were just emptied
-    const int more = ahead.size(R);
-    rows.fetch(more, at == 0 ? 2 : at - 1);
-    if constexpr (kRing) close_batch();
-    ahead.take(more);
-    worker_sum<R, kCta>(sum, slots[phase]);
-    float sq[R];
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      sum[k] *= p.inv_dim;
-      const F2 minus(-sum[k]);
-      F2 q(0.0f);
-#pragma unroll
-      for (int j = 0; j < K; j += 2) {
-        F2 d = F2(cur[k][j / E][j % E], cur[k][(j + 1) / E][(j + 1) % E]) + minus;
-        if (E == 1 || K != E) {  // what lies beyond the row is no deviation
-          const int v0 = j / E, v1 = (j + 1) / E;
-          if (E > 1) {
-            if ((v0 * lanes + t) * E >= p.dim) d = F2(0.0f);
-          } else {
-            float d0, d1;
-            d.get(d0, d1);
-            d = F2(v0 * lanes + t < p.dim ? d0 : 0.0f, v1 * lanes + t < p.dim ? d1 : 0.0f);
+        for (int v = 0; v < NV; ++v) {
+          if ((v * lanes + t) * E < p.dim) {
+            Vec<T, E> o;
+            o.set(y + v * E);
+            store_vec(out + v * lanes * E, o);
           }
-        } else if (t * E >= p.dim) {
-          d = F2(0.0f);
         }
-        q = fma(d, d, q);
-      }
-      sq[k] = q.sum();
-    }
-    worker_sum<R, kCta>(sq, slots[phase + 1]);
-    phase ^= 2;
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      if (k >= n[0]) continue;
-      const float rstd = rsqrtf(sq[k] * p.inv_dim + p.eps);
-      const F2 minus(-sum[k]), scale(rstd);
-      float y[K];
-#pragma unroll
-      for (int j = 0; j < K; j += 2) {
-        const F2 d = F2(cur[k][j / E][j % E], cur[k][(j + 1) / E][(j + 1) % E]) + minus;
-        fma(d * scale, w[j / 2], b[j / 2]).get(y[j], y[j + 1]);
-      }
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        if ((v * lanes + t) * E < p.dim) {
-          Vec<T, E> o;
-          o.set(y + v * E);
-          store_vec(out + v * lanes * E, o);
+        out += p.stride_y;
+        if (mean != nullptr && t == 0) {
+          mean[k] = sum[k];
+          rstds[k] = rstd;
         }
       }
-      out += p.stride_y;
-      if (p.mean != nullptr && t == 0) {
-        p.mean[r + k] = sum[k];
-        p.rstd[r + k] = rstd;
+      if (mean != nullptr) {
+        mean += n[0];
+        rstds += n[0];
       }
-    }
-    r += n[0];
-    if constexpr (kRing) {
-      n[0] = n[1];
-      n[1] = more;
-      at = at == 2 ? 0 : at + 1;
-    } else {
-      n[0] = more;
+      left -= n[0];
+      if constexpr (kRing) {
+        n[0] = n[1];
+        n[1] = more;
+        at = at == 2 ? 0 : at + 1;
+      } else {
+        n[0] = more;
+      }
     }
   }
 }
@@ -356,8 +386,12 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
   const int t = kCta ? threadIdx.x : (threadIdx.x & 31);
   const int64_t worker = kCta ? blockIdx.x : (int64_t)blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
   if (worker >= p.n_workers) return;
-  Batches ahead(p, worker);
-  int64_t r = ahead.at;
+  const int64_t r = first_row(worker, p.n_workers, p.rows);
+  int todo = (int)(first_row(worker + 1, p.n_workers, p.rows) - r);
+  int64_t g = r / p.rows_per_group;
+  const int per_group = (int)min(p.rows_per_group, (int64_t)0x7fffffff);
+  int here = (int)min((int64_t)todo, (g + 1) * p.rows_per_group - r);  // rows of the group at work
+  Batches ahead = {todo, (int)min((g + 1) * p.rows_per_group - r, (int64_t)0x7fffffff), per_group};
   T* out = reinterpret_cast<T*>(p.y) + r * p.stride_x + t * E;
   RowsAhead<T, E, NV, R, kRing> xs, ys;
   xs.from = reinterpret_cast<const T*>(x) + r * p.stride_x + t * E;
@@ -369,19 +403,25 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
   xs.lanes = ys.lanes = lanes;
   xs.t = ys.t = t;
   xs.dim = ys.dim = p.dim;
+  xs.clear_beyond();
+  ys.clear_beyond();
   float mean[R], rstd[R];  // of the next batch
-  auto stats = [&](int64_t row, int n) {
+  const float* means = p.mean_in + r;
+  const float* rstds = p.rstd_in + r;
+  auto stats = [&](int n) {
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      mean[k] = k < n ? p.mean_in[row + k] : 0.0f;
-      rstd[k] = k < n ? p.rstd_in[row + k] : 0.0f;
+      mean[k] = k < n ? means[k] : 0.0f;
+      rstd[k] = k < n ? rstds[k] : 0.0f;
     }
+    means += n;
+    rstds += n;
   };
   int n[3];
   n[0] = ahead.size(R);
   xs.fetch(n[0], 0);
   ys.fetch(n[0], 0);
-  stats(ahead.at, n[0]);
+  stats(n[0]);
   ahead.take(n[0]);
   n[1] = n[2] = 0;
   if constexpr (kRing) {
@@ -392,96 +432,81 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
     close_batch();
     ahead.take(n[1]);
   }
-  F2 w[K / 2], dw[K / 2], db[K / 2];
-#pragma unroll
-  for (int j = 0; j < K / 2; ++j) dw[j] = db[j] = F2(0.0f);
-  int64_t g = 0, group_end = r;
   int phase = 0, at = 0;
-  while (n[0] > 0) {
-    if (r >= group_end) {
-      g = r / p.rows_per_group;
-      group_end = min(ahead.end, (g + 1) * p.rows_per_group);
-      float wf[NV][E];
+  for (; todo > 0; todo -= here, ++g, here = min(todo, per_group)) {
+    F2 w[K / 2], dw[K / 2], db[K / 2];
+    load_pairs<T, E, NV>(p, p.weight, g, lanes, t, 1.0f, w);
 #pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        const int e = (v * lanes + t) * E;
+    for (int j = 0; j < K / 2; ++j) dw[j] = db[j] = F2(0.0f);
+#pragma unroll 1
+    for (int left = here; left > 0;) {
+      if constexpr (kRing) wait_batch();
+      F2 xh[R][K / 2], a[R][K / 2], scale[R];
+      float sum[2 * R];
 #pragma unroll
-        for (int i = 0; i < E; ++i) wf[v][i] = 0.0f;
-        if (e < p.dim) load_weights<T, E>(p.weight, g * p.dim + e, p.weights_fp32, 1.0f, wf[v]);
-      }
+      for (int k = 0; k < R; ++k) {
+        scale[k] = F2(rstd[k]);
+        const F2 shift(-mean[k]);
+        // beyond the row there is no gradient: dy is 0 there
+        xs.values(xh[k], k, at);
+        ys.values(a[k], k, at);
+        sum[2 * k] = sum[2 * k + 1] = 0.0f;
+        if (R > 1 && k >= n[0]) continue;
+        F2 s0(0.0f), s1(0.0f);
 #pragma unroll
-      for (int j = 0; j < K; j += 2) w[j / 2] = F2(wf[j / E][j % E], wf[(j + 1) / E][(j + 1) % E]);
-    }
-    if constexpr (kRing) wait_batch();
-    Vec<T, E> cx[R][NV], cy[R][NV];
-    F2 shift[R], scale[R];
-    float sum[2 * R];
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      scale[k] = F2(rstd[k]);
-      shift[k] = F2(-mean[k]);
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        if (k < n[0] && (v * lanes + t) * E < p.dim) {
-          cx[k][v] = xs.get(k, v, at);
-          cy[k][v] = ys.get(k, v, at);
-        } else {  // no gradient comes from there
-          cx[k][v].clear();
-          cy[k][v].clear();
+        for (int j = 0; j < K / 2; ++j) {
+          const F2 dy = a[k][j];
+          xh[k][j] = (xh[k][j] + shift) * scale[k];
+          a[k][j] = dy * w[j];
+          s0 = s0 + a[k][j];
+          s1 = fma(a[k][j], xh[k][j], s1);
+          dw[j] = fma(dy, xh[k][j], dw[j]);
+          db[j] = db[j] + dy;
         }
+        sum[2 * k] = s0.sum();
+        sum[2 * k + 1] = s1.sum();
       }
-      F2 s0(0.0f), s1(0.0f);
+      const int more = ahead.size(R);
+      xs.fetch(more, at == 0 ? 2 : at - 1);
+      ys.fetch(more, at == 0 ? 2 : at - 1);
+      if constexpr (kRing) close_batch();
+      ahead.take(more);
+      stats(kRing ? n[1] : more);
+      worker_sum<2 * R, kCta>(sum, slots[phase]);
+      phase ^= 1;
 #pragma unroll
-      for (int j = 0; j < K; j += 2) {
-        const F2 xh = (F2(cx[k][j / E][j % E], cx[k][(j + 1) / E][(j + 1) % E]) + shift[k]) * scale[k];
-        const F2 dy(cy[k][j / E][j % E], cy[k][(j + 1) / E][(j + 1) % E]);
-        const F2 a = dy * w[j / 2];
-        s0 = s0 + a;
-        s1 = fma(a, xh, s1);
-        dw[j / 2] = fma(dy, xh, dw[j / 2]);
-        db[j / 2] = db[j / 2] + dy;
-      }
-      sum[2 * k] = s0.sum();
-      sum[2 * k + 1] = s1.sum();
-    }
-    const int more = ahead.size(R);
-    xs.fetch(more, at == 0 ? 2 : at - 1);
-    ys.fetch(more, at == 0 ? 2 : at - 1);
-    if constexpr (kRing) close_batch();
-    ahead.take(more);
-    stats(r + n[0], kRing ? n[1] : more);
-    worker_sum<2 * R, kCta>(sum, slots[phase]);
-    phase ^= 1;
+      for (int k = 0; k < R; ++k) {
+        if (k >= n[0]) continue;
+        const F2 c0(-sum[2 * k] * p.inv_dim), c1(-sum[2 * k + 1] * p.inv_dim);
+        float dx[K];
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-      if (k >= n[0]) continue;
-      const F2 c0(-sum[2 * k] * p.inv_dim), c1(-sum[2 * k + 1] * p.inv_dim);
-      float dx[K];
+        for (int j = 0; j < K / 2; ++j) (scale[k] * fma(xh[k][j], c1, a[k][j] + c0)).get(dx[2 * j], dx[2 * j + 1]);
 #pragma unroll
-      for (int j = 0; j < K; j += 2) {
-        const F2 xh = (F2(cx[k][j / E][j % E], cx[k][(j + 1) / E][(j + 1) % E]) + shift[k]) * scale[k];
-        const F2 dy(cy[k][j / E][j % E], cy[k][(j + 1) / E][(j + 1) % E]);
-        (scale[k] * fma(xh, c1, fma(dy, w[j / 2], c0))).get(dx[j], dx[j + 1]);
-      }
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        if ((v * lanes + t) * E < p.dim) {
-          Vec<T, E> o;
-          o.set(dx + v * E);
-          store_vec(out + v * lanes * E, o);
+        for (int v = 0; v < NV; ++v) {
+          if ((v * lanes + t) * E < p.dim) {
+            Vec<T, E> o;
+            o.set(dx + v * E);
+            store_vec(out + v * lanes * E, o);
+          }
         }
+        out += p.stride_x;
       }
-      out += p.stride_x;
+      left -= n[0];
+      if constexpr (kRing) {
+        n[0] = n[1];
+        n[1] = more;
+        at = at == 2 ? 0 : at + 1;
+      } else {
+        n[0] = more;
+      }
     }
-    r += n[0];
-    if (p.want_weights && r == group_end) {
+    if (p.want_weights) {
       float* mine = p.partial + (worker + g) * 2 * p.dim;
 #pragma unroll
       for (int j = 0; j < K; j += 2) {
         float a[2], c[2];
         dw[j / 2].get(a[0], a[1]);
         db[j / 2].get(c[0], c[1]);
-        dw[j / 2] = db[j / 2] = F2(0.0f);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int e = ((j + i) / E * lanes + t) * E;
@@ -491,13 +516,6 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
           }
         }
       }
-    }
-    if constexpr (kRing) {
-      n[0] = n[1];
-      n[1] = more;
-      at = at == 2 ? 0 : at + 1;
-    } else {
-      n[0] = more;
     }
   }
 }
