@@ -43,7 +43,8 @@ struct GemmCfg {
   static constexpr int kA = kTileRows * 128, kB = BN / 2 * 128;  // bytes a stage of one CTA
   static constexpr int kStage = kA + kB;
   static constexpr int kStages = 196608 / kStage > 8 ? 8 : 196608 / kStage;
-  static constexpr int kOffBars = kStages * kStage;
+  static constexpr int kOffOut = kStages * kStage;  // each epilogue warp's 32 rows x 64 columns on their way out
+  static constexpr int kOffBars = kOffOut + kEpilogueWarps * 4096;
   static constexpr int kBars = 2 * kStages + 4;
   static constexpr int kBytes = kOffBars + kBars * 8 + 16;
   static constexpr int kDynamic = kBytes + 1024;  // the tiles are aligned to 1024 bytes
@@ -75,6 +76,26 @@ __device__ __forceinline__ void activate_both(int kind, float x, float& a, float
   }
 }
 
+// A warp's 32 rows x 64 columns to global memory: staged in its own 4 KB (128-byte swizzle: a row's 16-byte pieces in
+// turned places, so that lanes do not meet in a bank) and stored as one TMA tile, which writes whole lines and leaves out
+// what lies beyond the tensor.  16-byte stores from the registers, a row each, cost a forward call of 37800 x 5120 x 13824
+// that keeps its projections 9305 us.
+__device__ __forceinline__ void write_out(const CUtensorMap* to, uint8_t* mine, const uint32_t (&words)[32], int lane,
+                                          int col, int row, int cols, int rows) {
+  if (lane == 0) ptx::tma_store_wait_read();
+  __syncwarp();
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    *reinterpret_cast<uint4*>(mine + lane * 128 + ((e ^ (lane & 7)) << 4)) =
+        make_uint4(words[4 * e], words[4 * e + 1], words[4 * e + 2], words[4 * e + 3]);
+  ptx::fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0 && col < cols && row < rows) {
+    ptx::tma_store_2d(to, mine, col, row);
+    ptx::tma_store_commit();
+  }
+}
+
 // Tiles go in bands of `band` row tiles, column by column inside a band, so that the tiles at work at one time share
 // both their rows of A and their columns of B in L2.
 __device__ __forceinline__ void tile_at(const GemmParams& p, int tile, int& m, int& n) {
@@ -88,7 +109,9 @@ __device__ __forceinline__ void tile_at(const GemmParams& p, int tile, int& m, i
 template <typename T, int kMode, int BN>
 __global__ void __launch_bounds__(kGemmThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1,
-                const __grid_constant__ CUtensorMap b0, const __grid_constant__ CUtensorMap b1, const GemmParams p) {
+                const __grid_constant__ CUtensorMap b0, const __grid_constant__ CUtensorMap b1,
+                const __grid_constant__ CUtensorMap o0, const __grid_constant__ CUtensorMap o1,
+                const __grid_constant__ CUtensorMap o2, const GemmParams p) {
   using namespace ptx;
   using C = GemmCfg<BN>;
   extern __shared__ uint8_t dynamic[];
@@ -230,6 +253,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   } else {
     // ---- results: warp w has the lanes of quarter w % 4, and one half of the columns ----
     const int quarter = warp & 3, side = warp >> 2;
+    uint8_t* mine = smem + C::kOffOut + warp * 4096;
     int acc = 0;
     uint32_t acc_round = 0;
     const uint32_t even0 = cluster_addr(acc_empty, 0), even1 = cluster_addr(acc_empty + 1, 0);
@@ -255,63 +279,53 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
                                                 __uint_as_float(r[4 * e + 2]), __uint_as_float(r[4 * e + 3]));
         }
       } else if constexpr (kMode == kForward) {
-        const int64_t row = (int64_t)m * 256 + in_tile;
-        const int64_t at = row * p.ld_out;
+        const int row = m * 256 + (int)rank * kTileRows + quarter * 32;
 #pragma unroll 1
-        for (int c = side * (BN / 4); c < (side + 1) * (BN / 4); c += 32) {
-          uint32_t g[32], u[32];
-          tmem_ld32(from + c, g);
-          tmem_ld32(from + BN / 2 + c, u);
-          tmem_ld_wait(g);
-          tmem_ld_wait(u);
-          const int col = n * (BN / 2) + c;
-          if (row < p.rows) {
+        for (int c = side * (BN / 4); c < (side + 1) * (BN / 4); c += 64) {
+          // h, then the projections as they are: the second and third read tensor memory again
+          const int outputs = p.keep[0] != nullptr ? 3 : 1;
+#pragma unroll 1
+          for (int o = 0; o < outputs; ++o) {
+            uint32_t words[32];  // 64 columns of this thread's row
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (col + 8 * e >= p.cols) continue;
-              uint4 h, kg, ku;
-              uint32_t* hw = &h.x;
-              uint32_t* gw = &kg.x;
-              uint32_t* uw = &ku.x;
+            for (int half = 0; half < 2; ++half) {
+              uint32_t x[32];
+              tmem_ld32(from + (o == 2 ? BN / 2 : 0) + c + half * 32, x);
+              if (o == 0) {
+                uint32_t u[32];
+                tmem_ld32(from + BN / 2 + c + half * 32, u);
+                tmem_ld_wait(x);
+                tmem_ld_wait(u);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                const float ga = __uint_as_float(g[8 * e + 2 * i]), gb = __uint_as_float(g[8 * e + 2 * i + 1]);
-                const float ua = __uint_as_float(u[8 * e + 2 * i]), ub = __uint_as_float(u[8 * e + 2 * i + 1]);
-                hw[i] = pack2<T>(activate(p.activation, ga) * ua, activate(p.activation, gb) * ub);
-                gw[i] = pack2<T>(ga, gb);
-                uw[i] = pack2<T>(ua, ub);
+                for (int i = 0; i < 32; ++i)
+                  x[i] = __float_as_uint(activate(p.activation, __uint_as_float(x[i])) * __uint_as_float(u[i]));
+              } else {
+                tmem_ld_wait(x);
               }
-              *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.out[0]) + at + col + 8 * e) = h;
-              if (p.keep[0] != nullptr) {
-                *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.keep[0]) + at + col + 8 * e) = kg;
-                *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.keep[1]) + at + col + 8 * e) = ku;
-              }
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                words[half * 16 + i] = pack2<T>(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
             }
+            write_out(o == 0 ? &o0 : o == 1 ? &o1 : &o2, mine, words, lane, n * (BN / 2) + c, row, p.cols, p.rows);
           }
         }
       } else {
         const int half_m = p.m_tiles / 2;
         const bool second = kMode == kWeights && m >= half_m;
-        const int64_t row = (int64_t)(second ? m - half_m : m) * 256 + in_tile;
-        T* to = reinterpret_cast<T*>(second ? p.out[1] : p.out[0]) + row * p.ld_out;
+        const int row = (second ? m - half_m : m) * 256 + (int)rank * kTileRows + quarter * 32;
 #pragma unroll 1
-        for (int c = side * (BN / 2); c < (side + 1) * (BN / 2); c += 32) {
-          uint32_t r[32];
-          tmem_ld32(from + c, r);
-          tmem_ld_wait(r);
-          const int col = n * BN + c;
-          if (row < p.rows) {
+        for (int c = side * (BN / 2); c < (side + 1) * (BN / 2); c += 64) {
+          uint32_t words[32];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              if (col + 8 * e >= p.cols) continue;
-              uint4 o;
-              uint32_t* w = &o.x;
+          for (int half = 0; half < 2; ++half) {
+            uint32_t x[32];
+            tmem_ld32(from + c + half * 32, x);
+            tmem_ld_wait(x);
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                w[i] = pack2<T>(__uint_as_float(r[8 * e + 2 * i]), __uint_as_float(r[8 * e + 2 * i + 1]));
-              *reinterpret_cast<uint4*>(to + col + 8 * e) = o;
-            }
+            for (int i = 0; i < 16; ++i)
+              words[half * 16 + i] = pack2<T>(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
           }
+          write_out(second ? &o1 : &o0, mine, words, lane, n * BN + c, row, p.cols, p.rows);
         }
       }
       tc_fence_before();
@@ -320,6 +334,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
       acc ^= 1;
       if (acc == 0) acc_round ^= 1u;
     }
+    if (lane == 0) tma_store_wait();
   }
   __syncwarp();
   tc_fence_before();
@@ -435,7 +450,7 @@ static int make_map(CUtensorMap* out, int dtype, const void* base, int64_t rows,
 }
 
 template <typename T, int kMode, int BN>
-static int launch_gemm_t(GemmParams p, const CUtensorMap (&map)[4], int dtype, char* ws, cudaStream_t st) {
+static int launch_gemm_t(GemmParams p, const CUtensorMap (&map)[7], int dtype, char* ws, cudaStream_t st) {
   using C = GemmCfg<BN>;
   if ((int64_t)p.m_tiles * p.n_tiles > (1 << 30)) {
     set_error("%d x %d tiles are too many", p.m_tiles, p.n_tiles);
@@ -455,7 +470,8 @@ static int launch_gemm_t(GemmParams p, const CUtensorMap (&map)[4], int dtype, c
   auto kern = gemm_kernel<T, kMode, BN>;
   SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, C::kDynamic));
   const unsigned grid = 2u * (unsigned)std::min(p.units, kPairs);
-  SPARSP_CUDA_OK(launch_clusters(kern, dim3(grid), 2, kGemmThreads, C::kDynamic, st, map[0], map[1], map[2], map[3], p));
+  SPARSP_CUDA_OK(launch_clusters(kern, dim3(grid), 2, kGemmThreads, C::kDynamic, st, map[0], map[1], map[2], map[3], map[4],
+                                 map[5], map[6], p));
   if (p.splits > 1) {
     constexpr int kCols = kMode == kForward ? BN / 2 : BN;
     SPARSP_CUDA_OK(launch_kernel(gemm_join_kernel<T, kMode, BN>, dim3((unsigned)(tiles * (kCols / 8))), 256, 0, st, p));
@@ -464,7 +480,7 @@ static int launch_gemm_t(GemmParams p, const CUtensorMap (&map)[4], int dtype, c
 }
 
 template <int kMode, int BN>
-static int launch_gemm(const GemmParams& p, const CUtensorMap (&map)[4], int dtype, char* ws, cudaStream_t st) {
+static int launch_gemm(const GemmParams& p, const CUtensorMap (&map)[7], int dtype, char* ws, cudaStream_t st) {
   return dtype == SPARSP_BF16 ? launch_gemm_t<__nv_bfloat16, kMode, BN>(p, map, dtype, ws, st)
                               : launch_gemm_t<__half, kMode, BN>(p, map, dtype, ws, st);
 }
@@ -480,12 +496,18 @@ static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 int launch_ffn_fwd(const sparsp_ffn& f, const void* X, const void* Wg, const void* Wu, void* H, void* gate, void* up,
                    char* ws, cudaStream_t st) {
   constexpr int BN = 256;
-  CUtensorMap map[4];
+  CUtensorMap map[7];
   int rc;
   if ((rc = make_map(map + 0, f.dtype, X, f.tokens, f.dim, f.stride_x, kTileRows)) != SPARSP_OK) return rc;
   if ((rc = make_map(map + 2, f.dtype, Wg, f.hidden, f.dim, f.stride_w, BN / 2)) != SPARSP_OK) return rc;
   if ((rc = make_map(map + 3, f.dtype, Wu, f.hidden, f.dim, f.stride_w, BN / 2)) != SPARSP_OK) return rc;
   map[1] = map[0];
+  if ((rc = make_map(map + 4, f.dtype, H, f.tokens, f.hidden, f.stride_h, 32)) != SPARSP_OK) return rc;
+  map[5] = map[6] = map[4];
+  if (gate != nullptr) {
+    if ((rc = make_map(map + 5, f.dtype, gate, f.tokens, f.hidden, f.stride_h, 32)) != SPARSP_OK) return rc;
+    if ((rc = make_map(map + 6, f.dtype, up, f.tokens, f.hidden, f.stride_h, 32)) != SPARSP_OK) return rc;
+  }
   GemmParams p = {};
   p.out[0] = H;
   p.keep[0] = gate;
@@ -526,13 +548,15 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
     SPARSP_CUDA_OK(launch_kernel(gate_grad_kernel<__half>, grid, 256, 0, st, (const __half*)dH, (const __half*)gate,
                                  (const __half*)up, (__half*)dg, (__half*)du, f.stride_h, f.hidden, total,
                                  f.activation));
-  CUtensorMap map[4];
+  CUtensorMap map[7];
   int rc;
   if (dX != nullptr) {
     if ((rc = make_map(map + 0, f.dtype, dg, f.tokens, f.hidden, f.hidden, kTileRows)) != SPARSP_OK) return rc;
     if ((rc = make_map(map + 1, f.dtype, du, f.tokens, f.hidden, f.hidden, kTileRows)) != SPARSP_OK) return rc;
     if ((rc = make_map(map + 2, f.dtype, Wg, f.hidden, f.dim, f.stride_w, kStageK)) != SPARSP_OK) return rc;
     if ((rc = make_map(map + 3, f.dtype, Wu, f.hidden, f.dim, f.stride_w, kStageK)) != SPARSP_OK) return rc;
+    if ((rc = make_map(map + 4, f.dtype, dX, f.tokens, f.dim, f.stride_x, 32)) != SPARSP_OK) return rc;
+    map[5] = map[6] = map[4];
     GemmParams p = {};
     p.out[0] = dX;
     p.ld_out = f.stride_x;
@@ -548,6 +572,9 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
     if ((rc = make_map(map + 1, f.dtype, du, f.tokens, f.hidden, f.hidden, kStageK)) != SPARSP_OK) return rc;
     if ((rc = make_map(map + 2, f.dtype, X, f.tokens, f.dim, f.stride_x, kStageK)) != SPARSP_OK) return rc;
     map[3] = map[2];
+    if ((rc = make_map(map + 4, f.dtype, dWg, f.hidden, f.dim, f.stride_w, 32)) != SPARSP_OK) return rc;
+    if ((rc = make_map(map + 5, f.dtype, dWu, f.hidden, f.dim, f.stride_w, 32)) != SPARSP_OK) return rc;
+    map[6] = map[4];
     GemmParams p = {};
     p.out[0] = dWg;
     p.out[1] = dWu;
