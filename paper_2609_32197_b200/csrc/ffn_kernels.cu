@@ -347,6 +347,186 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   if (threadIdx.x == 0) report_abort(s_abort, p.status);
 }
 
+// ---- few tokens -----------------------------------------------------------------------------------------------------
+//
+// With a handful of tokens the call is one pass over the weights, and a 256-row tile of tokens would be all padding.  Here
+// the weights are the rows of the tile and the tokens its columns: D = [Wg; Wu] X^T, 2 F rows (F features of gate, then the
+// same of up) by N columns (the tokens, rounded up to 16).  A CTA has F features at a time, F as small as shares the hidden
+// size out evenly; the MMA takes 128 rows all the same, and those past 2 F are whatever lies behind in shared memory and
+// are never read.  Gate and up of a feature are in different lanes, so they meet in shared memory, where the order turns
+// to tokens by features for the store.
+struct FewParams {
+  void* out;
+  void* keep[2];
+  int64_t ld_out;
+  int32_t tokens, hidden;
+  int32_t features, columns;  // of a tile: F, N
+  int32_t tiles, k_blocks, stages, stage_bytes, ld_turn;
+  int32_t activation;
+  uint32_t idesc;
+  int32_t* status;
+  long long wait_limit;
+};
+
+constexpr int kFewThreads = 192;  // loads, products, four warps of results
+constexpr int kFewTokens = 128;
+constexpr int kFewSmem = 224 * 1024;
+
+template <typename T>
+__global__ void __launch_bounds__(kFewThreads, 1)
+    few_kernel(const __grid_constant__ CUtensorMap mg, const __grid_constant__ CUtensorMap mu,
+               const __grid_constant__ CUtensorMap mx, const FewParams p) {
+  using namespace ptx;
+  extern __shared__ uint8_t dynamic[];
+  uint8_t* smem = dynamic + ((1024 - (smem_u32(dynamic) & 1023)) & 1023);
+  __shared__ uint64_t full[16], empty[16], acc_full[2], acc_empty[2];
+  __shared__ uint32_t tmem_slot;
+  __shared__ int abort_word;
+  volatile int* s_abort = &abort_word;
+  // behind the stages: room for the last stage's rows past 2 F, then the results on their turn
+  float* turn = reinterpret_cast<float*>(smem + p.stages * p.stage_bytes + 16384);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) {
+      mbar_init(full + s, 1);
+      mbar_init(empty + s, 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(acc_full + a, 1);
+      mbar_init(acc_empty + a, 4);
+    }
+    *s_abort = 0;
+    mbar_init_fence();
+  }
+  if (warp == 1) {
+    tmem_alloc(&tmem_slot, 256);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = tmem_slot;
+  wait_previous_grids();
+  const int F = p.features, N = p.columns;
+
+  if (warp == 0) {
+    if (elect_one()) {
+      int s = 0;
+      uint32_t round = 0;
+      for (int tile = blockIdx.x; tile < p.tiles && !*s_abort; tile += gridDim.x) {
+        for (int k = 0; k < p.k_blocks; ++k) {
+          mbar_wait_bounded_inline(empty + s, round ^ 1u, s_abort, 11, p.wait_limit);
+          if (*s_abort) break;
+          uint8_t* at = smem + s * p.stage_bytes;
+          mbar_expect_tx(full + s, (2 * F + N) * 128);
+          tma_load_2d(at, &mg, full + s, k * kStageK, tile * F);
+          tma_load_2d(at + F * 128, &mu, full + s, k * kStageK, tile * F);
+          tma_load_2d(at + 2 * F * 128, &mx, full + s, k * kStageK, 0);
+          if (++s == p.stages) {
+            s = 0;
+            round ^= 1u;
+          }
+        }
+      }
+      if (*s_abort) {  // copies still in flight are waited for, within the same limit
+        const long long t0 = clock64();
+        for (int q = 0; q < p.stages; ++q) {
+          const uint32_t phase = q < s ? round : round ^ 1u;
+          while (!mbar_try_wait(full + q, phase) && clock64() - t0 < p.wait_limit) {
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (elect_one()) {
+      const uint64_t da = make_smem_desc(smem_u32(smem), 16u, 1024u);
+      const uint64_t db = make_smem_desc(smem_u32(smem) + 2 * F * 128, 16u, 1024u);
+      int s = 0, acc = 0;
+      uint32_t round = 0, acc_round = 0;
+      for (int tile = blockIdx.x; tile < p.tiles && !*s_abort; tile += gridDim.x) {
+        mbar_wait_bounded_inline(acc_empty + acc, acc_round ^ 1u, s_abort, 12, p.wait_limit);
+        tc_fence_after();
+        for (int k = 0; k < p.k_blocks; ++k) {
+          mbar_wait_bounded_inline(full + s, round, s_abort, 13, p.wait_limit);
+          tc_fence_after();
+          const uint64_t off = (uint64_t)((s * p.stage_bytes) >> 4);
+#pragma unroll
+          for (int kk = 0; kk < kStageK / 16; ++kk)
+            mma_ss(tmem + acc * kFewTokens, da + off + kk * 2, db + off + kk * 2, p.idesc, k > 0 || kk > 0);
+          mma_commit(empty + s);
+          if (++s == p.stages) {
+            s = 0;
+            round ^= 1u;
+          }
+        }
+        mma_commit(acc_full + acc);
+        acc ^= 1;
+        if (acc == 0) acc_round ^= 1u;
+      }
+    }
+  } else {
+    const int quarter = warp & 3, in_tile = quarter * 32 + lane;
+    const int ld = p.ld_turn;  // of `turn`, a row for each lane: odd, so that its columns do not meet in a bank
+    int acc = 0;
+    uint32_t acc_round = 0;
+    for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
+      mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 14, p.wait_limit);
+      if (*s_abort) break;
+      tc_fence_after();
+      if (quarter * 32 < 2 * F) {
+        for (int c = 0; c < N; c += 16) {
+          uint32_t r[16];
+          tmem_ld16(tmem + acc * kFewTokens + c + ((uint32_t)(quarter * 32) << 16), r);
+          tmem_ld_wait(r);
+          if (in_tile < 2 * F) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) turn[in_tile * ld + c + i] = __uint_as_float(r[i]);
+          }
+        }
+      }
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive(acc_empty + acc);
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      // eight features of a token a thread
+      const int per_row = F / 8;
+      for (int i = threadIdx.x - 64; i < p.tokens * per_row; i += 128) {
+        const int token = i / per_row, f = (i - token * per_row) * 8, col = tile * F + f;
+        if (col >= p.hidden) continue;
+        float g[8], u[8], h[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          g[e] = turn[(f + e) * ld + token];
+          u[e] = turn[(F + f + e) * ld + token];
+          h[e] = activate(p.activation, g[e]) * u[e];
+        }
+        const int64_t at = token * p.ld_out + col;
+        Vec<T, 8> v;
+        v.set(h);
+        store_vec(reinterpret_cast<T*>(p.out) + at, v);
+        if (p.keep[0] != nullptr) {
+          v.set(g);
+          store_vec(reinterpret_cast<T*>(p.keep[0]) + at, v);
+          v.set(u);
+          store_vec(reinterpret_cast<T*>(p.keep[1]) + at, v);
+        }
+      }
+      asm volatile("bar.sync 1, 128;" ::: "memory");
+      acc ^= 1;
+      if (acc == 0) acc_round ^= 1u;
+    }
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 256);
+  }
+  if (threadIdx.x == 0) report_abort(s_abort, p.status);
+}
+
 // Adds the splits of every tile and finishes it as gemm_kernel would have.  A thread has one row and eight columns (for
 // the forward call of both projections).
 template <typename T, int kMode, int BN>
@@ -442,7 +622,16 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(uint16_t* a, uint16_t* b
 // ---- host side ------------------------------------------------------------------------------------------------------
 
 constexpr int kPairs = kSms / 2;
+constexpr long long kWaitLimit = 200000000LL;  // of a wait in a kernel: about 0.1 s of SM clocks
 constexpr int64_t kPartialBytes = (int64_t)kPairs * 256 * 256 * 4;
+
+static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+// Instruction descriptor: bits 7 and 10 say that A and B are bf16, not fp16.
+static uint32_t instruction(int dtype, int M, int N, int a_mn_major, int b_mn_major) {
+  const uint32_t d = ptx::make_idesc_bf16(M, N, a_mn_major, b_mn_major);
+  return dtype == SPARSP_BF16 ? d : d & ~((1u << 7) | (1u << 10));
+}
 
 // [rows][cols] of 16-bit elements in boxes of 64 columns x box_rows rows, 128-byte swizzle
 static int make_map(CUtensorMap* out, int dtype, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
@@ -463,10 +652,9 @@ static int launch_gemm_t(GemmParams p, const CUtensorMap (&map)[7], int dtype, c
   p.band = 8;
   p.partial = reinterpret_cast<float*>(ws + kStatusWords * 4);
   p.status = reinterpret_cast<int32_t*>(ws);
-  p.wait_limit = 200000000LL;  // about 0.1 s of SM clocks
+  p.wait_limit = kWaitLimit;
   constexpr int a_mn = kMode == kWeights, b_mn = kMode != kForward;
-  p.idesc = ptx::make_idesc_bf16(256, BN, a_mn, b_mn);
-  if (dtype == SPARSP_FP16) p.idesc &= ~((1u << 7) | (1u << 10));
+  p.idesc = instruction(dtype, 256, BN, a_mn, b_mn);
   auto kern = gemm_kernel<T, kMode, BN>;
   SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, C::kDynamic));
   const unsigned grid = 2u * (unsigned)std::min(p.units, kPairs);
@@ -491,10 +679,46 @@ int64_t ffn_workspace_bytes(const sparsp_ffn& f, bool backward) {
   return kStatusWords * 4 + kPartialBytes + (backward ? 2 * hidden_bytes(f) : 0);
 }
 
-static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+static int launch_few(const sparsp_ffn& f, const void* X, const void* Wg, const void* Wu, void* H, void* gate,
+                      void* up, char* ws, cudaStream_t st) {
+  FewParams p = {};
+  p.columns = (int32_t)align_up(f.tokens, 16);
+  // features at a time: as few rounds of all SMs as can be, measured in features; larger tiles where it is the same
+  p.features = 64;
+  for (int F = 32; F >= 16; F /= 2)
+    if ((int64_t)ceil_div(ceil_div(f.hidden, F), kSms) * F < (int64_t)ceil_div(ceil_div(f.hidden, p.features), kSms) * p.features)
+      p.features = F;
+  p.tiles = ceil_div(f.hidden, p.features);
+  p.k_blocks = ceil_div(f.dim, kStageK);
+  p.stage_bytes = (2 * p.features + p.columns) * 128;
+  p.ld_turn = p.columns + 1;
+  const int turn = (int)align_up(2 * p.features * p.ld_turn * 4, 128);
+  p.stages = std::min(16, (kFewSmem - 16384 - turn - 1024) / p.stage_bytes);
+  p.out = H;
+  p.keep[0] = gate;
+  p.keep[1] = up;
+  p.ld_out = f.stride_h;
+  p.tokens = (int32_t)f.tokens;
+  p.hidden = f.hidden;
+  p.activation = f.activation;
+  p.idesc = instruction(f.dtype, 128, p.columns, 0, 0);
+  p.status = reinterpret_cast<int32_t*>(ws);
+  p.wait_limit = kWaitLimit;
+  CUtensorMap mg, mu, mx;
+  int rc;
+  if ((rc = make_map(&mg, f.dtype, Wg, f.hidden, f.dim, f.stride_w, p.features)) != SPARSP_OK) return rc;
+  if ((rc = make_map(&mu, f.dtype, Wu, f.hidden, f.dim, f.stride_w, p.features)) != SPARSP_OK) return rc;
+  if ((rc = make_map(&mx, f.dtype, X, f.tokens, f.dim, f.stride_x, p.columns)) != SPARSP_OK) return rc;
+  auto kern = f.dtype == SPARSP_BF16 ? few_kernel<__nv_bfloat16> : few_kernel<__half>;
+  const int smem = p.stages * p.stage_bytes + 16384 + turn + 1024;
+  SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, smem));
+  SPARSP_CUDA_OK(launch_kernel(kern, dim3((unsigned)std::min(p.tiles, kSms)), kFewThreads, smem, st, mg, mu, mx, p));
+  return SPARSP_OK;
+}
 
 int launch_ffn_fwd(const sparsp_ffn& f, const void* X, const void* Wg, const void* Wu, void* H, void* gate, void* up,
                    char* ws, cudaStream_t st) {
+  if (f.tokens <= kFewTokens) return launch_few(f, X, Wg, Wu, H, gate, up, ws, st);
   constexpr int BN = 256;
   CUtensorMap map[7];
   int rc;
