@@ -372,7 +372,7 @@ constexpr int kFewThreads = 192;  // loads, products, four warps of results
 constexpr int kFewTokens = 128;
 constexpr int kFewSmem = 224 * 1024;
 
-template <typename T>
+template <typename T, int kDeep>
 __global__ void __launch_bounds__(kFewThreads, 1)
     few_kernel(const __grid_constant__ CUtensorMap mg, const __grid_constant__ CUtensorMap mu,
                const __grid_constant__ CUtensorMap mx, const FewParams p) {
@@ -414,15 +414,25 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     if (elect_one()) {
       int s = 0;
       uint32_t round = 0;
+      const int block = (2 * F + N) * 128;
       for (int tile = blockIdx.x; tile < p.tiles && !*s_abort; tile += gridDim.x) {
-        for (int k = 0; k < p.k_blocks; ++k) {
-          mbar_wait_bounded_inline(empty + s, round ^ 1u, s_abort, 11, p.wait_limit);
-          if (*s_abort) break;
+        for (int k = 0; k < p.k_blocks; k += kDeep) {
+          if (!mbar_try_wait(empty + s, round ^ 1u)) {
+            mbar_wait_bounded_inline(empty + s, round ^ 1u, s_abort, 11, p.wait_limit);
+            if (*s_abort) break;
+          }
           uint8_t* at = smem + s * p.stage_bytes;
-          mbar_expect_tx(full + s, (2 * F + N) * 128);
-          tma_load_2d(at, &mg, full + s, k * kStageK, tile * F);
-          tma_load_2d(at + F * 128, &mu, full + s, k * kStageK, tile * F);
-          tma_load_2d(at + 2 * F * 128, &mx, full + s, k * kStageK, 0);
+          const int n = min(kDeep, p.k_blocks - k);
+          mbar_expect_tx(full + s, n * block);
+#pragma unroll
+          for (int q = 0; q < kDeep; ++q)
+            if (q < n) tma_load_2d(at + q * block, &mg, full + s, (k + q) * kStageK, tile * F);
+#pragma unroll
+          for (int q = 0; q < kDeep; ++q)
+            if (q < n) tma_load_2d(at + q * block + F * 128, &mu, full + s, (k + q) * kStageK, tile * F);
+#pragma unroll
+          for (int q = 0; q < kDeep; ++q)
+            if (q < n) tma_load_2d(at + q * block + 2 * F * 128, &mx, full + s, (k + q) * kStageK, 0);
           if (++s == p.stages) {
             s = 0;
             round ^= 1u;
@@ -442,18 +452,24 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     if (elect_one()) {
       const uint64_t da = make_smem_desc(smem_u32(smem), 16u, 1024u);
       const uint64_t db = make_smem_desc(smem_u32(smem) + 2 * F * 128, 16u, 1024u);
+      const int block = (2 * F + N) * 128;
       int s = 0, acc = 0;
       uint32_t round = 0, acc_round = 0;
       for (int tile = blockIdx.x; tile < p.tiles && !*s_abort; tile += gridDim.x) {
         mbar_wait_bounded_inline(acc_empty + acc, acc_round ^ 1u, s_abort, 12, p.wait_limit);
         tc_fence_after();
-        for (int k = 0; k < p.k_blocks; ++k) {
+        for (int k = 0; k < p.k_blocks; k += kDeep) {
           mbar_wait_bounded_inline(full + s, round, s_abort, 13, p.wait_limit);
           tc_fence_after();
           const uint64_t off = (uint64_t)((s * p.stage_bytes) >> 4);
 #pragma unroll
-          for (int kk = 0; kk < kStageK / 16; ++kk)
-            mma_ss(tmem + acc * kFewTokens, da + off + kk * 2, db + off + kk * 2, p.idesc, k > 0 || kk > 0);
+          for (int q = 0; q < kDeep; ++q)
+            if (q < p.k_blocks - k) {
+#pragma unroll
+              for (int kk = 0; kk < kStageK / 16; ++kk)
+                mma_ss(tmem + acc * kFewTokens, da + off + (q * block >> 4) + kk * 2, db + off + (q * block >> 4) + kk * 2,
+                       p.idesc, k + q > 0 || kk > 0);
+            }
           mma_commit(empty + s);
           if (++s == p.stages) {
             s = 0;
@@ -683,17 +699,20 @@ static int launch_few(const sparsp_ffn& f, const void* X, const void* Wg, const 
                       void* up, char* ws, cudaStream_t st) {
   FewParams p = {};
   p.columns = (int32_t)align_up(f.tokens, 16);
-  // features at a time: as few rounds of all SMs as can be, measured in features; larger tiles where it is the same
+  // features at a time: what a round of all SMs loads, 2 F rows of weights and N of tokens a CTA, times the rounds
+  auto cost = [&](int F) { return (int64_t)ceil_div(ceil_div(f.hidden, F), kSms) * (2 * F + p.columns); };
   p.features = 64;
   for (int F = 32; F >= 16; F /= 2)
-    if ((int64_t)ceil_div(ceil_div(f.hidden, F), kSms) * F < (int64_t)ceil_div(ceil_div(f.hidden, p.features), kSms) * p.features)
-      p.features = F;
+    if (cost(F) < cost(p.features)) p.features = F;
   p.tiles = ceil_div(f.hidden, p.features);
   p.k_blocks = ceil_div(f.dim, kStageK);
-  p.stage_bytes = (2 * p.features + p.columns) * 128;
   p.ld_turn = p.columns + 1;
-  const int turn = (int)align_up(2 * p.features * p.ld_turn * 4, 128);
-  p.stages = std::min(16, (kFewSmem - 16384 - turn - 1024) / p.stage_bytes);
+  const int turn = (int)align_up(2 * p.features * p.ld_turn * 4, 128), room = kFewSmem - 16384 - turn - 1024;
+  const int block = (2 * p.features + p.columns) * 128;
+  int deep = 4;  // blocks of K a stage, as many as leave four stages
+  while (deep > 1 && room / (deep * block) < 4) deep /= 2;
+  p.stage_bytes = deep * block;
+  p.stages = std::min(16, room / p.stage_bytes);
   p.out = H;
   p.keep[0] = gate;
   p.keep[1] = up;
@@ -709,7 +728,10 @@ static int launch_few(const sparsp_ffn& f, const void* X, const void* Wg, const 
   if ((rc = make_map(&mg, f.dtype, Wg, f.hidden, f.dim, f.stride_w, p.features)) != SPARSP_OK) return rc;
   if ((rc = make_map(&mu, f.dtype, Wu, f.hidden, f.dim, f.stride_w, p.features)) != SPARSP_OK) return rc;
   if ((rc = make_map(&mx, f.dtype, X, f.tokens, f.dim, f.stride_x, p.columns)) != SPARSP_OK) return rc;
-  auto kern = f.dtype == SPARSP_BF16 ? few_kernel<__nv_bfloat16> : few_kernel<__half>;
+  const bool bf = f.dtype == SPARSP_BF16;
+  auto kern = deep == 4   ? (bf ? few_kernel<__nv_bfloat16, 4> : few_kernel<__half, 4>)
+              : deep == 2 ? (bf ? few_kernel<__nv_bfloat16, 2> : few_kernel<__half, 2>)
+                          : (bf ? few_kernel<__nv_bfloat16, 1> : few_kernel<__half, 1>);
   const int smem = p.stages * p.stage_bytes + 16384 + turn + 1024;
   SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, smem));
   SPARSP_CUDA_OK(launch_kernel(kern, dim3((unsigned)std::min(p.tiles, kSms)), kFewThreads, smem, st, mg, mu, mx, p));
