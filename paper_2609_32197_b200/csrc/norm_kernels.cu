@@ -5,12 +5,17 @@
 
 namespace sparsp {
 
-// Rows are worked on by "workers": a warp each where a row is at most 512 values, otherwise a CTA.  Worker i of n has the
-// consecutive rows [i rows / n, (i + 1) rows / n) and holds the weights of the group it is in, so that they are read once
-// per worker, not once per row.  It takes R rows at a time, which share each barrier; their values stay in registers from
-// there to the store.  The 2R rows after them are on their way into shared memory: each thread copies the values that it
-// will itself use (cp.async), so nobody waits for anybody else's copies.  There are as many workers as fit the
-// multiprocessors by their registers and their shared memory, so none waits for another to end.
+// Rows are worked on by "workers": a warp each where a row is at most 512 values, otherwise a CTA.  A worker has consecutive
+// rows and holds the weights of the group it is in, so that they are read once per worker, not once per row.  It takes R
+// rows at a time, which share each barrier; their values stay in registers from there to the store.  The 2R rows after
+// them are on their way into shared memory: each thread copies the 16-byte pieces that it will itself use (cp.async), so
+// nobody waits for anybody else's copies.  There are as many workers as fit the multiprocessors by their registers and
+// their shared memory, so none waits for another to end.
+//
+// Rows of any length are read in 16-byte pieces.  Where a row is not a multiple of 16 bytes, every second, fourth or
+// eighth row begins at the same place inside its first piece: these make a class, and a worker has rows of one class
+// only, every P-th of its part, so that a thread's columns, and with them its weights and sums, do not change from row to
+// row.  (Value by value, backward over 15554 x 1921 fp32 took 153 us, with single 4-byte copies 111.)
 constexpr int kNormThreads = 256;  // of a CTA whose warps are workers
 constexpr int kAhead = 3;          // batches of R rows in shared memory: one in use, two on their way
 
@@ -26,6 +31,15 @@ __host__ __device__ constexpr int worker_registers(int kind) { return kind == kT
 // sums.
 __host__ __device__ constexpr int worker_rows(int kind, bool bwd) { return kind == kWarp8 ? (bwd ? 2 : 4) : kind == kLongestTeam || bwd ? 1 : 2; }
 
+// How a worker meets its rows.
+//   kPlain    every row begins on 16 bytes and is a multiple of them
+//   kShifted  rows in classes, pieces that a row shares with its neighbours
+//   kSingle   value by value: tensors that do not begin on 16 bytes or whose rows move against one another, and rows that
+//             shared memory does not hold
+// Plain rows have a form of their own because they leave the backward pass of 75600 x 5120 bf16 the registers that it
+// needs: 446 us in the other one.
+enum Form { kPlain, kShifted, kSingle };
+
 struct NormParams {
   const void* x;
   const void* dy;
@@ -38,30 +52,58 @@ struct NormParams {
   float* rstd;
   float* partial;  // backward: [slots][2][dim]
   int64_t rows, rows_per_group, stride_x, stride_y;
-  int32_t dim, weights_fp32, n_workers, want_weights;
-  int32_t ring_bytes;  // of a worker
+  int32_t dim, weights_fp32, want_weights;
+  int32_t parts, log_classes;  // workers: parts << log_classes
+  int32_t ring_bytes, ring_half;  // of a worker; where dy's begins
   float eps, inv_dim;
 };
 
-__host__ __device__ inline int64_t first_row(int64_t worker, int64_t n_workers, int64_t rows) {
-  return worker * (rows / n_workers) + (worker < rows % n_workers ? worker : rows % n_workers);
+__host__ __device__ inline int64_t first_row(int64_t part, int64_t parts, int64_t rows) {
+  return part * (rows / parts) + (part < rows % parts ? part : rows % parts);
 }
 
-template <typename T, int E>
-__device__ __forceinline__ void load_weights(const void* w, int64_t at, bool fp32, float missing, float (&out)[E]) {
-  if (w == nullptr) {
-#pragma unroll
-    for (int i = 0; i < E; ++i) out[i] = missing;
-  } else if (fp32) {
-    const float* p = reinterpret_cast<const float*>(w) + at;
-#pragma unroll
-    for (int i = 0; i < E; ++i) out[i] = p[i];
-  } else {
-    const T* p = reinterpret_cast<const T*>(w) + at;
-#pragma unroll
-    for (int i = 0; i < E; ++i) out[i] = to_float<T>(p[i]);
+// The rows of a worker: those of its class in its part.
+template <bool kClasses>
+struct Mine {
+  int64_t lo, hi, per_group;
+  int part, cls, log_of;
+  __device__ __forceinline__ Mine(const NormParams& p, int worker)
+      : per_group(p.rows_per_group), part(kClasses ? worker >> p.log_classes : worker),
+        cls(kClasses ? worker & ((1 << p.log_classes) - 1) : 0), log_of(kClasses ? p.log_classes : 0) {
+    lo = first_row(part, p.parts, p.rows);
+    hi = first_row(part + 1, p.parts, p.rows);
   }
-}
+  __device__ __forceinline__ int log_classes() const { return kClasses ? log_of : 0; }
+  // rows of the class below x; the class row with i such rows below it
+  __device__ __forceinline__ int64_t below(int64_t x) const {
+    return kClasses ? (x - cls + (1 << log_of) - 1) >> log_of : x;
+  }
+  __device__ __forceinline__ int64_t row(int64_t i) const { return kClasses ? cls + (i << log_of) : i; }
+};
+
+// ... in batches: at most R rows at a time, and none across two groups of weights.
+template <typename M>
+struct Batches {
+  int64_t end;  // of the group's rows
+  int left;     // of the group, yet to be fetched
+  __device__ __forceinline__ Batches(const M& m) {
+    end = min(m.hi, (m.lo / m.per_group + 1) * m.per_group);
+    left = (int)(m.below(end) - m.below(m.lo));
+    skip(m);
+  }
+  __device__ __forceinline__ void skip(const M& m) {
+    while (left == 0 && end < m.hi) {
+      const int64_t from = end;
+      end = min(m.hi, end + m.per_group);
+      left = (int)(m.below(end) - m.below(from));
+    }
+  }
+  __device__ __forceinline__ int size(int R) const { return min(R, left); }
+  __device__ __forceinline__ void take(const M& m, int n) {
+    left -= n;
+    if (left == 0) skip(m);
+  }
+};
 
 // Sums N values over the worker's threads, in an order that depends on its size alone; every thread gets the sums.
 // Inside a warp the values are halved with the lanes (after log2 N exchanges a lane carries one of them), so that N sums
@@ -136,170 +178,190 @@ __device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
   return r;
 }
 
-// The rows ahead of a worker, of one tensor.  kRing: through shared memory as above; otherwise (single 16-bit values,
-// rows too long for shared memory) the next R rows through registers.
-template <typename T, int E, int NV, int R, bool kRing>
+// The rows ahead of a worker, of one tensor: in shared memory as above, or (kSingle) the next R rows in registers.
+template <typename T, int kForm, int NV, int R>
 struct RowsAhead {
-  Vec<T, E> next[kRing ? 1 : R][kRing ? 1 : NV];
-  const T* from;  // this thread's first value of the next row to be fetched
+  static constexpr int E = kForm == kSingle ? 1 : 16 / sizeof(T);
+  Vec<T, E> next[E > 1 ? 1 : R][E > 1 ? 1 : NV];
+  const T* from;  // this thread's first piece of the next row to be fetched
   int64_t stride;
-  char* ring;  // this thread's places, `lanes` vectors from one to the next
-  int lanes, t, dim;
+  char* ring;  // this thread's places, `lanes` pieces from one to the next
+  int lanes, t, dim, shift;
 
-  __device__ __forceinline__ void fetch(int n, int batch) {
-#pragma unroll
-    for (int k = 0; k < R; ++k) {
-      if (k >= n) break;
-#pragma unroll
-      for (int v = 0; v < NV; ++v) {
-        if ((v * lanes + t) * E < dim) {
-          const T* at = from + v * lanes * E;
-          if constexpr (kRing) {
-            char* to = place(batch * R + k, v);
-            if constexpr (E * sizeof(T) == 16)
-              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                           "l"(at)
-                           : "memory");
-            else
-              asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"((uint32_t)__cvta_generic_to_shared(to)),
-                           "l"(at)
-                           : "memory");
-          } else {
-            next[k][v] = load_once<T, E>(at);
-          }
-        }
-      }
-      from += stride;
-    }
-  }
-  // Makes what lies beyond the row zero, once: nothing is ever fetched to there.
-  __device__ __forceinline__ void clear_beyond() {
+  __device__ __forceinline__ RowsAhead(const void* x, int64_t row, int64_t ld, int log_classes, char* place, int lanes,
+                                       int t, int dim)
+      : stride(ld << log_classes), lanes(lanes), t(t), dim(dim) {
+    shift = kForm == kShifted ? (int)((row * ld) & (E - 1)) : 0;
+    from = reinterpret_cast<const T*>(x) + row * ld - shift + t * E;
+    ring = place + t * (int)(E * sizeof(T));
+    // what lies beyond the row is zero, once: nothing is ever fetched to there
+    Vec<T, E> zero;
+    zero.clear();
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
-      Vec<T, E> zero;
-      zero.clear();
-      if constexpr (kRing) {
-        if ((v * lanes + t) * E >= dim)
-          for (int k = 0; k < kAhead * R; ++k) store_vec(reinterpret_cast<T*>(place(k, v)), zero);
+      if constexpr (E > 1) {
+        if (column(v) >= dim)
+          for (int k = 0; k < kAhead * R; ++k) store_vec(reinterpret_cast<T*>(at(k, v)), zero);
       } else {
 #pragma unroll
         for (int k = 0; k < R; ++k) next[k][v] = zero;
       }
     }
   }
-  // Row k of a batch as pairs, zeros beyond the row.  Where the batch has no row k, of an earlier one, or anything.
+  // First column of the thread's piece v; below 0 where the row begins inside it.
+  __device__ __forceinline__ int column(int v) const {
+    return (v * lanes + t) * E - (kForm == kShifted ? shift : 0);
+  }
+  __device__ __forceinline__ bool whole(int v) const {
+    return kForm == kShifted ? column(v) >= 0 && column(v) + E <= dim : column(v) < dim;
+  }
+  __device__ __forceinline__ char* at(int row, int v) const {
+    return ring + (row * NV + v) * lanes * (int)(E * sizeof(T));
+  }
+  __device__ __forceinline__ void fetch(int n, int batch) {
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      if (k >= n) break;
+#pragma unroll
+      for (int v = 0; v < NV; ++v) {
+        if (column(v) < dim) {
+          const T* p = from + v * lanes * E;
+          if constexpr (E > 1)  // nothing past the row is read, zeros take its place
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
+                             (uint32_t)__cvta_generic_to_shared(at(batch * R + k, v))),
+                         "l"(p), "r"(kForm == kPlain ? 16 : min(16, (dim - column(v)) * (int)sizeof(T)))
+                         : "memory");
+          else
+            next[k][v] = load_once<T, E>(p);
+        }
+      }
+      from += stride;
+    }
+  }
+  // Row k of a batch as pairs, zeros outside the row.  Where the batch has no row k: of an earlier one, or anything.
   __device__ __forceinline__ void values(F2 (&out)[NV * E / 2], int k, int batch) const {
     float f[NV * E];
 #pragma unroll
     for (int v = 0; v < NV; ++v) {
       Vec<T, E> x;
-      if constexpr (kRing)
-        x = load_vec<T, E>(reinterpret_cast<const T*>(place(batch * R + k, v)));
+      if constexpr (E > 1)
+        x = load_vec<T, E>(reinterpret_cast<const T*>(at(batch * R + k, v)));
       else
         x = next[k][v];
 #pragma unroll
       for (int i = 0; i < E; ++i) f[v * E + i] = x[i];
     }
+    if (kForm == kShifted && shift > 0 && t == 0) {  // the end of the row before
+#pragma unroll
+      for (int i = 0; i < E - 1; ++i)
+        if (i < shift) f[i] = 0.0f;
+    }
 #pragma unroll
     for (int j = 0; j < NV * E / 2; ++j) out[j] = F2(f[2 * j], f[2 * j + 1]);
   }
-  __device__ __forceinline__ char* place(int row, int v) const {
-    return ring + (row * NV + v) * lanes * (int)(E * sizeof(T));
-  }
-  // Makes pair j zero where it lies beyond the row.
-  __device__ __forceinline__ void inside(F2& x, int j) const {
-    if constexpr (E > 1) {
-      if ((2 * j / E * lanes + t) * E >= dim) x = F2(0.0f);
-    } else {
+  // Makes zero what lies outside the row, again.
+  __device__ __forceinline__ void mask(F2 (&x)[NV * E / 2]) const {
+#pragma unroll
+    for (int j = 0; j < NV * E / 2; ++j) {
       float a, b;
-      x.get(a, b);
-      x = F2(2 * j * lanes + t < dim ? a : 0.0f, (2 * j + 1) * lanes + t < dim ? b : 0.0f);
+      x[j].get(a, b);
+      const int c0 = column(2 * j / E) + 2 * j % E, c1 = column((2 * j + 1) / E) + (2 * j + 1) % E;
+      x[j] = F2(c0 >= 0 && c0 < dim ? a : 0.0f, c1 >= 0 && c1 < dim ? b : 0.0f);
+    }
+  }
+  __device__ __forceinline__ bool has_outside() const {
+    bool any = false;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) any = any || !whole(v);
+    return any;
+  }
+  // Stores a row's results; `to` is the thread's first piece of it.
+  __device__ __forceinline__ void store(T* to, const float (&y)[NV * E]) const {
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+      if (whole(v)) {
+        Vec<T, E> o;
+        o.set(y + v * E);
+        store_vec(to + v * lanes * E, o);
+      } else if (kForm == kShifted && column(v) < dim) {
+#pragma unroll
+        for (int i = 0; i < E; ++i)
+          if (column(v) + i >= 0 && column(v) + i < dim) to[v * lanes * E + i] = from_float<T>(y[v * E + i]);
+      }
     }
   }
 };
-// One group of copies per batch of rows (an empty one past the end); waits for the oldest batch.
+// One group of copies per batch of rows, an empty one past the end; at a batch's start all but the newest have to be there.
 __device__ __forceinline__ void close_batch() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-__device__ __forceinline__ void wait_batch() { asm volatile("cp.async.wait_group %0;" ::"n"(kAhead - 2) : "memory"); }
+__device__ __forceinline__ void wait_batch() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
 
-// A worker's rows in batches: at most R rows at a time, and none across two groups of weights.
-struct Batches {
-  int left, in_group, per_group;  // rows yet to be fetched, of them in the group
-  __device__ __forceinline__ int size(int R) const { return min(R, min(left, in_group)); }
-  __device__ __forceinline__ void take(int n) {
-    left -= n;
-    in_group -= n;
-    if (in_group == 0) in_group = per_group;
-  }
-};
-
-// A thread's weights of group g; zeros beyond the row.
-template <typename T, int E, int NV>
-__device__ __forceinline__ void load_pairs(const NormParams& p, const void* from, int64_t g, int lanes, int t,
-                                           float missing, F2 (&out)[NV * E / 2]) {
-  float f[NV * E];
+// A thread's weights of group g; zeros outside the row.
+template <typename T, int K, typename Rows>
+__device__ __forceinline__ void load_weights(const NormParams& p, const void* from, int64_t g, const Rows& rows, int E,
+                                             float missing, F2 (&out)[K / 2]) {
+  float f[K];
 #pragma unroll
-  for (int v = 0; v < NV; ++v) {
-    const int e = (v * lanes + t) * E;
-    float part[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) part[i] = 0.0f;
-    if (e < p.dim) load_weights<T, E>(from, g * p.dim + e, p.weights_fp32, missing, part);
-#pragma unroll
-    for (int i = 0; i < E; ++i) f[v * E + i] = part[i];
+  for (int j = 0; j < K; ++j) {
+    const int c = rows.column(j / E) + j % E;
+    f[j] = 0.0f;
+    if (c >= 0 && c < p.dim) {
+      if (from == nullptr)
+        f[j] = missing;
+      else if (p.weights_fp32)
+        f[j] = reinterpret_cast<const float*>(from)[g * p.dim + c];
+      else
+        f[j] = to_float<T>(reinterpret_cast<const T*>(from)[g * p.dim + c]);
+    }
   }
 #pragma unroll
-  for (int j = 0; j < NV * E / 2; ++j) out[j] = F2(f[2 * j], f[2 * j + 1]);
+  for (int j = 0; j < K / 2; ++j) out[j] = F2(f[2 * j], f[2 * j + 1]);
 }
 
-template <typename T, int E, int kKind, bool kRing>
+template <typename T, int kForm, int kKind>
 __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) norm_fwd_kernel(const NormParams p) {
   const void* x = p.x;
   enter_grid(x);
-  constexpr int K = worker_values(kKind), NV = K / E, R = worker_rows(kKind, false);
-  constexpr bool kCta = kKind >= kTeam;
+  constexpr int E = kForm == kSingle ? 1 : 16 / sizeof(T), K = worker_values(kKind), NV = K / E, R = worker_rows(kKind, false);
+  constexpr bool kCta = kKind >= kTeam, kRing = E > 1;
   extern __shared__ __align__(16) char ring[];
   __shared__ float slots[4][32][R];
   const int lanes = kCta ? blockDim.x : 32;
   const int t = kCta ? threadIdx.x : (threadIdx.x & 31);
-  const int64_t worker = kCta ? blockIdx.x : (int64_t)blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
-  if (worker >= p.n_workers) return;
-  const int64_t r = first_row(worker, p.n_workers, p.rows);
-  int todo = (int)(first_row(worker + 1, p.n_workers, p.rows) - r);
-  int64_t g = r / p.rows_per_group;
-  const int per_group = (int)min(p.rows_per_group, (int64_t)0x7fffffff);
-  int here = (int)min((int64_t)todo, (g + 1) * p.rows_per_group - r);  // rows of the group at work
-  Batches ahead = {todo, (int)min((g + 1) * p.rows_per_group - r, (int64_t)0x7fffffff), per_group};
-  T* out = reinterpret_cast<T*>(p.y) + r * p.stride_y + t * E;
-  RowsAhead<T, E, NV, R, kRing> rows;
-  rows.from = reinterpret_cast<const T*>(x) + r * p.stride_x + t * E;
-  rows.stride = p.stride_x;
-  rows.ring = ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes) + t * (E * sizeof(T));
-  rows.lanes = lanes;
-  rows.t = t;
-  rows.dim = p.dim;
-  rows.clear_beyond();
-  // n[0]: rows of the batch at work, n[1], n[2]: of the ones after it
-  int n[3];
+  const int worker = kCta ? blockIdx.x : blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
+  if (worker >= (kForm == kShifted ? p.parts << p.log_classes : p.parts)) return;
+  const Mine<kForm == kShifted> m(p, worker);
+  Batches<Mine<kForm == kShifted>> ahead(m);
+  const int64_t r = m.row(m.below(m.lo));
+  RowsAhead<T, kForm, NV, R> rows(x, r, p.stride_x, m.log_classes(), ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes),
+                              lanes, t, p.dim);
+  const bool ragged = rows.has_outside();
+  T* out = reinterpret_cast<T*>(p.y) + r * p.stride_y - rows.shift + t * E;
+  // n[0]: rows of the batch at work, n[1]: of the one after it
+  int n[2];
   n[0] = ahead.size(R);
   rows.fetch(n[0], 0);
-  ahead.take(n[0]);
-  n[1] = n[2] = 0;
+  ahead.take(m, n[0]);
+  n[1] = 0;
   if constexpr (kRing) {
     close_batch();
     n[1] = ahead.size(R);
     rows.fetch(n[1], 1);
     close_batch();
-    ahead.take(n[1]);
+    ahead.take(m, n[1]);
   }
   float* mean = p.mean == nullptr ? nullptr : p.mean + r;
   float* rstds = p.rstd + (p.mean == nullptr ? 0 : r);
   int phase = 0, at = 0;
-  for (; todo > 0; todo -= here, ++g, here = min(todo, per_group)) {
+  int64_t g = m.lo / m.per_group;
+  for (int64_t a = m.lo, e; a < m.hi; a = e, ++g) {
+    e = min(m.hi, (g + 1) * m.per_group);
+    int left = (int)(m.below(e) - m.below(a));
+    if (left == 0) continue;
     F2 w[K / 2], b[K / 2];
-    load_pairs<T, E, NV>(p, p.weight, g, lanes, t, 1.0f, w);
-    load_pairs<T, E, NV>(p, p.bias, g, lanes, t, 0.0f, b);
+    load_weights<T, K>(p, p.weight, g, rows, E, 1.0f, w);
+    load_weights<T, K>(p, p.bias, g, rows, E, 0.0f, b);
 #pragma unroll 1
-    for (int left = here; left > 0;) {
+    while (left > 0) {
       if constexpr (kRing) wait_batch();
       F2 cur[R][K / 2];
       float sum[R];
@@ -315,7 +377,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
       const int more = ahead.size(R);
       rows.fetch(more, at == 0 ? 2 : at - 1);
       if constexpr (kRing) close_batch();
-      ahead.take(more);
+      ahead.take(m, more);
       worker_sum<R, kCta>(sum, slots[phase]);
       float sq[R];
 #pragma unroll
@@ -324,11 +386,10 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
         const F2 minus(-sum[k]);
         F2 q(0.0f);
 #pragma unroll
-        for (int j = 0; j < K / 2; ++j) {
-          cur[k][j] = cur[k][j] + minus;
-          rows.inside(cur[k][j], j);  // what lies beyond the row is no deviation
-          q = fma(cur[k][j], cur[k][j], q);
-        }
+        for (int j = 0; j < K / 2; ++j) cur[k][j] = cur[k][j] + minus;
+        if (ragged) rows.mask(cur[k]);  // what lies outside the row is no deviation
+#pragma unroll
+        for (int j = 0; j < K / 2; ++j) q = fma(cur[k][j], cur[k][j], q);
         sq[k] = q.sum();
       }
       worker_sum<R, kCta>(sq, slots[phase + 1]);
@@ -341,23 +402,16 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
         float y[K];
 #pragma unroll
         for (int j = 0; j < K / 2; ++j) fma(cur[k][j] * scale, w[j], b[j]).get(y[2 * j], y[2 * j + 1]);
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          if ((v * lanes + t) * E < p.dim) {
-            Vec<T, E> o;
-            o.set(y + v * E);
-            store_vec(out + v * lanes * E, o);
-          }
-        }
-        out += p.stride_y;
+        rows.store(out, y);
+        out += p.stride_y << m.log_classes();
         if (mean != nullptr && t == 0) {
-          mean[k] = sum[k];
-          rstds[k] = rstd;
+          mean[(int64_t)k << m.log_classes()] = sum[k];
+          rstds[(int64_t)k << m.log_classes()] = rstd;
         }
       }
       if (mean != nullptr) {
-        mean += n[0];
-        rstds += n[0];
+        mean += (int64_t)n[0] << m.log_classes();
+        rstds += (int64_t)n[0] << m.log_classes();
       }
       left -= n[0];
       if constexpr (kRing) {
@@ -372,91 +426,96 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
 }
 
 // The gradients of the weights are sums over rows: each worker keeps those of its rows in registers and writes them out
-// when its group or its rows end, into slot worker + group, which no other (worker, group) has, as rows and with them
-// groups ascend from worker to worker.  norm_weights_kernel adds a group's slots.
-template <typename T, int E, int kKind, bool kRing>
+// where a group of its part ends.  Of P classes, class c of part i writes group g to slot (i + g) P + c, which no other
+// (worker, group) has, as rows and with them groups ascend from part to part.  norm_weights_kernel adds a group's slots.
+template <typename T, int kForm, int kKind>
 __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) norm_bwd_kernel(const NormParams p) {
   const void* x = p.x;
   enter_grid(x);
-  constexpr int K = worker_values(kKind), NV = K / E, R = worker_rows(kKind, true);
-  constexpr bool kCta = kKind >= kTeam;
+  constexpr int E = kForm == kSingle ? 1 : 16 / sizeof(T), K = worker_values(kKind), NV = K / E, R = worker_rows(kKind, true);
+  constexpr bool kCta = kKind >= kTeam, kRing = E > 1;
   extern __shared__ __align__(16) char ring[];
   __shared__ float slots[2][32][2 * R];
   const int lanes = kCta ? blockDim.x : 32;
   const int t = kCta ? threadIdx.x : (threadIdx.x & 31);
-  const int64_t worker = kCta ? blockIdx.x : (int64_t)blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
-  if (worker >= p.n_workers) return;
-  const int64_t r = first_row(worker, p.n_workers, p.rows);
-  int todo = (int)(first_row(worker + 1, p.n_workers, p.rows) - r);
-  int64_t g = r / p.rows_per_group;
-  const int per_group = (int)min(p.rows_per_group, (int64_t)0x7fffffff);
-  int here = (int)min((int64_t)todo, (g + 1) * p.rows_per_group - r);  // rows of the group at work
-  Batches ahead = {todo, (int)min((g + 1) * p.rows_per_group - r, (int64_t)0x7fffffff), per_group};
-  T* out = reinterpret_cast<T*>(p.y) + r * p.stride_x + t * E;
-  RowsAhead<T, E, NV, R, kRing> xs, ys;
-  xs.from = reinterpret_cast<const T*>(x) + r * p.stride_x + t * E;
-  ys.from = reinterpret_cast<const T*>(p.dy) + r * p.stride_y + t * E;
-  xs.stride = p.stride_x;
-  ys.stride = p.stride_y;
-  xs.ring = ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes) + t * (E * sizeof(T));
-  ys.ring = xs.ring + p.ring_bytes / 2;
-  xs.lanes = ys.lanes = lanes;
-  xs.t = ys.t = t;
-  xs.dim = ys.dim = p.dim;
-  xs.clear_beyond();
-  ys.clear_beyond();
-  float mean[R], rstd[R];  // of the next batch
-  const float* means = p.mean_in + r;
-  const float* rstds = p.rstd_in + r;
+  const int worker = kCta ? blockIdx.x : blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
+  if (worker >= (kForm == kShifted ? p.parts << p.log_classes : p.parts)) return;
+  const Mine<kForm == kShifted> m(p, worker);
+  Batches<Mine<kForm == kShifted>> ahead(m);
+  const int64_t r = m.row(m.below(m.lo));
+  char* place = ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes);
+  RowsAhead<T, kForm, NV, R> xs(x, r, p.stride_x, m.log_classes(), place, lanes, t, p.dim);
+  RowsAhead<T, kForm, NV, R> ys(p.dy, r, p.stride_y, m.log_classes(), place + p.ring_half, lanes, t, p.dim);
+  T* out = reinterpret_cast<T*>(p.y) + r * p.stride_x - xs.shift + t * E;
+  // a thread's weights, four from place to place of the threads: but for plain rows there are no registers for them
+  float4* ws = reinterpret_cast<float4*>(place + p.ring_bytes - lanes * K * 4) + t;
+  float mean[R], rstd[R];  // of the next batch, whose first row is row_ahead
+  int64_t row_ahead = r;
   auto stats = [&](int n) {
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      mean[k] = k < n ? means[k] : 0.0f;
-      rstd[k] = k < n ? rstds[k] : 0.0f;
+      mean[k] = k < n ? p.mean_in[row_ahead + (k << m.log_classes())] : 0.0f;
+      rstd[k] = k < n ? p.rstd_in[row_ahead + (k << m.log_classes())] : 0.0f;
     }
-    means += n;
-    rstds += n;
+    row_ahead += n << m.log_classes();
   };
-  int n[3];
+  int n[2];
   n[0] = ahead.size(R);
   xs.fetch(n[0], 0);
   ys.fetch(n[0], 0);
   stats(n[0]);
-  ahead.take(n[0]);
-  n[1] = n[2] = 0;
+  ahead.take(m, n[0]);
+  n[1] = 0;
   if constexpr (kRing) {
     close_batch();
     n[1] = ahead.size(R);
     xs.fetch(n[1], 1);
     ys.fetch(n[1], 1);
     close_batch();
-    ahead.take(n[1]);
+    ahead.take(m, n[1]);
   }
   int phase = 0, at = 0;
-  for (; todo > 0; todo -= here, ++g, here = min(todo, per_group)) {
+  int64_t g = m.lo / m.per_group;
+  for (int64_t a0 = m.lo, e; a0 < m.hi; a0 = e, ++g) {
+    e = min(m.hi, (g + 1) * m.per_group);
+    int left = (int)(m.below(e) - m.below(a0));
     F2 w[K / 2], dw[K / 2], db[K / 2];
-    load_pairs<T, E, NV>(p, p.weight, g, lanes, t, 1.0f, w);
+    load_weights<T, K>(p, p.weight, g, xs, E, 1.0f, w);
+    if constexpr (kForm != kPlain) {
+#pragma unroll
+      for (int j = 0; j < K / 4; ++j) {
+        float4 four;
+        w[2 * j].get(four.x, four.y);
+        w[2 * j + 1].get(four.z, four.w);
+        ws[j * lanes] = four;
+      }
+    }
 #pragma unroll
     for (int j = 0; j < K / 2; ++j) dw[j] = db[j] = F2(0.0f);
 #pragma unroll 1
-    for (int left = here; left > 0;) {
+    while (left > 0) {
       if constexpr (kRing) wait_batch();
       F2 xh[R][K / 2], a[R][K / 2], scale[R];
       float sum[2 * R];
 #pragma unroll
       for (int k = 0; k < R; ++k) {
         scale[k] = F2(rstd[k]);
-        const F2 shift(-mean[k]);
-        // beyond the row there is no gradient: dy is 0 there
+        const F2 minus(-mean[k]);
+        // outside the row there is no gradient: dy is 0 there
         xs.values(xh[k], k, at);
         ys.values(a[k], k, at);
         sum[2 * k] = sum[2 * k + 1] = 0.0f;
         if (R > 1 && k >= n[0]) continue;
         F2 s0(0.0f), s1(0.0f);
+        float4 four;
 #pragma unroll
         for (int j = 0; j < K / 2; ++j) {
           const F2 dy = a[k][j];
-          xh[k][j] = (xh[k][j] + shift) * scale[k];
+          if constexpr (kForm != kPlain) {
+            if (j % 2 == 0) four = ws[j / 2 * lanes];
+            w[j] = j % 2 == 0 ? F2(four.x, four.y) : F2(four.z, four.w);
+          }
+          xh[k][j] = (xh[k][j] + minus) * scale[k];
           a[k][j] = dy * w[j];
           s0 = s0 + a[k][j];
           s1 = fma(a[k][j], xh[k][j], s1);
@@ -470,7 +529,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
       xs.fetch(more, at == 0 ? 2 : at - 1);
       ys.fetch(more, at == 0 ? 2 : at - 1);
       if constexpr (kRing) close_batch();
-      ahead.take(more);
+      ahead.take(m, more);
       stats(kRing ? n[1] : more);
       worker_sum<2 * R, kCta>(sum, slots[phase]);
       phase ^= 1;
@@ -481,15 +540,8 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
         float dx[K];
 #pragma unroll
         for (int j = 0; j < K / 2; ++j) (scale[k] * fma(xh[k][j], c1, a[k][j] + c0)).get(dx[2 * j], dx[2 * j + 1]);
-#pragma unroll
-        for (int v = 0; v < NV; ++v) {
-          if ((v * lanes + t) * E < p.dim) {
-            Vec<T, E> o;
-            o.set(dx + v * E);
-            store_vec(out + v * lanes * E, o);
-          }
-        }
-        out += p.stride_x;
+        xs.store(out, dx);
+        out += p.stride_x << m.log_classes();
       }
       left -= n[0];
       if constexpr (kRing) {
@@ -501,7 +553,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
       }
     }
     if (p.want_weights) {
-      float* mine = p.partial + (worker + g) * 2 * p.dim;
+      float* mine = p.partial + (((m.part + g) << m.log_classes()) + m.cls) * 2 * p.dim;
 #pragma unroll
       for (int j = 0; j < K; j += 2) {
         float a[2], c[2];
@@ -509,10 +561,10 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
         db[j / 2].get(c[0], c[1]);
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int e = ((j + i) / E * lanes + t) * E;
-          if (e < p.dim) {
-            mine[e + (j + i) % E] = a[i];
-            mine[p.dim + e + (j + i) % E] = c[i];
+          const int col = xs.column((j + i) / E) + (j + i) % E;
+          if (col >= 0 && col < p.dim) {
+            mine[col] = a[i];
+            mine[p.dim + col] = c[i];
           }
         }
       }
@@ -520,49 +572,55 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
   }
 }
 
-// Adds the slots of each group.  A CTA has 32 columns of one group; its 8 warps take every 8th slot each and meet in
+// Adds the slots of each group.  A CTA has 32 columns of one group; its 32 warps take every 32nd slot each and meet in
 // shared memory, so the order is the same whatever runs when.
-__global__ void __launch_bounds__(256) norm_weights_kernel(const float* partial, int64_t rows, int64_t rows_per_group,
-                                                           int64_t n_workers, int dim, void* dweight, void* dbias,
-                                                           int dtype) {
+__global__ void __launch_bounds__(1024) norm_weights_kernel(const float* partial, int64_t rows, int64_t rows_per_group,
+                                                            int64_t parts, int log_classes, int dim,
+                                                            void* dweight, void* dbias, int dtype) {
   enter_grid(partial);
-  __shared__ float s[2][8][32];
+  __shared__ float s[2][32][33];
   const int tiles = (dim + 31) / 32;
   const int64_t g = blockIdx.x / tiles;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int col = (blockIdx.x % tiles) * 32 + lane;
+  const int first = (blockIdx.x % tiles) * 32, col = first + lane;
   float sw = 0.0f, sb = 0.0f;
   if (rows > 0) {
-    // workers with rows of this group: from the one that has the group's first row to the one that has its last
+    // parts with rows of this group: from the one that has the group's first row to the one that has its last
     const int64_t lo = g * rows_per_group, hi = min(lo + rows_per_group, rows) - 1;
-    const int64_t q = rows / n_workers, m = rows % n_workers;
-    const int64_t cut = m * (q + 1);  // rows of the workers that have one more
+    const int64_t q = rows / parts, m = rows % parts;
+    const int64_t cut = m * (q + 1);  // rows of the parts that have one more
     const int64_t w0 = lo < cut ? lo / (q + 1) : m + (lo - cut) / q;
     const int64_t w1 = hi < cut ? hi / (q + 1) : m + (hi - cut) / q;
-    if (col < dim)
-      for (int64_t w = w0 + warp; w <= w1; w += 8) {
-        const float* slot = partial + (w + g) * 2 * dim + col;
+    if (col < dim) {
+      const float* slot = partial + (((w0 + g) << log_classes) + warp) * 2 * dim + col;
+#pragma unroll 4
+      for (int left = (int)((w1 - w0 + 1) << log_classes) - warp; left > 0; left -= 32, slot += (int64_t)64 * dim) {
         sw += slot[0];
         sb += slot[dim];
       }
-  }
-  s[0][warp][lane] = sw;
-  s[1][warp][lane] = sb;
-  __syncthreads();
-  if (warp < 2 && col < dim) {
-    float v = 0.0f;
-#pragma unroll
-    for (int k = 0; k < 8; ++k) v += s[warp][k][lane];
-    void* to = warp == 0 ? dweight : dbias;
-    if (to != nullptr) {
-      const int64_t at = g * dim + col;
-      if (dtype == SPARSP_FP32)
-        reinterpret_cast<float*>(to)[at] = v;
-      else if (dtype == SPARSP_FP16)
-        reinterpret_cast<__half*>(to)[at] = __float2half_rn(v);
-      else
-        reinterpret_cast<__nv_bfloat16*>(to)[at] = __float2bfloat16_rn(v);
     }
+  }
+  s[0][lane][warp] = sw;
+  s[1][lane][warp] = sb;
+  __syncthreads();
+  // a warp adds what the warps have of column `first + warp`
+  float v[2] = {s[0][warp][lane], s[1][warp][lane]};
+  const int mine = first + warp;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    v[1] += __shfl_xor_sync(0xffffffffu, v[1], o);
+  }
+  void* to = lane == 0 ? dweight : dbias;
+  if (lane < 2 && mine < dim && to != nullptr) {
+    const int64_t at = g * dim + mine;
+    const float x = lane == 0 ? v[0] : v[1];
+    if (dtype == SPARSP_FP32)
+      reinterpret_cast<float*>(to)[at] = x;
+    else if (dtype == SPARSP_FP16)
+      reinterpret_cast<__half*>(to)[at] = __float2half_rn(x);
+    else
+      reinterpret_cast<__nv_bfloat16*>(to)[at] = __float2bfloat16_rn(x);
   }
 }
 
@@ -574,86 +632,91 @@ int64_t norm_groups(const sparsp_norm& n) {
 
 // How the rows are shared out.
 struct NormPlan {
-  bool vectors, ring;
-  int kind, threads;           // of a CTA
-  int ring_bytes, smem_bytes;  // of a worker, of a CTA
-  int64_t n_workers;
+  int form, kind, threads;                // threads of a CTA
+  int ring_bytes, ring_half, smem_bytes;  // of a worker, where dy's begins, of a CTA
+  int parts, log_classes;
   unsigned grid;
 };
 
 constexpr int kNormSmem = 224 * 1024;  // of a multiprocessor, for rings
 
-static NormPlan plan_norm(const sparsp_norm& n, bool vectors, bool bwd) {
-  NormPlan p;
-  p.vectors = vectors;
-  const int bytes = element_bytes(n.dtype), E = vectors ? 16 / bytes : 1;
-  p.kind = n.dim <= 256 ? kWarp8 : n.dim <= 512 ? kWarp16 : n.dim <= 5120 ? kTeam : n.dim <= 8192 ? kLongTeam : kLongestTeam;
-  const bool cta = p.kind >= kTeam;
-  p.threads = kNormThreads;
-  if (cta) {
-    const int units = (n.dim + E - 1) / E, per_thread = worker_values(p.kind) / E;
-    p.threads = ((units + per_thread - 1) / per_thread + 31) / 32 * 32;
+static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
+  NormPlan p = {};
+  const int bytes = element_bytes(n.dtype);
+  p.form = kSingle;
+  if (pieces) {
+    const int E = 16 / bytes;
+    if (n.rows > 1)
+      while ((n.stride_x << p.log_classes) % E) ++p.log_classes;
+    p.form = n.dim % E == 0 && p.log_classes == 0 ? kPlain : kShifted;
   }
-  int resident = std::min(32, 65536 / (p.threads * worker_registers(p.kind)));
-  const int workers = cta ? 1 : kNormThreads / 32;  // of a CTA
-  const int lanes = cta ? p.threads : 32;
-  p.ring_bytes = kAhead * worker_rows(p.kind, bwd) * lanes * worker_values(p.kind) * bytes * (bwd ? 2 : 1);
-  p.ring = E * bytes >= 4 && p.ring_bytes * workers <= kNormSmem - 4096;
-  p.smem_bytes = p.ring ? p.ring_bytes * workers : 0;
-  if (p.ring) resident = std::min(resident, kNormSmem / (p.smem_bytes + 4096));
-  p.n_workers = std::min<int64_t>(n.rows, (int64_t)kSms * resident * workers);
-  p.grid = (unsigned)((p.n_workers + workers - 1) / workers);
-  return p;
+  for (;;) {
+    const int E = p.form == kSingle ? 1 : 16 / bytes;
+    const int units = (n.dim + (p.log_classes > 0 ? E - 1 : 0) + E - 1) / E, span = units * E;
+    p.kind = span <= 256 ? kWarp8 : span <= 512 ? kWarp16 : span <= 5120 ? kTeam : span <= 8192 ? kLongTeam : kLongestTeam;
+    const bool cta = p.kind >= kTeam;
+    const int per_thread = worker_values(p.kind) / E;
+    p.threads = cta ? ((units + per_thread - 1) / per_thread + 31) / 32 * 32 : kNormThreads;
+    const int workers = cta ? 1 : kNormThreads / 32, lanes = cta ? p.threads : 32;  // workers of a CTA
+    const int values = lanes * worker_values(p.kind);
+    p.ring_half = p.form == kSingle ? 0 : kAhead * worker_rows(p.kind, bwd) * values * bytes;
+    p.ring_bytes = bwd ? 2 * p.ring_half + (p.form == kPlain ? 0 : values * 4) : p.ring_half;
+    p.smem_bytes = p.ring_bytes * workers;
+    // three long rows of x and of dy, and a row that begins behind the first of 16384 places, do not fit
+    if (p.form != kSingle && (p.smem_bytes > kNormSmem - 4096 || p.threads > worker_threads(p.kind))) {
+      p.form = kSingle;
+      p.log_classes = 0;
+      continue;
+    }
+    const int resident = std::min({32, 65536 / (p.threads * worker_registers(p.kind)), kNormSmem / (p.smem_bytes + 4096)});
+    const int64_t most = std::min<int64_t>(n.rows, (int64_t)kSms * resident * workers);
+    p.parts = (int)std::max<int64_t>(1, most >> p.log_classes);
+    const int all = p.parts << p.log_classes;
+    p.grid = (unsigned)((all + workers - 1) / workers);
+    return p;
+  }
 }
 
 int64_t norm_workspace_bytes(const sparsp_norm& n) {
-  const int64_t workers = std::max(plan_norm(n, true, true).n_workers, plan_norm(n, false, true).n_workers);
-  return kStatusWords * 4 + (workers + norm_groups(n)) * 2 * n.dim * 4;
-}
-
-static bool norm_vectors(const sparsp_norm& n, const void* a, const void* b, const void* c) {
-  const int E = 16 / element_bytes(n.dtype);
-  return n.dim % E == 0 && (n.rows <= 1 || (n.stride_x % E == 0 && n.stride_y % E == 0)) && (uintptr_t)a % 16 == 0 &&
-         (uintptr_t)b % 16 == 0 && (uintptr_t)c % 16 == 0;
-}
-
-template <typename T, int E, int kKind, bool kRing>
-static cudaError_t launch_norm_r(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
-  auto kern = bwd ? norm_bwd_kernel<T, E, kKind, kRing> : norm_fwd_kernel<T, E, kKind, kRing>;
-  if (kRing) {
-    const cudaError_t e = ensure_dynamic_smem((const void*)kern, plan.smem_bytes);
-    if (e != cudaSuccess) return e;
+  int64_t slots = 0;
+  for (const bool pieces : {true, false}) {
+    const NormPlan p = plan_norm(n, pieces, true);
+    slots = std::max(slots, (p.parts + norm_groups(n)) << p.log_classes);
   }
-  return launch_kernel(kern, dim3(plan.grid), plan.threads, plan.smem_bytes, st, p);
+  return kStatusWords * 4 + slots * 2 * n.dim * 4;
 }
 
-// Without a ring: single 16-bit values, and rows that are too long for shared memory.
-template <typename T, int E, int kKind>
+// Rows of all tensors have to begin at the same place of a 16-byte piece.
+static bool in_pieces(const sparsp_norm& n, const void* a, const void* b, const void* c) {
+  const int E = 16 / element_bytes(n.dtype);
+  return (n.rows <= 1 || (n.stride_x - n.stride_y) % E == 0) && (uintptr_t)a % 16 == 0 && (uintptr_t)b % 16 == 0 &&
+         (uintptr_t)c % 16 == 0;
+}
+
+template <typename T, int kForm, int kKind>
 static cudaError_t launch_norm_t(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
-  if constexpr (E * sizeof(T) < 4)
-    return launch_norm_r<T, E, kKind, false>(p, plan, bwd, st);
-  else if constexpr (kKind == kLongestTeam)
-    return plan.ring ? launch_norm_r<T, E, kKind, true>(p, plan, bwd, st)
-                     : launch_norm_r<T, E, kKind, false>(p, plan, bwd, st);
-  else
-    return launch_norm_r<T, E, kKind, true>(p, plan, bwd, st);
+  auto kern = bwd ? norm_bwd_kernel<T, kForm, kKind> : norm_fwd_kernel<T, kForm, kKind>;
+  const cudaError_t e = ensure_dynamic_smem((const void*)kern, plan.smem_bytes);
+  return e != cudaSuccess ? e : launch_kernel(kern, dim3(plan.grid), plan.threads, plan.smem_bytes, st, p);
 }
 
-template <typename T, int E>
-static cudaError_t launch_norm_e(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
+template <typename T, int kForm>
+static cudaError_t launch_norm_f(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
   switch (plan.kind) {
-    case kWarp8: return launch_norm_t<T, E, kWarp8>(p, plan, bwd, st);
-    case kWarp16: return launch_norm_t<T, E, kWarp16>(p, plan, bwd, st);
-    case kTeam: return launch_norm_t<T, E, kTeam>(p, plan, bwd, st);
-    case kLongTeam: return launch_norm_t<T, E, kLongTeam>(p, plan, bwd, st);
-    default: return launch_norm_t<T, E, kLongestTeam>(p, plan, bwd, st);
+    case kWarp8: return launch_norm_t<T, kForm, kWarp8>(p, plan, bwd, st);
+    case kWarp16: return launch_norm_t<T, kForm, kWarp16>(p, plan, bwd, st);
+    case kTeam: return launch_norm_t<T, kForm, kTeam>(p, plan, bwd, st);
+    case kLongTeam: return launch_norm_t<T, kForm, kLongTeam>(p, plan, bwd, st);
+    default: return launch_norm_t<T, kForm, kLongestTeam>(p, plan, bwd, st);
   }
 }
 
 static cudaError_t launch_norm(int dtype, const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
   cudaError_t e = cudaSuccess;
   SPARSP_WITH_TYPE(dtype, T, {
-    e = plan.vectors ? launch_norm_e<T, 16 / sizeof(T)>(p, plan, bwd, st) : launch_norm_e<T, 1>(p, plan, bwd, st);
+    e = plan.form == kPlain     ? launch_norm_f<T, kPlain>(p, plan, bwd, st)
+        : plan.form == kShifted ? launch_norm_f<T, kShifted>(p, plan, bwd, st)
+                                : launch_norm_f<T, kSingle>(p, plan, bwd, st);
   });
   return e;
 }
@@ -666,8 +729,10 @@ static NormParams norm_params(const sparsp_norm& n, const NormPlan& plan) {
   p.stride_y = n.stride_y;
   p.dim = n.dim;
   p.weights_fp32 = n.weight_dtype == SPARSP_FP32;
-  p.n_workers = (int32_t)plan.n_workers;
+  p.parts = plan.parts;
+  p.log_classes = plan.log_classes;
   p.ring_bytes = plan.ring_bytes;
+  p.ring_half = plan.ring_half;
   p.eps = n.eps;
   p.inv_dim = 1.0f / (float)n.dim;
   return p;
@@ -676,7 +741,7 @@ static NormParams norm_params(const sparsp_norm& n, const NormPlan& plan) {
 int launch_norm_fwd(const sparsp_norm& n, const void* X, const void* w, const void* b, void* Y, float* mean,
                     float* rstd, cudaStream_t st) {
   if (n.rows == 0) return SPARSP_OK;
-  const NormPlan plan = plan_norm(n, norm_vectors(n, X, Y, nullptr), false);
+  const NormPlan plan = plan_norm(n, in_pieces(n, X, Y, nullptr), false);
   NormParams p = norm_params(n, plan);
   p.x = X;
   p.weight = w;
@@ -690,7 +755,7 @@ int launch_norm_fwd(const sparsp_norm& n, const void* X, const void* w, const vo
 
 int launch_norm_bwd(const sparsp_norm& n, const void* dY, const void* X, const void* w, const float* mean,
                     const float* rstd, void* dX, void* dw, void* db, char* ws, cudaStream_t st) {
-  const NormPlan plan = plan_norm(n, norm_vectors(n, X, dY, dX), true);
+  const NormPlan plan = plan_norm(n, in_pieces(n, X, dY, dX), true);
   NormParams p = norm_params(n, plan);
   p.want_weights = dw != nullptr || db != nullptr;
   if (n.rows > 0) {
@@ -705,8 +770,8 @@ int launch_norm_bwd(const sparsp_norm& n, const void* dY, const void* X, const v
   }
   if (p.want_weights && norm_groups(n) > 0) {
     const unsigned grid = (unsigned)(norm_groups(n) * ((n.dim + 31) / 32));
-    SPARSP_CUDA_OK(launch_kernel(norm_weights_kernel, dim3(grid), 256, 0, st, p.partial, n.rows, p.rows_per_group,
-                                 std::max<int64_t>(plan.n_workers, 1), n.dim, dw, db, n.weight_dtype));
+    SPARSP_CUDA_OK(launch_kernel(norm_weights_kernel, dim3(grid), 1024, 0, st, p.partial, n.rows, p.rows_per_group,
+                                 (int64_t)plan.parts, plan.log_classes, n.dim, dw, db, n.weight_dtype));
   }
   return SPARSP_OK;
 }
