@@ -21,12 +21,14 @@ constexpr int kAhead = 3;          // batches of R rows in shared memory: one in
 
 // Who works on a row, by its length: a warp with 8 values a thread (up to 256) or 16 (512), or a CTA with 16 values a
 // thread and up to 320 threads (5120), of which a multiprocessor takes two or more, so that one computes while another
-// waits at its barrier; beyond that up to 512 threads with 16 values (8192) or 32.
-enum Worker { kWarp8, kWarp16, kTeam, kLongTeam, kLongestTeam };
-__host__ __device__ constexpr int worker_values(int kind) { return kind == kWarp8 ? 8 : kind == kLongestTeam ? 32 : 16; }
-__host__ __device__ constexpr int worker_threads(int kind) { return kind <= kWarp16 ? kNormThreads : kind == kTeam ? 320 : 512; }  // of a CTA, at most
-__host__ __device__ constexpr int worker_ctas(int kind) { return kind <= kTeam ? 2 : 1; }  // such CTAs that fit a multiprocessor
-__host__ __device__ constexpr int worker_registers(int kind) { return kind == kTeam ? 96 : 128; }
+// waits at its barrier; beyond that up to 512 threads with 16 values (8192) or 32.  Backward in fp32 it is shared memory
+// that says how many CTAs there are, and up to 2048 values more threads of 8 values each are better (15554 x 1921 70 us,
+// 112 with 16); elsewhere the sums over more threads cost more than they give (forward, 31000 x 1921 bf16: 89 and 61).
+enum Worker { kWarp8, kWarp16, kShortTeam, kTeam, kLongTeam, kLongestTeam };
+__host__ __device__ constexpr int worker_values(int kind) { return kind == kWarp8 || kind == kShortTeam ? 8 : kind == kLongestTeam ? 32 : 16; }
+__host__ __device__ constexpr int worker_threads(int kind) { return kind <= kWarp16 ? kNormThreads : kind == kShortTeam ? 256 : kind == kTeam ? 320 : 512; }  // of a CTA, at most
+__host__ __device__ constexpr int worker_ctas(int kind) { return kind == kShortTeam ? 3 : kind <= kTeam ? 2 : 1; }  // such CTAs that fit a multiprocessor
+__host__ __device__ constexpr int worker_registers(int kind) { return kind == kShortTeam ? 80 : kind == kTeam ? 96 : 128; }
 // Rows at a time, by what the registers hold: forward the row and two weights, backward two rows and three weights or
 // sums.
 __host__ __device__ constexpr int worker_rows(int kind, bool bwd) { return kind == kWarp8 ? (bwd ? 2 : 4) : kind == kLongestTeam || bwd ? 1 : 2; }
@@ -322,7 +324,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
   const void* x = p.x;
   enter_grid(x);
   constexpr int E = kForm == kSingle ? 1 : 16 / sizeof(T), K = worker_values(kKind), NV = K / E, R = worker_rows(kKind, false);
-  constexpr bool kCta = kKind >= kTeam, kRing = E > 1;
+  constexpr bool kCta = kKind >= kShortTeam, kRing = E > 1;
   extern __shared__ __align__(16) char ring[];
   __shared__ float slots[4][32][R];
   const int lanes = kCta ? blockDim.x : 32;
@@ -433,7 +435,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
   const void* x = p.x;
   enter_grid(x);
   constexpr int E = kForm == kSingle ? 1 : 16 / sizeof(T), K = worker_values(kKind), NV = K / E, R = worker_rows(kKind, true);
-  constexpr bool kCta = kKind >= kTeam, kRing = E > 1;
+  constexpr bool kCta = kKind >= kShortTeam, kRing = E > 1;
   extern __shared__ __align__(16) char ring[];
   __shared__ float slots[2][32][2 * R];
   const int lanes = kCta ? blockDim.x : 32;
@@ -654,7 +656,8 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
     const int E = p.form == kSingle ? 1 : 16 / bytes;
     const int units = (n.dim + (p.log_classes > 0 ? E - 1 : 0) + E - 1) / E, span = units * E;
     p.kind = span <= 256 ? kWarp8 : span <= 512 ? kWarp16 : span <= 5120 ? kTeam : span <= 8192 ? kLongTeam : kLongestTeam;
-    const bool cta = p.kind >= kTeam;
+    if (p.kind == kTeam && span <= 2048 && bwd && bytes == 4) p.kind = kShortTeam;
+    const bool cta = p.kind >= kShortTeam;
     const int per_thread = worker_values(p.kind) / E;
     p.threads = cta ? ((units + per_thread - 1) / per_thread + 31) / 32 * 32 : kNormThreads;
     const int workers = cta ? 1 : kNormThreads / 32, lanes = cta ? p.threads : 32;  // workers of a CTA
@@ -693,15 +696,21 @@ static bool in_pieces(const sparsp_norm& n, const void* a, const void* b, const 
          (uintptr_t)c % 16 == 0;
 }
 
-template <typename T, int kForm, int kKind>
-static cudaError_t launch_norm_t(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
-  auto kern = bwd ? norm_bwd_kernel<T, kForm, kKind> : norm_fwd_kernel<T, kForm, kKind>;
+static cudaError_t launch_kernel_of(void (*kern)(NormParams), const NormParams& p, const NormPlan& plan,
+                                    cudaStream_t st) {
   const cudaError_t e = ensure_dynamic_smem((const void*)kern, plan.smem_bytes);
   return e != cudaSuccess ? e : launch_kernel(kern, dim3(plan.grid), plan.threads, plan.smem_bytes, st, p);
 }
 
+template <typename T, int kForm, int kKind>
+static cudaError_t launch_norm_t(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
+  return launch_kernel_of(bwd ? norm_bwd_kernel<T, kForm, kKind> : norm_fwd_kernel<T, kForm, kKind>, p, plan, st);
+}
+
 template <typename T, int kForm>
 static cudaError_t launch_norm_f(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
+  if constexpr (sizeof(T) == 4)
+    if (plan.kind == kShortTeam) return launch_kernel_of(norm_bwd_kernel<T, kForm, kShortTeam>, p, plan, st);
   switch (plan.kind) {
     case kWarp8: return launch_norm_t<T, kForm, kWarp8>(p, plan, bwd, st);
     case kWarp16: return launch_norm_t<T, kForm, kWarp16>(p, plan, bwd, st);
