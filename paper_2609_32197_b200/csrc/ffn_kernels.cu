@@ -53,18 +53,21 @@ struct GemmCfg {
 __device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.0f, 1.0f + __expf(-x)); }
 constexpr float kTanhA = 2.0f * 0.7978845608028654f, kTanhB = 0.044715f;  // (1 + tanh(u)) / 2 = sigmoid(2u)
 
-__device__ __forceinline__ float activate(int kind, float x) {
-  if (kind == SPARSP_ACT_SILU) return x * sigmoid(x);
-  if (kind == SPARSP_ACT_GELU_TANH) return x * sigmoid(kTanhA * (x + kTanhB * x * x * x));
+// a(x), and a(x) with a'(x).  The kind is chosen once for many values: chosen value by value it kept their exponentials
+// and reciprocals from overlapping, and a tile's results took 4.1 us.
+template <int kKind>
+__device__ __forceinline__ float activate(float x) {
+  if constexpr (kKind == SPARSP_ACT_SILU) return x * sigmoid(x);
+  if constexpr (kKind == SPARSP_ACT_GELU_TANH) return x * sigmoid(kTanhA * (x + kTanhB * x * x * x));
   return x * 0.5f * (1.0f + erff(x * 0.70710678118654752f));
 }
-// a(x) and a'(x)
-__device__ __forceinline__ void activate_both(int kind, float x, float& a, float& slope) {
-  if (kind == SPARSP_ACT_SILU) {
+template <int kKind>
+__device__ __forceinline__ void activate(float x, float& a, float& slope) {
+  if constexpr (kKind == SPARSP_ACT_SILU) {
     const float s = sigmoid(x);
     a = x * s;
     slope = s * (1.0f + x * (1.0f - s));
-  } else if (kind == SPARSP_ACT_GELU_TANH) {
+  } else if constexpr (kKind == SPARSP_ACT_GELU_TANH) {
     const float s = sigmoid(kTanhA * (x + kTanhB * x * x * x));
     a = x * s;
     const float t = s * (1.0f - s);
@@ -74,6 +77,24 @@ __device__ __forceinline__ void activate_both(int kind, float x, float& a, float
     a = x * c;
     slope = c + x * 0.3989422804014327f * __expf(-0.5f * x * x);
   }
+}
+// Runs f with the kind as a constant.
+template <typename F>
+__device__ __forceinline__ void with_activation(int kind, F f) {
+  if (kind == SPARSP_ACT_SILU)
+    f(std::integral_constant<int, SPARSP_ACT_SILU>());
+  else if (kind == SPARSP_ACT_GELU_TANH)
+    f(std::integral_constant<int, SPARSP_ACT_GELU_TANH>());
+  else
+    f(std::integral_constant<int, SPARSP_ACT_GELU>());
+}
+// h = a(g) u
+template <int N>
+__device__ __forceinline__ void gate_product(int kind, const float (&g)[N], const float (&u)[N], float (&h)[N]) {
+  with_activation(kind, [&](auto k) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) h[i] = activate<decltype(k)::value>(g[i]) * u[i];
+  });
 }
 
 // A warp's 32 rows x 64 columns to global memory: staged in its own 4 KB (128-byte swizzle: a row's 16-byte pieces in
@@ -106,12 +127,12 @@ __device__ __forceinline__ void tile_at(const GemmParams& p, int tile, int& m, i
   m = b * p.band + in - n * height;
 }
 
+// One product, by pairs of CTAs `pair` of `pairs`; maps: A (two), B (two), results (up to three).
 template <typename T, int kMode, int BN>
-__global__ void __launch_bounds__(kGemmThreads, 1)
-    gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1,
-                const __grid_constant__ CUtensorMap b0, const __grid_constant__ CUtensorMap b1,
-                const __grid_constant__ CUtensorMap o0, const __grid_constant__ CUtensorMap o1,
-                const __grid_constant__ CUtensorMap o2, const GemmParams p) {
+__device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensorMap& a1, const CUtensorMap& b0,
+                                           const CUtensorMap& b1, const CUtensorMap& o0, const CUtensorMap& o1,
+                                           const CUtensorMap& o2, const GemmParams p, const int pair,
+                                           const int pairs) {
   using namespace ptx;
   using C = GemmCfg<BN>;
   extern __shared__ uint8_t dynamic[];
@@ -149,7 +170,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
   const uint32_t tmem = *tmem_slot;
   wait_previous_grids();
 
-  const int pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
   const int all_blocks = p.k_blocks * (kMode == kInput ? 2 : 1);
   constexpr bool kAMn = kMode == kWeights, kBMn = kMode != kForward;
 
@@ -289,22 +309,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
             uint32_t words[32];  // 64 columns of this thread's row
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
-              uint32_t x[32];
-              tmem_ld32(from + (o == 2 ? BN / 2 : 0) + c + half * 32, x);
+              float x[32];
+              tmem_ld32(from + (o == 2 ? BN / 2 : 0) + c + half * 32, reinterpret_cast<uint32_t*>(x));
               if (o == 0) {
-                uint32_t u[32];
-                tmem_ld32(from + BN / 2 + c + half * 32, u);
+                float u[32];
+                tmem_ld32(from + BN / 2 + c + half * 32, reinterpret_cast<uint32_t*>(u));
                 tmem_ld_wait(x);
                 tmem_ld_wait(u);
-#pragma unroll
-                for (int i = 0; i < 32; ++i)
-                  x[i] = __float_as_uint(activate(p.activation, __uint_as_float(x[i])) * __uint_as_float(u[i]));
+                gate_product(p.activation, x, u, x);
               } else {
                 tmem_ld_wait(x);
               }
 #pragma unroll
-              for (int i = 0; i < 16; ++i)
-                words[half * 16 + i] = pack2<T>(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
+              for (int i = 0; i < 16; ++i) words[half * 16 + i] = pack2<T>(x[2 * i], x[2 * i + 1]);
             }
             write_out(o == 0 ? &o0 : o == 1 ? &o1 : &o2, mine, words, lane, n * (BN / 2) + c, row, p.cols, p.rows);
           }
@@ -345,6 +362,32 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
     tmem_dealloc_pair(tmem, 512);
   }
   if (threadIdx.x == 0) report_abort(s_abort, p.status);
+}
+
+template <typename T, int kMode, int BN>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1,
+                const __grid_constant__ CUtensorMap b0, const __grid_constant__ CUtensorMap b1,
+                const __grid_constant__ CUtensorMap o0, const __grid_constant__ CUtensorMap o1,
+                const __grid_constant__ CUtensorMap o2, const GemmParams p) {
+  gemm_tiles<T, kMode, BN>(a0, a1, b0, b1, o0, o1, o2, p, blockIdx.x >> 1, gridDim.x >> 1);
+}
+
+struct GemmMaps {
+  CUtensorMap a0, a1, b0, b1, o0, o1, o2;
+};
+
+// dX and dW at once: the first `split` pairs make the one, the others the other.
+template <typename T, int BN>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+    gemm_both_kernel(const __grid_constant__ GemmMaps mi, const GemmParams pi,
+                     const __grid_constant__ GemmMaps mw, const GemmParams pw, const int split) {
+  const int pair = blockIdx.x >> 1;
+  if (pair < split)
+    gemm_tiles<T, kInput, BN>(mi.a0, mi.a1, mi.b0, mi.b1, mi.o0, mi.o1, mi.o2, pi, pair, split);
+  else
+    gemm_tiles<T, kWeights, BN>(mw.a0, mw.a1, mw.b0, mw.b1, mw.o0, mw.o1, mw.o2, pw, pair - split,
+                                (gridDim.x >> 1) - split);
 }
 
 // ---- few tokens -----------------------------------------------------------------------------------------------------
@@ -515,8 +558,8 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         for (int e = 0; e < 8; ++e) {
           g[e] = turn[(f + e) * ld + token];
           u[e] = turn[(F + f + e) * ld + token];
-          h[e] = activate(p.activation, g[e]) * u[e];
         }
+        gate_product(p.activation, g, u, h);
         const int64_t at = token * p.ld_out + col;
         Vec<T, 8> v;
         v.set(h);
@@ -546,11 +589,10 @@ __global__ void __launch_bounds__(kFewThreads, 1)
 // Adds the splits of every tile and finishes it as gemm_kernel would have.  A thread has one row and eight columns (for
 // the forward call of both projections).
 template <typename T, int kMode, int BN>
-__global__ void __launch_bounds__(256) gemm_join_kernel(const GemmParams p) {
+__device__ __forceinline__ void join_tile(const GemmParams p, int cta) {
   const float* partial = p.partial;
-  enter_grid(partial);
   constexpr int kCols = kMode == kForward ? BN / 2 : BN;  // result columns of a tile
-  const int tile = blockIdx.x / (kCols / 8), c = (blockIdx.x % (kCols / 8)) * 8;
+  const int tile = cta / (kCols / 8), c = (cta % (kCols / 8)) * 8;
   int m, n;
   tile_at(p, tile, m, n);
   const float4* from = reinterpret_cast<const float4*>(partial) + (int64_t)tile * p.splits * (BN / 4) * 256 + threadIdx.x;
@@ -580,45 +622,58 @@ __global__ void __launch_bounds__(256) gemm_join_kernel(const GemmParams p) {
   const int col = n * kCols + c;
   if (row >= p.rows || col >= p.cols) return;
   const int64_t at = row * p.ld_out + col;
-  uint4 o, kg, ku;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float a = v[2 * i], b = v[2 * i + 1];
-    if (kMode == kForward) {
-      (&o.x)[i] = pack2<T>(activate(p.activation, a) * u[2 * i], activate(p.activation, b) * u[2 * i + 1]);
-      (&kg.x)[i] = pack2<T>(a, b);
-      (&ku.x)[i] = pack2<T>(u[2 * i], u[2 * i + 1]);
-    } else {
-      (&o.x)[i] = pack2<T>(a, b);
+  Vec<T, 8> o;
+  if constexpr (kMode == kForward) {
+    if (p.keep[0] != nullptr) {
+      o.set(v);
+      store_vec(reinterpret_cast<T*>(p.keep[0]) + at, o);
+      o.set(u);
+      store_vec(reinterpret_cast<T*>(p.keep[1]) + at, o);
     }
+    gate_product(p.activation, v, u, v);
   }
-  *reinterpret_cast<uint4*>(reinterpret_cast<T*>(second ? p.out[1] : p.out[0]) + at) = o;
-  if (kMode == kForward && p.keep[0] != nullptr) {
-    *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.keep[0]) + at) = kg;
-    *reinterpret_cast<uint4*>(reinterpret_cast<T*>(p.keep[1]) + at) = ku;
-  }
+  o.set(v);
+  store_vec(reinterpret_cast<T*>(second ? p.out[1] : p.out[0]) + at, o);
+}
+
+template <typename T, int kMode, int BN>
+__global__ void __launch_bounds__(256) gemm_join_kernel(const GemmParams p) {
+  enter_grid();
+  join_tile<T, kMode, BN>(p, blockIdx.x);
+}
+// ... of dX by the first `split` CTAs, of dW by the others
+template <typename T, int BN>
+__global__ void __launch_bounds__(256)
+    gemm_join_both_kernel(const GemmParams pi, const GemmParams pw, const int split) {
+  enter_grid();
+  if (blockIdx.x < split)
+    join_tile<T, kInput, BN>(pi, blockIdx.x);
+  else
+    join_tile<T, kWeights, BN>(pw, blockIdx.x - split);
 }
 
 // dG = dH * up * a'(gate), dU = dH * a(gate), eight elements a thread.  A CTA has 2048 elements of one row, or of everything
 // where rows follow one another without gaps: a division a CTA, not one a thread (37800 x 13824: 1241 us with that).
 template <typename T>
 __global__ void __launch_bounds__(256) gate_grad_kernel(const T* dh, const T* gate, const T* up, T* dg, T* du,
-                                                        int64_t ld, int64_t row_length, int ctas_per_row,
-                                                        int activation) {
+                                                        int64_t ld, int64_t ld_out, int64_t row_length,
+                                                        int ctas_per_row, int activation) {
   enter_grid(dh, gate, up);
   const int row = blockIdx.x / ctas_per_row;
   const int64_t col = ((int64_t)(blockIdx.x - row * ctas_per_row) * 256 + threadIdx.x) * 8;
   if (col >= row_length) return;
-  const int64_t at = row * ld + col, to = row * row_length + col;
+  const int64_t at = row * ld + col, to = row * ld_out + col;
   const Vec<T, 8> h = load_once<T, 8>(dh + at), g = load_once<T, 8>(gate + at), u = load_once<T, 8>(up + at);
   float fg[8], fu[8];
+  with_activation(activation, [&](auto k) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    float a, slope;
-    activate_both(activation, g[e], a, slope);
-    fg[e] = h[e] * u[e] * slope;
-    fu[e] = h[e] * a;
-  }
+    for (int e = 0; e < 8; ++e) {
+      float a, slope;
+      activate<decltype(k)::value>(g[e], a, slope);
+      fg[e] = h[e] * u[e] * slope;
+      fu[e] = h[e] * a;
+    }
+  });
   Vec<T, 8> og, ou;
   og.set(fg);
   ou.set(fu);
@@ -654,42 +709,108 @@ static int make_map(CUtensorMap* out, int dtype, const void* base, int64_t rows,
   return make_matrix_tmap(out, base, dtype == SPARSP_BF16, rows, cols, ld, box_rows);
 }
 
-template <typename T, int kMode, int BN>
-static int launch_gemm_t(GemmParams p, const CUtensorMap (&map)[7], int dtype, char* ws, cudaStream_t st) {
-  using C = GemmCfg<BN>;
-  if ((int64_t)p.m_tiles * p.n_tiles > (1 << 30)) {
-    set_error("%d x %d tiles are too many", p.m_tiles, p.n_tiles);
+constexpr int BN = 256;
+using Bf = __nv_bfloat16;
+using Hf = __half;
+
+static int join_ctas(const GemmParams& p, int mode) {
+  return p.splits > 1 ? p.m_tiles * p.n_tiles * ((mode == kForward ? BN / 2 : BN) / 8) : 0;
+}
+
+// Clocks that a product takes on some pairs of SMs, and into how many pieces its K is split for that: 512 a block of K,
+// 2500 a unit for what no block hides, 12000 for writing sums out and the launch that adds them.  Split units have to fit
+// the pairs in one round, which is also what the workspace holds.
+static int64_t gemm_clocks(int tiles, int blocks, int pairs, int* splits) {
+  *splits = 1;
+  const int64_t whole = (int64_t)ceil_div(tiles, pairs) * (512LL * blocks + 2500);
+  const int most = std::min(pairs / tiles, blocks / 4);
+  if (most < 2) return whole;
+  const int64_t split = 512LL * ceil_div(blocks, most) + 2500 + 12000;
+  if (split >= whole) return whole;
+  *splits = most;
+  return split;
+}
+
+// What every product needs beside its sizes.
+static int prepare_gemm(GemmParams* p, int mode, const sparsp_ffn& f, char* ws) {
+  if ((int64_t)p->m_tiles * p->n_tiles > (1 << 30)) {
+    set_error("%d x %d tiles are too many", p->m_tiles, p->n_tiles);
     return SPARSP_ERR_UNSUPPORTED;
   }
-  const int tiles = p.m_tiles * p.n_tiles, blocks = p.k_blocks * (kMode == kInput ? 2 : 1);
-  // K is split where there are fewer tiles than pairs of SMs, into pieces of at least 8 blocks
-  p.splits = std::max(1, std::min(kPairs / std::max(tiles, 1), blocks / 8));
-  p.units = tiles * p.splits;
-  p.band = 8;
-  p.partial = reinterpret_cast<float*>(ws + kStatusWords * 4);
-  p.status = reinterpret_cast<int32_t*>(ws);
-  p.wait_limit = kWaitLimit;
-  constexpr int a_mn = kMode == kWeights, b_mn = kMode != kForward;
-  p.idesc = instruction(dtype, 256, BN, a_mn, b_mn);
-  auto kern = gemm_kernel<T, kMode, BN>;
+  gemm_clocks(p->m_tiles * p->n_tiles, p->k_blocks * (mode == kInput ? 2 : 1), kPairs, &p->splits);
+  p->units = p->m_tiles * p->n_tiles * p->splits;
+  p->band = 8;
+  p->partial = reinterpret_cast<float*>(ws + kStatusWords * 4);
+  p->status = reinterpret_cast<int32_t*>(ws);
+  p->wait_limit = kWaitLimit;
+  p->activation = f.activation;
+  p->idesc = instruction(f.dtype, 256, BN, mode == kWeights, mode != kForward);
+  return SPARSP_OK;
+}
+
+template <int kMode>
+static int launch_gemm(const GemmParams& p, const GemmMaps& m, int dtype, cudaStream_t st) {
+  using C = GemmCfg<BN>;
+  auto kern = dtype == SPARSP_BF16 ? gemm_kernel<Bf, kMode, BN> : gemm_kernel<Hf, kMode, BN>;
   SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, C::kDynamic));
   const unsigned grid = 2u * (unsigned)std::min(p.units, kPairs);
-  SPARSP_CUDA_OK(launch_clusters(kern, dim3(grid), 2, kGemmThreads, C::kDynamic, st, map[0], map[1], map[2], map[3], map[4],
-                                 map[5], map[6], p));
-  if (p.splits > 1) {
-    constexpr int kCols = kMode == kForward ? BN / 2 : BN;
-    SPARSP_CUDA_OK(launch_kernel(gemm_join_kernel<T, kMode, BN>, dim3((unsigned)(tiles * (kCols / 8))), 256, 0, st, p));
+  SPARSP_CUDA_OK(launch_clusters(kern, dim3(grid), 2, kGemmThreads, C::kDynamic, st, m.a0, m.a1, m.b0, m.b1, m.o0, m.o1,
+                                 m.o2, p));
+  if (const int ctas = join_ctas(p, kMode)) {
+    auto join = dtype == SPARSP_BF16 ? gemm_join_kernel<Bf, kMode, BN> : gemm_join_kernel<Hf, kMode, BN>;
+    SPARSP_CUDA_OK(launch_kernel(join, dim3((unsigned)ctas), 256, 0, st, p));
   }
   return SPARSP_OK;
 }
 
-template <int kMode, int BN>
-static int launch_gemm(const GemmParams& p, const CUtensorMap (&map)[7], int dtype, char* ws, cudaStream_t st) {
-  return dtype == SPARSP_BF16 ? launch_gemm_t<__nv_bfloat16, kMode, BN>(p, map, dtype, ws, st)
-                              : launch_gemm_t<__half, kMode, BN>(p, map, dtype, ws, st);
+// dX and dW together.  Alone, each of two small products leaves pairs of SMs without a tile in its last round; together
+// they share the pairs out so that both end at the same time.  The splits hold for either product alone too, so that it
+// gives the same bits.  Returns the pairs of dX.
+static int plan_both(GemmParams* pi, GemmParams* pw) {
+  const int ti = pi->m_tiles * pi->n_tiles, tw = pw->m_tiles * pw->n_tiles;
+  const int bi = 2 * pi->k_blocks, bw = pw->k_blocks;
+  int si, sw, low = 1, high = kPairs - 1;  // the fewest pairs with which dX is no later than dW
+  while (low < high) {
+    const int mid = (low + high) / 2;
+    if (gemm_clocks(ti, bi, mid, &si) <= gemm_clocks(tw, bw, kPairs - mid, &sw))
+      high = mid;
+    else
+      low = mid + 1;
+  }
+  int64_t best = INT64_MAX;
+  int pairs = low;
+  for (int s = std::max(1, low - 1); s <= low; ++s) {
+    const int64_t t = std::max(gemm_clocks(ti, bi, s, &si), gemm_clocks(tw, bw, kPairs - s, &sw));
+    if (t >= best) continue;
+    best = t;
+    pairs = s;
+    pi->splits = si;
+    pw->splits = sw;
+  }
+  pi->units = ti * pi->splits;
+  pw->units = tw * pw->splits;
+  if (pi->splits > 1) pw->partial += (int64_t)pi->units * 256 * BN;
+  return pairs;
 }
 
-static int64_t hidden_bytes(const sparsp_ffn& f) { return align_up(f.tokens * f.hidden * 2, 256); }
+static int launch_both(const GemmParams& pi, const GemmMaps& mi, const GemmParams& pw, const GemmMaps& mw, int pairs,
+                       int dtype, cudaStream_t st) {
+  using C = GemmCfg<BN>;
+  auto kern = dtype == SPARSP_BF16 ? gemm_both_kernel<Bf, BN> : gemm_both_kernel<Hf, BN>;
+  SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, C::kDynamic));
+  SPARSP_CUDA_OK(launch_clusters(kern, dim3(2 * kPairs), 2, kGemmThreads, C::kDynamic, st, mi, pi, mw, pw, pairs));
+  const int ji = join_ctas(pi, kInput), jw = join_ctas(pw, kWeights);
+  if (ji + jw > 0) {
+    auto join = dtype == SPARSP_BF16 ? gemm_join_both_kernel<Bf, BN> : gemm_join_both_kernel<Hf, BN>;
+    SPARSP_CUDA_OK(launch_kernel(join, dim3((unsigned)(ji + jw)), 256, 0, st, pi, pw, ji));
+  }
+  return SPARSP_OK;
+}
+
+// dG and dU have rows of whole 128-byte lines: a tile's rows of 128 bytes then lie in one line each, not in two (1003 x
+// 1160 x 2504, backward: 41 us without).
+static int64_t hidden_pitch(const sparsp_ffn& f) { return align_up(f.hidden, 64); }
+static int64_t hidden_bytes(const sparsp_ffn& f) { return align_up(f.tokens * hidden_pitch(f) * 2, 256); }
 
 int64_t ffn_workspace_bytes(const sparsp_ffn& f, bool backward) {
   return kStatusWords * 4 + kPartialBytes + (backward ? 2 * hidden_bytes(f) : 0);
@@ -741,18 +862,17 @@ static int launch_few(const sparsp_ffn& f, const void* X, const void* Wg, const 
 int launch_ffn_fwd(const sparsp_ffn& f, const void* X, const void* Wg, const void* Wu, void* H, void* gate, void* up,
                    char* ws, cudaStream_t st) {
   if (f.tokens <= kFewTokens) return launch_few(f, X, Wg, Wu, H, gate, up, ws, st);
-  constexpr int BN = 256;
-  CUtensorMap map[7];
+  GemmMaps m;
   int rc;
-  if ((rc = make_map(map + 0, f.dtype, X, f.tokens, f.dim, f.stride_x, kTileRows)) != SPARSP_OK) return rc;
-  if ((rc = make_map(map + 2, f.dtype, Wg, f.hidden, f.dim, f.stride_w, BN / 2)) != SPARSP_OK) return rc;
-  if ((rc = make_map(map + 3, f.dtype, Wu, f.hidden, f.dim, f.stride_w, BN / 2)) != SPARSP_OK) return rc;
-  map[1] = map[0];
-  if ((rc = make_map(map + 4, f.dtype, H, f.tokens, f.hidden, f.stride_h, 32)) != SPARSP_OK) return rc;
-  map[5] = map[6] = map[4];
+  if ((rc = make_map(&m.a0, f.dtype, X, f.tokens, f.dim, f.stride_x, kTileRows)) != SPARSP_OK) return rc;
+  if ((rc = make_map(&m.b0, f.dtype, Wg, f.hidden, f.dim, f.stride_w, BN / 2)) != SPARSP_OK) return rc;
+  if ((rc = make_map(&m.b1, f.dtype, Wu, f.hidden, f.dim, f.stride_w, BN / 2)) != SPARSP_OK) return rc;
+  m.a1 = m.a0;
+  if ((rc = make_map(&m.o0, f.dtype, H, f.tokens, f.hidden, f.stride_h, 32)) != SPARSP_OK) return rc;
+  m.o1 = m.o2 = m.o0;
   if (gate != nullptr) {
-    if ((rc = make_map(map + 5, f.dtype, gate, f.tokens, f.hidden, f.stride_h, 32)) != SPARSP_OK) return rc;
-    if ((rc = make_map(map + 6, f.dtype, up, f.tokens, f.hidden, f.stride_h, 32)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&m.o1, f.dtype, gate, f.tokens, f.hidden, f.stride_h, 32)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&m.o2, f.dtype, up, f.tokens, f.hidden, f.stride_h, 32)) != SPARSP_OK) return rc;
   }
   GemmParams p = {};
   p.out[0] = H;
@@ -764,13 +884,12 @@ int launch_ffn_fwd(const sparsp_ffn& f, const void* X, const void* Wg, const voi
   p.m_tiles = ceil_div(f.tokens, 256);
   p.n_tiles = ceil_div(f.hidden, BN / 2);
   p.k_blocks = ceil_div(f.dim, kStageK);
-  p.activation = f.activation;
-  return launch_gemm<kForward, BN>(p, map, f.dtype, ws, st);
+  if ((rc = prepare_gemm(&p, kForward, f, ws)) != SPARSP_OK) return rc;
+  return launch_gemm<kForward>(p, m, f.dtype, st);
 }
 
 int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const void* Wg, const void* Wu,
                    const void* gate, const void* up, void* dX, void* dWg, void* dWu, char* ws, cudaStream_t st) {
-  constexpr int BN = 256;
   if (f.tokens == 0) {
     if (dWg != nullptr)
       SPARSP_CUDA_OK(launch_kernel(zero_rows_kernel, dim3(2 * kSms), 256, 0, st, (uint16_t*)dWg, (uint16_t*)dWu,
@@ -780,7 +899,7 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
   if (dX == nullptr && dWg == nullptr) return SPARSP_OK;
   char* dg = ws + kStatusWords * 4 + kPartialBytes;
   char* du = dg + hidden_bytes(f);
-  const bool gaps = f.stride_h != f.hidden;
+  const bool gaps = f.stride_h != f.hidden || hidden_pitch(f) != f.hidden;
   const int64_t row_length = gaps ? f.hidden : f.tokens * f.hidden, rows = gaps ? f.tokens : 1;
   const int64_t ctas_per_row = (row_length + 2047) / 2048;
   if (ctas_per_row * rows > 0x7fffffffLL) {
@@ -791,47 +910,51 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
   auto grad = [&](auto* element) {
     using T = std::remove_pointer_t<decltype(element)>;
     return launch_kernel(gate_grad_kernel<T>, grid, 256, 0, st, (const T*)dH, (const T*)gate, (const T*)up, (T*)dg,
-                         (T*)du, f.stride_h, row_length, (int)ctas_per_row, f.activation);
+                         (T*)du, f.stride_h, hidden_pitch(f), row_length, (int)ctas_per_row, f.activation);
   };
   SPARSP_CUDA_OK(f.dtype == SPARSP_BF16 ? grad((__nv_bfloat16*)nullptr) : grad((__half*)nullptr));
-  CUtensorMap map[7];
+  GemmMaps mi, mw;
+  GemmParams pi = {}, pw = {};
   int rc;
+  pi.m_tiles = ceil_div(f.tokens, 256);
+  pw.m_tiles = 2 * ceil_div(f.hidden, 256);
+  pi.n_tiles = pw.n_tiles = ceil_div(f.dim, BN);
+  pi.k_blocks = ceil_div(f.hidden, kStageK);
+  pw.k_blocks = ceil_div(f.tokens, kStageK);
+  if ((rc = prepare_gemm(&pi, kInput, f, ws)) != SPARSP_OK) return rc;
+  if ((rc = prepare_gemm(&pw, kWeights, f, ws)) != SPARSP_OK) return rc;
+  // both at once up to four rounds of tiles: beyond that their last rounds matter less than that both want L2
+  const bool small = (int64_t)pi.m_tiles * pi.n_tiles + (int64_t)pw.m_tiles * pw.n_tiles <= 4 * kPairs;
+  const int pairs = small ? plan_both(&pi, &pw) : 0;
   if (dX != nullptr) {
-    if ((rc = make_map(map + 0, f.dtype, dg, f.tokens, f.hidden, f.hidden, kTileRows)) != SPARSP_OK) return rc;
-    if ((rc = make_map(map + 1, f.dtype, du, f.tokens, f.hidden, f.hidden, kTileRows)) != SPARSP_OK) return rc;
-    if ((rc = make_map(map + 2, f.dtype, Wg, f.hidden, f.dim, f.stride_w, kStageK)) != SPARSP_OK) return rc;
-    if ((rc = make_map(map + 3, f.dtype, Wu, f.hidden, f.dim, f.stride_w, kStageK)) != SPARSP_OK) return rc;
-    if ((rc = make_map(map + 4, f.dtype, dX, f.tokens, f.dim, f.stride_x, 32)) != SPARSP_OK) return rc;
-    map[5] = map[6] = map[4];
-    GemmParams p = {};
-    p.out[0] = dX;
-    p.ld_out = f.stride_x;
-    p.rows = (int32_t)f.tokens;
-    p.cols = f.dim;
-    p.m_tiles = ceil_div(f.tokens, 256);
-    p.n_tiles = ceil_div(f.dim, BN);
-    p.k_blocks = ceil_div(f.hidden, kStageK);
-    if ((rc = launch_gemm<kInput, BN>(p, map, f.dtype, ws, st)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mi.a0, f.dtype, dg, f.tokens, f.hidden, hidden_pitch(f), kTileRows)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mi.a1, f.dtype, du, f.tokens, f.hidden, hidden_pitch(f), kTileRows)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mi.b0, f.dtype, Wg, f.hidden, f.dim, f.stride_w, kStageK)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mi.b1, f.dtype, Wu, f.hidden, f.dim, f.stride_w, kStageK)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mi.o0, f.dtype, dX, f.tokens, f.dim, f.stride_x, 32)) != SPARSP_OK) return rc;
+    mi.o1 = mi.o2 = mi.o0;
+    pi.out[0] = dX;
+    pi.ld_out = f.stride_x;
+    pi.rows = (int32_t)f.tokens;
+    pi.cols = f.dim;
   }
   if (dWg != nullptr) {
-    if ((rc = make_map(map + 0, f.dtype, dg, f.tokens, f.hidden, f.hidden, kStageK)) != SPARSP_OK) return rc;
-    if ((rc = make_map(map + 1, f.dtype, du, f.tokens, f.hidden, f.hidden, kStageK)) != SPARSP_OK) return rc;
-    if ((rc = make_map(map + 2, f.dtype, X, f.tokens, f.dim, f.stride_x, kStageK)) != SPARSP_OK) return rc;
-    map[3] = map[2];
-    if ((rc = make_map(map + 4, f.dtype, dWg, f.hidden, f.dim, f.stride_w, 32)) != SPARSP_OK) return rc;
-    if ((rc = make_map(map + 5, f.dtype, dWu, f.hidden, f.dim, f.stride_w, 32)) != SPARSP_OK) return rc;
-    map[6] = map[4];
-    GemmParams p = {};
-    p.out[0] = dWg;
-    p.out[1] = dWu;
-    p.ld_out = f.stride_w;
-    p.rows = f.hidden;
-    p.cols = f.dim;
-    p.m_tiles = 2 * ceil_div(f.hidden, 256);
-    p.n_tiles = ceil_div(f.dim, BN);
-    p.k_blocks = ceil_div(f.tokens, kStageK);
-    if ((rc = launch_gemm<kWeights, BN>(p, map, f.dtype, ws, st)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mw.a0, f.dtype, dg, f.tokens, f.hidden, hidden_pitch(f), kStageK)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mw.a1, f.dtype, du, f.tokens, f.hidden, hidden_pitch(f), kStageK)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mw.b0, f.dtype, X, f.tokens, f.dim, f.stride_x, kStageK)) != SPARSP_OK) return rc;
+    mw.b1 = mw.b0;
+    if ((rc = make_map(&mw.o0, f.dtype, dWg, f.hidden, f.dim, f.stride_w, 32)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mw.o1, f.dtype, dWu, f.hidden, f.dim, f.stride_w, 32)) != SPARSP_OK) return rc;
+    mw.o2 = mw.o0;
+    pw.out[0] = dWg;
+    pw.out[1] = dWu;
+    pw.ld_out = f.stride_w;
+    pw.rows = f.hidden;
+    pw.cols = f.dim;
   }
+  if (small && dX != nullptr && dWg != nullptr) return launch_both(pi, mi, pw, mw, pairs, f.dtype, st);
+  if (dX != nullptr && (rc = launch_gemm<kInput>(pi, mi, f.dtype, st)) != SPARSP_OK) return rc;
+  if (dWg != nullptr && (rc = launch_gemm<kWeights>(pw, mw, f.dtype, st)) != SPARSP_OK) return rc;
   return SPARSP_OK;
 }
 
