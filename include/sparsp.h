@@ -503,7 +503,7 @@ typedef struct sparsp_ffn {
 } sparsp_ffn;
 
 /* Bytes of workspace that the forward call (backward = 0) or the backward call needs: dG and dU for the latter, and in
- * either case at most 20 MB of partial sums. */
+ * either case 39 MB for partial sums. */
 SPARSP_API int sparsp_gated_ffn_workspace_bytes(const sparsp_ffn* ffn, int32_t backward, int64_t* bytes);
 
 /* Both projections, the activation and the product.  Sums in fp32; H is rounded once, from the fp32 projections.

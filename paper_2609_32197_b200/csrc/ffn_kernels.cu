@@ -21,10 +21,11 @@ enum GemmMode { kForward, kInput, kWeights };
 struct GemmParams {
   void* out[2];           // kForward: H;  kInput: dX;  kWeights: dWg, dWu
   void* keep[2];          // kForward: gate, up or NULL
-  float* partial;         // sums of a tile's splits, when there are several
+  float* partial;         // sums of pieces of K
   int64_t ld_out;         // elements from row to row of out and keep
   int32_t rows, cols;     // of the result (kForward: tokens, hidden; kInput: tokens, dim; kWeights: hidden, dim)
-  int32_t m_tiles, n_tiles, splits, units, band;
+  int32_t m_tiles, n_tiles, band;
+  int32_t whole, shares;  // see Walk
   int32_t k_blocks;       // of 64, of one (A, B); kInput has two of them
   int32_t activation;
   uint32_t idesc;
@@ -127,6 +128,44 @@ __device__ __forceinline__ void tile_at(const GemmParams& p, int tile, int& m, i
   m = b * p.band + in - n * height;
 }
 
+// What a pair of CTAs works on.  The first `whole` tiles go to the pairs round by round; of the K blocks of the rest, which
+// would leave pairs without a tile, each of the first `shares` pairs has an equal run, so that a tile's sums are in pieces
+// that gemm_join_kernel adds.  A run is no longer than a tile and touches two at most.
+struct Walk {
+  int tile, k0, k1, slot;  // at work: tile, blocks of K, and where to put the sums (-1: the whole tile is done)
+  int next_whole, pairs, whole, blocks, lo, hi, next_slot;
+  __device__ __forceinline__ Walk(const GemmParams& p, int blocks, int pair, int pairs)
+      : next_whole(pair), pairs(pairs), whole(p.whole), blocks(blocks), lo(0), hi(0), next_slot(2 * pair) {
+    if (pair < p.shares) {
+      lo = share_begin(p, blocks, pair);
+      hi = share_begin(p, blocks, pair + 1);
+    }
+  }
+  // first of the rest's K blocks that pair q has
+  static __device__ __forceinline__ int share_begin(const GemmParams& p, int blocks, int q) {
+    return (int)((int64_t)(p.m_tiles * p.n_tiles - p.whole) * blocks * q / p.shares);
+  }
+  __device__ __forceinline__ bool next() {
+    if (next_whole < whole) {
+      tile = next_whole;
+      next_whole += pairs;
+      k0 = 0;
+      k1 = blocks;
+      slot = -1;
+      return true;
+    }
+    if (lo >= hi) return false;
+    const int r = lo / blocks;
+    tile = whole + r;
+    k0 = lo - r * blocks;
+    k1 = min(blocks, k0 + hi - lo);
+    slot = k1 - k0 == blocks ? -1 : next_slot;
+    ++next_slot;
+    lo += k1 - k0;
+    return true;
+  }
+};
+
 // One product, by pairs of CTAs `pair` of `pairs`; maps: A (two), B (two), results (up to three).
 template <typename T, int kMode, int BN>
 __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensorMap& a1, const CUtensorMap& b0,
@@ -170,7 +209,7 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
   const uint32_t tmem = *tmem_slot;
   wait_previous_grids();
 
-  const int all_blocks = p.k_blocks * (kMode == kInput ? 2 : 1);
+  Walk walk(p, p.k_blocks * (kMode == kInput ? 2 : 1), pair, pairs);
   constexpr bool kAMn = kMode == kWeights, kBMn = kMode != kForward;
 
   if (warp == kEpilogueWarps) {
@@ -181,12 +220,9 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
       for (int s = 0; s < C::kStages; ++s) full_of_even[s] = cluster_addr(full + s, 0);
       int s = 0;
       uint32_t round = 0;
-      for (int unit = pair; unit < p.units && !*s_abort; unit += pairs) {
-        const int tile = unit / p.splits, split = unit - tile * p.splits;
+      while (!*s_abort && walk.next()) {
         int m, n;
-        tile_at(p, tile, m, n);
-        const int k0 = (int)((int64_t)all_blocks * split / p.splits);
-        const int k1 = (int)((int64_t)all_blocks * (split + 1) / p.splits);
+        tile_at(p, walk.tile, m, n);
         const int half_m = p.m_tiles / 2;  // kWeights: the tiles of dWg, then those of dWu
         const CUtensorMap* ta = &a0;
         int row = (m * 2 + (int)rank) * kTileRows;
@@ -194,7 +230,7 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
           ta = &a1;
           row -= half_m * 2 * kTileRows;
         }
-        for (int k = k0; k < k1; ++k) {
+        for (int k = walk.k0; k < walk.k1; ++k) {
           mbar_wait_bounded_inline(empty + s, round ^ 1u, s_abort, 1, p.wait_limit);
           if (*s_abort) break;
           if (rank == 0) mbar_expect_tx(full + s, 2 * C::kStage);
@@ -245,20 +281,17 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
       constexpr uint32_t kStepA = kAMn ? 2048 : 32, kStepB = kBMn ? 2048 : 32;  // 16 elements of K
       int s = 0, acc = 0;
       uint32_t round = 0, acc_round = 0;
-      for (int unit = pair; unit < p.units && !*s_abort; unit += pairs) {
-        const int split = unit % p.splits;
-        const int k0 = (int)((int64_t)all_blocks * split / p.splits);
-        const int k1 = (int)((int64_t)all_blocks * (split + 1) / p.splits);
+      while (!*s_abort && walk.next()) {
         mbar_wait_bounded_inline(acc_empty + acc, acc_round ^ 1u, s_abort, 2, p.wait_limit);
         tc_fence_after();
-        for (int k = k0; k < k1; ++k) {
+        for (int k = walk.k0; k < walk.k1; ++k) {
           mbar_wait_bounded_inline(full + s, round, s_abort, 3, p.wait_limit);
           tc_fence_after();
           const uint64_t off = (uint64_t)((s * C::kStage) >> 4);
 #pragma unroll
           for (int kk = 0; kk < kStageK / 16; ++kk)
             mma_ss_pair(tmem + acc * BN, da + off + (kk * kStepA >> 4), db + off + (kk * kStepB >> 4), p.idesc,
-                        k > k0 || kk > 0);
+                        k > walk.k0 || kk > 0);
           mma_commit_pair(empty + s);
           if (++s == C::kStages) {
             s = 0;
@@ -277,17 +310,17 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
     int acc = 0;
     uint32_t acc_round = 0;
     const uint32_t even0 = cluster_addr(acc_empty, 0), even1 = cluster_addr(acc_empty + 1, 0);
-    for (int unit = pair; unit < p.units; unit += pairs) {
+    while (walk.next()) {
       int m, n;
-      tile_at(p, unit / p.splits, m, n);
+      tile_at(p, walk.tile, m, n);
       mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 4, p.wait_limit);
       if (*s_abort) break;
       tc_fence_after();
       const uint32_t from = tmem + acc * BN + ((uint32_t)(quarter * 32) << 16);
       const int in_tile = (int)rank * kTileRows + quarter * 32 + lane;
-      if (p.splits > 1) {
-        // [unit][BN / 4][256 rows] of four columns: lanes are rows, so a warp writes 512 bytes in a piece
-        float4* to = reinterpret_cast<float4*>(p.partial) + (int64_t)unit * (BN / 4) * 256 + in_tile;
+      if (walk.slot >= 0) {
+        // [slot][BN / 4][256 rows] of four columns: lanes are rows, so a warp writes 512 bytes in a piece
+        float4* to = reinterpret_cast<float4*>(p.partial) + (int64_t)walk.slot * (BN / 4) * 256 + in_tile;
 #pragma unroll 1
         for (int c = side * (BN / 2); c < (side + 1) * (BN / 2); c += 32) {
           uint32_t r[32];
@@ -586,33 +619,44 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   if (threadIdx.x == 0) report_abort(s_abort, p.status);
 }
 
-// Adds the splits of every tile and finishes it as gemm_kernel would have.  A thread has one row and eight columns (for
+// Adds the pieces of a tile, in the order of K, and finishes it as gemm_kernel would have.  A thread has one row and eight columns (for
 // the forward call of both projections).
 template <typename T, int kMode, int BN>
 __device__ __forceinline__ void join_tile(const GemmParams p, int cta) {
   const float* partial = p.partial;
   constexpr int kCols = kMode == kForward ? BN / 2 : BN;  // result columns of a tile
-  const int tile = cta / (kCols / 8), c = (cta % (kCols / 8)) * 8;
+  const int rest = cta / (kCols / 8), c = (cta % (kCols / 8)) * 8;
+  const int blocks = p.k_blocks * (kMode == kInput ? 2 : 1), lo = rest * blocks, hi = lo + blocks;
+  // pairs with blocks lo .. hi - 1; the first may have begun in the tile before, and has this one in its second slot then
+  int q = (int)((int64_t)lo * p.shares / ((int64_t)(p.m_tiles * p.n_tiles - p.whole) * blocks));
+  while (q > 0 && Walk::share_begin(p, blocks, q) > lo) --q;
+  while (Walk::share_begin(p, blocks, q + 1) <= lo) ++q;
+  if (Walk::share_begin(p, blocks, q) <= lo && Walk::share_begin(p, blocks, q + 1) >= hi) return;  // one pair had it all
   int m, n;
-  tile_at(p, tile, m, n);
-  const float4* from = reinterpret_cast<const float4*>(partial) + (int64_t)tile * p.splits * (BN / 4) * 256 + threadIdx.x;
+  tile_at(p, p.whole + rest, m, n);
   float v[8], u[8];
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = u[i] = 0.0f;
-  for (int s = 0; s < p.splits; ++s, from += (BN / 4) * 256) {
+  const int first = 2 * q + (Walk::share_begin(p, blocks, q) < lo ? 1 : 0);
+  int pieces = 1;
+  while (q + pieces < p.shares && Walk::share_begin(p, blocks, q + pieces) < hi) ++pieces;
+#pragma unroll 4
+  for (int i = 0; i < pieces; ++i) {
+    const float4* from = reinterpret_cast<const float4*>(partial) +
+                         (int64_t)(i == 0 ? first : 2 * (q + i)) * (BN / 4) * 256 + threadIdx.x;
 #pragma unroll
-    for (int q = 0; q < 2; ++q) {
-      const float4 x = from[(c / 4 + q) * 256];
-      v[4 * q] += x.x;
-      v[4 * q + 1] += x.y;
-      v[4 * q + 2] += x.z;
-      v[4 * q + 3] += x.w;
+    for (int h = 0; h < 2; ++h) {
+      const float4 x = from[(c / 4 + h) * 256];
+      v[4 * h] += x.x;
+      v[4 * h + 1] += x.y;
+      v[4 * h + 2] += x.z;
+      v[4 * h + 3] += x.w;
       if (kMode == kForward) {
-        const float4 y = from[((c + BN / 2) / 4 + q) * 256];
-        u[4 * q] += y.x;
-        u[4 * q + 1] += y.y;
-        u[4 * q + 2] += y.z;
-        u[4 * q + 3] += y.w;
+        const float4 y = from[((c + BN / 2) / 4 + h) * 256];
+        u[4 * h] += y.x;
+        u[4 * h + 1] += y.y;
+        u[4 * h + 2] += y.z;
+        u[4 * h + 3] += y.w;
       }
     }
   }
@@ -694,7 +738,7 @@ __global__ void __launch_bounds__(256) zero_rows_kernel(uint16_t* a, uint16_t* b
 
 constexpr int kPairs = kSms / 2;
 constexpr long long kWaitLimit = 200000000LL;  // of a wait in a kernel: about 0.1 s of SM clocks
-constexpr int64_t kPartialBytes = (int64_t)kPairs * 256 * 256 * 4;
+constexpr int64_t kPartialBytes = (int64_t)2 * kPairs * 256 * 256 * 4;
 
 static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
@@ -714,21 +758,40 @@ using Bf = __nv_bfloat16;
 using Hf = __half;
 
 static int join_ctas(const GemmParams& p, int mode) {
-  return p.splits > 1 ? p.m_tiles * p.n_tiles * ((mode == kForward ? BN / 2 : BN) / 8) : 0;
+  return (p.m_tiles * p.n_tiles - p.whole) * ((mode == kForward ? BN / 2 : BN) / 8);
 }
 
-// Clocks that a product takes on some pairs of SMs, and into how many pieces its K is split for that: 512 a block of K,
-// 2500 a unit for what no block hides, 12000 for writing sums out and the launch that adds them.  Split units have to fit
-// the pairs in one round, which is also what the workspace holds.
-static int64_t gemm_clocks(int tiles, int blocks, int pairs, int* splits) {
-  *splits = 1;
-  const int64_t whole = (int64_t)ceil_div(tiles, pairs) * (512LL * blocks + 2500);
-  const int most = std::min(pairs / tiles, blocks / 4);
-  if (most < 2) return whole;
-  const int64_t split = 512LL * ceil_div(blocks, most) + 2500 + 12000;
-  if (split >= whole) return whole;
-  *splits = most;
-  return split;
+// Clocks that a product takes on some pairs of SMs, and whether its last round is shared out by blocks of K for that (by
+// how many pairs; 0 = not): 512 a block of K, 2500 a unit for what no block hides, 12000 for writing sums out and the
+// launch that adds them.
+static int64_t gemm_clocks(int tiles, int blocks, int pairs, int* shares) {
+  *shares = 0;
+  const int rounds = tiles / pairs, rest = tiles % pairs;
+  const int64_t unit = 512LL * blocks + 2500, all_whole = (rounds + (rest > 0)) * unit;
+  if (rest == 0) return all_whole;
+  int64_t best = all_whole;
+  // equal runs for all pairs, of which most touch two tiles, or as many for each tile as there are pairs for it
+  const int all = (int)std::min<int64_t>(pairs, (int64_t)rest * blocks / 4), each = std::min(pairs / rest, blocks / 4);
+  if (all > rest) {
+    const int64_t t = rounds * unit + 512LL * ceil_div((int64_t)rest * blocks, all) + 2 * 2500 + 12000;
+    if (t < best) {
+      best = t;
+      *shares = all;
+    }
+  }
+  if (each > 1) {
+    const int64_t t = rounds * unit + 512LL * ceil_div(blocks, each) + 2500 + 12000;
+    if (t < best) {
+      best = t;
+      *shares = rest * each;
+    }
+  }
+  return best;
+}
+static void share_out(GemmParams* p, int pairs, int shares) {
+  const int tiles = p->m_tiles * p->n_tiles;
+  p->whole = shares > 0 ? tiles / pairs * pairs : tiles;
+  p->shares = shares;
 }
 
 // What every product needs beside its sizes.
@@ -737,8 +800,9 @@ static int prepare_gemm(GemmParams* p, int mode, const sparsp_ffn& f, char* ws) 
     set_error("%d x %d tiles are too many", p->m_tiles, p->n_tiles);
     return SPARSP_ERR_UNSUPPORTED;
   }
-  gemm_clocks(p->m_tiles * p->n_tiles, p->k_blocks * (mode == kInput ? 2 : 1), kPairs, &p->splits);
-  p->units = p->m_tiles * p->n_tiles * p->splits;
+  int shares;
+  gemm_clocks(p->m_tiles * p->n_tiles, p->k_blocks * (mode == kInput ? 2 : 1), kPairs, &shares);
+  share_out(p, kPairs, shares);
   p->band = 8;
   p->partial = reinterpret_cast<float*>(ws + kStatusWords * 4);
   p->status = reinterpret_cast<int32_t*>(ws);
@@ -753,7 +817,7 @@ static int launch_gemm(const GemmParams& p, const GemmMaps& m, int dtype, cudaSt
   using C = GemmCfg<BN>;
   auto kern = dtype == SPARSP_BF16 ? gemm_kernel<Bf, kMode, BN> : gemm_kernel<Hf, kMode, BN>;
   SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, C::kDynamic));
-  const unsigned grid = 2u * (unsigned)std::min(p.units, kPairs);
+  const unsigned grid = 2u * (unsigned)std::min(std::max(p.whole, p.shares), kPairs);
   SPARSP_CUDA_OK(launch_clusters(kern, dim3(grid), 2, kGemmThreads, C::kDynamic, st, m.a0, m.a1, m.b0, m.b1, m.o0, m.o1,
                                  m.o2, p));
   if (const int ctas = join_ctas(p, kMode)) {
@@ -764,8 +828,8 @@ static int launch_gemm(const GemmParams& p, const GemmMaps& m, int dtype, cudaSt
 }
 
 // dX and dW together.  Alone, each of two small products leaves pairs of SMs without a tile in its last round; together
-// they share the pairs out so that both end at the same time.  The splits hold for either product alone too, so that it
-// gives the same bits.  Returns the pairs of dX.
+// they share the pairs out so that both end at the same time.  What is shared out by blocks of K stays so for either product
+// alone, so that it gives the same bits.  Returns the pairs of dX.
 static int plan_both(GemmParams* pi, GemmParams* pw) {
   const int ti = pi->m_tiles * pi->n_tiles, tw = pw->m_tiles * pw->n_tiles;
   const int bi = 2 * pi->k_blocks, bw = pw->k_blocks;
@@ -784,12 +848,10 @@ static int plan_both(GemmParams* pi, GemmParams* pw) {
     if (t >= best) continue;
     best = t;
     pairs = s;
-    pi->splits = si;
-    pw->splits = sw;
+    share_out(pi, s, si);
+    share_out(pw, kPairs - s, sw);
   }
-  pi->units = ti * pi->splits;
-  pw->units = tw * pw->splits;
-  if (pi->splits > 1) pw->partial += (int64_t)pi->units * 256 * BN;
+  pw->partial += (int64_t)2 * pi->shares * 256 * BN;
   return pairs;
 }
 
