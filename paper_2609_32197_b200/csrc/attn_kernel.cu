@@ -1946,10 +1946,10 @@ int make_tile_tmap(CUtensorMap* out, const void* base, const sparsp_shape& s, co
   return SPARSP_OK;
 }
 
-// [rows][cols] of 16-bit elements (bf16 or fp16), `ld` elements from row to row, in boxes of 64 columns x box_rows rows with
-// 128-byte swizzle.
+// [rows][cols] of 16-bit elements (bf16 or fp16), `ld` elements from row to row, in boxes of box_cols (64 or 32) columns x
+// box_rows rows, swizzled by a row's length.
 int make_matrix_tmap(CUtensorMap* out, const void* base, bool bf16, int64_t rows, int64_t cols, int64_t ld,
-                     int box_rows) {
+                     int box_cols, int box_rows) {
   EncodeTiledFn enc = get_encode_fn();
   if (!enc) {
     set_error("cuTensorMapEncodeTiled is not available from the driver");
@@ -1957,11 +1957,12 @@ int make_matrix_tmap(CUtensorMap* out, const void* base, bool bf16, int64_t rows
   }
   cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
   cuuint64_t strides[1] = {(cuuint64_t)ld * 2};
-  cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+  cuuint32_t box[2] = {(cuuint32_t)box_cols, (cuuint32_t)box_rows};
   cuuint32_t estr[2] = {1, 1};
   CUresult r = enc(out, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2,
                    const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                   box_cols == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                   CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) {
     set_error("cuTensorMapEncodeTiled (matrix) failed with %d", (int)r);
     return SPARSP_ERR_CUDA;

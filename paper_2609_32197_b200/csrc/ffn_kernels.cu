@@ -34,7 +34,7 @@ struct GemmParams {
 };
 
 constexpr int kStageK = 64;           // K elements of a stage: one 128-byte swizzled row
-constexpr int kEpilogueWarps = 8;     // two for each quarter of the lanes
+constexpr int kEpilogueWarps = 16;    // four for each quarter of the lanes: eight left a tile's results 2.6 us, for latency
 constexpr int kGemmThreads = 32 * (kEpilogueWarps + 2);
 constexpr int kTileRows = 128;        // of one CTA
 
@@ -44,8 +44,8 @@ struct GemmCfg {
   static constexpr int kA = kTileRows * 128, kB = BN / 2 * 128;  // bytes a stage of one CTA
   static constexpr int kStage = kA + kB;
   static constexpr int kStages = 196608 / kStage > 8 ? 8 : 196608 / kStage;
-  static constexpr int kOffOut = kStages * kStage;  // each epilogue warp's 32 rows x 64 columns on their way out
-  static constexpr int kOffBars = kOffOut + kEpilogueWarps * 4096;
+  static constexpr int kOffOut = kStages * kStage;  // each epilogue warp's 32 rows x 32 columns on their way out
+  static constexpr int kOffBars = kOffOut + kEpilogueWarps * 2048;
   static constexpr int kBars = 2 * kStages + 4;
   static constexpr int kBytes = kOffBars + kBars * 8 + 16;
   static constexpr int kDynamic = kBytes + 1024;  // the tiles are aligned to 1024 bytes
@@ -98,17 +98,21 @@ __device__ __forceinline__ void gate_product(int kind, const float (&g)[N], cons
   });
 }
 
-// A warp's 32 rows x 64 columns to global memory: staged in its own 4 KB (128-byte swizzle: a row's 16-byte pieces in
-// turned places, so that lanes do not meet in a bank) and stored as one TMA tile, which writes whole lines and leaves out
+// A warp's 32 rows x 32 columns to global memory: staged in its own 2 KB (64-byte swizzle: a row's 16-byte pieces in
+// turned places, so that lanes do not meet in a bank) and stored as one TMA tile, which writes whole sectors and leaves out
 // what lies beyond the tensor.  16-byte stores from the registers, a row each, cost a forward call of 37800 x 5120 x 13824
 // that keeps its projections 9305 us.
-__device__ __forceinline__ void write_out(const CUtensorMap* to, uint8_t* mine, const uint32_t (&words)[32], int lane,
-                                          int col, int row, int cols, int rows) {
+template <typename T>
+__device__ __forceinline__ void write_out(const CUtensorMap* to, uint8_t* mine, const float (&x)[32], int lane, int col,
+                                          int row, int cols, int rows) {
+  uint32_t words[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) words[i] = pack2<T>(x[2 * i], x[2 * i + 1]);
   if (lane == 0) ptx::tma_store_wait_read();
   __syncwarp();
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    *reinterpret_cast<uint4*>(mine + lane * 128 + ((e ^ (lane & 7)) << 4)) =
+  for (int e = 0; e < 4; ++e)
+    *reinterpret_cast<uint4*>(mine + lane * 64 + ((e ^ ((lane >> 1) & 3)) << 4)) =
         make_uint4(words[4 * e], words[4 * e + 1], words[4 * e + 2], words[4 * e + 3]);
   ptx::fence_proxy_async_smem();
   __syncwarp();
@@ -304,9 +308,9 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
       }
     }
   } else {
-    // ---- results: warp w has the lanes of quarter w % 4, and one half of the columns ----
+    // ---- results: warp w has the lanes of quarter w % 4, and a fourth of the columns ----
     const int quarter = warp & 3, side = warp >> 2;
-    uint8_t* mine = smem + C::kOffOut + warp * 4096;
+    uint8_t* mine = smem + C::kOffOut + warp * 2048;
     int acc = 0;
     uint32_t acc_round = 0;
     const uint32_t even0 = cluster_addr(acc_empty, 0), even1 = cluster_addr(acc_empty + 1, 0);
@@ -322,7 +326,7 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
         // [slot][BN / 4][256 rows] of four columns: lanes are rows, so a warp writes 512 bytes in a piece
         float4* to = reinterpret_cast<float4*>(p.partial) + (int64_t)walk.slot * (BN / 4) * 256 + in_tile;
 #pragma unroll 1
-        for (int c = side * (BN / 2); c < (side + 1) * (BN / 2); c += 32) {
+        for (int c = side * (BN / 4); c < (side + 1) * (BN / 4); c += 32) {
           uint32_t r[32];
           tmem_ld32(from + c, r);
           tmem_ld_wait(r);
@@ -334,48 +338,30 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
       } else if constexpr (kMode == kForward) {
         const int row = m * 256 + (int)rank * kTileRows + quarter * 32;
 #pragma unroll 1
-        for (int c = side * (BN / 4); c < (side + 1) * (BN / 4); c += 64) {
-          // h, then the projections as they are: the second and third read tensor memory again
-          const int outputs = p.keep[0] != nullptr ? 3 : 1;
-#pragma unroll 1
-          for (int o = 0; o < outputs; ++o) {
-            uint32_t words[32];  // 64 columns of this thread's row
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              float x[32];
-              tmem_ld32(from + (o == 2 ? BN / 2 : 0) + c + half * 32, reinterpret_cast<uint32_t*>(x));
-              if (o == 0) {
-                float u[32];
-                tmem_ld32(from + BN / 2 + c + half * 32, reinterpret_cast<uint32_t*>(u));
-                tmem_ld_wait(x);
-                tmem_ld_wait(u);
-                gate_product(p.activation, x, u, x);
-              } else {
-                tmem_ld_wait(x);
-              }
-#pragma unroll
-              for (int i = 0; i < 16; ++i) words[half * 16 + i] = pack2<T>(x[2 * i], x[2 * i + 1]);
-            }
-            write_out(o == 0 ? &o0 : o == 1 ? &o1 : &o2, mine, words, lane, n * (BN / 2) + c, row, p.cols, p.rows);
+        for (int c = side * (BN / 8); c < (side + 1) * (BN / 8); c += 32) {
+          float g[32], u[32];
+          tmem_ld32(from + c, reinterpret_cast<uint32_t*>(g));
+          tmem_ld32(from + BN / 2 + c, reinterpret_cast<uint32_t*>(u));
+          tmem_ld_wait(g);
+          tmem_ld_wait(u);
+          const int col = n * (BN / 2) + c;
+          if (p.keep[0] != nullptr) {
+            write_out<T>(&o1, mine, g, lane, col, row, p.cols, p.rows);
+            write_out<T>(&o2, mine, u, lane, col, row, p.cols, p.rows);
           }
+          gate_product(p.activation, g, u, g);
+          write_out<T>(&o0, mine, g, lane, col, row, p.cols, p.rows);
         }
       } else {
         const int half_m = p.m_tiles / 2;
         const bool second = kMode == kWeights && m >= half_m;
         const int row = (second ? m - half_m : m) * 256 + (int)rank * kTileRows + quarter * 32;
 #pragma unroll 1
-        for (int c = side * (BN / 2); c < (side + 1) * (BN / 2); c += 64) {
-          uint32_t words[32];
-#pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            uint32_t x[32];
-            tmem_ld32(from + c + half * 32, x);
-            tmem_ld_wait(x);
-#pragma unroll
-            for (int i = 0; i < 16; ++i)
-              words[half * 16 + i] = pack2<T>(__uint_as_float(x[2 * i]), __uint_as_float(x[2 * i + 1]));
-          }
-          write_out(second ? &o1 : &o0, mine, words, lane, n * BN + c, row, p.cols, p.rows);
+        for (int c = side * (BN / 4); c < (side + 1) * (BN / 4); c += 32) {
+          float x[32];
+          tmem_ld32(from + c, reinterpret_cast<uint32_t*>(x));
+          tmem_ld_wait(x);
+          write_out<T>(second ? &o1 : &o0, mine, x, lane, n * BN + c, row, p.cols, p.rows);
         }
       }
       tc_fence_before();
@@ -748,9 +734,12 @@ static uint32_t instruction(int dtype, int M, int N, int a_mn_major, int b_mn_ma
   return dtype == SPARSP_BF16 ? d : d & ~((1u << 7) | (1u << 10));
 }
 
-// [rows][cols] of 16-bit elements in boxes of 64 columns x box_rows rows, 128-byte swizzle
+// [rows][cols] of 16-bit elements in boxes of 64 columns x box_rows rows, and for results of 32 x 32
 static int make_map(CUtensorMap* out, int dtype, const void* base, int64_t rows, int64_t cols, int64_t ld, int box_rows) {
-  return make_matrix_tmap(out, base, dtype == SPARSP_BF16, rows, cols, ld, box_rows);
+  return make_matrix_tmap(out, base, dtype == SPARSP_BF16, rows, cols, ld, 64, box_rows);
+}
+static int make_out_map(CUtensorMap* out, int dtype, const void* base, int64_t rows, int64_t cols, int64_t ld) {
+  return make_matrix_tmap(out, base, dtype == SPARSP_BF16, rows, cols, ld, 32, 32);
 }
 
 constexpr int BN = 256;
@@ -930,11 +919,11 @@ int launch_ffn_fwd(const sparsp_ffn& f, const void* X, const void* Wg, const voi
   if ((rc = make_map(&m.b0, f.dtype, Wg, f.hidden, f.dim, f.stride_w, BN / 2)) != SPARSP_OK) return rc;
   if ((rc = make_map(&m.b1, f.dtype, Wu, f.hidden, f.dim, f.stride_w, BN / 2)) != SPARSP_OK) return rc;
   m.a1 = m.a0;
-  if ((rc = make_map(&m.o0, f.dtype, H, f.tokens, f.hidden, f.stride_h, 32)) != SPARSP_OK) return rc;
+  if ((rc = make_out_map(&m.o0, f.dtype, H, f.tokens, f.hidden, f.stride_h)) != SPARSP_OK) return rc;
   m.o1 = m.o2 = m.o0;
   if (gate != nullptr) {
-    if ((rc = make_map(&m.o1, f.dtype, gate, f.tokens, f.hidden, f.stride_h, 32)) != SPARSP_OK) return rc;
-    if ((rc = make_map(&m.o2, f.dtype, up, f.tokens, f.hidden, f.stride_h, 32)) != SPARSP_OK) return rc;
+    if ((rc = make_out_map(&m.o1, f.dtype, gate, f.tokens, f.hidden, f.stride_h)) != SPARSP_OK) return rc;
+    if ((rc = make_out_map(&m.o2, f.dtype, up, f.tokens, f.hidden, f.stride_h)) != SPARSP_OK) return rc;
   }
   GemmParams p = {};
   p.out[0] = H;
@@ -993,7 +982,7 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
     if ((rc = make_map(&mi.a1, f.dtype, du, f.tokens, f.hidden, hidden_pitch(f), kTileRows)) != SPARSP_OK) return rc;
     if ((rc = make_map(&mi.b0, f.dtype, Wg, f.hidden, f.dim, f.stride_w, kStageK)) != SPARSP_OK) return rc;
     if ((rc = make_map(&mi.b1, f.dtype, Wu, f.hidden, f.dim, f.stride_w, kStageK)) != SPARSP_OK) return rc;
-    if ((rc = make_map(&mi.o0, f.dtype, dX, f.tokens, f.dim, f.stride_x, 32)) != SPARSP_OK) return rc;
+    if ((rc = make_out_map(&mi.o0, f.dtype, dX, f.tokens, f.dim, f.stride_x)) != SPARSP_OK) return rc;
     mi.o1 = mi.o2 = mi.o0;
     pi.out[0] = dX;
     pi.ld_out = f.stride_x;
@@ -1005,8 +994,8 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
     if ((rc = make_map(&mw.a1, f.dtype, du, f.tokens, f.hidden, hidden_pitch(f), kStageK)) != SPARSP_OK) return rc;
     if ((rc = make_map(&mw.b0, f.dtype, X, f.tokens, f.dim, f.stride_x, kStageK)) != SPARSP_OK) return rc;
     mw.b1 = mw.b0;
-    if ((rc = make_map(&mw.o0, f.dtype, dWg, f.hidden, f.dim, f.stride_w, 32)) != SPARSP_OK) return rc;
-    if ((rc = make_map(&mw.o1, f.dtype, dWu, f.hidden, f.dim, f.stride_w, 32)) != SPARSP_OK) return rc;
+    if ((rc = make_out_map(&mw.o0, f.dtype, dWg, f.hidden, f.dim, f.stride_w)) != SPARSP_OK) return rc;
+    if ((rc = make_out_map(&mw.o1, f.dtype, dWu, f.hidden, f.dim, f.stride_w)) != SPARSP_OK) return rc;
     mw.o2 = mw.o0;
     pw.out[0] = dWg;
     pw.out[1] = dWu;
