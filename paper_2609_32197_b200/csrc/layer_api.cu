@@ -62,7 +62,7 @@ int check_norm(const sparsp_norm* n) {
     SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "row strides must be at least dim");
   if (!(n->eps >= 0.0f) || std::isinf(n->eps)) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "eps must be finite and >= 0");
   if (n->rows > (1LL << 37)) SPARSP_REFUSE(SPARSP_ERR_UNSUPPORTED, "%lld rows are too many", (long long)n->rows);
-  if (norm_groups(*n) * ((n->dim + 31) / 32) > 0x7fffffffLL)
+  if (norm_groups(*n) * ((n->dim + 7) / 8) > 0x7fffffffLL)
     SPARSP_REFUSE(SPARSP_ERR_UNSUPPORTED, "%lld groups of rows are too many", (long long)norm_groups(*n));
   return SPARSP_OK;
 }

@@ -24,6 +24,7 @@ constexpr int kAhead = 3;          // batches of R rows in shared memory: one in
 // waits at its barrier; beyond that up to 512 threads with 16 values (8192) or 32.  Backward in fp32 it is shared memory
 // that says how many CTAs there are, and up to 2048 values more threads of 8 values each are better (15554 x 1921 70 us,
 // 112 with 16); elsewhere the sums over more threads cost more than they give (forward, 31000 x 1921 bf16: 89 and 61).
+// A warp takes several short rows at once: 4, 8 or 16 lanes have a row of up to 32, 64 or 128 values.
 enum Worker { kWarp8, kWarp16, kShortTeam, kTeam, kLongTeam, kLongestTeam };
 __host__ __device__ constexpr int worker_values(int kind) { return kind == kWarp8 || kind == kShortTeam ? 8 : kind == kLongestTeam ? 32 : 16; }
 __host__ __device__ constexpr int worker_threads(int kind) { return kind <= kWarp16 ? kNormThreads : kind == kShortTeam ? 256 : kind == kTeam ? 320 : 512; }  // of a CTA, at most
@@ -57,6 +58,7 @@ struct NormParams {
   int32_t dim, weights_fp32, want_weights;
   int32_t parts, log_classes;  // workers: parts << log_classes
   int32_t ring_bytes, ring_half;  // of a worker; where dy's begins
+  int32_t log_lanes;              // kWarp8: lanes of a row
   float eps, inv_dim;
 };
 
@@ -112,7 +114,7 @@ struct Batches {
 // take little more than one.  A CTA's warps meet in `slot`, which the caller alternates so that one barrier a call is
 // enough.
 template <int N, bool kCta>
-__device__ __forceinline__ void worker_sum(float (&v)[N], float (*slot)[N]) {
+__device__ __forceinline__ void worker_sum(float (&v)[N], float (*slot)[N], int lanes) {
   const int lane = threadIdx.x & 31;
 #pragma unroll
   for (int k = N / 2, o = 1; k > 0; k /= 2, o *= 2) {
@@ -128,7 +130,8 @@ __device__ __forceinline__ void worker_sum(float (&v)[N], float (*slot)[N]) {
 #pragma unroll
   for (int k = N / 2, o = 1; k > 0; k /= 2, o *= 2) mine += lane & o ? k : 0;
 #pragma unroll
-  for (int o = N; o < 32; o *= 2) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+  for (int o = N; o < 32; o *= 2)
+    if (kCta || o < lanes) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if constexpr (kCta) {
     const int warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
     if (lane < N) slot[warp][mine] = sum;
@@ -146,7 +149,7 @@ __device__ __forceinline__ void worker_sum(float (&v)[N], float (*slot)[N]) {
       int from = 0;
 #pragma unroll
       for (int k = N / 2, o = 1; k > 0; k /= 2, o *= 2) from |= i & k ? o : 0;
-      v[i] = __shfl_sync(0xffffffffu, sum, from);
+      v[i] = __shfl_sync(0xffffffffu, sum, from + (lane & -lanes));
     }
   }
 }
@@ -181,21 +184,37 @@ __device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
 }
 
 // The rows ahead of a worker, of one tensor: in shared memory as above, or (kSingle) the next R rows in registers.
+// A thread's place: among the lanes of its row, and among the threads of its worker.
+struct Place {
+  int lanes, t, threads, thread, at_once, sub;
+  __device__ __forceinline__ Place(bool cta, bool several, int log_lanes) {
+    threads = cta ? blockDim.x : 32;
+    thread = cta ? threadIdx.x : (threadIdx.x & 31);
+    lanes = several ? 1 << log_lanes : threads;
+    t = several ? thread & (lanes - 1) : thread;
+    at_once = several ? 32 >> log_lanes : 1;
+    sub = several ? thread >> log_lanes : 0;
+  }
+};
+
 template <typename T, int kForm, int NV, int R>
 struct RowsAhead {
   static constexpr int E = kForm == kSingle ? 1 : 16 / sizeof(T);
   Vec<T, E> next[E > 1 ? 1 : R][E > 1 ? 1 : NV];
   const T* from;  // this thread's first piece of the next row to be fetched
   int64_t stride;
-  char* ring;  // this thread's places, `lanes` pieces from one to the next
-  int lanes, t, dim, shift;
+  char* ring;  // this thread's places, `threads` pieces from one to the next
+  int lanes, t, dim, shift, threads;
+  int at_once, sub;  // rows that a warp has at once, and which of them is this thread's
 
-  __device__ __forceinline__ RowsAhead(const void* x, int64_t row, int64_t ld, int log_classes, char* place, int lanes,
-                                       int t, int dim)
-      : stride(ld << log_classes), lanes(lanes), t(t), dim(dim) {
+
+  __device__ __forceinline__ RowsAhead(const void* x, int64_t row, int64_t ld, int log_classes, char* place,
+                                       const Place& me, int dim)
+      : stride(ld << log_classes), lanes(me.lanes), t(me.t), dim(dim), threads(me.threads), at_once(me.at_once),
+        sub(me.sub) {
     shift = kForm == kShifted ? (int)((row * ld) & (E - 1)) : 0;
-    from = reinterpret_cast<const T*>(x) + row * ld - shift + t * E;
-    ring = place + t * (int)(E * sizeof(T));
+    from = reinterpret_cast<const T*>(x) + row * ld - shift + t * E + sub * stride;
+    ring = place + me.thread * (int)(E * sizeof(T));
     // what lies beyond the row is zero, once: nothing is ever fetched to there
     Vec<T, E> zero;
     zero.clear();
@@ -218,16 +237,16 @@ struct RowsAhead {
     return kForm == kShifted ? column(v) >= 0 && column(v) + E <= dim : column(v) < dim;
   }
   __device__ __forceinline__ char* at(int row, int v) const {
-    return ring + (row * NV + v) * lanes * (int)(E * sizeof(T));
+    return ring + (row * NV + v) * threads * (int)(E * sizeof(T));
   }
   __device__ __forceinline__ void fetch(int n, int batch) {
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      if (k >= n) break;
+      if (k * at_once + sub >= n) break;
 #pragma unroll
       for (int v = 0; v < NV; ++v) {
         if (column(v) < dim) {
-          const T* p = from + v * lanes * E;
+          const T* p = from + k * at_once * stride + v * lanes * E;
           if constexpr (E > 1)  // nothing past the row is read, zeros take its place
             asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(
                              (uint32_t)__cvta_generic_to_shared(at(batch * R + k, v))),
@@ -237,8 +256,8 @@ struct RowsAhead {
             next[k][v] = load_once<T, E>(p);
         }
       }
-      from += stride;
     }
+    from += n * stride;
   }
   // Row k of a batch as pairs, zeros outside the row.  Where the batch has no row k: of an earlier one, or anything.
   __device__ __forceinline__ void values(F2 (&out)[NV * E / 2], int k, int batch) const {
@@ -327,26 +346,27 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
   constexpr bool kCta = kKind >= kShortTeam, kRing = E > 1;
   extern __shared__ __align__(16) char ring[];
   __shared__ float slots[4][32][R];
-  const int lanes = kCta ? blockDim.x : 32;
-  const int t = kCta ? threadIdx.x : (threadIdx.x & 31);
+  const Place me(kCta, kKind == kWarp8, p.log_lanes);
+  const int t = me.t, batch = R * me.at_once;
   const int worker = kCta ? blockIdx.x : blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
   if (worker >= (kForm == kShifted ? p.parts << p.log_classes : p.parts)) return;
   const Mine<kForm == kShifted> m(p, worker);
   Batches<Mine<kForm == kShifted>> ahead(m);
   const int64_t r = m.row(m.below(m.lo));
-  RowsAhead<T, kForm, NV, R> rows(x, r, p.stride_x, m.log_classes(), ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes),
-                              lanes, t, p.dim);
+  RowsAhead<T, kForm, NV, R> rows(x, r, p.stride_x, m.log_classes(),
+                                  ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes), me, p.dim);
   const bool ragged = rows.has_outside();
-  T* out = reinterpret_cast<T*>(p.y) + r * p.stride_y - rows.shift + t * E;
+  const int64_t out_stride = p.stride_y << m.log_classes();
+  T* out = reinterpret_cast<T*>(p.y) + r * p.stride_y - rows.shift + t * E + me.sub * out_stride;
   // n[0]: rows of the batch at work, n[1]: of the one after it
   int n[2];
-  n[0] = ahead.size(R);
+  n[0] = ahead.size(batch);
   rows.fetch(n[0], 0);
   ahead.take(m, n[0]);
   n[1] = 0;
   if constexpr (kRing) {
     close_batch();
-    n[1] = ahead.size(R);
+    n[1] = ahead.size(batch);
     rows.fetch(n[1], 1);
     close_batch();
     ahead.take(m, n[1]);
@@ -376,11 +396,11 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
         sum[k] = s.sum();
       }
       // the batch after the next: into the places of the one before this, or the registers that were just emptied
-      const int more = ahead.size(R);
+      const int more = ahead.size(batch);
       rows.fetch(more, at == 0 ? 2 : at - 1);
       if constexpr (kRing) close_batch();
       ahead.take(m, more);
-      worker_sum<R, kCta>(sum, slots[phase]);
+      worker_sum<R, kCta>(sum, slots[phase], me.lanes);
       float sq[R];
 #pragma unroll
       for (int k = 0; k < R; ++k) {
@@ -394,23 +414,23 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
         for (int j = 0; j < K / 2; ++j) q = fma(cur[k][j], cur[k][j], q);
         sq[k] = q.sum();
       }
-      worker_sum<R, kCta>(sq, slots[phase + 1]);
+      worker_sum<R, kCta>(sq, slots[phase + 1], me.lanes);
       phase ^= 2;
 #pragma unroll
       for (int k = 0; k < R; ++k) {
-        if (k >= n[0]) continue;
+        if (k * me.at_once + me.sub >= n[0]) continue;
         const float rstd = rsqrtf(sq[k] * p.inv_dim + p.eps);
         const F2 scale(rstd);
         float y[K];
 #pragma unroll
         for (int j = 0; j < K / 2; ++j) fma(cur[k][j] * scale, w[j], b[j]).get(y[2 * j], y[2 * j + 1]);
-        rows.store(out, y);
-        out += p.stride_y << m.log_classes();
+        rows.store(out + k * me.at_once * out_stride, y);
         if (mean != nullptr && t == 0) {
-          mean[(int64_t)k << m.log_classes()] = sum[k];
-          rstds[(int64_t)k << m.log_classes()] = rstd;
+          mean[(k * me.at_once + me.sub) << m.log_classes()] = sum[k];
+          rstds[(k * me.at_once + me.sub) << m.log_classes()] = rstd;
         }
       }
+      out += n[0] * out_stride;
       if (mean != nullptr) {
         mean += (int64_t)n[0] << m.log_classes();
         rstds += (int64_t)n[0] << m.log_classes();
@@ -438,31 +458,32 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
   constexpr bool kCta = kKind >= kShortTeam, kRing = E > 1;
   extern __shared__ __align__(16) char ring[];
   __shared__ float slots[2][32][2 * R];
-  const int lanes = kCta ? blockDim.x : 32;
-  const int t = kCta ? threadIdx.x : (threadIdx.x & 31);
+  const Place me(kCta, kKind == kWarp8, p.log_lanes);
+  const int t = me.t, batch = R * me.at_once;
   const int worker = kCta ? blockIdx.x : blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
   if (worker >= (kForm == kShifted ? p.parts << p.log_classes : p.parts)) return;
   const Mine<kForm == kShifted> m(p, worker);
   Batches<Mine<kForm == kShifted>> ahead(m);
   const int64_t r = m.row(m.below(m.lo));
   char* place = ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes);
-  RowsAhead<T, kForm, NV, R> xs(x, r, p.stride_x, m.log_classes(), place, lanes, t, p.dim);
-  RowsAhead<T, kForm, NV, R> ys(p.dy, r, p.stride_y, m.log_classes(), place + p.ring_half, lanes, t, p.dim);
-  T* out = reinterpret_cast<T*>(p.y) + r * p.stride_x - xs.shift + t * E;
+  RowsAhead<T, kForm, NV, R> xs(x, r, p.stride_x, m.log_classes(), place, me, p.dim);
+  RowsAhead<T, kForm, NV, R> ys(p.dy, r, p.stride_y, m.log_classes(), place + p.ring_half, me, p.dim);
+  T* out = reinterpret_cast<T*>(p.y) + r * p.stride_x - xs.shift + t * E + me.sub * xs.stride;
   // a thread's weights, four from place to place of the threads: but for plain rows there are no registers for them
-  float4* ws = reinterpret_cast<float4*>(place + p.ring_bytes - lanes * K * 4) + t;
+  float4* ws = reinterpret_cast<float4*>(place + p.ring_bytes - me.threads * K * 4) + me.thread;
   float mean[R], rstd[R];  // of the next batch, whose first row is row_ahead
   int64_t row_ahead = r;
   auto stats = [&](int n) {
 #pragma unroll
     for (int k = 0; k < R; ++k) {
-      mean[k] = k < n ? p.mean_in[row_ahead + (k << m.log_classes())] : 0.0f;
-      rstd[k] = k < n ? p.rstd_in[row_ahead + (k << m.log_classes())] : 0.0f;
+      const int row = k * me.at_once + me.sub;
+      mean[k] = row < n ? p.mean_in[row_ahead + (row << m.log_classes())] : 0.0f;
+      rstd[k] = row < n ? p.rstd_in[row_ahead + (row << m.log_classes())] : 0.0f;
     }
     row_ahead += n << m.log_classes();
   };
   int n[2];
-  n[0] = ahead.size(R);
+  n[0] = ahead.size(batch);
   xs.fetch(n[0], 0);
   ys.fetch(n[0], 0);
   stats(n[0]);
@@ -470,7 +491,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
   n[1] = 0;
   if constexpr (kRing) {
     close_batch();
-    n[1] = ahead.size(R);
+    n[1] = ahead.size(batch);
     xs.fetch(n[1], 1);
     ys.fetch(n[1], 1);
     close_batch();
@@ -489,7 +510,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
         float4 four;
         w[2 * j].get(four.x, four.y);
         w[2 * j + 1].get(four.z, four.w);
-        ws[j * lanes] = four;
+        ws[j * me.threads] = four;
       }
     }
 #pragma unroll
@@ -507,14 +528,14 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
         xs.values(xh[k], k, at);
         ys.values(a[k], k, at);
         sum[2 * k] = sum[2 * k + 1] = 0.0f;
-        if (R > 1 && k >= n[0]) continue;
+        if ((R > 1 || me.at_once > 1) && k * me.at_once + me.sub >= n[0]) continue;
         F2 s0(0.0f), s1(0.0f);
         float4 four;
 #pragma unroll
         for (int j = 0; j < K / 2; ++j) {
           const F2 dy = a[k][j];
           if constexpr (kForm != kPlain) {
-            if (j % 2 == 0) four = ws[j / 2 * lanes];
+            if (j % 2 == 0) four = ws[j / 2 * me.threads];
             w[j] = j % 2 == 0 ? F2(four.x, four.y) : F2(four.z, four.w);
           }
           xh[k][j] = (xh[k][j] + minus) * scale[k];
@@ -527,24 +548,24 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
         sum[2 * k] = s0.sum();
         sum[2 * k + 1] = s1.sum();
       }
-      const int more = ahead.size(R);
+      const int more = ahead.size(batch);
       xs.fetch(more, at == 0 ? 2 : at - 1);
       ys.fetch(more, at == 0 ? 2 : at - 1);
       if constexpr (kRing) close_batch();
       ahead.take(m, more);
       stats(kRing ? n[1] : more);
-      worker_sum<2 * R, kCta>(sum, slots[phase]);
+      worker_sum<2 * R, kCta>(sum, slots[phase], me.lanes);
       phase ^= 1;
 #pragma unroll
       for (int k = 0; k < R; ++k) {
-        if (k >= n[0]) continue;
+        if (k * me.at_once + me.sub >= n[0]) continue;
         const F2 c0(-sum[2 * k] * p.inv_dim), c1(-sum[2 * k + 1] * p.inv_dim);
         float dx[K];
 #pragma unroll
         for (int j = 0; j < K / 2; ++j) (scale[k] * fma(xh[k][j], c1, a[k][j] + c0)).get(dx[2 * j], dx[2 * j + 1]);
-        xs.store(out, dx);
-        out += p.stride_x << m.log_classes();
+        xs.store(out + k * me.at_once * xs.stride, dx);
       }
+      out += n[0] * xs.stride;
       left -= n[0];
       if constexpr (kRing) {
         n[0] = n[1];
@@ -561,10 +582,18 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
         float a[2], c[2];
         dw[j / 2].get(a[0], a[1]);
         db[j / 2].get(c[0], c[1]);
+        if constexpr (kKind == kWarp8) {
+          for (int o = me.lanes; o < 32; o *= 2) {  // of the rows that the warp has at once
+            a[0] += __shfl_xor_sync(0xffffffffu, a[0], o);
+            a[1] += __shfl_xor_sync(0xffffffffu, a[1], o);
+            c[0] += __shfl_xor_sync(0xffffffffu, c[0], o);
+            c[1] += __shfl_xor_sync(0xffffffffu, c[1], o);
+          }
+        }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int col = xs.column((j + i) / E) + (j + i) % E;
-          if (col >= 0 && col < p.dim) {
+          if (me.sub == 0 && col >= 0 && col < p.dim) {
             mine[col] = a[i];
             mine[p.dim + col] = c[i];
           }
@@ -574,17 +603,20 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
   }
 }
 
-// Adds the slots of each group.  A CTA has 32 columns of one group; its 32 warps take every 32nd slot each and meet in
-// shared memory, so the order is the same whatever runs when.
+// Adds the slots of each group.  A CTA has kWeightColumns columns of one group; its threads take every 128th (32nd) slot
+// each and meet in shared memory, so the order is the same whatever runs when.  32 columns read whole lines; with eight,
+// narrow rows too have enough CTAs (70000 x 64 backward: 13.6 us, 21.3 with 32; 10000 x 8192: 112 us, 106 with 32).
+template <int kWeightColumns>
 __global__ void __launch_bounds__(1024) norm_weights_kernel(const float* partial, int64_t rows, int64_t rows_per_group,
                                                             int64_t parts, int log_classes, int dim,
                                                             void* dweight, void* dbias, int dtype) {
   enter_grid(partial);
-  __shared__ float s[2][32][33];
-  const int tiles = (dim + 31) / 32;
+  constexpr int kSlots = 1024 / kWeightColumns;
+  __shared__ float s[2][kWeightColumns][33];
+  const int tiles = (dim + kWeightColumns - 1) / kWeightColumns;
   const int64_t g = blockIdx.x / tiles;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int first = (blockIdx.x % tiles) * 32, col = first + lane;
+  const int first = (blockIdx.x % tiles) * kWeightColumns, col = first + lane % kWeightColumns;
   float sw = 0.0f, sb = 0.0f;
   if (rows > 0) {
     // parts with rows of this group: from the one that has the group's first row to the one that has its last
@@ -594,35 +626,42 @@ __global__ void __launch_bounds__(1024) norm_weights_kernel(const float* partial
     const int64_t w0 = lo < cut ? lo / (q + 1) : m + (lo - cut) / q;
     const int64_t w1 = hi < cut ? hi / (q + 1) : m + (hi - cut) / q;
     if (col < dim) {
-      const float* slot = partial + (((w0 + g) << log_classes) + warp) * 2 * dim + col;
+      const int mine = threadIdx.x / kWeightColumns;
+      const float* slot = partial + (((w0 + g) << log_classes) + mine) * 2 * dim + col;
 #pragma unroll 4
-      for (int left = (int)((w1 - w0 + 1) << log_classes) - warp; left > 0; left -= 32, slot += (int64_t)64 * dim) {
+      for (int left = (int)((w1 - w0 + 1) << log_classes) - mine; left > 0;
+           left -= kSlots, slot += (int64_t)2 * kSlots * dim) {
         sw += slot[0];
         sb += slot[dim];
       }
     }
   }
-  s[0][lane][warp] = sw;
-  s[1][lane][warp] = sb;
-  __syncthreads();
-  // a warp adds what the warps have of column `first + warp`
-  float v[2] = {s[0][warp][lane], s[1][warp][lane]};
-  const int mine = first + warp;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
-    v[1] += __shfl_xor_sync(0xffffffffu, v[1], o);
+  for (int o = kWeightColumns; o < 32; o *= 2) {
+    sw += __shfl_xor_sync(0xffffffffu, sw, o);
+    sb += __shfl_xor_sync(0xffffffffu, sb, o);
   }
-  void* to = lane == 0 ? dweight : dbias;
-  if (lane < 2 && mine < dim && to != nullptr) {
-    const int64_t at = g * dim + mine;
-    const float x = lane == 0 ? v[0] : v[1];
-    if (dtype == SPARSP_FP32)
-      reinterpret_cast<float*>(to)[at] = x;
-    else if (dtype == SPARSP_FP16)
-      reinterpret_cast<__half*>(to)[at] = __float2half_rn(x);
-    else
-      reinterpret_cast<__nv_bfloat16*>(to)[at] = __float2bfloat16_rn(x);
+  if (lane < kWeightColumns) {
+    s[0][lane][warp] = sw;
+    s[1][lane][warp] = sb;
+  }
+  __syncthreads();
+  // a warp adds what the warps have of a column of dweight or dbias
+  for (int i = warp; i < 2 * kWeightColumns; i += 32) {
+    const int which = i / kWeightColumns, at_col = i % kWeightColumns, mine = first + at_col;
+    float v = s[which][at_col][lane];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    void* to = which == 0 ? dweight : dbias;
+    if (lane == 0 && mine < dim && to != nullptr) {
+      const int64_t at = g * dim + mine;
+      if (dtype == SPARSP_FP32)
+        reinterpret_cast<float*>(to)[at] = v;
+      else if (dtype == SPARSP_FP16)
+        reinterpret_cast<__half*>(to)[at] = __float2half_rn(v);
+      else
+        reinterpret_cast<__nv_bfloat16*>(to)[at] = __float2bfloat16_rn(v);
+    }
   }
 }
 
@@ -636,7 +675,7 @@ int64_t norm_groups(const sparsp_norm& n) {
 struct NormPlan {
   int form, kind, threads;                // threads of a CTA
   int ring_bytes, ring_half, smem_bytes;  // of a worker, where dy's begins, of a CTA
-  int parts, log_classes;
+  int parts, log_classes, log_lanes;
   unsigned grid;
 };
 
@@ -657,6 +696,8 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
     const int units = (n.dim + (p.log_classes > 0 ? E - 1 : 0) + E - 1) / E, span = units * E;
     p.kind = span <= 256 ? kWarp8 : span <= 512 ? kWarp16 : span <= 5120 ? kTeam : span <= 8192 ? kLongTeam : kLongestTeam;
     if (p.kind == kTeam && span <= 2048 && bwd && bytes == 4) p.kind = kShortTeam;
+    p.log_lanes = 2;
+    while (p.log_lanes < 5 && (8 << p.log_lanes) < span) ++p.log_lanes;
     const bool cta = p.kind >= kShortTeam;
     const int per_thread = worker_values(p.kind) / E;
     p.threads = cta ? ((units + per_thread - 1) / per_thread + 31) / 32 * 32 : kNormThreads;
@@ -672,7 +713,8 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
       continue;
     }
     const int resident = std::min({32, 65536 / (p.threads * worker_registers(p.kind)), kNormSmem / (p.smem_bytes + 4096)});
-    const int64_t most = std::min<int64_t>(n.rows, (int64_t)kSms * resident * workers);
+    const int64_t rows = p.kind == kWarp8 ? (n.rows + (32 >> p.log_lanes) - 1) >> (5 - p.log_lanes) : n.rows;
+    const int64_t most = std::min<int64_t>(rows, (int64_t)kSms * resident * workers);
     p.parts = (int)std::max<int64_t>(1, most >> p.log_classes);
     const int all = p.parts << p.log_classes;
     p.grid = (unsigned)((all + workers - 1) / workers);
@@ -740,6 +782,7 @@ static NormParams norm_params(const sparsp_norm& n, const NormPlan& plan) {
   p.weights_fp32 = n.weight_dtype == SPARSP_FP32;
   p.parts = plan.parts;
   p.log_classes = plan.log_classes;
+  p.log_lanes = plan.log_lanes;
   p.ring_bytes = plan.ring_bytes;
   p.ring_half = plan.ring_half;
   p.eps = n.eps;
@@ -778,9 +821,12 @@ int launch_norm_bwd(const sparsp_norm& n, const void* dY, const void* X, const v
     SPARSP_CUDA_OK(launch_norm(n.dtype, p, plan, true, st));
   }
   if (p.want_weights && norm_groups(n) > 0) {
-    const unsigned grid = (unsigned)(norm_groups(n) * ((n.dim + 31) / 32));
-    SPARSP_CUDA_OK(launch_kernel(norm_weights_kernel, dim3(grid), 1024, 0, st, p.partial, n.rows, p.rows_per_group,
-                                 (int64_t)plan.parts, plan.log_classes, n.dim, dw, db, n.weight_dtype));
+    const bool wide = norm_groups(n) * ((n.dim + 31) / 32) >= 100;
+    const int columns = wide ? 32 : 8;
+    const unsigned grid = (unsigned)(norm_groups(n) * ((n.dim + columns - 1) / columns));
+    SPARSP_CUDA_OK(launch_kernel(wide ? norm_weights_kernel<32> : norm_weights_kernel<8>, dim3(grid), 1024, 0, st,
+                                 p.partial, n.rows, p.rows_per_group, (int64_t)plan.parts, plan.log_classes, n.dim, dw,
+                                 db, n.weight_dtype));
   }
   return SPARSP_OK;
 }
