@@ -1,0 +1,158 @@
+"""The token-wise operators where their work is shared out differently: rows in classes, few rows, groups smaller than a
+class, tiles whose K is shared, few tokens, and calls between the caller's own kernels.  Bounds as in the operators' own
+tests."""
+import pytest
+import torch
+
+import test_gpu_gated_ffn as ffn_tests
+from layer_reference import F32, TINY, UNIT, close, layer_norm, layer_norm_back
+from paper_2609_32197_b200 import binding
+from test_gpu_layer_norm import EPS, fwd_bounds, inputs
+
+pytestmark = pytest.mark.gpu
+BF, HF, FL = torch.bfloat16, torch.float16, torch.float32
+
+
+def check_norm(x, w, b, dy, per, groups, norm, y, dx):
+    rows, dim, dtype, wtype = *x.shape, x.dtype, w.dtype
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    binding.sparsp_layer_norm_fwd(norm, x, w, b, y, mean, rstd)
+    want, m, r = layer_norm(x.double(), w.double(), b.double(), EPS, per)
+    by, bm, br = fwd_bounds(x.double(), w.double(), want, m, r, per, dtype)
+    close(y, want, by, "y")
+    close(mean, m, bm, "mean")
+    close(rstd, r, br, "rstd")
+    ws = binding.make_norm_workspace(norm)
+    ws[256:].fill_(255)
+    dw, db = torch.full_like(w, float("nan")), torch.full_like(w, float("nan"))
+    binding.sparsp_layer_norm_bwd(norm, dy, x, w, mean, rstd, dx, dw, db, ws)
+    X, W, DY, M, R = x.double(), w.double(), dy.double(), mean.double(), rstd.double()
+    want, want_w, want_b = layer_norm_back(DY, X, W, M, R, per, groups)
+    g = torch.arange(rows, device="cuda") // per
+    xh = ((X - M[:, None]) * R[:, None]).abs()
+    exh = 3 * F32 * (xh + (X.abs() + M[:, None].abs()) * R[:, None])
+    a = (DY * W[g]).abs()
+    c0, c1 = 52 * F32 * a.mean(1, keepdim=True), (a * exh + 54 * F32 * a * xh).mean(1, keepdim=True)
+    off = R[:, None] * (4 * F32 * a + c0 + xh * c1 + (exh + 4 * F32 * xh) * (a * xh).mean(1, keepdim=True)) + 4 * F32 * want.abs()
+    close(dx, want, off + UNIT[dtype] * (want.abs() + off) + TINY[dtype], "dx")
+    n = min(rows, 64 + rows // 148)
+    for got, ref, terms, what in ((dw, want_w, DY.abs() * (xh + exh / F32 / n), "dw"), (db, want_b, DY.abs(), "db")):
+        off = (n + 20) * F32 * torch.zeros_like(W).index_add_(0, g, terms)
+        close(got, ref, off + UNIT[wtype] * (ref.abs() + off) + TINY[wtype], what)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF, FL])
+@pytest.mark.parametrize("dim", [2, 7, 9, 31, 33, 63, 64, 65, 100, 127, 129, 250, 255, 257, 263, 505, 511, 513, 1021, 2045, 2050])
+def test_widths_around_every_edge(dim, dtype):
+    for rows, groups in ((1, 1), (3, 3), (5, 1), (13, 5), (97, 4), (2500, 3)):
+        if rows * dim > 1500000:
+            continue
+        per = -(-rows // groups)
+        groups = -(-rows // per)
+        x, w, b, dy = inputs(rows, dim, groups, dtype, FL, seed=rows)
+        norm = binding.make_norm(rows, dim, per, EPS, dtype, FL)
+        check_norm(x, w, b, dy, per, groups, norm, torch.full_like(x, float("nan")), torch.full_like(x, float("nan")))
+
+
+@pytest.mark.parametrize("dtype,dim", [(BF, 5113), (BF, 5127), (HF, 8185), (HF, 8193), (FL, 4999), (FL, 8189), (BF, 16383),
+                                       (FL, 9001)])
+def test_long_rows_of_odd_length(dtype, dim):
+    x, w, b, dy = inputs(19, dim, 2, dtype, dtype, seed=3)
+    norm = binding.make_norm(19, dim, 10, EPS, dtype, dtype)
+    check_norm(x, w, b, dy, 10, 2, norm, torch.full_like(x, float("nan")), torch.full_like(x, float("nan")))
+
+
+@pytest.mark.parametrize("dtype,dim,pad_x,pad_y", [(BF, 70, 2, 10), (BF, 70, 2, 3), (FL, 1000, 1, 5), (FL, 1000, 1, 2),
+                                                    (HF, 300, 4, 4), (BF, 5121, 3, 3)])
+def test_rows_with_gaps_of_their_own(dtype, dim, pad_x, pad_y):
+    """x and y with different gaps: rows that begin alike, and rows that do not; nothing outside the rows changes."""
+    rows = 41
+    x, w, b, dy = inputs(rows, dim, 1, dtype, dtype, seed=5)
+    hold = [torch.full((rows, dim + p), 7.0, dtype=dtype, device="cuda") for p in (pad_x, pad_y, pad_y, pad_x)]
+    vx, vy, vdy, vdx = (h[:, :dim] for h in hold)
+    vx.copy_(x)
+    vdy.copy_(dy)
+    norm = binding.make_norm(rows, dim, 0, EPS, dtype, dtype, stride_x=dim + pad_x, stride_y=dim + pad_y)
+    check_norm(vx, w, b, vdy, rows, 1, norm, vy, vdx)
+    assert all(bool((h[:, dim:] == 7.0).all()) for h in hold)
+
+
+@pytest.mark.parametrize("m,d,f", [
+    (3, 328, 9600), (17, 136, 4800), (33, 72, 2400), (100, 1992, 2368), (127, 64, 9480),  # few tokens, every tile height
+    (512, 4096, 2048), (300, 4096, 5000), (200, 10240, 6400),  # forward: a last round shared out, in both ways
+])
+def test_forward_shared_out(m, d, f):
+    x, wg, wu, _ = ffn_tests.inputs(m, d, f, BF, seed=7)
+    ffn = binding.make_ffn(m, d, f, "silu", BF)
+    ws = binding.make_ffn_workspace(ffn, backward=False)
+    ws[256:].fill_(255)
+    h, gate, up = (torch.full((m, f), float("nan"), dtype=BF, device="cuda") for _ in range(3))
+    before = binding.sparsp_launch_count()
+    binding.sparsp_gated_ffn_fwd(ffn, x, wg, wu, h, gate, up, ws)
+    assert binding.sparsp_launch_count() - before == (1 if m <= 128 else 2)
+    assert binding.sparsp_status(ws) == binding.SPARSP_OK
+    ffn_tests.check_forward("silu", BF, x, wg, wu, h, gate, up)
+
+
+@pytest.mark.parametrize("m,d,f", [(1003, 1160, 2504), (9, 600, 4000), (2100, 1304, 1504), (4100, 264, 520), (130, 2600, 5000),
+                                   (5000, 1032, 3080)])
+def test_backward_shared_out(m, d, f):
+    """dX and dW in one launch or one after the other, whole tiles and shared ones."""
+    x, wg, wu, dh = ffn_tests.inputs(m, d, f, BF, seed=8)
+    gate, up = x @ wg.T, x @ wu.T
+    ffn = binding.make_ffn(m, d, f, "silu", BF)
+    ws = binding.make_ffn_workspace(ffn)
+    ws[256:].fill_(255)
+    dx, dwg, dwu = (torch.full_like(t, float("nan")) for t in (x, wg, wu))
+    binding.sparsp_gated_ffn_bwd(ffn, dh, x, wg, wu, gate, up, dx, dwg, dwu, ws)
+    assert binding.sparsp_status(ws) == binding.SPARSP_OK
+    ffn_tests.check_backward("silu", BF, dh, x, wg, wu, gate, up, dx, dwg, dwu)
+    dx2, dwg2, dwu2 = torch.empty_like(dx), torch.empty_like(dwg), torch.empty_like(dwu)
+    binding.sparsp_gated_ffn_bwd(ffn, dh, None, wg, wu, gate, up, dx2, None, None, ws)
+    binding.sparsp_gated_ffn_bwd(ffn, dh, x, None, None, gate, up, None, dwg2, dwu2, ws)
+    assert torch.equal(dx2, dx) and torch.equal(dwg2, dwg) and torch.equal(dwu2, dwu)
+
+
+def test_between_the_callers_own_kernels():
+    """Inputs written right before a call and outputs read and overwritten right after it, on a stream of the caller's."""
+    m, d, f = 260, 264, 520
+    x0, wg, wu, dh = ffn_tests.inputs(m, d, f, BF, seed=9)
+    ffn, norm = binding.make_ffn(m, d, f), binding.make_norm(m, d)
+    ws, nws = binding.make_ffn_workspace(ffn), binding.make_norm_workspace(norm)
+    w = torch.ones(1, d, dtype=BF, device="cuda")
+
+    def chain(x):
+        n, mean, rstd = torch.empty_like(x), torch.empty(m, device="cuda"), torch.empty(m, device="cuda")
+        h, gate, up = (torch.empty(m, f, dtype=BF, device="cuda") for _ in range(3))
+        dx, dwg, dwu, dn, dw, db = (torch.empty_like(t) for t in (x, wg, wu, x, w, w))
+        z = x * 1.0
+        binding.sparsp_layer_norm_fwd(norm, z, w, w, n, mean, rstd)
+        z.zero_()
+        n2 = n + 0
+        n.zero_()
+        binding.sparsp_gated_ffn_fwd(ffn, n2, wg, wu, h, gate, up, ws)
+        g2, u2 = gate + 0, up + 0
+        gate.zero_()
+        up.zero_()
+        binding.sparsp_gated_ffn_bwd(ffn, dh, n2, wg, wu, g2, u2, dx, dwg, dwu, ws)
+        g2.zero_()
+        n2.zero_()
+        dx2 = dx + 0
+        dx.zero_()
+        z.copy_(x)
+        binding.sparsp_layer_norm_bwd(norm, dx2, z, w, mean, rstd, dn, dw, db, nws)
+        dx2.zero_()
+        return [t + 0 for t in (h, dwg, dwu, dn, dw, db)]
+
+    want = []
+    for k in range(3):
+        want.append(chain(x0 * (k + 1)))
+        torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(10):
+            for k in range(3):
+                got = chain(x0 * (k + 1))
+                assert all(torch.equal(a, b) for a, b in zip(got, want[k]))
+    torch.cuda.current_stream().wait_stream(side)
