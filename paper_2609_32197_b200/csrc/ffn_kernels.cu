@@ -26,6 +26,7 @@ struct GemmParams {
   int32_t rows, cols;     // of the result (kForward: tokens, hidden; kInput: tokens, dim; kWeights: hidden, dim)
   int32_t m_tiles, n_tiles, band;
   int32_t whole, shares;  // see Walk
+  int32_t alternate;      // half the warps of a CTA take every other tile's results
   int32_t k_blocks;       // of 64, of one (A, B); kInput has two of them
   int32_t activation;
   uint32_t idesc;
@@ -51,25 +52,32 @@ struct GemmCfg {
   static constexpr int kDynamic = kBytes + 1024;  // the tiles are aligned to 1024 bytes
 };
 
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.0f, 1.0f + __expf(-x)); }
-constexpr float kTanhA = 2.0f * 0.7978845608028654f, kTanhB = 0.044715f;  // (1 + tanh(u)) / 2 = sigmoid(2u)
+// 1 / (1 + 2^t): with t = -x log2 e, the logistic function of x.  Far out on either side it is 1 or 0.
+__device__ __forceinline__ float logistic2(float t) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.0f + ptx::ex2(t)));
+  return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kTanhA = 2.0f * 0.7978845608028654f, kTanhB = 0.044715f;  // (1 + tanh(u)) / 2 = logistic(2 u)
 
 // a(x), and a(x) with a'(x).  The kind is chosen once for many values: chosen value by value it kept their exponentials
 // and reciprocals from overlapping, and a tile's results took 4.1 us.
 template <int kKind>
 __device__ __forceinline__ float activate(float x) {
-  if constexpr (kKind == SPARSP_ACT_SILU) return x * sigmoid(x);
-  if constexpr (kKind == SPARSP_ACT_GELU_TANH) return x * sigmoid(kTanhA * (x + kTanhB * x * x * x));
+  if constexpr (kKind == SPARSP_ACT_SILU) return x * logistic2(-kLog2e * x);
+  if constexpr (kKind == SPARSP_ACT_GELU_TANH)
+    return x * logistic2(x * fmaf(x * x, -kLog2e * kTanhA * kTanhB, -kLog2e * kTanhA));
   return x * 0.5f * (1.0f + erff(x * 0.70710678118654752f));
 }
 template <int kKind>
 __device__ __forceinline__ void activate(float x, float& a, float& slope) {
   if constexpr (kKind == SPARSP_ACT_SILU) {
-    const float s = sigmoid(x);
+    const float s = logistic2(-kLog2e * x);
     a = x * s;
     slope = s * (1.0f + x * (1.0f - s));
   } else if constexpr (kKind == SPARSP_ACT_GELU_TANH) {
-    const float s = sigmoid(kTanhA * (x + kTanhB * x * x * x));
+    const float s = logistic2(x * fmaf(x * x, -kLog2e * kTanhA * kTanhB, -kLog2e * kTanhA));
     a = x * s;
     const float t = s * (1.0f - s);
     slope = t == 0.0f ? s : s + x * t * kTanhA * (1.0f + 3.0f * kTanhB * x * x);  // far out x * x may be infinite
@@ -197,7 +205,7 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(acc_full + a, 1);
-      mbar_init(acc_empty + a, 2 * kEpilogueWarps);
+      mbar_init(acc_empty + a, p.alternate ? kEpilogueWarps : 2 * kEpilogueWarps);
     }
     *s_abort = 0;
     mbar_init_fence();
@@ -308,28 +316,42 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
       }
     }
   } else {
-    // ---- results: warp w has the lanes of quarter w % 4, and a fourth of the columns ----
-    const int quarter = warp & 3, side = warp >> 2;
+    // ---- results: warp w has the lanes of quarter w % 4, and a share of the columns ----
+    // With one tile or two a pair, all warps do each; with more, eight warps do one tile while eight do the next, so that
+    // one tile's loads and stores fill the time of the other's exponentials (2825 x 96 x 5456: 23 us all together).
+    const int quarter = warp & 3, sides = p.alternate ? 2 : 4, side = (warp >> 2) % sides;
+    const int turn = p.alternate ? warp >> 3 : -1;
     uint8_t* mine = smem + C::kOffOut + warp * 2048;
-    int acc = 0;
-    uint32_t acc_round = 0;
+    int acc = 1;
+    uint32_t acc_round = 1;
     const uint32_t even0 = cluster_addr(acc_empty, 0), even1 = cluster_addr(acc_empty + 1, 0);
     while (walk.next()) {
+      acc ^= 1;
+      if (acc == 0) acc_round ^= 1u;
+      if (turn == (acc ^ 1)) continue;
       int m, n;
       tile_at(p, walk.tile, m, n);
       mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 4, p.wait_limit);
       if (*s_abort) break;
       tc_fence_after();
       const uint32_t from = tmem + acc * BN + ((uint32_t)(quarter * 32) << 16);
+      // after a warp's last load: the next product may have these columns while it is still busy with the values
+      auto release = [&](bool last) {
+        if (!last) return;
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(acc == 0 ? even0 : even1);
+      };
       const int in_tile = (int)rank * kTileRows + quarter * 32 + lane;
       if (walk.slot >= 0) {
         // [slot][BN / 4][256 rows] of four columns: lanes are rows, so a warp writes 512 bytes in a piece
         float4* to = reinterpret_cast<float4*>(p.partial) + (int64_t)walk.slot * (BN / 4) * 256 + in_tile;
 #pragma unroll 1
-        for (int c = side * (BN / 4); c < (side + 1) * (BN / 4); c += 32) {
+        for (int c = side * (BN / sides); c < (side + 1) * (BN / sides); c += 32) {
           uint32_t r[32];
           tmem_ld32(from + c, r);
           tmem_ld_wait(r);
+          release(c + 32 == (side + 1) * (BN / sides));
 #pragma unroll
           for (int e = 0; e < 8; ++e)
             to[(c / 4 + e) * 256] = make_float4(__uint_as_float(r[4 * e]), __uint_as_float(r[4 * e + 1]),
@@ -338,12 +360,13 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
       } else if constexpr (kMode == kForward) {
         const int row = m * 256 + (int)rank * kTileRows + quarter * 32;
 #pragma unroll 1
-        for (int c = side * (BN / 8); c < (side + 1) * (BN / 8); c += 32) {
+        for (int c = side * (BN / 2 / sides); c < (side + 1) * (BN / 2 / sides); c += 32) {
           float g[32], u[32];
           tmem_ld32(from + c, reinterpret_cast<uint32_t*>(g));
           tmem_ld32(from + BN / 2 + c, reinterpret_cast<uint32_t*>(u));
           tmem_ld_wait(g);
           tmem_ld_wait(u);
+          release(c + 32 == (side + 1) * (BN / 2 / sides));
           const int col = n * (BN / 2) + c;
           if (p.keep[0] != nullptr) {
             write_out<T>(&o1, mine, g, lane, col, row, p.cols, p.rows);
@@ -357,18 +380,14 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
         const bool second = kMode == kWeights && m >= half_m;
         const int row = (second ? m - half_m : m) * 256 + (int)rank * kTileRows + quarter * 32;
 #pragma unroll 1
-        for (int c = side * (BN / 4); c < (side + 1) * (BN / 4); c += 32) {
+        for (int c = side * (BN / sides); c < (side + 1) * (BN / sides); c += 32) {
           float x[32];
           tmem_ld32(from + c, reinterpret_cast<uint32_t*>(x));
           tmem_ld_wait(x);
+          release(c + 32 == (side + 1) * (BN / sides));
           write_out<T>(second ? &o1 : &o0, mine, x, lane, n * BN + c, row, p.cols, p.rows);
         }
       }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive_cluster(acc == 0 ? even0 : even1);
-      acc ^= 1;
-      if (acc == 0) acc_round ^= 1u;
     }
     if (lane == 0) tma_store_wait();
   }
@@ -781,6 +800,7 @@ static void share_out(GemmParams* p, int pairs, int shares) {
   const int tiles = p->m_tiles * p->n_tiles;
   p->whole = shares > 0 ? tiles / pairs * pairs : tiles;
   p->shares = shares;
+  p->alternate = tiles >= 3 * pairs;
 }
 
 // What every product needs beside its sizes.
