@@ -475,7 +475,8 @@ typedef struct sparsp_norm {
  *   weight, bias in   [groups][dim] contiguous; each may be NULL (1, 0)
  *   Y            out  row stride stride_y; may be X itself when the strides are equal
  *   mean, rstd   out  fp32 [rows], for the backward pass; both or neither may be NULL
- * Data pointers are aligned to their element type; rows that are 16-byte aligned and a multiple of 16 bytes are faster. */
+ * Data pointers are aligned to their element type.  Tensors that begin on 16 bytes, with stride_x and stride_y equal or a
+ * multiple of 16 bytes apart, are several times faster than others. */
 SPARSP_API int sparsp_layer_norm_fwd(const sparsp_norm* norm, const void* X, const void* weight, const void* bias,
                                      void* Y, float* mean, float* rstd, void* stream);
 
@@ -502,8 +503,8 @@ typedef struct sparsp_ffn {
   int32_t activation;    /* SPARSP_ACT_* */
 } sparsp_ffn;
 
-/* Bytes of workspace that the forward call (backward = 0) or the backward call needs: dG and dU for the latter, and in
- * either case 39 MB for partial sums. */
+/* Bytes of workspace that the forward call (backward = 0) or the backward call needs: dG and dU for the latter, and 39 MB
+ * for partial sums in either case, but for a forward call of up to 128 tokens. */
 SPARSP_API int sparsp_gated_ffn_workspace_bytes(const sparsp_ffn* ffn, int32_t backward, int64_t* bytes);
 
 /* Both projections, the activation and the product.  Sums in fp32; H is rounded once, from the fp32 projections.
