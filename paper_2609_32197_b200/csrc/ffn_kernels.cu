@@ -61,13 +61,28 @@ __device__ __forceinline__ float logistic2(float t) {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kTanhA = 2.0f * 0.7978845608028654f, kTanhB = 0.044715f;  // (1 + tanh(u)) / 2 = logistic(2 u)
 
+// (1 + erf(x / sqrt 2)) / 2, and e = exp(-x^2 / 2): Abramowitz and Stegun 7.1.26, erf within 1.5e-7, with the exponential
+// that the slope needs too.  The library's erff took a forward call of 16384 x 64 x 9472 217 us.
+__device__ __forceinline__ float normal_below(float x, float& e) {
+  const float z = fabsf(x) * 0.70710678118654752f;
+  e = ptx::ex2(z * z * -kLog2e);
+  float t;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(fmaf(z, 0.3275911f, 1.0f)));
+  float q = fmaf(t, 0.5f * 1.061405429f, -0.5f * 1.453152027f);
+  q = fmaf(t, q, 0.5f * 1.421413741f);
+  q = fmaf(t, q, -0.5f * 0.284496736f);
+  q = fmaf(t, q, 0.5f * 0.254829592f) * t * e;
+  return x < 0.0f ? q : 1.0f - q;
+}
+
 // a(x), and a(x) with a'(x); each within 2^-20 of |x|, which results of 8 or 11 bits do not see.
 template <int kKind>
 __device__ __forceinline__ float activate(float x) {
   if constexpr (kKind == SPARSP_ACT_SILU) return x * logistic2(-kLog2e * x);
   if constexpr (kKind == SPARSP_ACT_GELU_TANH)
     return x * logistic2(x * fmaf(x * x, -kLog2e * kTanhA * kTanhB, -kLog2e * kTanhA));
-  return x * 0.5f * (1.0f + erff(x * 0.70710678118654752f));
+  float e;
+  return x * normal_below(x, e);
 }
 template <int kKind>
 __device__ __forceinline__ void activate(float x, float& a, float& slope) {
@@ -81,9 +96,10 @@ __device__ __forceinline__ void activate(float x, float& a, float& slope) {
     const float t = s * (1.0f - s);
     slope = t == 0.0f ? s : s + x * t * kTanhA * (1.0f + 3.0f * kTanhB * x * x);  // far out x * x may be infinite
   } else {
-    const float c = 0.5f * (1.0f + erff(x * 0.70710678118654752f));
+    float e;
+    const float c = normal_below(x, e);
     a = x * c;
-    slope = c + x * 0.3989422804014327f * __expf(-0.5f * x * x);
+    slope = c + x * 0.3989422804014327f * e;
   }
 }
 // Runs f with the kind as a constant.
@@ -434,7 +450,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 // same of up) by N columns (the tokens, rounded up to 16).  A CTA has F features at a time, F as small as shares the hidden
 // size out evenly; the MMA takes 128 rows all the same, and those past 2 F are whatever lies behind in shared memory and
 // are never read.  Gate and up of a feature are in different lanes, so they meet in shared memory, where the order turns
-// to tokens by features for the store.
+// to tokens by features for the store.  Where there are so few features that most SMs would have none, a cluster of CTAs
+// shares out K for each tile, and each adds a part of the results from the others' shared memory.
 struct FewParams {
   void* out;
   void* keep[2];
@@ -442,6 +459,7 @@ struct FewParams {
   int32_t tokens, hidden;
   int32_t features, columns;  // of a tile: F, N
   int32_t tiles, k_blocks, stages, stage_bytes, ld_turn;
+  int32_t splits;  // CTAs of a cluster that share out K; each then has one tile at most
   int32_t activation;
   uint32_t idesc;
   int32_t* status;
@@ -489,20 +507,22 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   const uint32_t tmem = tmem_slot;
   wait_previous_grids();
   const int F = p.features, N = p.columns;
+  const int rank = (int)cluster_rank(), first_tile = blockIdx.x / p.splits, step = gridDim.x / p.splits;
+  const int k0 = p.k_blocks * rank / p.splits, k1 = p.k_blocks * (rank + 1) / p.splits;
 
   if (warp == 0) {
     if (elect_one()) {
       int s = 0;
       uint32_t round = 0;
       const int block = (2 * F + N) * 128;
-      for (int tile = blockIdx.x; tile < p.tiles && !*s_abort; tile += gridDim.x) {
-        for (int k = 0; k < p.k_blocks; k += kDeep) {
+      for (int tile = first_tile; tile < p.tiles && !*s_abort; tile += step) {
+        for (int k = k0; k < k1; k += kDeep) {
           if (!mbar_try_wait(empty + s, round ^ 1u)) {
             mbar_wait_bounded_inline(empty + s, round ^ 1u, s_abort, 11, p.wait_limit);
             if (*s_abort) break;
           }
           uint8_t* at = smem + s * p.stage_bytes;
-          const int n = min(kDeep, p.k_blocks - k);
+          const int n = min(kDeep, k1 - k);
           mbar_expect_tx(full + s, n * block);
 #pragma unroll
           for (int q = 0; q < kDeep; ++q)
@@ -535,20 +555,20 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       const int block = (2 * F + N) * 128;
       int s = 0, acc = 0;
       uint32_t round = 0, acc_round = 0;
-      for (int tile = blockIdx.x; tile < p.tiles && !*s_abort; tile += gridDim.x) {
+      for (int tile = first_tile; tile < p.tiles && !*s_abort; tile += step) {
         mbar_wait_bounded_inline(acc_empty + acc, acc_round ^ 1u, s_abort, 12, p.wait_limit);
         tc_fence_after();
-        for (int k = 0; k < p.k_blocks; k += kDeep) {
+        for (int k = k0; k < k1; k += kDeep) {
           mbar_wait_bounded_inline(full + s, round, s_abort, 13, p.wait_limit);
           tc_fence_after();
           const uint64_t off = (uint64_t)((s * p.stage_bytes) >> 4);
 #pragma unroll
           for (int q = 0; q < kDeep; ++q)
-            if (q < p.k_blocks - k) {
+            if (q < k1 - k) {
 #pragma unroll
               for (int kk = 0; kk < kStageK / 16; ++kk)
                 mma_ss(tmem + acc * kFewTokens, da + off + (q * block >> 4) + kk * 2, db + off + (q * block >> 4) + kk * 2,
-                       p.idesc, k + q > 0 || kk > 0);
+                       p.idesc, k + q > k0 || kk > 0);
             }
           mma_commit(empty + s);
           if (++s == p.stages) {
@@ -566,7 +586,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     const int ld = p.ld_turn;  // of `turn`, a row for each lane: odd, so that its columns do not meet in a bank
     int acc = 0;
     uint32_t acc_round = 0;
-    for (int tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
+    for (int tile = first_tile; tile < p.tiles; tile += step) {
       mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 14, p.wait_limit);
       if (*s_abort) break;
       tc_fence_after();
@@ -587,7 +607,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       asm volatile("bar.sync 1, 128;" ::: "memory");
       // eight features of a token a thread
       const int per_row = F / 8;
-      for (int i = threadIdx.x - 64; i < p.tokens * per_row; i += 128) {
+      for (int i = threadIdx.x - 64; p.splits == 1 && i < p.tokens * per_row; i += 128) {
         const int token = i / per_row, f = (i - token * per_row) * 8, col = tile * F + f;
         if (col >= p.hidden) continue;
         float g[8], u[8], h[8];
@@ -616,6 +636,35 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  if (p.splits > 1) {
+    cluster_sync();  // the sums of all pieces of K are there
+    // two features of a token a thread; each piece's four sums are under way together
+    const uint32_t mine = smem_u32(turn);
+    for (int i = rank * kFewThreads + threadIdx.x; i < p.tokens * (F / 2); i += p.splits * kFewThreads) {
+      const int token = i / (F / 2), f = (i - token * (F / 2)) * 2, col = first_tile * F + f;
+      if (col >= p.hidden) continue;
+      float g[2] = {0.0f, 0.0f}, u[2] = {0.0f, 0.0f}, h[2];
+#pragma unroll 2
+      for (int r = 0; r < p.splits; ++r) {
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          x[e] = ld_cluster(mine + ((f + (e & 1) + (e < 2 ? 0 : F)) * p.ld_turn + token) * 4, r);
+        g[0] += x[0];
+        g[1] += x[1];
+        u[0] += x[2];
+        u[1] += x[3];
+      }
+      gate_product(p.activation, g, u, h);
+      const int64_t at = token * p.ld_out + col;
+      *reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(p.out) + at) = pack2<T>(h[0], h[1]);
+      if (p.keep[0] != nullptr) {
+        *reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(p.keep[0]) + at) = pack2<T>(g[0], g[1]);
+        *reinterpret_cast<uint32_t*>(reinterpret_cast<T*>(p.keep[1]) + at) = pack2<T>(u[0], u[1]);
+      }
+    }
+    cluster_sync();  // nobody leaves while others read here
+  }
   if (warp == 1) {
     tc_fence_after();
     tmem_dealloc(tmem, 256);
@@ -891,13 +940,24 @@ static int launch_few(const sparsp_ffn& f, const void* X, const void* Wg, const 
                       void* up, char* ws, cudaStream_t st) {
   FewParams p = {};
   p.columns = (int32_t)align_up(f.tokens, 16);
-  // features at a time: what a round of all SMs loads, 2 F rows of weights and N of tokens a CTA, times the rounds
-  auto cost = [&](int F) { return (int64_t)ceil_div(ceil_div(f.hidden, F), kSms) * (2 * F + p.columns); };
+  p.k_blocks = ceil_div(f.dim, kStageK);
+  // CTAs that share out K, where there are few tiles, in pieces of eight blocks at least (100 x 5120 x 512: alone 17.8 us,
+  // two 12.6, four 10.1; 2 x 824 x 1144, pieces of six: alone 4.5, two 5.3).  Clusters of four find room on 128 SMs, of two
+  // on all; of eight there is not room for enough at once.
+  auto splits = [&](int F) {
+    const int tiles = ceil_div(f.hidden, F);
+    if (tiles * 4 <= 128 && p.k_blocks >= 32) return 4;
+    return tiles * 2 <= kSms && p.k_blocks >= 16 ? 2 : 1;
+  };
+  // features at a time: what a CTA loads, 2 F rows of weights and N of tokens a block of K in each round
+  auto cost = [&](int F) {
+    return (int64_t)ceil_div(ceil_div(f.hidden, F), kSms) * (2 * F + p.columns) * ceil_div(p.k_blocks, splits(F));
+  };
   p.features = 64;
   for (int F = 32; F >= 16; F /= 2)
     if (cost(F) < cost(p.features)) p.features = F;
+  p.splits = splits(p.features);
   p.tiles = ceil_div(f.hidden, p.features);
-  p.k_blocks = ceil_div(f.dim, kStageK);
   p.ld_turn = p.columns + 1;
   const int turn = (int)align_up(2 * p.features * p.ld_turn * 4, 128), room = kFewSmem - 16384 - turn - 1024;
   const int block = (2 * p.features + p.columns) * 128;
@@ -926,7 +986,8 @@ static int launch_few(const sparsp_ffn& f, const void* X, const void* Wg, const 
                           : (bf ? few_kernel<__nv_bfloat16, 1> : few_kernel<__half, 1>);
   const int smem = p.stages * p.stage_bytes + 16384 + turn + 1024;
   SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, smem));
-  SPARSP_CUDA_OK(launch_kernel(kern, dim3((unsigned)std::min(p.tiles, kSms)), kFewThreads, smem, st, mg, mu, mx, p));
+  SPARSP_CUDA_OK(launch_clusters(kern, dim3((unsigned)(std::min(p.tiles, kSms) * p.splits)), p.splits, kFewThreads, smem,
+                                 st, mg, mu, mx, p));
   return SPARSP_OK;
 }
 

@@ -714,7 +714,9 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
     }
     const int resident = std::min({32, 65536 / (p.threads * worker_registers(p.kind)), kNormSmem / (p.smem_bytes + 4096)});
     const int64_t rows = p.kind == kWarp8 ? (n.rows + (32 >> p.log_lanes) - 1) >> (5 - p.log_lanes) : n.rows;
-    const int64_t most = std::min<int64_t>(rows, (int64_t)kSms * resident * workers);
+    int64_t most = std::min<int64_t>(rows, (int64_t)kSms * resident * workers);
+    // backward, a worker's sums are written and read again: eight rows of its own at least, if every SM has a worker
+    if (bwd) most = std::min(most, std::max<int64_t>(kSms, rows / 8));
     p.parts = (int)std::max<int64_t>(1, most >> p.log_classes);
     const int all = p.parts << p.log_classes;
     p.grid = (unsigned)((all + workers - 1) / workers);

@@ -342,6 +342,20 @@ __device__ __forceinline__ uint32_t cluster_addr(const void* p, uint32_t rank) {
   asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
   return r;
 }
+// fp32 at shared address `a` of this CTA, in CTA `rank` of the cluster.
+__device__ __forceinline__ float ld_cluster(uint32_t a, uint32_t rank) {
+  float v;
+  asm volatile(
+      "{\n\t"
+      ".reg .b32 at;\n\t"
+      "mapa.shared::cluster.u32 at, %1, %2;\n\t"
+      "ld.shared::cluster.f32 %0, [at];\n\t"
+      "}"
+      : "=f"(v)
+      : "r"(a), "r"(rank)
+      : "memory");
+  return v;
+}
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
