@@ -316,23 +316,42 @@ struct RowsAhead {
 __device__ __forceinline__ void close_batch() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void wait_batch() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
 
-// A thread's weights of group g; zeros outside the row.
-template <typename T, int K, typename Rows>
-__device__ __forceinline__ void load_weights(const NormParams& p, const void* from, int64_t g, const Rows& rows, int E,
-                                             float missing, F2 (&out)[K / 2]) {
-  float f[K];
+// A thread's values of a row of weights, in 16-byte pieces where they lie so; zeros outside the row.  All loads are under
+// way together.
+template <typename W, int K, typename Rows>
+__device__ __forceinline__ void load_row(const W* row, int dim, const Rows& rows, float (&f)[K]) {
+  constexpr int E = Rows::E;
+  if (E > 1 && rows.shift == 0 && dim % E == 0 && reinterpret_cast<uintptr_t>(row) % 16 == 0) {
+    constexpr int N = 16 / sizeof(W);  // weights of a piece
+#pragma unroll
+    for (int j = 0; j < K; j += E > N ? N : E) {
+      const int c = rows.column(j / E) + j % E;
+      Vec<W, E == 1 ? 1 : N> x;
+      x.clear();
+      if (c < dim) x = load_vec<W, E == 1 ? 1 : N>(row + c);
+#pragma unroll
+      for (int i = 0; i < (E > N ? N : E); ++i) f[j + i] = x[i];
+    }
+    return;
+  }
 #pragma unroll
   for (int j = 0; j < K; ++j) {
     const int c = rows.column(j / E) + j % E;
-    f[j] = 0.0f;
-    if (c >= 0 && c < p.dim) {
-      if (from == nullptr)
-        f[j] = missing;
-      else if (p.weights_fp32)
-        f[j] = reinterpret_cast<const float*>(from)[g * p.dim + c];
-      else
-        f[j] = to_float<T>(reinterpret_cast<const T*>(from)[g * p.dim + c]);
-    }
+    f[j] = c >= 0 && c < dim ? to_float<W>(row[c]) : 0.0f;
+  }
+}
+// ... of group g
+template <typename T, int K, typename Rows>
+__device__ __forceinline__ void load_weights(const NormParams& p, const void* from, int64_t g, const Rows& rows,
+                                             float missing, F2 (&out)[K / 2]) {
+  float f[K];
+  if (from == nullptr) {
+#pragma unroll
+    for (int j = 0; j < K; ++j) f[j] = missing;
+  } else if (p.weights_fp32) {
+    load_row(reinterpret_cast<const float*>(from) + g * p.dim, p.dim, rows, f);
+  } else {
+    load_row(reinterpret_cast<const T*>(from) + g * p.dim, p.dim, rows, f);
   }
 #pragma unroll
   for (int j = 0; j < K / 2; ++j) out[j] = F2(f[2 * j], f[2 * j + 1]);
@@ -380,8 +399,8 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
     int left = (int)(m.below(e) - m.below(a));
     if (left == 0) continue;
     F2 w[K / 2], b[K / 2];
-    load_weights<T, K>(p, p.weight, g, rows, E, 1.0f, w);
-    load_weights<T, K>(p, p.bias, g, rows, E, 0.0f, b);
+    load_weights<T, K>(p, p.weight, g, rows, 1.0f, w);
+    load_weights<T, K>(p, p.bias, g, rows, 0.0f, b);
 #pragma unroll 1
     while (left > 0) {
       if constexpr (kRing) wait_batch();
@@ -503,7 +522,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
     e = min(m.hi, (g + 1) * m.per_group);
     int left = (int)(m.below(e) - m.below(a0));
     F2 w[K / 2], dw[K / 2], db[K / 2];
-    load_weights<T, K>(p, p.weight, g, xs, E, 1.0f, w);
+    load_weights<T, K>(p, p.weight, g, xs, 1.0f, w);
     if constexpr (kForm != kPlain) {
 #pragma unroll
       for (int j = 0; j < K / 4; ++j) {
@@ -577,25 +596,39 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
     }
     if (p.want_weights) {
       float* mine = p.partial + (((m.part + g) << m.log_classes()) + m.cls) * 2 * p.dim;
+      constexpr int S = E > 1 ? 4 : 2;  // sums that are stored together
 #pragma unroll
-      for (int j = 0; j < K; j += 2) {
-        float a[2], c[2];
-        dw[j / 2].get(a[0], a[1]);
-        db[j / 2].get(c[0], c[1]);
+      for (int j = 0; j < K; j += S) {
+        float a[S], c[S];
+#pragma unroll
+        for (int i = 0; i < S; i += 2) {
+          dw[(j + i) / 2].get(a[i], a[i + 1]);
+          db[(j + i) / 2].get(c[i], c[i + 1]);
+        }
         if constexpr (kKind == kWarp8) {
           for (int o = me.lanes; o < 32; o *= 2) {  // of the rows that the warp has at once
-            a[0] += __shfl_xor_sync(0xffffffffu, a[0], o);
-            a[1] += __shfl_xor_sync(0xffffffffu, a[1], o);
-            c[0] += __shfl_xor_sync(0xffffffffu, c[0], o);
-            c[1] += __shfl_xor_sync(0xffffffffu, c[1], o);
+#pragma unroll
+            for (int i = 0; i < S; ++i) {
+              a[i] += __shfl_xor_sync(0xffffffffu, a[i], o);
+              c[i] += __shfl_xor_sync(0xffffffffu, c[i], o);
+            }
           }
         }
+        if (me.sub != 0) continue;
+        if (kForm == kPlain) {  // dim is a multiple of four, and so is the column
+          const int col = xs.column(j / E) + j % E;
+          if (col < p.dim) {
+            *reinterpret_cast<float4*>(mine + col) = make_float4(a[0], a[1], a[S - 2], a[S - 1]);
+            *reinterpret_cast<float4*>(mine + p.dim + col) = make_float4(c[0], c[1], c[S - 2], c[S - 1]);
+          }
+        } else {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const int col = xs.column((j + i) / E) + (j + i) % E;
-          if (me.sub == 0 && col >= 0 && col < p.dim) {
-            mine[col] = a[i];
-            mine[p.dim + col] = c[i];
+          for (int i = 0; i < S; ++i) {
+            const int col = xs.column((j + i) / E) + (j + i) % E;
+            if (col >= 0 && col < p.dim) {
+              mine[col] = a[i];
+              mine[p.dim + col] = c[i];
+            }
           }
         }
       }
@@ -715,8 +748,9 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
     const int resident = std::min({32, 65536 / (p.threads * worker_registers(p.kind)), kNormSmem / (p.smem_bytes + 4096)});
     const int64_t rows = p.kind == kWarp8 ? (n.rows + (32 >> p.log_lanes) - 1) >> (5 - p.log_lanes) : n.rows;
     int64_t most = std::min<int64_t>(rows, (int64_t)kSms * resident * workers);
-    // backward, a worker's sums are written and read again: eight rows of its own at least, if every SM has a worker
-    if (bwd) most = std::min(most, std::max<int64_t>(kSms, rows / 8));
+    // backward, a worker's sums are written and read again: four rows of its own at least, if every SM has a worker (3023 x 752
+    // fp32: 14.0 us, 17.3 with eight, 15.6 with one)
+    if (bwd) most = std::min(most, std::max<int64_t>(kSms, rows / 4));
     p.parts = (int)std::max<int64_t>(1, most >> p.log_classes);
     const int all = p.parts << p.log_classes;
     p.grid = (unsigned)((all + workers - 1) / workers);
