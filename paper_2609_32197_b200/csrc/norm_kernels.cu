@@ -348,7 +348,7 @@ __device__ __forceinline__ void load_weights(const NormParams& p, const void* fr
   if (from == nullptr) {
 #pragma unroll
     for (int j = 0; j < K; ++j) f[j] = missing;
-  } else if (p.weights_fp32) {
+  } else if (sizeof(T) == 4 || p.weights_fp32) {
     load_row(reinterpret_cast<const float*>(from) + g * p.dim, p.dim, rows, f);
   } else {
     load_row(reinterpret_cast<const T*>(from) + g * p.dim, p.dim, rows, f);
