@@ -516,7 +516,8 @@ SPARSP_API int sparsp_gated_ffn_workspace_bytes(const sparsp_ffn* ffn, int32_t b
 SPARSP_API int sparsp_gated_ffn_fwd(const sparsp_ffn* ffn, const void* X, const void* Wgate, const void* Wup, void* H,
                                     void* gate, void* up, void* workspace, void* stream);
 
-/* With dG = dH * up * a'(gate) and dU = dH * a(gate), both rounded to dtype (the tensor cores' operands):
+/* With dG = dH * up * a'(gate) and dU = dH * a(gate), both rounded to dtype (the tensor cores' operands; for up to 128
+ * tokens and dim up to 18432 as the sum of two such values):
  *   dX = dG Wgate + dU Wup,  dWgate = dG^T X,  dWup = dU^T X, sums in fp32
  *   dX             out  may be NULL (not wanted); Wgate and Wup may then be NULL too
  *   dWgate, dWup   out  both or neither NULL; X may be NULL without them.  Without tokens they are zero. */

@@ -8,7 +8,10 @@
 //             memory and the store.
 //   dX        A = dG then dU (K-major), B = Wg then Wu as they lie (MN-major): the sum over both is one accumulation.
 //   dW        A = dG^T or dU^T (MN-major), B = X (MN-major); summed over tokens.
-// dG and dU, which the last two read, are made element by element before them.
+// dG and dU, which the last two read, are made element by element before them, rounded to 16 bits.  Where there are few
+// tokens those roundings do not average out over many results, and time goes into the weights, not into products: then
+// both are in two parts, the rounded value and what it leaves, one 128 rows behind the other.  dX takes the two parts as
+// the two halves of its 256-row tile and adds them when the pieces of K are added, dW as more tokens.
 #include <algorithm>
 
 #include "layer.cuh"
@@ -26,6 +29,7 @@ struct GemmParams {
   int32_t rows, cols;     // of the result (kForward: tokens, hidden; kInput: tokens, dim; kWeights: hidden, dim)
   int32_t m_tiles, n_tiles, band;
   int32_t whole, shares;  // see Walk
+  int32_t two_parts;      // dG and dU are in two parts
   int32_t alternate;      // half the warps of a CTA take every other tile's results
   int32_t k_blocks;       // of 64, of one (A, B); kInput has two of them
   int32_t activation;
@@ -38,6 +42,7 @@ constexpr int kStageK = 64;           // K elements of a stage: one 128-byte swi
 constexpr int kEpilogueWarps = 16;    // four for each quarter of the lanes (256 x 2048 x 9472: 16.7 us, 18.3 with two)
 constexpr int kGemmThreads = 32 * (kEpilogueWarps + 2);
 constexpr int kTileRows = 128;        // of one CTA
+constexpr int kFewTokens = 128;       // up to so many tokens go their own ways
 
 // BN: columns of the accumulator, and of B over both CTAs.
 template <int BN>
@@ -161,8 +166,10 @@ __device__ __forceinline__ void tile_at(const GemmParams& p, int tile, int& m, i
 struct Walk {
   int tile, k0, k1, slot;  // at work: tile, blocks of K, and where to put the sums (-1: the whole tile is done)
   int next_whole, pairs, whole, blocks, lo, hi, next_slot;
-  __device__ __forceinline__ Walk(const GemmParams& p, int blocks, int pair, int pairs)
-      : next_whole(pair), pairs(pairs), whole(p.whole), blocks(blocks), lo(0), hi(0), next_slot(2 * pair) {
+  bool always;  // sums go through a slot even where a pair has all of a tile
+  __device__ __forceinline__ Walk(const GemmParams& p, int blocks, int pair, int pairs, bool adds_halves)
+      : next_whole(pair), pairs(pairs), whole(p.whole), blocks(blocks), lo(0), hi(0), next_slot(2 * pair),
+        always(adds_halves) {
     if (pair < p.shares) {
       lo = share_begin(p, blocks, pair);
       hi = share_begin(p, blocks, pair + 1);
@@ -186,7 +193,7 @@ struct Walk {
     tile = whole + r;
     k0 = lo - r * blocks;
     k1 = min(blocks, k0 + hi - lo);
-    slot = k1 - k0 == blocks ? -1 : next_slot;
+    slot = k1 - k0 == blocks && !always ? -1 : next_slot;
     ++next_slot;
     lo += k1 - k0;
     return true;
@@ -236,7 +243,7 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
   const uint32_t tmem = *tmem_slot;
   wait_previous_grids();
 
-  Walk walk(p, p.k_blocks * (kMode == kInput ? 2 : 1), pair, pairs);
+  Walk walk(p, p.k_blocks * (kMode == kInput ? 2 : 1), pair, pairs, kMode == kInput && p.two_parts);
   constexpr bool kAMn = kMode == kWeights, kBMn = kMode != kForward;
 
   if (warp == kEpilogueWarps) {
@@ -268,10 +275,12 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
           for (int q = 0; q < C::kStages; ++q)
             if (q == s) bar = full_of_even[q];
           const bool second = kMode == kInput && k >= p.k_blocks;
-          const int kk = (second ? k - p.k_blocks : k) * kStageK;
+          const bool left = kMode == kWeights && p.two_parts && k >= p.k_blocks / 2;  // what the rounding left
+          const int kk = (second ? k - p.k_blocks : left ? k - p.k_blocks / 2 : k) * kStageK;
           if constexpr (kAMn) {
-            tma_load_pair(A, ta, bar, row, kk);
-            tma_load_pair(A + 8192, ta, bar, row + 64, kk);
+            const int token = left ? kFewTokens + kk : kk;
+            tma_load_pair(A, ta, bar, row, token);
+            tma_load_pair(A + 8192, ta, bar, row + 64, token);
           } else {
             tma_load_pair(A, second ? &a1 : &a0, bar, kk, row);
           }
@@ -467,7 +476,6 @@ struct FewParams {
 };
 
 constexpr int kFewThreads = 192;  // loads, products, four warps of results
-constexpr int kFewTokens = 128;
 constexpr int kFewSmem = 224 * 1024;
 
 template <typename T, int kDeep>
@@ -684,7 +692,10 @@ __device__ __forceinline__ void join_tile(const GemmParams p, int cta) {
   int q = (int)((int64_t)lo * p.shares / ((int64_t)(p.m_tiles * p.n_tiles - p.whole) * blocks));
   while (q > 0 && Walk::share_begin(p, blocks, q) > lo) --q;
   while (Walk::share_begin(p, blocks, q + 1) <= lo) ++q;
-  if (Walk::share_begin(p, blocks, q) <= lo && Walk::share_begin(p, blocks, q + 1) >= hi) return;  // one pair had it all
+  const bool halves = kMode == kInput && p.two_parts;  // rows 128 and on belong to those 128 before
+  if (halves ? threadIdx.x >= kFewTokens
+             : Walk::share_begin(p, blocks, q) <= lo && Walk::share_begin(p, blocks, q + 1) >= hi)
+    return;  // one pair had it all
   int m, n;
   tile_at(p, p.whole + rest, m, n);
   float v[8], u[8];
@@ -704,6 +715,13 @@ __device__ __forceinline__ void join_tile(const GemmParams p, int cta) {
       v[4 * h + 1] += x.y;
       v[4 * h + 2] += x.z;
       v[4 * h + 3] += x.w;
+      if (halves) {
+        const float4 y = from[(c / 4 + h) * 256 + kFewTokens];
+        v[4 * h] += y.x;
+        v[4 * h + 1] += y.y;
+        v[4 * h + 2] += y.z;
+        v[4 * h + 3] += y.w;
+      }
       if (kMode == kForward) {
         const float4 y = from[((c + BN / 2) / 4 + h) * 256];
         u[4 * h] += y.x;
@@ -778,6 +796,50 @@ __global__ void __launch_bounds__(256) gate_grad_kernel(const T* dh, const T* ga
   store_vec<T, 8>(du + to, ou);
 }
 
+// ... in two parts: rows 0 .. tokens - 1 rounded, then zeros up to row 128, then what the roundings leave.
+template <typename T>
+__global__ void __launch_bounds__(256) gate_grad_parts_kernel(const T* dh, const T* gate, const T* up, T* dg, T* du,
+                                                              int64_t ld, int64_t ld_out, int hidden, int tokens,
+                                                              int activation) {
+  enter_grid(dh, gate, up);
+  const int row = blockIdx.y, col = (blockIdx.x * 256 + threadIdx.x) * 8;
+  if (col >= hidden) return;
+  const int64_t to = row * ld_out + col, rest = to + kFewTokens * ld_out;
+  Vec<T, 8> og, ou;
+  if (row >= tokens) {
+    og.clear();
+    store_vec(dg + to, og);
+    store_vec(du + to, og);
+    return;
+  }
+  const int64_t at = row * ld + col;
+  const Vec<T, 8> h = load_once<T, 8>(dh + at), g = load_once<T, 8>(gate + at), u = load_once<T, 8>(up + at);
+  float fg[8], fu[8];
+  with_activation(activation, [&](auto k) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float a, slope;
+      activate<decltype(k)::value>(g[e], a, slope);
+      fg[e] = h[e] * u[e] * slope;
+      fu[e] = h[e] * a;
+    }
+  });
+  og.set(fg);
+  ou.set(fu);
+  store_vec(dg + to, og);
+  store_vec(du + to, ou);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    // an infinity leaves nothing
+    fg[e] = isfinite(og[e]) ? fg[e] - og[e] : 0.0f;
+    fu[e] = isfinite(ou[e]) ? fu[e] - ou[e] : 0.0f;
+  }
+  og.set(fg);
+  ou.set(fu);
+  store_vec(dg + rest, og);
+  store_vec(du + rest, ou);
+}
+
 __global__ void __launch_bounds__(256) zero_rows_kernel(uint16_t* a, uint16_t* b, int rows, int cols, int64_t ld) {
   enter_grid();
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)rows * cols; i += (int64_t)gridDim.x * 256) {
@@ -819,15 +881,16 @@ static int join_ctas(const GemmParams& p, int mode) {
 
 // Clocks that a product takes on some pairs of SMs, and whether its last round is shared out by blocks of K for that (by
 // how many pairs; 0 = not): 512 a block of K, 2500 a unit for what no block hides, 12000 for writing sums out and the
-// launch that adds them.
-static int64_t gemm_clocks(int tiles, int blocks, int pairs, int* shares) {
+// launch that adds them.  share_all: every tile has to go that way (there are fewer than pairs).
+static int64_t gemm_clocks(int tiles, int blocks, int pairs, bool share_all, int* shares) {
   *shares = 0;
   const int rounds = tiles / pairs, rest = tiles % pairs;
   const int64_t unit = 512LL * blocks + 2500, all_whole = (rounds + (rest > 0)) * unit;
   if (rest == 0) return all_whole;
-  int64_t best = all_whole;
+  int64_t best = share_all ? INT64_MAX : all_whole;
   // equal runs for all pairs, of which most touch two tiles, or as many for each tile as there are pairs for it
-  const int all = (int)std::min<int64_t>(pairs, (int64_t)rest * blocks / 4), each = std::min(pairs / rest, blocks / 4);
+  const int all = (int)std::min<int64_t>(pairs, (int64_t)rest * blocks / 4);
+  const int each = std::max(1, std::min(pairs / rest, blocks / 4));
   if (all > rest) {
     const int64_t t = rounds * unit + 512LL * ceil_div((int64_t)rest * blocks, all) + 2 * 2500 + 12000;
     if (t < best) {
@@ -835,7 +898,7 @@ static int64_t gemm_clocks(int tiles, int blocks, int pairs, int* shares) {
       *shares = all;
     }
   }
-  if (each > 1) {
+  if (each > 1 || share_all) {
     const int64_t t = rounds * unit + 512LL * ceil_div(blocks, each) + 2500 + 12000;
     if (t < best) {
       best = t;
@@ -858,7 +921,8 @@ static int prepare_gemm(GemmParams* p, int mode, const sparsp_ffn& f, char* ws) 
     return SPARSP_ERR_UNSUPPORTED;
   }
   int shares;
-  gemm_clocks(p->m_tiles * p->n_tiles, p->k_blocks * (mode == kInput ? 2 : 1), kPairs, &shares);
+  gemm_clocks(p->m_tiles * p->n_tiles, p->k_blocks * (mode == kInput ? 2 : 1), kPairs, mode == kInput && p->two_parts,
+              &shares);
   share_out(p, kPairs, shares);
   p->band = 8;
   p->partial = reinterpret_cast<float*>(ws + kStatusWords * 4);
@@ -890,18 +954,20 @@ static int launch_gemm(const GemmParams& p, const GemmMaps& m, int dtype, cudaSt
 static int plan_both(GemmParams* pi, GemmParams* pw) {
   const int ti = pi->m_tiles * pi->n_tiles, tw = pw->m_tiles * pw->n_tiles;
   const int bi = 2 * pi->k_blocks, bw = pw->k_blocks;
-  int si, sw, low = 1, high = kPairs - 1;  // the fewest pairs with which dX is no later than dW
+  const bool all = pi->two_parts;
+  const int fewest = all ? ti + 1 : 1;
+  int si, sw, low = fewest, high = kPairs - 1;  // the fewest pairs with which dX is no later than dW
   while (low < high) {
     const int mid = (low + high) / 2;
-    if (gemm_clocks(ti, bi, mid, &si) <= gemm_clocks(tw, bw, kPairs - mid, &sw))
+    if (gemm_clocks(ti, bi, mid, all, &si) <= gemm_clocks(tw, bw, kPairs - mid, false, &sw))
       high = mid;
     else
       low = mid + 1;
   }
   int64_t best = INT64_MAX;
   int pairs = low;
-  for (int s = std::max(1, low - 1); s <= low; ++s) {
-    const int64_t t = std::max(gemm_clocks(ti, bi, s, &si), gemm_clocks(tw, bw, kPairs - s, &sw));
+  for (int s = std::max(fewest, low - 1); s <= low; ++s) {
+    const int64_t t = std::max(gemm_clocks(ti, bi, s, all, &si), gemm_clocks(tw, bw, kPairs - s, false, &sw));
     if (t >= best) continue;
     best = t;
     pairs = s;
@@ -929,7 +995,11 @@ static int launch_both(const GemmParams& pi, const GemmMaps& mi, const GemmParam
 // dG and dU have rows of whole 128-byte lines: a tile's rows of 128 bytes then lie in one line each, not in two (1003 x
 // 1160 x 2504, backward: 41 us without).
 static int64_t hidden_pitch(const sparsp_ffn& f) { return align_up(f.hidden, 64); }
-static int64_t hidden_bytes(const sparsp_ffn& f) { return align_up(f.tokens * hidden_pitch(f) * 2, 256); }
+// Two parts need the halves of every tile of dX to meet, in pieces of K that are added; rows of so many tiles that pairs
+// have a whole one each are left out of it.
+static bool two_parts(const sparsp_ffn& f) { return f.tokens <= kFewTokens && ceil_div(f.dim, BN) <= kPairs - 2; }
+static int64_t hidden_rows(const sparsp_ffn& f) { return two_parts(f) ? kFewTokens + f.tokens : f.tokens; }
+static int64_t hidden_bytes(const sparsp_ffn& f) { return align_up(hidden_rows(f) * hidden_pitch(f) * 2, 256); }
 
 int64_t ffn_workspace_bytes(const sparsp_ffn& f, bool backward) {
   if (!backward && f.tokens <= kFewTokens) return kStatusWords * 4;
@@ -1044,7 +1114,16 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
     return launch_kernel(gate_grad_kernel<T>, grid, 256, 0, st, (const T*)dH, (const T*)gate, (const T*)up, (T*)dg,
                          (T*)du, f.stride_h, hidden_pitch(f), row_length, (int)ctas_per_row, f.activation);
   };
-  SPARSP_CUDA_OK(f.dtype == SPARSP_BF16 ? grad((__nv_bfloat16*)nullptr) : grad((__half*)nullptr));
+  auto grad_parts = [&](auto* element) {
+    using T = std::remove_pointer_t<decltype(element)>;
+    return launch_kernel(gate_grad_parts_kernel<T>, dim3((unsigned)ceil_div(f.hidden, 2048), kFewTokens), 256, 0, st,
+                         (const T*)dH, (const T*)gate, (const T*)up, (T*)dg, (T*)du, f.stride_h, hidden_pitch(f),
+                         f.hidden, (int)f.tokens, f.activation);
+  };
+  if (two_parts(f))
+    SPARSP_CUDA_OK(f.dtype == SPARSP_BF16 ? grad_parts((Bf*)nullptr) : grad_parts((Hf*)nullptr));
+  else
+    SPARSP_CUDA_OK(f.dtype == SPARSP_BF16 ? grad((Bf*)nullptr) : grad((Hf*)nullptr));
   GemmMaps mi, mw;
   GemmParams pi = {}, pw = {};
   int rc;
@@ -1052,15 +1131,16 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
   pw.m_tiles = 2 * ceil_div(f.hidden, 256);
   pi.n_tiles = pw.n_tiles = ceil_div(f.dim, BN);
   pi.k_blocks = ceil_div(f.hidden, kStageK);
-  pw.k_blocks = ceil_div(f.tokens, kStageK);
+  pw.k_blocks = ceil_div(f.tokens, kStageK) * (two_parts(f) ? 2 : 1);
+  pi.two_parts = pw.two_parts = two_parts(f);
   if ((rc = prepare_gemm(&pi, kInput, f, ws)) != SPARSP_OK) return rc;
   if ((rc = prepare_gemm(&pw, kWeights, f, ws)) != SPARSP_OK) return rc;
   // both at once up to four rounds of tiles: beyond that their last rounds matter less than that both want L2
   const bool small = (int64_t)pi.m_tiles * pi.n_tiles + (int64_t)pw.m_tiles * pw.n_tiles <= 4 * kPairs;
   const int pairs = small ? plan_both(&pi, &pw) : 0;
   if (dX != nullptr) {
-    if ((rc = make_map(&mi.a0, f.dtype, dg, f.tokens, f.hidden, hidden_pitch(f), kTileRows)) != SPARSP_OK) return rc;
-    if ((rc = make_map(&mi.a1, f.dtype, du, f.tokens, f.hidden, hidden_pitch(f), kTileRows)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mi.a0, f.dtype, dg, hidden_rows(f), f.hidden, hidden_pitch(f), kTileRows)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mi.a1, f.dtype, du, hidden_rows(f), f.hidden, hidden_pitch(f), kTileRows)) != SPARSP_OK) return rc;
     if ((rc = make_map(&mi.b0, f.dtype, Wg, f.hidden, f.dim, f.stride_w, kStageK)) != SPARSP_OK) return rc;
     if ((rc = make_map(&mi.b1, f.dtype, Wu, f.hidden, f.dim, f.stride_w, kStageK)) != SPARSP_OK) return rc;
     if ((rc = make_out_map(&mi.o0, f.dtype, dX, f.tokens, f.dim, f.stride_x)) != SPARSP_OK) return rc;
@@ -1071,8 +1151,8 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
     pi.cols = f.dim;
   }
   if (dWg != nullptr) {
-    if ((rc = make_map(&mw.a0, f.dtype, dg, f.tokens, f.hidden, hidden_pitch(f), kStageK)) != SPARSP_OK) return rc;
-    if ((rc = make_map(&mw.a1, f.dtype, du, f.tokens, f.hidden, hidden_pitch(f), kStageK)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mw.a0, f.dtype, dg, hidden_rows(f), f.hidden, hidden_pitch(f), kStageK)) != SPARSP_OK) return rc;
+    if ((rc = make_map(&mw.a1, f.dtype, du, hidden_rows(f), f.hidden, hidden_pitch(f), kStageK)) != SPARSP_OK) return rc;
     if ((rc = make_map(&mw.b0, f.dtype, X, f.tokens, f.dim, f.stride_x, kStageK)) != SPARSP_OK) return rc;
     mw.b1 = mw.b0;
     if ((rc = make_out_map(&mw.o0, f.dtype, dWg, f.hidden, f.dim, f.stride_w)) != SPARSP_OK) return rc;

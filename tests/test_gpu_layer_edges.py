@@ -156,3 +156,44 @@ def test_between_the_callers_own_kernels():
                 got = chain(x0 * (k + 1))
                 assert all(torch.equal(a, b) for a, b in zip(got, want[k]))
     torch.cuda.current_stream().wait_stream(side)
+
+
+@pytest.mark.parametrize("m,d,f", [(1, 64, 128), (2, 88, 936), (64, 264, 72), (128, 600, 520), (100, 2600, 200)])
+@pytest.mark.parametrize("kind,dtype", [("silu", BF), ("gelu", HF)])
+def test_few_tokens_keep_what_the_operands_round_off(m, d, f, kind, dtype):
+    """Up to 128 tokens dG and dU are in two parts: off by the square of a rounding, and by what a(x) and a'(x) are."""
+    x, wg, wu, dh = ffn_tests.inputs(m, d, f, dtype, seed=11)
+    gate, up = x @ wg.T, x @ wu.T
+    ffn = binding.make_ffn(m, d, f, kind, dtype)
+    ws = binding.make_ffn_workspace(ffn)
+    ws[256:].fill_(255)
+    dx, dwg, dwu = (torch.full_like(t, float("nan")) for t in (x, wg, wu))
+    binding.sparsp_gated_ffn_bwd(ffn, dh, x, wg, wu, gate, up, dx, dwg, dwu, ws)
+    assert binding.sparsp_status(ws) == binding.SPARSP_OK
+    DH, X, G, U = (t.double() for t in (dh, x, wg, wu))
+    a, slope = ffn_tests.activation(kind, gate.double())
+    dg, du = DH * up.double() * slope, DH * a
+    eg = 2 * UNIT[dtype] ** 2 * dg.abs() + 2.0 ** -19 * (DH * up.double()).abs() + TINY[dtype]
+    eu = 2 * UNIT[dtype] ** 2 * du.abs() + 2.0 ** -19 * (DH * gate.double()).abs() + TINY[dtype]
+    want = dg @ G + du @ U
+    off = eg @ G.abs() + eu @ U.abs() + ffn_tests.acc(4 * f) * (dg.abs() @ G.abs() + du.abs() @ U.abs())
+    close(dx, want, off + UNIT[dtype] * (want.abs() + off) + TINY[dtype], "dX")
+    for got, t, e, what in ((dwg, dg, eg, "dWgate"), (dwu, du, eu, "dWup")):
+        want = t.T @ X
+        off = e.T @ X.abs() + ffn_tests.acc(2 * m) * (t.abs().T @ X.abs())
+        close(got, want, off + UNIT[dtype] * (want.abs() + off) + TINY[dtype], what)
+
+
+def test_infinite_gradients_of_few_tokens():
+    """A dG past the type's range is an infinity, as rounding makes it; what it leaves is not NaN by itself."""
+    m, d, f = 3, 64, 64
+    x, wg, wu, dh = ffn_tests.inputs(m, d, f, HF, seed=12)
+    gate, up = torch.full((m, f), 100.0, dtype=HF, device="cuda"), torch.full((m, f), 60000.0, dtype=HF, device="cuda")
+    dh.fill_(1.0)
+    dh[1] = 4.0  # 4 * 60000 * 1: infinite in 16 bits
+    wg.fill_(1.0)
+    ffn = binding.make_ffn(m, d, f, "silu", HF)
+    ws = binding.make_ffn_workspace(ffn)
+    dx, dwg, dwu = (torch.empty_like(t) for t in (x, wg, wu))
+    binding.sparsp_gated_ffn_bwd(ffn, dh, x, wg, wu * 0, gate, up, dx, dwg, dwu, ws)
+    assert bool(torch.isinf(dx[1]).all()) and not bool(torch.isnan(dx[1]).any())
