@@ -1,8 +1,8 @@
 // Gated feed-forward: H = a(X Wg^T) * (X Wu^T) in one kernel, and its backward pass.
 //
-// All three products are one matrix kernel.  A pair of CTAs (a cluster of two, tcgen05 cta_group::2) makes a 256-row tile
-// of the result: each CTA loads 128 of its rows of A and half of its columns of B by TMA, the even CTA issues the MMAs for
-// both, and each finds its 128 rows, all columns, as fp32 in its own tensor memory.
+// All three products are one matrix kernel.  A pair of CTAs (a cluster of two, tcgen05 cta_group::2) makes a 256-row
+// tile of the result: each CTA loads 128 of its rows of A and half of its columns of B by TMA, the even CTA issues the
+// MMAs for both, and each finds its 128 rows, all columns, as fp32 in its own tensor memory.
 //   forward   A = X (K-major), B = half a tile of Wg's rows in one CTA and the same rows of Wu in the other: the tile's
 //             columns are gate and up of the same features, and the activation and the product happen between tensor
 //             memory and the store.
@@ -10,8 +10,12 @@
 //   dW        A = dG^T or dU^T (MN-major), B = X (MN-major); summed over tokens.
 // dG and dU, which the last two read, are made element by element before them, rounded to 16 bits.  Where there are few
 // tokens those roundings do not average out over many results, and time goes into the weights, not into products: then
-// both are in two parts, the rounded value and what it leaves, one 128 rows behind the other.  dX takes the two parts as
-// the two halves of its 256-row tile and adds them when the pieces of K are added, dW as more tokens.
+// both are in two parts, the rounded value and what it leaves, one 128 rows behind the other.  dX takes the two parts
+// as the two halves of its 256-row tile and adds them when the pieces of K are added, dW as more tokens.
+//
+// Bound by the tensor cores where all sizes are large: 97 to 98 % of their cycles, at the 1.3 to 1.5 GHz that the power
+// limit leaves (37800 x 5120 x 13824 bf16, both projections kept: 7.9 ms = 1350 TFLOP/s; backward 17.1 to 20.3 ms =
+// 1050 to 1250).
 #include <algorithm>
 
 #include "layer.cuh"
@@ -66,21 +70,27 @@ __device__ __forceinline__ float logistic2(float t) {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kTanhA = 2.0f * 0.7978845608028654f, kTanhB = 0.044715f;  // (1 + tanh(u)) / 2 = logistic(2 u)
 
-// (1 + erf(x / sqrt 2)) / 2, and e = exp(-x^2 / 2): Abramowitz and Stegun 7.1.26, erf within 1.5e-7, with the exponential
-// that the slope needs too.  The library's erff took a forward call of 16384 x 64 x 9472 217 us.
+// (1 + erf(x / sqrt 2)) / 2, and e = exp(-x^2 / 2), which the slope needs too: with z = |x| / sqrt 2 and t = 1 / (1 +
+// 3/8 z), the way of Abramowitz and Stegun 7.1.26, erfc(z) / 2 is e times a polynomial in t, fitted here to the least
+// largest relative error: 2^-20 for every x whose e is above zero.  Their five terms, made for a small absolute error,
+// are off by 0.05 % at x = -4 and 0.4 % at -6, which 16-bit results show.  A forward call of 16384 x 64 x 9472 takes
+// 168 us (160 with five terms, 217 with the library's erff; in pairs of values by f32x2 instructions 167).
 __device__ __forceinline__ float normal_below(float x, float& e) {
   const float z = fabsf(x) * 0.70710678118654752f;
   e = ptx::ex2(z * z * -kLog2e);
   float t;
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(fmaf(z, 0.3275911f, 1.0f)));
-  float q = fmaf(t, 0.5f * 1.061405429f, -0.5f * 1.453152027f);
-  q = fmaf(t, q, 0.5f * 1.421413741f);
-  q = fmaf(t, q, -0.5f * 0.284496736f);
-  q = fmaf(t, q, 0.5f * 0.254829592f) * t * e;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(fmaf(z, 0.375f, 1.0f)));
+  float q = fmaf(t, -0.06754766983f, 0.19396793736f);
+  q = fmaf(t, q, -0.06479728835f);
+  q = fmaf(t, q, 0.14152977980f);
+  q = fmaf(t, q, 0.08333265443f);
+  q = fmaf(t, q, 0.10784451822f);
+  q = fmaf(t, q, 0.10566972979f) * t * e;
   return x < 0.0f ? q : 1.0f - q;
 }
 
-// a(x), and a(x) with a'(x); each within 2^-20 of |x|, which results of 8 or 11 bits do not see.
+// a(x), and a(x) with a'(x).  a(x) is within 2^-16 of itself as far down as x = -6 (roundings of the exponent's
+// argument).
 template <int kKind>
 __device__ __forceinline__ float activate(float x) {
   if constexpr (kKind == SPARSP_ACT_SILU) return x * logistic2(-kLog2e * x);
@@ -127,9 +137,9 @@ __device__ __forceinline__ void gate_product(int kind, const float (&g)[N], cons
 }
 
 // A warp's 32 rows x 32 columns to global memory: staged in its own 2 KB (64-byte swizzle: a row's 16-byte pieces in
-// turned places, so that lanes do not meet in a bank) and stored as one TMA tile, which writes whole sectors and leaves out
-// what lies beyond the tensor.  16-byte stores from the registers, a row each, cost a forward call of 37800 x 5120 x 13824
-// that keeps its projections 9305 us.
+// turned places, so that lanes do not meet in a bank) and stored as one TMA tile, which writes whole sectors and leaves
+// out what lies beyond the tensor.  16-byte stores from the registers, a row each, cost a forward call of 37800 x 5120
+// x 13824 that keeps its projections 9305 us.
 template <typename T>
 __device__ __forceinline__ void write_out(const CUtensorMap* to, uint8_t* mine, const float (&x)[32], int lane, int col,
                                           int row, int cols, int rows) {
@@ -151,7 +161,7 @@ __device__ __forceinline__ void write_out(const CUtensorMap* to, uint8_t* mine, 
 }
 
 // Tiles go in bands of `band` row tiles, column by column inside a band, so that the tiles at work at one time share
-// both their rows of A and their columns of B in L2.
+// both their rows of A and their columns of B in L2 (37800 x 5120 x 13824: bands of 4 to 24 are alike within 1 %).
 __device__ __forceinline__ void tile_at(const GemmParams& p, int tile, int& m, int& n) {
   const int per_band = p.band * p.n_tiles;
   const int b = tile / per_band, in = tile - b * per_band;
@@ -160,9 +170,9 @@ __device__ __forceinline__ void tile_at(const GemmParams& p, int tile, int& m, i
   m = b * p.band + in - n * height;
 }
 
-// What a pair of CTAs works on.  The first `whole` tiles go to the pairs round by round; of the K blocks of the rest, which
-// would leave pairs without a tile, each of the first `shares` pairs has an equal run, so that a tile's sums are in pieces
-// that gemm_join_kernel adds.  A run is no longer than a tile and touches two at most.
+// What a pair of CTAs works on.  The first `whole` tiles go to the pairs round by round; of the K blocks of the rest,
+// which would leave pairs without a tile, each of the first `shares` pairs has an equal run, so that a tile's sums are
+// in pieces that gemm_join_kernel adds.  A run is no longer than a tile and touches two at most.
 struct Walk {
   int tile, k0, k1, slot;  // at work: tile, blocks of K, and where to put the sums (-1: the whole tile is done)
   int next_whole, pairs, whole, blocks, lo, hi, next_slot;
@@ -298,7 +308,8 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
           }
         }
       }
-      // Copies still in flight after a wait that ran out are waited for, within the same limit: each stage's last phase.
+      // Copies still in flight after a wait that ran out are waited for, within the same limit: each stage's last
+      // phase.
       if (*s_abort && rank == 0) {
         const long long t0 = clock64();
         for (int q = 0; q < C::kStages; ++q) {
@@ -341,8 +352,9 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
     }
   } else {
     // ---- results: warp w has the lanes of quarter w % 4, and a share of the columns ----
-    // With one tile or two a pair, all warps do each; with more, eight warps do one tile while eight do the next, so that
-    // one tile's loads and stores fill the time of the other's exponentials (2825 x 96 x 5456: 23 us all together).
+    // With one tile or two a pair, all warps do each; with more, eight warps do one tile while eight do the next, so
+    // that one tile's loads and stores fill the time of the other's exponentials (2825 x 96 x 5456: 21.0 us, all
+    // together 24.5; 1024 x 512 x 2048, fewer than two tiles a pair: 9.2 all together, 9.6 in turn).
     const int quarter = warp & 3, sides = p.alternate ? 2 : 4, side = (warp >> 2) % sides;
     const int turn = p.alternate ? warp >> 3 : -1;
     uint8_t* mine = smem + C::kOffOut + warp * 2048;
@@ -454,13 +466,14 @@ __global__ void __launch_bounds__(kGemmThreads, 1)
 
 // ---- few tokens -----------------------------------------------------------------------------------------------------
 //
-// With a handful of tokens the call is one pass over the weights, and a 256-row tile of tokens would be all padding.  Here
-// the weights are the rows of the tile and the tokens its columns: D = [Wg; Wu] X^T, 2 F rows (F features of gate, then the
-// same of up) by N columns (the tokens, rounded up to 16).  A CTA has F features at a time, F as small as shares the hidden
-// size out evenly; the MMA takes 128 rows all the same, and those past 2 F are whatever lies behind in shared memory and
-// are never read.  Gate and up of a feature are in different lanes, so they meet in shared memory, where the order turns
-// to tokens by features for the store.  Where there are so few features that most SMs would have none, a cluster of CTAs
-// shares out K for each tile, and each adds a part of the results from the others' shared memory.
+// With a handful of tokens the call is one pass over the weights, and a 256-row tile of tokens would be all padding.
+// Here the weights are the rows of the tile and the tokens its columns: D = [Wg; Wu] X^T, 2 F rows (F features of gate,
+// then the same of up) by N columns (the tokens, rounded up to 16).  A CTA has F features at a time, F as small as
+// shares the hidden size out evenly; the MMA takes 128 rows all the same, and those past 2 F are whatever lies behind
+// in shared memory and are never read.  Gate and up of a feature are in different lanes, so they meet in shared memory,
+// where the order turns to tokens by features for the store.  Where there are so few features that most SMs would have
+// none, a cluster of CTAs shares out K for each tile, and each adds a part of the results from the others' shared
+// memory. Bound by HBM: 1 x 5120 x 13824 bf16 45 to 47 us = 6.0 to 6.3 TB/s, by L2 where the weights are there already.
 struct FewParams {
   void* out;
   void* keep[2];
@@ -680,15 +693,16 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   if (threadIdx.x == 0) report_abort(s_abort, p.status);
 }
 
-// Adds the pieces of a tile, in the order of K, and finishes it as gemm_kernel would have.  A thread has one row and eight columns (for
-// the forward call of both projections).
+// Adds the pieces of a tile, in the order of K, and finishes it as gemm_kernel would have.  A thread has one row and
+// eight columns (for the forward call of both projections).
 template <typename T, int kMode, int BN>
 __device__ __forceinline__ void join_tile(const GemmParams p, int cta) {
   const float* partial = p.partial;
   constexpr int kCols = kMode == kForward ? BN / 2 : BN;  // result columns of a tile
   const int rest = cta / (kCols / 8), c = (cta % (kCols / 8)) * 8;
   const int blocks = p.k_blocks * (kMode == kInput ? 2 : 1), lo = rest * blocks, hi = lo + blocks;
-  // pairs with blocks lo .. hi - 1; the first may have begun in the tile before, and has this one in its second slot then
+  // pairs with blocks lo .. hi - 1; the first may have begun in the tile before, and has this one in its second slot
+  // then
   int q = (int)((int64_t)lo * p.shares / ((int64_t)(p.m_tiles * p.n_tiles - p.whole) * blocks));
   while (q > 0 && Walk::share_begin(p, blocks, q) > lo) --q;
   while (Walk::share_begin(p, blocks, q + 1) <= lo) ++q;
@@ -767,8 +781,9 @@ __global__ void __launch_bounds__(256)
     join_tile<T, kWeights, BN>(pw, blockIdx.x - split);
 }
 
-// dG = dH * up * a'(gate), dU = dH * a(gate), eight elements a thread.  A CTA has 2048 elements of one row, or of everything
-// where rows follow one another without gaps: a division a CTA, not one a thread (37800 x 13824: 1241 us with that).
+// dG = dH * up * a'(gate), dU = dH * a(gate), eight elements a thread.  A CTA has 2048 elements of one row, or of
+// everything where rows follow one another without gaps: a division a CTA, not one a thread (37800 x 13824: 1241 us
+// with that).
 template <typename T>
 __global__ void __launch_bounds__(256) gate_grad_kernel(const T* dh, const T* gate, const T* up, T* dg, T* du,
                                                         int64_t ld, int64_t ld_out, int64_t row_length,
@@ -879,9 +894,9 @@ static int join_ctas(const GemmParams& p, int mode) {
   return (p.m_tiles * p.n_tiles - p.whole) * ((mode == kForward ? BN / 2 : BN) / 8);
 }
 
-// Clocks that a product takes on some pairs of SMs, and whether its last round is shared out by blocks of K for that (by
-// how many pairs; 0 = not): 512 a block of K, 2500 a unit for what no block hides, 12000 for writing sums out and the
-// launch that adds them.  share_all: every tile has to go that way (there are fewer than pairs).
+// Clocks that a product takes on some pairs of SMs, and whether its last round is shared out by blocks of K for that
+// (by how many pairs; 0 = not): 512 a block of K, 2500 a unit for what no block hides, 12000 for writing sums out and
+// the launch that adds them.  share_all: every tile has to go that way (there are fewer than pairs).
 static int64_t gemm_clocks(int tiles, int blocks, int pairs, bool share_all, int* shares) {
   *shares = 0;
   const int rounds = tiles / pairs, rest = tiles % pairs;
@@ -949,8 +964,8 @@ static int launch_gemm(const GemmParams& p, const GemmMaps& m, int dtype, cudaSt
 }
 
 // dX and dW together.  Alone, each of two small products leaves pairs of SMs without a tile in its last round; together
-// they share the pairs out so that both end at the same time.  What is shared out by blocks of K stays so for either product
-// alone, so that it gives the same bits.  Returns the pairs of dX.
+// they share the pairs out so that both end at the same time.  What is shared out by blocks of K stays so for either
+// product alone, so that it gives the same bits.  Returns the pairs of dX.
 static int plan_both(GemmParams* pi, GemmParams* pw) {
   const int ti = pi->m_tiles * pi->n_tiles, tw = pw->m_tiles * pw->n_tiles;
   const int bi = 2 * pi->k_blocks, bw = pw->k_blocks;
@@ -995,8 +1010,8 @@ static int launch_both(const GemmParams& pi, const GemmMaps& mi, const GemmParam
 // dG and dU have rows of whole 128-byte lines: a tile's rows of 128 bytes then lie in one line each, not in two (1003 x
 // 1160 x 2504, backward: 41 us without).
 static int64_t hidden_pitch(const sparsp_ffn& f) { return align_up(f.hidden, 64); }
-// Two parts need the halves of every tile of dX to meet, in pieces of K that are added; rows of so many tiles that pairs
-// have a whole one each are left out of it.
+// Two parts need the halves of every tile of dX to meet, in pieces of K that are added; rows of so many tiles that
+// pairs have a whole one each are left out of it.
 static bool two_parts(const sparsp_ffn& f) { return f.tokens <= kFewTokens && ceil_div(f.dim, BN) <= kPairs - 2; }
 static int64_t hidden_rows(const sparsp_ffn& f) { return two_parts(f) ? kFewTokens + f.tokens : f.tokens; }
 static int64_t hidden_bytes(const sparsp_ffn& f) { return align_up(hidden_rows(f) * hidden_pitch(f) * 2, 256); }
@@ -1011,9 +1026,9 @@ static int launch_few(const sparsp_ffn& f, const void* X, const void* Wg, const 
   FewParams p = {};
   p.columns = (int32_t)align_up(f.tokens, 16);
   p.k_blocks = ceil_div(f.dim, kStageK);
-  // CTAs that share out K, where there are few tiles, in pieces of eight blocks at least (100 x 5120 x 512: alone 17.8 us,
-  // two 12.6, four 10.1; 2 x 824 x 1144, pieces of six: alone 4.5, two 5.3).  Clusters of four find room on 128 SMs, of two
-  // on all; of eight there is not room for enough at once.
+  // CTAs that share out K, where there are few tiles, in pieces of eight blocks at least (100 x 5120 x 512: alone 17.8
+  // us, two 12.6, four 10.1; 2 x 824 x 1144, pieces of six: alone 4.5, two 5.3).  Clusters of four find room on 128
+  // SMs, of two on all; of eight there is not room for enough at once.
   auto splits = [&](int F) {
     const int tiles = ceil_div(f.hidden, F);
     if (tiles * 4 <= 128 && p.k_blocks >= 32) return 4;
@@ -1031,7 +1046,8 @@ static int launch_few(const sparsp_ffn& f, const void* X, const void* Wg, const 
   p.ld_turn = p.columns + 1;
   const int turn = (int)align_up(2 * p.features * p.ld_turn * 4, 128), room = kFewSmem - 16384 - turn - 1024;
   const int block = (2 * p.features + p.columns) * 128;
-  int deep = 4;  // blocks of K a stage, as many as leave four stages
+  // blocks of K a stage, as many as leave four stages (16 x 5120 x 13824: 44.5 us with four, 51.1 with one)
+  int deep = 4;
   while (deep > 1 && room / (deep * block) < 4) deep /= 2;
   p.stage_bytes = deep * block;
   p.stages = std::min(16, room / p.stage_bytes);
@@ -1135,7 +1151,9 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
   pi.two_parts = pw.two_parts = two_parts(f);
   if ((rc = prepare_gemm(&pi, kInput, f, ws)) != SPARSP_OK) return rc;
   if ((rc = prepare_gemm(&pw, kWeights, f, ws)) != SPARSP_OK) return rc;
-  // both at once up to four rounds of tiles: beyond that their last rounds matter less than that both want L2
+  // both at once up to four rounds of tiles (1003 x 1160 x 2504 36 us, one after the other 49; 2048 x 1024 x 4096, 3.5
+  // rounds, 67 and 77); with more, both ways are alike within what runs differ by (2048 x 2048 x 4096, 6.9 rounds:
+  // 114-122 and 115-118 us), and apart they read less at a time
   const bool small = (int64_t)pi.m_tiles * pi.n_tiles + (int64_t)pw.m_tiles * pw.n_tiles <= 4 * kPairs;
   const int pairs = small ? plan_both(&pi, &pw) : 0;
   if (dX != nullptr) {

@@ -12,8 +12,8 @@ namespace sparsp {
 
 constexpr int kMaxRotaryHeadDim = 256;
 constexpr int kMaxNormDim = 16384;
-// Work is shared out for the multiprocessors of a B200, whatever device a size of workspace is asked on: the shares also
-// decide in which order sums are made.
+// Work is shared out for the multiprocessors of a B200, whatever device a size of workspace is asked on: the shares
+// also decide in which order sums are made.
 constexpr int kSms = 148;
 
 inline int element_bytes(int dtype) { return dtype == SPARSP_FP32 ? 4 : 2; }

@@ -5,29 +5,36 @@
 
 namespace sparsp {
 
-// Rows are worked on by "workers": a warp each where a row is at most 512 values, otherwise a CTA.  A worker has consecutive
-// rows and holds the weights of the group it is in, so that they are read once per worker, not once per row.  It takes R
-// rows at a time, which share each barrier; their values stay in registers from there to the store.  The 2R rows after
-// them are on their way into shared memory: each thread copies the 16-byte pieces that it will itself use (cp.async), so
-// nobody waits for anybody else's copies.  There are as many workers as fit the multiprocessors by their registers and
-// their shared memory, so none waits for another to end.
+// Rows are worked on by "workers": a warp each where a row is at most 512 values, otherwise a CTA.  A worker has
+// consecutive rows and holds the weights of the group it is in, so that they are read once per worker, not once per
+// row.  It takes R rows at a time, which share each barrier; their values stay in registers from there to the store.
+// The 2R rows after them are on their way into shared memory: each thread copies the 16-byte pieces that it will itself
+// use (cp.async), so nobody waits for anybody else's copies.  There are as many workers as fit the multiprocessors by
+// their registers and their shared memory, so none waits for another to end.
 //
 // Rows of any length are read in 16-byte pieces.  Where a row is not a multiple of 16 bytes, every second, fourth or
 // eighth row begins at the same place inside its first piece: these make a class, and a worker has rows of one class
-// only, every P-th of its part, so that a thread's columns, and with them its weights and sums, do not change from row to
-// row.  (Value by value, backward over 15554 x 1921 fp32 took 153 us, with single 4-byte copies 111.)
+// only, every P-th of its part, so that a thread's columns, and with them its weights and sums, do not change from row
+// to row.  (Value by value, backward over 15554 x 1921 fp32 took 153 us, with single 4-byte copies 111.)
+//
+// Bound by HBM: 75600 x 5120 bf16 forward 253 to 274 us = 5.7 to 6.1 TB/s.  Backward, twice as much is read as written, and
+// by fewer warps, for the sums of the weights' gradients stay in registers: 397 to 446 us = 5.2 to 5.9 TB/s.
 constexpr int kNormThreads = 256;  // of a CTA whose warps are workers
 constexpr int kAhead = 3;          // batches of R rows in shared memory: one in use, two on their way
 
 // Who works on a row, by its length: a warp with 8 values a thread (up to 256) or 16 (512), or a CTA with 16 values a
 // thread and up to 320 threads (5120), of which a multiprocessor takes two or more, so that one computes while another
-// waits at its barrier; beyond that up to 512 threads with 16 values (8192) or 32.  Backward in fp32 it is shared memory
-// that says how many CTAs there are, and up to 2048 values more threads of 8 values each are better (15554 x 1921 70 us,
-// 112 with 16); elsewhere the sums over more threads cost more than they give (forward, 31000 x 1921 bf16: 89 and 61).
-// A warp takes several short rows at once: 4, 8 or 16 lanes have a row of up to 32, 64 or 128 values.
+// waits at its barrier; beyond that up to 512 threads with 16 values (8192) or 32.  Backward in fp32 it is shared
+// memory that says how many CTAs there are, and up to 2048 values more threads of 8 values each are better (15554 x
+// 1921 70 us, 112 with 16); elsewhere the sums over more threads cost more than they give (forward, 31000 x 1921 bf16:
+// 89 and 61). A warp takes several short rows at once: 4, 8 or 16 lanes have a row of up to 32, 64 or 128 values.
 enum Worker { kWarp8, kWarp16, kShortTeam, kTeam, kLongTeam, kLongestTeam };
-__host__ __device__ constexpr int worker_values(int kind) { return kind == kWarp8 || kind == kShortTeam ? 8 : kind == kLongestTeam ? 32 : 16; }
-__host__ __device__ constexpr int worker_threads(int kind) { return kind <= kWarp16 ? kNormThreads : kind == kShortTeam ? 256 : kind == kTeam ? 320 : 512; }  // of a CTA, at most
+__host__ __device__ constexpr int worker_values(int kind) {
+  return kind == kWarp8 || kind == kShortTeam ? 8 : kind == kLongestTeam ? 32 : 16;
+}
+__host__ __device__ constexpr int worker_threads(int kind) {  // of a CTA, at most
+  return kind <= kWarp16 ? kNormThreads : kind == kShortTeam ? 256 : kind == kTeam ? 320 : 512;
+}
 __host__ __device__ constexpr int worker_ctas(int kind) { return kind == kShortTeam ? 3 : kind <= kTeam ? 2 : 1; }  // such CTAs that fit a multiprocessor
 __host__ __device__ constexpr int worker_registers(int kind) { return kind == kShortTeam ? 80 : kind == kTeam ? 96 : 128; }
 // Rows at a time, by what the registers hold: forward the row and two weights, backward two rows and three weights or
@@ -37,7 +44,8 @@ __host__ __device__ constexpr int worker_rows(int kind, bool bwd) { return kind 
 // How a worker meets its rows.
 //   kPlain    every row begins on 16 bytes and is a multiple of them
 //   kShifted  rows in classes, pieces that a row shares with its neighbours
-//   kSingle   value by value: tensors that do not begin on 16 bytes or whose rows move against one another, and rows that
+//   kSingle   value by value: tensors that do not begin on 16 bytes or whose rows move against one another, and rows
+//   that
 //             shared memory does not hold
 // Plain rows have a form of their own because they leave the backward pass of 75600 x 5120 bf16 the registers that it
 // needs: 446 us in the other one.
@@ -110,9 +118,9 @@ struct Batches {
 };
 
 // Sums N values over the worker's threads, in an order that depends on its size alone; every thread gets the sums.
-// Inside a warp the values are halved with the lanes (after log2 N exchanges a lane carries one of them), so that N sums
-// take little more than one.  A CTA's warps meet in `slot`, which the caller alternates so that one barrier a call is
-// enough.
+// Inside a warp the values are halved with the lanes (after log2 N exchanges a lane carries one of them), so that N
+// sums take little more than one.  A CTA's warps meet in `slot`, which the caller alternates so that one barrier a call
+// is enough.
 template <int N, bool kCta>
 __device__ __forceinline__ void worker_sum(float (&v)[N], float (*slot)[N], int lanes) {
   const int lane = threadIdx.x & 31;
@@ -312,12 +320,13 @@ struct RowsAhead {
     }
   }
 };
-// One group of copies per batch of rows, an empty one past the end; at a batch's start all but the newest have to be there.
+// One group of copies per batch of rows, an empty one past the end; at a batch's start all but the newest have to be
+// there.
 __device__ __forceinline__ void close_batch() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void wait_batch() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
 
-// A thread's values of a row of weights, in 16-byte pieces where they lie so; zeros outside the row.  All loads are under
-// way together.
+// A thread's values of a row of weights, in 16-byte pieces where they lie so; zeros outside the row.  All loads are
+// under way together.
 template <typename W, int K, typename Rows>
 __device__ __forceinline__ void load_row(const W* row, int dim, const Rows& rows, float (&f)[K]) {
   constexpr int E = Rows::E;
@@ -468,7 +477,8 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
 
 // The gradients of the weights are sums over rows: each worker keeps those of its rows in registers and writes them out
 // where a group of its part ends.  Of P classes, class c of part i writes group g to slot (i + g) P + c, which no other
-// (worker, group) has, as rows and with them groups ascend from part to part.  norm_weights_kernel adds a group's slots.
+// (worker, group) has, as rows and with them groups ascend from part to part.  norm_weights_kernel adds a group's
+// slots.
 template <typename T, int kForm, int kKind>
 __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) norm_bwd_kernel(const NormParams p) {
   const void* x = p.x;
@@ -636,9 +646,10 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
   }
 }
 
-// Adds the slots of each group.  A CTA has kWeightColumns columns of one group; its threads take every 128th (32nd) slot
-// each and meet in shared memory, so the order is the same whatever runs when.  32 columns read whole lines; with eight,
-// narrow rows too have enough CTAs (70000 x 64 backward: 13.6 us, 21.3 with 32; 10000 x 8192: 112 us, 106 with 32).
+// Adds the slots of each group.  A CTA has kWeightColumns columns of one group; its threads take every 128th (32nd)
+// slot each and meet in shared memory, so the order is the same whatever runs when.  32 columns read whole lines; with
+// eight, narrow rows too have enough CTAs (70000 x 64 backward: 13.6 us, 21.3 with 32; 10000 x 8192: 112 us, 106 with
+// 32).
 template <int kWeightColumns>
 __global__ void __launch_bounds__(1024) norm_weights_kernel(const float* partial, int64_t rows, int64_t rows_per_group,
                                                             int64_t parts, int log_classes, int dim,
@@ -748,8 +759,8 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
     const int resident = std::min({32, 65536 / (p.threads * worker_registers(p.kind)), kNormSmem / (p.smem_bytes + 4096)});
     const int64_t rows = p.kind == kWarp8 ? (n.rows + (32 >> p.log_lanes) - 1) >> (5 - p.log_lanes) : n.rows;
     int64_t most = std::min<int64_t>(rows, (int64_t)kSms * resident * workers);
-    // backward, a worker's sums are written and read again: four rows of its own at least, if every SM has a worker (3023 x 752
-    // fp32: 14.0 us, 17.3 with eight, 15.6 with one)
+    // backward, a worker's sums are written and read again: four rows of its own at least, if every SM has a worker
+    // (3023 x 752 fp32: 14.0 us, 17.3 with eight, 15.6 with one)
     if (bwd) most = std::min(most, std::max<int64_t>(kSms, rows / 4));
     p.parts = (int)std::max<int64_t>(1, most >> p.log_classes);
     const int all = p.parts << p.log_classes;

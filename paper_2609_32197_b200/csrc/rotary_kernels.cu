@@ -5,8 +5,8 @@
 
 namespace sparsp {
 
-// One entry a thread.  The angle is coordinate * frequency in fp64: in fp32 the product alone would be 0.004 radians off
-// at position 100000.  Tables are made once per geometry.
+// One entry a thread.  The angle is coordinate * frequency in fp64: in fp32 the product alone would be 0.004 radians
+// off at position 100000.  Tables are made once per geometry.
 __global__ void __launch_bounds__(256) rotary_table_kernel(const double* __restrict__ inv_freq, double amplitude,
                                                            float2* __restrict__ table, int pt, int ph, int pw,
                                                            int64_t nt, int64_t nh, int64_t total) {
@@ -58,14 +58,17 @@ struct RotaryParams {
 };
 
 constexpr int kRotaryThreads = 256;
-constexpr int kRotaryHeads = 4;  // heads whose loads a thread has in flight at once
+// Heads whose loads a thread has in flight at once (48 heads x 17776 tokens x 64 fp16, token-major: 75.5 us, with two
+// 79.2, with eight, which leave fewer warps, 76.4; 40 heads x 75600 x 128: 491, 492, 502).
+constexpr int kRotaryHeads = 4;
 
 // A thread has one token and one unit of its row (16 bytes of interleaved pairs; two 16-byte vectors half the rotated
 // part apart; 16 bytes to be copied), finds the (cos, sin) of its pairs once and goes over the heads of Q and K with
 // them: the angles depend on the token alone, so the table costs little.  A token's units are consecutive lanes, so a
-// head's row is read and written whole; where heads lie closer together than tokens, a few heads of a token come next to
-// each other, so that a warp reads on in memory (48 heads x 17776 tokens x 64 fp16, token-major: 84 us without).
-// E: elements of a vector, 1 where the rotated part or the pairs do not begin and end on 16 bytes.
+// head's row is read and written whole; where heads lie closer together than tokens, a few heads of a token come next
+// to each other, so that a warp reads on in memory (48 heads x 17776 tokens x 64 fp16, token-major: 84 us without).
+// Bound by HBM: 40 heads x 75600 x 128 bf16, Q and K, 491 us = 6.3 TB/s. E: elements of a vector, 1 where the rotated
+// part or the pairs do not begin and end on 16 bytes.
 template <typename T, int E, bool kHalf>
 __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const RotaryParams p) {
   const int32_t* positions = p.positions;
@@ -199,7 +202,8 @@ static cudaError_t launch_rotary_t(RotaryParams p, int head_dim, cudaStream_t st
   p.head_lanes = p.sH < p.sT ? std::min(p.heads, std::max(1, 32 / p.units)) : 1;
   p.tokens_per_cta = kRotaryThreads / (p.units * p.head_lanes);
   const int64_t tiles = ((int64_t)p.all_tokens + p.tokens_per_cta - 1) / p.tokens_per_cta;
-  // all heads to a CTA, unless there are too few tokens to fill the GPU that way
+  // all heads to a CTA, unless there are too few tokens for eight CTAs an SM that way (40 heads x 5120 tokens x 128:
+  // 36.5 us, with four CTAs 39.4, with sixteen 37.7)
   int64_t per = p.heads;
   while (per > p.head_lanes && tiles * ((p.heads + per - 1) / per) < 8 * kSms) per = (per + 1) / 2;
   p.heads_per_cta = (int)per;

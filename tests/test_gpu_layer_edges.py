@@ -197,3 +197,22 @@ def test_infinite_gradients_of_few_tokens():
     dx, dwg, dwu = (torch.empty_like(t) for t in (x, wg, wu))
     binding.sparsp_gated_ffn_bwd(ffn, dh, x, wg, wu * 0, gate, up, dx, dwg, dwu, ws)
     assert bool(torch.isinf(dx[1]).all()) and not bool(torch.isnan(dx[1]).any())
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu_tanh", "gelu"])
+@pytest.mark.parametrize("m", [100, 300])
+def test_activations_keep_their_relative_error(m, kind):
+    """Gates from -6 to 3 as they are, each times powers of two: what is left of the activation far down shows.
+
+    Off by: the argument of the exponential, up to 40 in size, with four roundings (160 * 2^-24 * ln 2 = 2^-17.2), a
+    polynomial within 2^-20, six roundings; together below 2^-16.  Then one rounding to the type."""
+    d, f = 64, 208
+    x = torch.zeros(m, d, dtype=HF, device="cuda")
+    x[:, 0], x[:, 1] = torch.linspace(-6, 3, m).to("cuda", HF), 1
+    wg, wu = torch.zeros(f, d, dtype=HF, device="cuda"), torch.zeros(f, d, dtype=HF, device="cuda")
+    wg[:, 0], wu[:, 1] = 1, 2.0 ** (torch.arange(f, device="cuda") % 13)
+    h = torch.full((m, f), float("nan"), dtype=HF, device="cuda")
+    ffn = binding.make_ffn(m, d, f, kind, HF)
+    binding.sparsp_gated_ffn_fwd(ffn, x, wg, wu, h, None, None, binding.make_ffn_workspace(ffn, False))
+    want = ffn_tests.activation(kind, x[:, :1].double())[0] * wu[None, :, 1].double()
+    close(h, want, want.abs() * (UNIT[HF] + 2.0 ** -16) + TINY[HF], kind)
