@@ -45,8 +45,7 @@ __host__ __device__ constexpr int worker_rows(int kind, bool bwd) { return kind 
 //   kPlain    every row begins on 16 bytes and is a multiple of them
 //   kShifted  rows in classes, pieces that a row shares with its neighbours
 //   kSingle   value by value: tensors that do not begin on 16 bytes or whose rows move against one another, and rows
-//   that
-//             shared memory does not hold
+//             that shared memory does not hold
 // Plain rows have a form of their own because they leave the backward pass of 75600 x 5120 bf16 the registers that it
 // needs: 446 us in the other one.
 enum Form { kPlain, kShifted, kSingle };
