@@ -755,7 +755,10 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
       p.log_classes = 0;
       continue;
     }
-    const int resident = std::min({32, 65536 / (p.threads * worker_registers(p.kind)), kNormSmem / (p.smem_bytes + 4096)});
+    // each quarter of a multiprocessor has registers for so many warps of its own (100000 x 1536 bf16, CTAs of three warps,
+    // of which six fit, not seven: forward 110 us, 130 with seven; backward 185 and 210)
+    const int warps = 4 * (16384 / (32 * worker_registers(p.kind)));
+    const int resident = std::min({32, warps * 32 / p.threads, kNormSmem / (p.smem_bytes + 4096)});
     const int64_t rows = p.kind == kWarp8 ? (n.rows + (32 >> p.log_lanes) - 1) >> (5 - p.log_lanes) : n.rows;
     int64_t most = std::min<int64_t>(rows, (int64_t)kSms * resident * workers);
     // backward, a worker's sums are written and read again: four rows of its own at least, if every SM has a worker
