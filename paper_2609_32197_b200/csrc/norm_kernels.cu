@@ -5,10 +5,10 @@
 
 namespace sparsp {
 
-// Rows are worked on by "workers": a warp each where a row is at most 512 values, otherwise a CTA.  A worker has
+// Rows are worked on by "workers": a warp each where a row is at most 1280 values, otherwise a CTA.  A worker has
 // consecutive rows and holds the weights of the group it is in, so that they are read once per worker, not once per
 // row.  It takes R rows at a time, which share each barrier; their values stay in registers from there to the store.
-// The 2R rows after them are on their way into shared memory: each thread copies the 16-byte pieces that it will itself
+// The next 2R rows are on their way into shared memory: each thread copies the 16-byte pieces that it will itself
 // use (cp.async), so nobody waits for anybody else's copies.  There are as many workers as fit the multiprocessors by
 // their registers and their shared memory, so none waits for another to end.
 //
@@ -17,29 +17,41 @@ namespace sparsp {
 // only, every P-th of its part, so that a thread's columns, and with them its weights and sums, do not change from row
 // to row.  (Value by value, backward over 15554 x 1921 fp32 took 153 us, with single 4-byte copies 111.)
 //
-// Bound by HBM: 75600 x 5120 bf16 forward 253 to 274 us = 5.7 to 6.1 TB/s.  Backward, twice as much is read as written, and
-// by fewer warps, for the sums of the weights' gradients stay in registers: 397 to 446 us = 5.2 to 5.9 TB/s.
-constexpr int kNormThreads = 256;  // of a CTA whose warps are workers
-constexpr int kAhead = 3;          // batches of R rows in shared memory: one in use, two on their way
+// Bound by HBM: 75600 x 5120 bf16 forward 245 to 256 us = 6.1 to 6.3 TB/s.  Backward, twice as much is read as written,
+// by few warps, for the sums of the weights' gradients stay in registers: 383 to 409 us = 5.7 to 6.1 TB/s.
 
-// Who works on a row, by its length: a warp with 8 values a thread (up to 256) or 16 (512), or a CTA with 16 values a
-// thread and up to 320 threads (5120), of which a multiprocessor takes two or more, so that one computes while another
-// waits at its barrier; beyond that up to 512 threads with 16 values (8192) or 32.  Backward in fp32 it is shared
-// memory that says how many CTAs there are, and up to 2048 values more threads of 8 values each are better (15554 x
-// 1921 70 us, 112 with 16); elsewhere the sums over more threads cost more than they give (forward, 31000 x 1921 bf16:
-// 89 and 61). A warp takes several short rows at once: 4, 8 or 16 lanes have a row of up to 32, 64 or 128 values.
-enum Worker { kWarp8, kWarp16, kShortTeam, kTeam, kLongTeam, kLongestTeam };
-__host__ __device__ constexpr int worker_values(int kind) {
-  return kind == kWarp8 || kind == kShortTeam ? 8 : kind == kLongestTeam ? 32 : 16;
-}
-__host__ __device__ constexpr int worker_threads(int kind) {  // of a CTA, at most
-  return kind <= kWarp16 ? kNormThreads : kind == kShortTeam ? 256 : kind == kTeam ? 320 : 512;
-}
-__host__ __device__ constexpr int worker_ctas(int kind) { return kind == kShortTeam ? 3 : kind <= kTeam ? 2 : 1; }  // such CTAs that fit a multiprocessor
-__host__ __device__ constexpr int worker_registers(int kind) { return kind == kShortTeam ? 80 : kind == kTeam ? 96 : 128; }
-// Rows at a time, by what the registers hold: forward the row and two weights, backward two rows and three weights or
-// sums.
-__host__ __device__ constexpr int worker_rows(int kind, bool bwd) { return kind == kWarp8 ? (bwd ? 2 : 4) : kind == kLongestTeam || bwd ? 1 : 2; }
+// Who works on a row, by its length: a warp up to 1280 values, otherwise a team, a CTA of as few warps as hold the row
+// with 24, 32 or 40 values a thread.  Few warps with many registers are better than more with fewer: what a row costs
+// beside its values (sums over the lanes, barriers, turns of the loop) is shared by more of them, the loads ahead need
+// no warps, and a row that nearly fills its lanes wastes none (174000 x 1152 bf16 backward 195 us, 284 by three warps
+// with 16 values a thread; 260000 x 768 215 and 260; 98000 x 2048 204 and 217; 75600 x 5120 383 to 402 and 393 to 412
+// with 10 warps).  A warp takes several short rows at once: 4, 8 or 16 lanes have a row of up to 32, 64 or 128 values.
+enum Worker { kWarp8, kWarp16, kWarp24, kWarp32, kWarp40, kTeam24, kTeam32, kTeam40, kLongTeam };
+struct WorkerKind {  // pairs: forward, backward
+  int values;                     // of a thread
+  int threads[2], registers[2];   // of a multiprocessor's threads, and what that leaves a thread
+  int rows[2];                    // at a time
+  int ahead[2];                   // batches of so many rows in shared memory
+};
+// Rows at a time by what the registers hold: forward the row and two weights, backward two rows and three weights or
+// sums. Batches: one in use and two on their way, or two, the next but one of which follows the one in use to its place
+// as soon as that is in registers.  With two, backward, another CTA fits a multiprocessor where rows are long (21700 x
+// 4608 fp32 211 us, 261 with three); where nothing more fits, three are as good or better (300000 x 512 bf16 156 us,
+// 165 with two; 75600 x 5120 forward 251 and 254).
+constexpr WorkerKind kWorkers[] = {
+    {8, {512, 512}, {128, 128}, {4, 2}, {3, 3}},   // kWarp8
+    {16, {512, 512}, {128, 128}, {2, 1}, {3, 3}},  // kWarp16
+    {24, {384, 384}, {168, 168}, {2, 1}, {3, 2}},  // kWarp24
+    {32, {384, 256}, {168, 255}, {1, 1}, {3, 2}},  // kWarp32
+    {40, {384, 256}, {168, 255}, {1, 1}, {3, 2}},  // kWarp40
+    {24, {384, 384}, {168, 168}, {2, 1}, {3, 2}},  // kTeam24
+    {32, {384, 256}, {168, 255}, {1, 1}, {3, 2}},  // kTeam32
+    {40, {384, 256}, {168, 255}, {1, 1}, {3, 2}},  // kTeam40
+    {32, {512, 512}, {128, 128}, {1, 1}, {3, 2}},  // kLongTeam
+};
+
+// Threads of a CTA whose warps are workers
+__host__ __device__ constexpr int warp_threads(int kind) { return kind <= kWarp16 ? 256 : 128; }
 
 // How a worker meets its rows.
 //   kPlain    every row begins on 16 bytes and is a multiple of them
@@ -49,6 +61,11 @@ __host__ __device__ constexpr int worker_rows(int kind, bool bwd) { return kind 
 // Plain rows have a form of their own because they leave the backward pass of 75600 x 5120 bf16 the registers that it
 // needs: 446 us in the other one.
 enum Form { kPlain, kShifted, kSingle };
+
+// Backward, a thread's weights are in shared memory where there are no registers for them.
+__host__ __device__ constexpr bool weights_shared(int form, int kind) {
+  return form != kPlain || kind == kWarp40 || kind == kTeam40;
+}
 
 struct NormParams {
   const void* x;
@@ -204,7 +221,7 @@ struct Place {
   }
 };
 
-template <typename T, int kForm, int NV, int R>
+template <typename T, int kForm, int NV, int R, int kAhead>
 struct RowsAhead {
   static constexpr int E = kForm == kSingle ? 1 : 16 / sizeof(T);
   Vec<T, E> next[E > 1 ? 1 : R][E > 1 ? 1 : NV];
@@ -213,7 +230,6 @@ struct RowsAhead {
   char* ring;  // this thread's places, `threads` pieces from one to the next
   int lanes, t, dim, shift, threads;
   int at_once, sub;  // rows that a warp has at once, and which of them is this thread's
-
 
   __device__ __forceinline__ RowsAhead(const void* x, int64_t row, int64_t ld, int log_classes, char* place,
                                        const Place& me, int dim)
@@ -324,6 +340,12 @@ struct RowsAhead {
 __device__ __forceinline__ void close_batch() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void wait_batch() { asm volatile("cp.async.wait_group 1;" ::: "memory"); }
 
+// Where the batch after the next goes: to the one before this, or with two places to this one, which has been read.
+template <int kAhead>
+__device__ __forceinline__ int refilled(int at) {
+  return kAhead == 2 ? at : at == 0 ? kAhead - 1 : at - 1;
+}
+
 // A thread's values of a row of weights, in 16-byte pieces where they lie so; zeros outside the row.  All loads are
 // under way together.
 template <typename W, int K, typename Rows>
@@ -366,21 +388,22 @@ __device__ __forceinline__ void load_weights(const NormParams& p, const void* fr
 }
 
 template <typename T, int kForm, int kKind>
-__global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) norm_fwd_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kWorkers[kKind].threads[0], 1) norm_fwd_kernel(const NormParams p) {
   const void* x = p.x;
   enter_grid(x);
-  constexpr int E = kForm == kSingle ? 1 : 16 / sizeof(T), K = worker_values(kKind), NV = K / E, R = worker_rows(kKind, false);
-  constexpr bool kCta = kKind >= kShortTeam, kRing = E > 1;
+  constexpr int E = kForm == kSingle ? 1 : 16 / sizeof(T), K = kWorkers[kKind].values, NV = K / E;
+  constexpr int R = kWorkers[kKind].rows[0], kAhead = kWorkers[kKind].ahead[0];
+  constexpr bool kCta = kKind >= kTeam24, kRing = E > 1;
   extern __shared__ __align__(16) char ring[];
   __shared__ float slots[4][32][R];
   const Place me(kCta, kKind == kWarp8, p.log_lanes);
   const int t = me.t, batch = R * me.at_once;
-  const int worker = kCta ? blockIdx.x : blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
+  const int worker = kCta ? blockIdx.x : blockIdx.x * (warp_threads(kKind) / 32) + (threadIdx.x >> 5);
   if (worker >= (kForm == kShifted ? p.parts << p.log_classes : p.parts)) return;
   const Mine<kForm == kShifted> m(p, worker);
   Batches<Mine<kForm == kShifted>> ahead(m);
   const int64_t r = m.row(m.below(m.lo));
-  RowsAhead<T, kForm, NV, R> rows(x, r, p.stride_x, m.log_classes(),
+  RowsAhead<T, kForm, NV, R, kAhead> rows(x, r, p.stride_x, m.log_classes(),
                                   ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes), me, p.dim);
   const bool ragged = rows.has_outside();
   const int64_t out_stride = p.stride_y << m.log_classes();
@@ -422,9 +445,9 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
         for (int j = 1; j < K / 2; ++j) s = s + cur[k][j];
         sum[k] = s.sum();
       }
-      // the batch after the next: into the places of the one before this, or the registers that were just emptied
+      // the batch after the next: into the places that are free, or the registers that were just emptied
       const int more = ahead.size(batch);
-      rows.fetch(more, at == 0 ? 2 : at - 1);
+      rows.fetch(more, refilled<kAhead>(at));
       if constexpr (kRing) close_batch();
       ahead.take(m, more);
       worker_sum<R, kCta>(sum, slots[phase], me.lanes);
@@ -466,7 +489,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
       if constexpr (kRing) {
         n[0] = n[1];
         n[1] = more;
-        at = at == 2 ? 0 : at + 1;
+        at = at == kAhead - 1 ? 0 : at + 1;
       } else {
         n[0] = more;
       }
@@ -479,23 +502,24 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
 // (worker, group) has, as rows and with them groups ascend from part to part.  norm_weights_kernel adds a group's
 // slots.
 template <typename T, int kForm, int kKind>
-__global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) norm_bwd_kernel(const NormParams p) {
+__global__ void __launch_bounds__(kWorkers[kKind].threads[1], 1) norm_bwd_kernel(const NormParams p) {
   const void* x = p.x;
   enter_grid(x);
-  constexpr int E = kForm == kSingle ? 1 : 16 / sizeof(T), K = worker_values(kKind), NV = K / E, R = worker_rows(kKind, true);
-  constexpr bool kCta = kKind >= kShortTeam, kRing = E > 1;
+  constexpr int E = kForm == kSingle ? 1 : 16 / sizeof(T), K = kWorkers[kKind].values, NV = K / E;
+  constexpr int R = kWorkers[kKind].rows[1], kAhead = kWorkers[kKind].ahead[1];
+  constexpr bool kCta = kKind >= kTeam24, kRing = E > 1;
   extern __shared__ __align__(16) char ring[];
   __shared__ float slots[2][32][2 * R];
   const Place me(kCta, kKind == kWarp8, p.log_lanes);
   const int t = me.t, batch = R * me.at_once;
-  const int worker = kCta ? blockIdx.x : blockIdx.x * (kNormThreads / 32) + (threadIdx.x >> 5);
+  const int worker = kCta ? blockIdx.x : blockIdx.x * (warp_threads(kKind) / 32) + (threadIdx.x >> 5);
   if (worker >= (kForm == kShifted ? p.parts << p.log_classes : p.parts)) return;
   const Mine<kForm == kShifted> m(p, worker);
   Batches<Mine<kForm == kShifted>> ahead(m);
   const int64_t r = m.row(m.below(m.lo));
   char* place = ring + (kCta ? 0 : (threadIdx.x >> 5) * p.ring_bytes);
-  RowsAhead<T, kForm, NV, R> xs(x, r, p.stride_x, m.log_classes(), place, me, p.dim);
-  RowsAhead<T, kForm, NV, R> ys(p.dy, r, p.stride_y, m.log_classes(), place + p.ring_half, me, p.dim);
+  RowsAhead<T, kForm, NV, R, kAhead> xs(x, r, p.stride_x, m.log_classes(), place, me, p.dim);
+  RowsAhead<T, kForm, NV, R, kAhead> ys(p.dy, r, p.stride_y, m.log_classes(), place + p.ring_half, me, p.dim);
   T* out = reinterpret_cast<T*>(p.y) + r * p.stride_x - xs.shift + t * E + me.sub * xs.stride;
   // a thread's weights, four from place to place of the threads: but for plain rows there are no registers for them
   float4* ws = reinterpret_cast<float4*>(place + p.ring_bytes - me.threads * K * 4) + me.thread;
@@ -532,7 +556,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
     int left = (int)(m.below(e) - m.below(a0));
     F2 w[K / 2], dw[K / 2], db[K / 2];
     load_weights<T, K>(p, p.weight, g, xs, 1.0f, w);
-    if constexpr (kForm != kPlain) {
+    if constexpr (weights_shared(kForm, kKind)) {
 #pragma unroll
       for (int j = 0; j < K / 4; ++j) {
         float4 four;
@@ -562,7 +586,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
 #pragma unroll
         for (int j = 0; j < K / 2; ++j) {
           const F2 dy = a[k][j];
-          if constexpr (kForm != kPlain) {
+          if constexpr (weights_shared(kForm, kKind)) {
             if (j % 2 == 0) four = ws[j / 2 * me.threads];
             w[j] = j % 2 == 0 ? F2(four.x, four.y) : F2(four.z, four.w);
           }
@@ -577,8 +601,8 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
         sum[2 * k + 1] = s1.sum();
       }
       const int more = ahead.size(batch);
-      xs.fetch(more, at == 0 ? 2 : at - 1);
-      ys.fetch(more, at == 0 ? 2 : at - 1);
+      xs.fetch(more, refilled<kAhead>(at));
+      ys.fetch(more, refilled<kAhead>(at));
       if constexpr (kRing) close_batch();
       ahead.take(m, more);
       stats(kRing ? n[1] : more);
@@ -598,7 +622,7 @@ __global__ void __launch_bounds__(worker_threads(kKind), worker_ctas(kKind)) nor
       if constexpr (kRing) {
         n[0] = n[1];
         n[1] = more;
-        at = at == 2 ? 0 : at + 1;
+        at = at == kAhead - 1 ? 0 : at + 1;
       } else {
         n[0] = more;
       }
@@ -722,6 +746,30 @@ struct NormPlan {
   unsigned grid;
 };
 
+// By the values that a worker has to hold.  Teams: the least that holds them of those whose number of warps shares out
+// a multiprocessor's 12 or 8 (forward 16 of kLongTeam), a whole multiprocessor's beyond 5120 (backward) or 7680.
+static int worker_kind(int span, bool bwd) {
+  if (span <= 1280)
+    return span <= 256 ? kWarp8 : span <= 512 ? kWarp16 : span <= 768 ? kWarp24 : span <= 1024 ? kWarp32 : kWarp40;
+  struct Team {
+    int warps, kind;
+  };
+  static const Team both[] = {{2, kTeam24}, {2, kTeam32}, {3, kTeam24}, {2, kTeam40}, {4, kTeam24}, {4, kTeam32}, {4, kTeam40}};
+  static const Team forward[] = {{6, kTeam32}, {6, kTeam40}, {8, kLongTeam}, {12, kTeam24}};
+  static const Team backward[] = {{8, kTeam32}, {8, kTeam40}};
+  const auto holds = [&](const Team& t) { return span <= t.warps * 32 * kWorkers[t.kind].values; };
+  for (const Team& t : both)
+    if (holds(t)) return t.kind;
+  if (bwd) {
+    for (const Team& t : backward)
+      if (holds(t)) return t.kind;
+  } else {
+    for (const Team& t : forward)
+      if (holds(t)) return t.kind;
+  }
+  return kLongTeam;
+}
+
 constexpr int kNormSmem = 224 * 1024;  // of a multiprocessor, for rings
 
 static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
@@ -737,28 +785,28 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
   for (;;) {
     const int E = p.form == kSingle ? 1 : 16 / bytes;
     const int units = (n.dim + (p.log_classes > 0 ? E - 1 : 0) + E - 1) / E, span = units * E;
-    p.kind = span <= 256 ? kWarp8 : span <= 512 ? kWarp16 : span <= 5120 ? kTeam : span <= 8192 ? kLongTeam : kLongestTeam;
-    if (p.kind == kTeam && span <= 2048 && bwd && bytes == 4) p.kind = kShortTeam;
+    p.kind = worker_kind(span, bwd);
     p.log_lanes = 2;
     while (p.log_lanes < 5 && (8 << p.log_lanes) < span) ++p.log_lanes;
-    const bool cta = p.kind >= kShortTeam;
-    const int per_thread = worker_values(p.kind) / E;
-    p.threads = cta ? ((units + per_thread - 1) / per_thread + 31) / 32 * 32 : kNormThreads;
-    const int workers = cta ? 1 : kNormThreads / 32, lanes = cta ? p.threads : 32;  // workers of a CTA
-    const int values = lanes * worker_values(p.kind);
-    p.ring_half = p.form == kSingle ? 0 : kAhead * worker_rows(p.kind, bwd) * values * bytes;
-    p.ring_bytes = bwd ? 2 * p.ring_half + (p.form == kPlain ? 0 : values * 4) : p.ring_half;
+    const bool cta = p.kind >= kTeam24;
+    const WorkerKind& kind = kWorkers[p.kind];
+    const int per_thread = kind.values / E;
+    p.threads = cta ? ((units + per_thread - 1) / per_thread + 31) / 32 * 32 : warp_threads(p.kind);
+    const int workers = cta ? 1 : p.threads / 32, lanes = cta ? p.threads : 32;  // workers of a CTA
+    const int values = lanes * kind.values;
+    p.ring_half = p.form == kSingle ? 0 : kind.ahead[bwd] * kind.rows[bwd] * values * bytes;
+    p.ring_bytes = bwd ? 2 * p.ring_half + (weights_shared(p.form, p.kind) ? values * 4 : 0) : p.ring_half;
     p.smem_bytes = p.ring_bytes * workers;
-    // three long rows of x and of dy, and a row that begins behind the first of 16384 places, do not fit
-    if (p.form != kSingle && (p.smem_bytes > kNormSmem - 4096 || p.threads > worker_threads(p.kind))) {
+    // rows of x and of dy that are too long, and a row that begins behind the first of 16384 places, do not fit
+    if (p.form != kSingle && (p.smem_bytes > kNormSmem - 4096 || p.threads > kind.threads[bwd])) {
       p.form = kSingle;
       p.log_classes = 0;
       continue;
     }
-    // each quarter of a multiprocessor has registers for so many warps of its own (100000 x 1536 bf16, CTAs of three warps,
-    // of which six fit, not seven: forward 110 us, 130 with seven; backward 185 and 210)
-    const int warps = 4 * (16384 / (32 * worker_registers(p.kind)));
-    const int resident = std::min({32, warps * 32 / p.threads, kNormSmem / (p.smem_bytes + 4096)});
+    // each quarter of a multiprocessor has registers for so many warps of its own (100000 x 1536 bf16, CTAs of three
+    // warps, of which six fit, not seven: forward 110 us, 130 with seven; backward 185 and 210)
+    const int warps = 4 * (16384 / (32 * kind.registers[bwd]));
+    const int resident = std::min({32, warps * 32 / p.threads, kNormSmem / (p.smem_bytes + 2048)});
     const int64_t rows = p.kind == kWarp8 ? (n.rows + (32 >> p.log_lanes) - 1) >> (5 - p.log_lanes) : n.rows;
     int64_t most = std::min<int64_t>(rows, (int64_t)kSms * resident * workers);
     // backward, a worker's sums are written and read again: four rows of its own at least, if every SM has a worker
@@ -800,14 +848,16 @@ static cudaError_t launch_norm_t(const NormParams& p, const NormPlan& plan, bool
 
 template <typename T, int kForm>
 static cudaError_t launch_norm_f(const NormParams& p, const NormPlan& plan, bool bwd, cudaStream_t st) {
-  if constexpr (sizeof(T) == 4)
-    if (plan.kind == kShortTeam) return launch_kernel_of(norm_bwd_kernel<T, kForm, kShortTeam>, p, plan, st);
   switch (plan.kind) {
     case kWarp8: return launch_norm_t<T, kForm, kWarp8>(p, plan, bwd, st);
+    case kTeam24: return launch_norm_t<T, kForm, kTeam24>(p, plan, bwd, st);
+    case kTeam32: return launch_norm_t<T, kForm, kTeam32>(p, plan, bwd, st);
+    case kTeam40: return launch_norm_t<T, kForm, kTeam40>(p, plan, bwd, st);
+    case kWarp40: return launch_norm_t<T, kForm, kWarp40>(p, plan, bwd, st);
+    case kWarp32: return launch_norm_t<T, kForm, kWarp32>(p, plan, bwd, st);
+    case kWarp24: return launch_norm_t<T, kForm, kWarp24>(p, plan, bwd, st);
     case kWarp16: return launch_norm_t<T, kForm, kWarp16>(p, plan, bwd, st);
-    case kTeam: return launch_norm_t<T, kForm, kTeam>(p, plan, bwd, st);
-    case kLongTeam: return launch_norm_t<T, kForm, kLongTeam>(p, plan, bwd, st);
-    default: return launch_norm_t<T, kForm, kLongestTeam>(p, plan, bwd, st);
+    default: return launch_norm_t<T, kForm, kLongTeam>(p, plan, bwd, st);
   }
 }
 
