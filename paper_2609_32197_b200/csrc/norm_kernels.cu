@@ -26,15 +26,15 @@ namespace sparsp {
 // no warps, and a row that nearly fills its lanes wastes none (174000 x 1152 bf16 backward 195 us, 284 by three warps
 // with 16 values a thread; 260000 x 768 215 and 260; 98000 x 2048 204 and 217; 75600 x 5120 383 to 402 and 393 to 412
 // with 10 warps).  A warp takes several short rows at once: 4, 8 or 16 lanes have a row of up to 32, 64 or 128 values.
-enum Worker { kWarp8, kWarp16, kWarp24, kWarp32, kWarp40, kTeam24, kTeam32, kTeam40, kLongTeam };
+enum Worker { kWarp8, kWarp16, kWarp24, kWarp32, kWarp40, kTeam24, kTeam32, kTeam40, kWideTeam, kLongTeam };
 struct WorkerKind {  // pairs: forward, backward
-  int values;                     // of a thread
-  int threads[2], registers[2];   // of a multiprocessor's threads, and what that leaves a thread
-  int rows[2];                    // at a time
-  int ahead[2];                   // batches of so many rows in shared memory
+  int values;                    // of a thread
+  int threads[2], registers[2];  // of a multiprocessor, and what that leaves a thread
+  int rows[2];                   // at a time
+  int ahead[2];                  // batches of so many rows in shared memory
 };
 // Rows at a time by what the registers hold: forward the row and two weights, backward two rows and three weights or
-// sums. Batches: one in use and two on their way, or two, the next but one of which follows the one in use to its place
+// sums.  Batches: one in use and two on their way, or two, the next but one of which follows the one in use to its place
 // as soon as that is in registers.  With two, backward, another CTA fits a multiprocessor where rows are long (21700 x
 // 4608 fp32 211 us, 261 with three); where nothing more fits, three are as good or better (300000 x 512 bf16 156 us,
 // 165 with two; 75600 x 5120 forward 251 and 254).
@@ -47,10 +47,11 @@ constexpr WorkerKind kWorkers[] = {
     {24, {384, 384}, {168, 168}, {2, 1}, {3, 2}},  // kTeam24
     {32, {384, 256}, {168, 255}, {1, 1}, {3, 2}},  // kTeam32
     {40, {384, 256}, {168, 255}, {1, 1}, {3, 2}},  // kTeam40
+    {32, {384, 384}, {168, 168}, {1, 1}, {3, 2}},  // kWideTeam: backward, one on a multiprocessor
     {32, {512, 512}, {128, 128}, {1, 1}, {3, 2}},  // kLongTeam
 };
 
-// Threads of a CTA whose warps are workers
+// Threads of a CTA whose warps are workers (260000 x 384 fp32 backward: 211 us, 239 in CTAs of 128)
 __host__ __device__ constexpr int warp_threads(int kind) { return kind <= kWarp16 ? 256 : 128; }
 
 // How a worker meets its rows.
@@ -58,13 +59,13 @@ __host__ __device__ constexpr int warp_threads(int kind) { return kind <= kWarp1
 //   kShifted  rows in classes, pieces that a row shares with its neighbours
 //   kSingle   value by value: tensors that do not begin on 16 bytes or whose rows move against one another, and rows
 //             that shared memory does not hold
-// Plain rows have a form of their own because they leave the backward pass of 75600 x 5120 bf16 the registers that it
-// needs: 446 us in the other one.
+// Plain rows have a form of their own because nothing of theirs has to be masked (75600 x 5120 bf16 forward 246 us, 261 in
+// the other form, backward 387 and 406; 104000 x 1920 backward 210 and 240).
 enum Form { kPlain, kShifted, kSingle };
 
 // Backward, a thread's weights are in shared memory where there are no registers for them.
 __host__ __device__ constexpr bool weights_shared(int form, int kind) {
-  return form != kPlain || kind == kWarp40 || kind == kTeam40;
+  return form != kPlain || kind == kWarp40 || kind == kTeam40 || kind == kWideTeam;
 }
 
 struct NormParams {
@@ -754,9 +755,11 @@ static int worker_kind(int span, bool bwd) {
   struct Team {
     int warps, kind;
   };
-  static const Team both[] = {{2, kTeam24}, {2, kTeam32}, {3, kTeam24}, {2, kTeam40}, {4, kTeam24}, {4, kTeam32}, {4, kTeam40}};
+  static const Team both[] = {{2, kTeam24}, {2, kTeam32}, {3, kTeam24}, {2, kTeam40},
+                              {4, kTeam24}, {4, kTeam32}, {4, kTeam40}};
   static const Team forward[] = {{6, kTeam32}, {6, kTeam40}, {8, kLongTeam}, {12, kTeam24}};
-  static const Team backward[] = {{8, kTeam32}, {8, kTeam40}};
+  // 17400 x 11000 bf16 backward: 234 us, 565 by kLongTeam, which has to put registers aside
+  static const Team backward[] = {{8, kTeam32}, {8, kTeam40}, {12, kWideTeam}};
   const auto holds = [&](const Team& t) { return span <= t.warps * 32 * kWorkers[t.kind].values; };
   for (const Team& t : both)
     if (holds(t)) return t.kind;
@@ -782,10 +785,10 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
       while ((n.stride_x << p.log_classes) % E) ++p.log_classes;
     p.form = n.dim % E == 0 && p.log_classes == 0 ? kPlain : kShifted;
   }
-  for (;;) {
+  for (bool long_team = false;;) {
     const int E = p.form == kSingle ? 1 : 16 / bytes;
     const int units = (n.dim + (p.log_classes > 0 ? E - 1 : 0) + E - 1) / E, span = units * E;
-    p.kind = worker_kind(span, bwd);
+    p.kind = long_team ? kLongTeam : worker_kind(span, bwd);
     p.log_lanes = 2;
     while (p.log_lanes < 5 && (8 << p.log_lanes) < span) ++p.log_lanes;
     const bool cta = p.kind >= kTeam24;
@@ -799,6 +802,11 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
     p.smem_bytes = p.ring_bytes * workers;
     // rows of x and of dy that are too long, and a row that begins behind the first of 16384 places, do not fit
     if (p.form != kSingle && (p.smem_bytes > kNormSmem - 4096 || p.threads > kind.threads[bwd])) {
+      if (p.kind == kWideTeam) {  // kLongTeam has room for 12288 in fp32 (362 us; value by value 436)
+        long_team = true;
+        continue;
+      }
+      long_team = false;
       p.form = kSingle;
       p.log_classes = 0;
       continue;
@@ -857,6 +865,7 @@ static cudaError_t launch_norm_f(const NormParams& p, const NormPlan& plan, bool
     case kWarp32: return launch_norm_t<T, kForm, kWarp32>(p, plan, bwd, st);
     case kWarp24: return launch_norm_t<T, kForm, kWarp24>(p, plan, bwd, st);
     case kWarp16: return launch_norm_t<T, kForm, kWarp16>(p, plan, bwd, st);
+    case kWideTeam: return launch_kernel_of(norm_bwd_kernel<T, kForm, kWideTeam>, p, plan, st);
     default: return launch_norm_t<T, kForm, kLongTeam>(p, plan, bwd, st);
   }
 }

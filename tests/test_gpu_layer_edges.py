@@ -216,3 +216,19 @@ def test_activations_keep_their_relative_error(m, kind):
     binding.sparsp_gated_ffn_fwd(ffn, x, wg, wu, h, None, None, binding.make_ffn_workspace(ffn, False))
     want = ffn_tests.activation(kind, x[:, :1].double())[0] * wu[None, :, 1].double()
     close(h, want, want.abs() * (UNIT[HF] + 2.0 ** -16) + TINY[HF], kind)
+
+
+@pytest.mark.parametrize("dtype", [BF, FL])
+@pytest.mark.parametrize("dim", [761, 768, 776, 1017, 1024, 1032, 1273, 1280, 1288, 1536, 1544, 2048, 2056, 2304, 2312, 2560, 2568,
+                                 3079, 4096, 4104, 5120, 5128, 6144, 6152, 7680, 7688, 8192, 8200, 9216, 9224, 10240, 10248,
+                                 12281, 12288, 12296, 16384])
+def test_widths_where_another_worker_takes_over(dim, dtype):
+    """Rows that just fit a worker, and that just do not; with classes, without, and value by value (a shifted tensor)."""
+    for rows, groups, off in ((7, 2, 0), (211, 3, 0), (9, 1, 1)):
+        per = -(-rows // groups)
+        x, w, b, dy = inputs(rows, dim, groups, dtype, FL, seed=dim)
+        base = torch.empty(rows * dim + off, dtype=dtype, device="cuda")
+        base[off:] = x.flatten()
+        norm = binding.make_norm(rows, dim, per, EPS, dtype, FL)
+        check_norm(base[off:].view(rows, dim), w, b, dy, per, groups, norm, torch.full_like(x, float("nan")),
+                   torch.full_like(x, float("nan")))
