@@ -17,8 +17,8 @@ namespace sparsp {
 // only, every P-th of its part, so that a thread's columns, and with them its weights and sums, do not change from row
 // to row.  (Value by value, backward over 15554 x 1921 fp32 took 153 us, with single 4-byte copies 111.)
 //
-// Bound by HBM: 75600 x 5120 bf16 forward 245 to 256 us = 6.1 to 6.3 TB/s.  Backward, twice as much is read as written,
-// by few warps, for the sums of the weights' gradients stay in registers: 383 to 409 us = 5.7 to 6.1 TB/s.
+// Bound by HBM: 75600 x 5120 bf16 forward 245 to 264 us = 5.9 to 6.3 TB/s.  Backward, twice as much is read as written,
+// by few warps, for the sums of the weights' gradients stay in registers: 383 to 423 us = 5.5 to 6.1 TB/s.
 
 // Who works on a row, by its length: a warp up to 1280 values, otherwise a team, a CTA of as few warps as hold the row
 // with 24, 32 or 40 values a thread.  Few warps with many registers are better than more with fewer: what a row costs
@@ -51,7 +51,7 @@ constexpr WorkerKind kWorkers[] = {
     {32, {512, 512}, {128, 128}, {1, 1}, {3, 2}},  // kLongTeam
 };
 
-// Threads of a CTA whose warps are workers (260000 x 384 fp32 backward: 211 us, 239 in CTAs of 128)
+// Threads of a CTA whose warps are workers, where there are enough for every SM (260000 x 384 fp32 backward: 211 us, 239 in CTAs of 128)
 __host__ __device__ constexpr int warp_threads(int kind) { return kind <= kWarp16 ? 256 : 128; }
 
 // How a worker meets its rows.
@@ -399,7 +399,7 @@ __global__ void __launch_bounds__(kWorkers[kKind].threads[0], 1) norm_fwd_kernel
   __shared__ float slots[4][32][R];
   const Place me(kCta, kKind == kWarp8, p.log_lanes);
   const int t = me.t, batch = R * me.at_once;
-  const int worker = kCta ? blockIdx.x : blockIdx.x * (warp_threads(kKind) / 32) + (threadIdx.x >> 5);
+  const int worker = kCta ? blockIdx.x : blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   if (worker >= (kForm == kShifted ? p.parts << p.log_classes : p.parts)) return;
   const Mine<kForm == kShifted> m(p, worker);
   Batches<Mine<kForm == kShifted>> ahead(m);
@@ -513,7 +513,7 @@ __global__ void __launch_bounds__(kWorkers[kKind].threads[1], 1) norm_bwd_kernel
   __shared__ float slots[2][32][2 * R];
   const Place me(kCta, kKind == kWarp8, p.log_lanes);
   const int t = me.t, batch = R * me.at_once;
-  const int worker = kCta ? blockIdx.x : blockIdx.x * (warp_threads(kKind) / 32) + (threadIdx.x >> 5);
+  const int worker = kCta ? blockIdx.x : blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
   if (worker >= (kForm == kShifted ? p.parts << p.log_classes : p.parts)) return;
   const Mine<kForm == kShifted> m(p, worker);
   Batches<Mine<kForm == kShifted>> ahead(m);
@@ -795,7 +795,8 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
     const WorkerKind& kind = kWorkers[p.kind];
     const int per_thread = kind.values / E;
     p.threads = cta ? ((units + per_thread - 1) / per_thread + 31) / 32 * 32 : warp_threads(p.kind);
-    const int workers = cta ? 1 : p.threads / 32, lanes = cta ? p.threads : 32;  // workers of a CTA
+    int workers = cta ? 1 : p.threads / 32;  // of a CTA
+    const int lanes = cta ? p.threads : 32;
     const int values = lanes * kind.values;
     p.ring_half = p.form == kSingle ? 0 : kind.ahead[bwd] * kind.rows[bwd] * values * bytes;
     p.ring_bytes = bwd ? 2 * p.ring_half + (weights_shared(p.form, p.kind) ? values * 4 : 0) : p.ring_half;
@@ -822,6 +823,10 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
     if (bwd) most = std::min(most, std::max<int64_t>(kSms, rows / 4));
     p.parts = (int)std::max<int64_t>(1, most >> p.log_classes);
     const int all = p.parts << p.log_classes;
+    // few warps go to as many SMs as there are (300 x 512 bf16 backward 6.8 us, 8.6 by eights; 64 x 256 5.2 and 5.8)
+    while (workers > 1 && (all + workers - 1) / workers < kSms) workers /= 2;
+    if (!cta) p.threads = 32 * workers;
+    p.smem_bytes = p.ring_bytes * workers;
     p.grid = (unsigned)((all + workers - 1) / workers);
     return p;
   }
