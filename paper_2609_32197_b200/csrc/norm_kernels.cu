@@ -84,6 +84,9 @@ struct NormParams {
   int32_t parts, log_classes;  // workers: parts << log_classes
   int32_t ring_bytes, ring_half;  // of a worker; where dy's begins
   int32_t log_lanes;              // kWarp8: lanes of a row
+  int32_t row_ctas;               // backward: the CTAs behind these add columns
+  void* dweight;
+  void* dbias;
   float eps, inv_dim;
 };
 
@@ -498,6 +501,52 @@ __global__ void __launch_bounds__(kWorkers[kKind].threads[0], 1) norm_fwd_kernel
   }
 }
 
+__device__ __forceinline__ void store_weight(void* to, int64_t at, float v, bool fp32, bool fp16) {
+  if (fp32)
+    reinterpret_cast<float*>(to)[at] = v;
+  else if (fp16)
+    reinterpret_cast<__half*>(to)[at] = __float2half_rn(v);
+  else
+    reinterpret_cast<__nv_bfloat16*>(to)[at] = __float2bfloat16_rn(v);
+}
+
+// Few rows: the gradients of 16 columns' weights of a group straight from x and dy, by CTAs of the launch that makes dx.
+// Half a warp reads a row's columns; the sums of a thread's rows, then of the halves, then of the warps, in that order.
+template <typename T>
+__device__ __forceinline__ void add_columns(const NormParams& p, int cta, float* sums) {
+  const int tiles = (p.dim + 15) / 16, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t g = cta / tiles, lo = g * p.rows_per_group, hi = min(lo + p.rows_per_group, p.rows);
+  const int col = cta % tiles * 16 + (lane & 15);
+  float sw = 0.0f, sb = 0.0f;
+  if (col < p.dim) {
+    const T* x = reinterpret_cast<const T*>(p.x) + col;
+    const T* dy = reinterpret_cast<const T*>(p.dy) + col;
+#pragma unroll 8
+    for (int64_t row = lo + (threadIdx.x >> 4); row < hi; row += blockDim.x >> 4) {
+      const float d = (float)dy[row * p.stride_y];
+      sw = fmaf(d, ((float)x[row * p.stride_x] - p.mean_in[row]) * p.rstd_in[row], sw);
+      sb += d;
+    }
+  }
+  sw += __shfl_xor_sync(0xffffffffu, sw, 16);
+  sb += __shfl_xor_sync(0xffffffffu, sb, 16);
+  sums[threadIdx.x] = lane < 16 ? sw : sb;
+  __syncthreads();
+  void* to = lane < 16 ? p.dweight : p.dbias;
+  if (warp > 0 || col >= p.dim || to == nullptr) return;
+  float v = 0.0f;
+  for (int i = lane; i < (int)blockDim.x; i += 32) v += sums[i];
+  store_weight(to, g * p.dim + col, v, sizeof(T) == 4 || p.weights_fp32, std::is_same<T, __half>::value);
+}
+
+// ... in a launch of their own before dx is made, where dx takes the place of x or dy.
+template <typename T>
+__global__ void __launch_bounds__(512) norm_columns_kernel(const NormParams p) {
+  enter_grid();
+  __shared__ float sums[512];
+  add_columns<T>(p, blockIdx.x, sums);
+}
+
 // The gradients of the weights are sums over rows: each worker keeps those of its rows in registers and writes them out
 // where a group of its part ends.  Of P classes, class c of part i writes group g to slot (i + g) P + c, which no other
 // (worker, group) has, as rows and with them groups ascend from part to part.  norm_weights_kernel adds a group's
@@ -510,6 +559,7 @@ __global__ void __launch_bounds__(kWorkers[kKind].threads[1], 1) norm_bwd_kernel
   constexpr int R = kWorkers[kKind].rows[1], kAhead = kWorkers[kKind].ahead[1];
   constexpr bool kCta = kKind >= kTeam24, kRing = E > 1;
   extern __shared__ __align__(16) char ring[];
+  if (blockIdx.x >= p.row_ctas) return add_columns<T>(p, blockIdx.x - p.row_ctas, reinterpret_cast<float*>(ring));
   __shared__ float slots[2][32][2 * R];
   const Place me(kCta, kKind == kWarp8, p.log_lanes);
   const int t = me.t, batch = R * me.at_once;
@@ -723,12 +773,7 @@ __global__ void __launch_bounds__(1024) norm_weights_kernel(const float* partial
     void* to = which == 0 ? dweight : dbias;
     if (lane == 0 && mine < dim && to != nullptr) {
       const int64_t at = g * dim + mine;
-      if (dtype == SPARSP_FP32)
-        reinterpret_cast<float*>(to)[at] = v;
-      else if (dtype == SPARSP_FP16)
-        reinterpret_cast<__half*>(to)[at] = __float2half_rn(v);
-      else
-        reinterpret_cast<__nv_bfloat16*>(to)[at] = __float2bfloat16_rn(v);
+      store_weight(to, at, v, dtype == SPARSP_FP32, dtype == SPARSP_FP16);
     }
   }
 }
@@ -744,7 +789,8 @@ struct NormPlan {
   int form, kind, threads;                // threads of a CTA
   int ring_bytes, ring_half, smem_bytes;  // of a worker, where dy's begins, of a CTA
   int parts, log_classes, log_lanes;
-  unsigned grid;
+  int resident;  // CTAs on a multiprocessor
+  unsigned grid, column_ctas;  // rows', and behind them columns'
 };
 
 // By the values that a worker has to hold.  Teams: the least that holds them of those whose number of warps shares out
@@ -815,9 +861,9 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
     // each quarter of a multiprocessor has registers for so many warps of its own (100000 x 1536 bf16, CTAs of three
     // warps, of which six fit, not seven: forward 110 us, 130 with seven; backward 185 and 210)
     const int warps = 4 * (16384 / (32 * kind.registers[bwd]));
-    const int resident = std::min({32, warps * 32 / p.threads, kNormSmem / (p.smem_bytes + 2048)});
+    p.resident = std::min({32, warps * 32 / p.threads, kNormSmem / (p.smem_bytes + 2048)});
     const int64_t rows = p.kind == kWarp8 ? (n.rows + (32 >> p.log_lanes) - 1) >> (5 - p.log_lanes) : n.rows;
-    int64_t most = std::min<int64_t>(rows, (int64_t)kSms * resident * workers);
+    int64_t most = std::min<int64_t>(rows, (int64_t)kSms * p.resident * workers);
     // backward, a worker's sums are written and read again: four rows of its own at least, if every SM has a worker
     // (3023 x 752 fp32: 14.0 us, 17.3 with eight, 15.6 with one)
     if (bwd) most = std::min(most, std::max<int64_t>(kSms, rows / 4));
@@ -851,7 +897,7 @@ static bool in_pieces(const sparsp_norm& n, const void* a, const void* b, const 
 static cudaError_t launch_kernel_of(void (*kern)(NormParams), const NormParams& p, const NormPlan& plan,
                                     cudaStream_t st) {
   const cudaError_t e = ensure_dynamic_smem((const void*)kern, plan.smem_bytes);
-  return e != cudaSuccess ? e : launch_kernel(kern, dim3(plan.grid), plan.threads, plan.smem_bytes, st, p);
+  return e != cudaSuccess ? e : launch_kernel(kern, dim3(plan.grid + plan.column_ctas), plan.threads, plan.smem_bytes, st, p);
 }
 
 template <typename T, int kForm, int kKind>
@@ -920,9 +966,19 @@ int launch_norm_fwd(const sparsp_norm& n, const void* X, const void* w, const vo
 
 int launch_norm_bwd(const sparsp_norm& n, const void* dY, const void* X, const void* w, const float* mean,
                     const float* rstd, void* dX, void* dw, void* db, char* ws, cudaStream_t st) {
-  const NormPlan plan = plan_norm(n, in_pieces(n, X, dY, dX), true);
+  NormPlan plan = plan_norm(n, in_pieces(n, X, dY, dX), true);
   NormParams p = norm_params(n, plan);
   p.want_weights = dw != nullptr || db != nullptr;
+  // Few rows are added in the same launch (backward bf16 1 x 32: 2.1 us, 4.8 with sums of workers in a second launch; 64 x
+  // 5120 3.6 and 10.8): up to 32 of a group a thread of add_columns, and up to ten rounds of CTAs; half of both where a
+  // multiprocessor has one CTA at a time (500 x 8192 23 and 15 with 32; 2 groups of 250 x 8192, ten rounds, 29 and 20).
+  const int64_t columns = norm_groups(n) * ((n.dim + 15) / 16);
+  const int several = std::min(plan.resident, 2);
+  const bool direct = p.want_weights && n.rows > 0 && std::min(p.rows_per_group, n.rows) <= several * plan.threads &&
+                      plan.grid + columns <= 5 * several * kSms * plan.resident;
+  const unsigned column_ctas = (unsigned)columns;
+  if (direct) p.want_weights = 0;
+  p.row_ctas = (int32_t)plan.grid;
   if (n.rows > 0) {
     p.x = X;
     p.dy = dY;
@@ -931,6 +987,15 @@ int launch_norm_bwd(const sparsp_norm& n, const void* dY, const void* X, const v
     p.rstd_in = rstd;
     p.y = dX;
     p.partial = reinterpret_cast<float*>(ws + kStatusWords * 4);
+    p.dweight = dw;
+    p.dbias = db;
+    if (direct && dX != X && dX != dY) {
+      plan.column_ctas = column_ctas;
+    } else if (direct) {
+      SPARSP_WITH_TYPE(n.dtype, T, {
+        SPARSP_CUDA_OK(launch_kernel(norm_columns_kernel<T>, dim3(column_ctas), plan.threads, 0, st, p));
+      });
+    }
     SPARSP_CUDA_OK(launch_norm(n.dtype, p, plan, true, st));
   }
   if (p.want_weights && norm_groups(n) > 0) {

@@ -232,3 +232,13 @@ def test_widths_where_another_worker_takes_over(dim, dtype):
         norm = binding.make_norm(rows, dim, per, EPS, dtype, FL)
         check_norm(base[off:].view(rows, dim), w, b, dy, per, groups, norm, torch.full_like(x, float("nan")),
                    torch.full_like(x, float("nan")))
+
+
+@pytest.mark.parametrize("dim", [40, 130, 640, 1152, 2048, 5120, 8192])
+def test_few_rows_of_many_groups(dim):
+    """Either side of where the weights' gradients are added in the launch that makes dx."""
+    for per, groups in ((1, 1), (1, 7), (16, 8), (31, 1), (33, 1), (64, 5), (65, 2), (129, 1), (250, 2), (257, 1)):
+        rows = per * groups
+        x, w, b, dy = inputs(rows, dim, groups, BF, BF, seed=per)
+        norm = binding.make_norm(rows, dim, per, EPS, BF, BF)
+        check_norm(x, w, b, dy, per, groups, norm, torch.full_like(x, float("nan")), torch.full_like(x, float("nan")))
