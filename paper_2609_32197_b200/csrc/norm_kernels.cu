@@ -51,7 +51,8 @@ constexpr WorkerKind kWorkers[] = {
     {32, {512, 512}, {128, 128}, {1, 1}, {3, 2}},  // kLongTeam
 };
 
-// Threads of a CTA whose warps are workers, where there are enough for every SM (260000 x 384 fp32 backward: 211 us, 239 in CTAs of 128)
+// Threads of a CTA whose warps are workers, where there are enough for every SM (260000 x 384 fp32 backward: 211 us,
+// 239 in CTAs of 128)
 __host__ __device__ constexpr int warp_threads(int kind) { return kind <= kWarp16 ? 256 : 128; }
 
 // How a worker meets its rows.
@@ -59,8 +60,8 @@ __host__ __device__ constexpr int warp_threads(int kind) { return kind <= kWarp1
 //   kShifted  rows in classes, pieces that a row shares with its neighbours
 //   kSingle   value by value: tensors that do not begin on 16 bytes or whose rows move against one another, and rows
 //             that shared memory does not hold
-// Plain rows have a form of their own because nothing of theirs has to be masked (75600 x 5120 bf16 forward 246 us, 261 in
-// the other form, backward 387 and 406; 104000 x 1920 backward 210 and 240).
+// Plain rows have a form of their own because nothing of theirs has to be masked (75600 x 5120 bf16 forward 246 us, 261
+// in the other form, backward 387 and 406; 104000 x 1920 backward 210 and 240).
 enum Form { kPlain, kShifted, kSingle };
 
 // Backward, a thread's weights are in shared memory where there are no registers for them.
@@ -510,8 +511,9 @@ __device__ __forceinline__ void store_weight(void* to, int64_t at, float v, bool
     reinterpret_cast<__nv_bfloat16*>(to)[at] = __float2bfloat16_rn(v);
 }
 
-// Few rows: the gradients of 16 columns' weights of a group straight from x and dy, by CTAs of the launch that makes dx.
-// Half a warp reads a row's columns; the sums of a thread's rows, then of the halves, then of the warps, in that order.
+// Few rows: the gradients of 16 columns' weights of a group straight from x and dy, by CTAs of the launch that makes
+// dx. Half a warp reads a row's columns; the sums of a thread's rows, then of the halves, then of the warps, in that
+// order.
 template <typename T>
 __device__ __forceinline__ void add_columns(const NormParams& p, int cta, float* sums) {
   const int tiles = (p.dim + 15) / 16, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -969,9 +971,10 @@ int launch_norm_bwd(const sparsp_norm& n, const void* dY, const void* X, const v
   NormPlan plan = plan_norm(n, in_pieces(n, X, dY, dX), true);
   NormParams p = norm_params(n, plan);
   p.want_weights = dw != nullptr || db != nullptr;
-  // Few rows are added in the same launch (backward bf16 1 x 32: 2.1 us, 4.8 with sums of workers in a second launch; 64 x
-  // 5120 3.6 and 10.8): up to 32 of a group a thread of add_columns, and up to ten rounds of CTAs; half of both where a
-  // multiprocessor has one CTA at a time (500 x 8192 23 and 15 with 32; 2 groups of 250 x 8192, ten rounds, 29 and 20).
+  // Few rows are added in the same launch (backward bf16 1 x 32: 2.1 us, 4.8 with sums of workers in a second launch;
+  // 64 x 5120 3.6 and 10.8): up to 32 of a group a thread of add_columns, and up to ten rounds of CTAs; half of both
+  // where a multiprocessor has one CTA at a time (500 x 8192 23 and 15 with 32; 2 groups of 250 x 8192, ten rounds, 29
+  // and 20).
   const int64_t columns = norm_groups(n) * ((n.dim + 15) / 16);
   const int several = std::min(plan.resident, 2);
   const bool direct = p.want_weights && n.rows > 0 && std::min(p.rows_per_group, n.rows) <= several * plan.threads &&
