@@ -504,7 +504,8 @@ typedef struct sparsp_ffn {
 } sparsp_ffn;
 
 /* Bytes of workspace that the forward call (backward = 0) or the backward call needs: dG and dU for the latter, and 39 MB
- * for partial sums in either case, but for a forward call of up to 128 tokens. */
+ * for partial sums in either case, but for a forward call of up to 128 tokens.  More tokens, all else equal, never need
+ * less, so a workspace for the largest call serves smaller ones; backward it serves forward calls of that size too. */
 SPARSP_API int sparsp_gated_ffn_workspace_bytes(const sparsp_ffn* ffn, int32_t backward, int64_t* bytes);
 
 /* Both projections, the activation and the product.  Sums in fp32; H is rounded once, from the fp32 projections.

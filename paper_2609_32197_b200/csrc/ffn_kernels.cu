@@ -1014,11 +1014,14 @@ static int64_t hidden_pitch(const sparsp_ffn& f) { return align_up(f.hidden, 64)
 // pairs have a whole one each are left out of it.
 static bool two_parts(const sparsp_ffn& f) { return f.tokens <= kFewTokens && ceil_div(f.dim, BN) <= kPairs - 2; }
 static int64_t hidden_rows(const sparsp_ffn& f) { return two_parts(f) ? kFewTokens + f.tokens : f.tokens; }
-static int64_t hidden_bytes(const sparsp_ffn& f) { return align_up(hidden_rows(f) * hidden_pitch(f) * 2, 256); }
+static int64_t hidden_bytes(const sparsp_ffn& f, int64_t rows) { return align_up(rows * hidden_pitch(f) * 2, 256); }
 
+// Never less for more tokens, so that a workspace for the most tokens serves every call with fewer: always room for two
+// parts of kFewTokens rows.
 int64_t ffn_workspace_bytes(const sparsp_ffn& f, bool backward) {
   if (!backward && f.tokens <= kFewTokens) return kStatusWords * 4;
-  return kStatusWords * 4 + kPartialBytes + (backward ? 2 * hidden_bytes(f) : 0);
+  const int64_t rows = std::max<int64_t>(f.tokens, 2 * kFewTokens);
+  return kStatusWords * 4 + kPartialBytes + (backward ? 2 * hidden_bytes(f, rows) : 0);
 }
 
 static int launch_few(const sparsp_ffn& f, const void* X, const void* Wg, const void* Wu, void* H, void* gate,
@@ -1116,7 +1119,7 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
   }
   if (dX == nullptr && dWg == nullptr) return SPARSP_OK;
   char* dg = ws + kStatusWords * 4 + kPartialBytes;
-  char* du = dg + hidden_bytes(f);
+  char* du = dg + hidden_bytes(f, hidden_rows(f));
   const bool gaps = f.stride_h != f.hidden || hidden_pitch(f) != f.hidden;
   const int64_t row_length = gaps ? f.hidden : f.tokens * f.hidden, rows = gaps ? f.tokens : 1;
   const int64_t ctas_per_row = (row_length + 2047) / 2048;

@@ -242,3 +242,21 @@ def test_few_rows_of_many_groups(dim):
         x, w, b, dy = inputs(rows, dim, groups, BF, BF, seed=per)
         norm = binding.make_norm(rows, dim, per, EPS, BF, BF)
         check_norm(x, w, b, dy, per, groups, norm, torch.full_like(x, float("nan")), torch.full_like(x, float("nan")))
+
+
+@pytest.mark.parametrize("most,m", [(200, 100), (129, 128), (255, 73), (300, 1)])
+def test_a_workspace_for_more_tokens_serves_fewer(most, m):
+    """The last, shorter batch in the workspace of the others: right, and nothing behind the workspace changes."""
+    d, f = 264, 1000
+    size = binding.sparsp_gated_ffn_workspace_bytes(binding.make_ffn(most, d, f), True)
+    hold = torch.full((size + (4 << 20),), 77, dtype=torch.uint8, device="cuda")
+    ws = hold[:size]
+    ws[:256].zero_()
+    x, wg, wu, dh = ffn_tests.inputs(m, d, f, BF, seed=13)
+    gate, up = x @ wg.T, x @ wu.T
+    ffn = binding.make_ffn(m, d, f)
+    dx, dwg, dwu = (torch.full_like(t, float("nan")) for t in (x, wg, wu))
+    binding.sparsp_gated_ffn_bwd(ffn, dh, x, wg, wu, gate, up, dx, dwg, dwu, ws)
+    assert binding.sparsp_status(ws) == binding.SPARSP_OK
+    ffn_tests.check_backward("silu", BF, dh, x, wg, wu, gate, up, dx, dwg, dwu)
+    assert bool((hold[size:] == 77).all())

@@ -174,3 +174,20 @@ def test_ffn_refused():
     for i in (0, 1, 2, 3, 4, 5, 8, 9):
         refused(INVALID, binding.sparsp_gated_ffn_bwd, ffn, *[None if i == j else a for j, a in enumerate(good)])
     assert binding.sparsp_gated_ffn_workspace_bytes(ffn, True) > binding.sparsp_gated_ffn_workspace_bytes(ffn, False)
+
+
+@pytest.mark.parametrize("dim", [8, 5120, 18432, 18440])
+@pytest.mark.parametrize("hidden", [8, 1000, 13824])
+def test_a_workspace_for_more_tokens_serves_fewer(dim, hidden):
+    need = [[binding.sparsp_gated_ffn_workspace_bytes(binding.make_ffn(m, dim, hidden), back) for back in (False, True)]
+            for m in range(1, 600)]
+    assert all(a[0] <= b[0] and a[1] <= b[1] for a, b in zip(need, need[1:]))
+    assert all(forward <= backward for forward, backward in need)
+
+
+@pytest.mark.parametrize("dim,pad,per", [(64, 0, 0), (1000, 1, 3), (1921, 0, 100), (5120, 4, 1), (12288, 0, 0)])
+def test_a_norm_workspace_for_more_rows_serves_fewer(dim, pad, per):
+    rows = sorted({*range(1, 70), *(int(1.1 ** k) for k in range(44, 140))})
+    need = [binding.sparsp_layer_norm_workspace_bytes(binding.make_norm(r, dim, per, stride_x=dim + pad, stride_y=dim + pad))
+            for r in rows]
+    assert all(a <= b for a, b in zip(need, need[1:]))
