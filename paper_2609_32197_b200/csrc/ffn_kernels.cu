@@ -368,7 +368,7 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
       int m, n;
       tile_at(p, walk.tile, m, n);
       mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 4, p.wait_limit);
-      if (*s_abort) break;
+      if (__any_sync(0xffffffffu, *s_abort != 0)) break;  // (the same for all lanes)
       tc_fence_after();
       const uint32_t from = tmem + acc * BN + ((uint32_t)(quarter * 32) << 16);
       // after a warp's last load: the next product may have these columns while it is still busy with the values
@@ -607,9 +607,10 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     const int ld = p.ld_turn;  // of `turn`, a row for each lane: odd, so that its columns do not meet in a bank
     int acc = 0;
     uint32_t acc_round = 0;
+    // No way out before the last tile: the four warps meet at barrier 1 twice a tile, so all of them have to come, also
+    // after a wait that ran out, when one may see the flag before another does.  Waits return at once then.
     for (int tile = first_tile; tile < p.tiles; tile += step) {
       mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 14, p.wait_limit);
-      if (*s_abort) break;
       tc_fence_after();
       if (quarter * 32 < 2 * F) {
         for (int c = 0; c < N; c += 16) {

@@ -1,0 +1,78 @@
+"""What the kernels' waits rest on and no run on a GPU can show, for there a wait would have to run out: read from the
+sources.  A wait in a kernel has a limit, after which a flag is raised; from then on every warp has to come out."""
+import os
+import re
+
+import pytest
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2609_32197_b200", "csrc")
+FILES = sorted(f for f in os.listdir(CSRC) if f.endswith(".cu"))
+
+
+def code(name):
+    """The file without its comments."""
+    with open(os.path.join(CSRC, name)) as f:
+        text = f.read()
+    return re.sub(r"//[^\n]*|/\*.*?\*/", "", text, flags=re.S)
+
+
+def closing(text, at):
+    """Index behind the brace that closes the one at `at`."""
+    depth = 0
+    for i in range(at, len(text)):
+        depth += (text[i] == "{") - (text[i] == "}")
+        if depth == 0:
+            return i + 1
+    raise ValueError("unbalanced braces")
+
+
+def loops(text):
+    """(header, body) of every loop with braces."""
+    for m in re.finditer(r"\b(for|while)\s*\(", text):
+        at, depth = m.end(), 1
+        while depth:
+            depth += (text[at] == "(") - (text[at] == ")")
+            at += 1
+        rest = text[at:]
+        if rest.lstrip().startswith("{"):
+            begin = at + rest.index("{")
+            yield text[m.start():at], text[begin:closing(text, begin)]
+
+
+def without_inner_loops(body):
+    out, at = body[:1], 1
+    for header, inner in loops(body[1:]):
+        begin = body.find(header + body[body.find(header, at) + len(header):body.find(inner, at)] + inner, at)
+        if begin < at:
+            continue  # inside a loop that is out already
+        out += body[at:begin]
+        at = body.find(inner, begin) + len(inner)
+    return out + body[at:]
+
+
+def test_the_reading_itself():
+    text = "for (int i = 0; i < f(n); ++i) { a; while (x) { break; } if (y) { b; } }"
+    (head, body), (_, inner) = loops(text)
+    assert head == "for (int i = 0; i < f(n); ++i)" and inner == "{ break; }"
+    assert without_inner_loops(body).split() == "{ a; if (y) { b; } }".split()
+
+
+@pytest.mark.parametrize("name", FILES)
+def test_warps_that_meet_at_a_barrier_all_come(name):
+    """A loop in which some of a CTA's warps meet at a named barrier is left at its end alone: a warp that leaves as soon
+    as it sees the flag would make those wait for good that looked a moment earlier."""
+    for header, body in loops(code(name)):
+        own = without_inner_loops(body)
+        if re.search(r"bar(rier)?\.sync\s+[1-9%]", own):
+            assert not re.search(r"\b(break|return|goto|continue)\b", own), f"{name}: {header}"
+
+
+def test_results_of_the_products_leave_together():
+    """The flag is read once for a warp: its lanes go on to instructions that take all of them."""
+    text = code("ffn_kernels.cu")
+    at = text.index("while (walk.next()) {")
+    results = text[at:closing(text, text.index("{", at))]
+    assert "tmem_ld32" in results
+    for line in results.splitlines():
+        if "*s_abort" in line and "mbar_wait" not in line:
+            assert "__any_sync(0xffffffffu, *s_abort" in line, line
