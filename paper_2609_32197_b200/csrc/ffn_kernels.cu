@@ -56,7 +56,7 @@ struct GemmCfg {
   static constexpr int kStages = 196608 / kStage > 8 ? 8 : 196608 / kStage;
   static constexpr int kOffOut = kStages * kStage;  // each epilogue warp's 32 rows x 32 columns on their way out
   static constexpr int kOffBars = kOffOut + kEpilogueWarps * 2048;
-  static constexpr int kBars = 2 * kStages + 4;
+  static constexpr int kBars = 2 * kStages + 5;
   static constexpr int kBytes = kOffBars + kBars * 8 + 16;
   static constexpr int kDynamic = kBytes + 1024;  // the tiles are aligned to 1024 bytes
 };
@@ -134,6 +134,13 @@ __device__ __forceinline__ void gate_product(int kind, const float (&g)[N], cons
 #pragma unroll
     for (int i = 0; i < N; ++i) h[i] = activate<decltype(k)::value>(g[i]) * u[i];
   });
+}
+
+// One thread, before shared and tensor memory are given back: waits, within a limit, for the products issued here.
+__device__ __forceinline__ void wait_drained(uint64_t* drained, long long limit) {
+  const long long t0 = clock64();
+  while (!ptx::mbar_try_wait(drained, 0) && clock64() - t0 < limit) {
+  }
 }
 
 // A warp's 32 rows x 32 columns to global memory: staged in its own 2 KB (64-byte swizzle: a row's 16-byte pieces in
@@ -224,7 +231,8 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
   uint64_t* empty = full + C::kStages;                               // the stage has been multiplied
   uint64_t* acc_full = empty + C::kStages;                           // [2]
   uint64_t* acc_empty = acc_full + 2;                                // [2] of the even CTA: both have read theirs
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(acc_empty + 2);
+  uint64_t* drained = acc_empty + 2;                                 // every product has ended
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
   volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -239,6 +247,7 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
       mbar_init(acc_full + a, 1);
       mbar_init(acc_empty + a, p.alternate ? kEpilogueWarps : 2 * kEpilogueWarps);
     }
+    mbar_init(drained, 1);
     *s_abort = 0;
     mbar_init_fence();
   }
@@ -333,6 +342,7 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
         tc_fence_after();
         for (int k = walk.k0; k < walk.k1; ++k) {
           mbar_wait_bounded_inline(full + s, round, s_abort, 3, p.wait_limit);
+          if (*s_abort) break;
           tc_fence_after();
           const uint64_t off = (uint64_t)((s * C::kStage) >> 4);
 #pragma unroll
@@ -349,6 +359,7 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
         acc ^= 1;
         if (acc == 0) acc_round ^= 1u;
       }
+      mma_commit_pair(drained);
     }
   } else {
     // ---- results: warp w has the lanes of quarter w % 4, and a share of the columns ----
@@ -430,6 +441,9 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
   __syncwarp();
   tc_fence_before();
   __syncthreads();
+  // Products use both CTAs' memory until they have ended: after a wait that ran out nobody else has waited for them.
+  if (warp == kEpilogueWarps + 1 && elect_one()) wait_drained(drained, p.wait_limit);
+  __syncwarp();
   cluster_sync();  // the other CTA's arrivals and products here have ended
   if (warp == kEpilogueWarps + 1) {
     tc_fence_after();
@@ -498,7 +512,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   using namespace ptx;
   extern __shared__ uint8_t dynamic[];
   uint8_t* smem = dynamic + ((1024 - (smem_u32(dynamic) & 1023)) & 1023);
-  __shared__ uint64_t full[16], empty[16], acc_full[2], acc_empty[2];
+  __shared__ uint64_t full[16], empty[16], acc_full[2], acc_empty[2], drained;
   __shared__ uint32_t tmem_slot;
   __shared__ int abort_word;
   volatile int* s_abort = &abort_word;
@@ -515,6 +529,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       mbar_init(acc_full + a, 1);
       mbar_init(acc_empty + a, 4);
     }
+    mbar_init(&drained, 1);
     *s_abort = 0;
     mbar_init_fence();
   }
@@ -581,6 +596,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         tc_fence_after();
         for (int k = k0; k < k1; k += kDeep) {
           mbar_wait_bounded_inline(full + s, round, s_abort, 13, p.wait_limit);
+          if (*s_abort) break;
           tc_fence_after();
           const uint64_t off = (uint64_t)((s * p.stage_bytes) >> 4);
 #pragma unroll
@@ -601,6 +617,8 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         acc ^= 1;
         if (acc == 0) acc_round ^= 1u;
       }
+      mma_commit(&drained);
+      wait_drained(&drained, p.wait_limit);  // (as above)
     }
   } else {
     const int quarter = warp & 3, in_tile = quarter * 32 + lane;

@@ -76,3 +76,18 @@ def test_results_of_the_products_leave_together():
     for line in results.splitlines():
         if "*s_abort" in line and "mbar_wait" not in line:
             assert "__any_sync(0xffffffffu, *s_abort" in line, line
+
+
+def test_no_product_outlives_its_memory():
+    """After a wait that ran out nothing more is multiplied, and what was issued is waited for before tensor memory is
+    given back and the CTA, with its shared memory, ends."""
+    text = code("ffn_kernels.cu")
+    waits = [m.end() for m in re.finditer(r"mbar_wait_bounded_inline\(full \+ s[^;]*;", text)]
+    assert len(waits) == 2
+    for at in waits:
+        before = text[at:at + re.search(r"\bmma_ss", text[at:]).start()]
+        assert "if (*s_abort) break;" in before
+    for kernel, dealloc in (("void gemm_tiles", "tmem_dealloc_pair"), ("few_kernel(", "tmem_dealloc(")):
+        at = text.index(kernel)
+        body = text[at:text.index(dealloc, at)]
+        assert 0 < body.rindex("mma_commit") < body.index("wait_drained(")
