@@ -51,7 +51,8 @@ cudaError_t sm_count(int* sms);
 // serialisation): its CTAs take their places and set themselves up as soon as the previous kernel's have all started,
 // and wait in enter_grid() before they touch memory, so that the latency of a launch is hidden behind the kernel before
 // it. Every kernel launched here calls enter_grid() first thing, in every thread, or
-// wait_previous_grids() where the next launch is to begin only as its CTAs end.
+// wait_previous_grids() where the next launch is to begin only as its CTAs end. A kernel with tensor memory takes it
+// before: CTAs of the next launch that had it first would wait for this one's end, and this one for them.
 template <typename T>
 struct same_type {
   using type = T;

@@ -237,7 +237,6 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t rank = cluster_rank();
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::kStages; ++s) {
       mbar_init(full + s, 1);
@@ -260,7 +259,7 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
   cluster_sync();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  wait_previous_grids();
+  enter_grid();  // (the next launch may begin: tensor memory is ours, so its CTAs cannot have taken it before)
 
   Walk walk(p, p.k_blocks * (kMode == kInput ? 2 : 1), pair, pairs, kMode == kInput && p.two_parts);
   constexpr bool kAMn = kMode == kWeights, kBMn = kMode != kForward;
@@ -519,7 +518,6 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   // behind the stages: room for the last stage's rows past 2 F, then the results on their turn
   float* turn = reinterpret_cast<float*>(smem + p.stages * p.stage_bytes + 16384);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   if (threadIdx.x == 0) {
     for (int s = 0; s < p.stages; ++s) {
       mbar_init(full + s, 1);
@@ -541,7 +539,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
-  wait_previous_grids();
+  enter_grid();  // (after tensor memory is ours, as above)
   const int F = p.features, N = p.columns;
   const int rank = (int)cluster_rank(), first_tile = blockIdx.x / p.splits, step = gridDim.x / p.splits;
   const int k0 = p.k_blocks * rank / p.splits, k1 = p.k_blocks * (rank + 1) / p.splits;

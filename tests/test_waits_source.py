@@ -91,3 +91,15 @@ def test_no_product_outlives_its_memory():
         at = text.index(kernel)
         body = text[at:text.index(dealloc, at)]
         assert 0 < body.rindex("mma_commit") < body.index("wait_drained(")
+
+
+@pytest.mark.parametrize("name", FILES)
+def test_tensor_memory_is_taken_before_the_next_launch_may_begin(name):
+    """Else a CTA of the next launch could have the columns that this one waits for, and wait for this one's end."""
+    text = code(name)
+    for m in re.finditer(r"\btmem_alloc(_pair)?\(", text):
+        kernel = max(text.rfind("__global__", 0, m.start()), text.rfind("__device__", 0, m.start()))
+        begin = text.index("{", kernel)
+        body, at = text[begin:closing(text, begin)], m.start() - begin
+        first = re.search(r"launch_dependents|enter_grid\(", body)
+        assert first is not None and at < first.start(), f"{name}: {text[kernel:begin]}"
