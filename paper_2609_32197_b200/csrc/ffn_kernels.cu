@@ -340,8 +340,7 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
         mbar_wait_bounded_inline(acc_empty + acc, acc_round ^ 1u, s_abort, 2, p.wait_limit);
         tc_fence_after();
         for (int k = walk.k0; k < walk.k1; ++k) {
-          mbar_wait_bounded_inline(full + s, round, s_abort, 3, p.wait_limit);
-          if (*s_abort) break;
+          if (!mbar_wait_bounded_inline(full + s, round, s_abort, 3, p.wait_limit)) break;
           tc_fence_after();
           const uint64_t off = (uint64_t)((s * C::kStage) >> 4);
 #pragma unroll
@@ -593,8 +592,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
         mbar_wait_bounded_inline(acc_empty + acc, acc_round ^ 1u, s_abort, 12, p.wait_limit);
         tc_fence_after();
         for (int k = k0; k < k1; k += kDeep) {
-          mbar_wait_bounded_inline(full + s, round, s_abort, 13, p.wait_limit);
-          if (*s_abort) break;
+          if (!mbar_wait_bounded_inline(full + s, round, s_abort, 13, p.wait_limit)) break;
           tc_fence_after();
           const uint64_t off = (uint64_t)((s * p.stage_bytes) >> 4);
 #pragma unroll

@@ -98,18 +98,20 @@ __device__ __forceinline__ void mbar_wait_bounded(uint64_t* bar, uint32_t parity
 }
 // Same, fully inline and as small as possible: for waits inside hot loops whose threads hold most of their
 // registers live (a call there would have to save them).  On give-up only the CTA-wide flag is set, to
-// `where` + 1; the kernel reports it to the status words once, at its end (report_abort below).
-__device__ __forceinline__ void mbar_wait_bounded_inline(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
+// `where` + 1; the kernel reports it to the status words once, at its end (report_abort below).  Returns whether the
+// phase has completed.
+__device__ __forceinline__ bool mbar_wait_bounded_inline(uint64_t* bar, uint32_t parity, volatile int* abort_flag,
                                                          int where, long long limit_cycles) {
-  if (mbar_try_wait(bar, parity)) return;
+  if (mbar_try_wait(bar, parity)) return true;
   const long long t0 = clock64();
   while (!mbar_try_wait(bar, parity)) {
-    if (*abort_flag) return;
+    if (*abort_flag) return false;
     if (clock64() - t0 > limit_cycles) {
       *abort_flag = where + 1;
-      return;
+      return false;
     }
   }
+  return true;
 }
 // One thread, after the CTA's last barrier: turns a raised abort flag into the global status words
 // (unless an earlier report is already there).

@@ -82,11 +82,9 @@ def test_no_product_outlives_its_memory():
     """After a wait that ran out nothing more is multiplied, and what was issued is waited for before tensor memory is
     given back and the CTA, with its shared memory, ends."""
     text = code("ffn_kernels.cu")
-    waits = [m.end() for m in re.finditer(r"mbar_wait_bounded_inline\(full \+ s[^;]*;", text)]
-    assert len(waits) == 2
-    for at in waits:
-        before = text[at:at + re.search(r"\bmma_ss", text[at:]).start()]
-        assert "if (*s_abort) break;" in before
+    waits = re.findall(r"([^;{}]*)mbar_wait_bounded_inline\(full \+ s[^;]*;", text)
+    assert len(waits) == 2 and all(w.strip() == "if (!" for w in waits)
+    assert len(re.findall(r"mbar_wait_bounded_inline\(full \+ s[^;{}]*\)\) break;", text)) == 2
     for kernel, dealloc in (("void gemm_tiles", "tmem_dealloc_pair"), ("few_kernel(", "tmem_dealloc(")):
         at = text.index(kernel)
         body = text[at:text.index(dealloc, at)]
