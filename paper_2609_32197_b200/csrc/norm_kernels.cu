@@ -783,7 +783,7 @@ __global__ void __launch_bounds__(1024) norm_weights_kernel(const float* partial
 // ---- host side ------------------------------------------------------------------------------------------------------
 
 int64_t norm_groups(const sparsp_norm& n) {
-  return n.rows_per_group == 0 ? 1 : (n.rows + n.rows_per_group - 1) / n.rows_per_group;
+  return n.rows_per_group == 0 ? 1 : n.rows / n.rows_per_group + (n.rows % n.rows_per_group != 0);
 }
 
 // How the rows are shared out.
@@ -936,7 +936,8 @@ static cudaError_t launch_norm(int dtype, const NormParams& p, const NormPlan& p
 static NormParams norm_params(const sparsp_norm& n, const NormPlan& plan) {
   NormParams p = {};
   p.rows = n.rows;
-  p.rows_per_group = n.rows_per_group == 0 ? std::max<int64_t>(n.rows, 1) : n.rows_per_group;
+  // (no more than there are, so that a sum of a row and a group stays far from 2^63)
+  p.rows_per_group = std::max<int64_t>(n.rows_per_group == 0 ? n.rows : std::min(n.rows_per_group, n.rows), 1);
   p.stride_x = n.stride_x;
   p.stride_y = n.stride_y;
   p.dim = n.dim;

@@ -260,3 +260,12 @@ def test_a_workspace_for_more_tokens_serves_fewer(most, m):
     assert binding.sparsp_status(ws) == binding.SPARSP_OK
     ffn_tests.check_backward("silu", BF, dh, x, wg, wu, gate, up, dx, dwg, dwu)
     assert bool((hold[size:] == 77).all())
+
+
+@pytest.mark.parametrize("rows", [1, 20, 5000])  # the weights' gradients in the launch that makes dx, and in one of their own
+@pytest.mark.parametrize("per", [2 ** 62, 2 ** 63 - 1])
+def test_one_group_said_as_a_huge_one(rows, per):
+    dim = 264
+    x, w, b, dy = inputs(rows, dim, 1, BF, BF, seed=21)
+    check_norm(x, w, b, dy, rows, 1, binding.make_norm(rows, dim, per, EPS, BF, BF), torch.full_like(x, float("nan")),
+               torch.full_like(x, float("nan")))

@@ -191,3 +191,9 @@ def test_a_norm_workspace_for_more_rows_serves_fewer(dim, pad, per):
     need = [binding.sparsp_layer_norm_workspace_bytes(binding.make_norm(r, dim, per, stride_x=dim + pad, stride_y=dim + pad))
             for r in rows]
     assert all(a <= b for a, b in zip(need, need[1:]))
+
+
+@pytest.mark.parametrize("rows", [1, 5000])
+def test_a_group_of_more_rows_than_there_can_be(rows):
+    need = [binding.sparsp_layer_norm_workspace_bytes(binding.make_norm(rows, 64, per)) for per in (0, rows, 2 ** 62, 2 ** 63 - 1)]
+    assert len(set(need)) == 1
