@@ -418,7 +418,7 @@ typedef struct sparsp_rotary {
  *   linear  f_i / factor
  *   ntk     theta * factor^(n/(n-1)) in the place of theta, n = n_pairs > 1 (one pair is not scaled)
  *   yarn    per pair between f_i and f_i / factor: share s_i = 1 - clamp((i - low) / (high - low), 0, 1) of the first,
- *           where low = max(floor(at(beta_fast)), 0), high = min(ceil(at(beta_slow)), n - 1), high - low at least 0.001,
+ *           where low = max(floor(at(beta_fast)), 0), high = min(ceil(at(beta_slow)), 2n - 1), high - low at least 0.001,
  *           at(b) = n ln(original_length / (2 pi b)) / ln theta is the pair that turns b times over the original length
  * inv_freq   out  HOST double [n_pairs]; may be NULL with n_pairs = 0
  * amplitude  out  HOST double: yarn 0.1 ln(factor) + 1, otherwise 1; may be NULL

@@ -114,7 +114,9 @@ int sparsp_rotary_frequencies(int32_t n_pairs, double theta, int32_t scaling, do
     const double tau = 6.283185307179586476925286766559;
     auto at = [&](double beta) { return n * std::log(original_length / (tau * beta)) / std::log(theta); };
     low = std::max(std::floor(at(beta_fast)), 0.0);
-    high = std::min(std::ceil(at(beta_slow)), n - 1.0);
+    // the limit is the head's last rotated channel, not its last pair, as published: it matters where even the slowest
+    // pair turns more than beta_slow times, and pairs past the last are then part of the ramp
+    high = std::min(std::ceil(at(beta_slow)), 2.0 * n - 1.0);
   }
   for (int i = 0; i < n; ++i) {
     double f = std::pow(base, -(double)i / n);

@@ -59,6 +59,26 @@ def test_frequencies(n):
                 assert math.isclose(yarn[i], plain[i] / 4, rel_tol=1e-14)
 
 
+@pytest.mark.parametrize("n", [1, 3, 32, 64])
+@pytest.mark.parametrize("original,theta,factor", [(4096.0, 10000.0, 4.0), (32768.0, 10000.0, 8.0), (65536.0, 10000.0, 4.0),
+                                                   (262144.0, 10000.0, 2.0), (65536.0, 500000.0, 16.0)])
+def test_yarn_of_every_pair(n, original, theta, factor):
+    """As published, in rotated channels: a frequency is interpolated by how far its pair is between the channels that
+    turn 32 times and once over the original length, those limited to 0 .. channels - 1."""
+    channels = 2 * n
+    turning = lambda times: channels * math.log(original / (times * 2 * math.pi)) / (2 * math.log(theta))  # noqa: E731
+    low, high = max(math.floor(turning(32)), 0), min(math.ceil(turning(1)), channels - 1)
+    if low == high:
+        high += 0.001
+    got, amplitude = binding.sparsp_rotary_frequencies(n, theta, "yarn", factor, original, 32.0, 1.0)
+    for i in range(n):
+        extrapolated = 1.0 / theta ** (2 * i / channels)
+        ramp = min(max((i - low) / (high - low), 0.0), 1.0)
+        want = extrapolated / factor * ramp + extrapolated * (1.0 - ramp)
+        assert math.isclose(got[i], want, rel_tol=1e-13), (i, low, high)
+    assert math.isclose(amplitude, 0.1 * math.log(factor) + 1.0, rel_tol=1e-15)
+
+
 def test_frequencies_refused():
     f = binding.sparsp_rotary_frequencies
     refused(INVALID, f, -1)
