@@ -462,12 +462,29 @@ def make_status_workspace(device="cuda") -> torch.Tensor:
     return torch.zeros(256, dtype=torch.uint8, device=device)
 
 
+def _positions_stride(shape: sparsp_shape, positions) -> int:
+    """Elements from one batch item's positions to the next's, 0 where all have the same."""
+    if not isinstance(positions, torch.Tensor):
+        return 0
+    N, dims = shape.grid_t * shape.grid_h * shape.grid_w + shape.n_text, positions.shape
+    if positions.dtype is not torch.int32:
+        raise ValueError(f"positions have to be int32, not {positions.dtype}")
+    if dims != (N, 3) and dims != (shape.batch, N, 3) and dims != (1, N, 3):
+        raise ValueError(f"positions {tuple(dims)} for {shape.batch} x {N} tokens")
+    one = len(dims) == 2 or dims[0] == 1
+    if positions.is_contiguous():  # (asked first: the rest costs a call of one token half a microsecond)
+        return 0 if one else 3 * N
+    if positions.stride(-1) != 1 or (N > 1 and positions.stride(-2) != 3):
+        raise ValueError("a token's positions and the tokens have to follow one another in memory")
+    return 0 if one else positions.stride(0)
+
+
 def sparsp_rotary_apply(shape, rotary, table, positions, origin, Q, K, Q_out, K_out, inverse, workspace):
-    """positions: int32 [N][3] (for every batch item) or [B][N][3], or None; origin: first (t, h, w) without them."""
-    stride = 0 if positions is None or positions.dim() < 3 else positions.stride(0)
-    _check(lib().sparsp_rotary_apply(shape, rotary, _data(table), _data(positions), stride, *origin, _data(Q), _data(K),
-                                     _data(Q_out), _data(K_out), 1 if inverse else 0, _data(workspace),
-                                     _stream_handle()))
+    """positions: int32 [N][3] or [1][N][3] (for every batch item) or [B][N][3], or None; origin: first (t, h, w) without
+    them."""
+    _check(lib().sparsp_rotary_apply(shape, rotary, _data(table), _data(positions), _positions_stride(shape, positions),
+                                     *origin, _data(Q), _data(K), _data(Q_out), _data(K_out), 1 if inverse else 0,
+                                     _data(workspace), _stream_handle()))
 
 
 def make_norm(rows: int, dim: int, rows_per_group: int = 0, eps: float = 1e-5, dtype=torch.bfloat16, weight_dtype=None,

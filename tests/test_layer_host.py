@@ -2,6 +2,7 @@
 import math
 
 import pytest
+import torch
 
 from paper_2609_32197_b200 import binding
 from paper_2609_32197_b200.binding import SparspError
@@ -217,3 +218,28 @@ def test_a_norm_workspace_for_more_rows_serves_fewer(dim, pad, per):
 def test_a_group_of_more_rows_than_there_can_be(rows):
     need = [binding.sparsp_layer_norm_workspace_bytes(binding.make_norm(rows, 64, per)) for per in (0, rows, 2 ** 62, 2 ** 63 - 1)]
     assert len(set(need)) == 1
+
+
+def test_positions_as_tensors(monkeypatch):
+    """They are passed by address: what would be misread there is refused here, and the stride is that of batch items."""
+    seen = []
+
+    class Library:
+        def sparsp_rotary_apply(self, *args):
+            seen.append(args[4])
+            return binding.SPARSP_OK
+
+    monkeypatch.setattr(binding, "lib", Library)
+    shape, rotary, p = binding.make_shape(4, 64, (3, 4, 5), 2, 64, batch=2), binding.make_rotary((8, 8, 8), (3, 4, 5)), At()
+    call = lambda pos: binding.sparsp_rotary_apply(shape, rotary, p, pos, (0, 0, 0), p, p, p, p, False, p)  # noqa: E731
+    good = torch.zeros(2, 62, 3, dtype=torch.int32)
+    padded = torch.zeros(2, 64, 3, dtype=torch.int32)[:, :62]
+    for pos, stride in ((good, 62 * 3), (good[0], 0), (good[:1], 0), (good[:1].expand(2, -1, -1), 0), (padded, 64 * 3), (None, 0)):
+        call(pos)
+        assert seen.pop() == stride
+    for bad in (good.long(), good.float(), good[:, :61], good[..., :2], good[0, 0], good[None], torch.cat((good, good)),
+                torch.zeros(2, 3, 62, dtype=torch.int32).transpose(1, 2), torch.zeros(2, 62, 4, dtype=torch.int32)[..., :3],
+                torch.zeros(62, 2, 3, dtype=torch.int32).transpose(0, 1)):
+        with pytest.raises(ValueError):
+            call(bad)
+    assert not seen
