@@ -305,7 +305,7 @@ __device__ __forceinline__ void gemm_tiles(const CUtensorMap& a0, const CUtensor
           if constexpr (!kBMn) {
             tma_load_pair(B, rank == 0 ? &b0 : &b1, bar, kk, n * (BN / 2));
           } else {
-            const CUtensorMap* tb = second ? &b1 : &b0;
+            const CUtensorMap* tb = second || left ? &b1 : &b0;
 #pragma unroll
             for (int c = 0; c < BN / 128; ++c)
               tma_load_pair(B + c * 8192, tb, bar, n * BN + (int)rank * (BN / 2) + c * 64, kk);
@@ -744,12 +744,12 @@ __device__ __forceinline__ void join_tile(const GemmParams p, int cta) {
       v[4 * h + 1] += x.y;
       v[4 * h + 2] += x.z;
       v[4 * h + 3] += x.w;
-      if (halves) {
+      if (halves) {  // what the roundings left, of either sign, times an infinite weight is not to be added
         const float4 y = from[(c / 4 + h) * 256 + kFewTokens];
-        v[4 * h] += y.x;
-        v[4 * h + 1] += y.y;
-        v[4 * h + 2] += y.z;
-        v[4 * h + 3] += y.w;
+        v[4 * h] += isfinite(y.x) ? y.x : 0.0f;
+        v[4 * h + 1] += isfinite(y.y) ? y.y : 0.0f;
+        v[4 * h + 2] += isfinite(y.z) ? y.z : 0.0f;
+        v[4 * h + 3] += isfinite(y.w) ? y.w : 0.0f;
       }
       if (kMode == kForward) {
         const float4 y = from[((c + BN / 2) / 4 + h) * 256];
@@ -826,13 +826,27 @@ __global__ void __launch_bounds__(256) gate_grad_kernel(const T* dh, const T* ga
   store_vec<T, 8>(du + to, ou);
 }
 
-// ... in two parts: rows 0 .. tokens - 1 rounded, then zeros up to row 128, then what the roundings leave.
+// ... in two parts: rows 0 .. tokens - 1 rounded, then zeros up to row 128, then what the roundings leave.  The last is
+// multiplied by a copy of X without infinities and NaN, made here by the CTAs behind row 128: the rounded part times X
+// has them already, and what is left, of either sign or zero, would make NaN of infinities.
 template <typename T>
 __global__ void __launch_bounds__(256) gate_grad_parts_kernel(const T* dh, const T* gate, const T* up, T* dg, T* du,
                                                               int64_t ld, int64_t ld_out, int hidden, int tokens,
-                                                              int activation) {
-  enter_grid(dh, gate, up);
+                                                              int activation, const T* x, int64_t ld_x, T* finite_x,
+                                                              int dim) {
+  enter_grid(dh, gate, up, x);
   const int row = blockIdx.y, col = (blockIdx.x * 256 + threadIdx.x) * 8;
+  if (row >= kFewTokens) {
+    if (col >= dim) return;
+    const int64_t token = row - kFewTokens;
+    Vec<T, 8> v = load_vec<T, 8>(x + token * ld_x + col);
+    float keep[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) keep[e] = isfinite(v[e]) ? v[e] : 0.0f;
+    v.set(keep);
+    store_vec(finite_x + token * dim + col, v);
+    return;
+  }
   if (col >= hidden) return;
   const int64_t to = row * ld_out + col, rest = to + kFewTokens * ld_out;
   Vec<T, 8> og, ou;
@@ -1036,7 +1050,8 @@ static int64_t hidden_bytes(const sparsp_ffn& f, int64_t rows) { return align_up
 int64_t ffn_workspace_bytes(const sparsp_ffn& f, bool backward) {
   if (!backward && f.tokens <= kFewTokens) return kStatusWords * 4;
   const int64_t rows = std::max<int64_t>(f.tokens, 2 * kFewTokens);
-  return kStatusWords * 4 + kPartialBytes + (backward ? 2 * hidden_bytes(f, rows) : 0);
+  const int64_t finite_x = (int64_t)kFewTokens * std::min(f.dim, kPairs * BN) * 2;
+  return kStatusWords * 4 + kPartialBytes + (backward ? 2 * hidden_bytes(f, rows) + finite_x : 0);
 }
 
 static int launch_few(const sparsp_ffn& f, const void* X, const void* Wg, const void* Wu, void* H, void* gate,
@@ -1135,6 +1150,7 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
   if (dX == nullptr && dWg == nullptr) return SPARSP_OK;
   char* dg = ws + kStatusWords * 4 + kPartialBytes;
   char* du = dg + hidden_bytes(f, hidden_rows(f));
+  char* finite_x = du + hidden_bytes(f, hidden_rows(f));
   const bool gaps = f.stride_h != f.hidden || hidden_pitch(f) != f.hidden;
   const int64_t row_length = gaps ? f.hidden : f.tokens * f.hidden, rows = gaps ? f.tokens : 1;
   const int64_t ctas_per_row = (row_length + 2047) / 2048;
@@ -1150,9 +1166,11 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
   };
   auto grad_parts = [&](auto* element) {
     using T = std::remove_pointer_t<decltype(element)>;
-    return launch_kernel(gate_grad_parts_kernel<T>, dim3((unsigned)ceil_div(f.hidden, 2048), kFewTokens), 256, 0, st,
+    const int widest = dWg != nullptr ? std::max(f.hidden, f.dim) : f.hidden;
+    const int rows = kFewTokens + (dWg != nullptr ? (int)f.tokens : 0);
+    return launch_kernel(gate_grad_parts_kernel<T>, dim3((unsigned)ceil_div(widest, 2048), (unsigned)rows), 256, 0, st,
                          (const T*)dH, (const T*)gate, (const T*)up, (T*)dg, (T*)du, f.stride_h, hidden_pitch(f),
-                         f.hidden, (int)f.tokens, f.activation);
+                         f.hidden, (int)f.tokens, f.activation, (const T*)X, f.stride_x, (T*)finite_x, f.dim);
   };
   if (two_parts(f))
     SPARSP_CUDA_OK(f.dtype == SPARSP_BF16 ? grad_parts((Bf*)nullptr) : grad_parts((Hf*)nullptr));
@@ -1191,6 +1209,7 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
     if ((rc = make_map(&mw.a1, f.dtype, du, hidden_rows(f), f.hidden, hidden_pitch(f), kStageK)) != SPARSP_OK) return rc;
     if ((rc = make_map(&mw.b0, f.dtype, X, f.tokens, f.dim, f.stride_x, kStageK)) != SPARSP_OK) return rc;
     mw.b1 = mw.b0;
+    if (two_parts(f) && (rc = make_map(&mw.b1, f.dtype, finite_x, f.tokens, f.dim, f.dim, kStageK)) != SPARSP_OK) return rc;
     if ((rc = make_out_map(&mw.o0, f.dtype, dWg, f.hidden, f.dim, f.stride_w)) != SPARSP_OK) return rc;
     if ((rc = make_out_map(&mw.o1, f.dtype, dWu, f.hidden, f.dim, f.stride_w)) != SPARSP_OK) return rc;
     mw.o2 = mw.o0;

@@ -269,3 +269,22 @@ def test_one_group_said_as_a_huge_one(rows, per):
     x, w, b, dy = inputs(rows, dim, 1, BF, BF, seed=21)
     check_norm(x, w, b, dy, rows, 1, binding.make_norm(rows, dim, per, EPS, BF, BF), torch.full_like(x, float("nan")),
                torch.full_like(x, float("nan")))
+
+
+@pytest.mark.parametrize("m", [3, 100, 128, 200])
+def test_infinite_operands_of_the_backward_pass(m):
+    """An infinity in X or in the weights makes infinities where dG or dU is not zero, for few tokens too: what the first
+    part's rounding left has either sign, or is zero, and must not make NaN of them."""
+    d, f = 136, 264
+    x, wg, wu, dh = ffn_tests.inputs(m, d, f, BF, seed=23)
+    gate, up = x @ wg.T, x @ wu.T
+    x[m // 2, 5], x[m - 1, 77] = float("inf"), -float("inf")
+    wg[3, 9], wg[f - 1, 100], wu[70, 20] = float("inf"), -float("inf"), float("inf")
+    ffn = binding.make_ffn(m, d, f)
+    ws = binding.make_ffn_workspace(ffn)
+    ws[256:].fill_(255)
+    dx, dwg, dwu = (torch.full_like(t, float("nan")) for t in (x, wg, wu))
+    binding.sparsp_gated_ffn_bwd(ffn, dh, x, wg, wu, gate, up, dx, dwg, dwu, ws)
+    assert binding.sparsp_status(ws) == binding.SPARSP_OK
+    assert bool(torch.isinf(dwg[:, 5]).all()) and bool(torch.isinf(dx[:, 20]).all())
+    ffn_tests.check_backward("silu", BF, dh, x, wg, wu, gate, up, dx, dwg, dwu)
