@@ -994,7 +994,10 @@ static int launch_gemm(const GemmParams& p, const GemmMaps& m, int dtype, cudaSt
 
 // dX and dW together.  Alone, each of two small products leaves pairs of SMs without a tile in its last round; together
 // they share the pairs out so that both end at the same time.  What is shared out by blocks of K stays so for either
-// product alone, so that it gives the same bits.  Returns the pairs of dX.
+// product alone, so that it gives the same bits.  Returns the pairs of dX, or 0 where the two are better apart, with 4000
+// clocks for the second launch: in two parts dX needs a pair for each of its tiles and more, which may leave dW too few
+// (64 x 18432 x 256, 72 of 74: together 305 us, apart 31; x 16384, 64: 46 and 29; x 14336, 56: 29 and 28; x 12288: 24
+// and 27).
 static int plan_both(GemmParams* pi, GemmParams* pw) {
   const int ti = pi->m_tiles * pi->n_tiles, tw = pw->m_tiles * pw->n_tiles;
   const int bi = 2 * pi->k_blocks, bw = pw->k_blocks;
@@ -1008,8 +1011,8 @@ static int plan_both(GemmParams* pi, GemmParams* pw) {
     else
       low = mid + 1;
   }
-  int64_t best = INT64_MAX;
-  int pairs = low;
+  int64_t best = gemm_clocks(ti, bi, kPairs, all, &si) + gemm_clocks(tw, bw, kPairs, false, &sw) + 4000;
+  int pairs = 0;
   for (int s = std::max(fewest, low - 1); s <= low; ++s) {
     const int64_t t = std::max(gemm_clocks(ti, bi, s, all, &si), gemm_clocks(tw, bw, kPairs - s, false, &sw));
     if (t >= best) continue;
@@ -1018,7 +1021,7 @@ static int plan_both(GemmParams* pi, GemmParams* pw) {
     share_out(pi, s, si);
     share_out(pw, kPairs - s, sw);
   }
-  pw->partial += (int64_t)2 * pi->shares * 256 * BN;
+  if (pairs > 0) pw->partial += (int64_t)2 * pi->shares * 256 * BN;
   return pairs;
 }
 
@@ -1191,7 +1194,7 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
   // rounds, 67 and 77); with more, both ways are alike within what runs differ by (2048 x 2048 x 4096, 6.9 rounds:
   // 114-122 and 115-118 us), and apart they read less at a time
   const bool small = (int64_t)pi.m_tiles * pi.n_tiles + (int64_t)pw.m_tiles * pw.n_tiles <= 4 * kPairs;
-  const int pairs = small ? plan_both(&pi, &pw) : 0;
+  const int pairs = small ? plan_both(&pi, &pw) : 0;  // 0: apart
   if (dX != nullptr) {
     if ((rc = make_map(&mi.a0, f.dtype, dg, hidden_rows(f), f.hidden, hidden_pitch(f), kTileRows)) != SPARSP_OK) return rc;
     if ((rc = make_map(&mi.a1, f.dtype, du, hidden_rows(f), f.hidden, hidden_pitch(f), kTileRows)) != SPARSP_OK) return rc;
@@ -1219,7 +1222,7 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
     pw.rows = f.hidden;
     pw.cols = f.dim;
   }
-  if (small && dX != nullptr && dWg != nullptr) return launch_both(pi, mi, pw, mw, pairs, f.dtype, st);
+  if (pairs > 0 && dX != nullptr && dWg != nullptr) return launch_both(pi, mi, pw, mw, pairs, f.dtype, st);
   if (dX != nullptr && (rc = launch_gemm<kInput>(pi, mi, f.dtype, st)) != SPARSP_OK) return rc;
   if (dWg != nullptr && (rc = launch_gemm<kWeights>(pw, mw, f.dtype, st)) != SPARSP_OK) return rc;
   return SPARSP_OK;

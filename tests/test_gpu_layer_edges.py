@@ -288,3 +288,24 @@ def test_infinite_operands_of_the_backward_pass(m):
     assert binding.sparsp_status(ws) == binding.SPARSP_OK
     assert bool(torch.isinf(dwg[:, 5]).all()) and bool(torch.isinf(dx[:, 20]).all())
     ffn_tests.check_backward("silu", BF, dh, x, wg, wu, gate, up, dx, dwg, dwu)
+
+
+@pytest.mark.parametrize("m,d,f,together", [(64, 18432, 256, False), (3, 16640, 72, False), (64, 8192, 256, True),
+                                            (128, 12288, 512, True), (129, 18432, 256, True)])
+def test_one_launch_for_both_gradients_where_it_is_shorter(m, d, f, together):
+    """Few tokens of a wide layer: in one launch dX would take nearly all multiprocessors from a dW of more tiles."""
+    x, wg, wu, dh = ffn_tests.inputs(m, d, f, BF, seed=29)
+    gate, up = x @ wg.T, x @ wu.T
+    ffn = binding.make_ffn(m, d, f)
+    ws = binding.make_ffn_workspace(ffn)
+    ws[256:].fill_(255)
+    dx, dwg, dwu = (torch.full_like(t, float("nan")) for t in (x, wg, wu))
+    before = binding.sparsp_launch_count()
+    binding.sparsp_gated_ffn_bwd(ffn, dh, x, wg, wu, gate, up, dx, dwg, dwu, ws)
+    assert (binding.sparsp_launch_count() - before <= 3) == together
+    assert binding.sparsp_status(ws) == binding.SPARSP_OK
+    ffn_tests.check_backward("silu", BF, dh, x, wg, wu, gate, up, dx, dwg, dwu)
+    dx2, dwg2, dwu2 = torch.empty_like(dx), torch.empty_like(dwg), torch.empty_like(dwu)
+    binding.sparsp_gated_ffn_bwd(ffn, dh, None, wg, wu, gate, up, dx2, None, None, ws)
+    binding.sparsp_gated_ffn_bwd(ffn, dh, x, None, None, gate, up, None, dwg2, dwu2, ws)
+    assert torch.equal(dx2, dx) and torch.equal(dwg2, dwg) and torch.equal(dwu2, dwu)
