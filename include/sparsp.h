@@ -508,7 +508,8 @@ typedef struct sparsp_ffn {
  * less, so a workspace for the largest call serves smaller ones; backward it serves forward calls of that size too. */
 SPARSP_API int sparsp_gated_ffn_workspace_bytes(const sparsp_ffn* ffn, int32_t backward, int64_t* bytes);
 
-/* Both projections, the activation and the product.  Sums in fp32; H is rounded once, from the fp32 projections.
+/* Both projections, the activation and the product.  Sums in fp32; H is rounded once, from the fp32 projections.  No output
+ * may be an input.
  *   X            in   [tokens][dim]
  *   Wgate, Wup   in   [hidden][dim]
  *   H            out  [tokens][hidden]
@@ -519,7 +520,7 @@ SPARSP_API int sparsp_gated_ffn_fwd(const sparsp_ffn* ffn, const void* X, const 
 
 /* With dG = dH * up * a'(gate) and dU = dH * a(gate), both rounded to dtype (the tensor cores' operands; for up to 128
  * tokens and dim up to 18432 as the sum of two such values):
- *   dX = dG Wgate + dU Wup,  dWgate = dG^T X,  dWup = dU^T X, sums in fp32
+ *   dX = dG Wgate + dU Wup,  dWgate = dG^T X,  dWup = dU^T X, sums in fp32;  no output may be an X, Wgate or Wup that is read
  *   dX             out  may be NULL (not wanted); Wgate and Wup may then be NULL too
  *   dWgate, dWup   out  both or neither NULL; X may be NULL without them.  Without tokens they are zero. */
 SPARSP_API int sparsp_gated_ffn_bwd(const sparsp_ffn* ffn, const void* dH, const void* X, const void* Wgate,

@@ -1,6 +1,7 @@
 // extern "C" entry points of the token-wise operators: argument checking, launch order.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "layer.cuh"
 
@@ -68,6 +69,16 @@ int check_norm(const sparsp_norm* n) {
 }
 
 // ---- gated feed-forward ----
+// Tiles of the outputs are written while others of the inputs are still to be read.
+int apart(std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs) {
+  for (auto o = outputs.begin(); o != outputs.end(); ++o) {
+    if (*o == nullptr) continue;
+    if (std::find(inputs.begin(), inputs.end(), *o) != inputs.end() || std::find(o + 1, outputs.end(), *o) != outputs.end())
+      SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "an output may not be an input or another output");
+  }
+  return SPARSP_OK;
+}
+
 int check_ffn(const sparsp_ffn* f) {
   if (!f) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "ffn is NULL");
   if (f->dtype != SPARSP_BF16 && f->dtype != SPARSP_FP16)
@@ -263,6 +274,7 @@ int sparsp_gated_ffn_fwd(const sparsp_ffn* ffn, const void* X, const void* Wgate
   SPARSP_TRY(need(H, "H", 16));
   SPARSP_TRY(optional(gate, "gate", 16));
   SPARSP_TRY(optional(up, "up", 16));
+  SPARSP_TRY(apart({H, gate, up}, {X, Wgate, Wup}));
   SPARSP_TRY(need(workspace, "workspace", 256));
   return launch_ffn_fwd(*ffn, X, Wgate, Wup, H, gate, up, (char*)workspace, (cudaStream_t)stream);
 }
@@ -285,6 +297,7 @@ int sparsp_gated_ffn_bwd(const sparsp_ffn* ffn, const void* dH, const void* X, c
       SPARSP_TRY(need(Wup, "Wup", 16));
     }
     if (dWgate) SPARSP_TRY(need(X, "X", 16));
+    SPARSP_TRY(apart({dX, dWgate, dWup}, {dWgate ? X : nullptr, dX ? Wgate : nullptr, dX ? Wup : nullptr}));
   }
   return launch_ffn_bwd(*ffn, dH, X, Wgate, Wup, gate, up, dX, dWgate, dWup, (char*)workspace, (cudaStream_t)stream);
 }

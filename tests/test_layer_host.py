@@ -243,3 +243,20 @@ def test_positions_as_tensors(monkeypatch):
         with pytest.raises(ValueError):
             call(bad)
     assert not seen
+
+
+def test_ffn_outputs_in_the_place_of_inputs():
+    ffn = binding.make_ffn(4, 64, 64)
+    x, wg, wu, h, gate, up, dh, dx, dwg, dwu, ws = (At(4096 * i) for i in range(1, 12))
+    ok = [x, wg, wu, h, gate, up, ws]
+    for out, into in ((3, 0), (3, 1), (4, 0), (5, 2), (4, 3), (5, 4)):
+        args = list(ok)
+        args[out] = ok[into]
+        with pytest.raises(SparspError, match="output"):
+            binding.sparsp_gated_ffn_fwd(ffn, *args)
+    ok = [dh, x, wg, wu, gate, up, dx, dwg, dwu, ws]
+    for out, into in ((6, 1), (7, 2), (8, 3), (6, 2), (8, 7)):
+        args = list(ok)
+        args[out] = ok[into]
+        with pytest.raises(SparspError, match="output"):
+            binding.sparsp_gated_ffn_bwd(ffn, *args)
