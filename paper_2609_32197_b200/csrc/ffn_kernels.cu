@@ -17,6 +17,7 @@
 // limit leaves (37800 x 5120 x 13824 bf16, both projections kept: 7.9 ms = 1350 TFLOP/s; backward 17.1 to 20.3 ms =
 // 1050 to 1250).
 #include <algorithm>
+#include <cmath>
 
 #include "layer.cuh"
 #include "sm100_ptx.cuh"
@@ -923,32 +924,48 @@ static int join_ctas(const GemmParams& p, int mode) {
   return (p.m_tiles * p.n_tiles - p.whole) * ((mode == kForward ? BN / 2 : BN) / 8);
 }
 
-// Clocks that a product takes on some pairs of SMs, and whether its last round is shared out by blocks of K for that
-// (by how many pairs; 0 = not): 512 a block of K, 2500 a unit for what no block hides, 12000 for writing sums out and
-// the launch that adds them.  share_all: every tile has to go that way (there are fewer than pairs).
-static int64_t gemm_clocks(int tiles, int blocks, int pairs, bool share_all, int* shares) {
-  *shares = 0;
+// What a product takes on some pairs of SMs, in clocks, and whether its last round is shared out by blocks of K for that.
+//
+// 512 a block of K and 2500 a unit for what no block hides.  Sharing costs 8000 for the launch that adds the sums, 1200
+// for each piece of a tile, which are added one after the other, and 90 for each piece there is, which is written and
+// read: fitted to 361 sizes of all three products, each timed whole and in 2, 3, 4, 6 and as many pieces as there are
+// pairs; by these figures 0.3 % is lost on average against the best of them, 5 % at most against whole tiles.  (us, whole
+// and in pieces; tiles of the last round x blocks: 6 x 128 42.3, two 29.1, four 22.5, twelve 29.0; 6 x 32 behind a round
+// of 74 tiles 29.2, two 34.9; 20 x 32 16.3, two 18.1; 20 x 128 45.2, three 33.7; 37 x 64 26.8, two 29.4; 37 x 256 99,
+// two 72.)
+//
+// Where there are not two pairs for a tile, all pairs can have equal runs, most of which touch two tiles.  They read
+// different rows and columns at one time, so it takes long tiles and few of them: 24000 beside the blocks, and at most
+// seven tiles for ten pairs (40 x 256 102, 85 shared; 48 x 256 118, 110; 48 x 128 54, 58; 50 x 160 64, 70; 56 x 256 127,
+// 131; 64 x 512 254, 348).
+struct Clocks {
+  int64_t product, join;
+  int shares;  // pairs that the last round is shared out to, 0: none
+  int64_t all() const { return product + join; }
+};
+// share_all: every tile has to be shared (there are fewer than pairs).
+static Clocks gemm_clocks(int tiles, int blocks, int pairs, bool share_all) {
   const int rounds = tiles / pairs, rest = tiles % pairs;
-  const int64_t unit = 512LL * blocks + 2500, all_whole = (rounds + (rest > 0)) * unit;
-  if (rest == 0) return all_whole;
-  int64_t best = share_all ? INT64_MAX : all_whole;
-  // equal runs for all pairs, of which most touch two tiles, or as many for each tile as there are pairs for it
+  const int64_t unit = 512LL * blocks + 2500;
+  Clocks best = {(rounds + (rest > 0)) * unit, 0, 0};
+  if (rest == 0) return best;
+  if (share_all) best.product = INT64_MAX;
+  auto shorter = [&](int64_t k, int64_t more, int64_t join, int shares) {
+    const Clocks c = {rounds * unit + 512 * k + 2500 + more, join, shares};
+    if (c.all() < best.all()) best = c;
+  };
+  const int fewest = share_all ? 1 : 2, most = std::max(fewest, std::min(pairs / rest, blocks / 4));
+  if (pairs / rest >= fewest) {
+    // the least of 512 blocks / pieces + (1200 + 90 rest) pieces, from either side
+    const int near = (int)std::sqrt(512.0 * blocks / (1200 + 90 * rest));
+    for (int pieces : {near, near + 1}) {
+      pieces = std::min(std::max(pieces, fewest), most);
+      shorter(ceil_div(blocks, pieces), 90LL * rest * pieces, 8000 + 1200LL * pieces, rest * pieces);
+    }
+  }
   const int all = (int)std::min<int64_t>(pairs, (int64_t)rest * blocks / 4);
-  const int each = std::max(1, std::min(pairs / rest, blocks / 4));
-  if (all > rest) {
-    const int64_t t = rounds * unit + 512LL * ceil_div((int64_t)rest * blocks, all) + 2 * 2500 + 12000;
-    if (t < best) {
-      best = t;
-      *shares = all;
-    }
-  }
-  if (each > 1 || share_all) {
-    const int64_t t = rounds * unit + 512LL * ceil_div(blocks, each) + 2500 + 12000;
-    if (t < best) {
-      best = t;
-      *shares = rest * each;
-    }
-  }
+  if (pairs / rest < 2 && all > rest && 10 * rest <= 7 * pairs)
+    shorter(ceil_div((int64_t)rest * blocks, all), 12000, 12000, all);
   return best;
 }
 static void share_out(GemmParams* p, int pairs, int shares) {
@@ -964,10 +981,9 @@ static int prepare_gemm(GemmParams* p, int mode, const sparsp_ffn& f, char* ws) 
     set_error("%d x %d tiles are too many", p->m_tiles, p->n_tiles);
     return SPARSP_ERR_UNSUPPORTED;
   }
-  int shares;
-  gemm_clocks(p->m_tiles * p->n_tiles, p->k_blocks * (mode == kInput ? 2 : 1), kPairs, mode == kInput && p->two_parts,
-              &shares);
-  share_out(p, kPairs, shares);
+  const Clocks c = gemm_clocks(p->m_tiles * p->n_tiles, p->k_blocks * (mode == kInput ? 2 : 1), kPairs,
+                               mode == kInput && p->two_parts);
+  share_out(p, kPairs, c.shares);
   p->band = 8;
   p->partial = reinterpret_cast<float*>(ws + kStatusWords * 4);
   p->status = reinterpret_cast<int32_t*>(ws);
@@ -994,32 +1010,33 @@ static int launch_gemm(const GemmParams& p, const GemmMaps& m, int dtype, cudaSt
 
 // dX and dW together.  Alone, each of two small products leaves pairs of SMs without a tile in its last round; together
 // they share the pairs out so that both end at the same time.  What is shared out by blocks of K stays so for either
-// product alone, so that it gives the same bits.  Returns the pairs of dX, or 0 where the two are better apart, with 4000
-// clocks for the second launch: in two parts dX needs a pair for each of its tiles and more, which may leave dW too few
-// (64 x 18432 x 256, 72 of 74: together 305 us, apart 31; x 16384, 64: 46 and 29; x 14336, 56: 29 and 28; x 12288: 24
-// and 27).
+// product alone, so that it gives the same bits.  Returns the pairs of dX, or 0 where the two are better apart, with 10000
+// clocks for another launch and its wait: in two parts dX needs a pair for each of its tiles and more, which may leave dW
+// too few (64 x 18432 x 256, 72 of 74: together 305 us, apart 31; x 16384, 64: 46 and 29; x 14336, 56: 29 and 28; x
+// 12288: 21 and 27).
 static int plan_both(GemmParams* pi, GemmParams* pw) {
   const int ti = pi->m_tiles * pi->n_tiles, tw = pw->m_tiles * pw->n_tiles;
   const int bi = 2 * pi->k_blocks, bw = pw->k_blocks;
   const bool all = pi->two_parts;
   const int fewest = all ? ti + 1 : 1;
-  int si, sw, low = fewest, high = kPairs - 1;  // the fewest pairs with which dX is no later than dW
+  int low = fewest, high = kPairs - 1;  // the fewest pairs with which dX is no later than dW
   while (low < high) {
     const int mid = (low + high) / 2;
-    if (gemm_clocks(ti, bi, mid, all, &si) <= gemm_clocks(tw, bw, kPairs - mid, false, &sw))
+    if (gemm_clocks(ti, bi, mid, all).product <= gemm_clocks(tw, bw, kPairs - mid, false).product)
       high = mid;
     else
       low = mid + 1;
   }
-  int64_t best = gemm_clocks(ti, bi, kPairs, all, &si) + gemm_clocks(tw, bw, kPairs, false, &sw) + 4000;
+  int64_t best = gemm_clocks(ti, bi, kPairs, all).all() + gemm_clocks(tw, bw, kPairs, false).all() + 10000;
   int pairs = 0;
   for (int s = std::max(fewest, low - 1); s <= low; ++s) {
-    const int64_t t = std::max(gemm_clocks(ti, bi, s, all, &si), gemm_clocks(tw, bw, kPairs - s, false, &sw));
+    const Clocks i = gemm_clocks(ti, bi, s, all), w = gemm_clocks(tw, bw, kPairs - s, false);
+    const int64_t t = std::max(i.product, w.product) + std::max(i.join, w.join);
     if (t >= best) continue;
     best = t;
     pairs = s;
-    share_out(pi, s, si);
-    share_out(pw, kPairs - s, sw);
+    share_out(pi, s, i.shares);
+    share_out(pw, kPairs - s, w.shares);
   }
   if (pairs > 0) pw->partial += (int64_t)2 * pi->shares * 256 * BN;
   return pairs;
@@ -1190,8 +1207,8 @@ int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const voi
   pi.two_parts = pw.two_parts = two_parts(f);
   if ((rc = prepare_gemm(&pi, kInput, f, ws)) != SPARSP_OK) return rc;
   if ((rc = prepare_gemm(&pw, kWeights, f, ws)) != SPARSP_OK) return rc;
-  // both at once up to four rounds of tiles (1003 x 1160 x 2504 36 us, one after the other 49; 2048 x 1024 x 4096, 3.5
-  // rounds, 67 and 77); with more, both ways are alike within what runs differ by (2048 x 2048 x 4096, 6.9 rounds:
+  // both at once up to four rounds of tiles (1003 x 1160 x 2504 36 us, one after the other 46; 2048 x 1024 x 4096, 3.5
+  // rounds, 65 and 81); with more, both ways are alike within what runs differ by (2048 x 2048 x 4096, 6.9 rounds:
   // 114-122 and 115-118 us), and apart they read less at a time
   const bool small = (int64_t)pi.m_tiles * pi.n_tiles + (int64_t)pw.m_tiles * pw.n_tiles <= 4 * kPairs;
   const int pairs = small ? plan_both(&pi, &pw) : 0;  // 0: apart

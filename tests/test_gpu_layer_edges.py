@@ -309,3 +309,19 @@ def test_one_launch_for_both_gradients_where_it_is_shorter(m, d, f, together):
     binding.sparsp_gated_ffn_bwd(ffn, dh, None, wg, wu, gate, up, dx2, None, None, ws)
     binding.sparsp_gated_ffn_bwd(ffn, dh, x, None, None, gate, up, None, dwg2, dwu2, ws)
     assert torch.equal(dx2, dx) and torch.equal(dwg2, dwg) and torch.equal(dwu2, dwu)
+
+
+@pytest.mark.parametrize("m,d,f,launches", [(512, 2048, 5120, 1), (250, 2048, 2560, 1), (512, 8192, 5120, 2), (250, 8192, 2560, 2),
+                                            (256, 4096, 8192, 1), (256, 8192, 768, 2)])
+def test_a_last_round_is_shared_out_where_that_is_shorter(m, d, f, launches):
+    """Sums written, read and added by a launch of their own cost about as much as 16 to 40 blocks of K."""
+    x, wg, wu, _ = ffn_tests.inputs(m, d, f, BF, seed=31)
+    ffn = binding.make_ffn(m, d, f)
+    ws = binding.make_ffn_workspace(ffn, backward=False)
+    ws[256:].fill_(255)
+    h, gate, up = (torch.full((m, f), float("nan"), dtype=BF, device="cuda") for _ in range(3))
+    before = binding.sparsp_launch_count()
+    binding.sparsp_gated_ffn_fwd(ffn, x, wg, wu, h, gate, up, ws)
+    assert binding.sparsp_launch_count() - before == launches
+    assert binding.sparsp_status(ws) == binding.SPARSP_OK
+    ffn_tests.check_forward("silu", BF, x, wg, wu, h, gate, up)
