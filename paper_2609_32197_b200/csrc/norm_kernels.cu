@@ -86,6 +86,8 @@ struct NormParams {
   int32_t ring_bytes, ring_half;  // of a worker; where dy's begins
   int32_t log_lanes;              // kWarp8: lanes of a row
   int32_t row_ctas;               // backward: the CTAs behind these add columns
+  int32_t whole_groups;           // ... groups that a worker has all of are finished by it
+  int32_t vector_weights;         // ... and their gradients stored four at a time
   void* dweight;
   void* dbias;
   float eps, inv_dim;
@@ -511,6 +513,19 @@ __device__ __forceinline__ void store_weight(void* to, int64_t at, float v, bool
     reinterpret_cast<__nv_bfloat16*>(to)[at] = __float2bfloat16_rn(v);
 }
 
+// ... of four columns next to each other
+template <typename T>
+__device__ __forceinline__ void store_four_weights(void* to, int64_t at, const float* v, bool fp32) {
+  if (to == nullptr) return;
+  if constexpr (sizeof(T) == 2) {
+    if (!fp32) {
+      *reinterpret_cast<uint2*>(reinterpret_cast<T*>(to) + at) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+      return;
+    }
+  }
+  *reinterpret_cast<float4*>(reinterpret_cast<float*>(to) + at) = make_float4(v[0], v[1], v[2], v[3]);
+}
+
 // Few rows: the gradients of 16 columns' weights of a group straight from x and dy, by CTAs of the launch that makes
 // dx. Half a warp reads a row's columns; the sums of a thread's rows, then of the halves, then of the warps, in that
 // order.
@@ -553,6 +568,12 @@ __global__ void __launch_bounds__(512) norm_columns_kernel(const NormParams p) {
 // where a group of its part ends.  Of P classes, class c of part i writes group g to slot (i + g) P + c, which no other
 // (worker, group) has, as rows and with them groups ascend from part to part.  norm_weights_kernel adds a group's
 // slots.
+//
+// Without classes and with as many groups as workers or more (whole_groups) most groups lie in one part, and its worker
+// writes their gradients themselves.  Of those that lie across boundaries, part i writes the one that comes into it from
+// before to slot 2 i and the one that goes on behind it to slot 2 i + 1, and norm_few_slots_kernel adds them.  A row of
+// weights per row leaves nothing to add.  (75600 x 1920 bf16, a group a row: 412 us and 18 MB; with a slot and a CTA of
+// norm_weights_kernel for each group 43 ms and 1.2 GB.)
 template <typename T, int kForm, int kKind>
 __global__ void __launch_bounds__(kWorkers[kKind].threads[1], 1) norm_bwd_kernel(const NormParams p) {
   const void* x = p.x;
@@ -681,7 +702,19 @@ __global__ void __launch_bounds__(kWorkers[kKind].threads[1], 1) norm_bwd_kernel
       }
     }
     if (p.want_weights) {
-      float* mine = p.partial + (((m.part + g) << m.log_classes()) + m.cls) * 2 * p.dim;
+      // to the gradients themselves, or as fp32 to a slot
+      const int64_t begin = g * m.per_group;
+      const bool alone = p.whole_groups && begin >= m.lo && min(begin + m.per_group, p.rows) <= m.hi;
+      const int64_t slot =
+          p.whole_groups ? 2 * m.part + (begin >= m.lo) : ((m.part + g) << m.log_classes()) + m.cls;
+      const bool fp32 = sizeof(T) == 4 || !alone || p.weights_fp32;
+      char* to_w = reinterpret_cast<char*>(p.partial + slot * 2 * p.dim);
+      char* to_b = to_w + p.dim * 4;
+      if (alone) {
+        const int64_t row = g * p.dim * (fp32 ? 4 : 2);
+        to_w = p.dweight == nullptr ? nullptr : reinterpret_cast<char*>(p.dweight) + row;
+        to_b = p.dbias == nullptr ? nullptr : reinterpret_cast<char*>(p.dbias) + row;
+      }
       constexpr int S = E > 1 ? 4 : 2;  // sums that are stored together
 #pragma unroll
       for (int j = 0; j < K; j += S) {
@@ -701,26 +734,37 @@ __global__ void __launch_bounds__(kWorkers[kKind].threads[1], 1) norm_bwd_kernel
           }
         }
         if (me.sub != 0) continue;
-        if (kForm == kPlain) {  // dim is a multiple of four, and so is the column
-          const int col = xs.column(j / E) + j % E;
+        const int col = xs.column(j / E) + j % E;
+        if (kForm == kPlain && (!alone || p.vector_weights)) {  // dim is a multiple of four, and so is the column
           if (col < p.dim) {
-            *reinterpret_cast<float4*>(mine + col) = make_float4(a[0], a[1], a[S - 2], a[S - 1]);
-            *reinterpret_cast<float4*>(mine + p.dim + col) = make_float4(c[0], c[1], c[S - 2], c[S - 1]);
+            store_four_weights<T>(to_w, col, a, fp32);
+            store_four_weights<T>(to_b, col, c, fp32);
           }
         } else {
 #pragma unroll
           for (int i = 0; i < S; ++i) {
-            const int col = xs.column((j + i) / E) + (j + i) % E;
-            if (col >= 0 && col < p.dim) {
-              mine[col] = a[i];
-              mine[p.dim + col] = c[i];
-            }
+            const int one = E > 1 ? col + i : xs.column(j + i);
+            if (one < 0 || one >= p.dim) continue;
+            if (to_w != nullptr) store_weight(to_w, one, a[i], fp32, std::is_same<T, __half>::value);
+            if (to_b != nullptr) store_weight(to_b, one, c[i], fp32, std::is_same<T, __half>::value);
           }
         }
       }
     }
   }
 }
+
+// Parts with rows of a group: from the one that has the group's first row to the one that has its last.
+struct GroupParts {
+  int64_t first, last;
+  __device__ __forceinline__ GroupParts(int64_t g, int64_t rows, int64_t rows_per_group, int64_t parts) {
+    const int64_t lo = g * rows_per_group, hi = min(lo + rows_per_group, rows) - 1;
+    const int64_t q = rows / parts, m = rows % parts;
+    const int64_t cut = m * (q + 1);  // rows of the parts that have one more
+    first = lo < cut ? lo / (q + 1) : m + (lo - cut) / q;
+    last = hi < cut ? hi / (q + 1) : m + (hi - cut) / q;
+  }
+};
 
 // Adds the slots of each group.  A CTA has kWeightColumns columns of one group; its threads take every 128th (32nd)
 // slot each and meet in shared memory, so the order is the same whatever runs when.  32 columns read whole lines; with
@@ -739,17 +783,12 @@ __global__ void __launch_bounds__(1024) norm_weights_kernel(const float* partial
   const int first = (blockIdx.x % tiles) * kWeightColumns, col = first + lane % kWeightColumns;
   float sw = 0.0f, sb = 0.0f;
   if (rows > 0) {
-    // parts with rows of this group: from the one that has the group's first row to the one that has its last
-    const int64_t lo = g * rows_per_group, hi = min(lo + rows_per_group, rows) - 1;
-    const int64_t q = rows / parts, m = rows % parts;
-    const int64_t cut = m * (q + 1);  // rows of the parts that have one more
-    const int64_t w0 = lo < cut ? lo / (q + 1) : m + (lo - cut) / q;
-    const int64_t w1 = hi < cut ? hi / (q + 1) : m + (hi - cut) / q;
+    const GroupParts of(g, rows, rows_per_group, parts);
     if (col < dim) {
       const int mine = threadIdx.x / kWeightColumns;
-      const float* slot = partial + (((w0 + g) << log_classes) + mine) * 2 * dim + col;
+      const float* slot = partial + (((of.first + g) << log_classes) + mine) * 2 * dim + col;
 #pragma unroll 4
-      for (int left = (int)((w1 - w0 + 1) << log_classes) - mine; left > 0;
+      for (int left = (int)((of.last - of.first + 1) << log_classes) - mine; left > 0;
            left -= kSlots, slot += (int64_t)2 * kSlots * dim) {
         sw += slot[0];
         sb += slot[dim];
@@ -780,6 +819,45 @@ __global__ void __launch_bounds__(1024) norm_weights_kernel(const float* partial
   }
 }
 
+// ... where a group has few: a CTA has 256 columns of it, a thread one.  whole: of the groups that lie across boundaries of
+// parts, a CTA for each boundary, which has work if that is its group's first.
+__global__ void __launch_bounds__(256) norm_few_slots_kernel(const float* partial, int64_t rows, int64_t rows_per_group,
+                                                             int64_t parts, int log_classes, int dim, bool whole,
+                                                             void* dweight, void* dbias, int dtype) {
+  enter_grid(partial);
+  const int tiles = (dim + 255) / 256, col = (int)(blockIdx.x % tiles) * 256 + threadIdx.x;
+  if (col >= dim) return;
+  int64_t g = blockIdx.x / tiles;
+  float sw = 0.0f, sb = 0.0f;
+  const float* slot;
+  int n, step;
+  if (whole) {
+    const int64_t part = g + 1, boundary = first_row(part, parts, rows);
+    g = boundary / rows_per_group;
+    const int64_t lo = g * rows_per_group;
+    if (lo == boundary || first_row(part - 1, parts, rows) > lo) return;
+    slot = partial + (2 * part - 1) * 2 * dim + col;
+    sw = slot[0];
+    sb = slot[dim];
+    slot += 2 * dim;
+    n = (int)(GroupParts(g, rows, rows_per_group, parts).last - part + 1);
+    step = 4 * dim;
+  } else {
+    const GroupParts of(g, rows, rows_per_group, parts);
+    slot = partial + ((of.first + g) << log_classes) * 2 * dim + col;
+    n = (int)((of.last - of.first + 1) << log_classes);
+    step = 2 * dim;
+  }
+#pragma unroll 4
+  for (int i = 0; i < n; ++i, slot += step) {
+    sw += slot[0];
+    sb += slot[dim];
+  }
+  const bool fp32 = dtype == SPARSP_FP32, fp16 = dtype == SPARSP_FP16;
+  if (dweight != nullptr) store_weight(dweight, g * dim + col, sw, fp32, fp16);
+  if (dbias != nullptr) store_weight(dbias, g * dim + col, sb, fp32, fp16);
+}
+
 // ---- host side ------------------------------------------------------------------------------------------------------
 
 int64_t norm_groups(const sparsp_norm& n) {
@@ -793,6 +871,7 @@ struct NormPlan {
   int parts, log_classes, log_lanes;
   int resident;  // CTAs on a multiprocessor
   unsigned grid, column_ctas;  // rows', and behind them columns'
+  bool whole_groups;           // backward
 };
 
 // By the values that a worker has to hold.  Teams: the least that holds them of those whose number of warps shares out
@@ -821,7 +900,15 @@ static int worker_kind(int span, bool bwd) {
   return kLongTeam;
 }
 
+constexpr int kFewSlots = 24;
 constexpr int kNormSmem = 224 * 1024;  // of a multiprocessor, for rings
+
+// In classes a group has slots of every one of them: 16 bytes a column and class, written and read, beside 6 or 12 a
+// column and row.  Groups of so few rows go value by value, without classes (17776 x 1921 fp32, four classes, groups of 2
+// rows 187 us, 579 in classes; of 10 155 and 170; of 20 151 and 121; bf16, eight classes, of 20 150 and 230).
+static bool short_groups(const sparsp_norm& n, int log_classes) {
+  return n.rows_per_group > 0 && n.rows_per_group < (40 << log_classes) / (3 * element_bytes(n.dtype));
+}
 
 static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
   NormPlan p = {};
@@ -871,6 +958,7 @@ static NormPlan plan_norm(const sparsp_norm& n, bool pieces, bool bwd) {
     if (bwd) most = std::min(most, std::max<int64_t>(kSms, rows / 4));
     p.parts = (int)std::max<int64_t>(1, most >> p.log_classes);
     const int all = p.parts << p.log_classes;
+    p.whole_groups = bwd && norm_groups(n) >= all && p.log_classes == 0;
     // few warps go to as many SMs as there are (300 x 512 bf16 backward 6.8 us, 8.6 by eights; 64 x 256 5.2 and 5.8)
     while (workers > 1 && (all + workers - 1) / workers < kSms) workers /= 2;
     if (!cta) p.threads = 32 * workers;
@@ -884,7 +972,9 @@ int64_t norm_workspace_bytes(const sparsp_norm& n) {
   int64_t slots = 0;
   for (const bool pieces : {true, false}) {
     const NormPlan p = plan_norm(n, pieces, true);
-    slots = std::max(slots, (p.parts + norm_groups(n)) << p.log_classes);
+    int64_t groups = norm_groups(n);
+    if (p.log_classes == 0 || short_groups(n, p.log_classes)) groups = std::min<int64_t>(groups, p.parts << p.log_classes);
+    slots = std::max(slots, (p.parts + groups) << p.log_classes);
   }
   return kStatusWords * 4 + slots * 2 * n.dim * 4;
 }
@@ -947,6 +1037,7 @@ static NormParams norm_params(const sparsp_norm& n, const NormPlan& plan) {
   p.log_lanes = plan.log_lanes;
   p.ring_bytes = plan.ring_bytes;
   p.ring_half = plan.ring_half;
+  p.whole_groups = plan.whole_groups;
   p.eps = n.eps;
   p.inv_dim = 1.0f / (float)n.dim;
   return p;
@@ -970,15 +1061,19 @@ int launch_norm_fwd(const sparsp_norm& n, const void* X, const void* w, const vo
 int launch_norm_bwd(const sparsp_norm& n, const void* dY, const void* X, const void* w, const float* mean,
                     const float* rstd, void* dX, void* dw, void* db, char* ws, cudaStream_t st) {
   NormPlan plan = plan_norm(n, in_pieces(n, X, dY, dX), true);
+  if (plan.log_classes > 0 && short_groups(n, plan.log_classes) && norm_groups(n) >= plan.parts << plan.log_classes >> 2)
+    plan = plan_norm(n, false, true);  // (with fewer groups than that the slots are few as well)
   NormParams p = norm_params(n, plan);
   p.want_weights = dw != nullptr || db != nullptr;
   // Few rows are added in the same launch (backward bf16 1 x 32: 2.1 us, 4.8 with sums of workers in a second launch;
   // 64 x 5120 3.6 and 10.8): up to 32 of a group a thread of add_columns, and up to ten rounds of CTAs; half of both
   // where a multiprocessor has one CTA at a time (500 x 8192 23 and 15 with 32; 2 groups of 250 x 8192, ten rounds, 29
-  // and 20).
+  // and 20); up to 2^22 values, for x and dy are read twice (8 groups of 64 x 5120 15.2 and 17.3; of 250 x 5120 46 and
+  // 33; 64 of 250 x 256 17.4 and 16.5; 150 of 400 x 256 51 and 26).
   const int64_t columns = norm_groups(n) * ((n.dim + 15) / 16);
   const int several = std::min(plan.resident, 2);
-  const bool direct = p.want_weights && n.rows > 0 && std::min(p.rows_per_group, n.rows) <= several * plan.threads &&
+  const bool direct = p.want_weights && n.rows > 0 && n.rows * n.dim <= 1 << 22 &&
+                      std::min(p.rows_per_group, n.rows) <= several * plan.threads &&
                       plan.grid + columns <= 5 * several * kSms * plan.resident;
   const unsigned column_ctas = (unsigned)columns;
   if (direct) p.want_weights = 0;
@@ -993,6 +1088,7 @@ int launch_norm_bwd(const sparsp_norm& n, const void* dY, const void* X, const v
     p.partial = reinterpret_cast<float*>(ws + kStatusWords * 4);
     p.dweight = dw;
     p.dbias = db;
+    p.vector_weights = n.dim % 4 == 0 && (uintptr_t)dw % 16 == 0 && (uintptr_t)db % 16 == 0;
     if (direct && dX != X && dX != dY) {
       plan.column_ctas = column_ctas;
     } else if (direct) {
@@ -1003,6 +1099,17 @@ int launch_norm_bwd(const sparsp_norm& n, const void* dY, const void* X, const v
     SPARSP_CUDA_OK(launch_norm(n.dtype, p, plan, true, st));
   }
   if (p.want_weights && norm_groups(n) > 0) {
+    const int64_t groups = norm_groups(n), slots = (plan.parts + groups) << plan.log_classes;
+    // few slots of a group: a thread adds a column of them (17776 x 1920 bf16, groups of 40 rows, two slots: 54 us, 296 by
+    // CTAs; of 500, 12 slots, 49 and 65; of 1000, 25, 52 and 55; of 1500, 37, 56 and 51)
+    if (n.rows > 0 && (plan.whole_groups || slots <= kFewSlots * groups)) {
+      const int64_t items = plan.whole_groups ? (n.rows_per_group > 1 ? plan.parts - 1 : 0) : groups;
+      if (items > 0)
+        SPARSP_CUDA_OK(launch_kernel(norm_few_slots_kernel, dim3((unsigned)(items * ((n.dim + 255) / 256))), 256, 0, st,
+                                     p.partial, n.rows, p.rows_per_group, (int64_t)plan.parts, plan.log_classes, n.dim,
+                                     plan.whole_groups, dw, db, n.weight_dtype));
+      return SPARSP_OK;
+    }
     const bool wide = norm_groups(n) * ((n.dim + 31) / 32) >= 100;
     const int columns = wide ? 32 : 8;
     const unsigned grid = (unsigned)(norm_groups(n) * ((n.dim + columns - 1) / columns));

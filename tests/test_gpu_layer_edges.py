@@ -325,3 +325,62 @@ def test_a_last_round_is_shared_out_where_that_is_shorter(m, d, f, launches):
     assert binding.sparsp_launch_count() - before == launches
     assert binding.sparsp_status(ws) == binding.SPARSP_OK
     ffn_tests.check_forward("silu", BF, x, wg, wu, h, gate, up)
+
+
+@pytest.mark.parametrize("dtype,wtype", [(BF, BF), (BF, FL), (FL, FL), (HF, HF)])
+@pytest.mark.parametrize("dim", [24, 333, 1152, 1921, 5120, 5127])
+def test_many_groups(dim, dtype, wtype):
+    """Weights per row or per few rows: groups that one worker has all of, groups across the parts of two and more, few
+    slots of a group and many; in a workspace of just the size, with what lies behind it kept."""
+    for per, groups in ((1, 3001), (2, 1501), (3, 1000), (7, 700), (20, 250), (61, 75), (200, 20), (900, 5)):
+        rows = per * groups - (per > 2)  # the last group is smaller
+        if rows * dim > 1 << 24:
+            continue
+        x, w, b, dy = inputs(rows, dim, groups, dtype, wtype, seed=per)
+        norm = binding.make_norm(rows, dim, per, EPS, dtype, wtype)
+        size = binding.sparsp_layer_norm_workspace_bytes(norm)
+        hold = torch.full((size + (1 << 20),), 255, dtype=torch.uint8, device="cuda")
+        mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+        y, dx = torch.full_like(x, float("nan")), torch.full_like(x, float("nan"))
+        binding.sparsp_layer_norm_fwd(norm, x, w, b, y, mean, rstd)
+        dw, db = torch.full_like(w, float("nan")), torch.full_like(w, float("nan"))
+        binding.sparsp_layer_norm_bwd(norm, dy, x, w, mean, rstd, dx, dw, db, hold[:size])
+        assert bool((hold[size:] == 255).all())
+        check_norm(x, w, b, dy, per, groups, norm, y, dx)
+        check_weight_gradients(x, dy, mean, rstd, per, groups, dw, db)
+        # one of the two wanted, gradients that do not begin on 16 bytes: the same values
+        odd = torch.full((w.numel() + 1,), float("nan"), dtype=wtype, device="cuda")[1:].view_as(w)
+        binding.sparsp_layer_norm_bwd(norm, dy, x, w, mean, rstd, dx, odd, None, hold[:size])
+        assert torch.equal(odd, dw)
+        binding.sparsp_layer_norm_bwd(norm, dy, x, w, mean, rstd, dx, None, odd, hold[:size])
+        assert torch.equal(odd, db)
+
+
+def check_weight_gradients(x, dy, mean, rstd, per, groups, dw, db):
+    """Sums of a group's terms in fp32, by at most 32 + 60 additions in a row (a worker's rows, slots, lanes)."""
+    X, DY, M, R = x.double(), dy.double(), mean.double()[:, None], rstd.double()[:, None]
+    g = torch.arange(x.shape[0], device="cuda") // per
+    xh = (X - M) * R
+    of = lambda t: torch.zeros(groups, x.shape[1], dtype=torch.float64, device="cuda").index_add_(0, g, t)  # noqa: E731
+    exh = 3 * F32 * (xh.abs() + (X.abs() + M.abs()) * R)
+    terms = min(per, 900) + 8
+    for got, want, off in ((dw, of(DY * xh), of(DY.abs() * exh + terms * F32 * (DY * xh).abs())),
+                           (db, of(DY), of(terms * F32 * DY.abs()))):
+        close(got, want, off + UNIT[got.dtype] * (want.abs() + off) + TINY[got.dtype], "weights' gradients")
+
+
+@pytest.mark.parametrize("dim", [128, 1920, 1921])
+def test_a_row_of_weights_per_row_takes_one_launch(dim):
+    rows = 6000
+    x, w, b, dy = inputs(rows, dim, rows, BF, BF, seed=1)
+    norm = binding.make_norm(rows, dim, 1, EPS, BF, BF)
+    mean, rstd = torch.empty(rows, device="cuda"), torch.empty(rows, device="cuda")
+    y, dx, dw, db = (torch.empty_like(x) for _ in range(4))
+    binding.sparsp_layer_norm_fwd(norm, x, w, b, y, mean, rstd)
+    before = binding.sparsp_launch_count()
+    binding.sparsp_layer_norm_bwd(norm, dy, x, w, mean, rstd, dx, dw, db, binding.make_norm_workspace(norm))
+    assert binding.sparsp_launch_count() - before == 1
+    xh = (x.double() - mean.double()[:, None]) * rstd.double()[:, None]
+    close(dw, dy.double() * xh, (UNIT[BF] + 8 * F32) * (dy.double() * xh).abs() + 8 * F32 * dy.double().abs() *
+          (x.double().abs() + mean.double().abs()[:, None]) * rstd.double()[:, None], "dweight")
+    assert torch.equal(db, dy)

@@ -260,3 +260,11 @@ def test_ffn_outputs_in_the_place_of_inputs():
         args[out] = ok[into]
         with pytest.raises(SparspError, match="output"):
             binding.sparsp_gated_ffn_bwd(ffn, *args)
+
+
+@pytest.mark.parametrize("dim", [128, 1921, 5120])
+@pytest.mark.parametrize("per", [1, 2, 16])
+def test_a_norm_workspace_does_not_grow_with_small_groups(dim, per):
+    """What a group of one worker's rows needs is nothing: 3.1 GB for 75600 x 5120 with a slot a group."""
+    need = [binding.sparsp_layer_norm_workspace_bytes(binding.make_norm(r, dim, per)) for r in (75600, 10 ** 6)]
+    assert need[0] == need[1] <= 128 << 20
