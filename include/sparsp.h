@@ -378,9 +378,9 @@ SPARSP_API int sparsp_demand_plan_noalloc(const sparsp_shape* shape, const uint3
  *
  * What a layer computes beside its attention: rotary positions on Q and K, layer norm, the gated feed-forward half, each
  * with its backward pass.  They follow the conventions above and need no block mask, so NB and head_dim are not limited
- * to what the attention takes.  Element types are SPARSP_BF16, SPARSP_FP16 or SPARSP_FP32; all arithmetic is in fp32,
- * rounded once where a result is stored.  A result has no order of additions that varies from call to call: the same
- * inputs give the same bits.
+ * to what the attention takes.  Element types are SPARSP_BF16, SPARSP_FP16 or SPARSP_FP32; all arithmetic on them is in
+ * fp32, rounded once where a result is stored, but for dG and dU in sparsp_gated_ffn_bwd, which are rounded on the way.  A
+ * result has no order of additions that varies from call to call: the same inputs give the same bits.
  */
 #define SPARSP_BF16 0
 #define SPARSP_FP16 1
@@ -438,8 +438,9 @@ SPARSP_API int sparsp_rotary_table(const sparsp_rotary* rotary, const double* in
                                    void* stream);
 
 /* Rotates Q and, where it is given, K:
- *   (y0, y1) = (x0 c - x1 s, x0 s + x1 c), (c, s) from the table;  inverse != 0: -s in the place of s, which takes a
- *   rotation back and, applied to the gradient of the outputs, gives the gradient of the inputs.
+ *   (y0, y1) = (x0 c - x1 s, x0 s + x1 c), (c, s) from the table;  inverse != 0: -s in the place of s, which, applied to
+ *   the gradient of the outputs, gives the gradient of the inputs, and where the amplitude is 1 takes a rotation back (there
+ *   and back multiplies by the amplitude's square).
  * Coordinates of token n: with positions, positions[batch * positions_stride_batch + 3 n ..+2]; without, its place on the
  * latent grid plus (origin_t, origin_h, origin_w), which then has to stay inside the table.  A text token without
  * positions and a token whose first position is negative keep their values, as does one whose position is not in the
@@ -518,8 +519,9 @@ SPARSP_API int sparsp_gated_ffn_workspace_bytes(const sparsp_ffn* ffn, int32_t b
 SPARSP_API int sparsp_gated_ffn_fwd(const sparsp_ffn* ffn, const void* X, const void* Wgate, const void* Wup, void* H,
                                     void* gate, void* up, void* workspace, void* stream);
 
-/* With dG = dH * up * a'(gate) and dU = dH * a(gate), both rounded to dtype (the tensor cores' operands; for up to 128
- * tokens and dim up to 18432 as the sum of two such values):
+/* With dG = dH * up * a'(gate) and dU = dH * a(gate), both rounded to dtype (the tensor cores' operands: results are off
+ * by about 1.4 times what fp32 operands would leave after their own rounding; for up to 128 tokens and dim up to 18432
+ * the sum of two such values, which leaves no more than those):
  *   dX = dG Wgate + dU Wup,  dWgate = dG^T X,  dWup = dU^T X, sums in fp32;  no output may be an X, Wgate or Wup that is read
  *   dX             out  may be NULL (not wanted); Wgate and Wup may then be NULL too
  *   dWgate, dWup   out  both or neither NULL; X may be NULL without them.  Without tokens they are zero. */

@@ -13,9 +13,11 @@
 // both are in two parts, the rounded value and what it leaves, one 128 rows behind the other.  dX takes the two parts
 // as the two halves of its 256-row tile and adds them when the pieces of K are added, dW as more tokens.
 //
-// Bound by the tensor cores where all sizes are large: 97 to 98 % of their cycles, at the 1.3 to 1.5 GHz that the power
-// limit leaves (37800 x 5120 x 13824 bf16, both projections kept: 7.9 ms = 1350 TFLOP/s; backward 17.1 to 20.3 ms =
-// 1050 to 1250).
+// Bound by the tensor cores and by power where all sizes are large.  A single launch of 8192 x 5120 x 6912 bf16, both
+// projections kept, has them busy for 97.9 % of its cycles, at 1.38 GHz.  In a loop of seconds, at 980 to 990 W: 37800
+// x 5120 x 13824, both kept, 8.09 ms = 1320 TFLOP/s at a median of 1.21 GHz, so that the 8.85 million clocks of its
+// products are 91 % of the time; backward 20.1 ms = 1065 TFLOP/s at 1.00 GHz, 88 % (17.1 to 20.3 ms over GPUs and
+// shorter loops).
 #include <algorithm>
 #include <cmath>
 
@@ -924,20 +926,21 @@ static int join_ctas(const GemmParams& p, int mode) {
   return (p.m_tiles * p.n_tiles - p.whole) * ((mode == kForward ? BN / 2 : BN) / 8);
 }
 
-// What a product takes on some pairs of SMs, in clocks, and whether its last round is shared out by blocks of K for that.
+// What a product takes on some pairs of SMs, in clocks, and whether its last round is shared out by blocks of K for
+// that.
 //
 // 512 a block of K and 2500 a unit for what no block hides.  Sharing costs 8000 for the launch that adds the sums, 1200
 // for each piece of a tile, which are added one after the other, and 90 for each piece there is, which is written and
 // read: fitted to 361 sizes of all three products, each timed whole and in 2, 3, 4, 6 and as many pieces as there are
-// pairs; by these figures 0.3 % is lost on average against the best of them, 5 % at most against whole tiles.  (us, whole
-// and in pieces; tiles of the last round x blocks: 6 x 128 42.3, two 29.1, four 22.5, twelve 29.0; 6 x 32 behind a round
-// of 74 tiles 29.2, two 34.9; 20 x 32 16.3, two 18.1; 20 x 128 45.2, three 33.7; 37 x 64 26.8, two 29.4; 37 x 256 99,
-// two 72.)
+// pairs; by these figures 0.3 % is lost on average against the best of them, 5 % at most against whole tiles.  (us,
+// whole and in pieces; tiles of the last round x blocks: 6 x 128 42.3, two 29.1, four 22.5, twelve 29.0; 6 x 32 behind
+// a round of 74 tiles 29.2, two 34.9; 20 x 32 16.3, two 18.1; 20 x 128 45.2, three 33.7; 37 x 64 26.8, two 29.4; 37 x
+// 256 99, two 72.)
 //
 // Where there are not two pairs for a tile, all pairs can have equal runs, most of which touch two tiles.  They read
 // different rows and columns at one time, so it takes long tiles and few of them: 24000 beside the blocks, and at most
-// seven tiles for ten pairs (40 x 256 102, 85 shared; 48 x 256 118, 110; 48 x 128 54, 58; 50 x 160 64, 70; 56 x 256 127,
-// 131; 64 x 512 254, 348).
+// seven tiles for ten pairs (40 x 256 102, 85 shared; 48 x 256 118, 110; 48 x 128 54, 58; 50 x 160 64, 70; 56 x 256
+// 127, 131; 64 x 512 254, 348).
 struct Clocks {
   int64_t product, join;
   int shares;  // pairs that the last round is shared out to, 0: none
@@ -1010,10 +1013,10 @@ static int launch_gemm(const GemmParams& p, const GemmMaps& m, int dtype, cudaSt
 
 // dX and dW together.  Alone, each of two small products leaves pairs of SMs without a tile in its last round; together
 // they share the pairs out so that both end at the same time.  What is shared out by blocks of K stays so for either
-// product alone, so that it gives the same bits.  Returns the pairs of dX, or 0 where the two are better apart, with 10000
-// clocks for another launch and its wait: in two parts dX needs a pair for each of its tiles and more, which may leave dW
-// too few (64 x 18432 x 256, 72 of 74: together 305 us, apart 31; x 16384, 64: 46 and 29; x 14336, 56: 29 and 28; x
-// 12288: 21 and 27).
+// product alone, so that it gives the same bits.  Returns the pairs of dX, or 0 where the two are better apart, with
+// 10000 clocks for another launch and its wait: in two parts dX needs a pair for each of its tiles and more, which may
+// leave dW too few (64 x 18432 x 256, 72 of 74: together 305 us, apart 31; x 16384, 64: 46 and 29; x 14336, 56: 29 and
+// 28; x 12288: 21 and 27).
 static int plan_both(GemmParams* pi, GemmParams* pw) {
   const int ti = pi->m_tiles * pi->n_tiles, tw = pw->m_tiles * pw->n_tiles;
   const int bi = 2 * pi->k_blocks, bw = pw->k_blocks;
@@ -1060,7 +1063,10 @@ static int launch_both(const GemmParams& pi, const GemmMaps& mi, const GemmParam
 // 1160 x 2504, backward: 41 us without).
 static int64_t hidden_pitch(const sparsp_ffn& f) { return align_up(f.hidden, 64); }
 // Two parts need the halves of every tile of dX to meet, in pieces of K that are added; rows of so many tiles that
-// pairs have a whole one each are left out of it.
+// pairs have a whole one each are left out of it.  What they cost (backward us, two parts and one: 5120 x 13824, 1
+// token 143 and 144, 64 147 and 141, 128 170 and 151; 1920 x 7680, 128 tokens 58 and 55; 1160 x 2504 22 and 21; 4096 x
+// 1024 21 and 18) buys the error of fp32 operands, 1.4 times less; from 129 tokens on dX would take twice the tiles
+// and dW twice the blocks.
 static bool two_parts(const sparsp_ffn& f) { return f.tokens <= kFewTokens && ceil_div(f.dim, BN) <= kPairs - 2; }
 static int64_t hidden_rows(const sparsp_ffn& f) { return two_parts(f) ? kFewTokens + f.tokens : f.tokens; }
 static int64_t hidden_bytes(const sparsp_ffn& f, int64_t rows) { return align_up(rows * hidden_pitch(f) * 2, 256); }

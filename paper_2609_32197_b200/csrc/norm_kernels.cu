@@ -18,7 +18,7 @@ namespace sparsp {
 // to row.  (Value by value, backward over 15554 x 1921 fp32 took 153 us, with single 4-byte copies 111.)
 //
 // Bound by HBM: 75600 x 5120 bf16 forward 245 to 264 us = 5.9 to 6.3 TB/s.  Backward, twice as much is read as written,
-// by few warps, for the sums of the weights' gradients stay in registers: 383 to 423 us = 5.5 to 6.1 TB/s.
+// by few warps, for the sums of the weights' gradients stay in registers: 380 to 423 us = 5.5 to 6.1 TB/s.
 
 // Who works on a row, by its length: a warp up to 1280 values, otherwise a team, a CTA of as few warps as hold the row
 // with 24, 32 or 40 values a thread.  Few warps with many registers are better than more with fewer: what a row costs

@@ -67,8 +67,9 @@ constexpr int kRotaryHeads = 4;
 // them: the angles depend on the token alone, so the table costs little.  A token's units are consecutive lanes, so a
 // head's row is read and written whole; where heads lie closer together than tokens, a few heads of a token come next
 // to each other, so that a warp reads on in memory (48 heads x 17776 tokens x 64 fp16, token-major: 84 us without).
-// Bound by HBM: 40 heads x 75600 x 128 bf16, Q and K, 491 us = 6.3 TB/s. E: elements of a vector, 1 where the rotated
-// part or the pairs do not begin and end on 16 bytes.
+// Bound by HBM: 40 heads x 75600 x 128 bf16, Q and K, 491 us = 6.3 TB/s; with positions of permuted tokens 494. E:
+// elements of a vector, 1 where the rotated part or the pairs do not begin and end on 16 bytes; then by the number of loads
+// and stores, one an element (16 heads x 17776 x 72 bf16, halves of 36 pairs, 56 us; neighbours, on 16 bytes, 32).
 template <typename T, int E, bool kHalf>
 __global__ void __launch_bounds__(kRotaryThreads) rotary_kernel(const RotaryParams p) {
   const int32_t* positions = p.positions;
