@@ -481,7 +481,8 @@ typedef struct sparsp_norm {
 SPARSP_API int sparsp_layer_norm_fwd(const sparsp_norm* norm, const void* X, const void* weight, const void* bias,
                                      void* Y, float* mean, float* rstd, void* stream);
 
-/* Bytes of workspace that the backward pass needs (partial sums of the weights' gradients). */
+/* Bytes of workspace that the backward pass needs (partial sums of the weights' gradients).  More rows, all else equal,
+ * never need less. */
 SPARSP_API int sparsp_layer_norm_workspace_bytes(const sparsp_norm* norm, int64_t* bytes);
 
 /* With xh = (x - mean) rstd and a = dy * weight:
