@@ -530,6 +530,65 @@ SPARSP_API int sparsp_gated_ffn_bwd(const sparsp_ffn* ffn, const void* dH, const
                                     const void* Wup, const void* gate, const void* up, void* dX, void* dWgate,
                                     void* dWup, void* workspace, void* stream);
 
+/* 4-bit operands: a value is e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6, either sign) times the scale of its block, a run of a row's
+ * values, times 2^exponent for the whole matrix.
+ *   SPARSP_MXFP4  blocks of 32; a scale is a power of two (its exponent + 127 in 8 bits): the least with which the block's
+ *                 largest magnitude is at most 6; exponent is 0
+ *   SPARSP_NVFP4  blocks of 16; a scale is e4m3: the largest magnitude / 6 / 2^exponent, rounded to nearest even, at most 448.
+ *                 exponent = ceil(log2(largest of the matrix / 2688)) uses the whole range.
+ * Values are rounded to the nearest, ties to the even code; what lies beyond 6 scales becomes 6.  A block whose largest
+ * is 0 (NVFP4: whose scale rounds to 0) is all zeros.  A block with an infinity or NaN gets the scale NaN, which stays
+ * NaN in every product it is part of. */
+#define SPARSP_MXFP4 0
+#define SPARSP_NVFP4 1
+typedef struct sparsp_fp4 {
+  int64_t rows;     /* 0 is allowed */
+  int64_t stride_x; /* elements from row to row of X and values: a multiple of 8, >= cols */
+  int32_t cols;     /* a multiple of 32 */
+  int32_t format;   /* SPARSP_MXFP4 or SPARSP_NVFP4 */
+  int32_t exponent; /* -100 .. 100; 0 for SPARSP_MXFP4 */
+  int32_t dtype;    /* of X and values */
+} sparsp_fp4;
+
+/* Bytes of the scales of a matrix: ceil(rows / 128) * ceil(cols / (4 blocks)) * 512.  They lie in groups of 128 rows x 4
+ * blocks, the groups of a row behind one another; in a group row r, block b is at (r % 32) * 16 + (r / 32) * 4 + b. */
+SPARSP_API int sparsp_fp4_scales_bytes(const sparsp_fp4* fp4, int64_t* bytes);
+
+/* X to 4 bits.
+ *   X       in   [rows][cols], row stride stride_x
+ *   codes   out  [rows][cols / 2] bytes, the value of the lower column in the lower half
+ *   scales  out  sparsp_fp4_scales_bytes() bytes; those of rows and blocks that are not there are 0
+ *   values  out  what the operand stands for, rounded to dtype (exact for bf16 and fp32 inside their range): what a backward
+ *                pass through this rounding multiplies with; may be NULL, and may be X
+ * All pointers are 16-byte aligned. */
+SPARSP_API int sparsp_fp4_quantize(const sparsp_fp4* fp4, const void* X, void* codes, void* scales, void* values,
+                                   void* stream);
+
+/* C = A B^T 2^exponent + bias of two such operands of one format. */
+typedef struct sparsp_fp4_gemm {
+  int64_t rows;     /* of A and C; 0 is allowed */
+  int64_t stride_c; /* elements from row to row of C: a multiple of 8, >= cols */
+  int32_t cols;     /* of C, rows of B: a multiple of 8 */
+  int32_t depth;    /* columns of A and B: a multiple of 32 */
+  int32_t format;
+  int32_t exponent; /* the sum of both operands' exponents, -126 .. 126 */
+  int32_t dtype;    /* of C and bias */
+} sparsp_fp4_gemm;
+
+/* Bytes of workspace.  More rows, all else equal, never need less. */
+SPARSP_API int sparsp_fp4_product_workspace_bytes(const sparsp_fp4_gemm* product, int64_t* bytes);
+
+/* The product, summed in fp32 and rounded once.
+ *   A, A_scales   in   codes and scales of A [rows][depth]
+ *   B, B_scales   in   of B [cols][depth]: a projection's weight as it lies
+ *   bias          in   [cols]; may be NULL
+ *   C             out  [rows][cols], row stride stride_c; no input
+ *   workspace     in   sparsp_fp4_product_workspace_bytes() bytes, 256-byte aligned, its first 256 bytes zero before the
+ *                      first call; calls that may run at the same time take one each
+ * All pointers but the workspace are 16-byte aligned. */
+SPARSP_API int sparsp_fp4_product(const sparsp_fp4_gemm* product, const void* A, const void* A_scales, const void* B,
+                                  const void* B_scales, const void* bias, void* C, void* workspace, void* stream);
+
 /* Synchronises `stream` and returns the workspace's status word in *code (SPARSP_OK if no kernel
  * reported a problem since the last reset), then resets it. */
 SPARSP_API int sparsp_status(void* workspace, void* stream, int32_t* code);

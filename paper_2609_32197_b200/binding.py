@@ -37,6 +37,7 @@ EXPORTS = [
     "sparsp_rotary_frequencies", "sparsp_rotary_table_bytes", "sparsp_rotary_table", "sparsp_rotary_apply",
     "sparsp_layer_norm_fwd", "sparsp_layer_norm_workspace_bytes", "sparsp_layer_norm_bwd",
     "sparsp_gated_ffn_workspace_bytes", "sparsp_gated_ffn_fwd", "sparsp_gated_ffn_bwd",
+    "sparsp_fp4_scales_bytes", "sparsp_fp4_quantize", "sparsp_fp4_product_workspace_bytes", "sparsp_fp4_product",
 ]
 SPARSP_XCHG_HOST_MEMORY = 1
 SPARSP_BF16, SPARSP_FP16, SPARSP_FP32 = 0, 1, 2
@@ -44,9 +45,10 @@ DTYPES = {torch.bfloat16: SPARSP_BF16, torch.float16: SPARSP_FP16, torch.float32
 PAIRINGS = {"interleaved": 0, "half": 1}
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 ACTIVATIONS = {"silu": 0, "gelu_tanh": 1, "gelu": 2}
+FP4_FORMATS = {"mxfp4": 0, "nvfp4": 1}
 
-# Argument types of the calls that a layer makes (s: shape, r / n / m: description of rotary positions, a norm or a
-# feed-forward, p: pointer, i / l: 32 / 64-bit integer, f / d: 32 / 64-bit float), so that ctypes
+# Argument types of the calls that a layer makes (s: shape, r / n / m / q / g: description of rotary positions, a
+# norm, a feed-forward, a 4-bit operand or a product of two, p: pointer, i / l: 32 / 64-bit integer, f / d: 32 / 64-bit float), so that ctypes
 # converts plain values itself: a ctypes object per argument costs more than the call.
 _SIGNATURES = {
     "sparsp_block_mask": "sppippppppp",
@@ -70,6 +72,10 @@ _SIGNATURES = {
     "sparsp_gated_ffn_workspace_bytes": "mip",
     "sparsp_gated_ffn_fwd": "mpppppppp",
     "sparsp_gated_ffn_bwd": "mppppppppppp",
+    "sparsp_fp4_scales_bytes": "qp",
+    "sparsp_fp4_quantize": "qppppp",
+    "sparsp_fp4_product_workspace_bytes": "gp",
+    "sparsp_fp4_product": "gpppppppp",
 }
 
 
@@ -104,6 +110,17 @@ class sparsp_ffn(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32)]
 
 
+class sparsp_fp4(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("stride_x", ctypes.c_int64), ("cols", ctypes.c_int32),
+                ("format", ctypes.c_int32), ("exponent", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class sparsp_fp4_gemm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("stride_c", ctypes.c_int64), ("cols", ctypes.c_int32),
+                ("depth", ctypes.c_int32), ("format", ctypes.c_int32), ("exponent", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
+
+
 _lib = None
 
 
@@ -127,7 +144,8 @@ def lib() -> ctypes.CDLL:
         for name in EXPORTS:
             getattr(L, name)  # AttributeError if a declared symbol is not exported
         kinds = {"s": ctypes.POINTER(sparsp_shape), "r": ctypes.POINTER(sparsp_rotary),
-                 "n": ctypes.POINTER(sparsp_norm), "m": ctypes.POINTER(sparsp_ffn), "p": ctypes.c_void_p,
+                 "n": ctypes.POINTER(sparsp_norm), "m": ctypes.POINTER(sparsp_ffn),
+                 "q": ctypes.POINTER(sparsp_fp4), "g": ctypes.POINTER(sparsp_fp4_gemm), "p": ctypes.c_void_p,
                  "i": ctypes.c_int32, "l": ctypes.c_int64, "f": ctypes.c_float, "d": ctypes.c_double}
         for name, args in _SIGNATURES.items():
             getattr(L, name).argtypes = [kinds[a] for a in args]
@@ -543,6 +561,52 @@ def sparsp_gated_ffn_fwd(ffn, X, Wgate, Wup, H, gate, up, workspace):
 def sparsp_gated_ffn_bwd(ffn, dH, X, Wgate, Wup, gate, up, dX, dWgate, dWup, workspace):
     _check(lib().sparsp_gated_ffn_bwd(ffn, _data(dH), _data(X), _data(Wgate), _data(Wup), _data(gate), _data(up),
                                       _data(dX), _data(dWgate), _data(dWup), _data(workspace), _stream_handle()))
+
+
+# ---- 4-bit operands and their product ----
+def make_fp4(rows: int, cols: int, format: str = "mxfp4", exponent: int = 0, dtype=torch.bfloat16,
+             stride_x: int = 0) -> sparsp_fp4:
+    """stride_x 0: contiguous rows."""
+    return sparsp_fp4(rows, stride_x or cols, cols, FP4_FORMATS[format], exponent, _dtype(dtype))
+
+
+def sparsp_fp4_scales_bytes(fp4: sparsp_fp4) -> int:
+    out = ctypes.c_int64()
+    _check(lib().sparsp_fp4_scales_bytes(fp4, ctypes.addressof(out)))
+    return out.value
+
+
+def make_fp4_operand(fp4: sparsp_fp4, device="cuda"):
+    """-> (codes uint8 [rows][cols / 2], scales uint8), to be filled by sparsp_fp4_quantize"""
+    return (torch.empty(fp4.rows, fp4.cols // 2, dtype=torch.uint8, device=device),
+            torch.empty(sparsp_fp4_scales_bytes(fp4), dtype=torch.uint8, device=device))
+
+
+def sparsp_fp4_quantize(fp4, X, codes, scales, values):
+    _check(lib().sparsp_fp4_quantize(fp4, _data(X), _data(codes), _data(scales), _data(values), _stream_handle()))
+
+
+def make_fp4_product(rows: int, cols: int, depth: int, format: str = "mxfp4", exponent: int = 0, dtype=torch.bfloat16,
+                     stride_c: int = 0) -> sparsp_fp4_gemm:
+    """exponent: the sum of both operands' exponents; stride_c 0: contiguous rows."""
+    return sparsp_fp4_gemm(rows, stride_c or cols, cols, depth, FP4_FORMATS[format], exponent, _dtype(dtype))
+
+
+def sparsp_fp4_product_workspace_bytes(product: sparsp_fp4_gemm) -> int:
+    out = ctypes.c_int64()
+    _check(lib().sparsp_fp4_product_workspace_bytes(product, ctypes.addressof(out)))
+    return out.value
+
+
+def make_fp4_product_workspace(product: sparsp_fp4_gemm, device="cuda") -> torch.Tensor:
+    ws = torch.empty(sparsp_fp4_product_workspace_bytes(product), dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+def sparsp_fp4_product(product, A, A_scales, B, B_scales, bias, C, workspace):
+    _check(lib().sparsp_fp4_product(product, _data(A), _data(A_scales), _data(B), _data(B_scales), _data(bias), _data(C),
+                                    _data(workspace), _stream_handle()))
 
 
 def sparsp_status(workspace) -> int:

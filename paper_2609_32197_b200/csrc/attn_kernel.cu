@@ -1970,6 +1970,24 @@ int make_matrix_tmap(CUtensorMap* out, const void* base, bool bf16, int64_t rows
   return SPARSP_OK;
 }
 
+int encode_tmap(CUtensorMap* out, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims,
+                const cuuint64_t* strides, const cuuint32_t* box, CUtensorMapSwizzle swizzle) {
+  EncodeTiledFn enc = get_encode_fn();
+  if (!enc) {
+    set_error("cuTensorMapEncodeTiled is not available from the driver");
+    return SPARSP_ERR_CUDA;
+  }
+  const cuuint32_t steps[3] = {1, 1, 1};
+  const CUresult r = enc(out, type, (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, steps,
+                         CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) {
+    set_error("cuTensorMapEncodeTiled (%d dimensions) failed with %d", rank, (int)r);
+    return SPARSP_ERR_CUDA;
+  }
+  return SPARSP_OK;
+}
+
 // Packed buffer viewed as a sequence of (block x d) bf16 tiles: dims (d, block, n_tiles, 1).
 static int make_packed_tmap(CUtensorMap* out, const void* packed, int64_t capacity_bytes, const Geometry& g) {
   EncodeTiledFn enc = get_encode_fn();

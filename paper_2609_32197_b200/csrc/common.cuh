@@ -113,6 +113,10 @@ int make_tile_tmap(CUtensorMap* out, const void* base, const sparsp_shape& s, co
 int make_matrix_tmap(CUtensorMap* out, const void* base, bool bf16, int64_t rows, int64_t cols, int64_t ld,
                      int box_cols, int box_rows);
 
+// ... up to three dimensions, the innermost first
+int encode_tmap(CUtensorMap* out, CUtensorMapDataType type, int rank, const void* base, const cuuint64_t* dims,
+                const cuuint64_t* strides, const cuuint32_t* box, CUtensorMapSwizzle swizzle);
+
 // launchers implemented in the kernel files -------------------------------------------------
 int launch_pool(const sparsp_shape& s, const Geometry& g, const void* Q, const void* K, float* pq, float* pk, char* ws,
                 const WsLayout& L, cudaStream_t st);

@@ -1,0 +1,562 @@
+// 4-bit floating point with a scale for each small block of a row: quantisation, and the product of two such operands.
+//
+// A value is e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) times its block's scale: for MXFP4 a power of two for
+// 32 values, for NVFP4 an e4m3 number for 16 values, times a power of two for the whole tensor.  That last one is a
+// power of two, not any number, because a block's scale has a mantissa of its own: the tensor's only has to bring
+// scales into e4m3's range, and as it is, no step of the quantisation depends on how a product or a quotient is rounded
+// (a quotient within half a step of fp32 of a border between two values is that border).
+//
+// Scales lie as the tensor cores take them: in groups of 128 rows x 4 blocks, 512 bytes each, where row r and block b
+// are at (r % 32) * 16 + (r / 32) * 4 + b; groups along a row follow one another.
+#include <algorithm>
+#include <cmath>
+
+#include "layer.cuh"
+#include "sm100_ptx.cuh"
+
+namespace sparsp {
+
+__host__ __device__ constexpr int fp4_block(int format) { return format == SPARSP_MXFP4 ? 32 : 16; }
+// groups of four blocks along a row
+__host__ __device__ inline int64_t fp4_groups(int64_t cols, int format) {
+  const int span = 4 * fp4_block(format);
+  return (cols + span - 1) / span;
+}
+int64_t fp4_scales_bytes(const sparsp_fp4& f) { return (f.rows + 127) / 128 * fp4_groups(f.cols, f.format) * 512; }
+
+static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
+
+// ---- quantisation ---------------------------------------------------------------------------------------------------
+// A thread has eight values of a row, neighbouring lanes a block; a warp goes through 1024 values of a row at a time.
+
+// 2^k for -127 <= k <= 127, exact
+__device__ __forceinline__ float power_of_two(int k) {
+  return k == -127 ? __uint_as_float(0x00400000u) : __uint_as_float((uint32_t)(k + 127) << 23);
+}
+__device__ __forceinline__ float from_e4m3(uint32_t code) {
+  uint32_t h;
+  asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)code));
+  return __half2float(__ushort_as_half((uint16_t)h));
+}
+__device__ __forceinline__ uint32_t to_e4m3(float x) {
+  uint16_t h;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(0.0f), "f"(x));
+  return h;
+}
+// eight values in half steps of e2m1, ties to the even code, what is beyond 6 becomes 6; the first in the low bits
+__device__ __forceinline__ uint32_t to_e2m1(const float (&x)[8]) {
+  uint32_t r;
+  asm("{\n\t"
+      ".reg .b8 a, b, c, d;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n\t"
+      "mov.b32 %0, {a, b, c, d};\n\t"
+      "}"
+      : "=r"(r)
+      : "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]), "f"(x[4]), "f"(x[5]), "f"(x[6]), "f"(x[7]));
+  return r;
+}
+__device__ __forceinline__ void from_e2m1(uint32_t codes, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t h;
+    // (a byte by itself: taken out of a wider register by mov, the conversion sees its neighbours)
+    asm("{\n\t"
+        ".reg .b8 a, b;\n\t"
+        "mov.b16 {a, b}, %1;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+        "}"
+        : "=r"(h)
+        : "h"((uint16_t)(codes >> 8 * i & 0xffu)));
+    const float2 v = __half22float2(*reinterpret_cast<const __half2*>(&h));
+    x[2 * i] = v.x;
+    x[2 * i + 1] = v.y;
+  }
+}
+
+// Eight values as they lie in memory: one 16-byte access, two for fp32.
+template <typename T>
+struct Eight {
+  static constexpr int kParts = sizeof(T) / 2, kEach = 8 / kParts;
+  Vec<T, kEach> part[kParts];
+  __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) part[i] = load_once<T, kEach>(p + i * kEach);
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) part[i].clear();
+  }
+  __device__ __forceinline__ float operator[](int i) const { return part[i / kEach][i % kEach]; }
+  __device__ __forceinline__ void set(const float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) part[i].set(x + i * kEach);
+  }
+  __device__ __forceinline__ void store(T* p) const {
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) store_vec<T, kEach>(p + i * kEach, part[i]);
+  }
+};
+
+// The block's scale from its largest magnitude (as bits, so that NaN is above infinity and infinity above the rest):
+// its code, its value, and what takes a value to e2m1's range.
+template <int kFormat>
+struct BlockScale {
+  uint32_t code;
+  float value, inverse, part;  // NVFP4: `part` is the scale without the tensor's power of two
+  __device__ __forceinline__ BlockScale(uint32_t most, int exponent) {
+    const bool finite = most < 0x7f800000u;
+    if constexpr (kFormat == SPARSP_MXFP4) {
+      // the least power of two with most <= 6 times it: most = m 2^E goes to E - 2 for m <= 1.5, else to E - 1
+      const int c = max((int)((most + 0x3fffffu) >> 23) - 2, 0);
+      code = finite ? c : 0xffu;
+      value = finite ? power_of_two(c - 127) : __uint_as_float(0x7fc00000u);
+      inverse = finite ? power_of_two(127 - c) : 0.0f;
+    } else {
+      code = finite ? to_e4m3(__fdiv_rn(__uint_as_float(most) * power_of_two(-exponent), 6.0f)) : 0x7fu;
+      part = finite ? from_e4m3(code) : 0.0f;
+      value = finite ? part * power_of_two(exponent) : __uint_as_float(0x7fc00000u);
+      inverse = part > 0.0f ? __frcp_rn(part) : 0.0f;
+    }
+  }
+  // x over the scale, on the right side of every border between two values
+  __device__ __forceinline__ float apply(float x, float tensor) const {
+    if constexpr (kFormat == SPARSP_MXFP4) {
+      return x * inverse;
+    } else {
+      x *= tensor;
+      const float q = fminf(fmaxf(x * inverse, -8.0f), 8.0f);  // (nothing infinite in the next step)
+      return fmaf(fmaf(-q, part, x), inverse, q);
+    }
+  }
+};
+
+struct QuantizeParams {
+  const void* x;
+  uint8_t* codes;
+  uint8_t* scales;
+  void* values;
+  int64_t rows, all_rows, ld, groups;  // all_rows: a multiple of 128
+  int32_t cols, chunks, exponent;
+};
+constexpr int kQuantizeUnroll = 4;
+
+template <typename T, int kFormat>
+__global__ void __launch_bounds__(256) quantize_kernel(QuantizeParams p) {
+  enter_grid(p.x);
+  constexpr int kBlock = fp4_block(kFormat), kLanes = kBlock / 8;
+  const int lane = threadIdx.x & 31;
+  const int64_t units = p.all_rows * p.chunks, step = (int64_t)gridDim.x * 8;
+  const float tensor = kFormat == SPARSP_NVFP4 ? power_of_two(-p.exponent) : 1.0f;
+  for (int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); unit < units; unit += step) {
+    const int64_t row = unit / p.chunks;
+    const int first = (int)(unit - row * p.chunks) * (kQuantizeUnroll * 256) + lane * 8;
+    const bool there = row < p.rows;
+    const T* from = static_cast<const T*>(p.x) + row * p.ld;
+    Eight<T> v[kQuantizeUnroll];
+#pragma unroll
+    for (int i = 0; i < kQuantizeUnroll; ++i) {
+      if (there && first + i * 256 < p.cols)
+        v[i].load(from + first + i * 256);
+      else
+        v[i].clear();
+    }
+    uint8_t* to_scales = p.scales + (row >> 7) * p.groups * 512 + (row & 31) * 16 + ((row & 127) >> 5) * 4;
+#pragma unroll
+    for (int i = 0; i < kQuantizeUnroll; ++i) {
+      const int col = first + i * 256;
+      uint32_t most = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) most = max(most, __float_as_uint(v[i][e]) & 0x7fffffffu);
+#pragma unroll
+      for (int d = 1; d < kLanes; d *= 2) most = max(most, __shfl_xor_sync(0xffffffffu, most, d));
+      const BlockScale<kFormat> s(most, p.exponent);
+      const int block = col / kBlock;
+      if (lane % kLanes == 0 && block < p.groups * 4) to_scales[(int64_t)(block >> 2) * 512 + (block & 3)] = (uint8_t)s.code;
+      if (!there || col >= p.cols) continue;
+      float q[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) q[e] = s.apply(v[i][e], tensor);
+      const uint32_t codes = to_e2m1(q);
+      *reinterpret_cast<uint32_t*>(p.codes + (row * p.cols + col) / 2) = codes;
+      if (p.values != nullptr) {
+        from_e2m1(codes, q);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) q[e] *= s.value;
+        v[i].set(q);
+        v[i].store(static_cast<T*>(p.values) + row * p.ld + col);
+      }
+    }
+  }
+}
+
+int launch_fp4_quantize(const sparsp_fp4& f, const void* X, uint8_t* codes, uint8_t* scales, void* values,
+                        cudaStream_t st) {
+  QuantizeParams p = {};
+  p.x = X;
+  p.codes = codes;
+  p.scales = scales;
+  p.values = values;
+  p.rows = f.rows;
+  p.all_rows = align_up(f.rows, 128);
+  p.ld = f.stride_x;
+  p.groups = fp4_groups(f.cols, f.format);
+  p.cols = f.cols;
+  p.chunks = ceil_div(p.groups * 4 * fp4_block(f.format), kQuantizeUnroll * 256);
+  p.exponent = f.exponent;
+  const int64_t ctas = (p.all_rows * p.chunks + 7) / 8;
+  const dim3 grid((unsigned)std::min<int64_t>(ctas, 8 * kSms));
+  SPARSP_WITH_TYPE(f.dtype, T, {
+    auto kern = f.format == SPARSP_MXFP4 ? quantize_kernel<T, SPARSP_MXFP4> : quantize_kernel<T, SPARSP_NVFP4>;
+    SPARSP_CUDA_OK(launch_kernel(kern, grid, 256, 0, st, p));
+  });
+  return SPARSP_OK;
+}
+
+// ---- product --------------------------------------------------------------------------------------------------------
+// C = A B^T + bias.  A pair of CTAs (a cluster of two, tcgen05 cta_group::2) makes a tile of 256 rows x 256 columns: each
+// loads 128 rows of A and half of B's rows by TMA, the even CTA issues the MMAs for both, and each finds its 128 rows,
+// all columns, in its own tensor memory.  Scales go from shared to tensor memory by tcgen05.cp before the MMAs that
+// read them: a CTA has those of its rows of A and of all of the tile's rows of B.
+//
+// Two accumulators of 256 columns would fill tensor memory and leave none for scales.  They overlap by 64: the tile
+// after begins as soon as these 64 have been read, which is done first.
+struct ProductParams {
+  const void* bias;
+  int32_t rows, cols, depth;
+  int32_t m_tiles, n_tiles, band, k_blocks;
+  float factor;
+  uint32_t idesc;
+  int32_t* status;
+  long long wait_limit;
+};
+
+constexpr int kDeep = 256;  // K elements of a stage: one 128-byte swizzled row
+constexpr int kResultWarps = 16;
+constexpr int kProductThreads = 32 * (kResultWarps + 2);
+constexpr int kRows = 128;  // of one CTA
+constexpr long long kWaitLimit = 200000000LL;  // of a wait in a kernel: about 0.1 s of SM clocks
+constexpr int kPairs = kSms / 2;
+
+template <int kFormat, typename T>
+struct ProductCfg {
+  static constexpr int kGroups = kDeep / (4 * fp4_block(kFormat));  // of four blocks, of a stage
+  static constexpr int kA = kRows * 128, kB = kRows * 128;
+  static constexpr int kScalesA = kGroups * 512, kScalesB = 2 * kGroups * 512;
+  static constexpr int kStage = kA + kB + kScalesA + kScalesB;  // (6144 or 3072 of scales: tiles stay 1024 apart)
+  static constexpr int kTurn = sizeof(T) * 32 * 32;             // a warp's results on their way out
+  static constexpr int kStages = (227 * 1024 - 1024 - 256 - kResultWarps * kTurn) / kStage;
+  static constexpr int kOffOut = kStages * kStage, kOffBars = kOffOut + kResultWarps * kTurn;
+  static constexpr int kBars = 2 * kStages + 7;
+  static constexpr int kDynamic = kOffBars + kBars * 8 + 16 + 1024;  // the tiles are aligned to 1024 bytes
+  static constexpr int kScaleCols = kGroups * 12;                    // of tensor memory: 4 of A, 8 of B a group
+  static constexpr int kScaleSets = 64 / kScaleCols;
+};
+static_assert(ProductCfg<SPARSP_MXFP4, float>::kStage % 1024 == 0 && ProductCfg<SPARSP_NVFP4, float>::kStage % 1024 == 0, "");
+constexpr int kAccStep = 192, kScaleAt = 448;  // columns of tensor memory: accumulators at 0 and 192, then scales
+
+// Instruction descriptor: e2m1 operands, both K-major; bit 23 says that scales are powers of two.
+static uint32_t fp4_instruction(int format, int M, int N) {
+  return (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((format == SPARSP_MXFP4 ? 1u : 0u) << 23) |
+         ((uint32_t)(M >> 4) << 24);
+}
+
+// 32 rows x 32 columns of a warp, on their way out through its own shared memory (16-byte pieces of a row in turned
+// places, so that lanes do not meet in a bank) as one TMA tile, which leaves out what lies beyond the tensor.
+template <typename T>
+__device__ __forceinline__ void write_out(const CUtensorMap* to, uint8_t* mine, const float (&x)[32], int lane, int col,
+                                          int row, int cols, int rows) {
+  constexpr int kPieces = sizeof(T) * 2, kEach = 32 / kPieces;
+  Vec<T, kEach> piece[kPieces];
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) piece[i].set(x + i * kEach);
+  if (lane == 0) ptx::tma_store_wait_read();
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < kPieces; ++i) {
+    const int at = sizeof(T) == 4 ? i ^ (lane & 7) : i ^ ((lane >> 1) & 3);
+    store_vec<T, kEach>(reinterpret_cast<T*>(mine + lane * (32 * sizeof(T)) + at * 16), piece[i]);
+  }
+  ptx::fence_proxy_async_smem();
+  __syncwarp();
+  if (lane == 0 && col < cols && row < rows) {
+    ptx::tma_store_2d(to, mine, col, row);
+    ptx::tma_store_commit();
+  }
+}
+
+// x * factor + bias of 32 columns; columns past the last, of which there are multiples of 8, stay as they are
+template <typename T>
+__device__ __forceinline__ void finish(float (&x)[32], float factor, const T* bias, int col, int cols) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (bias != nullptr && col + i * 8 < cols) {
+      Eight<T> b;
+      b.load(bias + col + i * 8);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[8 * i + e] = fmaf(x[8 * i + e], factor, b[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[8 * i + e] *= factor;
+    }
+  }
+}
+
+template <typename T, int kFormat>
+__global__ void __launch_bounds__(kProductThreads, 1)
+    product_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
+                   const __grid_constant__ CUtensorMap msa, const __grid_constant__ CUtensorMap msb,
+                   const __grid_constant__ CUtensorMap mc, const ProductParams p) {
+  using namespace ptx;
+  using C = ProductCfg<kFormat, T>;
+  extern __shared__ uint8_t dynamic[];
+  uint8_t* smem = dynamic + ((1024 - (smem_u32(dynamic) & 1023)) & 1023);
+  uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::kOffBars);  // of the even CTA: both CTAs' tiles have arrived
+  uint64_t* empty = full + C::kStages;                               // the stage has been multiplied
+  uint64_t* acc_full = empty + C::kStages;                           // [2]
+  uint64_t* acc_read = acc_full + 2;                                 // [2] of the even CTA: both have read all of theirs
+  uint64_t* shared_read = acc_read + 2;  // [2] ... the 64 columns that this accumulator shares with the other
+  uint64_t* drained = shared_read + 2;   // every product has ended
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(tmem_slot + 1);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_rank();
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::kStages; ++s) {
+      mbar_init(full + s, 1);
+      mbar_init(empty + s, 1);
+    }
+    for (int a = 0; a < 2; ++a) {
+      mbar_init(acc_full + a, 1);
+      mbar_init(acc_read + a, 2 * kResultWarps);
+      mbar_init(shared_read + a, 2 * 4);
+    }
+    mbar_init(drained, 1);
+    *s_abort = 0;
+    mbar_init_fence();
+  }
+  if (warp == kResultWarps + 1) {
+    tmem_alloc_pair(tmem_slot, 512);
+    tmem_relinquish_pair();
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  enter_grid();  // (the next launch may begin: tensor memory is ours, so its CTAs cannot have taken it before)
+
+  const int tiles = p.m_tiles * p.n_tiles, pairs = gridDim.x >> 1;
+  auto tile_at = [&](int tile, int& m, int& n) {
+    const int per_band = p.band * p.n_tiles, b = tile / per_band, in = tile - b * per_band;
+    const int height = min(p.band, p.m_tiles - b * p.band);
+    n = in / height;
+    m = b * p.band + in - n * height;
+  };
+
+  if (warp == kResultWarps) {
+    // ---- loads ----
+    if (elect_one()) {
+      int s = 0;
+      uint32_t round = 0;
+      for (int tile = blockIdx.x >> 1; tile < tiles && !*s_abort; tile += pairs) {
+        int m, n;
+        tile_at(tile, m, n);
+        for (int k = 0; k < p.k_blocks; ++k) {
+          mbar_wait_bounded_inline(empty + s, round ^ 1u, s_abort, 21, p.wait_limit);
+          if (*s_abort) break;
+          if (rank == 0) mbar_expect_tx(full + s, 2 * C::kStage);
+          uint8_t* at = smem + s * C::kStage;
+          const uint32_t bar = cluster_addr(full + s, 0);
+          tma_load_pair(at, &ma, bar, k * 128, (m * 2 + (int)rank) * kRows);
+          tma_load_pair(at + C::kA, &mb, bar, k * 128, (n * 2 + (int)rank) * kRows);
+          tma_load_pair_3d(at + C::kA + C::kB, &msa, bar, 0, k * C::kGroups, m * 2 + (int)rank);
+          tma_load_pair_3d(at + C::kA + C::kB + C::kScalesA, &msb, bar, 0, k * C::kGroups, n * 2);
+          if (++s == C::kStages) {
+            s = 0;
+            round ^= 1u;
+          }
+        }
+      }
+      if (*s_abort && rank == 0) {  // copies still in flight are waited for, within the same limit
+        const long long t0 = clock64();
+        for (int q = 0; q < C::kStages; ++q) {
+          const uint32_t phase = q < s ? round : round ^ 1u;
+          while (!mbar_try_wait(full + q, phase) && clock64() - t0 < p.wait_limit) {
+          }
+        }
+      }
+    }
+  } else if (warp == kResultWarps + 1) {
+    // ---- products, for both CTAs ----
+    if (rank == 0 && elect_one()) {
+      const uint32_t base = smem_u32(smem);
+      const uint64_t da = make_smem_desc(base, 16u, 1024u), db = make_smem_desc(base + C::kA, 16u, 1024u);
+      const uint64_t dsa = make_scale_desc(base + C::kA + C::kB), dsb = make_scale_desc(base + C::kA + C::kB + C::kScalesA);
+      int s = 0, acc = 0, set = 0;
+      uint32_t round = 0, acc_round = 0;
+      for (int tile = blockIdx.x >> 1; tile < tiles && !*s_abort; tile += pairs) {
+        // this accumulator's last tile has been read, and of the other's, which is read now, what the two share
+        mbar_wait_bounded_inline(acc_read + acc, acc_round ^ 1u, s_abort, 22, p.wait_limit);
+        mbar_wait_bounded_inline(shared_read + (acc ^ 1), acc == 0 ? acc_round ^ 1u : acc_round, s_abort, 23, p.wait_limit);
+        tc_fence_after();
+        for (int k = 0; k < p.k_blocks; ++k) {
+          if (!mbar_wait_bounded_inline(full + s, round, s_abort, 24, p.wait_limit)) break;
+          tc_fence_after();
+          const uint64_t off = (uint64_t)((s * C::kStage) >> 4);
+          const uint32_t sa = tmem + kScaleAt + set * C::kScaleCols, sb = sa + 4 * C::kGroups;
+#pragma unroll
+          for (int g = 0; g < C::kGroups; ++g) {
+            copy_scales_pair(sa + 4 * g, dsa + off + g * 32);
+            copy_scales_pair(sb + 8 * g, dsb + off + g * 32);
+            copy_scales_pair(sb + 8 * g + 4, dsb + off + (C::kGroups + g) * 32);
+          }
+          const int steps = min(4, (p.depth - k * kDeep + 63) / 64);
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            if (kk >= steps) break;
+            const int g = kk * C::kGroups / 4;
+            // MXFP4: a group of four blocks serves two instructions, the second half of it the second
+            const uint32_t half = C::kGroups == 2 && (kk & 1) ? (2u << 4) | (2u << 29) : 0u;
+            mma_fp4_pair<kFormat == SPARSP_MXFP4>(tmem + acc * kAccStep, da + off + kk * 2, db + off + kk * 2, p.idesc | half,
+                                                  sa + 4 * g, sb + 8 * g, k > 0 || kk > 0);
+          }
+          mma_commit_pair(empty + s);
+          set = set + 1 == C::kScaleSets ? 0 : set + 1;
+          if (++s == C::kStages) {
+            s = 0;
+            round ^= 1u;
+          }
+        }
+        mma_commit_pair(acc_full + acc);
+        acc ^= 1;
+        if (acc == 0) acc_round ^= 1u;
+      }
+      mma_commit_pair(drained);
+    }
+  } else {
+    // ---- results: warp w has the lanes of quarter w % 4, and 64 columns ----
+    const int quarter = warp & 3, side = warp >> 2;
+    uint8_t* mine = smem + C::kOffOut + warp * C::kTurn;
+    int acc = 1;
+    uint32_t acc_round = 1;
+    for (int tile = blockIdx.x >> 1; tile < tiles; tile += pairs) {
+      acc ^= 1;
+      if (acc == 0) acc_round ^= 1u;
+      int m, n;
+      tile_at(tile, m, n);
+      mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 25, p.wait_limit);
+      if (__any_sync(0xffffffffu, *s_abort != 0)) break;  // (the same for all lanes)
+      tc_fence_after();
+      const uint32_t from = tmem + acc * kAccStep + side * 64 + ((uint32_t)(quarter * 32) << 16);
+      float x[32], y[32];
+      tmem_ld32(from, reinterpret_cast<uint32_t*>(x));
+      tmem_ld32(from + 32, reinterpret_cast<uint32_t*>(y));
+      tmem_ld_wait(x);
+      tmem_ld_wait(y);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) {
+        if (side == (acc == 0 ? 3 : 0)) mbar_arrive_cluster(cluster_addr(shared_read + acc, 0));
+        mbar_arrive_cluster(cluster_addr(acc_read + acc, 0));
+      }
+      const int row = (m * 2 + (int)rank) * kRows + quarter * 32, col = n * 256 + side * 64;
+      finish(x, p.factor, static_cast<const T*>(p.bias), col, p.cols);
+      write_out<T>(&mc, mine, x, lane, col, row, p.cols, p.rows);
+      finish(y, p.factor, static_cast<const T*>(p.bias), col + 32, p.cols);
+      write_out<T>(&mc, mine, y, lane, col + 32, row, p.cols, p.rows);
+    }
+    if (lane == 0) tma_store_wait();
+  }
+  __syncwarp();
+  tc_fence_before();
+  __syncthreads();
+  // Products use both CTAs' memory until they have ended: after a wait that ran out nobody else has waited for them.
+  if (warp == kResultWarps + 1 && elect_one()) {
+    const long long t0 = clock64();
+    while (!mbar_try_wait(drained, 0) && clock64() - t0 < p.wait_limit) {
+    }
+  }
+  __syncwarp();
+  cluster_sync();  // the other CTA's arrivals and products here have ended
+  if (warp == kResultWarps + 1) {
+    tc_fence_after();
+    tmem_dealloc_pair(tmem, 512);
+  }
+  if (threadIdx.x == 0) report_abort(s_abort, p.status);
+}
+
+// [rows][bytes] in boxes of 128 bytes x 128 rows, swizzled
+static int make_codes_map(CUtensorMap* out, const void* base, int64_t rows, int64_t bytes, int box_rows) {
+  const cuuint64_t dims[2] = {(cuuint64_t)bytes, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)bytes};
+  const cuuint32_t box[2] = {128, (cuuint32_t)box_rows};
+  return encode_tmap(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
+}
+// scales: [tiles of 128 rows][groups][512 bytes] in boxes of some groups of some tiles
+static int make_scales_map(CUtensorMap* out, const void* base, int64_t rows, int64_t groups, int box_groups, int box_tiles) {
+  const cuuint64_t dims[3] = {128, (cuuint64_t)groups, (cuuint64_t)((rows + 127) / 128)};
+  const cuuint64_t strides[2] = {512, (cuuint64_t)groups * 512};
+  const cuuint32_t box[3] = {128, (cuuint32_t)box_groups, (cuuint32_t)box_tiles};
+  return encode_tmap(out, CU_TENSOR_MAP_DATA_TYPE_UINT32, 3, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+static int make_result_map(CUtensorMap* out, int dtype, const void* base, int64_t rows, int64_t cols, int64_t ld) {
+  const int e = element_bytes(dtype);
+  const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * e};
+  const cuuint32_t box[2] = {32, 32};
+  return encode_tmap(out,
+                     dtype == SPARSP_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                     : dtype == SPARSP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                            : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                     2, base, dims, strides, box, e == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+}
+
+int64_t fp4_product_workspace_bytes(const sparsp_fp4_gemm&) { return kStatusWords * 4; }
+
+template <typename T, int kFormat>
+static int launch_pairs(const sparsp_fp4_gemm& f, const void* A, const void* As, const void* B, const void* Bs,
+                        const void* bias, void* C, char* ws, cudaStream_t st) {
+  using Cfg = ProductCfg<kFormat, T>;
+  const int64_t groups = fp4_groups(f.depth, kFormat);
+  CUtensorMap ma, mb, msa, msb, mc;
+  int rc;
+  if ((rc = make_codes_map(&ma, A, f.rows, f.depth / 2, kRows)) != SPARSP_OK) return rc;
+  if ((rc = make_codes_map(&mb, B, f.cols, f.depth / 2, kRows)) != SPARSP_OK) return rc;
+  if ((rc = make_scales_map(&msa, As, f.rows, groups, Cfg::kGroups, 1)) != SPARSP_OK) return rc;
+  if ((rc = make_scales_map(&msb, Bs, f.cols, groups, Cfg::kGroups, 2)) != SPARSP_OK) return rc;
+  if ((rc = make_result_map(&mc, f.dtype, C, f.rows, f.cols, f.stride_c)) != SPARSP_OK) return rc;
+  ProductParams p = {};
+  p.bias = bias;
+  p.rows = (int32_t)f.rows;
+  p.cols = f.cols;
+  p.depth = f.depth;
+  p.m_tiles = ceil_div(f.rows, 256);
+  p.n_tiles = ceil_div(f.cols, 256);
+  p.band = 8;
+  p.k_blocks = ceil_div(f.depth, kDeep);
+  p.factor = std::ldexp(1.0f, f.exponent);
+  p.idesc = fp4_instruction(kFormat, 256, 256);
+  p.status = reinterpret_cast<int32_t*>(ws);
+  p.wait_limit = kWaitLimit;
+  auto kern = product_kernel<T, kFormat>;
+  SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, Cfg::kDynamic));
+  const unsigned grid = 2u * (unsigned)std::min(p.m_tiles * p.n_tiles, kPairs);
+  SPARSP_CUDA_OK(launch_clusters(kern, dim3(grid), 2, kProductThreads, Cfg::kDynamic, st, ma, mb, msa, msb, mc, p));
+  return SPARSP_OK;
+}
+
+int launch_fp4_product(const sparsp_fp4_gemm& f, const void* A, const void* As, const void* B, const void* Bs,
+                       const void* bias, void* C, char* ws, cudaStream_t st) {
+  if ((int64_t)ceil_div(f.rows, 256) * ceil_div(f.cols, 256) > (1 << 30)) {
+    set_error("%d x %d tiles are too many", ceil_div(f.rows, 256), ceil_div(f.cols, 256));
+    return SPARSP_ERR_UNSUPPORTED;
+  }
+  SPARSP_WITH_TYPE(f.dtype, T, {
+    return f.format == SPARSP_MXFP4 ? launch_pairs<T, SPARSP_MXFP4>(f, A, As, B, Bs, bias, C, ws, st)
+                                    : launch_pairs<T, SPARSP_NVFP4>(f, A, As, B, Bs, bias, C, ws, st);
+  });
+}
+
+}  // namespace sparsp

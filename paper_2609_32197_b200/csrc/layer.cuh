@@ -171,4 +171,11 @@ int launch_ffn_fwd(const sparsp_ffn& f, const void* X, const void* Wg, const voi
 int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const void* Wg, const void* Wu,
                    const void* gate, const void* up, void* dX, void* dWg, void* dWu, char* ws, cudaStream_t st);
 
+int64_t fp4_scales_bytes(const sparsp_fp4& f);
+int launch_fp4_quantize(const sparsp_fp4& f, const void* X, uint8_t* codes, uint8_t* scales, void* values,
+                        cudaStream_t st);
+int64_t fp4_product_workspace_bytes(const sparsp_fp4_gemm& f);
+int launch_fp4_product(const sparsp_fp4_gemm& f, const void* A, const void* As, const void* B, const void* Bs,
+                       const void* bias, void* C, char* ws, cudaStream_t st);
+
 }  // namespace sparsp

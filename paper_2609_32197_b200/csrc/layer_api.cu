@@ -100,6 +100,47 @@ int check_ffn(const sparsp_ffn* f) {
   return SPARSP_OK;
 }
 
+// ---- 4-bit operands ----
+int check_format(int32_t format, int32_t exponent, int32_t most) {
+  if (format != SPARSP_MXFP4 && format != SPARSP_NVFP4) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "unknown format %d", format);
+  if (exponent < -most || exponent > most)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "exponent %d outside -%d .. %d", exponent, most, most);
+  if (format == SPARSP_MXFP4 && exponent != 0)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "exponent %d: the scales of this format need none", exponent);
+  return SPARSP_OK;
+}
+
+int check_fp4(const sparsp_fp4* f) {
+  if (!f) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "fp4 is NULL");
+  if (f->dtype < SPARSP_BF16 || f->dtype > SPARSP_FP32)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "unknown dtype %d", f->dtype);
+  SPARSP_TRY(check_format(f->format, f->exponent, 100));
+  if (f->rows < 0 || f->cols < 1) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "rows or cols is negative or zero");
+  if (f->cols % 32) SPARSP_REFUSE(SPARSP_ERR_UNSUPPORTED, "cols %d must be a multiple of 32", f->cols);
+  if (f->cols > (1 << 28)) SPARSP_REFUSE(SPARSP_ERR_UNSUPPORTED, "cols above 2^28");
+  if (f->rows > 0x7fffff00LL) SPARSP_REFUSE(SPARSP_ERR_UNSUPPORTED, "%lld rows are too many", (long long)f->rows);
+  if (f->stride_x < f->cols || f->stride_x % 8)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "stride_x must be a multiple of 8 elements and not less than a row");
+  return SPARSP_OK;
+}
+
+int check_fp4_gemm(const sparsp_fp4_gemm* f) {
+  if (!f) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "product is NULL");
+  if (f->dtype < SPARSP_BF16 || f->dtype > SPARSP_FP32)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "unknown dtype %d", f->dtype);
+  SPARSP_TRY(check_format(f->format, f->exponent, 126));
+  if (f->rows < 0 || f->cols < 1 || f->depth < 1)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "rows, cols or depth is negative or zero");
+  if (f->rows > 0x7fffff00LL) SPARSP_REFUSE(SPARSP_ERR_UNSUPPORTED, "%lld rows are too many", (long long)f->rows);
+  if (f->cols % 8 || f->depth % 32)
+    SPARSP_REFUSE(SPARSP_ERR_UNSUPPORTED, "cols %d must be a multiple of 8, depth %d of 32", f->cols, f->depth);
+  if (f->cols > (1 << 28) || f->depth > (1 << 28)) SPARSP_REFUSE(SPARSP_ERR_UNSUPPORTED, "cols or depth above 2^28");
+  if (f->stride_c < f->cols || f->stride_c % 8)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "stride_c must be a multiple of 8 elements and not less than a row");
+  if (f->stride_c > (1LL << 37)) SPARSP_REFUSE(SPARSP_ERR_UNSUPPORTED, "stride_c is above 2^37 elements");
+  return SPARSP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -300,6 +341,46 @@ int sparsp_gated_ffn_bwd(const sparsp_ffn* ffn, const void* dH, const void* X, c
     SPARSP_TRY(apart({dX, dWgate, dWup}, {dWgate ? X : nullptr, dX ? Wgate : nullptr, dX ? Wup : nullptr}));
   }
   return launch_ffn_bwd(*ffn, dH, X, Wgate, Wup, gate, up, dX, dWgate, dWup, (char*)workspace, (cudaStream_t)stream);
+}
+
+int sparsp_fp4_scales_bytes(const sparsp_fp4* fp4, int64_t* bytes) {
+  SPARSP_TRY(check_fp4(fp4));
+  if (!bytes) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = fp4_scales_bytes(*fp4);
+  return SPARSP_OK;
+}
+
+int sparsp_fp4_quantize(const sparsp_fp4* fp4, const void* X, void* codes, void* scales, void* values, void* stream) {
+  SPARSP_TRY(check_fp4(fp4));
+  if (fp4->rows == 0) return SPARSP_OK;
+  SPARSP_TRY(need(X, "X", 16));
+  SPARSP_TRY(need(codes, "codes", 16));
+  SPARSP_TRY(need(scales, "scales", 16));
+  SPARSP_TRY(optional(values, "values", 16));
+  SPARSP_TRY(apart({codes, scales}, {X, values}));
+  return launch_fp4_quantize(*fp4, X, (uint8_t*)codes, (uint8_t*)scales, values, (cudaStream_t)stream);
+}
+
+int sparsp_fp4_product_workspace_bytes(const sparsp_fp4_gemm* product, int64_t* bytes) {
+  SPARSP_TRY(check_fp4_gemm(product));
+  if (!bytes) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = fp4_product_workspace_bytes(*product);
+  return SPARSP_OK;
+}
+
+int sparsp_fp4_product(const sparsp_fp4_gemm* product, const void* A, const void* A_scales, const void* B,
+                       const void* B_scales, const void* bias, void* C, void* workspace, void* stream) {
+  SPARSP_TRY(check_fp4_gemm(product));
+  if (product->rows == 0) return SPARSP_OK;
+  SPARSP_TRY(need(A, "A", 16));
+  SPARSP_TRY(need(A_scales, "A_scales", 16));
+  SPARSP_TRY(need(B, "B", 16));
+  SPARSP_TRY(need(B_scales, "B_scales", 16));
+  SPARSP_TRY(optional(bias, "bias", 16));
+  SPARSP_TRY(need(C, "C", 16));
+  SPARSP_TRY(need(workspace, "workspace", 256));
+  SPARSP_TRY(apart({C}, {A, A_scales, B, B_scales, bias}));
+  return launch_fp4_product(*product, A, A_scales, B, B_scales, bias, C, (char*)workspace, (cudaStream_t)stream);
 }
 
 }  // extern "C"
