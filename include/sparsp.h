@@ -530,6 +530,60 @@ SPARSP_API int sparsp_gated_ffn_bwd(const sparsp_ffn* ffn, const void* dH, const
                                     const void* Wup, const void* gate, const void* up, void* dX, void* dWgate,
                                     void* dWup, void* workspace, void* stream);
 
+/* The residual step between two blocks of a layer, over rows of `dim` values:
+ *   u = norm_y(y) * weight_y + bias_y, or y itself where norm_y is SPARSP_NORM_NONE
+ *   r = x + gate * u                                the new residual stream
+ *   n = norm_r(r) * weight_r + bias_r               what the next block takes, unless norm_r is SPARSP_NORM_NONE
+ * Rows are in groups of rows_per_group (the last may be smaller); gate, weight_r and bias_r are [groups][dim] (what a
+ * conditioning network gives each sequence: weight_r = 1 + scale), weight_y and bias_y [dim], of the layer. */
+#define SPARSP_NORM_NONE 0
+#define SPARSP_NORM_LAYER 1 /* (v - mean) / sqrt(mean of (v - mean)^2 + eps) */
+#define SPARSP_NORM_RMS 2   /* v / sqrt(mean of v^2 + eps) */
+typedef struct sparsp_gated_norm {
+  int64_t rows;           /* 0 is allowed */
+  int64_t rows_per_group; /* 0 = all rows in one group */
+  int64_t stride_x;       /* elements from row to row of X, R, dR and dX: a multiple of 8, >= dim */
+  int64_t stride_y;       /* of Y and dY */
+  int64_t stride_n;       /* of N and dN */
+  int32_t dim;            /* a multiple of 8, at most 8192 */
+  int32_t dtype;          /* of all tensors of rows */
+  int32_t weight_dtype;   /* of gate and all weights, biases and their gradients: dtype or SPARSP_FP32 */
+  int32_t norm_y, norm_r; /* SPARSP_NORM_* */
+  float eps;              /* >= 0, of both norms */
+} sparsp_gated_norm;
+
+/* Forward.  n is computed from the unrounded r.
+ *   X, Y         in   [rows][dim]
+ *   gate, weight_y, bias_y, weight_r, bias_r   in   each may be NULL (1 for gate and weights, 0 for biases); weight_y and
+ *                     bias_y belong to norm_y, weight_r and bias_r to norm_r: without it they are refused
+ *   R            out  may be X itself
+ *   N            out  NULL without norm_r, otherwise not; may be Y itself when the strides are equal
+ *   stats_y, stats_r  out  fp32 [rows][2]: mean (0 for an rms norm) and 1 / deviation, for the backward pass; each may be
+ *                     NULL, and is without its norm
+ * Data pointers are 16-byte aligned, those of statistics 8-byte. */
+SPARSP_API int sparsp_gated_norm_fwd(const sparsp_gated_norm* step, const void* X, const void* Y, const void* gate,
+                                     const void* weight_y, const void* bias_y, const void* weight_r, const void* bias_r,
+                                     void* R, void* N, float* stats_y, float* stats_r, void* stream);
+
+/* Bytes of workspace that the backward pass needs (partial sums of the weights' gradients).  More rows, all else equal,
+ * never need less. */
+SPARSP_API int sparsp_gated_norm_workspace_bytes(const sparsp_gated_norm* step, int64_t* bytes);
+
+/* Backward, for dN at N and dR at R (what the residual stream brings back; NULL = nothing):
+ *   dX = dR + the gradient through norm_r;  dY = gate * dX, through norm_y
+ *   dgate, dweight_r, dbias_r [groups][dim]: sums over a group's rows;  dweight_y, dbias_y [dim]: over all rows
+ *   dN, R, stats_r  in   NULL without norm_r
+ *   stats_y         in   NULL without norm_y
+ *   dX, dY          out  each may be NULL (not wanted); dX may be dR itself
+ *   dgate, dweight_y, dbias_y, dweight_r, dbias_r   out  each may be NULL; those of a norm that is not there have to be.
+ *                        Without rows dweight_y and dbias_y are zero
+ *   workspace       in   sparsp_gated_norm_workspace_bytes() bytes, 256-byte aligned */
+SPARSP_API int sparsp_gated_norm_bwd(const sparsp_gated_norm* step, const void* dN, const void* dR, const void* R,
+                                     const void* Y, const void* gate, const void* weight_y, const void* bias_y,
+                                     const void* weight_r, const float* stats_y, const float* stats_r, void* dX, void* dY,
+                                     void* dgate, void* dweight_y, void* dbias_y, void* dweight_r, void* dbias_r,
+                                     void* workspace, void* stream);
+
 /* 4-bit operands: a value is e2m1 (0, 0.5, 1, 1.5, 2, 3, 4, 6, either sign) times the scale of its block, a run of a row's
  * values, times 2^exponent for the whole matrix.
  *   SPARSP_MXFP4  blocks of 32; a scale is a power of two (its exponent + 127 in 8 bits): the least with which the block's
@@ -588,6 +642,33 @@ SPARSP_API int sparsp_fp4_product_workspace_bytes(const sparsp_fp4_gemm* product
  * All pointers but the workspace are 16-byte aligned. */
 SPARSP_API int sparsp_fp4_product(const sparsp_fp4_gemm* product, const void* A, const void* A_scales, const void* B,
                                   const void* B_scales, const void* bias, void* C, void* workspace, void* stream);
+
+/* A list of gradients (arrays in HOST memory, of addresses in DEVICE memory; read before a call returns). */
+typedef struct sparsp_grad_list {
+  int32_t count;             /* 0 is allowed */
+  int32_t dtype;             /* of all of them; lists of several types: see sparsp_grad_squares */
+  const void* const* grads;  /* [count], aligned to their element type; NULL for one of size 0 */
+  void* const* outs;         /* [count]: where the clipped gradients go; NULL = in place.  Each may be its gradient, otherwise
+                              * none overlaps a gradient or another */
+  const int64_t* sizes;      /* [count] elements of each, >= 0 */
+} sparsp_grad_list;
+
+/* Bytes of workspace that both calls need, whatever the list.  The first 256 bytes are zero before the first call. */
+SPARSP_API int sparsp_grad_workspace_bytes(int64_t* bytes);
+
+/* The sum of the squares of all values, as a double at byte 256 of the workspace; accumulate != 0: added to what is there
+ * (lists of several types that share one norm).  Where gradients are spread over ranks, the ranks' sums are added there
+ * (an all-reduce of one double) before sparsp_grad_clip.  Added in fp64, and in fp32 over 32 values at most, wherever
+ * those are in fp32's range. */
+SPARSP_API int sparsp_grad_squares(const sparsp_grad_list* list, int32_t accumulate, void* workspace, void* stream);
+
+/* norm = sqrt(the sum at byte 256);  gradients times min(1, max_norm / (norm + 1e-6)), rounded once.  A norm that is not
+ * finite changes nothing (the caller sees it in `norm`), nor does one under the limit: in place, gradients are not read
+ * then.
+ *   max_norm   > 0; infinity only computes the norm
+ *   norm  out  fp32 [1] DEVICE; may be NULL */
+SPARSP_API int sparsp_grad_clip(const sparsp_grad_list* list, double max_norm, float* norm, void* workspace,
+                                void* stream);
 
 /* Synchronises `stream` and returns the workspace's status word in *code (SPARSP_OK if no kernel
  * reported a problem since the last reset), then resets it. */

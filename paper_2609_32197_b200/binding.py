@@ -37,6 +37,8 @@ EXPORTS = [
     "sparsp_rotary_frequencies", "sparsp_rotary_table_bytes", "sparsp_rotary_table", "sparsp_rotary_apply",
     "sparsp_layer_norm_fwd", "sparsp_layer_norm_workspace_bytes", "sparsp_layer_norm_bwd",
     "sparsp_gated_ffn_workspace_bytes", "sparsp_gated_ffn_fwd", "sparsp_gated_ffn_bwd",
+    "sparsp_gated_norm_fwd", "sparsp_gated_norm_workspace_bytes", "sparsp_gated_norm_bwd",
+    "sparsp_grad_workspace_bytes", "sparsp_grad_squares", "sparsp_grad_clip",
     "sparsp_fp4_scales_bytes", "sparsp_fp4_quantize", "sparsp_fp4_product_workspace_bytes", "sparsp_fp4_product",
 ]
 SPARSP_XCHG_HOST_MEMORY = 1
@@ -45,10 +47,11 @@ DTYPES = {torch.bfloat16: SPARSP_BF16, torch.float16: SPARSP_FP16, torch.float32
 PAIRINGS = {"interleaved": 0, "half": 1}
 SCALINGS = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}
 ACTIVATIONS = {"silu": 0, "gelu_tanh": 1, "gelu": 2}
+NORMS = {"none": 0, "layer": 1, "rms": 2}
 FP4_FORMATS = {"mxfp4": 0, "nvfp4": 1}
 
-# Argument types of the calls that a layer makes (s: shape, r / n / m / q / g: description of rotary positions, a
-# norm, a feed-forward, a 4-bit operand or a product of two, p: pointer, i / l: 32 / 64-bit integer, f / d: 32 / 64-bit float), so that ctypes
+# Argument types of the calls that a layer makes (s: shape, r / n / m / e / t / q / g: description of rotary
+# positions, a norm, a feed-forward, a residual step, a list of gradients, a 4-bit operand or a product of two, p: pointer, i / l: 32 / 64-bit integer, f / d: 32 / 64-bit float), so that ctypes
 # converts plain values itself: a ctypes object per argument costs more than the call.
 _SIGNATURES = {
     "sparsp_block_mask": "sppippppppp",
@@ -72,6 +75,12 @@ _SIGNATURES = {
     "sparsp_gated_ffn_workspace_bytes": "mip",
     "sparsp_gated_ffn_fwd": "mpppppppp",
     "sparsp_gated_ffn_bwd": "mppppppppppp",
+    "sparsp_gated_norm_fwd": "e" + 12 * "p",
+    "sparsp_gated_norm_workspace_bytes": "ep",
+    "sparsp_gated_norm_bwd": "e" + 19 * "p",
+    "sparsp_grad_workspace_bytes": "p",
+    "sparsp_grad_squares": "tipp",
+    "sparsp_grad_clip": "tdppp",
     "sparsp_fp4_scales_bytes": "qp",
     "sparsp_fp4_quantize": "qppppp",
     "sparsp_fp4_product_workspace_bytes": "gp",
@@ -110,6 +119,18 @@ class sparsp_ffn(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32)]
 
 
+class sparsp_gated_norm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("rows_per_group", ctypes.c_int64), ("stride_x", ctypes.c_int64),
+                ("stride_y", ctypes.c_int64), ("stride_n", ctypes.c_int64), ("dim", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32), ("norm_y", ctypes.c_int32),
+                ("norm_r", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class sparsp_grad_list(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int32), ("dtype", ctypes.c_int32), ("grads", ctypes.c_void_p),
+                ("outs", ctypes.c_void_p), ("sizes", ctypes.c_void_p)]
+
+
 class sparsp_fp4(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("stride_x", ctypes.c_int64), ("cols", ctypes.c_int32),
                 ("format", ctypes.c_int32), ("exponent", ctypes.c_int32), ("dtype", ctypes.c_int32)]
@@ -145,7 +166,7 @@ def lib() -> ctypes.CDLL:
             getattr(L, name)  # AttributeError if a declared symbol is not exported
         kinds = {"s": ctypes.POINTER(sparsp_shape), "r": ctypes.POINTER(sparsp_rotary),
                  "n": ctypes.POINTER(sparsp_norm), "m": ctypes.POINTER(sparsp_ffn),
-                 "q": ctypes.POINTER(sparsp_fp4), "g": ctypes.POINTER(sparsp_fp4_gemm), "p": ctypes.c_void_p,
+                 "e": ctypes.POINTER(sparsp_gated_norm), "t": ctypes.POINTER(sparsp_grad_list), "q": ctypes.POINTER(sparsp_fp4), "g": ctypes.POINTER(sparsp_fp4_gemm), "p": ctypes.c_void_p,
                  "i": ctypes.c_int32, "l": ctypes.c_int64, "f": ctypes.c_float, "d": ctypes.c_double}
         for name, args in _SIGNATURES.items():
             getattr(L, name).argtypes = [kinds[a] for a in args]
@@ -561,6 +582,86 @@ def sparsp_gated_ffn_fwd(ffn, X, Wgate, Wup, H, gate, up, workspace):
 def sparsp_gated_ffn_bwd(ffn, dH, X, Wgate, Wup, gate, up, dX, dWgate, dWup, workspace):
     _check(lib().sparsp_gated_ffn_bwd(ffn, _data(dH), _data(X), _data(Wgate), _data(Wup), _data(gate), _data(up),
                                       _data(dX), _data(dWgate), _data(dWup), _data(workspace), _stream_handle()))
+
+
+# ---- the residual step between two blocks ----
+def make_gated_norm(rows: int, dim: int, rows_per_group: int = 0, norm_y: str = "none", norm_r: str = "layer",
+                    eps: float = 1e-5, dtype=torch.bfloat16, weight_dtype=None, stride_x: int = 0, stride_y: int = 0,
+                    stride_n: int = 0) -> sparsp_gated_norm:
+    """Strides of 0: contiguous rows.  weight_dtype None: dtype."""
+    return sparsp_gated_norm(rows, rows_per_group, stride_x or dim, stride_y or dim, stride_n or dim, dim, _dtype(dtype),
+                             _dtype(dtype if weight_dtype is None else weight_dtype), NORMS[norm_y], NORMS[norm_r], eps)
+
+
+def sparsp_gated_norm_fwd(step, X, Y, gate, weight_y, bias_y, weight_r, bias_r, R, N, stats_y, stats_r):
+    _check(lib().sparsp_gated_norm_fwd(step, _data(X), _data(Y), _data(gate), _data(weight_y), _data(bias_y),
+                                       _data(weight_r), _data(bias_r), _data(R), _data(N), _data(stats_y),
+                                       _data(stats_r), _stream_handle()))
+
+
+def sparsp_gated_norm_workspace_bytes(step: sparsp_gated_norm) -> int:
+    out = ctypes.c_int64()
+    _check(lib().sparsp_gated_norm_workspace_bytes(step, ctypes.addressof(out)))
+    return out.value
+
+
+def make_gated_norm_workspace(step: sparsp_gated_norm, device="cuda") -> torch.Tensor:
+    ws = torch.empty(sparsp_gated_norm_workspace_bytes(step), dtype=torch.uint8, device=device)
+    ws[:256].zero_()
+    return ws
+
+
+def sparsp_gated_norm_bwd(step, dN, dR, R, Y, gate, weight_y, bias_y, weight_r, stats_y, stats_r, dX, dY, dgate, dweight_y,
+                          dbias_y, dweight_r, dbias_r, workspace):
+    _check(lib().sparsp_gated_norm_bwd(step, _data(dN), _data(dR), _data(R), _data(Y), _data(gate), _data(weight_y),
+                                       _data(bias_y), _data(weight_r), _data(stats_y), _data(stats_r), _data(dX),
+                                       _data(dY), _data(dgate), _data(dweight_y), _data(dbias_y), _data(dweight_r),
+                                       _data(dbias_r), _data(workspace), _stream_handle()))
+
+
+# ---- the norm of a list of gradients, and clipping ----
+def make_grad_list(grads, outs=None) -> sparsp_grad_list:
+    """grads: contiguous tensors of one type; outs: where the clipped ones go, None = in place.  The list keeps them
+    alive."""
+    grads, outs = list(grads), None if outs is None else list(outs)
+    if not grads:
+        return sparsp_grad_list(0, SPARSP_BF16, None, None, None)
+    if outs is not None and len(outs) != len(grads):
+        raise ValueError(f"{len(outs)} outputs for {len(grads)} gradients")
+    for i, t in enumerate(grads + (outs or [])):
+        if t.dtype != grads[0].dtype or not t.is_contiguous() or t.numel() != grads[i % len(grads)].numel():
+            raise ValueError(f"gradient {i % len(grads)}: contiguous tensors of one type, an output as large as its gradient")
+    n = len(grads)
+    addresses = (ctypes.c_void_p * n)(*(t.data_ptr() for t in grads))
+    to = None if outs is None else (ctypes.c_void_p * n)(*(t.data_ptr() for t in outs))
+    sizes = (ctypes.c_int64 * n)(*(t.numel() for t in grads))
+    out = sparsp_grad_list(n, _dtype(grads[0].dtype), ctypes.addressof(addresses),
+                           None if to is None else ctypes.addressof(to), ctypes.addressof(sizes))
+    out.kept = (grads, outs, addresses, to, sizes)
+    return out
+
+
+def sparsp_grad_workspace_bytes() -> int:
+    out = ctypes.c_int64()
+    _check(lib().sparsp_grad_workspace_bytes(ctypes.addressof(out)))
+    return out.value
+
+
+def make_grad_workspace(device="cuda") -> torch.Tensor:
+    return torch.zeros(sparsp_grad_workspace_bytes(), dtype=torch.uint8, device=device)
+
+
+def grad_square_sum(workspace) -> torch.Tensor:
+    """The sum of squares in the workspace, float64 [1]: what ranks that share a norm add up."""
+    return workspace[256:264].view(torch.float64)
+
+
+def sparsp_grad_squares(grad_list, workspace, accumulate=False):
+    _check(lib().sparsp_grad_squares(grad_list, 1 if accumulate else 0, _data(workspace), _stream_handle()))
+
+
+def sparsp_grad_clip(grad_list, max_norm, norm, workspace):
+    _check(lib().sparsp_grad_clip(grad_list, max_norm, _data(norm), _data(workspace), _stream_handle()))
 
 
 # ---- 4-bit operands and their product ----

@@ -1,0 +1,290 @@
+// The norm over a list of gradients, and their clipping.
+//
+// The list travels in the kernel's parameters (up to kMostTensors a launch), so that nothing is copied to the device and
+// a call can be captured.  Tensors are cut into chunks of 16 KB; a CTA takes every G-th.  Squares are added in fp32 over
+// the 32 values at most that a thread has of a chunk, then in fp64, and CTAs' sums in their order by the one that ends
+// last: the same list gives the same bits.  Scaling goes through the chunks from the last to the first, so that what the
+// first pass read last is still in L2.
+//
+// Bound by HBM: every value is read once for the norm, and read again and written where the norm is over the limit.
+#include <algorithm>
+#include <cmath>
+#include <new>
+#include <utility>
+#include <vector>
+
+#include "layer.cuh"
+
+namespace sparsp {
+
+constexpr int kMostTensors = 1024;  // 28 KB of parameters, of 32 KB that a launch takes
+constexpr int kFewTensors = 64;
+constexpr int kChunkBytes = 16384;
+constexpr int kGradThreads = 256;
+constexpr int kGradCtas = 8 * kSms;
+
+struct GradTensor {
+  const void* from;
+  void* to;
+  int64_t size;
+};
+template <int kMost>
+struct GradTable {
+  GradTensor tensor[kMost];
+  int32_t first_chunk[kMost + 1];
+  int32_t count;
+};
+struct GradParams {
+  double* sum;
+  double* partial;  // of each CTA
+  uint32_t* ticket;
+  float* norm;
+  double limit;
+  int32_t begin, end;  // the first and the last launch of a list
+  int32_t accumulate, in_place;
+};
+
+// elements before the first 16-byte boundary
+template <typename T>
+__host__ __device__ inline int64_t ahead(const void* p, int64_t size) {
+  const int64_t n = (16 - (int64_t)((uintptr_t)p & 15)) / (int)sizeof(T) % (16 / (int)sizeof(T));
+  return n < size ? n : size;
+}
+
+// Chunk number c of the list: the elements [first, last) of a tensor.  Chunks are cut at 16-byte boundaries of where the
+// tensor is read; what lies before the first one belongs to the first chunk.
+template <typename T, int kMost>
+__device__ __forceinline__ GradTensor chunk_at(const GradTable<kMost>& t, int c, int64_t& first, int64_t& last) {
+  int lo = 0, hi = t.count;  // first_chunk[lo] <= c < first_chunk[hi]
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (t.first_chunk[mid] <= c)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  const GradTensor x = t.tensor[lo];
+  const int64_t skip = ahead<T>(x.from, x.size), k = c - t.first_chunk[lo];
+  constexpr int64_t kEach = kChunkBytes / sizeof(T);
+  first = k == 0 ? 0 : skip + k * kEach;
+  last = min(skip + (k + 1) * kEach, x.size);
+  return x;
+}
+
+// f(values, from index, how many) for what this thread has of the elements [first, last): 16-byte pieces where
+// `pieces`, single elements at the ends
+template <typename T, typename Piece, typename Single>
+__device__ __forceinline__ void walk_chunk(const T* from, int64_t first, int64_t last, bool pieces, Piece piece,
+                                           Single single) {
+  constexpr int E = 16 / sizeof(T), kMine = kChunkBytes / 16 / kGradThreads;
+  const int64_t at = first + ahead<T>(from + first, last - first);
+  if (!pieces) {
+    for (int64_t i = first + threadIdx.x; i < last; i += kGradThreads) single(i);
+    return;
+  }
+  if (first + threadIdx.x < at) single(first + threadIdx.x);
+  Vec<T, E> v[kMine];
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const int64_t i = at + (k * kGradThreads + threadIdx.x) * E;
+    if (i + E <= last)
+      v[k] = load_vec<T, E>(from + i);
+    else
+      v[k].clear();
+  }
+  piece(v, at);
+  const int64_t rest = at + (last - at) / E * E;
+  if (rest + threadIdx.x < last) single(rest + threadIdx.x);
+}
+
+__device__ __forceinline__ double block_sum(double v, double* room) {
+#pragma unroll
+  for (int d = 16; d > 0; d /= 2) v += __shfl_xor_sync(0xffffffffu, v, d);
+  if ((threadIdx.x & 31) == 0) room[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = 0.0;
+  for (int w = 0; w < kGradThreads / 32; ++w) v += room[w];
+  __syncthreads();
+  return v;
+}
+
+template <typename T, int kMost>
+__global__ void __launch_bounds__(kGradThreads)
+    grad_squares_kernel(const __grid_constant__ GradTable<kMost> table, GradParams p) {
+  enter_grid(p.partial, p.ticket);
+  __shared__ double room[kGradThreads / 32];
+  __shared__ bool s_last;
+  constexpr int E = 16 / sizeof(T);
+  const int chunks = table.first_chunk[table.count];
+  double sum = 0.0;
+  for (int c = blockIdx.x; c < chunks; c += gridDim.x) {
+    int64_t first, last;
+    const GradTensor x = chunk_at<T>(table, c, first, last);
+    const T* from = static_cast<const T*>(x.from);
+    walk_chunk(
+        from, first, last, true,
+        [&](const auto& v, int64_t) {
+          float s = 0.0f;
+#pragma unroll
+          for (const auto& w : v)
+#pragma unroll
+            for (int e = 0; e < E; ++e) s = fmaf(w[e], w[e], s);
+          // outside these, squares may have been lost below fp32's range or gone beyond it
+          if (s >= 0x1p-80f && s <= 0x1p100f) {
+            sum += (double)s;
+          } else {
+            for (const auto& w : v)
+#pragma unroll
+              for (int e = 0; e < E; ++e) sum += (double)w[e] * (double)w[e];
+          }
+        },
+        [&](int64_t i) {
+          const double v = to_float(from[i]);
+          sum += v * v;
+        });
+  }
+  sum = block_sum(sum, room);
+  if (threadIdx.x == 0) {
+    p.partial[blockIdx.x] = p.begin ? sum : p.partial[blockIdx.x] + sum;
+    __threadfence();
+    s_last = p.end && atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!s_last) return;
+  __threadfence();
+  sum = 0.0;
+  for (int i = threadIdx.x; i < gridDim.x; i += kGradThreads) sum += __ldcg(p.partial + i);
+  sum = block_sum(sum, room);
+  if (threadIdx.x == 0) {
+    *p.sum = p.accumulate ? *p.sum + sum : sum;
+    *p.ticket = 0;
+  }
+}
+
+template <typename T, int kMost>
+__global__ void __launch_bounds__(kGradThreads)
+    grad_clip_kernel(const __grid_constant__ GradTable<kMost> table, GradParams p) {
+  enter_grid(p.sum);
+  constexpr int E = 16 / sizeof(T);
+  const double norm = sqrt(*p.sum);
+  if (p.norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = (float)norm;
+  // (a norm that is not a number is no reason to change anything: the caller sees it)
+  const float factor = isfinite(norm) ? (float)fmin(p.limit / (norm + 1e-6), 1.0) : 1.0f;
+  if (factor == 1.0f && p.in_place) return;
+  const int chunks = table.first_chunk[table.count];
+  for (int c = chunks - 1 - blockIdx.x; c >= 0; c -= gridDim.x) {
+    int64_t first, last;
+    const GradTensor x = chunk_at<T>(table, c, first, last);
+    const T* from = static_cast<const T*>(x.from);
+    T* to = static_cast<T*>(x.to);
+    const bool pieces = (((uintptr_t)from ^ (uintptr_t)to) & 15) == 0;
+    walk_chunk(
+        from, first, last, pieces,
+        [&](auto& v, int64_t at) {
+#pragma unroll
+          for (int k = 0; k < kChunkBytes / 16 / kGradThreads; ++k) {
+            const int64_t i = at + (k * kGradThreads + threadIdx.x) * E;
+            if (i + E > last) continue;
+            float y[E];
+#pragma unroll
+            for (int e = 0; e < E; ++e) y[e] = v[k][e] * factor;
+            v[k].set(y);
+            store_vec<T, E>(to + i, v[k]);
+          }
+        },
+        [&](int64_t i) { to[i] = from_float<T>(to_float(from[i]) * factor); });
+  }
+}
+
+int64_t grad_workspace_bytes() { return 512 + kGradCtas * 8; }
+
+template <typename T, int kMost>
+static int launch_grad(const sparsp_grad_list& l, int from, int to, bool squares, GradParams p, cudaStream_t st) {
+  static thread_local GradTable<kMost> table;  // (28 KB: not on the stack)
+  table.count = 0;
+  int64_t chunks = 0;
+  for (int i = from; i < to; ++i) {
+    const int64_t n = l.sizes[i];
+    if (n == 0) continue;
+    table.tensor[table.count] = {l.grads[i], l.outs != nullptr ? l.outs[i] : const_cast<void*>(l.grads[i]), n};
+    table.first_chunk[table.count++] = (int32_t)chunks;
+    const int64_t each = kChunkBytes / sizeof(T), rest = n - ahead<T>(l.grads[i], n);
+    chunks += std::max<int64_t>(1, (rest + each - 1) / each);
+    if (chunks > 0x7fffffff - 2 * kGradCtas) {
+      set_error("the gradients are too large");
+      return SPARSP_ERR_UNSUPPORTED;
+    }
+  }
+  table.first_chunk[table.count] = (int32_t)chunks;
+  p.begin = from == 0;
+  p.end = to == l.count;
+  // every launch of a list with the same CTAs: each adds to its own sum
+  const bool one = p.begin && p.end;
+  const unsigned ctas = one ? (unsigned)std::max<int64_t>(1, std::min<int64_t>(chunks, kGradCtas)) : kGradCtas;
+  auto kern = squares ? grad_squares_kernel<T, kMost> : grad_clip_kernel<T, kMost>;
+  SPARSP_CUDA_OK(launch_kernel(kern, dim3(ctas), kGradThreads, 0, st, table, p));
+  return SPARSP_OK;
+}
+
+static int launch_list(const sparsp_grad_list& l, bool squares, const GradParams& p, cudaStream_t st) {
+  SPARSP_WITH_TYPE(l.dtype, T, {
+    if (l.count <= kFewTensors) return launch_grad<T, kFewTensors>(l, 0, l.count, squares, p, st);
+    for (int from = 0; from < l.count; from += kMostTensors) {
+      const int rc = launch_grad<T, kMostTensors>(l, from, std::min(l.count, from + kMostTensors), squares, p, st);
+      if (rc != SPARSP_OK) return rc;
+    }
+  });
+  return SPARSP_OK;
+}
+
+static GradParams grad_params(char* ws) {
+  GradParams p = {};
+  p.ticket = reinterpret_cast<uint32_t*>(ws + 128);
+  p.sum = reinterpret_cast<double*>(ws + 256);
+  p.partial = reinterpret_cast<double*>(ws + 512);
+  return p;
+}
+
+int launch_grad_squares(const sparsp_grad_list& l, int accumulate, char* ws, cudaStream_t st) {
+  GradParams p = grad_params(ws);
+  p.accumulate = accumulate;
+  return launch_list(l, true, p, st);
+}
+
+int launch_grad_clip(const sparsp_grad_list& l, double limit, float* norm, char* ws, cudaStream_t st) {
+  GradParams p = grad_params(ws);
+  p.limit = limit;
+  p.norm = norm;
+  p.in_place = 1;
+  for (int i = 0; i < l.count && l.outs != nullptr; ++i)
+    if (l.sizes[i] > 0 && l.outs[i] != l.grads[i]) p.in_place = 0;
+  return launch_list(l, false, p, st);
+}
+
+// Whether what is written overlaps; -1: no host memory to find out.
+int grad_outputs_overlap(const sparsp_grad_list& l) {
+  const int64_t e = element_bytes(l.dtype);
+  auto at = [&](int i) { return (uintptr_t)(l.outs != nullptr ? l.outs[i] : l.grads[i]); };
+  uintptr_t end = 0;
+  bool ordered = true;
+  for (int i = 0; i < l.count && ordered; ++i) {
+    if (l.sizes[i] == 0) continue;
+    ordered = at(i) >= end;
+    end = at(i) + l.sizes[i] * e;
+  }
+  if (ordered) return 0;
+  try {
+    std::vector<std::pair<uintptr_t, uintptr_t>> runs;
+    runs.reserve(l.count);
+    for (int i = 0; i < l.count; ++i)
+      if (l.sizes[i] > 0) runs.emplace_back(at(i), at(i) + l.sizes[i] * e);
+    std::sort(runs.begin(), runs.end());
+    for (size_t i = 1; i < runs.size(); ++i)
+      if (runs[i].first < runs[i - 1].second) return 1;
+  } catch (const std::bad_alloc&) {
+    return -1;
+  }
+  return 0;
+}
+
+}  // namespace sparsp

@@ -12,6 +12,7 @@ namespace sparsp {
 
 constexpr int kMaxRotaryHeadDim = 256;
 constexpr int kMaxNormDim = 16384;
+constexpr int kMaxStepDim = 8192;
 // Work is shared out for the multiprocessors of a B200, whatever device a size of workspace is asked on: the shares
 // also decide in which order sums are made.
 constexpr int kSms = 148;
@@ -170,6 +171,21 @@ int launch_ffn_fwd(const sparsp_ffn& f, const void* X, const void* Wg, const voi
                    char* ws, cudaStream_t st);
 int launch_ffn_bwd(const sparsp_ffn& f, const void* dH, const void* X, const void* Wg, const void* Wu,
                    const void* gate, const void* up, void* dX, void* dWg, void* dWu, char* ws, cudaStream_t st);
+
+int64_t step_groups(const sparsp_gated_norm& n);
+int64_t step_workspace_bytes(const sparsp_gated_norm& n);
+int launch_gated_norm_fwd(const sparsp_gated_norm& n, const void* X, const void* Y, const void* gate, const void* wy,
+                          const void* by, const void* wr, const void* br, void* R, void* N, float* stats_y,
+                          float* stats_r, cudaStream_t st);
+int launch_gated_norm_bwd(const sparsp_gated_norm& n, const void* dN, const void* dR, const void* R, const void* Y,
+                          const void* gate, const void* wy, const void* by, const void* wr, const float* stats_y,
+                          const float* stats_r, void* dX, void* dY, void* dgate, void* dwy, void* dby, void* dwr,
+                          void* dbr, char* ws, cudaStream_t st);
+
+int64_t grad_workspace_bytes();
+int grad_outputs_overlap(const sparsp_grad_list& l);
+int launch_grad_squares(const sparsp_grad_list& l, int accumulate, char* ws, cudaStream_t st);
+int launch_grad_clip(const sparsp_grad_list& l, double limit, float* norm, char* ws, cudaStream_t st);
 
 int64_t fp4_scales_bytes(const sparsp_fp4& f);
 int launch_fp4_quantize(const sparsp_fp4& f, const void* X, uint8_t* codes, uint8_t* scales, void* values,

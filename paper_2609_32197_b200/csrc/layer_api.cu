@@ -100,6 +100,50 @@ int check_ffn(const sparsp_ffn* f) {
   return SPARSP_OK;
 }
 
+// ---- residual step ----
+int check_step(const sparsp_gated_norm* n) {
+  if (!n) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "step is NULL");
+  if (n->dtype < SPARSP_BF16 || n->dtype > SPARSP_FP32)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "unknown dtype %d", n->dtype);
+  if (n->weight_dtype != n->dtype && n->weight_dtype != SPARSP_FP32)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "weight_dtype %d is neither dtype nor fp32", n->weight_dtype);
+  if (n->norm_y < SPARSP_NORM_NONE || n->norm_y > SPARSP_NORM_RMS || n->norm_r < SPARSP_NORM_NONE ||
+      n->norm_r > SPARSP_NORM_RMS)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "unknown norm %d or %d", n->norm_y, n->norm_r);
+  if (n->rows < 0 || n->rows_per_group < 0 || n->dim < 1)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "rows, rows_per_group or dim is negative or zero");
+  if (n->dim % 8 || n->dim > kMaxStepDim)
+    SPARSP_REFUSE(SPARSP_ERR_UNSUPPORTED, "dim %d must be a multiple of 8 up to %d", n->dim, kMaxStepDim);
+  for (int64_t stride : {n->stride_x, n->stride_y, n->stride_n})
+    if (stride < n->dim || stride % 8)
+      SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "row strides must be multiples of 8 elements and not less than a row");
+  if (!(n->eps >= 0.0f) || std::isinf(n->eps)) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "eps must be finite and >= 0");
+  if (n->rows > (1LL << 37)) SPARSP_REFUSE(SPARSP_ERR_UNSUPPORTED, "%lld rows are too many", (long long)n->rows);
+  return SPARSP_OK;
+}
+int absent(const void* p, const char* name) {
+  if (p) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "%s belongs to a norm that is not there", name);
+  return SPARSP_OK;
+}
+
+// ---- lists of gradients ----
+int check_grads(const sparsp_grad_list* l) {
+  if (!l) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "list is NULL");
+  if (l->dtype < SPARSP_BF16 || l->dtype > SPARSP_FP32)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "unknown dtype %d", l->dtype);
+  if (l->count < 0) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "count is negative");
+  if (l->count > 0 && (!l->grads || !l->sizes)) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "grads or sizes is NULL");
+  const size_t e = element_bytes(l->dtype);
+  for (int i = 0; i < l->count; ++i) {
+    if (l->sizes[i] < 0 || l->sizes[i] > (1LL << 40))
+      SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "gradient %d has %lld values", i, (long long)l->sizes[i]);
+    if (l->sizes[i] == 0) continue;
+    if (!l->grads[i] || (uintptr_t)l->grads[i] % e || (l->outs && (!l->outs[i] || (uintptr_t)l->outs[i] % e)))
+      SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "gradient %d or its output is NULL or not aligned to its type", i);
+  }
+  return SPARSP_OK;
+}
+
 // ---- 4-bit operands ----
 int check_format(int32_t format, int32_t exponent, int32_t most) {
   if (format != SPARSP_MXFP4 && format != SPARSP_NVFP4) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "unknown format %d", format);
@@ -341,6 +385,123 @@ int sparsp_gated_ffn_bwd(const sparsp_ffn* ffn, const void* dH, const void* X, c
     SPARSP_TRY(apart({dX, dWgate, dWup}, {dWgate ? X : nullptr, dX ? Wgate : nullptr, dX ? Wup : nullptr}));
   }
   return launch_ffn_bwd(*ffn, dH, X, Wgate, Wup, gate, up, dX, dWgate, dWup, (char*)workspace, (cudaStream_t)stream);
+}
+
+int sparsp_gated_norm_fwd(const sparsp_gated_norm* step, const void* X, const void* Y, const void* gate,
+                          const void* weight_y, const void* bias_y, const void* weight_r, const void* bias_r, void* R,
+                          void* N, float* stats_y, float* stats_r, void* stream) {
+  SPARSP_TRY(check_step(step));
+  if (step->norm_y == SPARSP_NORM_NONE) {
+    SPARSP_TRY(absent(weight_y, "weight_y"));
+    SPARSP_TRY(absent(bias_y, "bias_y"));
+    SPARSP_TRY(absent(stats_y, "stats_y"));
+  }
+  if (step->norm_r == SPARSP_NORM_NONE) {
+    SPARSP_TRY(absent(weight_r, "weight_r"));
+    SPARSP_TRY(absent(bias_r, "bias_r"));
+    SPARSP_TRY(absent(stats_r, "stats_r"));
+    SPARSP_TRY(absent(N, "N"));
+  }
+  if (step->rows == 0) return SPARSP_OK;
+  SPARSP_TRY(need(X, "X", 16));
+  SPARSP_TRY(need(Y, "Y", 16));
+  SPARSP_TRY(need(R, "R", 16));
+  if (step->norm_r != SPARSP_NORM_NONE) SPARSP_TRY(need(N, "N", 16));
+  SPARSP_TRY(optional(gate, "gate", 16));
+  SPARSP_TRY(optional(weight_y, "weight_y", 16));
+  SPARSP_TRY(optional(bias_y, "bias_y", 16));
+  SPARSP_TRY(optional(weight_r, "weight_r", 16));
+  SPARSP_TRY(optional(bias_r, "bias_r", 16));
+  SPARSP_TRY(optional(stats_y, "stats_y", 8));
+  SPARSP_TRY(optional(stats_r, "stats_r", 8));
+  SPARSP_TRY(apart({R, N, stats_y, stats_r}, {gate, weight_y, bias_y, weight_r, bias_r}));
+  if (R == Y || N == X) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "R may not be Y, nor N be X");
+  if (N == Y && step->stride_n != step->stride_y)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "N may be Y only when the strides are equal");
+  return launch_gated_norm_fwd(*step, X, Y, gate, weight_y, bias_y, weight_r, bias_r, R, N, stats_y, stats_r,
+                               (cudaStream_t)stream);
+}
+
+int sparsp_gated_norm_workspace_bytes(const sparsp_gated_norm* step, int64_t* bytes) {
+  SPARSP_TRY(check_step(step));
+  if (!bytes) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = step_workspace_bytes(*step);
+  return SPARSP_OK;
+}
+
+int sparsp_gated_norm_bwd(const sparsp_gated_norm* step, const void* dN, const void* dR, const void* R, const void* Y,
+                          const void* gate, const void* weight_y, const void* bias_y, const void* weight_r,
+                          const float* stats_y, const float* stats_r, void* dX, void* dY, void* dgate, void* dweight_y,
+                          void* dbias_y, void* dweight_r, void* dbias_r, void* workspace, void* stream) {
+  SPARSP_TRY(check_step(step));
+  const bool norm_y = step->norm_y != SPARSP_NORM_NONE, norm_r = step->norm_r != SPARSP_NORM_NONE;
+  if (!norm_y) {
+    SPARSP_TRY(absent(weight_y, "weight_y"));
+    SPARSP_TRY(absent(bias_y, "bias_y"));
+    SPARSP_TRY(absent(stats_y, "stats_y"));
+    SPARSP_TRY(absent(dweight_y, "dweight_y"));
+    SPARSP_TRY(absent(dbias_y, "dbias_y"));
+  }
+  if (!norm_r) {
+    SPARSP_TRY(absent(dN, "dN"));
+    SPARSP_TRY(absent(R, "R"));
+    SPARSP_TRY(absent(weight_r, "weight_r"));
+    SPARSP_TRY(absent(stats_r, "stats_r"));
+    SPARSP_TRY(absent(dweight_r, "dweight_r"));
+    SPARSP_TRY(absent(dbias_r, "dbias_r"));
+  }
+  if (step->rows > 0) {
+    SPARSP_TRY(need(Y, "Y", 16));
+    if (norm_y) SPARSP_TRY(need(stats_y, "stats_y", 8));
+    if (norm_r) {
+      SPARSP_TRY(need(dN, "dN", 16));
+      SPARSP_TRY(need(R, "R", 16));
+      SPARSP_TRY(need(stats_r, "stats_r", 8));
+      SPARSP_TRY(optional(dR, "dR", 16));
+    } else {
+      SPARSP_TRY(need(dR, "dR", 16));
+    }
+    SPARSP_TRY(need(workspace, "workspace", 256));
+  }
+  SPARSP_TRY(optional(gate, "gate", 16));
+  SPARSP_TRY(optional(weight_y, "weight_y", 16));
+  SPARSP_TRY(optional(bias_y, "bias_y", 16));
+  SPARSP_TRY(optional(weight_r, "weight_r", 16));
+  SPARSP_TRY(optional(dX, "dX", 16));
+  SPARSP_TRY(optional(dY, "dY", 16));
+  SPARSP_TRY(optional(dgate, "dgate", 16));
+  SPARSP_TRY(optional(dweight_y, "dweight_y", 16));
+  SPARSP_TRY(optional(dbias_y, "dbias_y", 16));
+  SPARSP_TRY(optional(dweight_r, "dweight_r", 16));
+  SPARSP_TRY(optional(dbias_r, "dbias_r", 16));
+  SPARSP_TRY(apart({dX, dY, dgate, dweight_y, dbias_y, dweight_r, dbias_r},
+                   {dN, R, Y, gate, weight_y, bias_y, weight_r, stats_y, stats_r}));
+  SPARSP_TRY(apart({dY, dgate, dweight_y, dbias_y, dweight_r, dbias_r}, {dR}));
+  return launch_gated_norm_bwd(*step, dN, dR, R, Y, gate, weight_y, bias_y, weight_r, stats_y, stats_r, dX, dY, dgate,
+                               dweight_y, dbias_y, dweight_r, dbias_r, (char*)workspace, (cudaStream_t)stream);
+}
+
+int sparsp_grad_workspace_bytes(int64_t* bytes) {
+  if (!bytes) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = grad_workspace_bytes();
+  return SPARSP_OK;
+}
+
+int sparsp_grad_squares(const sparsp_grad_list* list, int32_t accumulate, void* workspace, void* stream) {
+  SPARSP_TRY(check_grads(list));
+  SPARSP_TRY(need(workspace, "workspace", 256));
+  return launch_grad_squares(*list, accumulate != 0, (char*)workspace, (cudaStream_t)stream);
+}
+
+int sparsp_grad_clip(const sparsp_grad_list* list, double max_norm, float* norm, void* workspace, void* stream) {
+  SPARSP_TRY(check_grads(list));
+  if (!(max_norm > 0.0)) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "max_norm %g must be above 0", max_norm);
+  SPARSP_TRY(optional(norm, "norm", 4));
+  SPARSP_TRY(need(workspace, "workspace", 256));
+  const int overlap = grad_outputs_overlap(*list);
+  if (overlap < 0) SPARSP_REFUSE(SPARSP_ERR_CAPACITY, "no host memory for a list of %d gradients", list->count);
+  if (overlap) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "two of the gradients that are written overlap");
+  return launch_grad_clip(*list, max_norm, norm, (char*)workspace, (cudaStream_t)stream);
 }
 
 int sparsp_fp4_scales_bytes(const sparsp_fp4* fp4, int64_t* bytes) {
