@@ -18,7 +18,7 @@ struct StepParams {
   float *partial, *partial_y;  // backward: [teams][2][4][dim], of a team's first group and its last, and [teams][2][dim]
   void *dgate, *dwy, *dby, *dwr, *dbr;
   int64_t rows, rows_per_group, stride_x, stride_y, stride_n;
-  int32_t dim, teams, lanes, stages, norm_y, norm_r;
+  int32_t dim, teams, lanes, stages, places, norm_y, norm_r;
   float eps, inv_dim;
 };
 
@@ -32,32 +32,36 @@ __host__ __device__ inline int64_t team_of(int64_t row, int64_t teams, int64_t r
 }
 
 // Sums over a team, the same in every lane.  kWarps: the team is a CTA; its warps meet at one barrier a call, by turns
-// of `room`.
+// of `room`, whose places of warps that are not there are 0.
+constexpr int kMostWarps = 16;
 template <bool kWarps, int N>
-__device__ __forceinline__ void team_sum(float (&v)[N], int lanes, float (*room)[32][2], int& turn) {
-  const int most = kWarps ? 16 : lanes / 2;
+__device__ __forceinline__ void team_sum(float (&v)[N], int lanes, float (*room)[2][kMostWarps], int& turn) {
 #pragma unroll
   for (int d = 16; d > 0; d /= 2)
-    if (kWarps || d <= most) {
+    if (kWarps || d < lanes) {
 #pragma unroll
       for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], d);
     }
   if constexpr (kWarps) {
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    float (*mine)[2] = room[turn];
+    const int warp = threadIdx.x >> 5;
+    float (*at)[kMostWarps] = room[turn];
     turn ^= 1;
-    if (lane == 0) {
+    if ((threadIdx.x & 31) == 0) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) mine[warp][i] = v[i];
+      for (int i = 0; i < N; ++i) at[i][warp] = v[i];
     }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = 0.0f;
-    for (int w = 0; w < warps; ++w) {
-#pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += mine[w][i];
+    for (int i = 0; i < N; ++i) {
+      const float4* w = reinterpret_cast<const float4*>(at[i]);
+      const float4 a = w[0], b = w[1], c = w[2], d = w[3];
+      v[i] = ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w)) + (((c.x + c.y) + (c.z + c.w)) + ((d.x + d.y) + (d.z + d.w)));
     }
   }
+}
+__device__ __forceinline__ void clear_room(float (*room)[2][kMostWarps]) {
+  if (threadIdx.x < 4 * kMostWarps) (&room[0][0][0])[threadIdx.x] = 0.0f;
+  __syncthreads();
 }
 
 // E values of a weight as they lie in memory, of type W, from its own 16-byte pieces.
@@ -81,81 +85,86 @@ struct Weights {
   }
 };
 
-// A thread's own 16-byte places in shared memory: nobody else's, so that nothing has to be waited for but its own copies.
-// Place k is at k * threads + this thread.
+// A thread's own 16-byte places in shared memory, one behind the other: nobody else's, so that nothing has to be waited
+// for but its own copies.  Their number is odd, so that eight lanes' places of one number lie in different banks.
 struct Places {
-  uint4* base;
-  __device__ __forceinline__ Places() {
+  uint8_t* base;
+  int pitch;
+  __device__ __forceinline__ Places(int places) {
     extern __shared__ uint4 dynamic[];
-    base = dynamic + threadIdx.x;
-  }
-  __device__ __forceinline__ uint4* at(int k) const { return base + k * (int)blockDim.x; }
-  template <typename T, int E>
-  __device__ __forceinline__ Vec<T, E> get(int k) const {
-    return load_vec<T, E>(reinterpret_cast<const T*>(at(k)));
+    base = reinterpret_cast<uint8_t*>(dynamic) + threadIdx.x * 16;
+    pitch = blockDim.x * 16;
   }
   template <typename W, int E>
   __device__ __forceinline__ Weights<W, E> weights(int k) const {
     Weights<W, E> w;
 #pragma unroll
-    for (int i = 0; i < Weights<W, E>::kParts; ++i) w.part[i] = get<W, Weights<W, E>::kEach>(k + i);
+    for (int i = 0; i < Weights<W, E>::kParts; ++i)
+      w.part[i] = load_vec<W, Weights<W, E>::kEach>(reinterpret_cast<const W*>(base + (k + i) * pitch));
     return w;
   }
   template <typename W, int E>
   __device__ __forceinline__ void put(int k, const Weights<W, E>& w) const {
 #pragma unroll
-    for (int i = 0; i < Weights<W, E>::kParts; ++i) store_vec(reinterpret_cast<W*>(at(k + i)), w.part[i]);
-  }
-  __device__ __forceinline__ void copy(int k, const void* from) const {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(at(k))), "l"(from)
-                 : "memory");
-  }
-  static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-  // until all but the last `behind` groups of this thread's copies have arrived
-  static __device__ __forceinline__ void wait(int behind) {
-    if (behind >= 3)
-      asm volatile("cp.async.wait_group 3;" ::: "memory");
-    else if (behind == 2)
-      asm volatile("cp.async.wait_group 2;" ::: "memory");
-    else if (behind == 1)
-      asm volatile("cp.async.wait_group 1;" ::: "memory");
-    else
-      asm volatile("cp.async.wait_group 0;" ::: "memory");
+    for (int i = 0; i < Weights<W, E>::kParts; ++i) store_vec(reinterpret_cast<W*>(base + (k + i) * pitch), w.part[i]);
   }
 };
 
-// Rows on their way into shared memory: `stages` rows of N tensors, V pieces each.
+// Rows on their way into shared memory, behind `first` places: `stages` rows of N tensors, V pieces each.  Tensor number
+// q is left out where it is NULL.
 template <typename T, int V, int N>
 struct Ring {
-  Places places;
-  int stages, slot, lanes, me, dim;
-  const T* from[N];
-  int64_t ld[N];
-  __device__ __forceinline__ void fetch(int64_t row, int64_t hi) const {
-    if (row < hi) {
+  static constexpr int E = 16 / sizeof(T), kRow = N * V;
+  const uint8_t* from[N];  // this thread's first piece of the next row to ask for
+  int64_t step[N];
+  uint8_t *begin, *end, *slot;
+  int across, left, stages, pitch;  // bytes from a piece to the next; rows still to be asked for
+  bool in[V];
+  __device__ __forceinline__ Ring(const Places& places, int first, int stages, const void* const (&tensors)[N],
+                                  const int64_t (&ld)[N], int64_t row, int rows, int lanes, int me, int dim)
+      : across(lanes * 16), left(rows), stages(stages) {
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+      step[q] = ld[q] * (int)sizeof(T);
+      from[q] = tensors[q] == nullptr ? nullptr : static_cast<const uint8_t*>(tensors[q]) + row * step[q] + me * 16;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) in[v] = (v * lanes + me) * E < dim;
+    pitch = places.pitch;
+    begin = slot = places.base + first * pitch;
+    end = begin + stages * kRow * pitch;
+    for (int i = 0; i < stages; ++i) next();
+  }
+  __device__ __forceinline__ Vec<T, E> get(int q, int v) const {
+    return load_vec<T, E>(reinterpret_cast<const T*>(slot + (q * V + v) * pitch));
+  }
+  // the row in use is done with: the one `stages` behind it takes its place
+  __device__ __forceinline__ void next() {
+    if (left > 0) {
+      --left;
+      const uint32_t to = (uint32_t)__cvta_generic_to_shared(slot);
 #pragma unroll
       for (int q = 0; q < N; ++q)
         if (from[q] != nullptr) {
 #pragma unroll
-          for (int v = 0; v < V; ++v) {
-            const int col = (v * lanes + me) * (16 / (int)sizeof(T));
-            if (col < dim) places.copy((slot * N + q) * V + v, from[q] + row * ld[q] + col);
-          }
+          for (int v = 0; v < V; ++v)
+            if (in[v])
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to + (q * V + v) * pitch), "l"(from[q] + v * across)
+                           : "memory");
+          from[q] += step[q];
         }
     }
-    places.commit();
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    slot = slot + kRow * pitch == end ? begin : slot + kRow * pitch;
   }
-  __device__ __forceinline__ void start(int64_t lo, int64_t hi) {
-    for (slot = 0; slot < stages; ++slot) fetch(lo + slot, hi);
-    slot = 0;
-  }
-  __device__ __forceinline__ Vec<T, 16 / sizeof(T)> get(int q, int v) const {
-    return places.get<T, 16 / sizeof(T)>((slot * N + q) * V + v);
-  }
-  // the row in use is done with: the one `stages` behind it takes its place
-  __device__ __forceinline__ void next(int64_t row, int64_t hi) {
-    fetch(row + stages, hi);
-    if (++slot == stages) slot = 0;
+  // until the row in use has arrived
+  __device__ __forceinline__ void wait() const {
+    if (stages == 3)
+      asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else if (stages == 2)
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
   }
 };
 
@@ -175,31 +184,44 @@ struct Group {
 // those past the last of a team doing nothing, for their lanes meet in the sums.
 template <bool kWarps>
 struct Member {
-  int lanes, team, me;
-  int64_t lo, hi, turns;
+  int lanes, team, me, rows, turns;
+  int64_t lo;
   __device__ __forceinline__ Member(const StepParams& p) {
     lanes = kWarps ? blockDim.x : p.lanes;
     team = kWarps ? blockIdx.x : (blockIdx.x * blockDim.x + threadIdx.x) / lanes;
     me = kWarps ? threadIdx.x : threadIdx.x & (lanes - 1);
     const bool there = team < p.teams;
     lo = there ? first_row(team, p.teams, p.rows) : 0;
-    hi = there ? first_row(team + 1, p.teams, p.rows) : 0;
-    turns = kWarps ? hi - lo : (p.rows + p.teams - 1) / p.teams;
+    rows = there ? (int)(first_row(team + 1, p.teams, p.rows) - lo) : 0;
+    turns = kWarps ? rows : (int)((p.rows + p.teams - 1) / p.teams);
   }
 };
 
-template <typename T, typename W, int V, bool kWarps, bool kNormY>
-__global__ void __launch_bounds__(kWarps ? 512 : 128, kWarps ? 2 : 8) step_kernel(StepParams p) {
+// kNormY: y has a norm.  Without it, registers hold the weights of a group; with it there are too many.
+template <typename T, typename W, int V, int kThreads, bool kNormY>
+__global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepParams p) {
+  constexpr bool kWarps = kThreads > 128;  // teams of 128 threads or fewer in a CTA of their own have room for 320
   enter_grid(p.x, p.y, p.gate, p.wy, p.by, p.wr, p.br);
   constexpr int E = 16 / sizeof(T);
-  __shared__ float room[2][32][2];
+  __shared__ __align__(16) float room[2][2][kMostWarps];
   int turn = 0;
+  if (kWarps) clear_room(room);
   const Member<kWarps> m(p);
-  Ring<T, V, 2> ring = {{}, p.stages, 0, m.lanes, m.me, p.dim, {static_cast<const T*>(p.x), static_cast<const T*>(p.y)},
-                        {p.stride_x, p.stride_y}};
-  ring.start(m.lo, m.hi);
+  const Places places(p.places);
+  Ring<T, V, 2> ring(places, 0, p.stages, {p.x, p.y}, {p.stride_x, p.stride_y}, m.lo, m.rows, m.lanes, m.me, p.dim);
   Group group(m.lo, p.rows_per_group);
-  auto column = [&](int v) { return (v * m.lanes + m.me) * E; };
+  Weights<W, E> gate[V], wr[V], br[V];
+  auto load_weights = [&] {
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+      if (ring.in[v]) {
+        const int64_t at = group.index * p.dim + (v * m.lanes + m.me) * E;
+        gate[v].load(p.gate, at, 1.0f);
+        wr[v].load(p.wr, at, 1.0f);
+        br[v].load(p.br, at, 0.0f);
+      }
+  };
+  if (!kNormY) load_weights();
   // mean and 1 / deviation of values of which those past the last column are 0
   auto statistics = [&](const float (&x)[V * E], int kind, float& mean, float& rstd) {
     mean = 0.0f;
@@ -213,7 +235,7 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128, kWarps ? 2 : 8) step_kerne
     float q[1] = {0.0f};
 #pragma unroll
     for (int v = 0; v < V; ++v)
-      if (column(v) < p.dim) {
+      if (ring.in[v]) {
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const float d = x[v * E + e] - mean;
@@ -223,37 +245,38 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128, kWarps ? 2 : 8) step_kerne
     team_sum<kWarps>(q, m.lanes, room, turn);
     rstd = 1.0f / sqrtf(fmaf(q[0], p.inv_dim, p.eps));
   };
-  for (int64_t i = 0; i < m.turns; ++i) {
-    const int64_t row = m.lo + i;
-    const bool live = row < m.hi;
-    if (live) group.advance(row, p.rows_per_group);
-    Places::wait(p.stages - 1);
+  T* to_r = static_cast<T*>(p.r) + m.lo * p.stride_x + m.me * E;
+  T* to_n = static_cast<T*>(p.n) + m.lo * p.stride_n + m.me * E;
+  for (int i = 0; i < m.turns; ++i, to_r += p.stride_x, to_n += p.stride_n) {
+    const bool live = i < m.rows;
+    if (live && group.advance(m.lo + i, p.rows_per_group) && !kNormY) load_weights();
+    ring.wait();
     float r[V * E], mean = 0.0f, rstd = 1.0f;
     if constexpr (kNormY) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         Vec<T, E> y;
         y.clear();
-        if (live && column(v) < p.dim) y = ring.get(1, v);
+        if (live && ring.in[v]) y = ring.get(1, v);
 #pragma unroll
         for (int e = 0; e < E; ++e) r[v * E + e] = y[e];
       }
       statistics(r, p.norm_y, mean, rstd);
-      if (p.stats_y != nullptr && live && m.me == 0) reinterpret_cast<float2*>(p.stats_y)[row] = make_float2(mean, rstd);
+      if (p.stats_y != nullptr && live && m.me == 0)
+        reinterpret_cast<float2*>(p.stats_y)[m.lo + i] = make_float2(mean, rstd);
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int col = column(v);
-      if (!live || col >= p.dim) {
+      if (!live || !ring.in[v]) {
 #pragma unroll
         for (int e = 0; e < E; ++e) r[v * E + e] = 0.0f;
         continue;
       }
       const Vec<T, E> x = ring.get(0, v);
-      Weights<W, E> g;
-      g.load(p.gate, group.index * p.dim + col, 1.0f);
       if constexpr (kNormY) {
-        Weights<W, E> w, b;
+        const int col = (v * m.lanes + m.me) * E;
+        Weights<W, E> g, w, b;
+        g.load(p.gate, group.index * p.dim + col, 1.0f);
         w.load(p.wy, col, 1.0f);
         b.load(p.by, col, 0.0f);
 #pragma unroll
@@ -261,30 +284,31 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128, kWarps ? 2 : 8) step_kerne
       } else {
         const Vec<T, E> y = ring.get(1, v);
 #pragma unroll
-        for (int e = 0; e < E; ++e) r[v * E + e] = fmaf(g[e], y[e], x[e]);
+        for (int e = 0; e < E; ++e) r[v * E + e] = fmaf(gate[v][e], y[e], x[e]);
       }
       Vec<T, E> out;
       out.set(r + v * E);
-      store_vec(static_cast<T*>(p.r) + row * p.stride_x + col, out);
+      store_vec(to_r + v * m.lanes * E, out);
     }
-    ring.next(row, m.hi);
+    ring.next();
     if (p.norm_r == SPARSP_NORM_NONE) continue;
     statistics(r, p.norm_r, mean, rstd);
     if (!live) continue;
-    if (p.stats_r != nullptr && m.me == 0) reinterpret_cast<float2*>(p.stats_r)[row] = make_float2(mean, rstd);
+    if (p.stats_r != nullptr && m.me == 0) reinterpret_cast<float2*>(p.stats_r)[m.lo + i] = make_float2(mean, rstd);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int col = column(v);
-      if (col >= p.dim) continue;
-      Weights<W, E> w, b;
-      w.load(p.wr, group.index * p.dim + col, 1.0f);
-      b.load(p.br, group.index * p.dim + col, 0.0f);
+      if (!ring.in[v]) continue;
+      if constexpr (kNormY) {
+        const int64_t at = group.index * p.dim + (v * m.lanes + m.me) * E;
+        wr[v].load(p.wr, at, 1.0f);
+        br[v].load(p.br, at, 0.0f);
+      }
       float n[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) n[e] = fmaf((r[v * E + e] - mean) * rstd, w[e], b[e]);
+      for (int e = 0; e < E; ++e) n[e] = fmaf((r[v * E + e] - mean) * rstd, wr[v][e], br[v][e]);
       Vec<T, E> out;
       out.set(n);
-      store_vec(static_cast<T*>(p.n) + row * p.stride_n + col, out);
+      store_vec(to_n + v * m.lanes * E, out);
     }
   }
 }
@@ -294,22 +318,22 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128, kWarps ? 2 : 8) step_kerne
 // norm.  (An rms norm has mean 0 and no sum a.)  Column sums over the rows of a group, in registers: dn rh, dn, t yh (or
 // t y), t; from these come all gradients of weights.  There are no registers for more: rows and weights stay in shared
 // memory and are read again for each step.
-template <typename T, typename W, int V, bool kWarps, bool kNormY>
-__global__ void __launch_bounds__(kWarps ? 512 : 128) step_back_kernel(StepParams p) {
+template <typename T, typename W, int V, int kThreads, bool kNormY>
+__global__ void __launch_bounds__(kThreads) step_back_kernel(StepParams p) {
+  constexpr bool kWarps = kThreads > 128;  // teams of 128 threads or fewer in a CTA of their own have room for 320
   enter_grid(p.x, p.y, p.dn, p.dr, p.gate, p.wy, p.wr, p.stats_y, p.stats_r);
   constexpr int E = 16 / sizeof(T), kSums = kNormY ? 4 : 3, kPart = Weights<W, E>::kParts;
-  __shared__ float room[2][32][2];
+  __shared__ __align__(16) float room[2][2][kMostWarps];
   int turn = 0;
+  if (kWarps) clear_room(room);
   const Member<kWarps> m(p);
   const bool norm_r = p.norm_r != SPARSP_NORM_NONE;
   enum { kDn, kR, kDr, kY };
-  Ring<T, V, 4> ring = {{}, p.stages, 0, m.lanes, m.me, p.dim,
-                        {static_cast<const T*>(p.dn), static_cast<const T*>(p.x), static_cast<const T*>(p.dr),
-                         static_cast<const T*>(p.y)},
-                        {p.stride_n, p.stride_x, p.stride_x, p.stride_y}};
-  ring.start(m.lo, m.hi);
-  const Places places;
-  const int wr_at = p.stages * 4 * V, gate_at = wr_at + V * kPart, wy_at = gate_at + V * kPart;
+  const Places places(p.places);
+  constexpr int kWrAt = 0, kGateAt = V * kPart, kWyAt = 2 * V * kPart;  // then rows
+  Ring<T, V, 4> ring(places, (kNormY ? 3 : 2) * V * kPart, p.stages, {p.dn, p.x, p.dr, p.y},
+                     {p.stride_n, p.stride_x, p.stride_x, p.stride_y}, m.lo, m.rows, m.lanes, m.me, p.dim);
+  const int64_t hi = m.lo + m.rows;
   auto column = [&](int v) { return (v * m.lanes + m.me) * E; };
   Group group(m.lo, p.rows_per_group);
   auto hold_weights = [&] {
@@ -320,16 +344,16 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128) step_back_kernel(StepParam
       const int64_t at = group.index * p.dim + col;
       Weights<W, E> w;
       w.load(p.wr, at, 1.0f);
-      places.put(wr_at + v * kPart, w);
+      places.put(kWrAt + v * kPart, w);
       w.load(p.gate, at, 1.0f);
-      places.put(gate_at + v * kPart, w);
+      places.put(kGateAt + v * kPart, w);
       if (kNormY) {
         w.load(p.wy, col, 1.0f);
-        places.put(wy_at + v * kPart, w);
+        places.put(kWyAt + v * kPart, w);
       }
     }
   };
-  if (m.lo < m.hi) hold_weights();
+  if (m.rows > 0) hold_weights();
 
   float sums[kSums][V * E];
 #pragma unroll
@@ -339,7 +363,7 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128) step_back_kernel(StepParam
   bool first_flush = true;
   auto flush = [&] {
     // a group that this team has all of is finished here
-    const bool whole = (group.index * p.rows_per_group >= m.lo) && (group.end <= m.hi || m.hi == p.rows);
+    const bool whole = (group.index * p.rows_per_group >= m.lo) && (group.end <= hi || hi == p.rows);
     float* to = p.partial + (2 * (int64_t)m.team + (group.index * p.rows_per_group > m.lo)) * 4 * p.dim;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
@@ -348,8 +372,8 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128) step_back_kernel(StepParam
       const int64_t at = group.index * p.dim + col;
       Weights<W, E> g, w, b;
       if (kNormY) {
-        g = places.weights<W, E>(gate_at + v * kPart);
-        w = places.weights<W, E>(wy_at + v * kPart);
+        g = places.weights<W, E>(kGateAt + v * kPart);
+        w = places.weights<W, E>(kWyAt + v * kPart);
         b.load(p.by, col, 0.0f);
       }
       auto put = [&](void* out, int e, float x) {
@@ -381,12 +405,14 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128) step_back_kernel(StepParam
 
   // the kept statistics of a row, asked for a row ahead
   auto kept = [&](const float* from, bool norm, int64_t row) {
-    return norm && row < m.hi ? reinterpret_cast<const float2*>(from)[row] : make_float2(0.0f, 1.0f);
+    return norm && row < hi ? reinterpret_cast<const float2*>(from)[row] : make_float2(0.0f, 1.0f);
   };
   float2 next_r = kept(p.stats_r, norm_r, m.lo), next_y = kept(p.stats_y, kNormY, m.lo);
-  for (int64_t i = 0; i < m.turns; ++i) {
+  T* to_x = static_cast<T*>(p.r) + m.lo * p.stride_x + m.me * E;
+  T* to_y = static_cast<T*>(p.n) + m.lo * p.stride_y + m.me * E;
+  for (int i = 0; i < m.turns; ++i, to_x += p.stride_x, to_y += p.stride_y) {
     const int64_t row = m.lo + i;
-    const bool live = row < m.hi;
+    const bool live = i < m.rows;
     if (live && row >= group.end) {
       flush();
       group.advance(row, p.rows_per_group);
@@ -395,14 +421,14 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128) step_back_kernel(StepParam
     const float2 sr = next_r, sy = next_y;
     next_r = kept(p.stats_r, norm_r, row + 1);
     next_y = kept(p.stats_y, kNormY, row + 1);
-    Places::wait(p.stages - 1);
+    ring.wait();
     float s[2] = {0.0f, 0.0f}, k0 = 0.0f, k1 = 0.0f;
     if (norm_r) {
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        if (!live || column(v) >= p.dim) continue;
+        if (!live || !ring.in[v]) continue;
         const Vec<T, E> dn = ring.get(kDn, v), r = ring.get(kR, v);
-        const Weights<W, E> w = places.weights<W, E>(wr_at + v * kPart);
+        const Weights<W, E> w = places.weights<W, E>(kWrAt + v * kPart);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const int k = v * E + e;
@@ -421,8 +447,7 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128) step_back_kernel(StepParam
     float b[V * E];
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int col = column(v);
-      if (!live || col >= p.dim) continue;
+      if (!live || !ring.in[v]) continue;
       float t[E];
       if (p.dr != nullptr) {
         const Vec<T, E> dr = ring.get(kDr, v);
@@ -434,7 +459,7 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128) step_back_kernel(StepParam
       }
       if (norm_r) {
         const Vec<T, E> dn = ring.get(kDn, v), r = ring.get(kR, v);
-        const Weights<W, E> w = places.weights<W, E>(wr_at + v * kPart);
+        const Weights<W, E> w = places.weights<W, E>(kWrAt + v * kPart);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const float rh = (r[e] - sr.x) * sr.y;
@@ -444,12 +469,12 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128) step_back_kernel(StepParam
       if (p.r != nullptr) {
         Vec<T, E> out;
         out.set(t);
-        store_vec(static_cast<T*>(p.r) + row * p.stride_x + col, out);
+        store_vec(to_x + v * m.lanes * E, out);
       }
       const Vec<T, E> y = ring.get(kY, v);
-      const Weights<W, E> g = places.weights<W, E>(gate_at + v * kPart);
+      const Weights<W, E> g = places.weights<W, E>(kGateAt + v * kPart);
       if constexpr (kNormY) {
-        const Weights<W, E> w = places.weights<W, E>(wy_at + v * kPart);
+        const Weights<W, E> w = places.weights<W, E>(kWyAt + v * kPart);
 #pragma unroll
         for (int e = 0; e < E; ++e) {
           const int k = v * E + e;
@@ -469,7 +494,7 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128) step_back_kernel(StepParam
         if (p.n != nullptr) {
           Vec<T, E> out;
           out.set(t);
-          store_vec(static_cast<T*>(p.n) + row * p.stride_y + col, out);
+          store_vec(to_y + v * m.lanes * E, out);
         }
       }
     }
@@ -479,20 +504,19 @@ __global__ void __launch_bounds__(kWarps ? 512 : 128) step_back_kernel(StepParam
       k1 = s[1] * p.inv_dim;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int col = column(v);
-        if (!live || col >= p.dim || p.n == nullptr) continue;
+        if (!live || !ring.in[v] || p.n == nullptr) continue;
         const Vec<T, E> y = ring.get(kY, v);
         float d[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) d[e] = sy.y * (b[v * E + e] - fmaf((y[e] - sy.x) * sy.y, k1, k0));
         Vec<T, E> out;
         out.set(d);
-        store_vec(static_cast<T*>(p.n) + row * p.stride_y + col, out);
+        store_vec(to_y + v * m.lanes * E, out);
       }
     }
-    ring.next(row, m.hi);
+    ring.next();
   }
-  if (m.lo < m.hi) flush();
+  if (m.rows > 0) flush();
 }
 
 // Adds what the teams left: blockIdx.y < `found`: the group of that number (or, of more groups than teams, the one that
@@ -566,11 +590,11 @@ int64_t step_groups(const sparsp_gated_norm& n) { return (n.rows + per_group(n) 
 // How rows are shared out: 16-byte pieces a thread (16 values at most), threads of a CTA, lanes of a team, teams; rows in
 // shared memory.
 struct StepPlan {
-  int pieces, threads, lanes, ctas, stages, smem;
+  int pieces, threads, lanes, ctas, stages, places, smem;
   bool by_warps;
   int64_t teams;
 };
-constexpr int kStepSmem = 226 * 1024;  // of a multiprocessor, without what CTAs reserve
+constexpr int kStepSmem = 228 * 1024;  // of a multiprocessor; each CTA has 1 KB more than it asks for
 
 static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
   StepPlan s;
@@ -596,14 +620,22 @@ static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
     }
     s.lanes = s.threads;
   }
-  const int threads_fit = backward ? 512 : 1024;  // by registers
-  int fit = std::max(1, threads_fit / s.threads);
-  const int piece = s.threads * 16, stage = piece * s.pieces * (backward ? 4 : 2);
-  const int held = backward ? s.pieces * 3 * piece * std::max(1, element_bytes(n.weight_dtype) / element_bytes(n.dtype)) : 0;
-  auto stages = [&](int ctas) { return (kStepSmem / ctas - 1536 - held) / stage; };
+  // CTAs of a multiprocessor by what registers hold
+  int fit = std::max(1, (backward ? 512 : 640) / s.threads);
+  const int row = s.pieces * (backward ? 4 : 2);
+  const int per_weight = std::max(1, element_bytes(n.weight_dtype) / element_bytes(n.dtype));
+  const int held = backward ? s.pieces * per_weight * (n.norm_y != SPARSP_NORM_NONE ? 3 : 2) : 0;
+  auto fits = [&](int places, int ctas) { return (places * s.threads * 16 + 1024 + 256) * ctas <= kStepSmem; };
+  auto stages = [&](int ctas) {
+    int k = 3;
+    while (k > 0 && !fits((k * row + held) | 1, ctas)) --k;
+    return k;
+  };
   while (fit > 1 && stages(fit) < 2) --fit;
-  s.stages = std::max(1, std::min(backward ? 3 : 2, stages(fit)));
-  s.smem = s.stages * stage + held;
+  s.stages = std::max(1, stages(fit));
+  s.places = s.stages * row + held;
+  if (fits(s.places | 1, 1)) s.places |= 1;  // (8192 fp32 values with all weights: even, for there is no room)
+  s.smem = s.places * s.threads * 16;
   s.teams = std::max<int64_t>(1, std::min<int64_t>(n.rows, (int64_t)kSms * fit * per_cta));
   s.ctas = (int)((s.teams + per_cta - 1) / per_cta);
   return s;
@@ -625,6 +657,7 @@ static StepParams step_params(const sparsp_gated_norm& n, const StepPlan& s) {
   p.teams = (int32_t)s.teams;
   p.lanes = s.lanes;
   p.stages = s.stages;
+  p.places = s.places;
   p.norm_y = n.norm_y;
   p.norm_r = n.norm_r;
   p.eps = n.eps;
@@ -632,9 +665,10 @@ static StepParams step_params(const sparsp_gated_norm& n, const StepPlan& s) {
   return p;
 }
 
-template <typename T, typename W, int V, bool kWarps, bool kNormY>
+template <typename T, typename W, int V, int kThreads, bool kNormY>
 static int launch_kind(const StepPlan& s, const StepParams& p, bool backward, cudaStream_t st) {
-  auto kern = backward ? step_back_kernel<T, W, V, kWarps, kNormY> : step_kernel<T, W, V, kWarps, kNormY>;
+  auto kern = backward ? step_back_kernel<T, W, V, kThreads == 320 ? 512 : kThreads, kNormY>
+                       : step_kernel<T, W, V, kThreads, kNormY>;
   SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, s.smem));
   SPARSP_CUDA_OK(launch_kernel(kern, dim3((unsigned)s.ctas), s.threads, (size_t)s.smem, st, p));
   return SPARSP_OK;
@@ -644,9 +678,13 @@ static int launch_pieces(const StepPlan& s, const StepParams& p, bool backward, 
   if constexpr (V * 16 / (int)sizeof(T) <= 16) {
     if (s.pieces > V) return launch_pieces<T, W, V + 1>(s, p, backward, st);
     const bool norm_y = p.norm_y != SPARSP_NORM_NONE;
-    if (s.by_warps)
-      return norm_y ? launch_kind<T, W, V, false, true>(s, p, backward, st) : launch_kind<T, W, V, false, false>(s, p, backward, st);
-    return norm_y ? launch_kind<T, W, V, true, true>(s, p, backward, st) : launch_kind<T, W, V, true, false>(s, p, backward, st);
+    auto kind = [&](auto threads) {
+      constexpr int kThreads = decltype(threads)::value;
+      return norm_y ? launch_kind<T, W, V, kThreads, true>(s, p, backward, st)
+                    : launch_kind<T, W, V, kThreads, false>(s, p, backward, st);
+    };
+    if (s.by_warps) return kind(std::integral_constant<int, 128>());
+    return s.threads <= 320 ? kind(std::integral_constant<int, 320>()) : kind(std::integral_constant<int, 512>());
   } else {
     return SPARSP_ERR_UNSUPPORTED;  // (plan_step has no more pieces)
   }
