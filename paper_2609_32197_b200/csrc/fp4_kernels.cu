@@ -491,18 +491,18 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 
 // ---- product of a few rows ------------------------------------------------------------------------------------------
 // With up to 128 rows the call is one pass over B, and a 256-row tile of A would be mostly padding.  Here B's rows are the
-// rows of the tile and A's its columns: D = B A^T, 128 rows by the rows of A, rounded up to 16.  The stages of 256
-// elements of K of all tiles, one behind the other, are shared out evenly: a CTA has a run of them, so that all load the
-// same, however many tiles there are.  A tile that several runs touch is in pieces in the workspace, which the CTA that
-// comes last (a count tells) adds in their order: the same bits, whoever that is, and nobody waits for anybody.
+// rows of the tile and A's its columns: D = B A^T, 128 rows by the rows of A, rounded up to 16.  A CTA has whole tiles,
+// where there are some for half of the SMs: these load as fast as memory gives.  With fewer, a tile's K is shared out to
+// `pieces` CTAs, whose sums meet in the workspace: the one that comes last (a count tells) adds them in their order, the
+// same bits whoever that is, and nobody waits for anybody.
 struct FewParams {
   const void* bias;
   void* c;
   int64_t ld_c;
-  float* partial;      // [2 slots of each CTA][columns][128]
-  uint32_t* counts;    // of pieces that are there, at the place of the first CTA that has one
+  float* partial;    // [CTA][columns][128]
+  uint32_t* counts;  // of a tile's pieces that are there
   int32_t rows, cols, depth, columns;
-  int32_t tiles, k_blocks, stages, stage_bytes;
+  int32_t tiles, k_blocks, pieces, stages, stage_bytes;
   float factor;
   uint32_t idesc;
   int32_t* status;
@@ -512,15 +512,6 @@ constexpr int kFewRows = 128;
 constexpr int kFewThreads = 192;  // loads, products, four warps of results
 constexpr int kFewSmem = 220 * 1024;
 constexpr int kFewScalesAt = 256;  // column of tensor memory: two accumulators of 128, then scales
-
-// The run of stages of a CTA.
-__host__ __device__ inline int64_t run_begin(int64_t units, int cta, int ctas) { return units * cta / ctas; }
-// the CTA that has a stage
-__device__ __forceinline__ int owner_of(int64_t units, int64_t unit, int ctas) {
-  int c = (int)(unit * ctas / units);
-  while (run_begin(units, c + 1, ctas) <= unit) ++c;
-  return c;
-}
 
 template <typename T, int kFormat>
 __global__ void __launch_bounds__(kFewThreads, 1)
@@ -557,31 +548,38 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   tc_fence_after();
   const uint32_t tmem = tmem_slot;
   enter_grid(p.bias);  // (after tensor memory is ours, as above)
-  const int N = p.columns, blocks = p.k_blocks;
-  const int64_t units = (int64_t)p.tiles * blocks;
-  const int64_t lo = run_begin(units, blockIdx.x, gridDim.x), hi = run_begin(units, blockIdx.x + 1, gridDim.x);
-  const int first_tile = (int)(lo / blocks);
+  const int N = p.columns;
+  // tiles [t0, t1), blocks of K [k0, k1) of each
+  int t0 = blockIdx.x, t1 = t0 + 1, k0 = 0, k1 = p.k_blocks;
+  if (p.pieces > 1) {
+    t0 = blockIdx.x / p.pieces;
+    t1 = t0 + 1;
+    const int piece = blockIdx.x - t0 * p.pieces;
+    k0 = p.k_blocks * piece / p.pieces;
+    k1 = p.k_blocks * (piece + 1) / p.pieces;
+  } else {
+    t0 = (int)((int64_t)p.tiles * blockIdx.x / gridDim.x);
+    t1 = (int)((int64_t)p.tiles * (blockIdx.x + 1) / gridDim.x);
+  }
 
   if (warp == 0) {
     if (elect_one()) {
-      int s = 0, tile = first_tile, k = (int)(lo - (int64_t)first_tile * blocks);
+      int s = 0;
       uint32_t round = 0;
-      for (int64_t unit = lo; unit < hi; ++unit) {
-        mbar_wait_bounded_inline(empty + s, round ^ 1u, s_abort, 31, p.wait_limit);
-        if (*s_abort) break;
-        uint8_t* at = smem + s * p.stage_bytes;
-        mbar_expect_tx(full + s, p.stage_bytes);
-        tma_load_2d(at, &mb, full + s, k * 128, tile * kRows);
-        tma_load_3d(at + kRows * 128 + N * 128, &msb, full + s, 0, k * kGroups, tile);
-        tma_load_2d(at + kRows * 128, &ma, full + s, k * 128, 0);
-        tma_load_3d(at + kRows * 128 + N * 128 + kScales, &msa, full + s, 0, k * kGroups, 0);
-        if (++k == blocks) {
-          k = 0;
-          ++tile;
-        }
-        if (++s == p.stages) {
-          s = 0;
-          round ^= 1u;
+      for (int tile = t0; tile < t1 && !*s_abort; ++tile) {
+        for (int k = k0; k < k1; ++k) {
+          mbar_wait_bounded_inline(empty + s, round ^ 1u, s_abort, 31, p.wait_limit);
+          if (*s_abort) break;
+          uint8_t* at = smem + s * p.stage_bytes;
+          mbar_expect_tx(full + s, p.stage_bytes);
+          tma_load_2d(at, &mb, full + s, k * 128, tile * kRows);
+          tma_load_3d(at + kRows * 128 + N * 128, &msb, full + s, 0, k * kGroups, tile);
+          tma_load_2d(at + kRows * 128, &ma, full + s, k * 128, 0);
+          tma_load_3d(at + kRows * 128 + N * 128 + kScales, &msa, full + s, 0, k * kGroups, 0);
+          if (++s == p.stages) {
+            s = 0;
+            round ^= 1u;
+          }
         }
       }
       if (*s_abort) {  // copies still in flight are waited for, within the same limit
@@ -598,43 +596,39 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       const uint32_t base = smem_u32(smem), scales = base + kRows * 128 + N * 128;
       const uint64_t db = make_smem_desc(base, 16u, 1024u), da = make_smem_desc(base + kRows * 128, 16u, 1024u);
       const uint64_t dsb = make_scale_desc(scales), dsa = make_scale_desc(scales + kScales);
-      int s = 0, acc = 0, set = 0, k = (int)(lo - (int64_t)first_tile * blocks);
+      int s = 0, acc = 0, set = 0;
       uint32_t round = 0, acc_round = 0;
-      bool fresh = true;
-      for (int64_t unit = lo; unit < hi && !*s_abort; ++unit) {
-        if (fresh) mbar_wait_bounded_inline(acc_read + acc, acc_round ^ 1u, s_abort, 32, p.wait_limit);
-        if (!mbar_wait_bounded_inline(full + s, round, s_abort, 33, p.wait_limit)) break;
-        tc_fence_after();
-        const uint64_t off = (uint64_t)((s * p.stage_bytes) >> 4);
-        const uint32_t sb = tmem + kFewScalesAt + set * (8 * kGroups), sa = sb + 4 * kGroups;
+      for (int tile = t0; tile < t1 && !*s_abort; ++tile) {
+        mbar_wait_bounded_inline(acc_read + acc, acc_round ^ 1u, s_abort, 32, p.wait_limit);
+        for (int k = k0; k < k1; ++k) {
+          if (!mbar_wait_bounded_inline(full + s, round, s_abort, 33, p.wait_limit)) break;
+          tc_fence_after();
+          const uint64_t off = (uint64_t)((s * p.stage_bytes) >> 4);
+          const uint32_t sb = tmem + kFewScalesAt + set * (8 * kGroups), sa = sb + 4 * kGroups;
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-          copy_scales(sb + 4 * g, dsb + off + g * 32);
-          copy_scales(sa + 4 * g, dsa + off + g * 32);
-        }
-        const int steps = min(4, (p.depth - k * kDeep + 63) / 64);
+          for (int g = 0; g < kGroups; ++g) {
+            copy_scales(sb + 4 * g, dsb + off + g * 32);
+            copy_scales(sa + 4 * g, dsa + off + g * 32);
+          }
+          const int steps = min(4, (p.depth - k * kDeep + 63) / 64);
 #pragma unroll
-        for (int kk = 0; kk < 4; ++kk) {
-          if (kk >= steps) break;
-          const int g = kk * kGroups / 4;
-          const uint32_t half = kGroups == 2 && (kk & 1) ? (2u << 4) | (2u << 29) : 0u;
-          mma_fp4<kFormat == SPARSP_MXFP4>(tmem + acc * 128, db + off + kk * 2, da + off + kk * 2, p.idesc | half, sb + 4 * g,
-                                           sa + 4 * g, !fresh || kk > 0);
+          for (int kk = 0; kk < 4; ++kk) {
+            if (kk >= steps) break;
+            const int g = kk * kGroups / 4;
+            const uint32_t half = kGroups == 2 && (kk & 1) ? (2u << 4) | (2u << 29) : 0u;
+            mma_fp4<kFormat == SPARSP_MXFP4>(tmem + acc * 128, db + off + kk * 2, da + off + kk * 2, p.idesc | half,
+                                             sb + 4 * g, sa + 4 * g, k > k0 || kk > 0);
+          }
+          mma_commit(empty + s);
+          set ^= 1;
+          if (++s == p.stages) {
+            s = 0;
+            round ^= 1u;
+          }
         }
-        mma_commit(empty + s);
-        set ^= 1;
-        fresh = false;
-        if (++k == blocks || unit + 1 == hi) {
-          mma_commit(acc_full + acc);
-          acc ^= 1;
-          if (acc == 0) acc_round ^= 1u;
-          fresh = true;
-        }
-        if (k == blocks) k = 0;
-        if (++s == p.stages) {
-          s = 0;
-          round ^= 1u;
-        }
+        mma_commit(acc_full + acc);
+        acc ^= 1;
+        if (acc == 0) acc_round ^= 1u;
       }
       mma_commit(&drained);
       const long long t0 = clock64();
@@ -648,24 +642,22 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     uint32_t acc_round = 0;
     // No way out before the last tile: the four warps meet at barrier 1, and pieces are counted, also after a wait that
     // ran out.  Waits return at once then.
-    for (int64_t unit = lo; unit < hi;) {
-      const int tile = (int)(unit / blocks);
-      const int64_t begin = (int64_t)tile * blocks, end = begin + blocks;
-      const bool whole = lo <= begin && end <= hi;
+    for (int tile = t0; tile < t1; ++tile) {
       mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 34, p.wait_limit);
       tc_fence_after();
       const int col = tile * kRows + in_tile;
       const float bias = p.bias != nullptr && col < p.cols ? to_float(static_cast<const T*>(p.bias)[col]) : 0.0f;
-      float* mine = p.partial + ((int64_t)(2 * blockIdx.x + (tile != first_tile)) * N) * kRows + in_tile;
-      for (int n = 0; n < N; n += 16) {
+      float* mine = p.partial + (int64_t)blockIdx.x * N * kRows + in_tile;
+      for (int n = 0; n < p.rows; n += 16) {
         float x[16];
         tmem_ld16(tmem + acc * 128 + n + ((uint32_t)(quarter * 32) << 16), reinterpret_cast<uint32_t*>(x));
         tmem_ld_wait(x);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          if (!whole)
+          if (n + i >= p.rows) break;
+          if (p.pieces > 1)
             mine[(n + i) * kRows] = x[i];
-          else if (n + i < p.rows && col < p.cols)
+          else if (col < p.cols)
             c[(n + i) * p.ld_c + col] = from_float<T>(fmaf(x[i], p.factor, bias));
         }
       }
@@ -674,28 +666,30 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       if (lane == 0) mbar_arrive(acc_read + acc);
       acc ^= 1;
       if (acc == 0) acc_round ^= 1u;
-      if (!whole) {
-        const int c0 = owner_of(units, begin, gridDim.x), c1 = owner_of(units, end - 1, gridDim.x);
+      if (p.pieces > 1) {
         __threadfence();
         asm volatile("bar.sync 1, 128;" ::: "memory");
         if (threadIdx.x == 64) {
-          s_last = atomicAdd(p.counts + c0, 1u) == (uint32_t)(c1 - c0);
-          if (s_last) p.counts[c0] = 0;
+          s_last = atomicAdd(p.counts + tile, 1u) == (uint32_t)p.pieces - 1;
+          if (s_last) p.counts[tile] = 0;
         }
         asm volatile("bar.sync 1, 128;" ::: "memory");
         if (s_last) {
           __threadfence();
-          // the tile is the last of its first CTA's run, the first of the others'
-          const int64_t behind = (int64_t)(run_begin(units, c0, gridDim.x) < begin) * N * kRows;
-          for (int n = 0; n < p.rows; ++n) {
-            const float* from = p.partial + ((int64_t)2 * c0 * N + n) * kRows + in_tile;
-            float sum = __ldcg(from + behind);
-            for (int q = c0 + 1; q <= c1; ++q) sum += __ldcg(from + (int64_t)2 * (q - c0) * N * kRows);
-            if (col < p.cols) c[n * p.ld_c + col] = from_float<T>(fmaf(sum, p.factor, bias));
+          const float* from = p.partial + (int64_t)tile * p.pieces * N * kRows + in_tile;
+          for (int n = 0; n < p.rows; n += 8) {  // (rows past the last are there in each piece's place)
+            float sum[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+            for (int q = 0; q < p.pieces; ++q)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) sum[i] += __ldcg(from + ((int64_t)q * N + n + i) * kRows);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (n + i < p.rows && col < p.cols) c[(n + i) * p.ld_c + col] = from_float<T>(fmaf(sum[i], p.factor, bias));
           }
         }
       }
-      unit = end;
     }
   }
   __syncwarp();
@@ -732,11 +726,11 @@ static int make_result_map(CUtensorMap* out, int dtype, const void* base, int64_
                      2, base, dims, strides, box, e == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
-// Few rows: the status words, counts, then two pieces of a CTA's run.  Never less for more rows.
+// Few rows: the status words, counts, then a piece of each CTA.  Never less for more rows.
 constexpr int kCountsAt = 256, kPartialAt = 1024;
 static int64_t few_columns(int64_t rows) { return align_up(std::min<int64_t>(std::max<int64_t>(rows, 1), kFewRows), 16); }
 int64_t fp4_product_workspace_bytes(const sparsp_fp4_gemm& f) {
-  return kPartialAt + 2 * kSms * few_columns(f.rows) * kRows * 4;
+  return kPartialAt + kSms * few_columns(f.rows) * kRows * 4;
 }
 
 template <typename T, int kFormat>
@@ -768,11 +762,11 @@ static int launch_few_rows(const sparsp_fp4_gemm& f, const void* A, const void* 
   if ((rc = make_codes_map(&mb, B, f.cols, f.depth / 2, kRows)) != SPARSP_OK) return rc;
   if ((rc = make_scales_map(&msa, As, f.rows, groups, kGroups, 1)) != SPARSP_OK) return rc;
   if ((rc = make_scales_map(&msb, Bs, f.cols, groups, kGroups, 1)) != SPARSP_OK) return rc;
-  const int64_t units = (int64_t)p.tiles * p.k_blocks;
+  p.pieces = p.tiles * 2 > kSms ? 1 : std::min(p.k_blocks, kSms / p.tiles);
   auto kern = few_rows_kernel<T, kFormat>;
   const int smem = p.stages * p.stage_bytes + 1024;
   SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, smem));
-  SPARSP_CUDA_OK(launch_kernel(kern, dim3((unsigned)std::min<int64_t>(units, kSms)), kFewThreads, (size_t)smem, st, ma, mb,
+  SPARSP_CUDA_OK(launch_kernel(kern, dim3((unsigned)std::min(p.tiles * p.pieces, kSms)), kFewThreads, (size_t)smem, st, ma, mb,
                                msa, msb, p));
   return SPARSP_OK;
 }
