@@ -637,7 +637,7 @@ SPARSP_API int sparsp_fp4_product_workspace_bytes(const sparsp_fp4_gemm* product
  *   B, B_scales   in   of B [cols][depth]: a projection's weight as it lies
  *   bias          in   [cols]; may be NULL
  *   C             out  [rows][cols], row stride stride_c; no input
- *   workspace     in   sparsp_fp4_product_workspace_bytes() bytes, 256-byte aligned, its first 1024 bytes zero before the
+ *   workspace     in   sparsp_fp4_product_workspace_bytes() bytes, 256-byte aligned, its first 256 bytes zero before the
  *                      first call; calls that may run at the same time take one each
  * All pointers but the workspace are 16-byte aligned. */
 SPARSP_API int sparsp_fp4_product(const sparsp_fp4_gemm* product, const void* A, const void* A_scales, const void* B,

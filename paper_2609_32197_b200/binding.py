@@ -701,7 +701,7 @@ def sparsp_fp4_product_workspace_bytes(product: sparsp_fp4_gemm) -> int:
 
 def make_fp4_product_workspace(product: sparsp_fp4_gemm, device="cuda") -> torch.Tensor:
     ws = torch.empty(sparsp_fp4_product_workspace_bytes(product), dtype=torch.uint8, device=device)
-    ws[:1024].zero_()
+    ws[:256].zero_()
     return ws
 
 

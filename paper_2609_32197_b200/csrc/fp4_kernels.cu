@@ -216,7 +216,7 @@ int launch_fp4_quantize(const sparsp_fp4& f, const void* X, uint8_t* codes, uint
 }
 
 // ---- product --------------------------------------------------------------------------------------------------------
-// C = A B^T + bias.  A pair of CTAs (a cluster of two, tcgen05 cta_group::2) makes a tile of 256 rows x 256 columns: each
+// C = A B^T + bias.  A pair of CTAs (a cluster of two, tcgen05 cta_group::2) makes a tile of 256 rows x BN columns: each
 // loads 128 rows of A and half of B's rows by TMA, the even CTA issues the MMAs for both, and each finds its 128 rows,
 // all columns, in its own tensor memory.  Scales go from shared to tensor memory by tcgen05.cp before the MMAs that
 // read them: a CTA has those of its rows of A and of all of the tile's rows of B.
@@ -240,22 +240,24 @@ constexpr int kRows = 128;  // of one CTA
 constexpr long long kWaitLimit = 200000000LL;  // of a wait in a kernel: about 0.1 s of SM clocks
 constexpr int kPairs = kSms / 2;
 
-template <int kFormat, typename T>
+template <int kFormat, typename T, int BN>
 struct ProductCfg {
   static constexpr int kGroups = kDeep / (4 * fp4_block(kFormat));  // of four blocks, of a stage
-  static constexpr int kA = kRows * 128, kB = kRows * 128;
-  static constexpr int kScalesA = kGroups * 512, kScalesB = 2 * kGroups * 512;
-  static constexpr int kStage = kA + kB + kScalesA + kScalesB;  // (6144 or 3072 of scales: tiles stay 1024 apart)
+  static constexpr int kA = kRows * 128, kB = BN / 2 * 128;
+  static constexpr int kTilesB = BN / 128;  // of scales
+  static constexpr int kScalesA = kGroups * 512, kScalesB = kTilesB * kGroups * 512;
+  static constexpr int kStage = kA + kB + kScalesA + kScalesB;
   static constexpr int kTurn = sizeof(T) * 32 * 32;             // a warp's results on their way out
   static constexpr int kStages = (227 * 1024 - 1024 - 256 - kResultWarps * kTurn) / kStage;
   static constexpr int kOffOut = kStages * kStage, kOffBars = kOffOut + kResultWarps * kTurn;
   static constexpr int kBars = 2 * kStages + 7;
   static constexpr int kDynamic = kOffBars + kBars * 8 + 16 + 1024;  // the tiles are aligned to 1024 bytes
-  static constexpr int kScaleCols = kGroups * 12;                    // of tensor memory: 4 of A, 8 of B a group
+  static constexpr int kScaleCols = kGroups * (4 + 4 * kTilesB);     // of tensor memory: 4 of A, 4 or 8 of B a group
   static constexpr int kScaleSets = 64 / kScaleCols;
+  static constexpr int kAccStep = BN == 256 ? 192 : 128;
+  static_assert(kStage % 1024 == 0, "tiles stay 1024 bytes apart");
 };
-static_assert(ProductCfg<SPARSP_MXFP4, float>::kStage % 1024 == 0 && ProductCfg<SPARSP_NVFP4, float>::kStage % 1024 == 0, "");
-constexpr int kAccStep = 192, kScaleAt = 448;  // columns of tensor memory: accumulators at 0 and 192, then scales
+constexpr int kScaleAt = 448;  // column of tensor memory: behind accumulators at 0 and 192 (of 256) or 128 (of 128)
 
 // Instruction descriptor: e2m1 operands, both K-major; bit 23 says that scales are powers of two.
 static uint32_t fp4_instruction(int format, int M, int N) {
@@ -304,13 +306,14 @@ __device__ __forceinline__ void finish(float (&x)[32], float factor, const T* bi
   }
 }
 
-template <typename T, int kFormat>
+template <typename T, int kFormat, int BN>
 __global__ void __launch_bounds__(kProductThreads, 1)
     product_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
                    const __grid_constant__ CUtensorMap msa, const __grid_constant__ CUtensorMap msb,
                    const __grid_constant__ CUtensorMap mc, const ProductParams p) {
   using namespace ptx;
-  using C = ProductCfg<kFormat, T>;
+  using C = ProductCfg<kFormat, T, BN>;
+  constexpr bool kOverlap = BN == 256;
   extern __shared__ uint8_t dynamic[];
   uint8_t* smem = dynamic + ((1024 - (smem_u32(dynamic) & 1023)) & 1023);
   uint64_t* full = reinterpret_cast<uint64_t*>(smem + C::kOffBars);  // of the even CTA: both CTAs' tiles have arrived
@@ -372,9 +375,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
           uint8_t* at = smem + s * C::kStage;
           const uint32_t bar = cluster_addr(full + s, 0);
           tma_load_pair(at, &ma, bar, k * 128, (m * 2 + (int)rank) * kRows);
-          tma_load_pair(at + C::kA, &mb, bar, k * 128, (n * 2 + (int)rank) * kRows);
+          tma_load_pair(at + C::kA, &mb, bar, k * 128, (n * 2 + (int)rank) * (BN / 2));
           tma_load_pair_3d(at + C::kA + C::kB, &msa, bar, 0, k * C::kGroups, m * 2 + (int)rank);
-          tma_load_pair_3d(at + C::kA + C::kB + C::kScalesA, &msb, bar, 0, k * C::kGroups, n * 2);
+          tma_load_pair_3d(at + C::kA + C::kB + C::kScalesA, &msb, bar, 0, k * C::kGroups, n * C::kTilesB);
           if (++s == C::kStages) {
             s = 0;
             round ^= 1u;
@@ -401,7 +404,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
       for (int tile = blockIdx.x >> 1; tile < tiles && !*s_abort; tile += pairs) {
         // this accumulator's last tile has been read, and of the other's, which is read now, what the two share
         mbar_wait_bounded_inline(acc_read + acc, acc_round ^ 1u, s_abort, 22, p.wait_limit);
-        mbar_wait_bounded_inline(shared_read + (acc ^ 1), acc == 0 ? acc_round ^ 1u : acc_round, s_abort, 23, p.wait_limit);
+        if (kOverlap)
+          mbar_wait_bounded_inline(shared_read + (acc ^ 1), acc == 0 ? acc_round ^ 1u : acc_round, s_abort, 23, p.wait_limit);
         tc_fence_after();
         for (int k = 0; k < p.k_blocks; ++k) {
           if (!mbar_wait_bounded_inline(full + s, round, s_abort, 24, p.wait_limit)) break;
@@ -411,8 +415,9 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 #pragma unroll
           for (int g = 0; g < C::kGroups; ++g) {
             copy_scales_pair(sa + 4 * g, dsa + off + g * 32);
-            copy_scales_pair(sb + 8 * g, dsb + off + g * 32);
-            copy_scales_pair(sb + 8 * g + 4, dsb + off + (C::kGroups + g) * 32);
+#pragma unroll
+            for (int t = 0; t < C::kTilesB; ++t)
+              copy_scales_pair(sb + 4 * (C::kTilesB * g + t), dsb + off + (C::kGroups * t + g) * 32);
           }
           const int steps = min(4, (p.depth - k * kDeep + 63) / 64);
 #pragma unroll
@@ -421,8 +426,8 @@ __global__ void __launch_bounds__(kProductThreads, 1)
             const int g = kk * C::kGroups / 4;
             // MXFP4: a group of four blocks serves two instructions, the second half of it the second
             const uint32_t half = C::kGroups == 2 && (kk & 1) ? (2u << 4) | (2u << 29) : 0u;
-            mma_fp4_pair<kFormat == SPARSP_MXFP4>(tmem + acc * kAccStep, da + off + kk * 2, db + off + kk * 2, p.idesc | half,
-                                                  sa + 4 * g, sb + 8 * g, k > 0 || kk > 0);
+            mma_fp4_pair<kFormat == SPARSP_MXFP4>(tmem + acc * C::kAccStep, da + off + kk * 2, db + off + kk * 2,
+                                                  p.idesc | half, sa + 4 * g, sb + 4 * C::kTilesB * g, k > 0 || kk > 0);
           }
           mma_commit_pair(empty + s);
           set = set + 1 == C::kScaleSets ? 0 : set + 1;
@@ -438,7 +443,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
       mma_commit_pair(drained);
     }
   } else {
-    // ---- results: warp w has the lanes of quarter w % 4, and 64 columns ----
+    // ---- results: warp w has the lanes of quarter w % 4, and a quarter of the columns ----
     const int quarter = warp & 3, side = warp >> 2;
     uint8_t* mine = smem + C::kOffOut + warp * C::kTurn;
     int acc = 1;
@@ -451,23 +456,25 @@ __global__ void __launch_bounds__(kProductThreads, 1)
       mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 25, p.wait_limit);
       if (__any_sync(0xffffffffu, *s_abort != 0)) break;  // (the same for all lanes)
       tc_fence_after();
-      const uint32_t from = tmem + acc * kAccStep + side * 64 + ((uint32_t)(quarter * 32) << 16);
-      float x[32], y[32];
-      tmem_ld32(from, reinterpret_cast<uint32_t*>(x));
-      tmem_ld32(from + 32, reinterpret_cast<uint32_t*>(y));
-      tmem_ld_wait(x);
-      tmem_ld_wait(y);
+      constexpr int kMine = BN / 4;  // columns
+      const uint32_t from = tmem + acc * C::kAccStep + side * kMine + ((uint32_t)(quarter * 32) << 16);
+      float x[kMine / 32][32];
+#pragma unroll
+      for (int h = 0; h < kMine / 32; ++h) tmem_ld32(from + h * 32, reinterpret_cast<uint32_t*>(x[h]));
+#pragma unroll
+      for (int h = 0; h < kMine / 32; ++h) tmem_ld_wait(x[h]);
       tc_fence_before();
       __syncwarp();
       if (lane == 0) {
-        if (side == (acc == 0 ? 3 : 0)) mbar_arrive_cluster(cluster_addr(shared_read + acc, 0));
+        if (kOverlap && side == (acc == 0 ? 3 : 0)) mbar_arrive_cluster(cluster_addr(shared_read + acc, 0));
         mbar_arrive_cluster(cluster_addr(acc_read + acc, 0));
       }
-      const int row = (m * 2 + (int)rank) * kRows + quarter * 32, col = n * 256 + side * 64;
-      finish(x, p.factor, static_cast<const T*>(p.bias), col, p.cols);
-      write_out<T>(&mc, mine, x, lane, col, row, p.cols, p.rows);
-      finish(y, p.factor, static_cast<const T*>(p.bias), col + 32, p.cols);
-      write_out<T>(&mc, mine, y, lane, col + 32, row, p.cols, p.rows);
+      const int row = (m * 2 + (int)rank) * kRows + quarter * 32, col = n * BN + side * kMine;
+#pragma unroll
+      for (int h = 0; h < kMine / 32; ++h) {
+        finish(x[h], p.factor, static_cast<const T*>(p.bias), col + h * 32, p.cols);
+        write_out<T>(&mc, mine, x[h], lane, col + h * 32, row, p.cols, p.rows);
+      }
     }
     if (lane == 0) tma_store_wait();
   }
@@ -492,24 +499,22 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 // ---- product of a few rows ------------------------------------------------------------------------------------------
 // With up to 128 rows the call is one pass over B, and a 256-row tile of A would be mostly padding.  Here B's rows are the
 // rows of the tile and A's its columns: D = B A^T, 128 rows by the rows of A, rounded up to 16.  A CTA has whole tiles,
-// where there are some for half of the SMs: these load as fast as memory gives.  With fewer, a tile's K is shared out to
-// `pieces` CTAs, whose sums meet in the workspace: the one that comes last (a count tells) adds them in their order, the
-// same bits whoever that is, and nobody waits for anybody.
+// where there are some for half of the SMs: these load as fast as memory gives.  With fewer, a cluster of CTAs shares
+// out a tile's K, and each adds some of the rows from the others' shared memory.
 struct FewParams {
   const void* bias;
   void* c;
   int64_t ld_c;
-  float* partial;    // [CTA][columns][128]
-  uint32_t* counts;  // of a tile's pieces that are there
   int32_t rows, cols, depth, columns;
-  int32_t tiles, k_blocks, pieces, stages, stage_bytes;
+  int32_t tiles, k_blocks, pieces, stages, stage_bytes;  // pieces: CTAs of a cluster
   float factor;
   uint32_t idesc;
   int32_t* status;
   long long wait_limit;
 };
 constexpr int kFewRows = 128;
-constexpr int kFewThreads = 192;  // loads, products, four warps of results
+constexpr int kFewWarps = 8;  // of results
+constexpr int kFewThreads = 64 + 32 * kFewWarps;
 constexpr int kFewSmem = 220 * 1024;
 constexpr int kFewScalesAt = 256;  // column of tensor memory: two accumulators of 128, then scales
 
@@ -523,7 +528,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   uint8_t* smem = dynamic + ((1024 - (smem_u32(dynamic) & 1023)) & 1023);
   __shared__ uint64_t full[16], empty[16], acc_full[2], acc_read[2], drained;
   __shared__ uint32_t tmem_slot;
-  __shared__ int abort_word, s_last;
+  __shared__ int abort_word;
   volatile int* s_abort = &abort_word;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   if (threadIdx.x == 0) {
@@ -533,7 +538,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     }
     for (int a = 0; a < 2; ++a) {
       mbar_init(acc_full + a, 1);
-      mbar_init(acc_read + a, 4);
+      mbar_init(acc_read + a, kFewWarps);
     }
     mbar_init(&drained, 1);
     *s_abort = 0;
@@ -549,6 +554,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
   const uint32_t tmem = tmem_slot;
   enter_grid(p.bias);  // (after tensor memory is ours, as above)
   const int N = p.columns;
+  float* sums = reinterpret_cast<float*>(smem);  // [rows of A][128], after the products
   // tiles [t0, t1), blocks of K [k0, k1) of each
   int t0 = blockIdx.x, t1 = t0 + 1, k0 = 0, k1 = p.k_blocks;
   if (p.pieces > 1) {
@@ -636,29 +642,29 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       }
     }
   } else {
-    const int quarter = warp & 3, in_tile = quarter * 32 + lane;
+    // warp w has the lanes of quarter w % 4, and every other 16 columns
+    const int quarter = warp & 3, side = (warp - 2) >> 2, in_tile = quarter * 32 + lane;
     T* c = static_cast<T*>(p.c);
     int acc = 0;
     uint32_t acc_round = 0;
-    // No way out before the last tile: the four warps meet at barrier 1, and pieces are counted, also after a wait that
-    // ran out.  Waits return at once then.
     for (int tile = t0; tile < t1; ++tile) {
       mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 34, p.wait_limit);
       tc_fence_after();
       const int col = tile * kRows + in_tile;
-      const float bias = p.bias != nullptr && col < p.cols ? to_float(static_cast<const T*>(p.bias)[col]) : 0.0f;
-      float* mine = p.partial + (int64_t)blockIdx.x * N * kRows + in_tile;
-      for (int n = 0; n < p.rows; n += 16) {
+      const bool in = col < p.cols;
+      const float bias = p.bias != nullptr && in ? to_float(static_cast<const T*>(p.bias)[col]) : 0.0f;
+      for (int n = side * 16; n < p.rows; n += 32) {
         float x[16];
         tmem_ld16(tmem + acc * 128 + n + ((uint32_t)(quarter * 32) << 16), reinterpret_cast<uint32_t*>(x));
         tmem_ld_wait(x);
+        if (p.pieces > 1) {  // (all of this CTA's products have ended: their stages are free)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          if (n + i >= p.rows) break;
-          if (p.pieces > 1)
-            mine[(n + i) * kRows] = x[i];
-          else if (col < p.cols)
-            c[(n + i) * p.ld_c + col] = from_float<T>(fmaf(x[i], p.factor, bias));
+          for (int i = 0; i < 16; ++i) sums[(n + i) * kRows + in_tile] = x[i];
+        } else if (in) {
+          T* to = c + (int64_t)n * p.ld_c + col;
+#pragma unroll
+          for (int i = 0; i < 16; ++i, to += p.ld_c)
+            if (n + i < p.rows) *to = from_float<T>(fmaf(x[i], p.factor, bias));
         }
       }
       tc_fence_before();
@@ -666,33 +672,29 @@ __global__ void __launch_bounds__(kFewThreads, 1)
       if (lane == 0) mbar_arrive(acc_read + acc);
       acc ^= 1;
       if (acc == 0) acc_round ^= 1u;
-      if (p.pieces > 1) {
-        __threadfence();
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (threadIdx.x == 64) {
-          s_last = atomicAdd(p.counts + tile, 1u) == (uint32_t)p.pieces - 1;
-          if (s_last) p.counts[tile] = 0;
-        }
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (s_last) {
-          __threadfence();
-          const float* from = p.partial + (int64_t)tile * p.pieces * N * kRows + in_tile;
-          for (int n = 0; n < p.rows; n += 8) {  // (rows past the last are there in each piece's place)
-            float sum[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
-            for (int q = 0; q < p.pieces; ++q)
-#pragma unroll
-              for (int i = 0; i < 8; ++i) sum[i] += __ldcg(from + ((int64_t)q * N + n + i) * kRows);
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-              if (n + i < p.rows && col < p.cols) c[(n + i) * p.ld_c + col] = from_float<T>(fmaf(sum[i], p.factor, bias));
-          }
-        }
-      }
     }
   }
   __syncwarp();
+  if (p.pieces > 1) {
+    cluster_sync();
+    if (warp >= 2) {
+      const int in_tile = (threadIdx.x - 64) & 127, col = t0 * kRows + in_tile;
+      const float bias = p.bias != nullptr && col < p.cols ? to_float(static_cast<const T*>(p.bias)[col]) : 0.0f;
+      // each half of the warps of each CTA has some of the rows, four at a time
+      const int share = 2 * (int)cluster_rank() + (int)(threadIdx.x - 64) / 128;
+      for (int n = share * 4; n < p.rows; n += 8 * p.pieces) {
+        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int q = 0; q < p.pieces; ++q)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[i] += ld_cluster(smem_u32(sums + (n + i) * kRows + in_tile), q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (n + i < p.rows && col < p.cols)
+            static_cast<T*>(p.c)[(n + i) * p.ld_c + col] = from_float<T>(fmaf(sum[i], p.factor, bias));
+      }
+    }
+    cluster_sync();  // nobody's memory goes before it has been read
+  }
   tc_fence_before();
   __syncthreads();
   if (warp == 1) {
@@ -726,12 +728,8 @@ static int make_result_map(CUtensorMap* out, int dtype, const void* base, int64_
                      2, base, dims, strides, box, e == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
-// Few rows: the status words, counts, then a piece of each CTA.  Never less for more rows.
-constexpr int kCountsAt = 256, kPartialAt = 1024;
-static int64_t few_columns(int64_t rows) { return align_up(std::min<int64_t>(std::max<int64_t>(rows, 1), kFewRows), 16); }
-int64_t fp4_product_workspace_bytes(const sparsp_fp4_gemm& f) {
-  return kPartialAt + kSms * few_columns(f.rows) * kRows * 4;
-}
+static int few_columns(int64_t rows) { return (int)align_up(std::min<int64_t>(std::max<int64_t>(rows, 1), kFewRows), 16); }
+int64_t fp4_product_workspace_bytes(const sparsp_fp4_gemm&) { return kStatusWords * 4; }
 
 template <typename T, int kFormat>
 static int launch_few_rows(const sparsp_fp4_gemm& f, const void* A, const void* As, const void* B, const void* Bs,
@@ -742,12 +740,10 @@ static int launch_few_rows(const sparsp_fp4_gemm& f, const void* A, const void* 
   p.bias = bias;
   p.c = C;
   p.ld_c = f.stride_c;
-  p.partial = reinterpret_cast<float*>(ws + kPartialAt);
-  p.counts = reinterpret_cast<uint32_t*>(ws + kCountsAt);
   p.rows = (int32_t)f.rows;
   p.cols = f.cols;
   p.depth = f.depth;
-  p.columns = (int32_t)few_columns(f.rows);
+  p.columns = few_columns(f.rows);
   p.tiles = ceil_div(f.cols, kRows);
   p.k_blocks = ceil_div(f.depth, kDeep);
   p.stage_bytes = (kRows + p.columns) * 128 + 2 * kGroups * 512;
@@ -762,26 +758,32 @@ static int launch_few_rows(const sparsp_fp4_gemm& f, const void* A, const void* 
   if ((rc = make_codes_map(&mb, B, f.cols, f.depth / 2, kRows)) != SPARSP_OK) return rc;
   if ((rc = make_scales_map(&msa, As, f.rows, groups, kGroups, 1)) != SPARSP_OK) return rc;
   if ((rc = make_scales_map(&msb, Bs, f.cols, groups, kGroups, 1)) != SPARSP_OK) return rc;
-  p.pieces = p.tiles * 2 > kSms ? 1 : std::min(p.k_blocks, kSms / p.tiles);
+  // 290 ns a block of K, and for sums that meet 1400 ns and 40 a row, which the pieces share (7680 x 1920, rows and us in
+  // one and in two pieces: 1 4.9 5.1, 32 5.0 6.0, 128 6.0 8.8; 5120 x 5120: 1 8.4 6.6, 64 8.9 8.6, 128 9.7 10.5; 1280 x
+  // 5120, also in four: 32 8.4 7.4 5.8, 128 9.4 10.1 7.5).  Clusters of four find room on 128 SMs, of two on all.
+  auto cost = [&](int pieces) { return 290 * p.k_blocks / pieces + (pieces > 1 ? 1400 + 40 * p.rows / pieces : 0); };
+  p.pieces = 1;
+  if (p.tiles * 2 <= kSms && p.k_blocks >= 2 && cost(2) < cost(1)) p.pieces = 2;
+  if (p.tiles * 4 <= 128 && p.k_blocks >= 4 && cost(4) < cost(p.pieces)) p.pieces = 4;
   auto kern = few_rows_kernel<T, kFormat>;
-  const int smem = p.stages * p.stage_bytes + 1024;
+  const int smem = std::max(p.stages * p.stage_bytes, p.columns * kRows * 4) + 1024;
   SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, smem));
-  SPARSP_CUDA_OK(launch_kernel(kern, dim3((unsigned)std::min(p.tiles * p.pieces, kSms)), kFewThreads, (size_t)smem, st, ma, mb,
-                               msa, msb, p));
+  SPARSP_CUDA_OK(launch_clusters(kern, dim3((unsigned)std::min(p.tiles * p.pieces, kSms)), p.pieces, kFewThreads,
+                                 (size_t)smem, st, ma, mb, msa, msb, p));
   return SPARSP_OK;
 }
 
-template <typename T, int kFormat>
+template <typename T, int kFormat, int BN>
 static int launch_pairs(const sparsp_fp4_gemm& f, const void* A, const void* As, const void* B, const void* Bs,
                         const void* bias, void* C, char* ws, cudaStream_t st) {
-  using Cfg = ProductCfg<kFormat, T>;
+  using Cfg = ProductCfg<kFormat, T, BN>;
   const int64_t groups = fp4_groups(f.depth, kFormat);
   CUtensorMap ma, mb, msa, msb, mc;
   int rc;
   if ((rc = make_codes_map(&ma, A, f.rows, f.depth / 2, kRows)) != SPARSP_OK) return rc;
-  if ((rc = make_codes_map(&mb, B, f.cols, f.depth / 2, kRows)) != SPARSP_OK) return rc;
+  if ((rc = make_codes_map(&mb, B, f.cols, f.depth / 2, BN / 2)) != SPARSP_OK) return rc;
   if ((rc = make_scales_map(&msa, As, f.rows, groups, Cfg::kGroups, 1)) != SPARSP_OK) return rc;
-  if ((rc = make_scales_map(&msb, Bs, f.cols, groups, Cfg::kGroups, 2)) != SPARSP_OK) return rc;
+  if ((rc = make_scales_map(&msb, Bs, f.cols, groups, Cfg::kGroups, Cfg::kTilesB)) != SPARSP_OK) return rc;
   if ((rc = make_result_map(&mc, f.dtype, C, f.rows, f.cols, f.stride_c)) != SPARSP_OK) return rc;
   ProductParams p = {};
   p.bias = bias;
@@ -789,32 +791,44 @@ static int launch_pairs(const sparsp_fp4_gemm& f, const void* A, const void* As,
   p.cols = f.cols;
   p.depth = f.depth;
   p.m_tiles = ceil_div(f.rows, 256);
-  p.n_tiles = ceil_div(f.cols, 256);
+  p.n_tiles = ceil_div(f.cols, BN);
   p.band = 8;
   p.k_blocks = ceil_div(f.depth, kDeep);
   p.factor = std::ldexp(1.0f, f.exponent);
-  p.idesc = fp4_instruction(kFormat, 256, 256);
+  p.idesc = fp4_instruction(kFormat, 256, BN);
   p.status = reinterpret_cast<int32_t*>(ws);
   p.wait_limit = kWaitLimit;
-  auto kern = product_kernel<T, kFormat>;
+  auto kern = product_kernel<T, kFormat, BN>;
   SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, Cfg::kDynamic));
   const unsigned grid = 2u * (unsigned)std::min(p.m_tiles * p.n_tiles, kPairs);
   SPARSP_CUDA_OK(launch_clusters(kern, dim3(grid), 2, kProductThreads, Cfg::kDynamic, st, ma, mb, msa, msb, mc, p));
   return SPARSP_OK;
 }
 
+// Tiles of 128 columns where these make fewer rounds: they take half the time of those of 256, but each value that they
+// load serves fewer products.
+static bool narrow_tiles(const sparsp_fp4_gemm& f) {
+  const int64_t m = ceil_div(f.rows, 256);
+  return 128 * 7 * ceil_div(m * ceil_div(f.cols, 128), kPairs) < 256 * 5 * ceil_div(m * ceil_div(f.cols, 256), kPairs);
+}
+
+template <typename T, int kFormat>
+static int launch_product(const sparsp_fp4_gemm& f, const void* A, const void* As, const void* B, const void* Bs,
+                          const void* bias, void* C, char* ws, cudaStream_t st) {
+  if (f.rows <= kFewRows) return launch_few_rows<T, kFormat>(f, A, As, B, Bs, bias, C, ws, st);
+  return narrow_tiles(f) ? launch_pairs<T, kFormat, 128>(f, A, As, B, Bs, bias, C, ws, st)
+                         : launch_pairs<T, kFormat, 256>(f, A, As, B, Bs, bias, C, ws, st);
+}
+
 int launch_fp4_product(const sparsp_fp4_gemm& f, const void* A, const void* As, const void* B, const void* Bs,
                        const void* bias, void* C, char* ws, cudaStream_t st) {
-  if ((int64_t)ceil_div(f.rows, 256) * ceil_div(f.cols, 256) > (1 << 30)) {
-    set_error("%d x %d tiles are too many", ceil_div(f.rows, 256), ceil_div(f.cols, 256));
+  if ((int64_t)ceil_div(f.rows, 256) * ceil_div(f.cols, 128) > (1 << 30)) {
+    set_error("%d x %d tiles are too many", ceil_div(f.rows, 256), ceil_div(f.cols, 128));
     return SPARSP_ERR_UNSUPPORTED;
   }
   SPARSP_WITH_TYPE(f.dtype, T, {
-    if (f.rows <= kFewRows)
-      return f.format == SPARSP_MXFP4 ? launch_few_rows<T, SPARSP_MXFP4>(f, A, As, B, Bs, bias, C, ws, st)
-                                      : launch_few_rows<T, SPARSP_NVFP4>(f, A, As, B, Bs, bias, C, ws, st);
-    return f.format == SPARSP_MXFP4 ? launch_pairs<T, SPARSP_MXFP4>(f, A, As, B, Bs, bias, C, ws, st)
-                                    : launch_pairs<T, SPARSP_NVFP4>(f, A, As, B, Bs, bias, C, ws, st);
+    return f.format == SPARSP_MXFP4 ? launch_product<T, SPARSP_MXFP4>(f, A, As, B, Bs, bias, C, ws, st)
+                                    : launch_product<T, SPARSP_NVFP4>(f, A, As, B, Bs, bias, C, ws, st);
   });
 }
 
