@@ -234,7 +234,7 @@ struct ProductParams {
 };
 
 constexpr int kDeep = 256;  // K elements of a stage: one 128-byte swizzled row
-constexpr int kResultWarps = 16;
+constexpr int kResultWarps = 8;
 constexpr int kProductThreads = 32 * (kResultWarps + 2);
 constexpr int kRows = 128;  // of one CTA
 constexpr long long kWaitLimit = 200000000LL;  // of a wait in a kernel: about 0.1 s of SM clocks
@@ -247,9 +247,12 @@ struct ProductCfg {
   static constexpr int kTilesB = BN / 128;  // of scales
   static constexpr int kScalesA = kGroups * 512, kScalesB = kTilesB * kGroups * 512;
   static constexpr int kStage = kA + kB + kScalesA + kScalesB;
-  static constexpr int kTurn = sizeof(T) * 32 * 32;             // a warp's results on their way out
-  static constexpr int kStages = (227 * 1024 - 1024 - 256 - kResultWarps * kTurn) / kStage;
-  static constexpr int kOffOut = kStages * kStage, kOffBars = kOffOut + kResultWarps * kTurn;
+  static constexpr int kTurn = 4096;            // a warp's results on their way out: 32 rows of 128 bytes
+  static constexpr int kMine = BN / 2;          // columns of a warp
+  static constexpr int kBias = kMine * 4;       // ... and their bias
+  static constexpr int kStages = (227 * 1024 - 1024 - 256 - kResultWarps * (kTurn + kBias)) / kStage;
+  static constexpr int kOffOut = kStages * kStage, kOffBias = kOffOut + kResultWarps * kTurn;
+  static constexpr int kOffBars = kOffBias + kResultWarps * kBias;
   static constexpr int kBars = 2 * kStages + 7;
   static constexpr int kDynamic = kOffBars + kBars * 8 + 16 + 1024;  // the tiles are aligned to 1024 bytes
   static constexpr int kScaleCols = kGroups * (4 + 4 * kTilesB);     // of tensor memory: 4 of A, 4 or 8 of B a group
@@ -265,44 +268,24 @@ static uint32_t fp4_instruction(int format, int M, int N) {
          ((uint32_t)(M >> 4) << 24);
 }
 
-// 32 rows x 32 columns of a warp, on their way out through its own shared memory (16-byte pieces of a row in turned
+// 32 rows x 128 bytes of a warp, on their way out through its own shared memory (16-byte pieces of a row in turned
 // places, so that lanes do not meet in a bank) as one TMA tile, which leaves out what lies beyond the tensor.
-template <typename T>
-__device__ __forceinline__ void write_out(const CUtensorMap* to, uint8_t* mine, const float (&x)[32], int lane, int col,
-                                          int row, int cols, int rows) {
-  constexpr int kPieces = sizeof(T) * 2, kEach = 32 / kPieces;
-  Vec<T, kEach> piece[kPieces];
+template <typename T, int N>
+__device__ __forceinline__ void write_out(const CUtensorMap* to, uint8_t* mine, const float (&x)[N], int first, int lane,
+                                          int col, int row, int cols, int rows) {
+  constexpr int kEach = 16 / sizeof(T);
+  Vec<T, kEach> piece[8];
 #pragma unroll
-  for (int i = 0; i < kPieces; ++i) piece[i].set(x + i * kEach);
+  for (int i = 0; i < 8; ++i) piece[i].set(x + first + i * kEach);
   if (lane == 0) ptx::tma_store_wait_read();
   __syncwarp();
 #pragma unroll
-  for (int i = 0; i < kPieces; ++i) {
-    const int at = sizeof(T) == 4 ? i ^ (lane & 7) : i ^ ((lane >> 1) & 3);
-    store_vec<T, kEach>(reinterpret_cast<T*>(mine + lane * (32 * sizeof(T)) + at * 16), piece[i]);
-  }
+  for (int i = 0; i < 8; ++i) store_vec<T, kEach>(reinterpret_cast<T*>(mine + lane * 128 + ((i ^ (lane & 7)) << 4)), piece[i]);
   ptx::fence_proxy_async_smem();
   __syncwarp();
   if (lane == 0 && col < cols && row < rows) {
     ptx::tma_store_2d(to, mine, col, row);
     ptx::tma_store_commit();
-  }
-}
-
-// x * factor + bias of 32 columns; columns past the last, of which there are multiples of 8, stay as they are
-template <typename T>
-__device__ __forceinline__ void finish(float (&x)[32], float factor, const T* bias, int col, int cols) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (bias != nullptr && col + i * 8 < cols) {
-      Eight<T> b;
-      b.load(bias + col + i * 8);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[8 * i + e] = fmaf(x[8 * i + e], factor, b[e]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) x[8 * i + e] *= factor;
-    }
   }
 }
 
@@ -443,9 +426,13 @@ __global__ void __launch_bounds__(kProductThreads, 1)
       mma_commit_pair(drained);
     }
   } else {
-    // ---- results: warp w has the lanes of quarter w % 4, and a quarter of the columns ----
+    // ---- results: warp w has the lanes of quarter w % 4, and half of the columns, 64 at a time ----
     const int quarter = warp & 3, side = warp >> 2;
     uint8_t* mine = smem + C::kOffOut + warp * C::kTurn;
+    float* held_bias = reinterpret_cast<float*>(smem + C::kOffBias + warp * C::kBias);
+    const T* bias = static_cast<const T*>(p.bias);
+    if (bias == nullptr)
+      for (int i = lane; i < C::kMine; i += 32) held_bias[i] = 0.0f;
     int acc = 1;
     uint32_t acc_round = 1;
     for (int tile = blockIdx.x >> 1; tile < tiles; tile += pairs) {
@@ -453,27 +440,43 @@ __global__ void __launch_bounds__(kProductThreads, 1)
       if (acc == 0) acc_round ^= 1u;
       int m, n;
       tile_at(tile, m, n);
+      const int row = (m * 2 + (int)rank) * kRows + quarter * 32, col = n * BN + side * C::kMine;
+      if (bias != nullptr) {  // while the products are made
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < C::kMine; i += 32) held_bias[i + lane] = col + i + lane < p.cols ? to_float(bias[col + i + lane]) : 0.0f;
+      }
+      __syncwarp();
       mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 25, p.wait_limit);
       if (__any_sync(0xffffffffu, *s_abort != 0)) break;  // (the same for all lanes)
       tc_fence_after();
-      constexpr int kMine = BN / 4;  // columns
-      const uint32_t from = tmem + acc * C::kAccStep + side * kMine + ((uint32_t)(quarter * 32) << 16);
-      float x[kMine / 32][32];
+      const uint32_t from = tmem + acc * C::kAccStep + side * C::kMine + ((uint32_t)(quarter * 32) << 16);
+      // first the columns that both accumulators share: the last of one, the first of the other
+      const int flip = kOverlap && acc == 0 ? 1 : 0;
+#pragma unroll 1
+      for (int h = 0; h < C::kMine / 64; ++h) {
+        const int at = (h ^ flip) * 64;
+        float x[64];
+        tmem_ld32(from + at, reinterpret_cast<uint32_t*>(x));
+        tmem_ld32(from + at + 32, reinterpret_cast<uint32_t*>(x + 32));
+        tmem_ld_wait(x);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) {
+          if (kOverlap && h == 0 && side == flip) mbar_arrive_cluster_relaxed(cluster_addr(shared_read + acc, 0));
+          if (h == C::kMine / 64 - 1) mbar_arrive_cluster_relaxed(cluster_addr(acc_read + acc, 0));
+        }
 #pragma unroll
-      for (int h = 0; h < kMine / 32; ++h) tmem_ld32(from + h * 32, reinterpret_cast<uint32_t*>(x[h]));
+        for (int i = 0; i < 64; i += 4) {
+          const float4 b = *reinterpret_cast<const float4*>(held_bias + at + i);
+          x[i] = fmaf(x[i], p.factor, b.x);
+          x[i + 1] = fmaf(x[i + 1], p.factor, b.y);
+          x[i + 2] = fmaf(x[i + 2], p.factor, b.z);
+          x[i + 3] = fmaf(x[i + 3], p.factor, b.w);
+        }
 #pragma unroll
-      for (int h = 0; h < kMine / 32; ++h) tmem_ld_wait(x[h]);
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) {
-        if (kOverlap && side == (acc == 0 ? 3 : 0)) mbar_arrive_cluster(cluster_addr(shared_read + acc, 0));
-        mbar_arrive_cluster(cluster_addr(acc_read + acc, 0));
-      }
-      const int row = (m * 2 + (int)rank) * kRows + quarter * 32, col = n * BN + side * kMine;
-#pragma unroll
-      for (int h = 0; h < kMine / 32; ++h) {
-        finish(x[h], p.factor, static_cast<const T*>(p.bias), col + h * 32, p.cols);
-        write_out<T>(&mc, mine, x[h], lane, col + h * 32, row, p.cols, p.rows);
+        for (int i = 0; i < 64; i += 128 / (int)sizeof(T))
+          write_out<T>(&mc, mine, x, i, lane, col + at + i, row, p.cols, p.rows);
       }
     }
     if (lane == 0) tma_store_wait();
@@ -720,12 +723,12 @@ static int make_scales_map(CUtensorMap* out, const void* base, int64_t rows, int
 static int make_result_map(CUtensorMap* out, int dtype, const void* base, int64_t rows, int64_t cols, int64_t ld) {
   const int e = element_bytes(dtype);
   const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * e};
-  const cuuint32_t box[2] = {32, 32};
+  const cuuint32_t box[2] = {128u / (unsigned)e, 32};
   return encode_tmap(out,
                      dtype == SPARSP_FP32   ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                      : dtype == SPARSP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                             : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                     2, base, dims, strides, box, e == 4 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
+                     2, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 static int few_columns(int64_t rows) { return (int)align_up(std::min<int64_t>(std::max<int64_t>(rows, 1), kFewRows), 16); }

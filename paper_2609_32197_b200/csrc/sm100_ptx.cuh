@@ -371,6 +371,10 @@ __device__ __forceinline__ float ld_cluster(uint32_t a, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+// ... where nothing in memory has to be seen by who waits: without the wait for this thread's earlier stores
+__device__ __forceinline__ void mbar_arrive_cluster_relaxed(uint32_t bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
 // 2-D tile load into this CTA's shared memory, completion counted on an mbarrier of either CTA of the pair.
 __device__ __forceinline__ void tma_load_pair(void* smem_dst, const CUtensorMap* m, uint32_t bar, int c0, int c1) {
   asm volatile(
