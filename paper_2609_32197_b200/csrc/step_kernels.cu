@@ -33,7 +33,7 @@ __host__ __device__ inline int64_t team_of(int64_t row, int64_t teams, int64_t r
 
 // Sums over a team, the same in every lane.  kWarps: the team is a CTA; its warps meet at one barrier a call, by turns
 // of `room`, whose places of warps that are not there are 0.
-constexpr int kMostWarps = 16;
+constexpr int kMostWarps = 20;
 template <bool kWarps, int N>
 __device__ __forceinline__ void team_sum(float (&v)[N], int lanes, float (*room)[2][kMostWarps], int& turn) {
 #pragma unroll
@@ -54,8 +54,10 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int lanes, float (*room)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float4* w = reinterpret_cast<const float4*>(at[i]);
-      const float4 a = w[0], b = w[1], c = w[2], d = w[3];
-      v[i] = ((a.x + a.y) + (a.z + a.w)) + ((b.x + b.y) + (b.z + b.w)) + (((c.x + c.y) + (c.z + c.w)) + ((d.x + d.y) + (d.z + d.w)));
+      float s[kMostWarps / 4];
+#pragma unroll
+      for (int k = 0; k < kMostWarps / 4; ++k) s[k] = (w[k].x + w[k].y) + (w[k].z + w[k].w);
+      v[i] = ((s[0] + s[1]) + (s[2] + s[3])) + s[4];
     }
   }
 }
@@ -319,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
 // t y), t; from these come all gradients of weights.  There are no registers for more: rows and weights stay in shared
 // memory and are read again for each step.
 template <typename T, typename W, int V, int kThreads, bool kNormY>
-__global__ void __launch_bounds__(kThreads) step_back_kernel(StepParams p) {
+__global__ void __launch_bounds__(kThreads, kThreads == 320 ? 2 : 1) step_back_kernel(StepParams p) {
   constexpr bool kWarps = kThreads > 128;  // teams of 128 threads or fewer in a CTA of their own have room for 320
   enter_grid(p.x, p.y, p.dn, p.dr, p.gate, p.wy, p.wr, p.stats_y, p.stats_r);
   constexpr int E = 16 / sizeof(T), kSums = kNormY ? 4 : 3, kPart = Weights<W, E>::kParts;
@@ -539,12 +541,14 @@ __global__ void __launch_bounds__(512) step_columns_kernel(StepParams p, int fou
   // the group is the last of its first team, and the first of the others
   const int64_t behind = !last && group * p.rows_per_group > first_row(t0, p.teams, p.rows) ? 1 : 0;
   float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  const int there = last ? 2 : p.norm_y != SPARSP_NORM_NONE ? 4 : 3;
   if (col < p.dim)
+#pragma unroll 4
     for (int64_t t = t0 + part; t < t1; t += 16) {
       const int64_t slot = last ? t : 2 * t + (t == t0 ? behind : 0);
 #pragma unroll
       for (int q = 0; q < 4; ++q)
-        if (q < (last ? 2 : p.norm_y != SPARSP_NORM_NONE ? 4 : 3)) s[q] += from[(slot * sums + q) * p.dim + col];
+        if (q < there) s[q] += from[(slot * sums + q) * p.dim + col];
     }
 #pragma unroll
   for (int q = 0; q < 4; ++q) room[part][q][lane] = s[q];
@@ -598,9 +602,12 @@ constexpr int kStepSmem = 228 * 1024;  // of a multiprocessor; each CTA has 1 KB
 
 static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
   StepPlan s;
-  const int each = 16 / element_bytes(n.dtype), vectors = n.dim / each, most = 16 / each;
+  const int each = 16 / element_bytes(n.dtype), vectors = n.dim / each;
   int64_t per_cta = 1;
-  s.by_warps = vectors <= 32 * most;
+  s.by_warps = n.dim <= 32 * 16;
+  // values of a thread, and threads that registers then hold: of a CTA, of a multiprocessor
+  const int values = backward && !s.by_warps && n.dim <= 640 * 8 ? 8 : 16, most = values / each;
+  const int most_threads = values == 8 ? 640 : 512, all_threads = backward && values == 16 ? 512 : 640;
   s.pieces = 1;
   if (s.by_warps) {  // a warp, or lanes of one
     s.pieces = (vectors + 31) / 32;
@@ -612,7 +619,7 @@ static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
     int best = 1 << 30;
     for (int v = 1; v <= most; ++v) {
       const int threads = (vectors + 32 * v - 1) / (32 * v) * 32;
-      if (threads <= 512 && threads * v <= best) {
+      if (threads <= most_threads && threads * v <= best) {
         best = threads * v;
         s.pieces = v;
         s.threads = threads;
@@ -621,7 +628,7 @@ static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
     s.lanes = s.threads;
   }
   // CTAs of a multiprocessor by what registers hold
-  int fit = std::max(1, (backward ? 512 : 640) / s.threads);
+  int fit = std::max(1, all_threads / s.threads);
   const int row = s.pieces * (backward ? 4 : 2);
   const int per_weight = std::max(1, element_bytes(n.weight_dtype) / element_bytes(n.dtype));
   const int held = backward ? s.pieces * per_weight * (n.norm_y != SPARSP_NORM_NONE ? 3 : 2) : 0;
@@ -665,26 +672,34 @@ static StepParams step_params(const sparsp_gated_norm& n, const StepPlan& s) {
   return p;
 }
 
-template <typename T, typename W, int V, int kThreads, bool kNormY>
-static int launch_kind(const StepPlan& s, const StepParams& p, bool backward, cudaStream_t st) {
-  auto kern = backward ? step_back_kernel<T, W, V, kThreads == 320 ? 512 : kThreads, kNormY>
-                       : step_kernel<T, W, V, kThreads, kNormY>;
-  SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, s.smem));
-  SPARSP_CUDA_OK(launch_kernel(kern, dim3((unsigned)s.ctas), s.threads, (size_t)s.smem, st, p));
-  return SPARSP_OK;
+template <typename T, typename W, int V, int kThreads, bool kBack>
+static int launch_kind(const StepPlan& s, const StepParams& p, cudaStream_t st) {
+  auto launch = [&](auto kern) {
+    SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, s.smem));
+    SPARSP_CUDA_OK(launch_kernel(kern, dim3((unsigned)s.ctas), s.threads, (size_t)s.smem, st, p));
+    return (int)SPARSP_OK;
+  };
+  if constexpr (kBack)
+    return p.norm_y != SPARSP_NORM_NONE ? launch(step_back_kernel<T, W, V, kThreads, true>)
+                                        : launch(step_back_kernel<T, W, V, kThreads, false>);
+  else
+    return p.norm_y != SPARSP_NORM_NONE ? launch(step_kernel<T, W, V, kThreads, true>)
+                                        : launch(step_kernel<T, W, V, kThreads, false>);
 }
 template <typename T, typename W, int V>
 static int launch_pieces(const StepPlan& s, const StepParams& p, bool backward, cudaStream_t st) {
-  if constexpr (V * 16 / (int)sizeof(T) <= 16) {
+  constexpr int kValues = V * 16 / (int)sizeof(T);
+  if constexpr (kValues <= 16) {
     if (s.pieces > V) return launch_pieces<T, W, V + 1>(s, p, backward, st);
-    const bool norm_y = p.norm_y != SPARSP_NORM_NONE;
-    auto kind = [&](auto threads) {
-      constexpr int kThreads = decltype(threads)::value;
-      return norm_y ? launch_kind<T, W, V, kThreads, true>(s, p, backward, st)
-                    : launch_kind<T, W, V, kThreads, false>(s, p, backward, st);
-    };
-    if (s.by_warps) return kind(std::integral_constant<int, 128>());
-    return s.threads <= 320 ? kind(std::integral_constant<int, 320>()) : kind(std::integral_constant<int, 512>());
+    if (!backward) {
+      if (s.by_warps) return launch_kind<T, W, V, 128, false>(s, p, st);
+      return s.threads <= 320 ? launch_kind<T, W, V, 320, false>(s, p, st) : launch_kind<T, W, V, 512, false>(s, p, st);
+    }
+    if (s.by_warps) return launch_kind<T, W, V, 128, true>(s, p, st);
+    if constexpr (kValues <= 8)
+      return s.threads <= 320 ? launch_kind<T, W, V, 320, true>(s, p, st) : launch_kind<T, W, V, 640, true>(s, p, st);
+    else
+      return launch_kind<T, W, V, 512, true>(s, p, st);
   } else {
     return SPARSP_ERR_UNSUPPORTED;  // (plan_step has no more pieces)
   }
