@@ -9,6 +9,7 @@
 // Bound by HBM: every value is read once for the norm, and read again and written where the norm is over the limit.
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 #include <new>
 #include <utility>
 #include <vector>
@@ -18,7 +19,7 @@
 namespace sparsp {
 
 constexpr int kMostTensors = 1024;  // 28 KB of parameters, of 32 KB that a launch takes
-constexpr int kFewTensors = 64;
+constexpr int kFewTensors = 64, kSomeTensors = 320;  // smaller tables for shorter lists: each SM reads all of it
 constexpr int kChunkBytes = 16384;
 constexpr int kGradThreads = 256;
 constexpr int kGradCtas = 8 * kSms;
@@ -198,6 +199,24 @@ __global__ void __launch_bounds__(kGradThreads)
 
 int64_t grad_workspace_bytes() { return 512 + kGradCtas * 8; }
 
+// As launch_kernel, for parameters of many KB, which that would copy.
+static cudaError_t launch_by_address(const void* kernel, dim3 grid, int threads, cudaStream_t st,
+                                     std::initializer_list<const void*> args) {
+  cudaLaunchAttribute attr[1] = {};
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3((unsigned)threads);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  void* list[2] = {const_cast<void*>(args.begin()[0]), const_cast<void*>(args.begin()[1])};
+  const cudaError_t e = cudaLaunchKernelExC(&cfg, kernel, list);
+  if (e == cudaSuccess) count_launch();
+  return e;
+}
+
 template <typename T, int kMost>
 static int launch_grad(const sparsp_grad_list& l, int from, int to, bool squares, GradParams p, cudaStream_t st) {
   static thread_local GradTable<kMost> table;  // (28 KB: not on the stack)
@@ -222,13 +241,14 @@ static int launch_grad(const sparsp_grad_list& l, int from, int to, bool squares
   const bool one = p.begin && p.end;
   const unsigned ctas = one ? (unsigned)std::max<int64_t>(1, std::min<int64_t>(chunks, kGradCtas)) : kGradCtas;
   auto kern = squares ? grad_squares_kernel<T, kMost> : grad_clip_kernel<T, kMost>;
-  SPARSP_CUDA_OK(launch_kernel(kern, dim3(ctas), kGradThreads, 0, st, table, p));
+  SPARSP_CUDA_OK(launch_by_address((const void*)kern, dim3(ctas), kGradThreads, st, {&table, &p}));
   return SPARSP_OK;
 }
 
 static int launch_list(const sparsp_grad_list& l, bool squares, const GradParams& p, cudaStream_t st) {
   SPARSP_WITH_TYPE(l.dtype, T, {
     if (l.count <= kFewTensors) return launch_grad<T, kFewTensors>(l, 0, l.count, squares, p, st);
+    if (l.count <= kSomeTensors) return launch_grad<T, kSomeTensors>(l, 0, l.count, squares, p, st);
     for (int from = 0; from < l.count; from += kMostTensors) {
       const int rc = launch_grad<T, kMostTensors>(l, from, std::min(l.count, from + kMostTensors), squares, p, st);
       if (rc != SPARSP_OK) return rc;

@@ -35,7 +35,7 @@ __host__ __device__ inline int64_t team_of(int64_t row, int64_t teams, int64_t r
 // of `room`, whose places of warps that are not there are 0.
 constexpr int kMostWarps = 20;
 template <bool kWarps, int N>
-__device__ __forceinline__ void team_sum(float (&v)[N], int lanes, float (*room)[2][kMostWarps], int& turn) {
+__device__ __forceinline__ void team_sum(float (&v)[N], int lanes, float (*room)[4][kMostWarps], int& turn) {
 #pragma unroll
   for (int d = 16; d > 0; d /= 2)
     if (kWarps || d < lanes) {
@@ -61,8 +61,8 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int lanes, float (*room)
     }
   }
 }
-__device__ __forceinline__ void clear_room(float (*room)[2][kMostWarps]) {
-  if (threadIdx.x < 4 * kMostWarps) (&room[0][0][0])[threadIdx.x] = 0.0f;
+__device__ __forceinline__ void clear_room(float (*room)[4][kMostWarps]) {
+  for (int i = threadIdx.x; i < 8 * kMostWarps; i += blockDim.x) (&room[0][0][0])[i] = 0.0f;
   __syncthreads();
 }
 
@@ -137,8 +137,11 @@ struct Ring {
     end = begin + stages * kRow * pitch;
     for (int i = 0; i < stages; ++i) next();
   }
-  __device__ __forceinline__ Vec<T, E> get(int q, int v) const {
-    return load_vec<T, E>(reinterpret_cast<const T*>(slot + (q * V + v) * pitch));
+  // piece v of tensor q of the row in use, or of the one behind it
+  __device__ __forceinline__ Vec<T, E> get(int q, int v, int behind = 0) const {
+    const uint8_t* at = slot;
+    if (behind > 0) at = slot + kRow * pitch == end ? begin : slot + kRow * pitch;
+    return load_vec<T, E>(reinterpret_cast<const T*>(at + (q * V + v) * pitch));
   }
   // the row in use is done with: the one `stages` behind it takes its place
   __device__ __forceinline__ void next() {
@@ -159,11 +162,14 @@ struct Ring {
     asm volatile("cp.async.commit_group;" ::: "memory");
     slot = slot + kRow * pitch == end ? begin : slot + kRow * pitch;
   }
-  // until the row in use has arrived
-  __device__ __forceinline__ void wait() const {
-    if (stages == 3)
+  // until the rows in use, one or two, have arrived
+  __device__ __forceinline__ void wait(int rows = 1) const {
+    const int behind = stages - rows;
+    if (behind >= 3)
+      asm volatile("cp.async.wait_group 3;" ::: "memory");
+    else if (behind == 2)
       asm volatile("cp.async.wait_group 2;" ::: "memory");
-    else if (stages == 2)
+    else if (behind == 1)
       asm volatile("cp.async.wait_group 1;" ::: "memory");
     else
       asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -205,7 +211,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
   constexpr bool kWarps = kThreads > 128;  // teams of 128 threads or fewer in a CTA of their own have room for 320
   enter_grid(p.x, p.y, p.gate, p.wy, p.by, p.wr, p.br);
   constexpr int E = 16 / sizeof(T);
-  __shared__ __align__(16) float room[2][2][kMostWarps];
+  __shared__ __align__(16) float room[2][4][kMostWarps];
   int turn = 0;
   if (kWarps) clear_room(room);
   const Member<kWarps> m(p);
@@ -320,12 +326,12 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
 // norm.  (An rms norm has mean 0 and no sum a.)  Column sums over the rows of a group, in registers: dn rh, dn, t yh (or
 // t y), t; from these come all gradients of weights.  There are no registers for more: rows and weights stay in shared
 // memory and are read again for each step.
-template <typename T, typename W, int V, int kThreads, bool kNormY>
-__global__ void __launch_bounds__(kThreads, kThreads == 320 ? 2 : 1) step_back_kernel(StepParams p) {
+template <typename T, typename W, int V, int kThreads, int R, bool kNormY>
+__global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) step_back_kernel(StepParams p) {
   constexpr bool kWarps = kThreads > 128;  // teams of 128 threads or fewer in a CTA of their own have room for 320
   enter_grid(p.x, p.y, p.dn, p.dr, p.gate, p.wy, p.wr, p.stats_y, p.stats_r);
   constexpr int E = 16 / sizeof(T), kSums = kNormY ? 4 : 3, kPart = Weights<W, E>::kParts;
-  __shared__ __align__(16) float room[2][2][kMostWarps];
+  __shared__ __align__(16) float room[2][4][kMostWarps];
   int turn = 0;
   if (kWarps) clear_room(room);
   const Member<kWarps> m(p);
@@ -405,14 +411,141 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 ? 2 : 1) step_back_k
     first_flush = false;
   };
 
-  // the kept statistics of a row, asked for a row ahead
+  // the kept statistics of rows, asked for a turn ahead
   auto kept = [&](const float* from, bool norm, int64_t row) {
     return norm && row < hi ? reinterpret_cast<const float2*>(from)[row] : make_float2(0.0f, 1.0f);
   };
-  float2 next_r = kept(p.stats_r, norm_r, m.lo), next_y = kept(p.stats_y, kNormY, m.lo);
+  float2 next_r[R], next_y[R];
+  auto ask = [&](int64_t row) {
+#pragma unroll
+    for (int q = 0; q < R; ++q) {
+      next_r[q] = kept(p.stats_r, norm_r, row + q);
+      next_y[q] = kept(p.stats_y, kNormY, row + q);
+    }
+  };
+  ask(m.lo);
   T* to_x = static_cast<T*>(p.r) + m.lo * p.stride_x + m.me * E;
   T* to_y = static_cast<T*>(p.n) + m.lo * p.stride_y + m.me * E;
-  for (int i = 0; i < m.turns; ++i, to_x += p.stride_x, to_y += p.stride_y) {
+  // C rows of one group
+  auto process = [&](auto count, const float2 (&sr)[R], const float2 (&sy)[R], bool live) {
+    constexpr int C = decltype(count)::value;
+    float k0[C], k1[C];
+#pragma unroll
+    for (int q = 0; q < C; ++q) k0[q] = k1[q] = 0.0f;
+    float s[2 * C];
+    auto along_rows = [&](int kind) {
+      team_sum<kWarps>(s, m.lanes, room, turn);
+#pragma unroll
+      for (int q = 0; q < C; ++q) {
+        k0[q] = kind == SPARSP_NORM_LAYER ? s[2 * q] * p.inv_dim : 0.0f;
+        k1[q] = s[2 * q + 1] * p.inv_dim;
+        s[2 * q] = s[2 * q + 1] = 0.0f;
+      }
+    };
+#pragma unroll
+    for (int q = 0; q < 2 * C; ++q) s[q] = 0.0f;
+    if (norm_r) {
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (!live || !ring.in[v]) continue;
+        const Weights<W, E> w = places.weights<W, E>(kWrAt + v * kPart);
+#pragma unroll
+        for (int q = 0; q < C; ++q) {
+          const Vec<T, E> dn = ring.get(kDn, v, q), r = ring.get(kR, v, q);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const int k = v * E + e;
+            const float d = dn[e], a = d * w[e], rh = (r[e] - sr[q].x) * sr[q].y;
+            s[2 * q] += a;
+            s[2 * q + 1] = fmaf(a, rh, s[2 * q + 1]);
+            sums[0][k] = fmaf(d, rh, sums[0][k]);
+            sums[1][k] += d;
+          }
+        }
+      }
+      along_rows(p.norm_r);
+    }
+    float b[kNormY ? C : 1][V * E];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      if (!live || !ring.in[v]) continue;
+#pragma unroll
+      for (int q = 0; q < C; ++q) {
+        float t[E];
+        if (p.dr != nullptr) {
+          const Vec<T, E> dr = ring.get(kDr, v, q);
+#pragma unroll
+          for (int e = 0; e < E; ++e) t[e] = dr[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) t[e] = 0.0f;
+        }
+        if (norm_r) {
+          const Vec<T, E> dn = ring.get(kDn, v, q), r = ring.get(kR, v, q);
+          const Weights<W, E> w = places.weights<W, E>(kWrAt + v * kPart);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const float rh = (r[e] - sr[q].x) * sr[q].y;
+            t[e] = fmaf(sr[q].y, fmaf(dn[e], w[e], -fmaf(rh, k1[q], k0[q])), t[e]);
+          }
+        }
+        if (p.r != nullptr) {
+          Vec<T, E> out;
+          out.set(t);
+          store_vec(to_x + q * p.stride_x + v * m.lanes * E, out);
+        }
+        const Vec<T, E> y = ring.get(kY, v, q);
+        const Weights<W, E> g = places.weights<W, E>(kGateAt + v * kPart);
+        if constexpr (kNormY) {
+          const Weights<W, E> wy = places.weights<W, E>(kWyAt + v * kPart);
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const int k = v * E + e;
+            const float yh = (y[e] - sy[q].x) * sy[q].y;
+            sums[2][k] = fmaf(t[e], yh, sums[2][k]);
+            sums[kSums - 1][k] += t[e];
+            b[q][k] = t[e] * g[e] * wy[e];
+            s[2 * q] += b[q][k];
+            s[2 * q + 1] = fmaf(b[q][k], yh, s[2 * q + 1]);
+          }
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            sums[2][v * E + e] = fmaf(t[e], y[e], sums[2][v * E + e]);
+            t[e] *= g[e];
+          }
+          if (p.n != nullptr) {
+            Vec<T, E> out;
+            out.set(t);
+            store_vec(to_y + q * p.stride_y + v * m.lanes * E, out);
+          }
+        }
+      }
+    }
+    if constexpr (kNormY) {
+      along_rows(p.norm_y);
+#pragma unroll
+      for (int v = 0; v < V; ++v) {
+        if (!live || !ring.in[v] || p.n == nullptr) continue;
+#pragma unroll
+        for (int q = 0; q < C; ++q) {
+          const Vec<T, E> y = ring.get(kY, v, q);
+          float d[E];
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            d[e] = sy[q].y * (b[q][v * E + e] - fmaf((y[e] - sy[q].x) * sy[q].y, k1[q], k0[q]));
+          Vec<T, E> out;
+          out.set(d);
+          store_vec(to_y + q * p.stride_y + v * m.lanes * E, out);
+        }
+      }
+    }
+#pragma unroll
+    for (int q = 0; q < C; ++q) ring.next();
+    to_x += C * p.stride_x;
+    to_y += C * p.stride_y;
+  };
+  for (int i = 0; i < m.turns;) {
     const int64_t row = m.lo + i;
     const bool live = i < m.rows;
     if (live && row >= group.end) {
@@ -420,103 +553,20 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 ? 2 : 1) step_back_k
       group.advance(row, p.rows_per_group);
       hold_weights();
     }
-    const float2 sr = next_r, sy = next_y;
-    next_r = kept(p.stats_r, norm_r, row + 1);
-    next_y = kept(p.stats_y, kNormY, row + 1);
-    ring.wait();
-    float s[2] = {0.0f, 0.0f}, k0 = 0.0f, k1 = 0.0f;
-    if (norm_r) {
+    const bool two = R == 2 && row + 1 < hi && row + 1 < group.end;
+    float2 sr[R], sy[R];
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (!live || !ring.in[v]) continue;
-        const Vec<T, E> dn = ring.get(kDn, v), r = ring.get(kR, v);
-        const Weights<W, E> w = places.weights<W, E>(kWrAt + v * kPart);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int k = v * E + e;
-          const float d = dn[e], a = d * w[e], rh = (r[e] - sr.x) * sr.y;
-          s[0] += a;
-          s[1] = fmaf(a, rh, s[1]);
-          sums[0][k] = fmaf(d, rh, sums[0][k]);
-          sums[1][k] += d;
-        }
-      }
-      team_sum<kWarps>(s, m.lanes, room, turn);
-      k0 = p.norm_r == SPARSP_NORM_LAYER ? s[0] * p.inv_dim : 0.0f;
-      k1 = s[1] * p.inv_dim;
+    for (int q = 0; q < R; ++q) {
+      sr[q] = next_r[q];
+      sy[q] = next_y[q];
     }
-    s[0] = s[1] = 0.0f;
-    float b[V * E];
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-      if (!live || !ring.in[v]) continue;
-      float t[E];
-      if (p.dr != nullptr) {
-        const Vec<T, E> dr = ring.get(kDr, v);
-#pragma unroll
-        for (int e = 0; e < E; ++e) t[e] = dr[e];
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) t[e] = 0.0f;
-      }
-      if (norm_r) {
-        const Vec<T, E> dn = ring.get(kDn, v), r = ring.get(kR, v);
-        const Weights<W, E> w = places.weights<W, E>(kWrAt + v * kPart);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const float rh = (r[e] - sr.x) * sr.y;
-          t[e] = fmaf(sr.y, fmaf(dn[e], w[e], -fmaf(rh, k1, k0)), t[e]);
-        }
-      }
-      if (p.r != nullptr) {
-        Vec<T, E> out;
-        out.set(t);
-        store_vec(to_x + v * m.lanes * E, out);
-      }
-      const Vec<T, E> y = ring.get(kY, v);
-      const Weights<W, E> g = places.weights<W, E>(kGateAt + v * kPart);
-      if constexpr (kNormY) {
-        const Weights<W, E> w = places.weights<W, E>(kWyAt + v * kPart);
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int k = v * E + e;
-          const float yh = (y[e] - sy.x) * sy.y;
-          sums[2][k] = fmaf(t[e], yh, sums[2][k]);
-          sums[kSums - 1][k] += t[e];
-          b[k] = t[e] * g[e] * w[e];
-          s[0] += b[k];
-          s[1] = fmaf(b[k], yh, s[1]);
-        }
-      } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          sums[2][v * E + e] = fmaf(t[e], y[e], sums[2][v * E + e]);
-          t[e] *= g[e];
-        }
-        if (p.n != nullptr) {
-          Vec<T, E> out;
-          out.set(t);
-          store_vec(to_y + v * m.lanes * E, out);
-        }
-      }
-    }
-    if constexpr (kNormY) {
-      team_sum<kWarps>(s, m.lanes, room, turn);
-      k0 = p.norm_y == SPARSP_NORM_LAYER ? s[0] * p.inv_dim : 0.0f;
-      k1 = s[1] * p.inv_dim;
-#pragma unroll
-      for (int v = 0; v < V; ++v) {
-        if (!live || !ring.in[v] || p.n == nullptr) continue;
-        const Vec<T, E> y = ring.get(kY, v);
-        float d[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) d[e] = sy.y * (b[v * E + e] - fmaf((y[e] - sy.x) * sy.y, k1, k0));
-        Vec<T, E> out;
-        out.set(d);
-        store_vec(to_y + v * m.lanes * E, out);
-      }
-    }
-    ring.next();
+    ask(row + (two ? 2 : 1));
+    ring.wait(R);
+    if (R == 2 && two)
+      process(std::integral_constant<int, R>(), sr, sy, true);
+    else
+      process(std::integral_constant<int, 1>(), sr, sy, live);
+    i += two ? 2 : 1;
   }
   if (m.rows > 0) flush();
 }
@@ -595,7 +645,7 @@ int64_t step_groups(const sparsp_gated_norm& n) { return (n.rows + per_group(n) 
 // shared memory.
 struct StepPlan {
   int pieces, threads, lanes, ctas, stages, places, smem;
-  bool by_warps;
+  bool by_warps, two_rows;
   int64_t teams;
 };
 constexpr int kStepSmem = 228 * 1024;  // of a multiprocessor; each CTA has 1 KB more than it asks for
@@ -606,7 +656,8 @@ static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
   int64_t per_cta = 1;
   s.by_warps = n.dim <= 32 * 16;
   // values of a thread, and threads that registers then hold: of a CTA, of a multiprocessor
-  const int values = backward && !s.by_warps && n.dim <= 640 * 8 ? 8 : 16, most = values / each;
+  s.two_rows = backward && each == 8 && n.dim > 320 * 8 && n.dim <= 320 * 16;
+  const int values = backward && !s.by_warps && !s.two_rows && n.dim <= 640 * 8 ? 8 : 16, most = values / each;
   const int most_threads = values == 8 ? 640 : 512, all_threads = backward && values == 16 ? 512 : 640;
   s.pieces = 1;
   if (s.by_warps) {  // a warp, or lanes of one
@@ -634,7 +685,7 @@ static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
   const int held = backward ? s.pieces * per_weight * (n.norm_y != SPARSP_NORM_NONE ? 3 : 2) : 0;
   auto fits = [&](int places, int ctas) { return (places * s.threads * 16 + 1024 + 256) * ctas <= kStepSmem; };
   auto stages = [&](int ctas) {
-    int k = 3;
+    int k = s.two_rows ? 4 : 3;
     while (k > 0 && !fits((k * row + held) | 1, ctas)) --k;
     return k;
   };
@@ -672,7 +723,7 @@ static StepParams step_params(const sparsp_gated_norm& n, const StepPlan& s) {
   return p;
 }
 
-template <typename T, typename W, int V, int kThreads, bool kBack>
+template <typename T, typename W, int V, int kThreads, bool kBack, int R = 1>
 static int launch_kind(const StepPlan& s, const StepParams& p, cudaStream_t st) {
   auto launch = [&](auto kern) {
     SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, s.smem));
@@ -680,8 +731,8 @@ static int launch_kind(const StepPlan& s, const StepParams& p, cudaStream_t st) 
     return (int)SPARSP_OK;
   };
   if constexpr (kBack)
-    return p.norm_y != SPARSP_NORM_NONE ? launch(step_back_kernel<T, W, V, kThreads, true>)
-                                        : launch(step_back_kernel<T, W, V, kThreads, false>);
+    return p.norm_y != SPARSP_NORM_NONE ? launch(step_back_kernel<T, W, V, kThreads, R, true>)
+                                        : launch(step_back_kernel<T, W, V, kThreads, R, false>);
   else
     return p.norm_y != SPARSP_NORM_NONE ? launch(step_kernel<T, W, V, kThreads, true>)
                                         : launch(step_kernel<T, W, V, kThreads, false>);
@@ -698,6 +749,8 @@ static int launch_pieces(const StepPlan& s, const StepParams& p, bool backward, 
     if (s.by_warps) return launch_kind<T, W, V, 128, true>(s, p, st);
     if constexpr (kValues <= 8)
       return s.threads <= 320 ? launch_kind<T, W, V, 320, true>(s, p, st) : launch_kind<T, W, V, 640, true>(s, p, st);
+    else if (sizeof(T) == 2 && s.two_rows)
+      return launch_kind<T, W, V, 320, true, sizeof(T) == 2 ? 2 : 1>(s, p, st);
     else
       return launch_kind<T, W, V, 512, true>(s, p, st);
   } else {
