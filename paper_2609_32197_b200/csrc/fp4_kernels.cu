@@ -139,7 +139,8 @@ struct OverScale {
     if constexpr (kFormat == SPARSP_MXFP4) {
       return x * inverse;
     } else if constexpr (sizeof(T) == 2) {
-      return fmaf(x, inverse, 1536.0f) - 1536.0f;
+      const float q = fmaf(x, inverse, 1536.0f) - 1536.0f;
+      return __uint_as_float(__float_as_uint(q) | (__float_as_uint(x) & 0x80000000u));  // (also where q is zero)
     } else {
       x *= tensor;
       const float q = fminf(fmaxf(x * inverse, -8.0f), 8.0f);  // (nothing infinite in the next step)
