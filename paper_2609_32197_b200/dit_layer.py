@@ -7,7 +7,14 @@ used together, forward, and a training step of the layer's feed-forward half.
 The norms, the rotary positions, the block mask, the attention and the gated feed-forward are the library's calls; the
 plain projections are torch products.  All buffers are made once, so that a step is stream-ordered work alone.
 
-    python -m paper_2609_32197_b200.dit_layer --workload tiny [--steps 20]
+GatedDitLayer is the layer whose condition also gates what each half adds, and whose projections can be in 4 bits:
+
+    x1 = x + gate1 Wo attention(...),  y = x1 + gate2 Wd (a(Wg m) * (Wu m))
+
+with its residual steps in one call each, the norm behind the first of them included, and a training step of what follows
+the attention that ends with clipped gradients.
+
+    python -m paper_2609_32197_b200.dit_layer --workload tiny [--steps 20] [--gated] [--projections nvfp4]
 """
 from __future__ import annotations
 
@@ -70,15 +77,22 @@ class DitLayer:
         self.m, self.mean, self.rstd = empty(N, D), empty(N, dtype=torch.float32), empty(N, dtype=torch.float32)
         self.h, self.gate, self.up = (empty(N, hidden) for _ in range(3))
 
-    def attention_half(self, x: torch.Tensor) -> torch.Tensor:
+    def project_qkv(self):
         D = self.width
-        q, k, v = self.qkv
-        binding.sparsp_layer_norm_fwd(self.norm, x, self.scale1, self.shift1, self.n, None, None)
         for i, out in enumerate(self.qkv):
             torch.matmul(self.n, self.w_qkv[i * D:(i + 1) * D].T, out=out)
+
+    def attention(self, x: torch.Tensor):
+        """Fills o, what the output projection takes."""
+        q, k, v = self.qkv
+        binding.sparsp_layer_norm_fwd(self.norm, x, self.scale1, self.shift1, self.n, None, None)
+        self.project_qkv()
         binding.sparsp_rotary_apply(self.shape, self.rotary, self.table, None, (0, 0, 0), q, k, q, k, False, None)
         binding.sparsp_block_mask(self.shape, q, k, self.topk, self.mask, None, None, None, None, self.workspace)
         binding.sparsp_sparse_attn_fwd(self.shape, q, k, v, self.mask, 0.0, self.o, None, self.workspace)
+
+    def attention_half(self, x: torch.Tensor) -> torch.Tensor:
+        self.attention(x)
         return torch.addmm(x, self.o, self.w_out.T)
 
     def feed_forward_half(self, x1: torch.Tensor, training: bool = False) -> torch.Tensor:
@@ -111,6 +125,126 @@ class DitLayer:
         return next((s for s in (binding.sparsp_status(w) for w in (self.workspace, self.ffn_workspace)) if s), 0)
 
 
+class Fp4Linear:
+    """y = x W^T with W, and x as it comes, in 4 bits.  `exponent` is that of x (nvfp4; from what x is seen to be)."""
+
+    def __init__(self, weight: torch.Tensor, tokens: int, fmt: str, exponent: int = 0):
+        cols, depth = weight.shape
+        exponent_w = 0
+        if fmt == "nvfp4":
+            exponent_w = math.ceil(math.log2(max(float(weight.abs().max()), 2.0 ** -60) / (6 * 448)))
+        else:
+            exponent = 0
+        device, dtype = weight.device, weight.dtype
+        self.described = binding.make_fp4(cols, depth, fmt, exponent_w, dtype, weight.stride(0))
+        self.weight = binding.make_fp4_operand(self.described, device)
+        self.values = torch.empty_strided(weight.shape, weight.stride(), dtype=dtype, device=device)  # what W stands for
+        binding.sparsp_fp4_quantize(self.described, weight, *self.weight, self.values)
+        self.input = binding.make_fp4(tokens, depth, fmt, exponent, dtype)
+        self.product = binding.make_fp4_product(tokens, cols, depth, fmt, exponent + exponent_w, dtype)
+        self.workspace = binding.make_fp4_product_workspace(self.product, device)
+
+    def quantize(self, x, operand, values=None):
+        binding.sparsp_fp4_quantize(self.input, x, *operand, values)
+
+    def __call__(self, operand, out):
+        binding.sparsp_fp4_product(self.product, *operand, *self.weight, None, out, self.workspace)
+
+
+class GatedDitLayer(DitLayer):
+    """projections: "bf16" (torch products), "mxfp4" or "nvfp4" for all but the feed-forward's first two."""
+
+    def __init__(self, wl: synth.Workload, hidden: int, seed: int = 0, dtype=torch.bfloat16, device="cuda",
+                 projections: str = "bf16", activation_exponent: int = -4):
+        super().__init__(wl, hidden, seed, dtype, device)
+        N, D = wl.n_tokens, self.width
+        gen = torch.Generator(device=device).manual_seed(seed + 1)
+        self.gate1, self.gate2 = (torch.empty(1, D, device=device).normal_(0.0, 0.5, generator=gen) for _ in range(2))
+        self.step1 = binding.make_gated_norm(N, D, dtype=dtype, weight_dtype=torch.float32)
+        self.step2 = binding.make_gated_norm(N, D, norm_r="none", dtype=dtype, weight_dtype=torch.float32)
+        self.step_workspace = binding.make_gated_norm_workspace(self.step1, device)
+        self.grad_workspace = binding.make_grad_workspace(device)
+
+        def empty(*dims, dtype=dtype):
+            return torch.empty(dims, dtype=dtype, device=device)
+
+        self.a, self.f, self.x1 = empty(N, D), empty(N, D), empty(N, D)  # what each half adds, and the stream between them
+        self.stats = empty(N, 2, dtype=torch.float32)
+        self.grad_norm = empty(1, dtype=torch.float32)
+        self.fp4 = {}
+        if projections != "bf16":
+            for name, weight in [("out", self.w_out), ("down", self.w_down)] + [
+                    (f"qkv{i}", self.w_qkv[i * D:(i + 1) * D]) for i in range(3)]:
+                self.fp4[name] = Fp4Linear(weight, N, projections, activation_exponent)
+            self.operand = binding.make_fp4_operand(self.fp4["out"].input, device)  # of the width's activations
+            self.hidden_operand = binding.make_fp4_operand(self.fp4["down"].input, device)
+            self.h_values = empty(N, hidden)
+
+    def project_qkv(self):
+        if not self.fp4:
+            return super().project_qkv()
+        self.fp4["qkv0"].quantize(self.n, self.operand)
+        for i, out in enumerate(self.qkv):
+            self.fp4[f"qkv{i}"](self.operand, out)
+
+    def project_out(self):
+        if not self.fp4:
+            torch.matmul(self.o, self.w_out.T, out=self.a)
+        else:
+            self.fp4["out"].quantize(self.o, self.operand)
+            self.fp4["out"](self.operand, self.a)
+
+    def project_down(self, training: bool):
+        if not self.fp4:
+            torch.matmul(self.h, self.w_down.T, out=self.f)
+        else:
+            self.fp4["down"].quantize(self.h, self.hidden_operand, self.h_values if training else None)
+            self.fp4["down"](self.hidden_operand, self.f)
+
+    def behind_attention(self, x: torch.Tensor, training: bool = False) -> torch.Tensor:
+        """y from the layer's input x and what the attention half adds, a."""
+        keep = (self.gate, self.up) if training else (None, None)
+        binding.sparsp_gated_norm_fwd(self.step1, x, self.a, self.gate1, None, None, self.scale2, self.shift2, self.x1, self.m,
+                                      None, self.stats if training else None)
+        binding.sparsp_gated_ffn_fwd(self.ffn, self.m, self.w_gate, self.w_up, self.h, *keep, self.ffn_workspace)
+        self.project_down(training)
+        y = torch.empty_like(x)
+        binding.sparsp_gated_norm_fwd(self.step2, self.x1, self.f, self.gate2, None, None, None, None, y, None, None, None)
+        return y
+
+    def forward(self, x: torch.Tensor) -> torch.Tensor:
+        """x, y [tokens][width]"""
+        self.attention(x)
+        self.project_out()
+        return self.behind_attention(x)
+
+    def training_step(self, x: torch.Tensor, dy: torch.Tensor, max_norm: float = math.inf) -> dict:
+        """Gradients of what follows the attention, for dy at the layer's output, forward pass included: of its weights,
+        clipped together to max_norm, and "x" and "a", the gradients of what it takes.  Roundings to 4 bits have the
+        gradient of nothing (straight through): products go on with the values that were multiplied."""
+        self.behind_attention(x, training=True)
+        w_down, h = (self.fp4["down"].values, self.h_values) if self.fp4 else (self.w_down, self.h)
+        grads = {k: torch.empty_like(getattr(self, k)) for k in ("w_gate", "w_up", "gate1", "gate2", "scale2", "shift2")}
+        df, dm, dx, da = (torch.empty_like(x) for _ in range(4))
+        binding.sparsp_gated_norm_bwd(self.step2, None, dy, None, self.f, self.gate2, None, None, None, None, None, None, df,
+                                      grads["gate2"], None, None, None, None, self.step_workspace)
+        grads["w_down"] = df.T @ h
+        binding.sparsp_gated_ffn_bwd(self.ffn, df @ w_down, self.m, self.w_gate, self.w_up, self.gate, self.up, dm,
+                                     grads["w_gate"], grads["w_up"], self.ffn_workspace)
+        binding.sparsp_gated_norm_bwd(self.step1, dm, dy, self.x1, self.a, self.gate1, None, None, self.scale2, None,
+                                      self.stats, dx, da, grads["gate1"], None, None, grads["scale2"], grads["shift2"],
+                                      self.step_workspace)
+        lists = [binding.make_grad_list([g for g in grads.values() if g.dtype == t]) for t in (x.dtype, torch.float32)]
+        for i, g in enumerate(lists):  # one norm over both types
+            binding.sparsp_grad_squares(g, self.grad_workspace, accumulate=i > 0)
+        for g in lists:
+            binding.sparsp_grad_clip(g, max_norm, self.grad_norm, self.grad_workspace)
+        return {**grads, "x": dx, "a": da}
+
+    def status(self) -> int:
+        return super().status() or next((s for s in (binding.sparsp_status(f.workspace) for f in self.fp4.values()) if s), 0)
+
+
 def _time(f, steps: int) -> float:
     for _ in range(3):
         f()
@@ -124,15 +258,31 @@ def _time(f, steps: int) -> float:
     return begin.elapsed_time(end) / steps * 1e3
 
 
+def _gated(wl, width: int, hidden: int, args):
+    layer = GatedDitLayer(wl, hidden, projections=args.projections)
+    x, dy = (torch.empty(wl.n_tokens, width, dtype=torch.bfloat16, device="cuda").normal_(0.0, 1.0) for _ in range(2))
+    layer.forward(x)
+    print(f"{wl.name}: {wl.n_tokens} tokens, width {width}, feed-forward {hidden}, projections in {args.projections}")
+    for name, f in (("layer", lambda: layer.forward(x)),
+                    ("training step behind the attention, clipped", lambda: layer.training_step(x, dy, 1.0))):
+        print(f"  {name}: {_time(f, args.steps):.1f} us")
+    if layer.status() != binding.SPARSP_OK:
+        raise SystemExit(binding.sparsp_last_error())
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description="One layer: times of its halves and of a training step of the second.")
     ap.add_argument("--workload", default="tiny", choices=sorted(synth.WORKLOADS))
     ap.add_argument("--hidden", type=int, default=0, help="feed-forward width; default 8/3 of the layer's, in steps of 256")
     ap.add_argument("--steps", type=int, default=20)
+    ap.add_argument("--gated", action="store_true", help="the layer with gates, its steps in one call each")
+    ap.add_argument("--projections", default="bf16", choices=("bf16", "mxfp4", "nvfp4"), help="of the gated layer")
     args = ap.parse_args(argv)
     wl = synth.WORKLOADS[args.workload]
     width = wl.heads * wl.head_dim
     hidden = args.hidden or math.ceil(width * 8 / 3 / 256) * 256
+    if args.gated or args.projections != "bf16":
+        return _gated(wl, width, hidden, args)
     layer = DitLayer(wl, hidden)
     x = torch.empty(wl.n_tokens, width, dtype=torch.bfloat16, device="cuda").normal_(0.0, 1.0)
     dy = torch.empty_like(x).normal_(0.0, 1.0)
