@@ -643,7 +643,7 @@ SPARSP_API int sparsp_fp4_product_workspace_bytes(const sparsp_fp4_gemm* product
 SPARSP_API int sparsp_fp4_product(const sparsp_fp4_gemm* product, const void* A, const void* A_scales, const void* B,
                                   const void* B_scales, const void* bias, void* C, void* workspace, void* stream);
 
-/* A list of gradients (arrays in HOST memory, of addresses in DEVICE memory; read before a call returns). */
+/* A list of gradients: arrays in HOST memory, of addresses in DEVICE memory. */
 typedef struct sparsp_grad_list {
   int32_t count;             /* 0 is allowed */
   int32_t dtype;             /* of all of them; lists of several types: see sparsp_grad_squares */
@@ -651,24 +651,34 @@ typedef struct sparsp_grad_list {
   void* const* outs;         /* [count]: where the clipped gradients go; NULL = in place.  Each may be its gradient, otherwise
                               * none overlaps a gradient or another */
   const int64_t* sizes;      /* [count] elements of each, >= 0 */
+  int32_t chunks, ctas, in_place; /* set by sparsp_grad_table */
 } sparsp_grad_list;
 
-/* Bytes of workspace that both calls need, whatever the list.  The first 256 bytes are zero before the first call. */
+/* The list's table, which the calls below read in its place: made once, in HOST memory, 16-byte aligned, and copied by the
+ * caller to the device that has the gradients (a copy in stream order before the calls).  It serves for as long as
+ * the tensors stay where they are; grads, outs and sizes are not read after this. */
+SPARSP_API int sparsp_grad_table_bytes(const sparsp_grad_list* list, int64_t* bytes);
+SPARSP_API int sparsp_grad_table(sparsp_grad_list* list, void* table);
+
+/* Bytes of workspace that both calls need, whatever the list.  The first 256 bytes are zero before the first call; calls
+ * that may run at the same time take one each. */
 SPARSP_API int sparsp_grad_workspace_bytes(int64_t* bytes);
 
 /* The sum of the squares of all values, as a double at byte 256 of the workspace; accumulate != 0: added to what is there
  * (lists of several types that share one norm).  Where gradients are spread over ranks, the ranks' sums are added there
  * (an all-reduce of one double) before sparsp_grad_clip.  Added in fp64, and in fp32 over 32 values at most, wherever
- * those are in fp32's range. */
-SPARSP_API int sparsp_grad_squares(const sparsp_grad_list* list, int32_t accumulate, void* workspace, void* stream);
+ * those are in fp32's range.
+ *   table  in  DEVICE, 16-byte aligned */
+SPARSP_API int sparsp_grad_squares(const sparsp_grad_list* list, const void* table, int32_t accumulate, void* workspace,
+                                   void* stream);
 
 /* norm = sqrt(the sum at byte 256);  gradients times min(1, max_norm / (norm + 1e-6)), rounded once.  A norm that is not
  * finite changes nothing (the caller sees it in `norm`), nor does one under the limit: in place, gradients are not read
  * then.
  *   max_norm   > 0; infinity only computes the norm
  *   norm  out  fp32 [1] DEVICE; may be NULL */
-SPARSP_API int sparsp_grad_clip(const sparsp_grad_list* list, double max_norm, float* norm, void* workspace,
-                                void* stream);
+SPARSP_API int sparsp_grad_clip(const sparsp_grad_list* list, const void* table, double max_norm, float* norm,
+                                void* workspace, void* stream);
 
 /* Synchronises `stream` and returns the workspace's status word in *code (SPARSP_OK if no kernel
  * reported a problem since the last reset), then resets it. */

@@ -38,7 +38,7 @@ EXPORTS = [
     "sparsp_layer_norm_fwd", "sparsp_layer_norm_workspace_bytes", "sparsp_layer_norm_bwd",
     "sparsp_gated_ffn_workspace_bytes", "sparsp_gated_ffn_fwd", "sparsp_gated_ffn_bwd",
     "sparsp_gated_norm_fwd", "sparsp_gated_norm_workspace_bytes", "sparsp_gated_norm_bwd",
-    "sparsp_grad_workspace_bytes", "sparsp_grad_squares", "sparsp_grad_clip",
+    "sparsp_grad_table_bytes", "sparsp_grad_table", "sparsp_grad_workspace_bytes", "sparsp_grad_squares", "sparsp_grad_clip",
     "sparsp_fp4_scales_bytes", "sparsp_fp4_quantize", "sparsp_fp4_product_workspace_bytes", "sparsp_fp4_product",
 ]
 SPARSP_XCHG_HOST_MEMORY = 1
@@ -79,8 +79,10 @@ _SIGNATURES = {
     "sparsp_gated_norm_workspace_bytes": "ep",
     "sparsp_gated_norm_bwd": "e" + 19 * "p",
     "sparsp_grad_workspace_bytes": "p",
-    "sparsp_grad_squares": "tipp",
-    "sparsp_grad_clip": "tdppp",
+    "sparsp_grad_table_bytes": "tp",
+    "sparsp_grad_table": "tp",
+    "sparsp_grad_squares": "tpipp",
+    "sparsp_grad_clip": "tpdppp",
     "sparsp_fp4_scales_bytes": "qp",
     "sparsp_fp4_quantize": "qppppp",
     "sparsp_fp4_product_workspace_bytes": "gp",
@@ -128,7 +130,8 @@ class sparsp_gated_norm(ctypes.Structure):
 
 class sparsp_grad_list(ctypes.Structure):
     _fields_ = [("count", ctypes.c_int32), ("dtype", ctypes.c_int32), ("grads", ctypes.c_void_p),
-                ("outs", ctypes.c_void_p), ("sizes", ctypes.c_void_p)]
+                ("outs", ctypes.c_void_p), ("sizes", ctypes.c_void_p), ("chunks", ctypes.c_int32),
+                ("ctas", ctypes.c_int32), ("in_place", ctypes.c_int32)]
 
 
 class sparsp_fp4(ctypes.Structure):
@@ -620,23 +623,36 @@ def sparsp_gated_norm_bwd(step, dN, dR, R, Y, gate, weight_y, bias_y, weight_r, 
 
 
 # ---- the norm of a list of gradients, and clipping ----
+def sparsp_grad_table_bytes(grad_list: sparsp_grad_list) -> int:
+    out = ctypes.c_int64()
+    _check(lib().sparsp_grad_table_bytes(grad_list, ctypes.addressof(out)))
+    return out.value
+
+
+def sparsp_grad_table(grad_list: sparsp_grad_list, table: torch.Tensor):
+    """table: uint8 on the host"""
+    _check(lib().sparsp_grad_table(grad_list, _data(table)))
+
+
 def make_grad_list(grads, outs=None) -> sparsp_grad_list:
-    """grads: contiguous tensors of one type; outs: where the clipped ones go, None = in place.  The list keeps them
-    alive."""
+    """grads: contiguous tensors of one type on one device; outs: where the clipped ones go, None = in place.  The list keeps
+    them and its table alive; it is made once, outside of a graph's capture, and serves as long as they stay where they are."""
     grads, outs = list(grads), None if outs is None else list(outs)
-    if not grads:
-        return sparsp_grad_list(0, SPARSP_BF16, None, None, None)
     if outs is not None and len(outs) != len(grads):
         raise ValueError(f"{len(outs)} outputs for {len(grads)} gradients")
-    for i, t in enumerate(grads + (outs or [])):
-        if t.dtype != grads[0].dtype or not t.is_contiguous() or t.numel() != grads[i % len(grads)].numel():
-            raise ValueError(f"gradient {i % len(grads)}: contiguous tensors of one type, an output as large as its gradient")
     n = len(grads)
-    addresses = (ctypes.c_void_p * n)(*(t.data_ptr() for t in grads))
-    to = None if outs is None else (ctypes.c_void_p * n)(*(t.data_ptr() for t in outs))
-    sizes = (ctypes.c_int64 * n)(*(t.numel() for t in grads))
-    out = sparsp_grad_list(n, _dtype(grads[0].dtype), ctypes.addressof(addresses),
-                           None if to is None else ctypes.addressof(to), ctypes.addressof(sizes))
+    for i, t in enumerate(grads + (outs or [])):
+        if (t.dtype != grads[0].dtype or t.device != grads[0].device or not t.is_contiguous()
+                or t.numel() != grads[i % n].numel()):
+            raise ValueError(f"gradient {i % n}: contiguous tensors of one type and device, an output as large as its gradient")
+    addresses = (ctypes.c_void_p * max(n, 1))(*(t.data_ptr() for t in grads))
+    to = None if outs is None else (ctypes.c_void_p * max(n, 1))(*(t.data_ptr() for t in outs))
+    sizes = (ctypes.c_int64 * max(n, 1))(*(t.numel() for t in grads))
+    out = sparsp_grad_list(n, _dtype(grads[0].dtype) if n else SPARSP_BF16, ctypes.addressof(addresses),
+                           None if to is None else ctypes.addressof(to), ctypes.addressof(sizes), 0, 0, 0)
+    table = torch.zeros(sparsp_grad_table_bytes(out), dtype=torch.uint8)
+    sparsp_grad_table(out, table)
+    out.table = table.to(grads[0].device if n else "cuda")
     out.kept = (grads, outs, addresses, to, sizes)
     return out
 
@@ -657,11 +673,13 @@ def grad_square_sum(workspace) -> torch.Tensor:
 
 
 def sparsp_grad_squares(grad_list, workspace, accumulate=False):
-    _check(lib().sparsp_grad_squares(grad_list, 1 if accumulate else 0, _data(workspace), _stream_handle()))
+    _check(lib().sparsp_grad_squares(grad_list, _data(grad_list.table), 1 if accumulate else 0, _data(workspace),
+                                     _stream_handle()))
 
 
 def sparsp_grad_clip(grad_list, max_norm, norm, workspace):
-    _check(lib().sparsp_grad_clip(grad_list, max_norm, _data(norm), _data(workspace), _stream_handle()))
+    _check(lib().sparsp_grad_clip(grad_list, _data(grad_list.table), max_norm, _data(norm), _data(workspace),
+                                  _stream_handle()))
 
 
 # ---- 4-bit operands and their product ----

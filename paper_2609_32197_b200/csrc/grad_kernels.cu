@@ -1,16 +1,15 @@
 // The norm over a list of gradients, and their clipping.
 //
-// The list travels in the kernel's parameters (up to kMostTensors a launch), so that nothing is copied to the device and
-// a call can be captured.  Tensors are cut into chunks of 16 KB; a CTA has a run of them and is told which tensor that
-// begins in (looked for by the CTAs themselves, 300 small tensors took 2 us longer in each pass).  Squares are added in fp32 over
-// the 32 values at most that a thread has of a chunk, then in fp64, and CTAs' sums in their order by the one that ends
-// last: the same list gives the same bits.  Scaling goes through each run from its end, so that what the first
-// pass read last is still in L2.
+// A table in device memory, made once for a list, says where its tensors are; nothing of it goes through a call, so that
+// calls cost the host the same for one tensor and for thousands (as kernel parameters, 12 KB for 300 tensors, they cost
+// 10 us each).  Tensors are cut into chunks of 16 KB; a CTA has a run of them and is told which tensor that begins in.
+// Squares are added in fp32 over the 32 values at most that a thread has of a chunk, then in fp64, and CTAs' sums in
+// their order by the one that ends last: the same list gives the same bits.  Scaling goes through each run from its end,
+// so that what the first pass read last is still in L2.
 //
 // Bound by HBM: every value is read once for the norm, and read again and written where the norm is over the limit.
 #include <algorithm>
 #include <cmath>
-#include <initializer_list>
 #include <new>
 #include <utility>
 #include <vector>
@@ -19,8 +18,6 @@
 
 namespace sparsp {
 
-constexpr int kMostTensors = 1024;  // 31 KB of parameters, of 32764 bytes that a launch takes
-constexpr int kFewTensors = 64, kSomeTensors = 320;  // smaller tables for shorter lists: each SM reads all of it
 constexpr int kChunkBytes = 16384;
 constexpr int kGradThreads = 256;
 constexpr int kGradCtas = 8 * kSms;
@@ -29,23 +26,19 @@ struct GradTensor {
   const void* from;
   void* to;
   int64_t size;
+  int64_t first_chunk;  // that of the entry behind the last tensor: the number of chunks
 };
-template <int kMost>
-struct GradTable {
-  GradTensor tensor[kMost];
-  int32_t first_chunk[kMost + 1];
-  int32_t count;
-  uint16_t begins_in[kGradCtas + 1];  // tensor of the first chunk of each CTA's run (count behind the last)
-};
-static_assert(sizeof(GradTable<kMostTensors>) < 32600, "");
+// The table: tensors that have values, one entry behind them, then int32 [ctas + 1]: the tensor of the first chunk of each
+// CTA's run.
 struct GradParams {
+  const GradTensor* tensors;
+  const int32_t* begins_in;
   double* sum;
   double* partial;  // of each CTA
   uint32_t* ticket;
   float* norm;
   double limit;
-  int32_t begin, end;  // the first and the last launch of a list
-  int32_t accumulate, in_place;
+  int32_t chunks, accumulate, in_place;
 };
 
 // elements before the first 16-byte boundary
@@ -62,16 +55,14 @@ struct Runs {
   __host__ __device__ int begin(int cta) const { return cta * each + (cta < more ? cta : more); }
 };
 
-// Chunk number c of the list, one of tensor t: its elements [first, last).  Chunks are cut at 16-byte boundaries of where
+// Chunk number c of the list, one of tensor x: its elements [first, last).  Chunks are cut at 16-byte boundaries of where
 // the tensor is read; what lies before the first one belongs to the first chunk.
-template <typename T, int kMost>
-__device__ __forceinline__ GradTensor chunk_at(const GradTable<kMost>& table, int t, int c, int64_t& first, int64_t& last) {
-  const GradTensor x = table.tensor[t];
-  const int64_t skip = ahead<T>(x.from, x.size), k = c - table.first_chunk[t];
+template <typename T>
+__device__ __forceinline__ void chunk_of(const GradTensor& x, int c, int64_t& first, int64_t& last) {
+  const int64_t skip = ahead<T>(x.from, x.size), k = c - x.first_chunk;
   constexpr int64_t kEach = kChunkBytes / sizeof(T);
   first = k == 0 ? 0 : skip + k * kEach;
   last = min(skip + (k + 1) * kEach, x.size);
-  return x;
 }
 
 // f(values, from index, how many) for what this thread has of the elements [first, last): 16-byte pieces where
@@ -111,22 +102,21 @@ __device__ __forceinline__ double block_sum(double v, double* room) {
   return v;
 }
 
-template <typename T, int kMost>
-__global__ void __launch_bounds__(kGradThreads)
-    grad_squares_kernel(const __grid_constant__ GradTable<kMost> table, GradParams p) {
-  enter_grid(p.partial, p.ticket);
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads) grad_squares_kernel(GradParams p) {
+  enter_grid(p.tensors, p.begins_in, p.partial, p.ticket);
   __shared__ double room[kGradThreads / 32];
   __shared__ bool s_last;
   constexpr int E = 16 / sizeof(T);
-  const int chunks = table.first_chunk[table.count];
-  const Runs runs(chunks, gridDim.x);
+  const Runs runs(p.chunks, gridDim.x);
   const int end = runs.begin(blockIdx.x + 1);
   double sum = 0.0;
-  int t = table.begins_in[blockIdx.x];
+  int t = p.begins_in[blockIdx.x];
   for (int c = runs.begin(blockIdx.x); c < end; ++c) {
-    if (c == table.first_chunk[t + 1]) ++t;
+    if (c == p.tensors[t + 1].first_chunk) ++t;
+    const GradTensor x = p.tensors[t];
     int64_t first, last;
-    const GradTensor x = chunk_at<T>(table, t, c, first, last);
+    chunk_of<T>(x, c, first, last);
     const T* from = static_cast<const T*>(x.from);
     walk_chunk(
         from, first, last, true,
@@ -152,9 +142,9 @@ __global__ void __launch_bounds__(kGradThreads)
   }
   sum = block_sum(sum, room);
   if (threadIdx.x == 0) {
-    p.partial[blockIdx.x] = p.begin ? sum : p.partial[blockIdx.x] + sum;
+    p.partial[blockIdx.x] = sum;
     __threadfence();
-    s_last = p.end && atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+    s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
   }
   __syncthreads();
   if (!s_last) return;
@@ -168,24 +158,23 @@ __global__ void __launch_bounds__(kGradThreads)
   }
 }
 
-template <typename T, int kMost>
-__global__ void __launch_bounds__(kGradThreads)
-    grad_clip_kernel(const __grid_constant__ GradTable<kMost> table, GradParams p) {
-  enter_grid(p.sum);
+template <typename T>
+__global__ void __launch_bounds__(kGradThreads) grad_clip_kernel(GradParams p) {
+  enter_grid(p.tensors, p.begins_in, p.sum);
   constexpr int E = 16 / sizeof(T);
   const double norm = sqrt(*p.sum);
   if (p.norm != nullptr && blockIdx.x == 0 && threadIdx.x == 0) *p.norm = (float)norm;
   // (a norm that is not a number is no reason to change anything: the caller sees it)
   const float factor = isfinite(norm) ? (float)fmin(p.limit / (norm + 1e-6), 1.0) : 1.0f;
   if (factor == 1.0f && p.in_place) return;
-  const int chunks = table.first_chunk[table.count];
-  const Runs runs(chunks, gridDim.x);
+  const Runs runs(p.chunks, gridDim.x);
   const int begin = runs.begin(blockIdx.x);
-  int t = table.begins_in[blockIdx.x + 1];
+  int t = p.begins_in[blockIdx.x + 1];
   for (int c = runs.begin(blockIdx.x + 1) - 1; c >= begin; --c) {
-    if (c < table.first_chunk[t]) --t;
+    if (c < p.tensors[t].first_chunk) --t;
+    const GradTensor x = p.tensors[t];
     int64_t first, last;
-    const GradTensor x = chunk_at<T>(table, t, c, first, last);
+    chunk_of<T>(x, c, first, last);
     const T* from = static_cast<const T*>(x.from);
     T* to = static_cast<T*>(x.to);
     const bool pieces = (((uintptr_t)from ^ (uintptr_t)to) & 15) == 0;
@@ -207,93 +196,74 @@ __global__ void __launch_bounds__(kGradThreads)
   }
 }
 
+// ---- host side ------------------------------------------------------------------------------------------------------
+
 int64_t grad_workspace_bytes() { return 512 + kGradCtas * 8; }
 
-// As launch_kernel, for parameters of many KB, which that would copy.
-static cudaError_t launch_by_address(const void* kernel, dim3 grid, int threads, cudaStream_t st,
-                                     std::initializer_list<const void*> args) {
-  cudaLaunchAttribute attr[1] = {};
-  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  attr[0].val.programmaticStreamSerializationAllowed = 1;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid;
-  cfg.blockDim = dim3((unsigned)threads);
-  cfg.stream = st;
-  cfg.attrs = attr;
-  cfg.numAttrs = 1;
-  void* list[2] = {const_cast<void*>(args.begin()[0]), const_cast<void*>(args.begin()[1])};
-  const cudaError_t e = cudaLaunchKernelExC(&cfg, kernel, list);
-  if (e == cudaSuccess) count_launch();
-  return e;
+int64_t grad_table_bytes(const sparsp_grad_list& l) {
+  return ((int64_t)l.count + 1) * (int64_t)sizeof(GradTensor) + (kGradCtas + 1) * 4;
 }
 
-template <typename T, int kMost>
-static int launch_grad(const sparsp_grad_list& l, int from, int to, bool squares, GradParams p, cudaStream_t st) {
-  static thread_local GradTable<kMost> table;  // (28 KB: not on the stack)
-  table.count = 0;
+int fill_grad_table(sparsp_grad_list* l, void* table) {
+  GradTensor* tensor = static_cast<GradTensor*>(table);
+  int32_t* begins_in = reinterpret_cast<int32_t*>(tensor + l->count + 1);
+  const int e = element_bytes(l->dtype);
+  const int64_t each = kChunkBytes / e;
   int64_t chunks = 0;
-  for (int i = from; i < to; ++i) {
-    const int64_t n = l.sizes[i];
-    if (n == 0) continue;
-    table.tensor[table.count] = {l.grads[i], l.outs != nullptr ? l.outs[i] : const_cast<void*>(l.grads[i]), n};
-    table.first_chunk[table.count++] = (int32_t)chunks;
-    const int64_t each = kChunkBytes / sizeof(T), rest = n - ahead<T>(l.grads[i], n);
-    chunks += std::max<int64_t>(1, (rest + each - 1) / each);
+  int n = 0;
+  l->in_place = 1;
+  for (int i = 0; i < l->count; ++i) {
+    const int64_t size = l->sizes[i];
+    if (size == 0) continue;
+    void* to = l->outs != nullptr ? l->outs[i] : const_cast<void*>(l->grads[i]);
+    if (to != l->grads[i]) l->in_place = 0;
+    tensor[n++] = {l->grads[i], to, size, chunks};
+    const int64_t skip = e == 4 ? ahead<float>(l->grads[i], size) : ahead<__half>(l->grads[i], size);
+    chunks += std::max<int64_t>(1, (size - skip + each - 1) / each);
     if (chunks > 0x7fffffff - 2 * kGradCtas) {
       set_error("the gradients are too large");
       return SPARSP_ERR_UNSUPPORTED;
     }
   }
-  table.first_chunk[table.count] = (int32_t)chunks;
-  p.begin = from == 0;
-  p.end = to == l.count;
-  // every launch of a list with the same CTAs: each adds to its own sum
-  const bool one = p.begin && p.end;
-  const int ctas = one ? (int)std::max<int64_t>(1, std::min<int64_t>(chunks, kGradCtas)) : kGradCtas;
-  const Runs runs((int)chunks, ctas);
-  for (int b = 0, t = 0; b <= ctas; ++b) {
-    while (t < table.count && table.first_chunk[t + 1] <= runs.begin(b)) ++t;
-    table.begins_in[b] = (uint16_t)t;
+  tensor[n] = {nullptr, nullptr, 0, chunks};
+  l->chunks = (int32_t)chunks;
+  l->ctas = (int32_t)std::max<int64_t>(1, std::min<int64_t>(chunks, kGradCtas));
+  const Runs runs(l->chunks, l->ctas);
+  for (int b = 0, t = 0; b <= l->ctas; ++b) {
+    while (t < n && tensor[t + 1].first_chunk <= runs.begin(b)) ++t;
+    begins_in[b] = t;
   }
-  auto kern = squares ? grad_squares_kernel<T, kMost> : grad_clip_kernel<T, kMost>;
-  SPARSP_CUDA_OK(launch_by_address((const void*)kern, dim3((unsigned)ctas), kGradThreads, st, {&table, &p}));
   return SPARSP_OK;
 }
 
-static int launch_list(const sparsp_grad_list& l, bool squares, const GradParams& p, cudaStream_t st) {
-  SPARSP_WITH_TYPE(l.dtype, T, {
-    if (l.count <= kFewTensors) return launch_grad<T, kFewTensors>(l, 0, l.count, squares, p, st);
-    if (l.count <= kSomeTensors) return launch_grad<T, kSomeTensors>(l, 0, l.count, squares, p, st);
-    for (int from = 0; from < l.count; from += kMostTensors) {
-      const int rc = launch_grad<T, kMostTensors>(l, from, std::min(l.count, from + kMostTensors), squares, p, st);
-      if (rc != SPARSP_OK) return rc;
-    }
-  });
-  return SPARSP_OK;
-}
-
-static GradParams grad_params(char* ws) {
+static GradParams grad_params(const sparsp_grad_list& l, const void* table, char* ws) {
   GradParams p = {};
+  p.tensors = static_cast<const GradTensor*>(table);
+  p.begins_in = reinterpret_cast<const int32_t*>(p.tensors + l.count + 1);
   p.ticket = reinterpret_cast<uint32_t*>(ws + 128);
   p.sum = reinterpret_cast<double*>(ws + 256);
   p.partial = reinterpret_cast<double*>(ws + 512);
+  p.chunks = l.chunks;
+  p.in_place = l.in_place;
   return p;
 }
 
-int launch_grad_squares(const sparsp_grad_list& l, int accumulate, char* ws, cudaStream_t st) {
-  GradParams p = grad_params(ws);
+int launch_grad_squares(const sparsp_grad_list& l, const void* table, int accumulate, char* ws, cudaStream_t st) {
+  GradParams p = grad_params(l, table, ws);
   p.accumulate = accumulate;
-  return launch_list(l, true, p, st);
+  SPARSP_WITH_TYPE(l.dtype, T, SPARSP_CUDA_OK(launch_kernel(grad_squares_kernel<T>, dim3((unsigned)l.ctas), kGradThreads, 0,
+                                                            st, p)));
+  return SPARSP_OK;
 }
 
-int launch_grad_clip(const sparsp_grad_list& l, double limit, float* norm, char* ws, cudaStream_t st) {
-  GradParams p = grad_params(ws);
+int launch_grad_clip(const sparsp_grad_list& l, const void* table, double limit, float* norm, char* ws,
+                     cudaStream_t st) {
+  GradParams p = grad_params(l, table, ws);
   p.limit = limit;
   p.norm = norm;
-  p.in_place = 1;
-  for (int i = 0; i < l.count && l.outs != nullptr; ++i)
-    if (l.sizes[i] > 0 && l.outs[i] != l.grads[i]) p.in_place = 0;
-  return launch_list(l, false, p, st);
+  SPARSP_WITH_TYPE(l.dtype, T, SPARSP_CUDA_OK(launch_kernel(grad_clip_kernel<T>, dim3((unsigned)l.ctas), kGradThreads, 0, st,
+                                                            p)));
+  return SPARSP_OK;
 }
 
 // Whether what is written overlaps; -1: no host memory to find out.

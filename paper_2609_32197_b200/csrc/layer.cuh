@@ -183,9 +183,12 @@ int launch_gated_norm_bwd(const sparsp_gated_norm& n, const void* dN, const void
                           void* dbr, char* ws, cudaStream_t st);
 
 int64_t grad_workspace_bytes();
+int64_t grad_table_bytes(const sparsp_grad_list& l);
 int grad_outputs_overlap(const sparsp_grad_list& l);
-int launch_grad_squares(const sparsp_grad_list& l, int accumulate, char* ws, cudaStream_t st);
-int launch_grad_clip(const sparsp_grad_list& l, double limit, float* norm, char* ws, cudaStream_t st);
+int fill_grad_table(sparsp_grad_list* l, void* table);
+int launch_grad_squares(const sparsp_grad_list& l, const void* table, int accumulate, char* ws, cudaStream_t st);
+int launch_grad_clip(const sparsp_grad_list& l, const void* table, double limit, float* norm, char* ws,
+                     cudaStream_t st);
 
 int64_t fp4_scales_bytes(const sparsp_fp4& f);
 int launch_fp4_quantize(const sparsp_fp4& f, const void* X, uint8_t* codes, uint8_t* scales, void* values,

@@ -133,15 +133,24 @@ int check_grads(const sparsp_grad_list* l) {
     SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "unknown dtype %d", l->dtype);
   if (l->count < 0) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "count is negative");
   if (l->count > 0 && (!l->grads || !l->sizes)) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "grads or sizes is NULL");
-  const size_t e = element_bytes(l->dtype);
+  const uintptr_t odd = element_bytes(l->dtype) - 1;
   for (int i = 0; i < l->count; ++i) {
     if (l->sizes[i] < 0 || l->sizes[i] > (1LL << 40))
       SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "gradient %d has %lld values", i, (long long)l->sizes[i]);
     if (l->sizes[i] == 0) continue;
-    if (!l->grads[i] || (uintptr_t)l->grads[i] % e || (l->outs && (!l->outs[i] || (uintptr_t)l->outs[i] % e)))
+    if (!l->grads[i] || ((uintptr_t)l->grads[i] & odd) || (l->outs && (!l->outs[i] || ((uintptr_t)l->outs[i] & odd))))
       SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "gradient %d or its output is NULL or not aligned to its type", i);
   }
   return SPARSP_OK;
+}
+// ... of a list whose table has been made
+int check_grad_table(const sparsp_grad_list* l, const void* table) {
+  if (!l) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "list is NULL");
+  if (l->dtype < SPARSP_BF16 || l->dtype > SPARSP_FP32)
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "unknown dtype %d", l->dtype);
+  if (l->count < 0 || l->chunks < 0 || l->ctas < 1 || l->ctas > (1 << 20))
+    SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "the list's table has not been made");
+  return need(table, "table", 16);
 }
 
 // ---- 4-bit operands ----
@@ -487,21 +496,36 @@ int sparsp_grad_workspace_bytes(int64_t* bytes) {
   return SPARSP_OK;
 }
 
-int sparsp_grad_squares(const sparsp_grad_list* list, int32_t accumulate, void* workspace, void* stream) {
+int sparsp_grad_table_bytes(const sparsp_grad_list* list, int64_t* bytes) {
   SPARSP_TRY(check_grads(list));
-  SPARSP_TRY(need(workspace, "workspace", 256));
-  return launch_grad_squares(*list, accumulate != 0, (char*)workspace, (cudaStream_t)stream);
+  if (!bytes) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "bytes is NULL");
+  *bytes = grad_table_bytes(*list);
+  return SPARSP_OK;
 }
 
-int sparsp_grad_clip(const sparsp_grad_list* list, double max_norm, float* norm, void* workspace, void* stream) {
+int sparsp_grad_table(sparsp_grad_list* list, void* table) {
   SPARSP_TRY(check_grads(list));
-  if (!(max_norm > 0.0)) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "max_norm %g must be above 0", max_norm);
-  SPARSP_TRY(optional(norm, "norm", 4));
-  SPARSP_TRY(need(workspace, "workspace", 256));
+  SPARSP_TRY(need(table, "table", 16));
   const int overlap = grad_outputs_overlap(*list);
   if (overlap < 0) SPARSP_REFUSE(SPARSP_ERR_CAPACITY, "no host memory for a list of %d gradients", list->count);
   if (overlap) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "two of the gradients that are written overlap");
-  return launch_grad_clip(*list, max_norm, norm, (char*)workspace, (cudaStream_t)stream);
+  return fill_grad_table(list, table);
+}
+
+int sparsp_grad_squares(const sparsp_grad_list* list, const void* table, int32_t accumulate, void* workspace,
+                        void* stream) {
+  SPARSP_TRY(check_grad_table(list, table));
+  SPARSP_TRY(need(workspace, "workspace", 256));
+  return launch_grad_squares(*list, table, accumulate != 0, (char*)workspace, (cudaStream_t)stream);
+}
+
+int sparsp_grad_clip(const sparsp_grad_list* list, const void* table, double max_norm, float* norm, void* workspace,
+                     void* stream) {
+  SPARSP_TRY(check_grad_table(list, table));
+  if (!(max_norm > 0.0)) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "max_norm %g must be above 0", max_norm);
+  SPARSP_TRY(optional(norm, "norm", 4));
+  SPARSP_TRY(need(workspace, "workspace", 256));
+  return launch_grad_clip(*list, table, max_norm, norm, (char*)workspace, (cudaStream_t)stream);
 }
 
 int sparsp_fp4_scales_bytes(const sparsp_fp4* fp4, int64_t* bytes) {

@@ -171,6 +171,10 @@ class GatedDitLayer(DitLayer):
         self.a, self.f, self.x1 = empty(N, D), empty(N, D), empty(N, D)  # what each half adds, and the stream between them
         self.stats = empty(N, 2, dtype=torch.float32)
         self.grad_norm = empty(1, dtype=torch.float32)
+        self.grads = {k: torch.empty_like(getattr(self, k))
+                      for k in ("w_gate", "w_up", "w_down", "gate1", "gate2", "scale2", "shift2")}
+        self.grad_lists = [binding.make_grad_list([g for g in self.grads.values() if g.dtype == t])
+                           for t in (dtype, torch.float32)]
         self.fp4 = {}
         if projections != "bf16":
             for name, weight in [("out", self.w_out), ("down", self.w_down)] + [
@@ -224,20 +228,19 @@ class GatedDitLayer(DitLayer):
         gradient of nothing (straight through): products go on with the values that were multiplied."""
         self.behind_attention(x, training=True)
         w_down, h = (self.fp4["down"].values, self.h_values) if self.fp4 else (self.w_down, self.h)
-        grads = {k: torch.empty_like(getattr(self, k)) for k in ("w_gate", "w_up", "gate1", "gate2", "scale2", "shift2")}
+        grads = self.grads  # (of one step: the next writes them again)
         df, dm, dx, da = (torch.empty_like(x) for _ in range(4))
         binding.sparsp_gated_norm_bwd(self.step2, None, dy, None, self.f, self.gate2, None, None, None, None, None, None, df,
                                       grads["gate2"], None, None, None, None, self.step_workspace)
-        grads["w_down"] = df.T @ h
+        torch.matmul(df.T, h, out=grads["w_down"])
         binding.sparsp_gated_ffn_bwd(self.ffn, df @ w_down, self.m, self.w_gate, self.w_up, self.gate, self.up, dm,
                                      grads["w_gate"], grads["w_up"], self.ffn_workspace)
         binding.sparsp_gated_norm_bwd(self.step1, dm, dy, self.x1, self.a, self.gate1, None, None, self.scale2, None,
                                       self.stats, dx, da, grads["gate1"], None, None, grads["scale2"], grads["shift2"],
                                       self.step_workspace)
-        lists = [binding.make_grad_list([g for g in grads.values() if g.dtype == t]) for t in (x.dtype, torch.float32)]
-        for i, g in enumerate(lists):  # one norm over both types
+        for i, g in enumerate(self.grad_lists):  # one norm over both types
             binding.sparsp_grad_squares(g, self.grad_workspace, accumulate=i > 0)
-        for g in lists:
+        for g in self.grad_lists:
             binding.sparsp_grad_clip(g, max_norm, self.grad_norm, self.grad_workspace)
         return {**grads, "x": dx, "a": da}
 

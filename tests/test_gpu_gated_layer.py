@@ -49,7 +49,7 @@ def test_a_training_step(share):
     layer, x, dy = make((3, 10, 11), 21, 4, 64, 616)
     layer.attention(x)
     layer.project_out()
-    whole = layer.training_step(x, dy)
+    whole = {k: v.clone() for k, v in layer.training_step(x, dy).items()}
     norm = float(layer.grad_norm)
     leaves = {k: getattr(layer, k).double().requires_grad_() for k in NAMES}
     X, A = x.double().requires_grad_(), layer.a.double().requires_grad_()
@@ -105,7 +105,7 @@ def test_a_layer_in_a_graph_beside_an_eager_one():
     layer, x, dy = make((3, 10, 11), 21, 2, 64, 288, "nvfp4")
     other, _, _ = make((3, 10, 11), 21, 2, 64, 288)
     layer.forward(x)
-    eager = other.training_step(x, dy, 1.0)
+    eager = {k: v.clone() for k, v in other.training_step(x, dy, 1.0).items()}
     graph = torch.cuda.CUDAGraph()
     held = x.clone()
     with torch.cuda.graph(graph):

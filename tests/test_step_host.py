@@ -89,44 +89,92 @@ def grads(*parts, outs=None, dtype=torch.bfloat16):
     a, s = (ctypes.c_void_p * n)(*(p[0] for p in parts)), (ctypes.c_int64 * n)(*(p[1] for p in parts))
     o = None if outs is None else (ctypes.c_void_p * n)(*outs)
     lst = binding.sparsp_grad_list(n, binding.DTYPES[dtype], ctypes.addressof(a), None if o is None else ctypes.addressof(o),
-                                   ctypes.addressof(s))
+                                   ctypes.addressof(s), 0, 0, 0)
     lst.kept = (a, s, o)
     return lst
 
 
+def table_of(lst):
+    return torch.zeros(binding.sparsp_grad_table_bytes(lst), dtype=torch.uint8)
+
+
 def test_refused_lists():
-    ws = At(1 << 20)
-    for bad in (grads((4096, -1)), grads((0, 8)), grads((4097, 8)), grads((4098, 8), dtype=torch.float32),
-                grads((4096, 8), outs=[None]), grads((4096, 8), outs=[8193]), grads((4096, 1 << 41))):
-        refused(INVALID, binding.sparsp_grad_squares, bad, ws)
-        refused(INVALID, binding.sparsp_grad_clip, bad, 1.0, None, ws)
-    good = grads((4096, 8), (8192, 8))
+    room = torch.zeros(1 << 16, dtype=torch.uint8)
+    bad = [grads((4096, -1)), grads((0, 8)), grads((4097, 8)), grads((4098, 8), dtype=torch.float32),
+           grads((4096, 8), outs=[None]), grads((4096, 8), outs=[8193]), grads((4096, 1 << 41))]
     for change in ({"dtype": 3}, {"count": -1}, {"grads": None}, {"sizes": None}):
-        lst = grads((4096, 8), (8192, 8))
+        bad.append(grads((4096, 8), (8192, 8)))
         for k, v in change.items():
-            setattr(lst, k, v)
+            setattr(bad[-1], k, v)
+    for lst in bad:
+        refused(INVALID, binding.sparsp_grad_table_bytes, lst)
+        refused(INVALID, binding.sparsp_grad_table, lst, room)
+    good = grads((4096, 8), (8192, 8))
+    refused(INVALID, binding.sparsp_grad_table, good, None)
+    refused(INVALID, binding.sparsp_grad_table, good, At(4104))
+
+
+def test_refused_calls():
+    ws = At(1 << 20)
+    lst = grads((4096, 8), (8192, 8))
+    lst.table = At(1 << 16)
+    refused(INVALID, binding.sparsp_grad_squares, lst, ws)  # no table yet
+    refused(INVALID, binding.sparsp_grad_clip, lst, 1.0, None, ws)
+    binding.sparsp_grad_table(lst, table_of(lst))
+    assert (lst.chunks, lst.ctas, lst.in_place) == (2, 2, 1)
+    for limit in (0.0, -1.0, math.nan):
+        refused(INVALID, binding.sparsp_grad_clip, lst, limit, None, ws)
+    for bad in (None, At((1 << 20) + 16)):
+        refused(INVALID, binding.sparsp_grad_squares, lst, bad)
+        refused(INVALID, binding.sparsp_grad_clip, lst, 1.0, None, bad)
+    refused(INVALID, binding.sparsp_grad_clip, lst, 1.0, At(4098), ws)
+    for bad in (None, At(4104)):
+        lst.table = bad
         refused(INVALID, binding.sparsp_grad_squares, lst, ws)
         refused(INVALID, binding.sparsp_grad_clip, lst, 1.0, None, ws)
-    for limit in (0.0, -1.0, math.nan):
-        refused(INVALID, binding.sparsp_grad_clip, good, limit, None, ws)
-    for bad in (None, At((1 << 20) + 16)):
-        refused(INVALID, binding.sparsp_grad_squares, good, bad)
-        refused(INVALID, binding.sparsp_grad_clip, good, 1.0, None, bad)
-    refused(INVALID, binding.sparsp_grad_clip, good, 1.0, At(4098), ws)
 
 
-def test_gradients_that_overlap_are_not_clipped():
-    ws = At(1 << 20)
+def test_gradients_that_overlap_are_refused():
     for bad in (grads((8192, 8), (8192, 8)), grads((8192, 8), (8200, 8)), grads((8192, 8), (4096, 2049)),
                 grads((4096, 8), (8192, 8), outs=[65536, 65536])):
-        refused(INVALID, binding.sparsp_grad_clip, bad, 1.0, None, ws)
+        refused(INVALID, binding.sparsp_grad_table, bad, table_of(bad))
+
+
+@pytest.mark.parametrize("count,dtype", [(0, torch.bfloat16), (1, torch.bfloat16), (700, torch.float32), (3000, torch.float16)])
+def test_table(count, dtype):
+    """Every chunk of every tensor belongs to the run of one CTA, which knows the tensor that it begins in."""
+    import random
+    rng = random.Random(count)
+    e = 4 if dtype == torch.float32 else 2
+    parts, at = [], 1 << 20
+    for _ in range(count):
+        size = rng.choice((0, 1, 7, 4095, 4096, 4097, 8192, 8193, 50000))
+        at += rng.choice((0, e, 16))
+        parts.append((at, size))
+        at += size * e
+    lst = grads(*parts, dtype=dtype)
+    table = table_of(lst)
+    binding.sparsp_grad_table(lst, table)
+    words = table[:(count + 1) * 32].view(torch.int64).view(-1, 4).tolist()
+    begins = table[(count + 1) * 32:].view(torch.int32).tolist()
+    each, chunk = 16384 // e, 0
+    there = [p for p in parts if p[1] > 0]
+    for (address, size), (source, to, n, first) in zip(there, words):
+        assert (source, to, n, first) == (address, address, size, chunk)
+        skip = min(-address % 16 // e, size)
+        chunk += max(1, -(-(size - skip) // each))
+    assert words[len(there)][3] == chunk == lst.chunks and lst.ctas == max(1, min(chunk, 8 * 148))
+    firsts = [w[3] for w in words[:len(there) + 1]]
+    q, r = divmod(chunk, lst.ctas)
+    for b in range(lst.ctas + 1):
+        begin, t = b * q + min(b, r), begins[b]
+        assert t == len(there) if begin == chunk else firsts[t] <= begin < firsts[t + 1]
 
 
 def test_make_grad_list():
     a, b = torch.zeros(4), torch.zeros(6)
     lst = binding.make_grad_list([a, b])
     assert (lst.count, lst.dtype) == (2, binding.SPARSP_FP32)
-    assert binding.make_grad_list([]).count == 0
     for bad in (([a, b.double()],), ([a, b.half()],), ([b.view(2, 3).T],), ([a], [b]), ([a, b], [a]), ([a], [a.half()])):
         with pytest.raises(ValueError):
             binding.make_grad_list(*bad)
