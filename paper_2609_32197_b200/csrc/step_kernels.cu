@@ -8,7 +8,7 @@
 //
 // Bound by HBM, forward: 75600 x 5120 bf16 509 to 556 us = 5.6 to 6.1 TB/s (weights from L1 for each row 728).  Backward the sums
 // of columns take the registers that more warps would need, and a row's sums along it are waited for: 75600 x 5120
-// 843 to 877 us = 5.3 to 5.5 TB/s, with norms on both sides 1265.
+// 768 us = 6.0 TB/s, with norms on both sides 1205.
 #include <algorithm>
 
 #include "layer.cuh"
@@ -39,9 +39,8 @@ __host__ __device__ inline int64_t team_of(int64_t row, int64_t teams, int64_t r
 
 // Sums over a team, the same in every lane.  kWarps: the team is a CTA; its warps meet at one barrier a call, by turns
 // of `room`, whose places of warps that are not there are 0.
-constexpr int kMostWarps = 20;
-template <bool kWarps, int N>
-__device__ __forceinline__ void team_sum(float (&v)[N], int lanes, float (*room)[4][kMostWarps], int& turn) {
+template <bool kWarps, int N, int kPlaces>
+__device__ __forceinline__ void team_sum(float (&v)[N], int lanes, float (*room)[4][kPlaces], int& turn) {
 #pragma unroll
   for (int d = 16; d > 0; d /= 2)
     if (kWarps || d < lanes) {
@@ -50,7 +49,7 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int lanes, float (*room)
     }
   if constexpr (kWarps) {
     const int warp = threadIdx.x >> 5;
-    float (*at)[kMostWarps] = room[turn];
+    float (*at)[kPlaces] = room[turn];
     turn ^= 1;
     if ((threadIdx.x & 31) == 0) {
 #pragma unroll
@@ -60,15 +59,20 @@ __device__ __forceinline__ void team_sum(float (&v)[N], int lanes, float (*room)
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const float4* w = reinterpret_cast<const float4*>(at[i]);
-      float s[kMostWarps / 4];
+      float s[kPlaces / 4];
 #pragma unroll
-      for (int k = 0; k < kMostWarps / 4; ++k) s[k] = (w[k].x + w[k].y) + (w[k].z + w[k].w);
-      v[i] = ((s[0] + s[1]) + (s[2] + s[3])) + s[4];
+      for (int k = 0; k < kPlaces / 4; ++k) s[k] = (w[k].x + w[k].y) + (w[k].z + w[k].w);
+      v[i] = s[0];
+#pragma unroll
+      for (int k = 1; k < kPlaces / 4; ++k) v[i] += s[k];
     }
   }
 }
-__device__ __forceinline__ void clear_room(float (*room)[4][kMostWarps]) {
-  for (int i = threadIdx.x; i < 8 * kMostWarps; i += blockDim.x) (&room[0][0][0])[i] = 0.0f;
+// places of a kernel of so many threads at most, four at a time
+__host__ __device__ constexpr int room_places(int threads) { return (threads / 32 + 3) / 4 * 4; }
+template <int kPlaces>
+__device__ __forceinline__ void clear_room(float (*room)[4][kPlaces]) {
+  for (int i = threadIdx.x; i < 8 * kPlaces; i += blockDim.x) (&room[0][0][0])[i] = 0.0f;
   __syncthreads();
 }
 
@@ -217,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
   constexpr bool kWarps = kThreads > 128;  // teams of 128 threads or fewer in a CTA of their own have room for 320
   enter_grid(p.x, p.y, p.gate, p.wy, p.by, p.wr, p.br);
   constexpr int E = 16 / sizeof(T);
-  __shared__ __align__(16) float room[2][4][kMostWarps];
+  __shared__ __align__(16) float room[2][4][room_places(kThreads)];
   int turn = 0;
   if (kWarps) clear_room(room);
   const Member<kWarps> m(p);
@@ -279,6 +283,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
       if (p.stats_y != nullptr && live && m.me == 0)
         reinterpret_cast<float2*>(p.stats_y)[m.lo + i] = make_float2(mean, rstd);
     }
+    float shift = -mean * rstd;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (!live || !ring.in[v]) {
@@ -294,7 +299,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
         w.load(p.wy, col, 1.0f);
         b.load(p.by, col, 0.0f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) r[v * E + e] = fmaf(g[e], fmaf((r[v * E + e] - mean) * rstd, w[e], b[e]), x[e]);
+        for (int e = 0; e < E; ++e) r[v * E + e] = fmaf(g[e], fmaf(fmaf(r[v * E + e], rstd, shift), w[e], b[e]), x[e]);
       } else {
         const Vec<T, E> y = ring.get(1, v);
 #pragma unroll
@@ -307,6 +312,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
     ring.next();
     if (p.norm_r == SPARSP_NORM_NONE) continue;
     statistics(r, p.norm_r, mean, rstd);
+    shift = -mean * rstd;
     if (!live) continue;
     if (p.stats_r != nullptr && m.me == 0) reinterpret_cast<float2*>(p.stats_r)[m.lo + i] = make_float2(mean, rstd);
 #pragma unroll
@@ -319,7 +325,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
       }
       float n[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) n[e] = fmaf((r[v * E + e] - mean) * rstd, wr[v][e], br[v][e]);
+      for (int e = 0; e < E; ++e) n[e] = fmaf(fmaf(r[v * E + e], rstd, shift), wr[v][e], br[v][e]);
       Vec<T, E> out;
       out.set(n);
       store_vec(to_n + v * m.lanes * E, out);
@@ -337,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
   constexpr bool kWarps = kThreads > 128;  // teams of 128 threads or fewer in a CTA of their own have room for 320
   enter_grid(p.x, p.y, p.dn, p.dr, p.gate, p.wy, p.wr, p.stats_y, p.stats_r);
   constexpr int E = 16 / sizeof(T), kSums = kNormY ? 4 : 3, kPart = Weights<W, E>::kParts;
-  __shared__ __align__(16) float room[2][4][kMostWarps];
+  __shared__ __align__(16) float room[2][4][room_places(kThreads)];
   int turn = 0;
   if (kWarps) clear_room(room);
   const Member<kWarps> m(p);
@@ -439,12 +445,13 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
 #pragma unroll
     for (int q = 0; q < C; ++q) k0[q] = k1[q] = 0.0f;
     float s[2 * C];
-    auto along_rows = [&](int kind) {
+    auto along_rows = [&](int kind, const float2 (&kept)[R]) {
       team_sum<kWarps>(s, m.lanes, room, turn);
 #pragma unroll
       for (int q = 0; q < C; ++q) {
-        k0[q] = kind == SPARSP_NORM_LAYER ? s[2 * q] * p.inv_dim : 0.0f;
         k1[q] = s[2 * q + 1] * p.inv_dim;
+        k0[q] = fmaf(kept[q].x, k1[q], kind == SPARSP_NORM_LAYER ? s[2 * q] * p.inv_dim : 0.0f);
+        k1[q] *= kept[q].y;
         s[2 * q] = s[2 * q + 1] = 0.0f;
       }
     };
@@ -461,7 +468,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
 #pragma unroll
           for (int e = 0; e < E; ++e) {
             const int k = v * E + e;
-            const float d = dn[e], a = d * w[e], rh = (r[e] - sr[q].x) * sr[q].y;
+            const float d = dn[e], a = d * w[e], rh = fmaf(r[e], sr[q].y, sr[q].x);
             s[2 * q] += a;
             s[2 * q + 1] = fmaf(a, rh, s[2 * q + 1]);
             sums[0][k] = fmaf(d, rh, sums[0][k]);
@@ -469,7 +476,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
           }
         }
       }
-      along_rows(p.norm_r);
+      along_rows(p.norm_r, sr);
     }
     float b[kNormY ? C : 1][V * E];
 #pragma unroll
@@ -491,8 +498,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
           const Weights<W, E> w = places.weights<W, E>(kWrAt + v * kPart);
 #pragma unroll
           for (int e = 0; e < E; ++e) {
-            const float rh = (r[e] - sr[q].x) * sr[q].y;
-            t[e] = fmaf(sr[q].y, fmaf(dn[e], w[e], -fmaf(rh, k1[q], k0[q])), t[e]);
+            // (k1 rh + k0 as a line in r)
+            t[e] = fmaf(sr[q].y, fmaf(dn[e], w[e], -fmaf(r[e], k1[q], k0[q])), t[e]);
           }
         }
         if (p.r != nullptr) {
@@ -507,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
 #pragma unroll
           for (int e = 0; e < E; ++e) {
             const int k = v * E + e;
-            const float yh = (y[e] - sy[q].x) * sy[q].y;
+            const float yh = fmaf(y[e], sy[q].y, sy[q].x);
             sums[2][k] = fmaf(t[e], yh, sums[2][k]);
             sums[kSums - 1][k] += t[e];
             b[q][k] = t[e] * g[e] * wy[e];
@@ -529,7 +536,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
       }
     }
     if constexpr (kNormY) {
-      along_rows(p.norm_y);
+      along_rows(p.norm_y, sy);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         if (!live || !ring.in[v] || p.n == nullptr) continue;
@@ -539,7 +546,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
           float d[E];
 #pragma unroll
           for (int e = 0; e < E; ++e)
-            d[e] = sy[q].y * (b[q][v * E + e] - fmaf((y[e] - sy[q].x) * sy[q].y, k1[q], k0[q]));
+            d[e] = sy[q].y * (b[q][v * E + e] - fmaf(y[e], k1[q], k0[q]));
           Vec<T, E> out;
           out.set(d);
           store_vec(to_y + q * p.stride_y + v * m.lanes * E, out);
@@ -563,8 +570,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
     float2 sr[R], sy[R];
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      sr[q] = next_r[q];
-      sy[q] = next_y[q];
+      sr[q] = make_float2(-next_r[q].x * next_r[q].y, next_r[q].y);  // (v - mean) rstd = v rstd + this
+      sy[q] = make_float2(-next_y[q].x * next_y[q].y, next_y[q].y);
     }
     ask(row + (two ? 2 : 1));
     ring.wait(R);
@@ -663,7 +670,8 @@ static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
   s.by_warps = n.dim <= 32 * 16;
   // Values of a thread, and threads that registers then hold: of a CTA, of a multiprocessor.  Backward, 8 values leave room
   // for twice the warps (15554 x 1928 fp32 with two norms 168 us, 216 with 16); where only one CTA fits, 16, and two rows
-  // at a time whose sums are waited for together (75600 x 5120 bf16 843, 962 with 8 and one row, 922 with 16 and one).
+  // at a time whose sums are waited for together (75600 x 5120 bf16 843, 962 with 8 and one row, 922 with 16 and one;
+  // 768 since fewer operations make a value).
   s.two_rows = backward && each == 8 && n.dim > 320 * 8 && n.dim <= 320 * 16;
   const int values = backward && !s.by_warps && !s.two_rows && n.dim <= 640 * 8 ? 8 : 16, most = values / each;
   const int most_threads = values == 8 ? 640 : 512, all_threads = backward && values == 16 ? 512 : 640;
