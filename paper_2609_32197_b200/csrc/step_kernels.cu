@@ -21,6 +21,7 @@ struct StepParams {
   const void *gate, *wy, *by, *wr, *br;
   void *r, *n;           // backward: dx, dy
   float *stats_y, *stats_r;
+  float* joined;               // backward: [found and last][parts][4][dim], see step_columns_kernel
   float *partial, *partial_y;  // backward: [teams][2][4][dim], of a team's first group and its last, and [teams][2][dim]
   void *dgate, *dwy, *dby, *dwr, *dbr;
   int64_t rows, rows_per_group, stride_x, stride_y, stride_n;
@@ -584,31 +585,61 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
   if (m.rows > 0) flush();
 }
 
-// Adds what the teams left: blockIdx.y < `found`: the group of that number (or, of more groups than teams, the one that
-// begins in that team and goes on in others), behind them dwy and dby.  A CTA has 32 columns and 16 teams at a time.
+// What the sums of 32 columns are of: blockIdx.y < `found`: the group of that number (or, of more groups than teams, the one
+// that begins in that team and goes on in others), behind them dwy and dby.
+struct Columns {
+  int64_t group, t0, t1;  // teams that have rows of it
+  bool last, none;        // none: finished by its team, or found by another
+  __device__ __forceinline__ Columns(const StepParams& p, int found, bool by_team)
+      : group(blockIdx.y), t0(0), t1(p.teams), last((int)blockIdx.y >= found), none(false) {
+    if (last) return;
+    if (by_team) group = (first_row((int64_t)blockIdx.y + 1, p.teams, p.rows) - 1) / p.rows_per_group;
+    t0 = team_of(group * p.rows_per_group, p.teams, p.rows);
+    t1 = team_of(min((group + 1) * p.rows_per_group, p.rows) - 1, p.teams, p.rows) + 1;
+    none = t1 - t0 < 2 || (by_team && t0 != blockIdx.y);
+  }
+  template <typename W>
+  __device__ __forceinline__ void finish(const StepParams& p, int col, const float (&s)[4]) const {
+    auto put = [&](void* out, int64_t at, float x) {
+      if (out != nullptr) static_cast<W*>(out)[at] = from_float<W>(x);
+    };
+    if (last) {
+      put(p.dwy, col, s[0]);
+      put(p.dby, col, s[1]);
+      return;
+    }
+    const int64_t at = group * p.dim + col;
+    auto weight = [&](const void* w, float fill) {
+      return w == nullptr ? fill : to_float<W>(static_cast<const W*>(w)[col]);
+    };
+    put(p.dwr, at, s[0]);
+    put(p.dbr, at, s[1]);
+    put(p.dgate, at, p.norm_y == SPARSP_NORM_NONE ? s[2] : fmaf(weight(p.wy, 1.0f), s[2], weight(p.by, 0.0f) * s[3]));
+  }
+};
+
+// Adds what the teams left.  A CTA has 32 columns and 16 teams at a time; where there are few columns and many teams,
+// gridDim.z CTAs share the teams out, and step_join_kernel adds their sums (75600 x 64: 153 us in one CTA for 32 columns,
+// 45 so).
 template <typename W>
 __global__ void __launch_bounds__(512) step_columns_kernel(StepParams p, int found, bool by_team) {
   enter_grid(p.partial, p.partial_y);
   __shared__ float room[16][4][33];
   const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
-  const bool last = (int)blockIdx.y >= found;
-  int64_t group = blockIdx.y, t0 = 0, t1 = p.teams;
-  if (!last) {
-    if (by_team) group = (first_row((int64_t)blockIdx.y + 1, p.teams, p.rows) - 1) / p.rows_per_group;
-    t0 = team_of(group * p.rows_per_group, p.teams, p.rows);
-    t1 = team_of(min((group + 1) * p.rows_per_group, p.rows) - 1, p.teams, p.rows) + 1;
-    if (t1 - t0 < 2 || (by_team && t0 != blockIdx.y)) return;  // (finished by its team, or found by another)
-  }
-  const int sums = last ? 2 : 4;
-  const float* from = last ? p.partial_y : p.partial;
+  const Columns c(p, found, by_team);
+  if (c.none) return;
+  const int sums = c.last ? 2 : 4;
+  const float* from = c.last ? p.partial_y : p.partial;
   // the group is the last of its first team, and the first of the others
-  const int64_t behind = !last && group * p.rows_per_group > first_row(t0, p.teams, p.rows) ? 1 : 0;
+  const int64_t behind = !c.last && c.group * p.rows_per_group > first_row(c.t0, p.teams, p.rows) ? 1 : 0;
+  const int64_t begin = c.t0 + first_row(blockIdx.z, gridDim.z, c.t1 - c.t0);
+  const int64_t end = c.t0 + first_row(blockIdx.z + 1, gridDim.z, c.t1 - c.t0);
   float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-  const int there = last ? 2 : p.norm_y != SPARSP_NORM_NONE ? 4 : 3;
+  const int there = c.last ? 2 : p.norm_y != SPARSP_NORM_NONE ? 4 : 3;
   if (col < p.dim)
 #pragma unroll 4
-    for (int64_t t = t0 + part; t < t1; t += 16) {
-      const int64_t slot = last ? t : 2 * t + (t == t0 ? behind : 0);
+    for (int64_t t = begin + part; t < end; t += 16) {
+      const int64_t slot = c.last ? t : 2 * t + (t == c.t0 ? behind : 0);
 #pragma unroll
       for (int q = 0; q < 4; ++q)
         if (q < there) s[q] += from[(slot * sums + q) * p.dim + col];
@@ -620,21 +651,25 @@ __global__ void __launch_bounds__(512) step_columns_kernel(StepParams p, int fou
 #pragma unroll
   for (int q = 0; q < 4; ++q)
     for (int i = 1; i < 16; ++i) s[q] += room[i][q][lane];
-  auto put = [&](void* out, int64_t at, float x) {
-    if (out != nullptr) static_cast<W*>(out)[at] = from_float<W>(x);
-  };
-  if (last) {
-    put(p.dwy, col, s[0]);
-    put(p.dby, col, s[1]);
+  if (gridDim.z == 1) {
+    c.finish<W>(p, col, s);
     return;
   }
-  const int64_t at = group * p.dim + col;
-  auto weight = [&](const void* w, float fill) {
-    return w == nullptr ? fill : to_float<W>(static_cast<const W*>(w)[col]);
-  };
-  put(p.dwr, at, s[0]);
-  put(p.dbr, at, s[1]);
-  put(p.dgate, at, p.norm_y == SPARSP_NORM_NONE ? s[2] : fmaf(weight(p.wy, 1.0f), s[2], weight(p.by, 0.0f) * s[3]));
+#pragma unroll
+  for (int q = 0; q < 4; ++q) p.joined[(((int64_t)blockIdx.y * gridDim.z + blockIdx.z) * 4 + q) * p.dim + col] = s[q];
+}
+template <typename W>
+__global__ void __launch_bounds__(32) step_join_kernel(StepParams p, int found, bool by_team, int parts) {
+  enter_grid(p.joined);
+  const int col = blockIdx.x * 32 + threadIdx.x;
+  const Columns c(p, found, by_team);
+  if (c.none || col >= p.dim) return;
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+  for (int z = 0; z < parts; ++z)
+#pragma unroll
+    for (int q = 0; q < 4; ++q) s[q] += p.joined[(((int64_t)blockIdx.y * parts + z) * 4 + q) * p.dim + col];
+  c.finish<W>(p, col, s);
 }
 
 // gradients of no rows
@@ -715,9 +750,11 @@ static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
   return s;
 }
 
+constexpr int kMostJoined = 4 * kSms;  // sums of 32 columns that CTAs share out, times those CTAs
+
 int64_t step_workspace_bytes(const sparsp_gated_norm& n) {
   const StepPlan s = plan_step(n, true);
-  return 256 + s.teams * 10 * n.dim * 4;
+  return 256 + (s.teams * 10 + kMostJoined * 4) * n.dim * 4;
 }
 
 static StepParams step_params(const sparsp_gated_norm& n, const StepPlan& s) {
@@ -838,8 +875,18 @@ int launch_gated_norm_bwd(const sparsp_gated_norm& n, const void* dN, const void
   const bool wanted = dgate != nullptr || dwr != nullptr || dbr != nullptr;
   const int found = wanted ? (int)std::min(groups, s.teams) : 0, last = dwy != nullptr || dby != nullptr;
   if (found + last == 0) return SPARSP_OK;
-  const dim3 grid((unsigned)((n.dim + 31) / 32), (unsigned)(found + last));
-  SPARSP_WITH_TYPE(n.weight_dtype, W, SPARSP_CUDA_OK(launch_kernel(step_columns_kernel<W>, grid, 512, 0, st, p, found, by_team)));
+  p.joined = p.partial + s.teams * 8 * n.dim;
+  // CTAs for a sum: up to two for each SM in all, 32 teams for one at least (1: no second launch)
+  const int columns = (n.dim + 31) / 32, sums = found + last;
+  int parts = (int)std::min<int64_t>(2 * kSms / ((int64_t)columns * sums), s.teams / std::min(groups, s.teams) / 32);
+  if (parts < 2) parts = 1;
+  const dim3 grid((unsigned)columns, (unsigned)sums, (unsigned)parts);
+  SPARSP_WITH_TYPE(n.weight_dtype, W, {
+    SPARSP_CUDA_OK(launch_kernel(step_columns_kernel<W>, grid, 512, 0, st, p, found, by_team));
+    if (parts > 1)
+      SPARSP_CUDA_OK(launch_kernel(step_join_kernel<W>, dim3((unsigned)columns, (unsigned)sums), 32, 0, st, p, found, by_team,
+                                   parts));
+  });
   return SPARSP_OK;
 }
 
