@@ -98,6 +98,17 @@ struct Weights {
   }
 };
 
+// E values to `at`, rounded to W
+template <typename W, int E>
+__device__ __forceinline__ void store_pieces(void* out, int64_t at, const float (&x)[E]) {
+  Weights<W, E> w;
+#pragma unroll
+  for (int i = 0; i < Weights<W, E>::kParts; ++i) {
+    w.part[i].set(x + i * Weights<W, E>::kEach);
+    store_vec(static_cast<W*>(out) + at + i * Weights<W, E>::kEach, w.part[i]);
+  }
+}
+
 // A thread's own 16-byte places in shared memory, one behind the other: nobody else's, so that nothing has to be waited
 // for but its own copies.  Their number is odd, so that eight lanes' places of one number lie in different banks.
 struct Places {
@@ -397,29 +408,46 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
         w = places.weights<W, E>(kWyAt + v * kPart);
         b.load(p.by, col, 0.0f);
       }
-      auto put = [&](void* out, int e, float x) {
-        if (out != nullptr) static_cast<W*>(out)[at + e] = from_float<W>(x);
+      auto sum = [&](int q, float (&x)[E]) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) x[e] = sums[q][v * E + e];
       };
+      float x[E], y[E];
+      if (kNormY) {
+        float* py = p.partial_y + (int64_t)m.team * 2 * p.dim + col;
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const int k = v * E + e;
-        const float alone = kNormY ? sums[kSums - 1][k] : 0.0f;
-        if (kNormY) {
-          float* py = p.partial_y + (int64_t)m.team * 2 * p.dim + col + e;
-          py[0] = (first_flush ? 0.0f : py[0]) + g[e] * sums[2][k];
-          py[p.dim] = (first_flush ? 0.0f : py[p.dim]) + g[e] * alone;
+        for (int q = 0; q < 2; ++q) {
+          Weights<float, E> held;
+          if (!first_flush) held.load(py, q * (int64_t)p.dim, 0.0f);
+          sum(q == 0 ? 2 : kSums - 1, x);
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[e] = first_flush ? g[e] * x[e] : fmaf(g[e], x[e], held[e]);
+          store_pieces<float, E>(py, q * (int64_t)p.dim, x);
         }
-        if (whole) {
-          put(p.dwr, e, sums[0][k]);
-          put(p.dbr, e, sums[1][k]);
-          put(p.dgate, e, kNormY ? fmaf(w[e], sums[2][k], b[e] * alone) : sums[2][k]);
-        } else {
-#pragma unroll
-          for (int q = 0; q < kSums; ++q) to[q * (int64_t)p.dim + col + e] = sums[q][k];
-        }
-#pragma unroll
-        for (int q = 0; q < kSums; ++q) sums[q][k] = 0.0f;
       }
+      if (whole) {
+        sum(0, x);
+        if (p.dwr != nullptr) store_pieces<W, E>(p.dwr, at, x);
+        sum(1, x);
+        if (p.dbr != nullptr) store_pieces<W, E>(p.dbr, at, x);
+        sum(2, x);
+        if (kNormY) {
+          sum(kSums - 1, y);
+#pragma unroll
+          for (int e = 0; e < E; ++e) x[e] = fmaf(w[e], x[e], b[e] * y[e]);
+        }
+        if (p.dgate != nullptr) store_pieces<W, E>(p.dgate, at, x);
+      } else {
+#pragma unroll
+        for (int q = 0; q < kSums; ++q) {
+          sum(q, x);
+          store_pieces<float, E>(to, q * (int64_t)p.dim + col, x);
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < kSums; ++q)
+#pragma unroll
+        for (int e = 0; e < E; ++e) sums[q][v * E + e] = 0.0f;
     }
     first_flush = false;
   };
