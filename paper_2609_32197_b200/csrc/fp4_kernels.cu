@@ -117,10 +117,14 @@ struct BlockScale {
       value = finite ? power_of_two(c - 127) : __uint_as_float(0x7fc00000u);
       inverse = finite ? power_of_two(127 - c) : 0.0f;
     } else {
-      code = finite ? to_e4m3(__fdiv_rn(__uint_as_float(most) * power_of_two(-exponent), 6.0f)) : 0x7fu;
+      // most / 6, correctly rounded: the product with the rounded 1/6, corrected by what it leaves (Markstein's division)
+      // of what stays finite: from 2688 on the scale is 448 anyway
+      const float x = fminf(__uint_as_float(most) * power_of_two(-exponent), 1e30f), sixth = 1.0f / 6.0f, q = x * sixth;
+      code = finite ? to_e4m3(fmaf(fmaf(-6.0f, q, x), sixth, q)) : 0x7fu;
       part = finite ? from_e4m3(code) : 0.0f;
       value = finite ? part * power_of_two(exponent) : __uint_as_float(0x7fc00000u);
-      inverse = part > 0.0f ? __frcp_rn(part) : 0.0f;
+      asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inverse) : "f"(part));  // (a step of fp32 off is near enough, see OverScale)
+      if (part == 0.0f) inverse = 0.0f;
     }
   }
 };

@@ -93,6 +93,13 @@ def test_quantize_extremes(fmt, dtype):
     check_quantized(x, fmt)
 
 
+@pytest.mark.parametrize("dtype", [BF, F4])
+@pytest.mark.parametrize("exponent,size", [(-100, 1e30), (-100, 3.0), (100, 1e-3), (100, 1e38), (-3, 3e38)])
+def test_quantize_with_an_exponent_far_off(exponent, size, dtype):
+    """Scales of 448 under values that do not fit, and of zero over values that are too small."""
+    check_quantized((matrix(9, 96, F4, 77, 0.5) * size).clamp(-3.3e38, 3.3e38).to(dtype), "nvfp4", exponent)
+
+
 def test_quantize_strided_and_in_place():
     wide = matrix(130, 512, BF, 5)
     x = wide[:, 64:416]
