@@ -27,9 +27,9 @@ int64_t fp4_scales_bytes(const sparsp_fp4& f) { return (f.rows + 127) / 128 * fp
 static int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // ---- quantisation ---------------------------------------------------------------------------------------------------
-// A thread has eight values of a row, neighbouring lanes a block; a warp goes through 1024 values of a row at a time, all
+// A thread has eight values of a row, neighbouring lanes a block; a warp has up to four pieces of 256 values of a row, all
 // of whose loads are on their way before the first is used.  Bound by HBM and by instructions at once, about 12 a value in
-// mxfp4 and 16 in nvfp4: 75600 x 5120 bf16 with the values written too, 312 to 319 us = 5.5 TB/s, nvfp4 336 us.
+// mxfp4 and 14 in nvfp4: 75600 x 5120 bf16 with the values written too, 303 us = 5.8 TB/s, nvfp4 315 us.
 
 // 2^k for -127 <= k <= 127, exact
 __device__ __forceinline__ float power_of_two(int k) {
@@ -133,7 +133,7 @@ struct BlockScale {
 // NVFP4: a border is a multiple of 2^-2 and met exactly or missed by a step of x's type, 2^-13 at least for 16-bit types:
 // a quotient rounded to a multiple of 2^-13, as the sum with 1.5 * 2^10 is, is on the border where x is and otherwise on
 // x's side of it.  fp32 misses by less: there the quotient is corrected by what it leaves, which is off by far less than
-// half a step (75600 x 5120 bf16 with values 361 us that way, 335 this way).
+// half a step (75600 x 5120 bf16 with values 361 us that way, 335 this way at the time).
 template <typename T, int kFormat>
 struct OverScale {
   float inverse, part, tensor;
@@ -185,9 +185,9 @@ struct QuantizeParams {
   uint8_t* scales;
   void* values;
   int64_t rows, all_rows, ld, groups;  // all_rows: a multiple of 128
-  int32_t cols, chunks, exponent;
+  int32_t cols, chunks, pieces, exponent;  // pieces: of 256 values, of a chunk
 };
-constexpr int kQuantizeUnroll = 4;
+constexpr int kQuantizeUnroll = 4;  // pieces of a warp at a time, at most
 
 template <typename T, int kFormat>
 __global__ void __launch_bounds__(256) quantize_kernel(QuantizeParams p) {
@@ -197,13 +197,13 @@ __global__ void __launch_bounds__(256) quantize_kernel(QuantizeParams p) {
   const int64_t units = p.all_rows * p.chunks, step = (int64_t)gridDim.x * 8;
   for (int64_t unit = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5); unit < units; unit += step) {
     const int64_t row = unit / p.chunks;
-    const int first = (int)(unit - row * p.chunks) * (kQuantizeUnroll * 256) + lane * 8;
+    const int first = (int)(unit - row * p.chunks) * (p.pieces * 256) + lane * 8;
     const bool there = row < p.rows;
     const T* from = static_cast<const T*>(p.x) + row * p.ld;
     Eight<T> v[kQuantizeUnroll];
 #pragma unroll
     for (int i = 0; i < kQuantizeUnroll; ++i) {
-      if (there && first + i * 256 < p.cols)
+      if (there && i < p.pieces && first + i * 256 < p.cols)
         v[i].load(from + first + i * 256);
       else
         v[i].clear();
@@ -211,6 +211,7 @@ __global__ void __launch_bounds__(256) quantize_kernel(QuantizeParams p) {
     uint8_t* to_scales = p.scales + (row >> 7) * p.groups * 512 + (row & 31) * 16 + ((row & 127) >> 5) * 4;
 #pragma unroll
     for (int i = 0; i < kQuantizeUnroll; ++i) {
+      if (i >= p.pieces) break;
       const int col = first + i * 256;
       uint32_t most = largest(v[i]);
 #pragma unroll
@@ -248,10 +249,13 @@ int launch_fp4_quantize(const sparsp_fp4& f, const void* X, uint8_t* codes, uint
   p.ld = f.stride_x;
   p.groups = fp4_groups(f.cols, f.format);
   p.cols = f.cols;
-  p.chunks = ceil_div(p.groups * 4 * fp4_block(f.format), kQuantizeUnroll * 256);
+  const int pieces = ceil_div(p.groups * 4 * fp4_block(f.format), 256);
+  p.chunks = ceil_div(pieces, kQuantizeUnroll);
+  p.pieces = ceil_div(pieces, p.chunks);
   p.exponent = f.exponent;
   const int64_t ctas = (p.all_rows * p.chunks + 7) / 8;
-  const dim3 grid((unsigned)std::min<int64_t>(ctas, 8 * kSms));
+  // as many CTAs as there is work (75600 x 5120 bf16 nvfp4 315 us; eight for each SM, which take what is left by turns, 340)
+  const dim3 grid((unsigned)std::min<int64_t>(ctas, 0x7fffffff));
   SPARSP_WITH_TYPE(f.dtype, T, {
     auto kern = f.format == SPARSP_MXFP4 ? quantize_kernel<T, SPARSP_MXFP4> : quantize_kernel<T, SPARSP_NVFP4>;
     SPARSP_CUDA_OK(launch_kernel(kern, grid, 256, 0, st, p));
