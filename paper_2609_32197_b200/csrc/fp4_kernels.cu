@@ -276,7 +276,7 @@ int launch_fp4_quantize(const sparsp_fp4& f, const void* X, uint8_t* codes, uint
 //
 // Bound by what copies of scales leave of the tensor cores, and by power: one launch of 8192 x 13824 x 5120 at 1.72 GHz
 // keeps them busy for 78 % of its cycles in mxfp4 (6 copies a stage) and for 69 % in nvfp4 (12); copied half a stage at
-// a time, in places taken by turns: no different.  75600 x 13824 x 5120 nvfp4 2.39 to 2.42 ms = 4.4 PFLOP/s, mxfp4 2.10.
+// a time, in places taken by turns: no different.  75600 x 13824 x 5120 nvfp4 2.29 ms = 4.7 PFLOP/s, mxfp4 2.1.
 struct ProductParams {
   const void* bias;
   int32_t rows, cols, depth;
@@ -572,7 +572,8 @@ struct FewParams {
   int32_t* status;
   long long wait_limit;
 };
-constexpr int kFewRows = 128;
+constexpr int kFewRows = 128;  // (us, this way and by pairs: 16 x 7680 x 1920 4.9 and 6.4, 128 x 6.1 and 6.8; 1 x 30720 x 5120 18.8
+                               // and 31.5, 128 x 21.1 and 24.6; 64 x 5120 x 5120 8.5 and 8.5, 128 x 9.7 and 8.9)
 constexpr int kFewWarps = 8;  // of results
 constexpr int kFewThreads = 64 + 32 * kFewWarps;
 constexpr int kFewSmem = 220 * 1024;
@@ -852,7 +853,9 @@ static int launch_pairs(const sparsp_fp4_gemm& f, const void* A, const void* As,
   p.depth = f.depth;
   p.m_tiles = ceil_div(f.rows, 256);
   p.n_tiles = ceil_div(f.cols, BN);
-  p.band = 8;
+  // row tiles in a band, whose tiles go column by column: those at work at one time share rows of A and of B in L2 (75600 x
+  // 13824 x 5120 and x 5120 x 13824 nvfp4, bands of 4 2425 and 2162 us, 8 2373 and 2236, 16 2291 and 2190, 37 2284 and 2486)
+  p.band = 16;
   p.k_blocks = ceil_div(f.depth, kDeep);
   p.factor = std::ldexp(1.0f, f.exponent);
   p.idesc = fp4_instruction(kFormat, 256, BN);
@@ -865,8 +868,9 @@ static int launch_pairs(const sparsp_fp4_gemm& f, const void* A, const void* As,
   return SPARSP_OK;
 }
 
-// Tiles of 128 columns where these make fewer rounds: they take half the time of those of 256, but each value that they
-// load serves fewer products.
+// Tiles of 128 columns where these make fewer rounds: a round of them takes 0.7 of one of 256, for each value that they load
+// serves fewer products (us, 256 and 128 columns: 226 x 7680 x 1920 6.8 and 6.1, 1003 x 1160 x 5120 10.6 and 8.9, one round of
+// either; 1000 x 7680 x 1920, two and four rounds, 11.1 and 13.2; 2000 x 5120 x 5120, three and five, 28.5 and 30.1).
 static bool narrow_tiles(const sparsp_fp4_gemm& f) {
   const int64_t m = ceil_div(f.rows, 256);
   return 128 * 7 * ceil_div(m * ceil_div(f.cols, 128), kPairs) < 256 * 5 * ceil_div(m * ceil_div(f.cols, 256), kPairs);
