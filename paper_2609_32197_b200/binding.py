@@ -641,18 +641,21 @@ def make_grad_list(grads, outs=None) -> sparsp_grad_list:
     if outs is not None and len(outs) != len(grads):
         raise ValueError(f"{len(outs)} outputs for {len(grads)} gradients")
     n = len(grads)
-    for i, t in enumerate(grads + (outs or [])):
-        if (t.dtype != grads[0].dtype or t.device != grads[0].device or not t.is_contiguous()
-                or t.numel() != grads[i % n].numel()):
-            raise ValueError(f"gradient {i % n}: contiguous tensors of one type and device, an output as large as its gradient")
-    addresses = (ctypes.c_void_p * max(n, 1))(*(t.data_ptr() for t in grads))
-    to = None if outs is None else (ctypes.c_void_p * max(n, 1))(*(t.data_ptr() for t in outs))
-    sizes = (ctypes.c_int64 * max(n, 1))(*(t.numel() for t in grads))
-    out = sparsp_grad_list(n, _dtype(grads[0].dtype) if n else SPARSP_BF16, ctypes.addressof(addresses),
-                           None if to is None else ctypes.addressof(to), ctypes.addressof(sizes), 0, 0, 0)
+    dtype, device = (grads[0].dtype, grads[0].device) if n else (torch.bfloat16, torch.device("cuda"))
+    sizes = [t.numel() for t in grads]
+    for tensors in (grads, outs or []):
+        for i, t in enumerate(tensors):
+            if t.dtype is not dtype or t.device != device or not t.is_contiguous() or t.numel() != sizes[i]:
+                raise ValueError(f"gradient {i}: contiguous tensors of one type and device, an output as large as its gradient")
+    room = ctypes.c_void_p * max(n, 1)
+    addresses = room(*[t.data_ptr() for t in grads])
+    to = None if outs is None else room(*[t.data_ptr() for t in outs])
+    sizes = (ctypes.c_int64 * max(n, 1))(*sizes)
+    out = sparsp_grad_list(n, _dtype(dtype), ctypes.addressof(addresses), None if to is None else ctypes.addressof(to),
+                           ctypes.addressof(sizes), 0, 0, 0)
     table = torch.zeros(sparsp_grad_table_bytes(out), dtype=torch.uint8)
     sparsp_grad_table(out, table)
-    out.table = table.to(grads[0].device if n else "cuda")
+    out.table = table.to(device)
     out.kept = (grads, outs, addresses, to, sizes)
     return out
 
