@@ -1,12 +1,12 @@
 // The residual step between two blocks of a layer: r = x + gate * u, u = norm_y(y) or y, n = norm_r(r), and its backward
 // pass with the reduction of the gate's and the weights' gradients.
 //
-// A row is worked on by a team: 4 to 32 lanes of a warp up to 512 values, otherwise a CTA.  Teams have consecutive rows, so
-// that weights of a group are read once for many.  The rows ahead are on their way into shared memory, each thread
+// A row is worked on by a team: 4 to 32 lanes of a warp up to 512 values, otherwise a CTA.  Teams have rows of one group for
+// as long as they can, so that its weights are read once for many.  The rows ahead are on their way into shared memory, each thread
 // copying the 16-byte pieces that it will itself use, so that nobody waits for anybody else's copies; a thread's
 // pieces lie a CTA's width apart (one behind the other, copies took twice as long: backward 75600 x 5120 1302 us, 922).
 //
-// Bound by HBM, forward: 75600 x 5120 bf16 509 to 556 us = 5.6 to 6.1 TB/s (weights from L1 for each row 728).  Backward the sums
+// Bound by HBM, forward: 75600 x 5120 bf16 525 to 535 us = 5.8 to 5.9 TB/s (weights from L1 for each row 728).  Backward the sums
 // of columns take the registers that more warps would need, and a row's sums along it are waited for: 75600 x 5120
 // 743 to 765 us = 6.1 to 6.2 TB/s, with norms on both sides 1205.
 #include <algorithm>
@@ -25,7 +25,7 @@ struct StepParams {
   float *partial, *partial_y;  // backward: [teams][2][4][dim], of a team's first group and its last, and [teams][2][dim]
   void *dgate, *dwy, *dby, *dwr, *dbr;
   int64_t rows, rows_per_group, stride_x, stride_y, stride_n;
-  int32_t dim, teams, lanes, stages, places, norm_y, norm_r;
+  int32_t dim, teams, lanes, stages, places, by_turns, norm_y, norm_r;
   float eps, inv_dim;
 };
 
@@ -145,12 +145,14 @@ struct Ring {
   int across, left, stages, pitch;  // bytes from a piece to the next; rows still to be asked for
   bool in[V];
   __device__ __forceinline__ Ring(const Places& places, int first, int stages, const void* const (&tensors)[N],
-                                  const int64_t (&ld)[N], int64_t row, int rows, int lanes, int me, int dim)
+                                  const int64_t (&ld)[N], int64_t row, int64_t apart, int rows, int lanes, int me,
+                                  int dim)
       : across(lanes * 16), left(rows), stages(stages) {
 #pragma unroll
     for (int q = 0; q < N; ++q) {
       step[q] = ld[q] * (int)sizeof(T);
       from[q] = tensors[q] == nullptr ? nullptr : static_cast<const uint8_t*>(tensors[q]) + row * step[q] + me * 16;
+      step[q] *= apart;
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) in[v] = (v * lanes + me) * E < dim;
@@ -204,8 +206,8 @@ struct Group {
   __device__ __forceinline__ Group(int64_t row, int64_t per) : index(row / per), end((index + 1) * per) {}
   __device__ __forceinline__ bool advance(int64_t row, int64_t per) {
     if (row < end) return false;
-    ++index;  // (one at a time is enough: rows come one by one)
-    end += per;
+    index = row / per;
+    end = (index + 1) * per;
     return true;
   }
 };
@@ -215,14 +217,14 @@ struct Group {
 template <bool kWarps>
 struct Member {
   int lanes, team, me, rows, turns;
-  int64_t lo;
-  __device__ __forceinline__ Member(const StepParams& p) {
+  int64_t lo, apart;  // first row; from one of its rows to the next
+  __device__ __forceinline__ Member(const StepParams& p) : apart(p.by_turns ? p.teams : 1) {
     lanes = kWarps ? blockDim.x : p.lanes;
     team = kWarps ? blockIdx.x : (blockIdx.x * blockDim.x + threadIdx.x) / lanes;
     me = kWarps ? threadIdx.x : threadIdx.x & (lanes - 1);
     const bool there = team < p.teams;
-    lo = there ? first_row(team, p.teams, p.rows) : 0;
-    rows = there ? (int)(first_row(team + 1, p.teams, p.rows) - lo) : 0;
+    lo = !there ? 0 : p.by_turns ? team : first_row(team, p.teams, p.rows);
+    rows = !there ? 0 : (int)(p.by_turns ? (p.rows - team + p.teams - 1) / p.teams : first_row(team + 1, p.teams, p.rows) - lo);
     turns = kWarps ? rows : (int)((p.rows + p.teams - 1) / p.teams);
   }
 };
@@ -238,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
   if (kWarps) clear_room(room);
   const Member<kWarps> m(p);
   const Places places(p.places);
-  Ring<T, V, 2> ring(places, 0, p.stages, {p.x, p.y}, {p.stride_x, p.stride_y}, m.lo, m.rows, m.lanes, m.me, p.dim);
+  Ring<T, V, 2> ring(places, 0, p.stages, {p.x, p.y}, {p.stride_x, p.stride_y}, m.lo, m.apart, m.rows, m.lanes, m.me, p.dim);
   Group group(m.lo, p.rows_per_group);
   Weights<W, E> gate[V], wr[V], br[V];
   auto load_weights = [&] {
@@ -277,9 +279,10 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
   };
   T* to_r = static_cast<T*>(p.r) + m.lo * p.stride_x + m.me * E;
   T* to_n = static_cast<T*>(p.n) + m.lo * p.stride_n + m.me * E;
-  for (int i = 0; i < m.turns; ++i, to_r += p.stride_x, to_n += p.stride_n) {
+  int64_t row = m.lo;
+  for (int i = 0; i < m.turns; ++i, row += m.apart, to_r += m.apart * p.stride_x, to_n += m.apart * p.stride_n) {
     const bool live = i < m.rows;
-    if (live && group.advance(m.lo + i, p.rows_per_group) && !kNormY) load_weights();
+    if (live && group.advance(row, p.rows_per_group) && !kNormY) load_weights();
     ring.wait();
     float r[V * E], mean = 0.0f, rstd = 1.0f;
     if constexpr (kNormY) {
@@ -293,7 +296,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
       }
       statistics(r, p.norm_y, mean, rstd);
       if (p.stats_y != nullptr && live && m.me == 0)
-        reinterpret_cast<float2*>(p.stats_y)[m.lo + i] = make_float2(mean, rstd);
+        reinterpret_cast<float2*>(p.stats_y)[row] = make_float2(mean, rstd);
     }
     float shift = -mean * rstd;
 #pragma unroll
@@ -326,7 +329,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
     statistics(r, p.norm_r, mean, rstd);
     shift = -mean * rstd;
     if (!live) continue;
-    if (p.stats_r != nullptr && m.me == 0) reinterpret_cast<float2*>(p.stats_r)[m.lo + i] = make_float2(mean, rstd);
+    if (p.stats_r != nullptr && m.me == 0) reinterpret_cast<float2*>(p.stats_r)[row] = make_float2(mean, rstd);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (!ring.in[v]) continue;
@@ -364,7 +367,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
   const Places places(p.places);
   constexpr int kWrAt = 0, kGateAt = V * kPart, kWyAt = 2 * V * kPart;  // then rows
   Ring<T, V, 4> ring(places, (kNormY ? 3 : 2) * V * kPart, p.stages, {p.dn, p.x, p.dr, p.y},
-                     {p.stride_n, p.stride_x, p.stride_x, p.stride_y}, m.lo, m.rows, m.lanes, m.me, p.dim);
+                     {p.stride_n, p.stride_x, p.stride_x, p.stride_y}, m.lo, m.apart, m.rows, m.lanes, m.me, p.dim);
   const int64_t hi = m.lo + m.rows;
   auto column = [&](int v) { return (v * m.lanes + m.me) * E; };
   Group group(m.lo, p.rows_per_group);
@@ -764,7 +767,7 @@ static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
   const int held = backward ? s.pieces * per_weight * (n.norm_y != SPARSP_NORM_NONE ? 3 : 2) : 0;
   auto fits = [&](int places, int ctas) { return (places * s.threads * 16 + 1024 + 256) * ctas <= kStepSmem; };
   auto stages = [&](int ctas) {
-    int k = s.two_rows ? 4 : 3;
+    int k = s.two_rows ? 4 : backward ? 3 : 2;  // (forward 75600 x 5120 bf16 532 us, 550 with three)
     while (k > 0 && !fits((k * row + held) | 1, ctas)) --k;
     return k;
   };
@@ -850,6 +853,9 @@ int launch_gated_norm_fwd(const sparsp_gated_norm& n, const void* X, const void*
                           float* stats_r, cudaStream_t st) {
   const StepPlan s = plan_step(n, false);
   StepParams p = step_params(n, s);
+  // Teams take rows by turns, so that those at work at one time lie near each other (75600 x 5120 bf16 525 us, 532 with rows
+  // one behind the other), unless a team would meet new weights every few rows.
+  p.by_turns = p.rows_per_group >= 16 * s.teams || p.rows_per_group >= n.rows;
   p.x = X;
   p.y = Y;
   p.gate = gate;
