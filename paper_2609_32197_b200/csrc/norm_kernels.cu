@@ -185,35 +185,6 @@ __device__ __forceinline__ void worker_sum(float (&v)[N], float (*slot)[N], int 
   }
 }
 
-// Two fp32 values in a 64-bit register: one instruction adds or multiplies both.
-struct F2 {
-  unsigned long long v;
-  __device__ __forceinline__ F2() {}
-  __device__ __forceinline__ F2(float a, float b) { asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(a), "f"(b)); }
-  __device__ __forceinline__ explicit F2(float a) : F2(a, a) {}
-  __device__ __forceinline__ void get(float& a, float& b) const { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-  __device__ __forceinline__ float sum() const {
-    float a, b;
-    get(a, b);
-    return a + b;
-  }
-};
-__device__ __forceinline__ F2 operator+(F2 a, F2 b) {
-  F2 r;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ F2 operator*(F2 a, F2 b) {
-  F2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
-  return r;
-}
-__device__ __forceinline__ F2 fma(F2 a, F2 b, F2 c) {
-  F2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-  return r;
-}
-
 // The rows ahead of a worker, of one tensor: in shared memory as above, or (kSingle) the next R rows in registers.
 // A thread's place: among the lanes of its row, and among the threads of its worker.
 struct Place {

@@ -1,6 +1,10 @@
 // The residual step between two blocks of a layer: r = x + gate * u, u = norm_y(y) or y, n = norm_r(r), and its backward
 // pass with the reduction of the gate's and the weights' gradients.
 //
+// A norm takes the difference to the mean before it scales: that of nearby values is exact, while v rstd - mean rstd, an
+// operation less, is off by |mean| / deviation roundings (dweight of rows with a mean of 1000 deviations 2e-5 of itself, 1.5e-7 so).
+// Backward these operations go by pairs of values (75600 x 5120 bf16 in a graph 714 us, one by one 808).
+//
 // A row is worked on by a team: 4 to 32 lanes of a warp up to 512 values, otherwise a CTA.  Teams have rows of one group for
 // as long as they can, so that its weights are read once for many.  The rows ahead are on their way into shared memory, each thread
 // copying the 16-byte pieces that it will itself use, so that nobody waits for anybody else's copies; a thread's
@@ -298,7 +302,6 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
       if (p.stats_y != nullptr && live && m.me == 0)
         reinterpret_cast<float2*>(p.stats_y)[row] = make_float2(mean, rstd);
     }
-    float shift = -mean * rstd;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       if (!live || !ring.in[v]) {
@@ -314,7 +317,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
         w.load(p.wy, col, 1.0f);
         b.load(p.by, col, 0.0f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) r[v * E + e] = fmaf(g[e], fmaf(fmaf(r[v * E + e], rstd, shift), w[e], b[e]), x[e]);
+        for (int e = 0; e < E; ++e) r[v * E + e] = fmaf(g[e], fmaf((r[v * E + e] - mean) * rstd, w[e], b[e]), x[e]);
       } else {
         const Vec<T, E> y = ring.get(1, v);
 #pragma unroll
@@ -327,7 +330,6 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
     ring.next();
     if (p.norm_r == SPARSP_NORM_NONE) continue;
     statistics(r, p.norm_r, mean, rstd);
-    shift = -mean * rstd;
     if (!live) continue;
     if (p.stats_r != nullptr && m.me == 0) reinterpret_cast<float2*>(p.stats_r)[row] = make_float2(mean, rstd);
 #pragma unroll
@@ -340,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
       }
       float n[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) n[e] = fmaf(fmaf(r[v * E + e], rstd, shift), wr[v][e], br[v][e]);
+      for (int e = 0; e < E; ++e) n[e] = fmaf((r[v * E + e] - mean) * rstd, wr[v][e], br[v][e]);
       Vec<T, E> out;
       out.set(n);
       store_vec(to_n + v * m.lanes * E, out);
@@ -482,8 +484,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
 #pragma unroll
       for (int q = 0; q < C; ++q) {
         k1[q] = s[2 * q + 1] * p.inv_dim;
-        k0[q] = fmaf(kept[q].x, k1[q], kind == SPARSP_NORM_LAYER ? s[2 * q] * p.inv_dim : 0.0f);
-        k1[q] *= kept[q].y;
+        k0[q] = kind == SPARSP_NORM_LAYER ? s[2 * q] * p.inv_dim : 0.0f;
+        k1[q] *= kept[q].y;  // (of the difference to the mean)
         s[2 * q] = s[2 * q + 1] = 0.0f;
       }
     };
@@ -498,13 +500,18 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
         for (int q = 0; q < C; ++q) {
           const Vec<T, E> dn = ring.get(kDn, v, q), r = ring.get(kR, v, q);
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const int k = v * E + e;
-            const float d = dn[e], a = d * w[e], rh = fmaf(r[e], sr[q].y, sr[q].x);
-            s[2 * q] += a;
-            s[2 * q + 1] = fmaf(a, rh, s[2 * q + 1]);
-            sums[0][k] = fmaf(d, rh, sums[0][k]);
-            sums[1][k] += d;
+          for (int e = 0; e < E; e += 2) {
+            float rh[2];
+            ((F2(r[e], r[e + 1]) + F2(sr[q].x)) * F2(sr[q].y)).get(rh[0], rh[1]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int k = v * E + e + i;
+              const float d = dn[e + i], a = d * w[e + i];
+              s[2 * q] += a;
+              s[2 * q + 1] = fmaf(a, rh[i], s[2 * q + 1]);
+              sums[0][k] = fmaf(d, rh[i], sums[0][k]);
+              sums[1][k] += d;
+            }
           }
         }
       }
@@ -529,9 +536,11 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
           const Vec<T, E> dn = ring.get(kDn, v, q), r = ring.get(kR, v, q);
           const Weights<W, E> w = places.weights<W, E>(kWrAt + v * kPart);
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            // (k1 rh + k0 as a line in r)
-            t[e] = fmaf(sr[q].y, fmaf(dn[e], w[e], -fmaf(r[e], k1[q], k0[q])), t[e]);
+          for (int e = 0; e < E; e += 2) {
+            float line[2];
+            fma(F2(r[e], r[e + 1]) + F2(sr[q].x), F2(k1[q]), F2(k0[q])).get(line[0], line[1]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) t[e + i] = fmaf(sr[q].y, fmaf(dn[e + i], w[e + i], -line[i]), t[e + i]);
           }
         }
         if (p.r != nullptr) {
@@ -544,14 +553,18 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
         if constexpr (kNormY) {
           const Weights<W, E> wy = places.weights<W, E>(kWyAt + v * kPart);
 #pragma unroll
-          for (int e = 0; e < E; ++e) {
-            const int k = v * E + e;
-            const float yh = fmaf(y[e], sy[q].y, sy[q].x);
-            sums[2][k] = fmaf(t[e], yh, sums[2][k]);
-            sums[kSums - 1][k] += t[e];
-            b[q][k] = t[e] * g[e] * wy[e];
-            s[2 * q] += b[q][k];
-            s[2 * q + 1] = fmaf(b[q][k], yh, s[2 * q + 1]);
+          for (int e = 0; e < E; e += 2) {
+            float yh[2];
+            ((F2(y[e], y[e + 1]) + F2(sy[q].x)) * F2(sy[q].y)).get(yh[0], yh[1]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int k = v * E + e + i;
+              sums[2][k] = fmaf(t[e + i], yh[i], sums[2][k]);
+              sums[kSums - 1][k] += t[e + i];
+              b[q][k] = t[e + i] * g[e + i] * wy[e + i];
+              s[2 * q] += b[q][k];
+              s[2 * q + 1] = fmaf(b[q][k], yh[i], s[2 * q + 1]);
+            }
           }
         } else {
 #pragma unroll
@@ -577,8 +590,12 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
           const Vec<T, E> y = ring.get(kY, v, q);
           float d[E];
 #pragma unroll
-          for (int e = 0; e < E; ++e)
-            d[e] = sy[q].y * (b[q][v * E + e] - fmaf(y[e], k1[q], k0[q]));
+          for (int e = 0; e < E; e += 2) {
+            float line[2];
+            fma(F2(y[e], y[e + 1]) + F2(sy[q].x), F2(k1[q]), F2(k0[q])).get(line[0], line[1]);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) d[e + i] = sy[q].y * (b[q][v * E + e + i] - line[i]);
+          }
           Vec<T, E> out;
           out.set(d);
           store_vec(to_y + q * p.stride_y + v * m.lanes * E, out);
@@ -602,8 +619,8 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
     float2 sr[R], sy[R];
 #pragma unroll
     for (int q = 0; q < R; ++q) {
-      sr[q] = make_float2(-next_r[q].x * next_r[q].y, next_r[q].y);  // (v - mean) rstd = v rstd + this
-      sy[q] = make_float2(-next_y[q].x * next_y[q].y, next_y[q].y);
+      sr[q] = make_float2(-next_r[q].x, next_r[q].y);
+      sy[q] = make_float2(-next_y[q].x, next_y[q].y);
     }
     ask(row + (two ? 2 : 1));
     ring.wait(R);
