@@ -141,16 +141,19 @@ struct OverScale {
       : inverse(s.inverse), part(s.part), tensor(kFormat == SPARSP_NVFP4 ? power_of_two(-exponent) : 1.0f) {
     if (sizeof(T) == 2 && kFormat == SPARSP_NVFP4) inverse *= tensor;
   }
+  // for a quotient that is zero where x is negative or -0
+  static __device__ __forceinline__ float with_sign_of(float x, float q) {
+    return __uint_as_float(__float_as_uint(q) | (__float_as_uint(x) & 0x80000000u));
+  }
   __device__ __forceinline__ float operator()(float x) const {
     if constexpr (kFormat == SPARSP_MXFP4) {
       return x * inverse;
     } else if constexpr (sizeof(T) == 2) {
-      const float q = fmaf(x, inverse, 1536.0f) - 1536.0f;
-      return __uint_as_float(__float_as_uint(q) | (__float_as_uint(x) & 0x80000000u));  // (also where q is zero)
+      return with_sign_of(x, fmaf(x, inverse, 1536.0f) - 1536.0f);
     } else {
       x *= tensor;
       const float q = fminf(fmaxf(x * inverse, -8.0f), 8.0f);  // (nothing infinite in the next step)
-      return fmaf(fmaf(-q, part, x), inverse, q);
+      return with_sign_of(x, fmaf(fmaf(-q, part, x), inverse, q));
     }
   }
 };
