@@ -11,7 +11,6 @@
 #include <algorithm>
 #include <cmath>
 #include <new>
-#include <utility>
 #include <vector>
 
 #include "layer.cuh"
@@ -266,26 +265,38 @@ int launch_grad_clip(const sparsp_grad_list& l, const void* table, double limit,
   return SPARSP_OK;
 }
 
-// Whether what is written overlaps; -1: no host memory to find out.
+// Whether something is written where something else is read or written; -1: no host memory to find out.  A gradient that
+// is clipped in place counts as written alone.
 int grad_outputs_overlap(const sparsp_grad_list& l) {
   const int64_t e = element_bytes(l.dtype);
-  auto at = [&](int i) { return (uintptr_t)(l.outs != nullptr ? l.outs[i] : l.grads[i]); };
+  auto out = [&](int i) { return l.outs != nullptr ? l.outs[i] : l.grads[i]; };
   uintptr_t end = 0;
-  bool ordered = true;
+  bool ordered = true;  // all in place, one behind the other
   for (int i = 0; i < l.count && ordered; ++i) {
     if (l.sizes[i] == 0) continue;
-    ordered = at(i) >= end;
-    end = at(i) + l.sizes[i] * e;
+    ordered = out(i) == l.grads[i] && (uintptr_t)out(i) >= end;
+    end = (uintptr_t)out(i) + l.sizes[i] * e;
   }
   if (ordered) return 0;
+  struct Run {
+    uintptr_t begin, end;
+    bool written;
+  };
   try {
-    std::vector<std::pair<uintptr_t, uintptr_t>> runs;
-    runs.reserve(l.count);
-    for (int i = 0; i < l.count; ++i)
-      if (l.sizes[i] > 0) runs.emplace_back(at(i), at(i) + l.sizes[i] * e);
-    std::sort(runs.begin(), runs.end());
-    for (size_t i = 1; i < runs.size(); ++i)
-      if (runs[i].first < runs[i - 1].second) return 1;
+    std::vector<Run> runs;
+    runs.reserve(2 * (size_t)l.count);
+    for (int i = 0; i < l.count; ++i) {
+      if (l.sizes[i] == 0) continue;
+      const uintptr_t at = (uintptr_t)out(i), from = (uintptr_t)l.grads[i], bytes = l.sizes[i] * e;
+      runs.push_back({at, at + bytes, true});
+      if (from != at) runs.push_back({from, from + bytes, false});
+    }
+    std::sort(runs.begin(), runs.end(), [](const Run& a, const Run& b) { return a.begin < b.begin; });
+    uintptr_t read = 0, written = 0;  // ends of what has begun
+    for (const Run& r : runs) {
+      if (r.begin < written || (r.written && r.begin < read)) return 1;
+      (r.written ? written : read) = std::max(r.written ? written : read, r.end);
+    }
   } catch (const std::bad_alloc&) {
     return -1;
   }

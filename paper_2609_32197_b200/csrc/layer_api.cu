@@ -508,7 +508,7 @@ int sparsp_grad_table(sparsp_grad_list* list, void* table) {
   SPARSP_TRY(need(table, "table", 16));
   const int overlap = grad_outputs_overlap(*list);
   if (overlap < 0) SPARSP_REFUSE(SPARSP_ERR_CAPACITY, "no host memory for a list of %d gradients", list->count);
-  if (overlap) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "two of the gradients that are written overlap");
+  if (overlap) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "what is written overlaps another gradient or output");
   return fill_grad_table(list, table);
 }
 
