@@ -733,7 +733,8 @@ __global__ void __launch_bounds__(256) step_zero_kernel(W* a, W* b, int64_t n) {
 // ---- host side ------------------------------------------------------------------------------------------------------
 
 static int64_t per_group(const sparsp_gated_norm& n) {
-  return n.rows_per_group > 0 ? n.rows_per_group : std::max<int64_t>(n.rows, 1);
+  const int64_t all = std::max<int64_t>(n.rows, 1);  // (any number that is not less is one group)
+  return n.rows_per_group > 0 ? std::min(n.rows_per_group, all) : all;
 }
 int64_t step_groups(const sparsp_gated_norm& n) { return (n.rows + per_group(n) - 1) / per_group(n); }
 
