@@ -755,10 +755,14 @@ static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
   // Values of a thread, and threads that registers then hold: of a CTA, of a multiprocessor.  Backward, 8 values leave room
   // for twice the warps (15554 x 1928 fp32 with two norms 168 us, 216 with 16); where only one CTA fits, 16, and two rows
   // at a time whose sums are waited for together (75600 x 5120 bf16 843, 962 with 8 and one row, 922 with 16 and one;
-  // 768 since fewer operations make a value).
+  // 714 now).
+  // Two rows take 157 to 168 registers: 384 threads, two CTAs up to 192 (40000 x 2816 bf16 240 us, 279 with one, 335 with 8 values
+  // and one row, with a norm of y 344, 502 and 867; x 4096 with one 313, with two of which one has to wait 421).  A
+  // norm of y over more than 4 values of lanes of a warp takes 158 to 224: two CTAs of 128 (75600 x 512 bf16 115 us, 155 with
+  // four, x 256 85 and 90).
   s.two_rows = backward && each == 8 && n.dim > 320 * 8 && n.dim <= 320 * 16;
   const int values = backward && !s.by_warps && !s.two_rows && n.dim <= 640 * 8 ? 8 : 16, most = values / each;
-  const int most_threads = values == 8 ? 640 : 512, all_threads = backward && values == 16 ? 512 : 640;
+  const int most_threads = values == 8 ? 640 : 512;
   s.pieces = 1;
   if (s.by_warps) {  // a warp, or lanes of one
     s.pieces = (vectors + 31) / 32;
@@ -768,7 +772,7 @@ static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
     per_cta = s.threads / s.lanes;
   } else {
     int best = 1 << 30;
-    for (int v = 1; v <= most; ++v) {
+    for (int v = s.two_rows ? most : 1; v <= most; ++v) {
       const int threads = (vectors + 32 * v - 1) / (32 * v) * 32;
       if (threads <= most_threads && threads * v <= best) {
         best = threads * v;
@@ -779,6 +783,8 @@ static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
     s.lanes = s.threads;
   }
   // CTAs of a multiprocessor by what registers hold
+  const bool many_sums = s.by_warps && n.norm_y != SPARSP_NORM_NONE && s.pieces * each > 4;
+  const int all_threads = !backward || values == 8 ? 640 : s.two_rows ? 384 : many_sums ? 256 : 512;
   int fit = std::max(1, all_threads / s.threads);
   const int row = s.pieces * (backward ? 4 : 2);
   const int per_weight = std::max(1, element_bytes(n.weight_dtype) / element_bytes(n.dtype));
@@ -851,10 +857,9 @@ static int launch_pieces(const StepPlan& s, const StepParams& p, bool backward, 
     if (s.by_warps) return launch_kind<T, W, V, 128, true>(s, p, st);
     if constexpr (kValues <= 8)
       return s.threads <= 320 ? launch_kind<T, W, V, 320, true>(s, p, st) : launch_kind<T, W, V, 640, true>(s, p, st);
-    else if (sizeof(T) == 2 && s.two_rows)
-      return launch_kind<T, W, V, 320, true, sizeof(T) == 2 ? 2 : 1>(s, p, st);
-    else
-      return launch_kind<T, W, V, 512, true>(s, p, st);
+    if constexpr (sizeof(T) == 2)
+      if (s.two_rows) return launch_kind<T, W, V, 320, true, 2>(s, p, st);
+    return launch_kind<T, W, V, 512, true>(s, p, st);
   } else {
     return SPARSP_ERR_UNSUPPORTED;  // (plan_step has no more pieces)
   }
