@@ -29,7 +29,7 @@ struct StepParams {
   float *partial, *partial_y;  // backward: [teams][2][4][dim], of a team's first group and its last, and [teams][2][dim]
   void *dgate, *dwy, *dby, *dwr, *dbr;
   int64_t rows, rows_per_group, stride_x, stride_y, stride_n;
-  int32_t dim, teams, lanes, stages, places, by_turns, norm_y, norm_r;
+  int32_t dim, teams, lanes, stages, by_turns, norm_y, norm_r;
   float eps, inv_dim;
 };
 
@@ -113,12 +113,12 @@ __device__ __forceinline__ void store_pieces(void* out, int64_t at, const float 
   }
 }
 
-// A thread's own 16-byte places in shared memory, one behind the other: nobody else's, so that nothing has to be waited
-// for but its own copies.  Their number is odd, so that eight lanes' places of one number lie in different banks.
+// A thread's own 16-byte places in shared memory, each a CTA's width behind the last: nobody else's, so that nothing has to
+// be waited for but its own copies; lanes' places of one number lie next to each other, in different banks.
 struct Places {
   uint8_t* base;
   int pitch;
-  __device__ __forceinline__ Places(int places) {
+  __device__ __forceinline__ Places() {
     extern __shared__ uint4 dynamic[];
     base = reinterpret_cast<uint8_t*>(dynamic) + threadIdx.x * 16;
     pitch = blockDim.x * 16;
@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
   int turn = 0;
   if (kWarps) clear_room(room);
   const Member<kWarps> m(p);
-  const Places places(p.places);
+  const Places places;
   Ring<T, V, 2> ring(places, 0, p.stages, {p.x, p.y}, {p.stride_x, p.stride_y}, m.lo, m.apart, m.rows, m.lanes, m.me, p.dim);
   Group group(m.lo, p.rows_per_group);
   Weights<W, E> gate[V], wr[V], br[V];
@@ -366,7 +366,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
   const Member<kWarps> m(p);
   const bool norm_r = p.norm_r != SPARSP_NORM_NONE;
   enum { kDn, kR, kDr, kY };
-  const Places places(p.places);
+  const Places places;
   constexpr int kWrAt = 0, kGateAt = V * kPart, kWyAt = 2 * V * kPart;  // then rows
   Ring<T, V, 4> ring(places, (kNormY ? 3 : 2) * V * kPart, p.stages, {p.dn, p.x, p.dr, p.y},
                      {p.stride_n, p.stride_x, p.stride_x, p.stride_y}, m.lo, m.apart, m.rows, m.lanes, m.me, p.dim);
@@ -741,7 +741,7 @@ int64_t step_groups(const sparsp_gated_norm& n) { return (n.rows + per_group(n) 
 // How rows are shared out: 16-byte pieces a thread (16 values at most), threads of a CTA, lanes of a team, teams; rows in
 // shared memory.
 struct StepPlan {
-  int pieces, threads, lanes, ctas, stages, places, smem;
+  int pieces, threads, lanes, ctas, stages, smem;
   bool by_warps, two_rows;
   int64_t teams;
 };
@@ -792,14 +792,12 @@ static StepPlan plan_step(const sparsp_gated_norm& n, bool backward) {
   auto fits = [&](int places, int ctas) { return (places * s.threads * 16 + 1024 + 256) * ctas <= kStepSmem; };
   auto stages = [&](int ctas) {
     int k = s.two_rows ? 4 : backward ? 3 : 2;  // (forward 75600 x 5120 bf16 532 us, 550 with three)
-    while (k > 0 && !fits((k * row + held) | 1, ctas)) --k;
+    while (k > 0 && !fits(k * row + held, ctas)) --k;
     return k;
   };
   while (fit > 1 && stages(fit) < 2) --fit;
   s.stages = std::max(1, stages(fit));
-  s.places = s.stages * row + held;
-  if (fits(s.places | 1, 1)) s.places |= 1;  // (8192 fp32 values with all weights: even, for there is no room)
-  s.smem = s.places * s.threads * 16;
+  s.smem = (s.stages * row + held) * s.threads * 16;
   s.teams = std::max<int64_t>(1, std::min<int64_t>(n.rows, (int64_t)kSms * fit * per_cta));
   s.ctas = (int)((s.teams + per_cta - 1) / per_cta);
   return s;
@@ -823,7 +821,6 @@ static StepParams step_params(const sparsp_gated_norm& n, const StepPlan& s) {
   p.teams = (int32_t)s.teams;
   p.lanes = s.lanes;
   p.stages = s.stages;
-  p.places = s.places;
   p.norm_y = n.norm_y;
   p.norm_r = n.norm_r;
   p.eps = n.eps;
