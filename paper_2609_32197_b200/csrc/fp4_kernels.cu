@@ -350,7 +350,7 @@ template <typename T, int kFormat, int BN>
 __global__ void __launch_bounds__(kProductThreads, 1)
     product_kernel(const __grid_constant__ CUtensorMap ma, const __grid_constant__ CUtensorMap mb,
                    const __grid_constant__ CUtensorMap msa, const __grid_constant__ CUtensorMap msb,
-                   const __grid_constant__ CUtensorMap mc, const ProductParams p) {
+                   const __grid_constant__ CUtensorMap mc, ProductParams p) {
   using namespace ptx;
   using C = ProductCfg<kFormat, T, BN>;
   constexpr bool kOverlap = BN == 256;
@@ -390,7 +390,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
   cluster_sync();
   tc_fence_after();
   const uint32_t tmem = *tmem_slot;
-  enter_grid();  // (the next launch may begin: tensor memory is ours, so its CTAs cannot have taken it before)
+  enter_grid(p.bias);  // (the next launch may begin: tensor memory is ours, so its CTAs cannot have taken it before)
 
   const int tiles = p.m_tiles * p.n_tiles, pairs = gridDim.x >> 1;
   auto tile_at = [&](int tile, int& m, int& n) {

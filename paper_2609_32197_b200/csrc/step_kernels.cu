@@ -358,7 +358,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
 template <typename T, typename W, int V, int kThreads, int R, bool kNormY>
 __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) step_back_kernel(StepParams p) {
   constexpr bool kWarps = kThreads > 128;  // teams of 128 threads or fewer in a CTA of their own have room for 320
-  enter_grid(p.x, p.y, p.dn, p.dr, p.gate, p.wy, p.wr, p.stats_y, p.stats_r);
+  enter_grid(p.x, p.y, p.dn, p.dr, p.gate, p.wy, p.by, p.wr, p.stats_y, p.stats_r);
   constexpr int E = 16 / sizeof(T), kSums = kNormY ? 4 : 3, kPart = Weights<W, E>::kParts;
   __shared__ __align__(16) float room[2][4][room_places(kThreads)];
   int turn = 0;
@@ -671,7 +671,7 @@ struct Columns {
 // with one CTA for 32 columns, 45 so).
 template <typename W>
 __global__ void __launch_bounds__(512) step_columns_kernel(StepParams p, int found, bool by_team) {
-  enter_grid(p.partial, p.partial_y);
+  enter_grid(p.partial, p.partial_y, p.wy, p.by);
   __shared__ float room[16][4][33];
   const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, col = blockIdx.x * 32 + lane;
   const Columns c(p, found, by_team);
@@ -708,7 +708,7 @@ __global__ void __launch_bounds__(512) step_columns_kernel(StepParams p, int fou
 }
 template <typename W>
 __global__ void __launch_bounds__(32) step_join_kernel(StepParams p, int found, bool by_team, int parts) {
-  enter_grid(p.joined);
+  enter_grid(p.joined, p.wy, p.by);
   const int col = blockIdx.x * 32 + threadIdx.x;
   const Columns c(p, found, by_team);
   if (c.none || col >= p.dim) return;
