@@ -126,23 +126,31 @@ class DitLayer:
 
 
 class Fp4Linear:
-    """y = x W^T with W, and x as it comes, in 4 bits.  `exponent` is that of x (nvfp4; from what x is seen to be)."""
+    """y = x W^T with W, and x as it comes, in 4 bits.  `exponent` is that of x (nvfp4; from what x is seen to be: magnitudes
+    above 2688 2^exponent become that).  The copy of W in 4 bits is that of requantize(), which follows a W that has changed."""
 
     def __init__(self, weight: torch.Tensor, tokens: int, fmt: str, exponent: int = 0):
         cols, depth = weight.shape
-        exponent_w = 0
-        if fmt == "nvfp4":
-            exponent_w = math.ceil(math.log2(max(float(weight.abs().max()), 2.0 ** -60) / (6 * 448)))
-        else:
-            exponent = 0
         device, dtype = weight.device, weight.dtype
-        self.described = binding.make_fp4(cols, depth, fmt, exponent_w, dtype, weight.stride(0))
+        self.source, self.exponent = weight, exponent if fmt == "nvfp4" else 0
+        self.described = binding.make_fp4(cols, depth, fmt, 0, dtype, weight.stride(0))
         self.weight = binding.make_fp4_operand(self.described, device)
         self.values = torch.empty_strided(weight.shape, weight.stride(), dtype=dtype, device=device)  # what W stands for
-        binding.sparsp_fp4_quantize(self.described, weight, *self.weight, self.values)
-        self.input = binding.make_fp4(tokens, depth, fmt, exponent, dtype)
-        self.product = binding.make_fp4_product(tokens, cols, depth, fmt, exponent + exponent_w, dtype)
+        self.input = binding.make_fp4(tokens, depth, fmt, self.exponent, dtype)
+        self.product = binding.make_fp4_product(tokens, cols, depth, fmt, self.exponent, dtype)
         self.workspace = binding.make_fp4_product_workspace(self.product, device)
+        self.requantize()
+
+    def requantize(self, keep_exponent: bool = False):
+        """W as it is now, in the same buffers.  Its exponent (nvfp4) follows its largest value, which is asked of the device, and a
+        captured product goes on with the exponent of its capture; kept, all is stream-ordered work, and magnitudes above
+        2688 2^exponent become that."""
+        if not keep_exponent and self.described.format == binding.FP4_FORMATS["nvfp4"]:
+            most = float(self.source.abs().max())
+            if math.isfinite(most):
+                self.described.exponent = min(math.ceil(math.log2(max(most, 2.0 ** -60) / (6 * 448))), 100)
+                self.product.exponent = self.exponent + self.described.exponent
+        binding.sparsp_fp4_quantize(self.described, self.source, *self.weight, self.values)
 
     def quantize(self, x, operand, values=None):
         binding.sparsp_fp4_quantize(self.input, x, *operand, values)
@@ -152,7 +160,9 @@ class Fp4Linear:
 
 
 class GatedDitLayer(DitLayer):
-    """projections: "bf16" (torch products), "mxfp4" or "nvfp4" for all but the feed-forward's first two."""
+    """projections: "bf16" (torch products), "mxfp4" or "nvfp4" for all but the feed-forward's first two.  In 4 bits
+    update_weights() follows every change of w_qkv, w_out or w_down; activation_exponent (nvfp4) holds activations up to 2688
+    times its power of two, 168 as it is, and what is above becomes that."""
 
     def __init__(self, wl: synth.Workload, hidden: int, seed: int = 0, dtype=torch.bfloat16, device="cuda",
                  projections: str = "bf16", activation_exponent: int = -4):
@@ -183,6 +193,11 @@ class GatedDitLayer(DitLayer):
             self.operand = binding.make_fp4_operand(self.fp4["out"].input, device)  # of the width's activations
             self.hidden_operand = binding.make_fp4_operand(self.fp4["down"].input, device)
             self.h_values = empty(N, hidden)
+
+    def update_weights(self):
+        """The 4-bit copies of the projections' weights, as these are now."""
+        for linear in self.fp4.values():
+            linear.requantize()
 
     def project_qkv(self):
         if not self.fp4:
@@ -225,7 +240,10 @@ class GatedDitLayer(DitLayer):
     def training_step(self, x: torch.Tensor, dy: torch.Tensor, max_norm: float = math.inf) -> dict:
         """Gradients of what follows the attention, for dy at the layer's output, forward pass included: of its weights,
         clipped together to max_norm, and "x" and "a", the gradients of what it takes.  Roundings to 4 bits have the
-        gradient of nothing (straight through): products go on with the values that were multiplied."""
+        gradient of nothing (straight through): products go on with the values that were multiplied.  w_down is rounded anew
+        in each step, under the exponent of the last update_weights()."""
+        if self.fp4:
+            self.fp4["down"].requantize(keep_exponent=True)
         self.behind_attention(x, training=True)
         w_down, h = (self.fp4["down"].values, self.h_values) if self.fp4 else (self.w_down, self.h)
         grads = self.grads  # (of one step: the next writes them again)
