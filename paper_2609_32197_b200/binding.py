@@ -129,6 +129,7 @@ class sparsp_gated_norm(ctypes.Structure):
 
 
 class sparsp_grad_list(ctypes.Structure):
+    stream = None  # that make_grad_list's table was made on
     _fields_ = [("count", ctypes.c_int32), ("dtype", ctypes.c_int32), ("grads", ctypes.c_void_p),
                 ("outs", ctypes.c_void_p), ("sizes", ctypes.c_void_p), ("chunks", ctypes.c_int32),
                 ("ctas", ctypes.c_int32), ("in_place", ctypes.c_int32)]
@@ -636,7 +637,8 @@ def sparsp_grad_table(grad_list: sparsp_grad_list, table: torch.Tensor):
 
 def make_grad_list(grads, outs=None) -> sparsp_grad_list:
     """grads: contiguous tensors of one type on one device; outs: where the clipped ones go, None = in place.  The list keeps
-    them and its table alive; it is made once, outside of a graph's capture, and serves as long as they stay where they are."""
+    them and its table alive; it is made once, outside of a graph's capture, and serves as long as they stay where they are.
+    It may be dropped while calls on any stream still run; what a captured graph replays needs it for as long as the graph."""
     grads, outs = list(grads), None if outs is None else list(outs)
     if outs is not None and len(outs) != len(grads):
         raise ValueError(f"{len(outs)} outputs for {len(grads)} gradients")
@@ -656,6 +658,8 @@ def make_grad_list(grads, outs=None) -> sparsp_grad_list:
     table = torch.zeros(sparsp_grad_table_bytes(out), dtype=torch.uint8)
     sparsp_grad_table(out, table)
     out.table = table.to(device)
+    if out.table.is_cuda:
+        out.stream = torch._C._cuda_getCurrentRawStream(out.table.device.index)
     out.kept = (grads, outs, addresses, to, sizes)
     return out
 
@@ -675,14 +679,23 @@ def grad_square_sum(workspace) -> torch.Tensor:
     return workspace[256:264].view(torch.float64)
 
 
+def _grad_table_on(grad_list, stream):
+    """The list's table for a call on `stream`: its memory is not given out again before what that stream has now is done."""
+    if grad_list.stream is not None and stream != grad_list.stream:
+        grad_list.table.record_stream(torch.cuda.current_stream())
+    return _data(grad_list.table)
+
+
 def sparsp_grad_squares(grad_list, workspace, accumulate=False):
-    _check(lib().sparsp_grad_squares(grad_list, _data(grad_list.table), 1 if accumulate else 0, _data(workspace),
-                                     _stream_handle()))
+    stream = _stream_handle()
+    _check(lib().sparsp_grad_squares(grad_list, _grad_table_on(grad_list, stream), 1 if accumulate else 0, _data(workspace),
+                                     stream))
 
 
 def sparsp_grad_clip(grad_list, max_norm, norm, workspace):
-    _check(lib().sparsp_grad_clip(grad_list, _data(grad_list.table), max_norm, _data(norm), _data(workspace),
-                                  _stream_handle()))
+    stream = _stream_handle()
+    _check(lib().sparsp_grad_clip(grad_list, _grad_table_on(grad_list, stream), max_norm, _data(norm), _data(workspace),
+                                  stream))
 
 
 # ---- 4-bit operands and their product ----
