@@ -19,7 +19,6 @@ namespace sparsp {
 
 constexpr int kChunkBytes = 16384;
 constexpr int kGradThreads = 256;
-constexpr int kGradCtas = 8 * kSms;
 
 struct GradTensor {
   const void* from;

@@ -16,6 +16,7 @@ constexpr int kMaxStepDim = 8192;
 // Work is shared out for the multiprocessors of a B200, whatever device a size of workspace is asked on: the shares
 // also decide in which order sums are made.
 constexpr int kSms = 148;
+constexpr int kGradCtas = 8 * kSms;  // that go through a list of gradients, each with a place in the workspace
 
 inline int element_bytes(int dtype) { return dtype == SPARSP_FP32 ? 4 : 2; }
 

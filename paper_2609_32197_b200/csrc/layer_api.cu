@@ -148,7 +148,7 @@ int check_grad_table(const sparsp_grad_list* l, const void* table) {
   if (!l) SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "list is NULL");
   if (l->dtype < SPARSP_BF16 || l->dtype > SPARSP_FP32)
     SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "unknown dtype %d", l->dtype);
-  if (l->count < 0 || l->chunks < 0 || l->ctas < 1 || l->ctas > (1 << 20))
+  if (l->count < 0 || l->chunks < 0 || l->ctas < 1 || l->ctas > kGradCtas)
     SPARSP_REFUSE(SPARSP_ERR_INVALID_ARG, "the list's table has not been made");
   return need(table, "table", 16);
 }
