@@ -287,7 +287,7 @@ struct ProductParams {
   float factor;
   uint32_t idesc;
   int32_t* status;
-  long long wait_limit;
+  long long wait_limit, tile_limit;  // of a wait for one stage, and for a tile's products
 };
 
 constexpr int kDeep = 256;  // K elements of a stage: one 128-byte swizzled row
@@ -295,6 +295,7 @@ constexpr int kResultWarps = 8;
 constexpr int kProductThreads = 32 * (kResultWarps + 2);
 constexpr int kRows = 128;  // of one CTA
 constexpr long long kWaitLimit = 200000000LL;  // of a wait in a kernel: about 0.1 s of SM clocks
+constexpr long long kStageLimit = 8192;  // ... and what a stage adds to that of its tile (it takes 300 to 1200 clocks)
 constexpr int kPairs = kSms / 2;
 
 template <int kFormat, typename T, int BN>
@@ -504,7 +505,7 @@ __global__ void __launch_bounds__(kProductThreads, 1)
         for (int i = 0; i < C::kMine; i += 32) held_bias[i + lane] = col + i + lane < p.cols ? to_float(bias[col + i + lane]) : 0.0f;
       }
       __syncwarp();
-      mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 25, p.wait_limit);
+      mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 25, p.tile_limit);
       if (__any_sync(0xffffffffu, *s_abort != 0)) break;  // (the same for all lanes)
       tc_fence_after();
       const uint32_t from = tmem + acc * C::kAccStep + side * C::kMine + ((uint32_t)(quarter * 32) << 16);
@@ -573,7 +574,7 @@ struct FewParams {
   float factor;
   uint32_t idesc;
   int32_t* status;
-  long long wait_limit;
+  long long wait_limit, tile_limit;  // of a wait for one stage, and for a tile's products
 };
 constexpr int kFewRows = 128;  // (us, this way and by pairs: 16 x 7680 x 1920 4.9 and 6.4, 128 x 6.1 and 6.8; 1 x 30720 x 5120 18.8
                                // and 31.5, 128 x 21.1 and 24.6; 64 x 5120 x 5120 8.5 and 8.5, 128 x 9.7 and 8.9)
@@ -712,7 +713,7 @@ __global__ void __launch_bounds__(kFewThreads, 1)
     int acc = 0;
     uint32_t acc_round = 0;
     for (int tile = t0; tile < t1; ++tile) {
-      mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 34, p.wait_limit);
+      mbar_wait_bounded_inline(acc_full + acc, acc_round, s_abort, 34, p.tile_limit);
       tc_fence_after();
       const int col = tile * kRows + in_tile;
       const bool in = col < p.cols;
@@ -816,6 +817,7 @@ static int launch_few_rows(const sparsp_fp4_gemm& f, const void* A, const void* 
   p.idesc = fp4_instruction(kFormat, 128, p.columns);
   p.status = reinterpret_cast<int32_t*>(ws);
   p.wait_limit = kWaitLimit;
+  p.tile_limit = kWaitLimit + kStageLimit * p.k_blocks;
   CUtensorMap ma, mb, msa, msb;
   int rc;
   if ((rc = make_codes_map(&ma, A, f.rows, f.depth / 2, p.columns)) != SPARSP_OK) return rc;
@@ -864,6 +866,7 @@ static int launch_pairs(const sparsp_fp4_gemm& f, const void* A, const void* As,
   p.idesc = fp4_instruction(kFormat, 256, BN);
   p.status = reinterpret_cast<int32_t*>(ws);
   p.wait_limit = kWaitLimit;
+  p.tile_limit = kWaitLimit + kStageLimit * p.k_blocks;
   auto kern = product_kernel<T, kFormat, BN>;
   SPARSP_CUDA_OK(ensure_dynamic_smem((const void*)kern, Cfg::kDynamic));
   const unsigned grid = 2u * (unsigned)std::min(p.m_tiles * p.n_tiles, kPairs);
