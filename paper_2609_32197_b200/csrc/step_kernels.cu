@@ -3,7 +3,7 @@
 //
 // A norm takes the difference to the mean before it scales: that of nearby values is exact, while v rstd - mean rstd, an
 // operation less, is off by |mean| / deviation roundings (dweight of rows with a mean of 1000 deviations 2e-5 of itself, 1.5e-7 so).
-// Backward these operations go by pairs of values (75600 x 5120 bf16 in a graph 714 us, one by one 808).
+// These operations go by pairs of values (75600 x 5120 bf16 backward, in a graph, 714 us, one by one 808).
 //
 // A row is worked on by a team: 4 to 32 lanes of a warp up to 512 values, otherwise a CTA.  Teams have rows of one group for
 // as long as they can, so that its weights are read once for many.  The rows ahead are on their way into shared memory, each thread
@@ -317,7 +317,12 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
         w.load(p.wy, col, 1.0f);
         b.load(p.by, col, 0.0f);
 #pragma unroll
-        for (int e = 0; e < E; ++e) r[v * E + e] = fmaf(g[e], fmaf((r[v * E + e] - mean) * rstd, w[e], b[e]), x[e]);
+        for (int e = 0; e < E; e += 2) {
+          float* at = r + v * E + e;
+          ((F2(at[0], at[1]) + F2(-mean)) * F2(rstd)).get(at[0], at[1]);
+#pragma unroll
+          for (int i = 0; i < 2; ++i) at[i] = fmaf(g[e + i], fmaf(at[i], w[e + i], b[e + i]), x[e + i]);
+        }
       } else {
         const Vec<T, E> y = ring.get(1, v);
 #pragma unroll
@@ -342,7 +347,11 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
       }
       float n[E];
 #pragma unroll
-      for (int e = 0; e < E; ++e) n[e] = fmaf((r[v * E + e] - mean) * rstd, wr[v][e], br[v][e]);
+      for (int e = 0; e < E; e += 2) {
+        ((F2(r[v * E + e], r[v * E + e + 1]) + F2(-mean)) * F2(rstd)).get(n[e], n[e + 1]);
+#pragma unroll
+        for (int i = e; i < e + 2; ++i) n[i] = fmaf(n[i], wr[v][i], br[v][i]);
+      }
       Vec<T, E> out;
       out.set(n);
       store_vec(to_n + v * m.lanes * E, out);
