@@ -208,6 +208,10 @@ struct Ring {
 struct Group {
   int64_t index, end;
   __device__ __forceinline__ Group(int64_t row, int64_t per) : index(row / per), end((index + 1) * per) {}
+  __device__ __forceinline__ void next(int64_t per) {
+    ++index;
+    end += per;
+  }
   __device__ __forceinline__ bool advance(int64_t row, int64_t per) {
     if (row < end) return false;
     index = row / per;
@@ -217,18 +221,22 @@ struct Group {
 };
 
 // What a thread is: of which team, and with which rows.  Teams of less than a CTA go through the same number of rows,
-// those past the last of a team doing nothing, for their lanes meet in the sums.
-template <bool kWarps>
+// those past the last of a team doing nothing, for their lanes meet in the sums.  kTurns: rows may go by turns.  Backward they
+// do not, and are known not to: the registers of a distance between rows are missing there (15554 x 1928 fp32 with two norms
+// 157 us, 202 with it; 50000 x 8192 bf16 with two 1339 and 1988).
+template <bool kWarps, bool kTurns>
 struct Member {
   int lanes, team, me, rows, turns;
   int64_t lo, apart;  // first row; from one of its rows to the next
-  __device__ __forceinline__ Member(const StepParams& p) : apart(p.by_turns ? p.teams : 1) {
+  __device__ __forceinline__ Member(const StepParams& p) {
+    const bool by_turns = kTurns && p.by_turns;
+    apart = by_turns ? p.teams : 1;
     lanes = kWarps ? blockDim.x : p.lanes;
     team = kWarps ? blockIdx.x : (blockIdx.x * blockDim.x + threadIdx.x) / lanes;
     me = kWarps ? threadIdx.x : threadIdx.x & (lanes - 1);
     const bool there = team < p.teams;
-    lo = !there ? 0 : p.by_turns ? team : first_row(team, p.teams, p.rows);
-    rows = !there ? 0 : (int)(p.by_turns ? (p.rows - team + p.teams - 1) / p.teams : first_row(team + 1, p.teams, p.rows) - lo);
+    lo = !there ? 0 : by_turns ? team : first_row(team, p.teams, p.rows);
+    rows = !there ? 0 : (int)(by_turns ? (p.rows - team + p.teams - 1) / p.teams : first_row(team + 1, p.teams, p.rows) - lo);
     turns = kWarps ? rows : (int)((p.rows + p.teams - 1) / p.teams);
   }
 };
@@ -242,7 +250,7 @@ __global__ void __launch_bounds__(kThreads, 640 / kThreads) step_kernel(StepPara
   __shared__ __align__(16) float room[2][4][room_places(kThreads)];
   int turn = 0;
   if (kWarps) clear_room(room);
-  const Member<kWarps> m(p);
+  const Member<kWarps, true> m(p);
   const Places places;
   Ring<T, V, 2> ring(places, 0, p.stages, {p.x, p.y}, {p.stride_x, p.stride_y}, m.lo, m.apart, m.rows, m.lanes, m.me, p.dim);
   Group group(m.lo, p.rows_per_group);
@@ -372,7 +380,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
   __shared__ __align__(16) float room[2][4][room_places(kThreads)];
   int turn = 0;
   if (kWarps) clear_room(room);
-  const Member<kWarps> m(p);
+  const Member<kWarps, false> m(p);
   const bool norm_r = p.norm_r != SPARSP_NORM_NONE;
   enum { kDn, kR, kDr, kY };
   const Places places;
@@ -621,7 +629,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 320 && R == 1 ? 2 : 1) s
     const bool live = i < m.rows;
     if (live && row >= group.end) {
       flush();
-      group.advance(row, p.rows_per_group);
+      group.next(p.rows_per_group);  // (rows come one by one)
       hold_weights();
     }
     const bool two = R == 2 && row + 1 < hi && row + 1 < group.end;
@@ -861,11 +869,13 @@ static int launch_pieces(const StepPlan& s, const StepParams& p, bool backward, 
       return s.threads <= 320 ? launch_kind<T, W, V, 320, false>(s, p, st) : launch_kind<T, W, V, 512, false>(s, p, st);
     }
     if (s.by_warps) return launch_kind<T, W, V, 128, true>(s, p, st);
-    if constexpr (kValues <= 8)
+    if constexpr (kValues <= 8) {
       return s.threads <= 320 ? launch_kind<T, W, V, 320, true>(s, p, st) : launch_kind<T, W, V, 640, true>(s, p, st);
-    if constexpr (sizeof(T) == 2)
-      if (s.two_rows) return launch_kind<T, W, V, 320, true, 2>(s, p, st);
-    return launch_kind<T, W, V, 512, true>(s, p, st);
+    } else {
+      if constexpr (sizeof(T) == 2)
+        if (s.two_rows) return launch_kind<T, W, V, 320, true, 2>(s, p, st);
+      return launch_kind<T, W, V, 512, true>(s, p, st);
+    }
   } else {
     return SPARSP_ERR_UNSUPPORTED;  // (plan_step has no more pieces)
   }
