@@ -649,7 +649,7 @@ typedef struct sparsp_grad_list {
   int32_t dtype;             /* of all of them; lists of several types: see sparsp_grad_squares */
   const void* const* grads;  /* [count], aligned to their element type; NULL for one of size 0 */
   void* const* outs;         /* [count]: where the clipped gradients go; NULL = in place.  Each may be its gradient, otherwise
-                              * none overlaps a gradient or another */
+                              * none overlaps a gradient or another (sparsp_grad_table refuses it) */
   const int64_t* sizes;      /* [count] elements of each, >= 0 */
   int32_t chunks, ctas, in_place; /* set by sparsp_grad_table */
 } sparsp_grad_list;

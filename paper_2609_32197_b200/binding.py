@@ -637,7 +637,8 @@ def sparsp_grad_table(grad_list: sparsp_grad_list, table: torch.Tensor):
 
 def make_grad_list(grads, outs=None) -> sparsp_grad_list:
     """grads: contiguous tensors of one type on one device; outs: where the clipped ones go, None = in place.  The list keeps
-    them and its table alive; it is made once, outside of a graph's capture, and serves as long as they stay where they are.
+    them and its table alive; it is made once, outside of a graph's capture, and serves as long as they stay where they are:
+    once for gradients that are kept and zeroed, each time for those that are made anew (about 0.6 us a tensor on the host).
     It may be dropped while calls on any stream still run; what a captured graph replays needs it for as long as the graph."""
     grads, outs = list(grads), None if outs is None else list(outs)
     if outs is not None and len(outs) != len(grads):

@@ -10,9 +10,9 @@
 // copying the 16-byte pieces that it will itself use, so that nobody waits for anybody else's copies; a thread's
 // pieces lie a CTA's width apart (one behind the other, copies took twice as long: backward 75600 x 5120 1302 us, 922).
 //
-// Bound by HBM, forward: 75600 x 5120 bf16 525 to 535 us = 5.8 to 5.9 TB/s (weights from L1 for each row 728).  Backward the sums
-// of columns take the registers that more warps would need, and a row's sums along it are waited for: 75600 x 5120
-// 743 to 765 us = 6.1 to 6.2 TB/s, with norms on both sides 1205.
+// Bound by HBM, forward: 75600 x 5120 bf16 500 to 538 us = 5.8 to 6.2 TB/s (weights from L1 for each row 728; with a norm of y, which
+// reads them so, 970).  Backward the sums of columns take the registers that more warps would need, and a row's sums along it
+// are waited for: 75600 x 5120 742 to 807 us = 5.8 to 6.3 TB/s, with norms on both sides 1220.
 #include <algorithm>
 
 #include "layer.cuh"
