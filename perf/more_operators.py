@@ -257,7 +257,8 @@ def _run_own(c, x):
         binding.sparsp_gated_norm_fwd(x["step"], x["x"], x["y"], x["gate"], x.get("wy"), x.get("by"), x.get("wr"), x.get("br"),
                                       o["r"], o.get("n"), o.get("stats_y"), o.get("stats_r"))
     elif c["op"] == "step_bwd":
-        binding.sparsp_gated_norm_bwd(x["step"], x.get("dn"), x["dr"], x["r"], x["y"], x["gate"], x.get("wy"), x.get("by"),
+        r = x["r"] if c["norm_r"] != "none" else None
+        binding.sparsp_gated_norm_bwd(x["step"], x.get("dn"), x["dr"], r, x["y"], x["gate"], x.get("wy"), x.get("by"),
                                       x.get("wr"), x["stats_y"], x["stats_r"], o["dx"], o["dy"], o["dgate"], o.get("dwy"),
                                       o.get("dby"), o.get("dwr"), o.get("dbr"), x["workspace"])
     else:
