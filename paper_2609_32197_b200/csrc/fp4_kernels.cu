@@ -562,9 +562,10 @@ __global__ void __launch_bounds__(kProductThreads, 1)
 // rows of the tile and A's its columns: D = B A^T, 128 rows by the rows of A, rounded up to 16.  A CTA has whole tiles,
 // where there are some for half of the SMs: these load as fast as memory gives.  With fewer, a cluster of CTAs shares
 // out a tile's K, and each adds some of the rows from the others' shared memory.  Bound by HBM and by a start and an end of
-// 5 us: 148 tiles of 5120 values 13.0 us, 296 21.3, the 240 of 1 x 30720 x 5120 nvfp4 19.5, for 92 SMs have two and 56 one.  (Stages of all tiles shared out evenly, pieces joined through
-// global memory by the CTA that came last: 21.5 us, and 15 instead of 6 for 100 x 7680 x 1920.  Loads of several
-// stages next to each other, as a feed-forward's weights want: no different.)
+// 5 us: 148 tiles of 5120 values 13.0 us, 296 21.3, the 240 of 1 x 30720 x 5120 nvfp4 19.5, for 92 SMs have two and 56
+// one.  (Stages of all tiles shared out evenly, pieces joined through global memory by the CTA that came last: 21.5 us, and
+// 15 instead of 6 for 100 x 7680 x 1920.  Loads of several stages next to each other, as a feed-forward's weights want: no
+// different.)
 struct FewParams {
   const void* bias;
   void* c;

@@ -2,10 +2,11 @@
 //
 // A table in device memory, made once for a list, says where its tensors are; nothing of it goes through a call, so that
 // calls cost the host the same for one tensor and for thousands (as kernel parameters, 12 KB for 300 tensors, they cost
-// 10 us each; making it costs 180 us for 300 tensors in Python, most of it questions to each).  Tensors are cut into chunks of 16 KB; a CTA has a run of them and is told which tensor that begins in.
-// Squares are added in fp32 over the 32 values at most that a thread has of a chunk, then in fp64, and CTAs' sums in
-// their order by the one that ends last: the same list gives the same bits.  Scaling goes through each run from its end,
-// so that what the first pass read last is still in L2.
+// 10 us each; making it costs 180 us for 300 tensors in Python, most of it questions to each).  Tensors are cut into
+// chunks of 16 KB; a CTA has a run of them and is told which tensor that begins in.  Squares are added in fp32 over the 32
+// values at most that a thread has of a chunk, then in fp64, and CTAs' sums in their order by the one that ends last: the
+// same list gives the same bits.  Scaling goes through each run from its end, so that what the first pass read last is
+// still in L2.
 //
 // Bound by HBM: every value is read once for the norm, and read again and written where the norm is over the limit.
 #include <algorithm>
